@@ -42,11 +42,15 @@ typedef enum {
 } dpar_status_t;
 
 /* Element types.  A DPAR_U32_MAT2X2 element is a 2x2 matrix of uint32 stored
- * row-major as [a00, a01, a10, a11] (16 bytes). */
+ * row-major as [a00, a01, a10, a11] (16 bytes).  The 16-bit types belong to
+ * the layer products (dpar_linear and the entry points after it); the
+ * reduction sums their 32-bit results. */
 typedef enum {
     DPAR_INT32 = 0,
     DPAR_FLOAT32 = 1,
-    DPAR_U32_MAT2X2 = 2
+    DPAR_U32_MAT2X2 = 2,
+    DPAR_BFLOAT16 = 3,
+    DPAR_FLOAT16 = 4
 } dpar_dtype_t;
 
 /* Operators (Section 1: associative, possibly non-commutative).  Valid
@@ -418,6 +422,127 @@ const char* dpar_last_error(void);
  *                           (kernel=: subtree calls of SPLIT and of fused
  *                           launches run level items, fused calls of at most
  *                           8 ranks the register kernel) */
+
+/* ---------------------------------------------------------------------------
+ * Layer products: what makes the rows that reduction-to-all sums when a layer
+ * is split over p ranks, and the gradients of it.  Each rank i has `rows` rows
+ * of `in` values and weights of `out` rows of `in` values; one call runs all
+ * ranks.
+ *
+ *   dpar_linear           z = x w^T + bias,  y = act(z) + residual
+ *   dpar_linear_backward  dz = dy * act'(z), dx = dz w, dw = dz^T x,
+ *                         dbias = sum of dz over the rows
+ *   dpar_gated            g = x wg^T + bg, u = x wu^T + bu, h = act(g) * u
+ *   dpar_gated_backward   dg = dh * u * act'(g), du = dh * act(g),
+ *                         dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x,
+ *                         dbg, dbu = sums of dg, du over the rows
+ *
+ * Types: BFLOAT16, FLOAT16 or FLOAT32 (`dtype`) for every operand and kept
+ * value; results (y, h, the gradients) and the residual have `out_dtype`,
+ * which is dtype or FLOAT32: 32-bit results of 16-bit products are the rows
+ * dpar_allreduce sums.  Every sum is held in 32 bits and rounded once, to
+ * nearest even.  dz, dg and du are rounded to dtype before the products that
+ * read them.  FLOAT32 products are 32-bit throughout.
+ *
+ * Every array argument is a HOST array of p DEVICE pointers, read before the
+ * call returns; an entry may be NULL where its matrix has no element.  An
+ * array marked optional may be NULL as a whole; bias, bg, bu and residual may
+ * also hold NULL for single ranks: a split layer adds them on one rank only.
+ * Inputs may coincide (p ranks may share one x); no output may overlap an
+ * input or another output (DPAR_ERR_ALIAS), except that dz may be z or dy of
+ * its rank, dg may be g or dh and du may be u (same address and row distance).
+ * Matrices of one row distance may lie side by side in one buffer.
+ *
+ * Pointers are aligned to their element.  Rows that start on 16-byte
+ * boundaries, and for operands an `in` and `out` that fill whole 16-byte
+ * pieces, are read and written fastest.  Elements between a row's last value
+ * and the next row are neither read into a result nor written.
+ *
+ * rows, in and out may be 0: with in == 0 the products are zero (y = act(bias)
+ * + residual), with rows == 0 the weights' gradients are zero, without a
+ * result element the call does nothing.
+ *
+ * The calls enqueue kernels only: they allocate nothing, keep nothing from
+ * one call to the next, may run on concurrent streams and may be captured into a
+ * HIP graph with any executor state.  A product with few result tiles and a
+ * long sum splits the sum over workgroups and joins the parts in a fixed order
+ * in a workspace (dpar_product_workspace); without one it runs unsplit.
+ * Results are the same from run to run; with and without a workspace they
+ * differ by the order of 32-bit additions. */
+typedef enum {
+    DPAR_ACT_NONE = 0,
+    DPAR_ACT_RELU = 1,      /* max(z, 0); slope 0 at 0 */
+    DPAR_ACT_GELU = 2,      /* z (1 + erf(z / sqrt 2)) / 2 */
+    DPAR_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi)(z + 0.044715 z^3))) / 2 */
+    DPAR_ACT_SILU = 4       /* z / (1 + exp(-z)) */
+} dpar_act_t;
+
+/* Sizes, types and row distances (in elements; 0: packed) of a layer product.
+ *   ldx   x                          (packed: in)
+ *   ldw   w, wg, wu                  (packed: in)
+ *   ldy   y, h, dy, dh               (packed: out)
+ *   ldr   residual                   (packed: out)
+ *   ldz   z, g, u, dz, dg, du        (packed: out)
+ *   lddx  dx                         (packed: in)
+ *   lddw  dw, dwg, dwu               (packed: in) */
+typedef struct {
+    size_t rows, in, out;
+    dpar_dtype_t dtype, out_dtype;
+    dpar_act_t act;
+    size_t ldx, ldw, ldy, ldr, ldz, lddx, lddw;
+} dpar_product_t;
+
+typedef enum {
+    DPAR_LINEAR = 0,
+    DPAR_LINEAR_BACKWARD = 1,
+    DPAR_GATED = 2,
+    DPAR_GATED_BACKWARD = 3
+} dpar_product_call_t;
+
+/* y = act(x w^T + bias) + residual.  Optional: bias, residual, z.
+ * z receives x w^T + bias (dtype), for the backward call.
+ * workspace: 16-byte aligned device memory of dpar_product_workspace bytes,
+ * in use until the stream's work completes, or NULL. */
+int dpar_linear(const void* const* x, const void* const* w,
+                const void* const* bias, const void* const* residual,
+                void* const* y, void* const* z, int p,
+                const dpar_product_t* opt, void* workspace,
+                size_t workspace_bytes, hipStream_t stream);
+
+/* Optional: dx, dw, dbias (what is not wanted is not computed; dbias only
+ * with the same rank's dw).  With DPAR_ACT_NONE z and dz may be NULL and are
+ * not touched; else z is what dpar_linear kept and dz receives dy * act'(z).
+ * dx of a layer whose x is shared is per rank: dpar_allreduce sums it. */
+int dpar_linear_backward(const void* const* dy, const void* const* x,
+                         const void* const* w, const void* const* z,
+                         void* const* dx, void* const* dw, void* const* dbias,
+                         void* const* dz, int p, const dpar_product_t* opt,
+                         void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/* h = act(x wg^T + bg) * (x wu^T + bu).  Optional: bg, bu, g, u (g and u
+ * receive the two projections, for the backward call; both or neither). */
+int dpar_gated(const void* const* x, const void* const* wg,
+               const void* const* wu, const void* const* bg,
+               const void* const* bu, void* const* h, void* const* g,
+               void* const* u, int p, const dpar_product_t* opt,
+               void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Optional: dx; dwg with dwu; dbg with dbu (only with dwg, dwu).  dg and du
+ * receive the projections' gradients (dtype). */
+int dpar_gated_backward(const void* const* dh, const void* const* x,
+                        const void* const* wg, const void* const* wu,
+                        const void* const* g, const void* const* u,
+                        void* const* dx, void* const* dwg, void* const* dwu,
+                        void* const* dbg, void* const* dbu, void* const* dg,
+                        void* const* du, int p, const dpar_product_t* opt,
+                        void* workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+
+/* *bytes: the workspace with which a call of these sizes runs fastest on the
+ * current device (0: it takes none).  No device work. */
+int dpar_product_workspace(dpar_product_call_t call, int p,
+                           const dpar_product_t* opt, size_t* bytes);
 
 /* Frees every library-owned device and pinned host buffer (device tables,
  * counters, staging).  The library re-creates them lazily on the next call.

@@ -1,6 +1,7 @@
 """Builds libdpar.so in place: HIP kernels for gfx950 with hipcc, host C++
 with g++, linked by hipcc.  ``python -m paper_2109_12626_amd.build``."""
 
+import concurrent.futures
 import os
 import subprocess
 import sys
@@ -20,6 +21,7 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-result",
 ]
+HIP_SOURCES = ["kernels.hip", "products.hip"]
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
               "-Wno-unused-parameter", "-D__HIP_PLATFORM_AMD__"]
 
@@ -27,6 +29,14 @@ HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
 def _run(cmd):
     print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
+
+
+def _run_all(cmds):
+    """The commands side by side, as many as the machine is meant to run."""
+    jobs = int(os.environ.get("MAX_JOBS") or min(8, os.cpu_count() or 1))
+    with concurrent.futures.ThreadPoolExecutor(max(1, jobs)) as pool:
+        for done in [pool.submit(_run, c) for c in cmds]:
+            done.result()
 
 
 def build(verbose=True, out=None, defines=(), host_sanitize=False):
@@ -44,15 +54,18 @@ def build(verbose=True, out=None, defines=(), host_sanitize=False):
     hipcc = os.path.join(ROCM, "bin", "hipcc")
     objs = []
     san = ["-fsanitize=address,undefined", "-g"] if host_sanitize else []
-    for src in ("plan.cpp", "api.cpp"):
+    for src in ("plan.cpp", "api.cpp", "products_api.cpp"):
         obj = os.path.join(build_dir, src + ".o")
         _run(["g++"] + HOST_FLAGS + san + inc +
              ["-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    obj = os.path.join(build_dir, "kernels.hip.o")
-    _run([hipcc] + HIP_FLAGS + [f"-D{d}" for d in defines] + inc
-         + ["-c", os.path.join(CSRC, "kernels.hip"), "-o", obj])
-    objs.append(obj)
+    cmds = []
+    for src in HIP_SOURCES:
+        obj = os.path.join(build_dir, src + ".o")
+        cmds.append([hipcc] + HIP_FLAGS + [f"-D{d}" for d in defines] + inc
+                    + ["-c", os.path.join(CSRC, src), "-o", obj])
+        objs.append(obj)
+    _run_all(cmds)
     lib = LIB if out is None else out
     tmp = lib + ".tmp"
     link_san = (["-Xarch_host", "-fsanitize=address",

@@ -16,6 +16,7 @@
 #include <unistd.h>
 
 #include "dpar.h"
+#include "errors.hpp"
 #include "kernels.hpp"
 #include "plan.hpp"
 
@@ -38,6 +39,15 @@ int fail(int code, const char* fmt, ...) {
 int hip_fail(hipError_t e, const char* what) {
   return fail(DPAR_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace
+
+int dpar::set_error(int code, const char* text) {
+  g_err = text;
+  return code;
+}
+
+namespace {
 
 constexpr int kCounterSlots = 64;      // concurrent calls before reuse
 using dpar::kCounterStride;            // uint32 words: 128-byte lines

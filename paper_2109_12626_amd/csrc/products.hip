@@ -1,0 +1,710 @@
+// Layer products on gfx950's matrix cores: one tiled kernel for every form
+// (products.hpp), types bf16, fp16 and fp32, results accumulated in fp32.
+#include <hip/hip_runtime.h>
+
+#include "products.hpp"
+
+namespace dpar {
+namespace products {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+#define LDS __attribute__((address_space(3)))
+
+// A piece is 16 bytes; every tile holds 128 bytes of the contraction: 64
+// 16-bit or 32 32-bit values, in two steps of 4 pieces (one per lane group
+// of 16).
+constexpr int kLine = 128;
+
+template <Type T> struct Elem;
+template <> struct Elem<Type::BF16> {
+  using V = __bf16;
+  static __device__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        __builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+        0);
+  }
+  static __device__ i32x4 ones() {
+    const bf16x8 v = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    return __builtin_bit_cast(i32x4, v);
+  }
+};
+template <> struct Elem<Type::F16> {
+  using V = _Float16;
+  static __device__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(
+        __builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+        0);
+  }
+  static __device__ i32x4 ones() {
+    const f16x8 v = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    return __builtin_bit_cast(i32x4, v);
+  }
+};
+template <> struct Elem<Type::F32> {
+  using V = float;
+  // Component s of the four lane groups' pieces makes one product of depth 4;
+  // both operands order the contraction alike.
+  static __device__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
+    const f32x4 x = __builtin_bit_cast(f32x4, a),
+                y = __builtin_bit_cast(f32x4, b);
+    for (int s = 0; s < 4; ++s)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], y[s], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ i32x4 ones() {
+    const f32x4 v = {1.f, 1.f, 1.f, 1.f};
+    return __builtin_bit_cast(i32x4, v);
+  }
+};
+
+// ---------------------------------------------------------------- activations
+
+__device__ inline float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
+
+// 0.5 (1 + tanh a) = sigmoid(2 a)
+constexpr float kTanh2 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+constexpr float kCubic = 0.044715f;
+constexpr float kInvSqrt2 = 0.70710678118654752f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+
+// The limits at infinity included: below -128 every activation but RELU and
+// NONE is -0 in 32 bits.
+__device__ inline float act_of(int act, float z) {
+  if (act >= (int)Act::GELU) z = z < -128.f ? -128.f : z;
+  switch (act) {
+    case (int)Act::RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+    case (int)Act::GELU: return 0.5f * z * (1.f + erff(z * kInvSqrt2));
+    case (int)Act::GELU_TANH:
+      return z * sigmoid(kTanh2 * (z + kCubic * z * z * z));
+    case (int)Act::SILU: return z * sigmoid(z);
+    default: return z;
+  }
+}
+
+// act(z) and act'(z); beyond 128 the slopes are 0 and 1
+__device__ inline float slope_of(int act, float z, float* value) {
+  if (act >= (int)Act::GELU) {
+    *value = act_of(act, z);
+    z = z < -128.f ? -128.f : z > 128.f ? 128.f : z;
+  }
+  switch (act) {
+    case (int)Act::RELU:
+      *value = act_of(act, z);
+      return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    case (int)Act::GELU: {
+      const float c = 0.5f * (1.f + erff(z * kInvSqrt2));
+      return c + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
+    }
+    case (int)Act::GELU_TANH: {
+      const float s = sigmoid(kTanh2 * (z + kCubic * z * z * z));
+      return s + z * s * (1.f - s) * kTanh2 * (1.f + 3.f * kCubic * z * z);
+    }
+    case (int)Act::SILU: {
+      const float s = sigmoid(z);
+      return s * (1.f + z * (1.f - s));
+    }
+    default: *value = z; return 1.f;
+  }
+}
+
+// ---------------------------------------------------------------- tiles
+
+__device__ const i32x4 g_zero = {0, 0, 0, 0};
+
+// Where a piece lies in its LDS row: pieces are exchanged by a key of the row
+// so that the 16 lanes that read together touch all banks.
+//   CC (row of the operand, 8 pieces): lanes read one piece of 16 rows.
+//   RC (one step of the contraction, W values): lanes read 4 contraction
+//      rows x 16 values (16-bit, transposing reads), or one value each (32).
+// G: distance of the 4-value groups that one matrix row index takes.
+template <Type T, bool CC, int W, int G>
+__device__ inline int key_of(int row) {
+  if (CC) {
+    if (G == 4) return row & 7;
+    return (row & 3) | ((row / G & 1) << 2);
+  }
+  if (T == Type::F32) {
+    const int q = (row >> 2) & 3;
+    return G == 4 ? q * 4 : q;
+  }
+  // 64 values: two rows share the banks' 256 bytes
+  const int r = W == 64 ? (row >> 1) & 1 : row & 3;
+  const int hi = W == 64 ? (row >> 3) & 1 : 0;
+  if (G == 4) return (r | hi << 1 | (W == 64 ? 0 : ((row >> 3) & 1) << 2)) * 2;
+  if (G == 8) return r * 4;
+  return (r & 1) | ((r >> 1) << 3);
+}
+
+template <typename V>
+__device__ inline i32x4 load_piece(const V* p, long n) {
+  constexpr int E = 16 / sizeof(V);
+  i32x4 v = {0, 0, 0, 0};
+  if (n >= E) {
+    __builtin_memcpy(&v, p, 16);       // any alignment
+  } else if (n > 0) {
+    V t[E];
+    for (int k = 0; k < E; ++k) t[k] = k < n ? p[k] : (V)0.f;
+    __builtin_memcpy(&v, t, 16);
+  }
+  return v;
+}
+
+__device__ inline void dma16(const void* g, LDS void* l) {
+  __builtin_amdgcn_global_load_lds(
+      (const __attribute__((address_space(1))) void*)g, l, 16, 0, 0);
+}
+
+// One operand's tile: W rows (CC) or W values of every contraction step (RC).
+template <Type T, bool CC, int W, int G, int THREADS>
+struct Operand {
+  using V = typename Elem<T>::V;
+  static constexpr int E = 16 / sizeof(V);       // values per piece
+  static constexpr int KT = kLine / sizeof(V);   // contraction per tile
+  static constexpr int N = W * 8 / THREADS;      // pieces per thread
+  static constexpr int P = CC ? 8 : W / E;       // pieces per LDS row
+
+  // row, first value of thread t's n-th piece (LDS order is linear in t)
+  static __device__ void at(int n, int t, int* row, int* val) {
+    const int o = n * THREADS + t;
+    *row = o / P;
+    *val = ((o % P) ^ key_of<T, CC, W, G>(*row)) * E;
+  }
+
+  // The address of a piece, g_zero past the contraction's end; rows and
+  // values past the operand's end give the last ones (their results are not
+  // stored).  Whole pieces only (fast operands).
+  static __device__ const void* source(const V* base, size_t ld, size_t i0,
+                                       size_t ni, size_t c0, size_t nc, int n,
+                                       int t, bool tail) {
+    int row, val;
+    at(n, t, &row, &val);
+    size_t i, c;
+    if (CC) {
+      i = i0 + row;
+      c = c0 + val;
+      if (i >= ni) i = ni - 1;
+      if (tail && c >= nc) return &g_zero;
+      return base + i * ld + c;
+    }
+    c = c0 + row;
+    i = i0 + val;
+    if (i >= ni) i = ni - E;
+    if (tail && c >= nc) return &g_zero;
+    return base + c * ld + i;
+  }
+
+  // The same for any alignment and length, into registers.
+  static __device__ i32x4 fetch(const V* base, size_t ld, size_t i0, size_t ni,
+                                size_t c0, size_t nc, int n, int t) {
+    int row, val;
+    at(n, t, &row, &val);
+    if (CC) {
+      size_t i = i0 + row;
+      const size_t c = c0 + val;
+      if (i >= ni) i = ni - 1;
+      return load_piece<V>(base + i * ld + c, (long)nc - (long)c);
+    }
+    const size_t c = c0 + row, i = i0 + val;
+    return load_piece<V>(base + c * ld + i,
+                         c < nc ? (long)ni - (long)i : 0);
+  }
+
+  // The piece of the contraction that lane group q feeds the matrix cores
+  // with in step ks, for the 16 rows (CC: row of lane r; RC: values from
+  // first + group of 4 * G).
+  static __device__ i32x4 frag(LDS char* s, int ks, int first, int lane) {
+    const int r = lane & 15, q = lane >> 4;
+    if constexpr (CC) {
+      const int row = first + (r >> 2) * G + (r & 3);
+      const int piece = (ks * 4 + q) ^ key_of<T, CC, W, G>(row);
+      return *(LDS i32x4*)(s + row * kLine + piece * 16);
+    } else if constexpr (T == Type::F32) {
+      i32x4 v;
+      const int col = first + (r >> 2) * G + (r & 3);
+      for (int k = 0; k < 4; ++k) {
+        const int c = ks * 16 + q * 4 + k;
+        v[k] = *(LDS int*)(s + c * (W * 4) +
+                           ((col >> 2) ^ key_of<T, CC, W, G>(c)) * 16 +
+                           (col & 3) * 4);
+      }
+      return v;
+    } else {
+      // transposing read: within 16 lanes, lane 4 k + g gives the address of
+      // 4 values of group g in contraction row k; lane r receives value
+      // r % 4 of group r / 4 from the four rows
+      i16x4 h[2];
+      const int col = first + (r & 3) * G;
+      for (int k = 0; k < 2; ++k) {
+        const int c = ks * 32 + q * 8 + k * 4 + (r >> 2);
+        h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (LDS i16x4*)(s + c * (W * 2) +
+                         ((col >> 3) ^ key_of<T, CC, W, G>(c)) * 16 +
+                         ((col >> 2) & 1) * 8));
+      }
+      i32x4 v;
+      __builtin_memcpy(&v, h, 16);
+      return v;
+    }
+  }
+};
+
+// ---------------------------------------------------------------- results
+
+// n consecutive results of a row: whole 16-byte pieces, or one by one up to
+// `left`.
+template <typename V, int N>
+__device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
+  constexpr int E = 16 / sizeof(V);
+  if (wide && left >= N) {
+    for (int k = 0; k < N; k += E) {
+      V t[E];
+      for (int e = 0; e < E; ++e) t[e] = (V)v[k + e];
+      i32x4 w;
+      __builtin_memcpy(&w, t, 16);
+      *(i32x4*)(p + k) = w;
+    }
+    return;
+  }
+  for (int k = 0; k < N; ++k)
+    if (k < left) p[k] = (V)v[k];
+}
+
+template <typename V, int N>
+__device__ inline void fetch_vals(const V* p, float* v, long left, bool wide) {
+  constexpr int E = 16 / sizeof(V);
+  if (wide && left >= N) {
+    for (int k = 0; k < N; k += E) {
+      const i32x4 w = *(const i32x4*)(p + k);
+      V t[E];
+      __builtin_memcpy(t, &w, 16);
+      for (int e = 0; e < E; ++e) v[k + e] = (float)t[e];
+    }
+    return;
+  }
+  for (int k = 0; k < N; ++k) v[k] = k < left ? (float)p[k] : 0.f;
+}
+
+template <int N>
+__device__ inline void store_out(void* o, size_t at, const float* v, long left,
+                                 int out32, bool wide, float) {
+  store_vals<float, N>((float*)o + at, v, left, wide);
+}
+template <int N, typename V>
+__device__ inline void store_out(void* o, size_t at, const float* v, long left,
+                                 int out32, bool wide, V) {
+  if (out32)
+    store_vals<float, N>((float*)o + at, v, left, wide);
+  else
+    store_vals<V, N>((V*)o + at, v, left, wide);
+}
+
+// N consecutive values j .. of row i: bias, activation, residual, rounding,
+// stores.  v: the product's sums (GATED: v of g, u2 of u).
+template <Type T, Form F, int N>
+__device__ inline void finish(const Args& a, int rank, int pair, size_t i,
+                              size_t j, float* v, float* u2) {
+  using V = typename Elem<T>::V;
+  const long left = (long)a.nj - (long)j;
+  const bool wide = a.wide_out;
+  if constexpr (F == Form::LINEAR) {
+    if (const V* b = (const V*)a.e[0][rank]) {
+      float t[N];
+      fetch_vals<V, N>(b + j, t, left, wide);
+      for (int k = 0; k < N; ++k) v[k] += t[k];
+    }
+    if (V* z = (V*)a.o[1][rank])
+      store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
+    if (a.act)
+      for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]);
+    if (const void* r = a.e[1][rank]) {
+      float t[N];
+      if (a.out32)
+        fetch_vals<float, N>((const float*)r + i * a.lde + j, t, left, wide);
+      else
+        fetch_vals<V, N>((const V*)r + i * a.lde + j, t, left, wide);
+      for (int k = 0; k < N; ++k) v[k] += t[k];
+    }
+    store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
+  } else if constexpr (F == Form::GATED) {
+    float t[N];
+    if (const V* b = (const V*)a.e[0][rank]) {
+      fetch_vals<V, N>(b + j, t, left, wide);
+      for (int k = 0; k < N; ++k) v[k] += t[k];
+    }
+    if (const V* b = (const V*)a.e[1][rank]) {
+      fetch_vals<V, N>(b + j, t, left, wide);
+      for (int k = 0; k < N; ++k) u2[k] += t[k];
+    }
+    if (V* g = (V*)a.o[1][rank])
+      store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
+    if (V* u = (V*)a.u[0][rank])
+      store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
+    for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]) * u2[k];
+    store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
+  } else {
+    store_out<N>(a.o[F == Form::DW ? pair : 0][rank], i * a.ldo + j, v, left,
+                 a.out32, wide, V());
+  }
+}
+
+// ---------------------------------------------------------------- the kernel
+
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+struct Tiled {
+  using V = typename Elem<T>::V;
+  static constexpr bool kGated = F == Form::GATED;
+  static constexpr bool kACC = F != Form::DW;
+  static constexpr bool kBCC = F == Form::LINEAR || F == Form::GATED;
+  static constexpr int kThreads = BM / WM * (BN / WN) * 64;
+  static constexpr int MI = WM / 16, NJ = WN / 16;
+  // a lane's consecutive results: 4 per tile of 16, over all tiles of the
+  // wave (GATED: half are g's, half u's)
+  static constexpr int NT = kGated ? NJ / 2 : NJ;
+  static constexpr int G = 4 * NT;
+  static constexpr int BJ = kGated ? BN / 2 : BN;   // result columns
+  using OA = Operand<T, kACC, BM, 4, kThreads>;
+  using OB = Operand<T, kBCC, BN, G, kThreads>;
+  static constexpr int KT = OA::KT;
+  static constexpr int kBytesA = BM * kLine, kBytes = (BM + BN) * kLine;
+
+  static __device__ void run(const Args& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int wm = wave / (BN / WN), wn = wave % (BN / WN);
+    // (weights' gradients without columns still have bias sums)
+    const size_t mt = (a.ni + BM - 1) / BM,
+                 nt = a.nj ? (a.nj + BJ - 1) / BJ : 1;
+    // consecutive workgroups go to the 8 XCDs in turn: give each XCD a run of
+    // neighbouring tiles so that they share operands in its L2
+    unsigned id = blockIdx.x;
+    {
+      const unsigned n = gridDim.x, per = n / 8, rest = n % 8;
+      const unsigned x = id % 8, k = id / 8;
+      id = x * per + (x < rest ? x : rest) + k;
+    }
+    const size_t tiles = mt * nt;
+    const int split = id % a.splits;
+    unsigned r1 = id / a.splits;
+    size_t tile = r1 % tiles;
+    r1 /= (unsigned)tiles;
+    const int pair = F == Form::DW ? r1 % a.pairs : 0;
+    const int rank = F == Form::DW ? r1 / a.pairs : r1;
+    // groups of 8 tile rows, columns inside
+    const size_t grp = tile / (8 * nt), first = grp * 8;
+    const size_t high = mt - first < 8 ? mt - first : 8;
+    const size_t in = tile % (8 * nt);
+    const size_t i0 = (first + in % high) * BM, j0 = in / high * BJ;
+
+    const size_t nk1 = (a.nc + KT - 1) / KT;
+    const size_t nk = F == Form::DX ? nk1 * a.pairs : nk1;
+    const size_t k0 = nk * split / a.splits, k1 = nk * (split + 1) / a.splits;
+
+    f32x4 acc[MI][NJ] = {};
+    f32x4 sum[F == Form::DW ? MI : 1] = {};
+    const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0 && wn == 0;
+
+    i32x4 ra[FAST ? 1 : OA::N], rb[FAST ? 1 : OB::N];
+
+    auto bases = [&](size_t kt, const V** pa, const V** pb, const V** pb2,
+                     size_t* c0) {
+      const int s = F == Form::DX ? (kt >= nk1) : pair;
+      *c0 = (F == Form::DX ? kt - s * nk1 : kt) * KT;
+      *pa = (const V*)a.a[s][rank];
+      *pb = (const V*)a.b[kGated ? 0 : (F == Form::DW ? 0 : s)][rank];
+      *pb2 = kGated ? (const V*)a.b[1][rank] : *pb;
+    };
+    auto issue = [&](size_t kt, int buf) {
+      const V *pa, *pb, *pb2;
+      size_t c0;
+      bases(kt, &pa, &pb, &pb2, &c0);
+      const bool tail = c0 + KT > a.nc;
+      LDS char* d = lds + buf * kBytes + wave * 1024;
+      if constexpr (FAST) {
+#pragma unroll
+        for (int n = 0; n < OA::N; ++n)
+          dma16(OA::source(pa, a.lda, i0, a.ni, c0, a.nc, n, t, tail),
+                d + n * kThreads * 16);
+        d += kBytesA;
+#pragma unroll
+        for (int n = 0; n < OB::N; ++n) {
+          const bool up = kGated && n >= OB::N / 2;
+          dma16(OB::source(up ? pb2 : pb, a.ldb,
+                           up ? j0 - BJ : j0, a.nj, c0, a.nc, n, t, tail),
+                d + n * kThreads * 16);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < OA::N; ++n)
+          ra[n] = OA::fetch(pa, a.lda, i0, a.ni, c0, a.nc, n, t);
+#pragma unroll
+        for (int n = 0; n < OB::N; ++n) {
+          const bool up = kGated && n >= OB::N / 2;
+          rb[n] = OB::fetch(up ? pb2 : pb, a.ldb, up ? j0 - BJ : j0, a.nj, c0,
+                            a.nc, n, t);
+        }
+      }
+    };
+    auto land = [&](int buf) {
+      if constexpr (!FAST) {
+        LDS char* d = lds + buf * kBytes + t * 16;
+#pragma unroll
+        for (int n = 0; n < OA::N; ++n)
+          *(LDS i32x4*)(d + n * kThreads * 16) = ra[n];
+        d += kBytesA;
+#pragma unroll
+        for (int n = 0; n < OB::N; ++n)
+          *(LDS i32x4*)(d + n * kThreads * 16) = rb[n];
+      }
+    };
+
+    if (k0 < k1) issue(k0, 0);
+    for (size_t kt = k0; kt < k1; ++kt) {
+      const int buf = (kt - k0) & 1;
+      land(buf);
+      __syncthreads();
+      if (kt + 1 < k1) issue(kt + 1, buf ^ 1);
+      LDS char* sa = lds + buf * kBytes;
+      LDS char* sb = sa + kBytesA;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        i32x4 fa[MI], fb[NJ];
+#pragma unroll
+        for (int n = 0; n < NJ; ++n) {
+          const int first = kGated
+              ? (n < NT ? 0 : BJ) + wn * (WN / 2) + (n % NT) * 4
+              : wn * WN + n * 4;
+          fb[n] = OB::frag(sb, ks, first, lane);
+        }
+#pragma unroll
+        for (int m = 0; m < MI; ++m)
+          fa[m] = OA::frag(sa, ks, wm * WM + m * 16, lane);
+#pragma unroll
+        for (int m = 0; m < MI; ++m)
+#pragma unroll
+          for (int n = 0; n < NJ; ++n)
+            acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
+        if constexpr (F == Form::DW)
+          if (sums)
+            for (int m = 0; m < MI; ++m)
+              sum[m] = Elem<T>::mma(Elem<T>::ones(), fa[m], sum[m]);
+      }
+    }
+
+    // lane (r, q): row r of each 16, results q * G ... of the wave's columns
+    const int r = lane & 15, q = lane >> 4;
+    const size_t j = j0 + wn * (kGated ? WN / 2 : WN) + q * G;
+#pragma unroll
+    for (int m = 0; m < MI; ++m) {
+      const size_t i = i0 + wm * WM + m * 16 + r;
+      if (i >= a.ni) continue;
+      float v[G], u2[kGated ? G : 1];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 4; ++e) {
+          v[n * 4 + e] = acc[m][n][e];
+          if constexpr (kGated) u2[n * 4 + e] = acc[m][n + NT][e];
+        }
+      if (F == Form::DW && sums && q == 0) {
+        if (a.splits == 1) {
+          float s = sum[m][0];
+          store_out<1>(a.u[pair][rank], i, &s, 1, a.out32, false, V());
+        } else {
+          // after all partial results: [split][rank][pair][row]
+          a.part[(size_t)a.splits * a.ranks * a.pairs * a.ni * a.nj +
+                 (((size_t)split * a.ranks + rank) * a.pairs + pair) * a.ni +
+                 i] = sum[m][0];
+        }
+      }
+      if (j >= a.nj) continue;
+      if (a.splits == 1) {
+        finish<T, F, G>(a, rank, pair, i, j, v, u2);
+      } else {
+        // [split][rank][pair or projection][row][column]
+        const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
+        const size_t sz = a.ni * a.nj;
+        float* w = a.part + (((size_t)split * a.ranks + rank) * np + pair) * sz
+                   + i * a.nj + j;
+        const long left = (long)a.nj - (long)j;
+        const bool wide = a.nj % 4 == 0;
+        store_vals<float, G>(w, v, left, wide);
+        if constexpr (kGated) store_vals<float, G>(w + sz, u2, left, wide);
+      }
+    }
+  }
+};
+
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args a) {
+  extern __shared__ char lds[];
+  Tiled<T, F, FAST, BM, BN, WM, WN>::run(a, (LDS char*)lds);
+}
+
+// Joins the parts of a split contraction in their order and finishes: 4
+// results per thread.
+template <Type T, Form F>
+__global__ __launch_bounds__(256) void k_join(Args a) {
+  using V = typename Elem<T>::V;
+  const size_t per = (a.nj + 3) / 4;
+  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int np = F == Form::DW ? a.pairs : 1;
+  const size_t all = per * a.ni * a.ranks * np;
+  const size_t sz = a.ni * a.nj;
+  constexpr int NP = F == Form::GATED ? 2 : 1;
+  if (id < all) {
+    const size_t j = id % per * 4, x = id / per;
+    const size_t i = x % a.ni;
+    const int pair = x / a.ni % np, rank = x / a.ni / np;
+    const long left = (long)a.nj - (long)j;
+    float v[4] = {}, u2[4] = {}, t[4];
+    const size_t step = (size_t)a.ranks * np * NP * sz;
+    const float* w = a.part + ((size_t)rank * np + pair) * NP * sz + i * a.nj
+                     + j;
+    for (int s = 0; s < a.splits; ++s, w += step) {
+      fetch_vals<float, 4>(w, t, left, a.nj % 4 == 0);
+      for (int k = 0; k < 4; ++k) v[k] += t[k];
+      if (F == Form::GATED) {
+        fetch_vals<float, 4>(w + sz, t, left, a.nj % 4 == 0);
+        for (int k = 0; k < 4; ++k) u2[k] += t[k];
+      }
+    }
+    finish<T, F, 4>(a, rank, pair, i, j, v, u2);
+  }
+  if (F == Form::DW) {
+    const size_t n = (size_t)a.ranks * a.pairs * a.ni;
+    if (id < n && a.u[id / a.ni % a.pairs][id / a.ni / a.pairs]) {
+      const float* w = a.part +
+                       (size_t)a.splits * a.ranks * a.pairs * sz + id;
+      float s = 0.f;
+      for (int k = 0; k < a.splits; ++k) s += w[k * n];
+      store_out<1>(a.u[id / a.ni % a.pairs][id / a.ni / a.pairs], id % a.ni,
+                   &s, 1, a.out32, false, V());
+    }
+  }
+}
+
+template <Type T, bool GATED>
+__global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
+  using V = typename Elem<T>::V;
+  constexpr int E = 16 / sizeof(V);
+  const int rank = blockIdx.y;
+  const size_t per = (a.cols + E - 1) / E, all = per * a.rows;
+  const V* dy = (const V*)a.dy[rank];
+  const V* z = (const V*)a.z[rank];
+  const V* u = GATED ? (const V*)a.u[rank] : nullptr;
+  V* dz = (V*)a.dz[rank];
+  V* du = GATED ? (V*)a.du[rank] : nullptr;
+  for (size_t id = (size_t)blockIdx.x * 256 + threadIdx.x; id < all;
+       id += (size_t)gridDim.x * 256) {
+    const size_t i = id / per, j = id % per * E;
+    const long left = (long)a.cols - (long)j;
+    float d[E], s[E], g[E], o[E];
+    fetch_vals<V, E>(dy + i * a.ldy + j, d, left, a.wide);
+    fetch_vals<V, E>(z + i * a.ldz + j, g, left, a.wide);
+    if (GATED) fetch_vals<V, E>(u + i * a.ldz + j, s, left, a.wide);
+    for (int k = 0; k < E; ++k) {
+      float v;
+      const float c = slope_of(a.act, g[k], &v);
+      if (GATED) {
+        o[k] = d[k] * v;
+        d[k] = d[k] * s[k] * c;
+      } else {
+        d[k] *= c;
+      }
+    }
+    store_vals<V, E>(dz + i * a.ldz + j, d, left, a.wide);
+    if (GATED) store_vals<V, E>(du + i * a.ldz + j, o, left, a.wide);
+  }
+}
+
+// ---------------------------------------------------------------- launches
+
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+hipError_t go(const Args& a, hipStream_t stream) {
+  using K = Tiled<T, F, FAST, BM, BN, WM, WN>;
+  const size_t tiles =
+      (a.ni + BM - 1) / BM * (a.nj ? (a.nj + K::BJ - 1) / K::BJ : 1);
+  const size_t n = tiles * a.ranks * (F == Form::DW ? a.pairs : 1) * a.splits;
+  if (n == 0) return hipSuccess;
+  if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
+  const size_t bytes = 2 * K::kBytes;
+  auto k = k_tiled<T, F, FAST, BM, BN, WM, WN>;
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(
+        (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
+        (int)bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(K::kThreads), bytes, stream,
+                     a);
+  return hipGetLastError();
+}
+
+template <Type T, Form F>
+hipError_t pick(const Args& a, hipStream_t stream) {
+  hipError_t e;
+  if (a.fast)
+    e = go<T, F, true, 128, 128, 64, 64>(a, stream);
+  else
+    e = go<T, F, false, 128, 128, 64, 64>(a, stream);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const size_t n = (a.nj + 3) / 4 * a.ni * a.ranks *
+                   (F == Form::DW ? a.pairs : 1);
+  hipLaunchKernelGGL((k_join<T, F>), dim3((unsigned)((n + 255) / 256)),
+                     dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <Form F>
+hipError_t by_type(Type t, const Args& a, hipStream_t stream) {
+  switch (t) {
+    case Type::BF16: return pick<Type::BF16, F>(a, stream);
+    case Type::F16: return pick<Type::F16, F>(a, stream);
+    default: return pick<Type::F32, F>(a, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch(Form f, Type t, const Args& a, hipStream_t stream) {
+  switch (f) {
+    case Form::LINEAR: return by_type<Form::LINEAR>(t, a, stream);
+    case Form::GATED: return by_type<Form::GATED>(t, a, stream);
+    case Form::DX: return by_type<Form::DX>(t, a, stream);
+    default: return by_type<Form::DW>(t, a, stream);
+  }
+}
+
+template <Type T>
+static hipError_t slope(const SlopeArgs& a, hipStream_t stream) {
+  constexpr int E = 16 / sizeof(typename Elem<T>::V);
+  const size_t n = (a.cols + E - 1) / E * a.rows;
+  const size_t blocks = (n + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096), a.ranks);
+  if (a.gated)
+    hipLaunchKernelGGL((k_slope<T, true>), grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_slope<T, false>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_slope(Type t, const SlopeArgs& a, hipStream_t stream) {
+  switch (t) {
+    case Type::BF16: return slope<Type::BF16>(a, stream);
+    case Type::F16: return slope<Type::F16>(a, stream);
+    default: return slope<Type::F32>(a, stream);
+  }
+}
+
+size_t part_bytes(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
+                  size_t nc, int cus, int* splits) {
+  *splits = 1;
+  return 0;
+}
+
+}  // namespace products
+}  // namespace dpar

@@ -1,0 +1,72 @@
+// Interface between the C entry points of the layer products and their
+// kernels.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace dpar {
+namespace products {
+
+// Element types (values of dpar_dtype_t).
+enum class Type : int { F32 = 1, BF16 = 3, F16 = 4 };
+// Activations (values of dpar_act_t).
+enum class Act : int { NONE = 0, RELU = 1, GELU = 2, GELU_TANH = 3, SILU = 4 };
+
+// One launch covers up to this many ranks: their addresses travel in the
+// kernel arguments (8 arrays of 48 addresses, 3 KB of the 4 KB a launch
+// takes), so a call stages nothing, allocates nothing and can be captured.
+constexpr int kRanks = 48;
+
+// C[i][j] = sum over c of A(i, c) B(j, c), for every rank of a launch.
+//   LINEAR  A = x[i][c],  B = w[j][c];        C = act(.. + bias) + residual
+//   GATED   A = x[i][c],  B = wg, wu[j][c];   C = act(g) * u
+//   DX      A = dz[i][c], B = w[c][j], one or two pairs summed
+//   DW      A = dz[c][i], B = x[c][j]; with two pairs two results, and the
+//           sums of A over c (bias gradients)
+enum class Form : int { LINEAR = 0, GATED = 1, DX = 2, DW = 3 };
+
+struct Args {
+  const void* a[2][kRanks];
+  const void* b[2][kRanks];
+  // LINEAR: bias, residual; GATED: bias of g, of u
+  const void* e[2][kRanks];
+  // LINEAR: y, z; GATED: h, g (u is in `u`); DX: dx; DW: dw, dw of u
+  void* o[2][kRanks];
+  // GATED: u; DW: bias gradients
+  void* u[2][kRanks];
+  size_t ni, nj, nc;         // rows and columns of C, contraction
+  size_t lda, ldb, ldo, ldk, lde;  // row distances (elements): A, B, result,
+                                   // kept values, residual
+  float* part;               // partial results of a split contraction
+  int ranks, pairs;
+  int act;
+  int out32;                 // result in 32 bits
+  int splits;                // parts of the contraction
+  int fast;                  // A, B: 16-byte rows and whole 16-byte pieces
+  int wide_out;              // results, kept values, residual, bias: 16-byte
+                             // pieces
+};
+
+// Bytes of workspace that a launch of this form takes (0: none).
+size_t part_bytes(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
+                  size_t nc, int cus, int* splits);
+
+hipError_t launch(Form f, Type t, const Args& a, hipStream_t stream);
+
+// dz = dy act'(z) (gated == 0), or dg = dy u act'(g), du = dy act(g).
+struct SlopeArgs {
+  const void* dy[kRanks];
+  const void* z[kRanks];
+  const void* u[kRanks];
+  void* dz[kRanks];
+  void* du[kRanks];
+  size_t rows, cols, ldy, ldz;
+  int ranks, act, gated, wide;
+};
+hipError_t launch_slope(Type t, const SlopeArgs& a, hipStream_t stream);
+
+}  // namespace products
+}  // namespace dpar

@@ -1,0 +1,587 @@
+// C entry points of the layer products: argument and alias checks, the rules
+// that choose a kernel, launches of at most kRanks ranks.
+#include <hip/hip_runtime_api.h>
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+#include <vector>
+
+#include "dpar.h"
+#include "errors.hpp"
+#include "products.hpp"
+
+using dpar::products::Args;
+using dpar::products::Form;
+using dpar::products::kRanks;
+using dpar::products::SlopeArgs;
+using dpar::products::Type;
+
+namespace {
+
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+int fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return dpar::set_error(code, buf);
+}
+
+// One array argument: p matrices of rows x cols elements, `ld` elements
+// apart.
+struct Mat {
+  const char* name;
+  const void* const* at;
+  size_t rows, cols, ld, esz;
+  bool out;
+  bool gaps;               // entries may be null (bias, residual)
+  bool used;
+  const void* const* twin[2] = {nullptr, nullptr};  // inputs it may be
+
+  size_t extent() const {
+    return rows && cols ? ((rows - 1) * ld + cols) * esz : 0;
+  }
+  // every row starts on 16 bytes
+  bool aligned(int p) const {
+    if (!used || !extent()) return true;
+    uintptr_t bits = rows > 1 ? ld * esz : 0;
+    for (int i = 0; i < p; ++i) bits |= (uintptr_t)at[i];
+    return (bits & 15) == 0;
+  }
+  const void* rank(int i) const { return used ? at[i] : nullptr; }
+};
+
+struct Range {
+  uintptr_t lo, hi;
+  size_t width, pitch;
+  int mat, rank;
+};
+
+// Whether two matrices share a byte; ranges overlap already.  Matrices of one
+// row distance may lie side by side.
+bool share(const Range& a, const Range& b) {
+  if (a.pitch == b.pitch && a.pitch != 0) {
+    const size_t d = (b.lo - a.lo) % a.pitch;   // b.lo >= a.lo
+    if (d >= a.width && d + b.width <= a.pitch) return false;
+  }
+  return true;
+}
+
+int check_alias(const Mat* mats, int n, int p, const char* call) {
+  thread_local std::vector<Range> r;
+  r.clear();
+  for (int k = 0; k < n; ++k) {
+    const Mat& m = mats[k];
+    if (!m.used || !m.extent()) continue;
+    for (int i = 0; i < p; ++i)
+      if (const uintptr_t a = (uintptr_t)m.at[i])
+        r.push_back({a, a + m.extent(), m.cols * m.esz, m.ld * m.esz, k, i});
+  }
+  std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) {
+    return a.lo != b.lo ? a.lo < b.lo : a.mat < b.mat;
+  });
+  // the same matrix read by many ranks counts once
+  r.erase(std::unique(r.begin(), r.end(),
+                      [&](const Range& a, const Range& b) {
+                        return !mats[a.mat].out && a.mat == b.mat &&
+                               a.lo == b.lo;
+                      }),
+          r.end());
+  for (size_t k = 0; k < r.size(); ++k)
+    for (size_t l = k + 1; l < r.size() && r[l].lo < r[k].hi; ++l) {
+      const Mat &a = mats[r[k].mat], &b = mats[r[l].mat];
+      if (!a.out && !b.out) continue;
+      if (!share(r[k], r[l])) continue;
+      // an output in place of its rank's input
+      const Range &o = a.out ? r[k] : r[l], &in = a.out ? r[l] : r[k];
+      const Mat &mo = mats[o.mat], &mi = mats[in.mat];
+      if (!mi.out && o.lo == in.lo && mo.ld == mi.ld &&
+          (mo.twin[0] == mi.at || mo.twin[1] == mi.at) &&
+          mi.at[o.rank] == mo.at[o.rank]) {
+        // read by no other rank
+        bool alone = true;
+        for (int i = 0; i < p; ++i)
+          if (i != o.rank && mi.at[i] == mo.at[o.rank]) alone = false;
+        if (alone) continue;
+      }
+      return fail(DPAR_ERR_ALIAS, "%s: %s of rank %d overlaps %s of rank %d",
+                  call, a.name, r[k].rank, b.name, r[l].rank);
+    }
+  return DPAR_SUCCESS;
+}
+
+int check_mats(const Mat* mats, int n, int p, const char* call) {
+  for (int k = 0; k < n; ++k) {
+    const Mat& m = mats[k];
+    if (!m.used) continue;
+    if (m.ld < m.cols && m.rows > 1)
+      return fail(DPAR_ERR_INVALID_ARG, "%s: rows of %s overlap: distance "
+                  "%zu, length %zu", call, m.name, m.ld, m.cols);
+    if (!m.at) return fail(DPAR_ERR_INVALID_ARG, "%s: null array %s", call,
+                           m.name);
+    const bool empty = m.extent() == 0;
+    for (int i = 0; i < p; ++i) {
+      const uintptr_t a = (uintptr_t)m.at[i];
+      if (!a) {
+        if (m.gaps || empty) continue;
+        return fail(DPAR_ERR_INVALID_ARG, "%s: %s of rank %d is null", call,
+                    m.name, i);
+      }
+      if (a % m.esz)
+        return fail(DPAR_ERR_INVALID_ARG, "%s: %s of rank %d is not aligned "
+                    "to its element", call, m.name, i);
+      if (a >> 48)
+        return fail(DPAR_ERR_UNSUPPORTED, "%s: address of %s of rank %d above "
+                    "2^48", call, m.name, i);
+    }
+  }
+  return check_alias(mats, n, p, call);
+}
+
+constexpr size_t kMost = (size_t)1 << 31;     // rows, in, out
+constexpr size_t kMostPitch = (size_t)1 << 38;
+
+// The options with row distances filled in.
+int check_options(const char* call, int p, const dpar_product_t* opt,
+                  dpar_product_t* o, Type* t, size_t* esz, size_t* osz) {
+  dpar::set_error(0, "");
+  if (p < 1) return fail(DPAR_ERR_INVALID_ARG, "%s: p must be >= 1", call);
+  if (!opt) return fail(DPAR_ERR_INVALID_ARG, "%s: null options", call);
+  *o = *opt;
+  switch (o->dtype) {
+    case DPAR_FLOAT32: *t = Type::F32; break;
+    case DPAR_BFLOAT16: *t = Type::BF16; break;
+    case DPAR_FLOAT16: *t = Type::F16; break;
+    default:
+      return fail(DPAR_ERR_UNSUPPORTED, "%s: dtype %d", call, (int)o->dtype);
+  }
+  if (o->out_dtype != o->dtype && o->out_dtype != DPAR_FLOAT32)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: out_dtype %d with dtype %d", call,
+                (int)o->out_dtype, (int)o->dtype);
+  if ((int)o->act < DPAR_ACT_NONE || (int)o->act > DPAR_ACT_SILU)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: unknown activation %d", call,
+                (int)o->act);
+  if (o->rows >= kMost || o->in >= kMost || o->out >= kMost)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: a size beyond 2^31", call);
+  *esz = o->dtype == DPAR_FLOAT32 ? 4 : 2;
+  *osz = o->out_dtype == DPAR_FLOAT32 ? 4 : 2;
+  size_t* const in[] = {&o->ldx, &o->ldw, &o->lddx, &o->lddw};
+  size_t* const out[] = {&o->ldy, &o->ldr, &o->ldz};
+  for (size_t* v : in)
+    if (!*v) *v = o->in;
+  for (size_t* v : out)
+    if (!*v) *v = o->out;
+  for (size_t v : {o->ldx, o->ldw, o->lddx, o->lddw, o->ldy, o->ldr, o->ldz})
+    if (v > kMostPitch)
+      return fail(DPAR_ERR_UNSUPPORTED, "%s: a row distance beyond 2^38",
+                  call);
+  return DPAR_SUCCESS;
+}
+
+int cu_count() {
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount,
+                            dev) != hipSuccess || cus < 1) {
+    (void)hipGetLastError();
+    return 256;
+  }
+  return cus;
+}
+
+// Ranks of the largest launch: p ranks in as few launches as they need, all
+// about equal.
+int ranks_per_launch(int p) {
+  const int n = (p + kRanks - 1) / kRanks;
+  return (p + n - 1) / n;
+}
+
+struct Step {
+  Form form;
+  int pairs;
+  size_t ni, nj, nc;
+};
+
+// The products of a call.
+int steps_of(dpar_product_call_t call, const dpar_product_t& o, bool dx,
+             bool dw, Step* s) {
+  int n = 0;
+  switch (call) {
+    case DPAR_LINEAR:
+      s[n++] = {Form::LINEAR, 1, o.rows, o.out, o.in};
+      break;
+    case DPAR_GATED:
+      s[n++] = {Form::GATED, 1, o.rows, o.out, o.in};
+      break;
+    default: {
+      const int pairs = call == DPAR_GATED_BACKWARD ? 2 : 1;
+      if (dx) s[n++] = {Form::DX, pairs, o.rows, o.in, o.out};
+      if (dw) s[n++] = {Form::DW, pairs, o.out, o.in, o.rows};
+    }
+  }
+  return n;
+}
+
+size_t workspace_of(dpar_product_call_t call, Type t, int p,
+                    const dpar_product_t& o, int cus) {
+  Step s[2];
+  const int n = steps_of(call, o, true, true, s);
+  size_t most = 0;
+  for (int k = 0; k < n; ++k) {
+    int splits;
+    most = std::max(most, dpar::products::part_bytes(
+                              s[k].form, t, ranks_per_launch(p), s[k].pairs,
+                              s[k].ni, s[k].nj, s[k].nc, cus, &splits));
+  }
+  return most;
+}
+
+int check_workspace(const char* call, dpar_product_call_t which, Type t, int p,
+                    const dpar_product_t& o, void* ws, size_t bytes,
+                    int* cus) {
+  *cus = cu_count();
+  if (!ws) return DPAR_SUCCESS;
+  const size_t need = workspace_of(which, t, p, o, *cus);
+  if (bytes < need)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: workspace of %zu bytes, %zu needed",
+                call, bytes, need);
+  if ((uintptr_t)ws & 15)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: workspace not on 16 bytes", call);
+  return DPAR_SUCCESS;
+}
+
+int launched(const char* call, hipError_t e) {
+  if (e == hipSuccess) return DPAR_SUCCESS;
+  return fail(DPAR_ERR_HIP, "%s: %s", call, hipGetErrorString(e));
+}
+
+// Runs one product over all ranks.  a: everything but the addresses, which
+// `fill` writes for a rank.
+template <typename Fill>
+int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
+                int cus, hipStream_t stream, Fill fill) {
+  const int per = ranks_per_launch(p);
+  int splits = 1;
+  if (ws)
+    dpar::products::part_bytes(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
+                               &splits);
+  a->splits = splits;
+  a->part = (float*)ws;
+  for (int r0 = 0; r0 < p; r0 += per) {
+    a->ranks = std::min(per, p - r0);
+    for (int k = 0; k < a->ranks; ++k) fill(k, r0 + k);
+    const int rc = launched(call, dpar::products::launch(f, t, *a, stream));
+    if (rc) return rc;
+  }
+  return DPAR_SUCCESS;
+}
+
+template <typename Body>
+int guarded(const char* call, Body body) {
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return fail(DPAR_ERR_NOMEM, "%s: out of host memory", call);
+  } catch (...) {
+    return fail(DPAR_ERR_HIP, "%s: unexpected failure", call);
+  }
+}
+
+// Addresses of the array arguments as the checks take them.
+const void* const* in_array(void* const* a) { return (const void* const*)a; }
+
+int linear_impl(const void* const* x, const void* const* w,
+                const void* const* bias, const void* const* residual,
+                void* const* y, void* const* z, int p,
+                const dpar_product_t* opt, void* ws, size_t bytes,
+                hipStream_t stream) {
+  const char* call = "dpar_linear";
+  dpar_product_t o;
+  Type t;
+  size_t e, eo;
+  int rc = check_options(call, p, opt, &o, &t, &e, &eo);
+  if (rc) return rc;
+  const Mat m[] = {
+      {"x", x, o.rows, o.in, o.ldx, e, false, false, true},
+      {"w", w, o.out, o.in, o.ldw, e, false, false, true},
+      {"bias", bias, 1, o.out, o.out, e, false, true, bias != nullptr},
+      {"residual", residual, o.rows, o.out, o.ldr, eo, false, true,
+       residual != nullptr},
+      {"y", in_array(y), o.rows, o.out, o.ldy, eo, true, false, true},
+      {"z", in_array(z), o.rows, o.out, o.ldz, e, true, false, z != nullptr}};
+  if ((rc = check_mats(m, 6, p, call))) return rc;
+  int cus;
+  if ((rc = check_workspace(call, DPAR_LINEAR, t, p, o, ws, bytes, &cus)))
+    return rc;
+  if (!o.rows || !o.out) return DPAR_SUCCESS;
+  Args a = {};
+  a.ni = o.rows, a.nj = o.out, a.nc = o.in;
+  a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz, a.lde = o.ldr;
+  a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
+  a.fast = m[0].aligned(p) && m[1].aligned(p) && o.in * e % 16 == 0 && o.in;
+  a.wide_out = m[2].aligned(p) && m[3].aligned(p) && m[4].aligned(p) &&
+               m[5].aligned(p);
+  return run_product(call, Form::LINEAR, t, p, &a, ws, cus, stream,
+                     [&](int k, int i) {
+                       a.a[0][k] = m[0].rank(i);
+                       a.b[0][k] = m[1].rank(i);
+                       a.e[0][k] = m[2].rank(i);
+                       a.e[1][k] = m[3].rank(i);
+                       a.o[0][k] = (void*)m[4].rank(i);
+                       a.o[1][k] = (void*)m[5].rank(i);
+                     });
+}
+
+int gated_impl(const void* const* x, const void* const* wg,
+               const void* const* wu, const void* const* bg,
+               const void* const* bu, void* const* h, void* const* g,
+               void* const* u, int p, const dpar_product_t* opt, void* ws,
+               size_t bytes, hipStream_t stream) {
+  const char* call = "dpar_gated";
+  dpar_product_t o;
+  Type t;
+  size_t e, eo;
+  int rc = check_options(call, p, opt, &o, &t, &e, &eo);
+  if (rc) return rc;
+  if (!g != !u)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: g without u or u without g", call);
+  const Mat m[] = {
+      {"x", x, o.rows, o.in, o.ldx, e, false, false, true},
+      {"wg", wg, o.out, o.in, o.ldw, e, false, false, true},
+      {"wu", wu, o.out, o.in, o.ldw, e, false, false, true},
+      {"bg", bg, 1, o.out, o.out, e, false, true, bg != nullptr},
+      {"bu", bu, 1, o.out, o.out, e, false, true, bu != nullptr},
+      {"h", in_array(h), o.rows, o.out, o.ldy, eo, true, false, true},
+      {"g", in_array(g), o.rows, o.out, o.ldz, e, true, false, g != nullptr},
+      {"u", in_array(u), o.rows, o.out, o.ldz, e, true, false, u != nullptr}};
+  if ((rc = check_mats(m, 8, p, call))) return rc;
+  int cus;
+  if ((rc = check_workspace(call, DPAR_GATED, t, p, o, ws, bytes, &cus)))
+    return rc;
+  if (!o.rows || !o.out) return DPAR_SUCCESS;
+  Args a = {};
+  a.ni = o.rows, a.nj = o.out, a.nc = o.in;
+  a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz;
+  a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
+  a.fast = m[0].aligned(p) && m[1].aligned(p) && m[2].aligned(p) &&
+           o.in * e % 16 == 0 && o.in;
+  a.wide_out = m[3].aligned(p) && m[4].aligned(p) && m[5].aligned(p) &&
+               m[6].aligned(p) && m[7].aligned(p);
+  return run_product(call, Form::GATED, t, p, &a, ws, cus, stream,
+                     [&](int k, int i) {
+                       a.a[0][k] = m[0].rank(i);
+                       a.b[0][k] = m[1].rank(i);
+                       a.b[1][k] = m[2].rank(i);
+                       a.e[0][k] = m[3].rank(i);
+                       a.e[1][k] = m[4].rank(i);
+                       a.o[0][k] = (void*)m[5].rank(i);
+                       a.o[1][k] = (void*)m[6].rank(i);
+                       a.u[0][k] = (void*)m[7].rank(i);
+                     });
+}
+
+// Both backward calls; pairs: 1 (dpar_linear_backward) or 2.
+struct Back {
+  const void* const* dy;
+  const void* const* x;
+  const void* const* w[2];
+  const void* const* z[2];     // z; g, u
+  void* const* dx;
+  void* const* dw[2];
+  void* const* db[2];
+  void* const* dz[2];
+};
+
+int backward_impl(const char* call, int pairs, const Back& b, int p,
+                  const dpar_product_t* opt, void* ws, size_t bytes,
+                  hipStream_t stream) {
+  dpar_product_t o;
+  Type t;
+  size_t e, eo;
+  int rc = check_options(call, p, opt, &o, &t, &e, &eo);
+  if (rc) return rc;
+  const bool gated = pairs == 2;
+  const bool slope = gated || o.act != DPAR_ACT_NONE;
+  const bool dx = b.dx != nullptr, dw = b.dw[0] != nullptr,
+             db = b.db[0] != nullptr;
+  if (gated && (!b.dw[0] != !b.dw[1] || !b.db[0] != !b.db[1]))
+    return fail(DPAR_ERR_INVALID_ARG, "%s: the gradients of one projection "
+                "without the other's", call);
+  if (db && !dw)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: bias gradients without the weights' "
+                "gradients", call);
+  static const char* names[2][4] = {{"w", "z", "dz", "dw"},
+                                    {"wg", "g", "dg", "dwg"}};
+  static const char* names2[4] = {"wu", "u", "du", "dwu"};
+  const char* const* n1 = names[gated];
+  Mat m[14] = {
+      {gated ? "dh" : "dy", b.dy, o.rows, o.out, o.ldy, e, false, false, true},
+      {"x", b.x, o.rows, o.in, o.ldx, e, false, false, dw},
+      {n1[0], b.w[0], o.out, o.in, o.ldw, e, false, false, dx},
+      {names2[0], b.w[1], o.out, o.in, o.ldw, e, false, false, dx && gated},
+      {n1[1], b.z[0], o.rows, o.out, o.ldz, e, false, false, slope},
+      {names2[1], b.z[1], o.rows, o.out, o.ldz, e, false, false, gated},
+      {n1[2], in_array(b.dz[0]), o.rows, o.out, o.ldz, e, true, false, slope},
+      {names2[2], in_array(b.dz[1]), o.rows, o.out, o.ldz, e, true, false,
+       gated},
+      {"dx", in_array(b.dx), o.rows, o.in, o.lddx, eo, true, false, dx},
+      {n1[3], in_array(b.dw[0]), o.out, o.in, o.lddw, eo, true, false, dw},
+      {names2[3], in_array(b.dw[1]), o.out, o.in, o.lddw, eo, true, false,
+       dw && gated},
+      {gated ? "dbg" : "dbias", in_array(b.db[0]), 1, o.out, o.out, eo, true,
+       false, db},
+      {"dbu", in_array(b.db[1]), 1, o.out, o.out, eo, true, false,
+       db && gated}};
+  constexpr int kMats = 13;
+  m[6].twin[0] = b.z[0], m[6].twin[1] = b.dy;
+  if (gated) m[7].twin[0] = b.z[1];
+  if ((rc = check_mats(m, kMats, p, call))) return rc;
+  int cus;
+  if ((rc = check_workspace(call,
+                            gated ? DPAR_GATED_BACKWARD : DPAR_LINEAR_BACKWARD,
+                            t, p, o, ws, bytes, &cus)))
+    return rc;
+
+  if (slope && o.rows && o.out) {
+    SlopeArgs s = {};
+    s.rows = o.rows, s.cols = o.out, s.ldy = o.ldy, s.ldz = o.ldz;
+    s.act = o.act, s.gated = gated;
+    s.wide = m[0].aligned(p);
+    for (int k = 4; k < 8; ++k) s.wide &= m[k].aligned(p);
+    const int per = ranks_per_launch(p);
+    for (int r0 = 0; r0 < p; r0 += per) {
+      s.ranks = std::min(per, p - r0);
+      for (int k = 0; k < s.ranks; ++k) {
+        s.dy[k] = m[0].rank(r0 + k);
+        s.z[k] = m[4].rank(r0 + k);
+        s.u[k] = m[5].rank(r0 + k);
+        s.dz[k] = (void*)m[6].rank(r0 + k);
+        s.du[k] = (void*)m[7].rank(r0 + k);
+      }
+      if ((rc = launched(call, dpar::products::launch_slope(t, s, stream))))
+        return rc;
+    }
+  }
+  // with no activation the products read dy itself
+  const Mat& d0 = slope ? m[6] : m[0];
+  const Mat& d1 = m[7];
+  if (dx && o.rows && o.in) {
+    Args a = {};
+    a.ni = o.rows, a.nj = o.in, a.nc = o.out;
+    a.lda = d0.ld, a.ldb = o.ldw, a.ldo = o.lddx;
+    a.pairs = pairs, a.out32 = eo == 4;
+    a.fast = d0.aligned(p) && d1.aligned(p) && m[2].aligned(p) &&
+             m[3].aligned(p) && o.out * e % 16 == 0 && o.in * e % 16 == 0 &&
+             o.out;
+    a.wide_out = m[8].aligned(p);
+    rc = run_product(call, Form::DX, t, p, &a, ws, cus, stream,
+                     [&](int k, int i) {
+                       a.a[0][k] = d0.rank(i);
+                       a.a[1][k] = d1.rank(i);
+                       a.b[0][k] = m[2].rank(i);
+                       a.b[1][k] = m[3].rank(i);
+                       a.o[0][k] = (void*)m[8].rank(i);
+                     });
+    if (rc) return rc;
+  }
+  if (dw && o.out && (o.in || db)) {
+    Args a = {};
+    a.ni = o.out, a.nj = o.in, a.nc = o.rows;
+    a.lda = d0.ld, a.ldb = o.ldx, a.ldo = o.lddw;
+    a.pairs = pairs, a.out32 = eo == 4;
+    a.fast = d0.aligned(p) && d1.aligned(p) && m[1].aligned(p) &&
+             o.out * e % 16 == 0 && o.in * e % 16 == 0 && o.in && o.rows;
+    a.wide_out = m[9].aligned(p) && m[10].aligned(p);
+    rc = run_product(call, Form::DW, t, p, &a, ws, cus, stream,
+                     [&](int k, int i) {
+                       a.a[0][k] = d0.rank(i);
+                       a.a[1][k] = d1.rank(i);
+                       a.b[0][k] = m[1].rank(i);
+                       a.o[0][k] = (void*)m[9].rank(i);
+                       a.o[1][k] = (void*)m[10].rank(i);
+                       a.u[0][k] = (void*)m[11].rank(i);
+                       a.u[1][k] = (void*)m[12].rank(i);
+                     });
+    if (rc) return rc;
+  }
+  return DPAR_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dpar_linear(const void* const* x, const void* const* w,
+                const void* const* bias, const void* const* residual,
+                void* const* y, void* const* z, int p,
+                const dpar_product_t* opt, void* workspace,
+                size_t workspace_bytes, hipStream_t stream) {
+  return guarded("dpar_linear", [&] {
+    return linear_impl(x, w, bias, residual, y, z, p, opt, workspace,
+                       workspace_bytes, stream);
+  });
+}
+
+int dpar_linear_backward(const void* const* dy, const void* const* x,
+                         const void* const* w, const void* const* z,
+                         void* const* dx, void* const* dw, void* const* dbias,
+                         void* const* dz, int p, const dpar_product_t* opt,
+                         void* workspace, size_t workspace_bytes,
+                         hipStream_t stream) {
+  return guarded("dpar_linear_backward", [&] {
+    const Back b = {dy, x, {w, nullptr}, {z, nullptr}, dx, {dw, nullptr},
+                    {dbias, nullptr}, {dz, nullptr}};
+    return backward_impl("dpar_linear_backward", 1, b, p, opt, workspace,
+                         workspace_bytes, stream);
+  });
+}
+
+int dpar_gated(const void* const* x, const void* const* wg,
+               const void* const* wu, const void* const* bg,
+               const void* const* bu, void* const* h, void* const* g,
+               void* const* u, int p, const dpar_product_t* opt,
+               void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return guarded("dpar_gated", [&] {
+    return gated_impl(x, wg, wu, bg, bu, h, g, u, p, opt, workspace,
+                      workspace_bytes, stream);
+  });
+}
+
+int dpar_gated_backward(const void* const* dh, const void* const* x,
+                        const void* const* wg, const void* const* wu,
+                        const void* const* g, const void* const* u,
+                        void* const* dx, void* const* dwg, void* const* dwu,
+                        void* const* dbg, void* const* dbu, void* const* dg,
+                        void* const* du, int p, const dpar_product_t* opt,
+                        void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  return guarded("dpar_gated_backward", [&] {
+    const Back b = {dh, x, {wg, wu}, {g, u}, dx, {dwg, dwu}, {dbg, dbu},
+                    {dg, du}};
+    return backward_impl("dpar_gated_backward", 2, b, p, opt, workspace,
+                         workspace_bytes, stream);
+  });
+}
+
+int dpar_product_workspace(dpar_product_call_t call, int p,
+                           const dpar_product_t* opt, size_t* bytes) {
+  return guarded("dpar_product_workspace", [&] {
+    const char* name = "dpar_product_workspace";
+    dpar_product_t o;
+    Type t;
+    size_t e, eo;
+    const int rc = check_options(name, p, opt, &o, &t, &e, &eo);
+    if (rc) return rc;
+    if ((int)call < DPAR_LINEAR || (int)call > DPAR_GATED_BACKWARD)
+      return fail(DPAR_ERR_INVALID_ARG, "%s: unknown call %d", name,
+                  (int)call);
+    if (!bytes) return fail(DPAR_ERR_INVALID_ARG, "%s: null result", name);
+    *bytes = workspace_of(call, t, p, o, cu_count());
+    return (int)DPAR_SUCCESS;
+  });
+}
+
+}  // extern "C"

@@ -24,15 +24,21 @@ DPAR_ERR_NOMEM = -4
 DPAR_ERR_HIP = -5
 DPAR_ERR_TIMEOUT = -6
 
-DPAR_INT32, DPAR_FLOAT32, DPAR_U32_MAT2X2 = 0, 1, 2
+DPAR_INT32, DPAR_FLOAT32, DPAR_U32_MAT2X2, DPAR_BFLOAT16, DPAR_FLOAT16 = \
+    0, 1, 2, 3, 4
 DPAR_SUM, DPAR_MAX, DPAR_MATMUL = 0, 1, 2
 DPAR_EXEC_AUTO, DPAR_EXEC_LAUNCH_PER_ROUND, DPAR_EXEC_GRID_BARRIER, \
     DPAR_EXEC_TICKET, DPAR_EXEC_SPLIT, DPAR_EXEC_ROUNDS, \
     DPAR_EXEC_ROUNDS_BARRIER = 0, 1, 2, 3, 4, 5, 6
 DPAR_ALG_DUAL_ROOT, DPAR_ALG_SINGLE_TREE, DPAR_ALG_REDUCE_BCAST = 0, 1, 2
 
+DPAR_ACT_NONE, DPAR_ACT_RELU, DPAR_ACT_GELU, DPAR_ACT_GELU_TANH, \
+    DPAR_ACT_SILU = 0, 1, 2, 3, 4
+DPAR_LINEAR, DPAR_LINEAR_BACKWARD, DPAR_GATED, DPAR_GATED_BACKWARD = 0, 1, 2, 3
+
 DTYPES = {"int32": DPAR_INT32, "float32": DPAR_FLOAT32,
-          "u32mat2x2": DPAR_U32_MAT2X2}
+          "u32mat2x2": DPAR_U32_MAT2X2, "bfloat16": DPAR_BFLOAT16,
+          "float16": DPAR_FLOAT16}
 OPS = {"sum": DPAR_SUM, "max": DPAR_MAX, "matmul": DPAR_MATMUL}
 EXECS = {"auto": DPAR_EXEC_AUTO, "launch": DPAR_EXEC_LAUNCH_PER_ROUND,
          "barrier": DPAR_EXEC_GRID_BARRIER, "ticket": DPAR_EXEC_TICKET,
@@ -40,6 +46,11 @@ EXECS = {"auto": DPAR_EXEC_AUTO, "launch": DPAR_EXEC_LAUNCH_PER_ROUND,
          "rounds_barrier": DPAR_EXEC_ROUNDS_BARRIER}
 ALGS = {"dual": DPAR_ALG_DUAL_ROOT, "single": DPAR_ALG_SINGLE_TREE,
         "reduce_bcast": DPAR_ALG_REDUCE_BCAST}
+
+ACTS = {"none": DPAR_ACT_NONE, "relu": DPAR_ACT_RELU, "gelu": DPAR_ACT_GELU,
+        "gelu_tanh": DPAR_ACT_GELU_TANH, "silu": DPAR_ACT_SILU}
+PRODUCTS = {"linear": DPAR_LINEAR, "linear_backward": DPAR_LINEAR_BACKWARD,
+            "gated": DPAR_GATED, "gated_backward": DPAR_GATED_BACKWARD}
 
 
 class DparError(RuntimeError):
@@ -65,6 +76,16 @@ class dpar_schedule_t(ctypes.Structure):
                 ("nquanta", ctypes.c_size_t), ("tail_elems", ctypes.c_size_t),
                 ("chunks_per_block", ctypes.c_int), ("height", ctypes.c_int),
                 ("waves_per_chunk", ctypes.c_int)]
+
+
+class dpar_product_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_size_t), ("in_", ctypes.c_size_t),
+                ("out", ctypes.c_size_t), ("dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("act", ctypes.c_int),
+                ("ldx", ctypes.c_size_t), ("ldw", ctypes.c_size_t),
+                ("ldy", ctypes.c_size_t), ("ldr", ctypes.c_size_t),
+                ("ldz", ctypes.c_size_t), ("lddx", ctypes.c_size_t),
+                ("lddw", ctypes.c_size_t)]
 
 
 _lib = None
@@ -97,6 +118,13 @@ def lib():
                                     ctypes.POINTER(sz), ctypes.POINTER(sz)]
     L.dpar_check_status.argtypes = [vp]
     L.dpar_set_phase_event.argtypes = [vp]
+    opt = ctypes.POINTER(dpar_product_t)
+    tail = [i, opt, vp, sz, vp]     # p, options, workspace, bytes, stream
+    L.dpar_linear.argtypes = [vp] * 6 + tail
+    L.dpar_linear_backward.argtypes = [vp] * 8 + tail
+    L.dpar_gated.argtypes = [vp] * 8 + tail
+    L.dpar_gated_backward.argtypes = [vp] * 13 + tail
+    L.dpar_product_workspace.argtypes = [i, i, opt, ctypes.POINTER(sz)]
     L.dpar_last_error.restype = ctypes.c_char_p
     L.dpar_last_error.argtypes = []
     L.dpar_finalize.argtypes = []
@@ -106,7 +134,9 @@ def lib():
                  "dpar_schedule_rounds", "dpar_block_rule", "dpar_rounds",
                  "dpar_schedule_info", "dpar_block_bounds",
                  "dpar_check_status", "dpar_finalize",
-                 "dpar_set_phase_event"):
+                 "dpar_set_phase_event", "dpar_linear",
+                 "dpar_linear_backward", "dpar_gated", "dpar_gated_backward",
+                 "dpar_product_workspace"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -255,6 +285,63 @@ def dpar_set_phase_event(event):
     else:
         h = ctypes.c_void_p(int(event))
     return _check(lib().dpar_set_phase_event(h))
+
+
+# ---------------------------------------------------------- layer products
+
+def product_options(rows, n_in, n_out, dtype, out_dtype=None, act="none",
+                    ldx=0, ldw=0, ldy=0, ldr=0, ldz=0, lddx=0, lddw=0):
+    """Sizes, types and row distances of a layer product (dpar_product_t), to
+    be kept and passed to any number of calls."""
+    dt = _enum(DTYPES, dtype)
+    return dpar_product_t(rows, n_in, n_out, dt,
+                          dt if out_dtype is None else _enum(DTYPES, out_dtype),
+                          _enum(ACTS, act), ldx, ldw, ldy, ldr, ldz, lddx,
+                          lddw)
+
+
+def dpar_product_workspace(call, p, opt):
+    out = ctypes.c_size_t()
+    _check(lib().dpar_product_workspace(_enum(PRODUCTS, call), int(p),
+                                        ctypes.byref(opt), ctypes.byref(out)))
+    return out.value
+
+
+def _product(fn, arrays, p, opt, workspace, workspace_bytes, stream):
+    if workspace is not None and not isinstance(workspace, int):
+        workspace = workspace.data_ptr()
+    return _check(fn(
+        *[a if a is None or isinstance(a, ctypes.Array) else _ptr_array(a)
+          for a in arrays],
+        p, ctypes.byref(opt), workspace, workspace_bytes, _stream(stream)))
+
+
+def dpar_linear(x, w, bias, residual, y, z, p, opt, workspace=None,
+                workspace_bytes=0, stream=None):
+    """Sequences of p device addresses (ints or tensors; 0 where a rank has no
+    bias or residual), or None where optional; opt: product_options()."""
+    return _product(lib().dpar_linear, (x, w, bias, residual, y, z), p, opt,
+                    workspace, workspace_bytes, stream)
+
+
+def dpar_linear_backward(dy, x, w, z, dx, dw, dbias, dz, p, opt,
+                         workspace=None, workspace_bytes=0, stream=None):
+    return _product(lib().dpar_linear_backward,
+                    (dy, x, w, z, dx, dw, dbias, dz), p, opt, workspace,
+                    workspace_bytes, stream)
+
+
+def dpar_gated(x, wg, wu, bg, bu, h, g, u, p, opt, workspace=None,
+               workspace_bytes=0, stream=None):
+    return _product(lib().dpar_gated, (x, wg, wu, bg, bu, h, g, u), p, opt,
+                    workspace, workspace_bytes, stream)
+
+
+def dpar_gated_backward(dh, x, wg, wu, g, u, dx, dwg, dwu, dbg, dbu, dg, du, p,
+                        opt, workspace=None, workspace_bytes=0, stream=None):
+    return _product(lib().dpar_gated_backward,
+                    (dh, x, wg, wu, g, u, dx, dwg, dwu, dbg, dbu, dg, du), p,
+                    opt, workspace, workspace_bytes, stream)
 
 
 def dpar_last_error():
