@@ -21,7 +21,8 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-result",
 ]
-HIP_SOURCES = ["kernels.hip", "products.hip"]
+HIP_SOURCES = ["kernels.hip", "products_bf16.hip", "products_f16.hip",
+               "products_f32.hip"]
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
               "-Wno-unused-parameter", "-D__HIP_PLATFORM_AMD__"]
 

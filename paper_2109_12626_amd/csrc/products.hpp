@@ -45,16 +45,11 @@ struct Args {
   int act;
   int out32;                 // result in 32 bits
   int splits;                // parts of the contraction
+  int tile;                  // 64 << tile rows and columns per workgroup
   int fast;                  // A, B: 16-byte rows and whole 16-byte pieces
   int wide_out;              // results, kept values, residual, bias: 16-byte
                              // pieces
 };
-
-// Bytes of workspace that a launch of this form takes (0: none).
-size_t part_bytes(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
-                  size_t nc, int cus, int* splits);
-
-hipError_t launch(Form f, Type t, const Args& a, hipStream_t stream);
 
 // dz = dy act'(z) (gated == 0), or dg = dy u act'(g), du = dy act(g).
 struct SlopeArgs {
@@ -66,7 +61,14 @@ struct SlopeArgs {
   size_t rows, cols, ldy, ldz;
   int ranks, act, gated, wide;
 };
-hipError_t launch_slope(Type t, const SlopeArgs& a, hipStream_t stream);
+
+// One source file per type.
+hipError_t launch_bf16(Form f, const Args& a, hipStream_t stream);
+hipError_t launch_f16(Form f, const Args& a, hipStream_t stream);
+hipError_t launch_f32(Form f, const Args& a, hipStream_t stream);
+hipError_t launch_slope_bf16(const SlopeArgs& a, hipStream_t stream);
+hipError_t launch_slope_f16(const SlopeArgs& a, hipStream_t stream);
+hipError_t launch_slope_f32(const SlopeArgs& a, hipStream_t stream);
 
 }  // namespace products
 }  // namespace dpar

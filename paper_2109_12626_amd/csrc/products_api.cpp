@@ -141,6 +141,9 @@ int check_mats(const Mat* mats, int n, int p, const char* call) {
   return check_alias(mats, n, p, call);
 }
 
+// 256 rows of an operand lie within the kernels' 32-bit offsets (the fast
+// loads; others use 64-bit addresses throughout).
+constexpr size_t kFastPitch = (size_t)1 << 23;
 constexpr size_t kMost = (size_t)1 << 31;     // rows, in, out
 constexpr size_t kMostPitch = (size_t)1 << 38;
 
@@ -199,6 +202,26 @@ int ranks_per_launch(int p) {
   return (p + n - 1) / n;
 }
 
+// How a product runs.
+struct Shape {
+  int tile, splits;
+  size_t part;           // bytes of workspace
+};
+
+Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
+               size_t nc, int cus) {
+  // the largest tiles that still give every CU one
+  auto count = [&](size_t bm, size_t bn) {
+    return (ni + bm - 1) / bm * ((nj + bn - 1) / bn) * ranks *
+           (f == Form::DW ? pairs : 1);
+  };
+  const int half = f == Form::GATED ? 2 : 1;
+  int tile = 0;
+  if (count(128, 128 / half) >= (size_t)cus) tile = 1;
+  if (t != Type::F32 && count(256, 256 / half) >= (size_t)cus) tile = 2;
+  return {tile, 1, 0};
+}
+
 struct Step {
   Form form;
   int pairs;
@@ -230,12 +253,10 @@ size_t workspace_of(dpar_product_call_t call, Type t, int p,
   Step s[2];
   const int n = steps_of(call, o, true, true, s);
   size_t most = 0;
-  for (int k = 0; k < n; ++k) {
-    int splits;
-    most = std::max(most, dpar::products::part_bytes(
-                              s[k].form, t, ranks_per_launch(p), s[k].pairs,
-                              s[k].ni, s[k].nj, s[k].nc, cus, &splits));
-  }
+  for (int k = 0; k < n; ++k)
+    most = std::max(most, shape_of(s[k].form, t, ranks_per_launch(p),
+                                   s[k].pairs, s[k].ni, s[k].nj, s[k].nc,
+                                   cus).part);
   return most;
 }
 
@@ -264,16 +285,20 @@ template <typename Fill>
 int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
                 int cus, hipStream_t stream, Fill fill) {
   const int per = ranks_per_launch(p);
-  int splits = 1;
-  if (ws)
-    dpar::products::part_bytes(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
-                               &splits);
-  a->splits = splits;
+  const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus);
+  a->tile = s.tile;
+  a->splits = ws ? s.splits : 1;
   a->part = (float*)ws;
   for (int r0 = 0; r0 < p; r0 += per) {
     a->ranks = std::min(per, p - r0);
     for (int k = 0; k < a->ranks; ++k) fill(k, r0 + k);
-    const int rc = launched(call, dpar::products::launch(f, t, *a, stream));
+    hipError_t e;
+    switch (t) {
+      case Type::BF16: e = dpar::products::launch_bf16(f, *a, stream); break;
+      case Type::F16: e = dpar::products::launch_f16(f, *a, stream); break;
+      default: e = dpar::products::launch_f32(f, *a, stream);
+    }
+    const int rc = launched(call, e);
     if (rc) return rc;
   }
   return DPAR_SUCCESS;
@@ -321,7 +346,8 @@ int linear_impl(const void* const* x, const void* const* w,
   a.ni = o.rows, a.nj = o.out, a.nc = o.in;
   a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz, a.lde = o.ldr;
   a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
-  a.fast = m[0].aligned(p) && m[1].aligned(p) && o.in * e % 16 == 0 && o.in;
+  a.fast = m[0].aligned(p) && m[1].aligned(p) && o.in * e % 16 == 0 &&
+           o.in && o.ldx < kFastPitch && o.ldw < kFastPitch;
   a.wide_out = m[2].aligned(p) && m[3].aligned(p) && m[4].aligned(p) &&
                m[5].aligned(p);
   return run_product(call, Form::LINEAR, t, p, &a, ws, cus, stream,
@@ -367,7 +393,8 @@ int gated_impl(const void* const* x, const void* const* wg,
   a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz;
   a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
   a.fast = m[0].aligned(p) && m[1].aligned(p) && m[2].aligned(p) &&
-           o.in * e % 16 == 0 && o.in;
+           o.in * e % 16 == 0 && o.in && o.ldx < kFastPitch &&
+           o.ldw < kFastPitch;
   a.wide_out = m[3].aligned(p) && m[4].aligned(p) && m[5].aligned(p) &&
                m[6].aligned(p) && m[7].aligned(p);
   return run_product(call, Form::GATED, t, p, &a, ws, cus, stream,
@@ -461,8 +488,13 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
         s.dz[k] = (void*)m[6].rank(r0 + k);
         s.du[k] = (void*)m[7].rank(r0 + k);
       }
-      if ((rc = launched(call, dpar::products::launch_slope(t, s, stream))))
-        return rc;
+      hipError_t e;
+      switch (t) {
+        case Type::BF16: e = dpar::products::launch_slope_bf16(s, stream); break;
+        case Type::F16: e = dpar::products::launch_slope_f16(s, stream); break;
+        default: e = dpar::products::launch_slope_f32(s, stream);
+      }
+      if ((rc = launched(call, e))) return rc;
     }
   }
   // with no activation the products read dy itself
@@ -475,7 +507,7 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
     a.pairs = pairs, a.out32 = eo == 4;
     a.fast = d0.aligned(p) && d1.aligned(p) && m[2].aligned(p) &&
              m[3].aligned(p) && o.out * e % 16 == 0 && o.in * e % 16 == 0 &&
-             o.out;
+             o.out && d0.ld < kFastPitch && o.ldw < kFastPitch;
     a.wide_out = m[8].aligned(p);
     rc = run_product(call, Form::DX, t, p, &a, ws, cus, stream,
                      [&](int k, int i) {
@@ -493,7 +525,8 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
     a.lda = d0.ld, a.ldb = o.ldx, a.ldo = o.lddw;
     a.pairs = pairs, a.out32 = eo == 4;
     a.fast = d0.aligned(p) && d1.aligned(p) && m[1].aligned(p) &&
-             o.out * e % 16 == 0 && o.in * e % 16 == 0 && o.in && o.rows;
+             o.out * e % 16 == 0 && o.in * e % 16 == 0 && o.in && o.rows &&
+             d0.ld < kFastPitch && o.ldx < kFastPitch;
     a.wide_out = m[9].aligned(p) && m[10].aligned(p);
     rc = run_product(call, Form::DW, t, p, &a, ws, cus, stream,
                      [&](int k, int i) {

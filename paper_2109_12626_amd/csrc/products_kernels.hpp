@@ -1,5 +1,7 @@
 // Layer products on gfx950's matrix cores: one tiled kernel for every form
 // (products.hpp), types bf16, fp16 and fp32, results accumulated in fp32.
+#pragma once
+
 #include <hip/hip_runtime.h>
 
 #include "products.hpp"
@@ -15,6 +17,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 #define LDS __attribute__((address_space(3)))
+
+// The arguments as the kernel finds them: read in place with scalar loads
+// (indexing a by-value copy by rank would put all of it in scratch memory).
+using Given = const __attribute__((address_space(4))) Args;
+using GivenSlope = const __attribute__((address_space(4))) SlopeArgs;
 
 // A piece is 16 bytes; every tile holds 128 bytes of the contraction: 64
 // 16-bit or 32 32-bit values, in two steps of 4 pieces (one per lane group
@@ -155,9 +162,36 @@ __device__ inline i32x4 load_piece(const V* p, long n) {
   return v;
 }
 
-__device__ inline void dma16(const void* g, LDS void* l) {
-  __builtin_amdgcn_global_load_lds(
-      (const __attribute__((address_space(1))) void*)g, l, 16, 0, 0);
+// Sixteen bytes per lane straight from memory to LDS, lane after lane from
+// `lds` on (the same address in the whole wavefront).  Written as assembly so
+// that the compiler does not wait for them before every LDS read: the kernel
+// waits itself (landed()) before the barrier that publishes a tile.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0: set before every use
+__device__ inline void dma16(uint32_t lds, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ inline void dma16_at(uint32_t lds, const void* p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, off"
+               :: "s"(lds), "v"(p) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int LEFT>
+__device__ inline void landed() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(LEFT) : "memory");
+}
+
+// A value that is the same in every lane, in scalar registers.
+__device__ inline uint32_t uniform(uint32_t v) {
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ inline const char* uniform(const char* p) {
+  const uint64_t v = (uint64_t)p;
+  return (const char*)((uint64_t)uniform((uint32_t)(v >> 32)) << 32 |
+                       uniform((uint32_t)v));
 }
 
 // One operand's tile: W rows (CC) or W values of every contraction step (RC).
@@ -176,29 +210,35 @@ struct Operand {
     *val = ((o % P) ^ key_of<T, CC, W, G>(*row)) * E;
   }
 
-  // The address of a piece, g_zero past the contraction's end; rows and
-  // values past the operand's end give the last ones (their results are not
-  // stored).  Whole pieces only (fast operands).
-  static __device__ const void* source(const V* base, size_t ld, size_t i0,
-                                       size_t ni, size_t c0, size_t nc, int n,
-                                       int t, bool tail) {
+  // Byte offset of a piece from the tile's first value at contraction 0.
+  // Rows and values past the operand's end give the last ones (their results
+  // are not stored).  Whole pieces only (fast operands).
+  static __device__ uint32_t offset(size_t ld, size_t i0, size_t ni, int n,
+                                    int t) {
     int row, val;
     at(n, t, &row, &val);
-    size_t i, c;
+    const size_t most = ni - i0;        // i0 < ni
     if (CC) {
-      i = i0 + row;
-      c = c0 + val;
-      if (i >= ni) i = ni - 1;
-      if (tail && c >= nc) return &g_zero;
-      return base + i * ld + c;
+      if ((size_t)row >= most) row = (int)most - 1;
+      return (uint32_t)(((size_t)row * ld + val) * sizeof(V));
     }
-    c = c0 + row;
-    i = i0 + val;
-    if (i >= ni) i = ni - E;
-    if (tail && c >= nc) return &g_zero;
-    return base + c * ld + i;
+    if ((size_t)val >= most) val = (int)most - E;
+    return (uint32_t)(((size_t)row * ld + val) * sizeof(V));
   }
-
+  // Bytes from one contraction tile to the next, and to the tile's first
+  // value.
+  static __device__ size_t step(size_t ld) {
+    return CC ? (size_t)kLine : (size_t)KT * ld * sizeof(V);
+  }
+  static __device__ size_t origin(size_t ld, size_t i0) {
+    return (CC ? i0 * ld : i0) * sizeof(V);
+  }
+  // Whether a piece lies past the contraction's end (the last tile only).
+  static __device__ bool past(size_t c0, size_t nc, int n, int t) {
+    int row, val;
+    at(n, t, &row, &val);
+    return c0 + (CC ? val : row) >= nc;
+  }
   // The same for any alignment and length, into registers.
   static __device__ i32x4 fetch(const V* base, size_t ld, size_t i0, size_t ni,
                                 size_t c0, size_t nc, int n, int t) {
@@ -262,8 +302,10 @@ template <typename V, int N>
 __device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
   constexpr int E = 16 / sizeof(V);
   if (wide && left >= N) {
+#pragma unroll
     for (int k = 0; k < N; k += E) {
       V t[E];
+#pragma unroll
       for (int e = 0; e < E; ++e) t[e] = (V)v[k + e];
       i32x4 w;
       __builtin_memcpy(&w, t, 16);
@@ -271,6 +313,7 @@ __device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
     }
     return;
   }
+#pragma unroll
   for (int k = 0; k < N; ++k)
     if (k < left) p[k] = (V)v[k];
 }
@@ -279,14 +322,17 @@ template <typename V, int N>
 __device__ inline void fetch_vals(const V* p, float* v, long left, bool wide) {
   constexpr int E = 16 / sizeof(V);
   if (wide && left >= N) {
+#pragma unroll
     for (int k = 0; k < N; k += E) {
       const i32x4 w = *(const i32x4*)(p + k);
       V t[E];
       __builtin_memcpy(t, &w, 16);
+#pragma unroll
       for (int e = 0; e < E; ++e) v[k + e] = (float)t[e];
     }
     return;
   }
+#pragma unroll
   for (int k = 0; k < N; ++k) v[k] = k < left ? (float)p[k] : 0.f;
 }
 
@@ -307,7 +353,7 @@ __device__ inline void store_out(void* o, size_t at, const float* v, long left,
 // N consecutive values j .. of row i: bias, activation, residual, rounding,
 // stores.  v: the product's sums (GATED: v of g, u2 of u).
 template <Type T, Form F, int N>
-__device__ inline void finish(const Args& a, int rank, int pair, size_t i,
+__device__ inline void finish(Given& a, int rank, int pair, size_t i,
                               size_t j, float* v, float* u2) {
   using V = typename Elem<T>::V;
   const long left = (long)a.nj - (long)j;
@@ -316,11 +362,13 @@ __device__ inline void finish(const Args& a, int rank, int pair, size_t i,
     if (const V* b = (const V*)a.e[0][rank]) {
       float t[N];
       fetch_vals<V, N>(b + j, t, left, wide);
+#pragma unroll
       for (int k = 0; k < N; ++k) v[k] += t[k];
     }
     if (V* z = (V*)a.o[1][rank])
       store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
     if (a.act)
+#pragma unroll
       for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]);
     if (const void* r = a.e[1][rank]) {
       float t[N];
@@ -328,6 +376,7 @@ __device__ inline void finish(const Args& a, int rank, int pair, size_t i,
         fetch_vals<float, N>((const float*)r + i * a.lde + j, t, left, wide);
       else
         fetch_vals<V, N>((const V*)r + i * a.lde + j, t, left, wide);
+#pragma unroll
       for (int k = 0; k < N; ++k) v[k] += t[k];
     }
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
@@ -335,16 +384,19 @@ __device__ inline void finish(const Args& a, int rank, int pair, size_t i,
     float t[N];
     if (const V* b = (const V*)a.e[0][rank]) {
       fetch_vals<V, N>(b + j, t, left, wide);
+#pragma unroll
       for (int k = 0; k < N; ++k) v[k] += t[k];
     }
     if (const V* b = (const V*)a.e[1][rank]) {
       fetch_vals<V, N>(b + j, t, left, wide);
+#pragma unroll
       for (int k = 0; k < N; ++k) u2[k] += t[k];
     }
     if (V* g = (V*)a.o[1][rank])
       store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
     if (V* u = (V*)a.u[0][rank])
       store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
+#pragma unroll
     for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]) * u2[k];
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else {
@@ -373,7 +425,7 @@ struct Tiled {
   static constexpr int KT = OA::KT;
   static constexpr int kBytesA = BM * kLine, kBytes = (BM + BN) * kLine;
 
-  static __device__ void run(const Args& a, LDS char* lds) {
+  static __device__ void run(Given& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int wm = wave / (BN / WN), wn = wave % (BN / WN);
     // (weights' gradients without columns still have bias sums)
@@ -383,69 +435,94 @@ struct Tiled {
     // neighbouring tiles so that they share operands in its L2
     unsigned id = blockIdx.x;
     {
-      const unsigned n = gridDim.x, per = n / 8, rest = n % 8;
+      const unsigned n = gridDim.x, per = n / 8, more = n % 8;
       const unsigned x = id % 8, k = id / 8;
-      id = x * per + (x < rest ? x : rest) + k;
+      id = x * per + (x < more ? x : more) + k;
     }
-    const size_t tiles = mt * nt;
-    const int split = id % a.splits;
-    unsigned r1 = id / a.splits;
-    size_t tile = r1 % tiles;
-    r1 /= (unsigned)tiles;
-    const int pair = F == Form::DW ? r1 % a.pairs : 0;
-    const int rank = F == Form::DW ? r1 / a.pairs : r1;
+    // (the host keeps the number of workgroups below 2^31)
+    const unsigned tiles = (unsigned)mt * (unsigned)nt;
+    const unsigned split = uniform(id % a.splits);
+    unsigned rest = id / a.splits;
+    const unsigned tile = rest % tiles;
+    rest = uniform(rest / tiles);
+    const int pair = F == Form::DW ? rest % a.pairs : 0;
+    const int rank = F == Form::DW ? rest / a.pairs : rest;
     // groups of 8 tile rows, columns inside
-    const size_t grp = tile / (8 * nt), first = grp * 8;
-    const size_t high = mt - first < 8 ? mt - first : 8;
-    const size_t in = tile % (8 * nt);
-    const size_t i0 = (first + in % high) * BM, j0 = in / high * BJ;
+    const unsigned row8 = tile / (8 * (unsigned)nt), in = tile % (8 * (unsigned)nt);
+    const unsigned left = (unsigned)mt - row8 * 8, high = left < 8 ? left : 8;
+    const size_t i0 = (size_t)uniform(row8 * 8 + in % high) * BM,
+                 j0 = (size_t)uniform(in / high) * BJ;
 
     const size_t nk1 = (a.nc + KT - 1) / KT;
     const size_t nk = F == Form::DX ? nk1 * a.pairs : nk1;
     const size_t k0 = nk * split / a.splits, k1 = nk * (split + 1) / a.splits;
 
     f32x4 acc[MI][NJ] = {};
-    f32x4 sum[F == Form::DW ? MI : 1] = {};
+    f32x4 sum = {};
     const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0 && wn == 0;
 
+    // addresses: a 64-bit base per operand and contraction tile (scalar), a
+    // 32-bit offset per piece
+    uint32_t va[FAST ? OA::N : 1], vb[FAST ? OB::N : 1];
     i32x4 ra[FAST ? 1 : OA::N], rb[FAST ? 1 : OB::N];
+    if constexpr (FAST) {
+#pragma unroll
+      for (int n = 0; n < OA::N; ++n)
+        va[n] = OA::offset(a.lda, i0, a.ni, n, t);
+      // (GATED: the tile's second half holds u's rows, from j0 again)
+#pragma unroll
+      for (int n = 0; n < OB::N; ++n)
+        vb[n] = kGated ? OB::offset(a.ldb, j0, a.nj, n % (OB::N / 2), t)
+                       : OB::offset(a.ldb, j0, a.nj, n, t);
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds +
+                          uniform(wave) * 1024;
 
-    auto bases = [&](size_t kt, const V** pa, const V** pb, const V** pb2,
-                     size_t* c0) {
-      const int s = F == Form::DX ? (kt >= nk1) : pair;
-      *c0 = (F == Form::DX ? kt - s * nk1 : kt) * KT;
-      *pa = (const V*)a.a[s][rank];
-      *pb = (const V*)a.b[kGated ? 0 : (F == Form::DW ? 0 : s)][rank];
-      *pb2 = kGated ? (const V*)a.b[1][rank] : *pb;
-    };
+    // Loads contraction tile kt: FAST into LDS, else into registers.
     auto issue = [&](size_t kt, int buf) {
-      const V *pa, *pb, *pb2;
-      size_t c0;
-      bases(kt, &pa, &pb, &pb2, &c0);
-      const bool tail = c0 + KT > a.nc;
-      LDS char* d = lds + buf * kBytes + wave * 1024;
+      const int s = F == Form::DX ? (kt >= nk1) : pair;
+      const size_t c = F == Form::DX && s ? kt - nk1 : kt;
+      const char* pa = (const char*)a.a[s][rank];
+      const char* pb =
+          (const char*)a.b[kGated || F == Form::DW ? 0 : s][rank];
+      const char* pu = kGated ? (const char*)a.b[1][rank] : pb;
       if constexpr (FAST) {
+        pa += OA::origin(a.lda, i0) + c * OA::step(a.lda);
+        const size_t ob = OB::origin(a.ldb, j0) + c * OB::step(a.ldb);
+        pa = uniform(pa);
+        pu = uniform(pu + ob);
+        pb = uniform(pb + ob);
+        const uint32_t d = lds0 + buf * kBytes;
+        if (c * KT + KT <= a.nc) {
 #pragma unroll
-        for (int n = 0; n < OA::N; ++n)
-          dma16(OA::source(pa, a.lda, i0, a.ni, c0, a.nc, n, t, tail),
-                d + n * kThreads * 16);
-        d += kBytesA;
+          for (int n = 0; n < OA::N; ++n)
+            dma16(d + n * kThreads * 16, pa, va[n]);
 #pragma unroll
-        for (int n = 0; n < OB::N; ++n) {
-          const bool up = kGated && n >= OB::N / 2;
-          dma16(OB::source(up ? pb2 : pb, a.ldb,
-                           up ? j0 - BJ : j0, a.nj, c0, a.nc, n, t, tail),
-                d + n * kThreads * 16);
+          for (int n = 0; n < OB::N; ++n)
+            dma16(d + kBytesA + n * kThreads * 16,
+                  kGated && n >= OB::N / 2 ? pu : pb, vb[n]);
+        } else {
+#pragma unroll
+          for (int n = 0; n < OA::N; ++n)
+            dma16_at(d + n * kThreads * 16,
+                     OA::past(c * KT, a.nc, n, t) ? (const char*)&g_zero
+                                                  : pa + va[n]);
+#pragma unroll
+          for (int n = 0; n < OB::N; ++n)
+            dma16_at(d + kBytesA + n * kThreads * 16,
+                     OB::past(c * KT, a.nc, n, t)
+                         ? (const char*)&g_zero
+                         : (kGated && n >= OB::N / 2 ? pu : pb) + vb[n]);
         }
       } else {
 #pragma unroll
         for (int n = 0; n < OA::N; ++n)
-          ra[n] = OA::fetch(pa, a.lda, i0, a.ni, c0, a.nc, n, t);
+          ra[n] = OA::fetch((const V*)pa, a.lda, i0, a.ni, c * KT, a.nc, n, t);
 #pragma unroll
         for (int n = 0; n < OB::N; ++n) {
           const bool up = kGated && n >= OB::N / 2;
-          rb[n] = OB::fetch(up ? pb2 : pb, a.ldb, up ? j0 - BJ : j0, a.nj, c0,
-                            a.nc, n, t);
+          rb[n] = OB::fetch((const V*)(up ? pu : pb), a.ldb,
+                            up ? j0 - BJ : j0, a.nj, c * KT, a.nc, n, t);
         }
       }
     };
@@ -462,84 +539,145 @@ struct Tiled {
       }
     };
 
-    if (k0 < k1) issue(k0, 0);
+    // Two steps per tile.  While the matrix cores work on one step, the next
+    // one's fragments are read: B's into registers of their own, A's row by
+    // row into those the products have just used.  One barrier per tile,
+    // between the steps: by then every wavefront has read all of this tile,
+    // so its buffer takes the tile after next, and the next tile, asked for
+    // one tile ago, has landed.
+    i32x4 fa[MI], fb[2][NJ];
+    auto read_b = [&](int ks, int buf) {
+      LDS char* sb = lds + buf * kBytes + kBytesA;
+#pragma unroll
+      for (int n = 0; n < NJ; ++n) {
+        const int first = kGated
+            ? (n < NT ? 0 : BJ) + wn * (WN / 2) + (n % NT) * 4
+            : wn * WN + n * 4;
+        fb[ks][n] = OB::frag(sb, ks, first, lane);
+      }
+    };
+    auto read_a = [&](int m, int ks, int buf) {
+      fa[m] = OA::frag(lds + buf * kBytes, ks, wm * WM + m * 16, lane);
+    };
+    // step ks, then step ks ^ 1 of the tile in `buf`
+    auto multiply = [&](int ks, int buf) {
+      read_b(ks ^ 1, buf);
+#pragma unroll
+      for (int m = 0; m < MI; ++m) {
+#pragma unroll
+        for (int n = 0; n < NJ; ++n)
+          acc[m][n] = Elem<T>::mma(fb[ks][n], fa[m], acc[m][n]);
+        if constexpr (F == Form::DW)
+          if (sums)   // row m of `sum`: the sums of A's rows m * 16 ..
+            sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
+                               fa[m], sum);
+        read_a(m, ks ^ 1, buf);
+      }
+    };
+
+    if (k0 < k1) {
+      issue(k0, 0);
+      land(0);
+      if (k0 + 1 < k1) {
+        issue(k0 + 1, 1);
+        land(1);
+        landed<FAST ? OA::N + OB::N : 0>();
+      } else {
+        landed<0>();
+      }
+      __builtin_amdgcn_s_barrier();
+      read_b(0, 0);
+#pragma unroll
+      for (int m = 0; m < MI; ++m) read_a(m, 0, 0);
+    }
+#pragma unroll 1
     for (size_t kt = k0; kt < k1; ++kt) {
       const int buf = (kt - k0) & 1;
-      land(buf);
-      __syncthreads();
-      if (kt + 1 < k1) issue(kt + 1, buf ^ 1);
-      LDS char* sa = lds + buf * kBytes;
-      LDS char* sb = sa + kBytesA;
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        i32x4 fa[MI], fb[NJ];
-#pragma unroll
-        for (int n = 0; n < NJ; ++n) {
-          const int first = kGated
-              ? (n < NT ? 0 : BJ) + wn * (WN / 2) + (n % NT) * 4
-              : wn * WN + n * 4;
-          fb[n] = OB::frag(sb, ks, first, lane);
-        }
-#pragma unroll
-        for (int m = 0; m < MI; ++m)
-          fa[m] = OA::frag(sa, ks, wm * WM + m * 16, lane);
-#pragma unroll
-        for (int m = 0; m < MI; ++m)
-#pragma unroll
-          for (int n = 0; n < NJ; ++n)
-            acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
-        if constexpr (F == Form::DW)
-          if (sums)
-            for (int m = 0; m < MI; ++m)
-              sum[m] = Elem<T>::mma(Elem<T>::ones(), fa[m], sum[m]);
+      if (!FAST && kt + 2 < k1) issue(kt + 2, buf);
+      multiply(0, buf);
+      landed<0>();
+      __builtin_amdgcn_s_barrier();
+      if (kt + 2 < k1) {
+        if (FAST) issue(kt + 2, buf);
+        land(buf);
       }
+      // (after the last tile this reads a buffer that nothing uses any more)
+      multiply(1, buf ^ 1);
     }
 
-    // lane (r, q): row r of each 16, results q * G ... of the wave's columns
-    const int r = lane & 15, q = lane >> 4;
-    const size_t j = j0 + wn * (kGated ? WN / 2 : WN) + q * G;
+    if constexpr (F == Form::DW)
+      if (sums) {
+        // lane (r, q) holds the sums of rows r of tiles q * 4 ..
 #pragma unroll
-    for (int m = 0; m < MI; ++m) {
-      const size_t i = i0 + wm * WM + m * 16 + r;
-      if (i >= a.ni) continue;
-      float v[G], u2[kGated ? G : 1];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
         for (int e = 0; e < 4; ++e) {
-          v[n * 4 + e] = acc[m][n][e];
-          if constexpr (kGated) u2[n * 4 + e] = acc[m][n + NT][e];
-        }
-      if (F == Form::DW && sums && q == 0) {
-        if (a.splits == 1) {
-          float s = sum[m][0];
-          store_out<1>(a.u[pair][rank], i, &s, 1, a.out32, false, V());
-        } else {
-          // after all partial results: [split][rank][pair][row]
-          a.part[(size_t)a.splits * a.ranks * a.pairs * a.ni * a.nj +
-                 (((size_t)split * a.ranks + rank) * a.pairs + pair) * a.ni +
-                 i] = sum[m][0];
+          const int m = (lane >> 4) * 4 + e;
+          const size_t i = i0 + wm * WM + m * 16 + (lane & 15);
+          if (m >= MI || i >= a.ni) continue;
+          float v = sum[e];
+          if (a.splits == 1)
+            store_out<1>(a.u[pair][rank], i, &v, 1, a.out32, false, V());
+          else    // after all partial results: [split][rank][pair][row]
+            a.part[(size_t)a.splits * a.ranks * a.pairs * a.ni * a.nj +
+                   (((size_t)split * a.ranks + rank) * a.pairs + pair) * a.ni +
+                   i] = v;
         }
       }
-      if (j >= a.nj) continue;
-      if (a.splits == 1) {
-        finish<T, F, G>(a, rank, pair, i, j, v, u2);
-      } else {
-        // [split][rank][pair or projection][row][column]
-        const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
-        const size_t sz = a.ni * a.nj;
-        float* w = a.part + (((size_t)split * a.ranks + rank) * np + pair) * sz
-                   + i * a.nj + j;
-        const long left = (long)a.nj - (long)j;
-        const bool wide = a.nj % 4 == 0;
-        store_vals<float, G>(w, v, left, wide);
-        if constexpr (kGated) store_vals<float, G>(w + sz, u2, left, wide);
+
+    // Results by way of LDS (each wavefront its own part, MH of its tile rows
+    // at a time), so that 8 consecutive ones are in one lane, whole rows side
+    // by side in a store, and the code that finishes them stays short.
+    constexpr int MH = MI < 4 ? MI : 4, CH = WN / 4, PER = (kGated ? WN / 2 : WN) / 8;
+    LDS char* mine = lds + wave * (MH * 16 * WN * 4);
+    landed<0>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int mh = 0; mh < MI; mh += MH) {
+      const int r = lane & 15, q = lane >> 4;
+#pragma unroll
+      for (int m = 0; m < MH; ++m)
+#pragma unroll
+        for (int n = 0; n < NJ; ++n) {
+          // lane (r, q): row r, columns q * G + n * 4 ..; u's after g's
+          const int c = n < NT ? q * NT + n : CH / 2 + q * NT + n - NT;
+          *(LDS f32x4*)(mine + (m * 16 + r) * (WN * 4) +
+                        (c ^ (r & (CH - 1))) * 16) = acc[mh + m][n];
+        }
+#pragma unroll 1
+      for (int w = lane; w < MH * 16 * PER; w += 64) {
+        const int row = w / PER, c = w % PER * 2;
+        const size_t i = i0 + wm * WM + mh * 16 + row;
+        const size_t j = j0 + wn * (kGated ? WN / 2 : WN) + c * 4;
+        if (i >= a.ni || j >= a.nj) continue;
+        float v[8], u2[8];
+        LDS char* at = mine + row * (WN * 4);
+        const int x = row & (CH - 1);
+        *(f32x4*)v = *(LDS f32x4*)(at + (c ^ x) * 16);
+        *(f32x4*)(v + 4) = *(LDS f32x4*)(at + ((c + 1) ^ x) * 16);
+        if constexpr (kGated) {
+          *(f32x4*)u2 = *(LDS f32x4*)(at + ((CH / 2 + c) ^ x) * 16);
+          *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
+        }
+        if (a.splits == 1) {
+          finish<T, F, 8>(a, rank, pair, i, j, v, u2);
+        } else {
+          // [split][rank][pair or projection][row][column]
+          const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
+          const size_t sz = a.ni * a.nj;
+          float* p = a.part + (((size_t)split * a.ranks + rank) * np + pair)
+                     * sz + i * a.nj + j;
+          const long left = (long)a.nj - (long)j;
+          const bool wide = a.nj % 4 == 0;
+          store_vals<float, 8>(p, v, left, wide);
+          if constexpr (kGated) store_vals<float, 8>(p + sz, u2, left, wide);
+        }
       }
     }
   }
 };
 
 template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args a) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
   Tiled<T, F, FAST, BM, BN, WM, WN>::run(a, (LDS char*)lds);
 }
@@ -547,7 +685,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args a) {
 // Joins the parts of a split contraction in their order and finishes: 4
 // results per thread.
 template <Type T, Form F>
-__global__ __launch_bounds__(256) void k_join(Args a) {
+__global__ __launch_bounds__(256) void k_join(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   using V = typename Elem<T>::V;
   const size_t per = (a.nj + 3) / 4;
   const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -588,7 +727,8 @@ __global__ __launch_bounds__(256) void k_join(Args a) {
 }
 
 template <Type T, bool GATED>
-__global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
+__global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
+  GivenSlope& a = *(GivenSlope*)__builtin_amdgcn_kernarg_segment_ptr();
   using V = typename Elem<T>::V;
   constexpr int E = 16 / sizeof(V);
   const int rank = blockIdx.y;
@@ -644,13 +784,19 @@ hipError_t go(const Args& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <Type T, Form F>
+template <Type T, Form F, bool FAST>
 hipError_t pick(const Args& a, hipStream_t stream) {
-  hipError_t e;
-  if (a.fast)
-    e = go<T, F, true, 128, 128, 64, 64>(a, stream);
-  else
-    e = go<T, F, false, 128, 128, 64, 64>(a, stream);
+  if constexpr (T != Type::F32 && FAST)
+    if (a.tile == 2)
+    return go<T, F, FAST, 256, 256, 128, 64>(a, stream);
+  if (a.tile >= 1) return go<T, F, FAST, 128, 128, 64, 64>(a, stream);
+  return go<T, F, FAST, 64, 64, 32, 32>(a, stream);
+}
+
+template <Type T, Form F>
+hipError_t run_form(const Args& a, hipStream_t stream) {
+  const hipError_t e = a.fast ? pick<T, F, true>(a, stream)
+                              : pick<T, F, false>(a, stream);
   if (e != hipSuccess || a.splits == 1) return e;
   const size_t n = (a.nj + 3) / 4 * a.ni * a.ranks *
                    (F == Form::DW ? a.pairs : 1);
@@ -659,28 +805,18 @@ hipError_t pick(const Args& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <Form F>
-hipError_t by_type(Type t, const Args& a, hipStream_t stream) {
-  switch (t) {
-    case Type::BF16: return pick<Type::BF16, F>(a, stream);
-    case Type::F16: return pick<Type::F16, F>(a, stream);
-    default: return pick<Type::F32, F>(a, stream);
-  }
-}
-
-}  // namespace
-
-hipError_t launch(Form f, Type t, const Args& a, hipStream_t stream) {
+template <Type T>
+hipError_t run_type(Form f, const Args& a, hipStream_t stream) {
   switch (f) {
-    case Form::LINEAR: return by_type<Form::LINEAR>(t, a, stream);
-    case Form::GATED: return by_type<Form::GATED>(t, a, stream);
-    case Form::DX: return by_type<Form::DX>(t, a, stream);
-    default: return by_type<Form::DW>(t, a, stream);
+    case Form::LINEAR: return run_form<T, Form::LINEAR>(a, stream);
+    case Form::GATED: return run_form<T, Form::GATED>(a, stream);
+    case Form::DX: return run_form<T, Form::DX>(a, stream);
+    default: return run_form<T, Form::DW>(a, stream);
   }
 }
 
 template <Type T>
-static hipError_t slope(const SlopeArgs& a, hipStream_t stream) {
+hipError_t run_slope(const SlopeArgs& a, hipStream_t stream) {
   constexpr int E = 16 / sizeof(typename Elem<T>::V);
   const size_t n = (a.cols + E - 1) / E * a.rows;
   const size_t blocks = (n + 255) / 256;
@@ -692,19 +828,6 @@ static hipError_t slope(const SlopeArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_slope(Type t, const SlopeArgs& a, hipStream_t stream) {
-  switch (t) {
-    case Type::BF16: return slope<Type::BF16>(a, stream);
-    case Type::F16: return slope<Type::F16>(a, stream);
-    default: return slope<Type::F32>(a, stream);
-  }
-}
-
-size_t part_bytes(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
-                  size_t nc, int cus, int* splits) {
-  *splits = 1;
-  return 0;
-}
-
+}  // namespace
 }  // namespace products
 }  // namespace dpar
