@@ -45,6 +45,8 @@ struct Args {
   int act;
   int out32;                 // result in 32 bits
   int splits;                // parts of the contraction
+  int waves;                 // few rows: parts of the contraction per
+                             // workgroup (0: tiles)
   int tile;                  // 64 << tile rows and columns per workgroup
   int fast;                  // A, B: 16-byte rows and whole 16-byte pieces
   int wide_out;              // results, kept values, residual, bias: 16-byte

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -204,22 +205,76 @@ int ranks_per_launch(int p) {
 
 // How a product runs.
 struct Shape {
-  int tile, splits;
+  int waves, tile, splits;
   size_t part;           // bytes of workspace
 };
 
+// Time of one contraction tile (128 bytes of every row) of a workgroup on a
+// CU, in ns: its share of the CU's rate when the CU is full, and the least it
+// takes alone (memory latency over the two tiles in flight); workgroups
+// resident.  Measured on an MI355X.
+struct TileCost {
+  double rate, alone;
+  int resident;
+};
+constexpr TileCost kCost16[] = {{220, 500, 5}, {610, 800, 2}, {1850, 1450, 1}};
+constexpr TileCost kCost32[] = {{530, 700, 5}, {2100, 2100, 2}};
+// Joining a split contraction: a second launch, and its bytes (written by the
+// first) per ns.
+constexpr double kJoinNs = 4000, kJoinRate = 2300;
+constexpr double kStartNs = 2000;      // first loads and last stores
+constexpr size_t kMostPart = (size_t)256 << 20;
+
+// Rows up to which the forward forms take the few-rows kernel: 64 x 4096 x
+// 16384 43 us (tiles: 53), 48 x 4096 x 8192 gated 37 us (53).
+constexpr size_t kFewRows = 64;
+
 Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
-               size_t nc, int cus) {
-  // the largest tiles that still give every CU one
-  auto count = [&](size_t bm, size_t bn) {
-    return (ni + bm - 1) / bm * ((nj + bn - 1) / bn) * ranks *
-           (f == Form::DW ? pairs : 1);
-  };
-  const int half = f == Form::GATED ? 2 : 1;
-  int tile = 0;
-  if (count(128, 128 / half) >= (size_t)cus) tile = 1;
-  if (t != Type::F32 && count(256, 256 / half) >= (size_t)cus) tile = 2;
-  return {tile, 1, 0};
+               size_t nc, int cus, bool split) {
+  if ((f == Form::LINEAR || f == Form::GATED) && ni <= kFewRows) {
+    // Wavefronts per workgroup: 16 per CU in all, 8 once there are 4 (each
+    // takes a part of the contraction, at least a chunk of 512 bytes).
+    // Measured with 16 / 8 per CU: 8 x 1 x 4096 x 2048 gated 42.4 / 46.2 us,
+    // 8 x 16 x 2048 x 4096 28.7 / 31.5 us; 16 x 4096 x 8192 gated 26.3 (8
+    // wavefronts) / 23.5 us (4).
+    const size_t cols = f == Form::GATED || ni <= 16 ? 16 : 32;
+    const size_t tiles = (nj + cols - 1) / cols * ranks;
+    const size_t chunks = nc / (t == Type::F32 ? 128 : 256);
+    int w = 1;
+    while (w < 8 && tiles * w < (size_t)cus * (w < 4 ? 16 : 8) &&
+           chunks >= (size_t)w * 2)
+      w *= 2;
+    return {w, 0, 1, 0};
+  }
+  const size_t kt = t == Type::F32 ? 32 : 64;
+  const size_t nk = (nc + kt - 1) / kt * (f == Form::DX ? pairs : 1);
+  const size_t cells = ni * nj * ranks * (f == Form::DW ? pairs : 1) *
+                       (f == Form::GATED ? 2 : 1);
+  const int tiles = t == Type::F32 ? 2 : 3;
+  const TileCost* cost = t == Type::F32 ? kCost32 : kCost16;
+  Shape best = {0, 0, 1, 0};
+  double least = 0;
+  for (int tile = 0; tile < tiles; ++tile) {
+    const size_t bm = (size_t)64 << tile, bn = f == Form::GATED ? bm / 2 : bm;
+    const double n = (double)((ni + bm - 1) / bm) * ((nj + bn - 1) / bn) *
+                     ranks * (f == Form::DW ? pairs : 1);
+    for (int s = 1; s <= (split ? 16 : 1); s += s < 4 ? 1 : s < 8 ? 2 : 4) {
+      const size_t part = s > 1 ? (cells + (f == Form::DW ? ni * ranks * pairs
+                                                          : 0)) * s * 4 : 0;
+      if (s > 1 && (nk < (size_t)s * 2 || part > kMostPart)) break;
+      const double wgs = n * s, steps = (double)((nk + s - 1) / s);
+      const double turns = std::ceil(wgs / ((double)cus * cost[tile].resident));
+      const double per = std::ceil(wgs / cus);
+      double ns = kStartNs + steps * std::max(turns * cost[tile].alone,
+                                              per * cost[tile].rate);
+      if (s > 1) ns += kJoinNs + part / kJoinRate;
+      if (least == 0 || ns < least) {
+        least = ns;
+        best = {0, tile, s, part};
+      }
+    }
+  }
+  return best;
 }
 
 struct Step {
@@ -256,7 +311,7 @@ size_t workspace_of(dpar_product_call_t call, Type t, int p,
   for (int k = 0; k < n; ++k)
     most = std::max(most, shape_of(s[k].form, t, ranks_per_launch(p),
                                    s[k].pairs, s[k].ni, s[k].nj, s[k].nc,
-                                   cus).part);
+                                   cus, true).part);
   return most;
 }
 
@@ -285,9 +340,11 @@ template <typename Fill>
 int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
                 int cus, hipStream_t stream, Fill fill) {
   const int per = ranks_per_launch(p);
-  const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus);
+  const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
+                           ws != nullptr);
+  a->waves = s.waves;
   a->tile = s.tile;
-  a->splits = ws ? s.splits : 1;
+  a->splits = s.splits;
   a->part = (float*)ws;
   for (int r0 = 0; r0 < p; r0 += per) {
     a->ranks = std::min(per, p - r0);

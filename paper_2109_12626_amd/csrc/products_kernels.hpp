@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "products.hpp"
 
 namespace dpar {
@@ -162,6 +164,15 @@ __device__ inline i32x4 load_piece(const V* p, long n) {
   return v;
 }
 
+// A whole piece.
+template <bool ALIGNED, typename V>
+__device__ inline i32x4 load_whole(const V* p) {
+  if constexpr (ALIGNED) return *(const i32x4*)p;
+  i32x4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
 // Sixteen bytes per lane straight from memory to LDS, lane after lane from
 // `lds` on (the same address in the whole wavefront).  Written as assembly so
 // that the compiler does not wait for them before every LDS read: the kernel
@@ -171,6 +182,13 @@ __device__ inline i32x4 load_piece(const V* p, long n) {
 __device__ inline void dma16(uint32_t lds, const void* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
                "global_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+// The same for data that is read once.
+__device__ inline void dma16_once(uint32_t lds, const void* base,
+                                  uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+               "global_load_lds_dwordx4 %1, %2 nt"
                :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ inline void dma16_at(uint32_t lds, const void* p) {
@@ -296,20 +314,27 @@ struct Operand {
 
 // ---------------------------------------------------------------- results
 
-// n consecutive results of a row: whole 16-byte pieces, or one by one up to
-// `left`.
+template <int BYTES> struct Piece;
+template <> struct Piece<16> { using I = i32x4; };
+template <> struct Piece<8> { using I = long; };
+template <> struct Piece<4> { using I = int; };
+template <> struct Piece<2> { using I = short; };
+
+// N consecutive results of a row: in pieces of up to 16 bytes where they are
+// aligned to that and all there (`left` are), else one by one.
 template <typename V, int N>
 __device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
-  constexpr int E = 16 / sizeof(V);
+  constexpr int B = N * sizeof(V) < 16 ? N * sizeof(V) : 16, E = B / sizeof(V);
+  using I = typename Piece<B>::I;
   if (wide && left >= N) {
 #pragma unroll
     for (int k = 0; k < N; k += E) {
       V t[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) t[e] = (V)v[k + e];
-      i32x4 w;
-      __builtin_memcpy(&w, t, 16);
-      *(i32x4*)(p + k) = w;
+      I w;
+      __builtin_memcpy(&w, t, B);
+      *(I*)(p + k) = w;
     }
     return;
   }
@@ -320,13 +345,14 @@ __device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
 
 template <typename V, int N>
 __device__ inline void fetch_vals(const V* p, float* v, long left, bool wide) {
-  constexpr int E = 16 / sizeof(V);
+  constexpr int B = N * sizeof(V) < 16 ? N * sizeof(V) : 16, E = B / sizeof(V);
+  using I = typename Piece<B>::I;
   if (wide && left >= N) {
 #pragma unroll
     for (int k = 0; k < N; k += E) {
-      const i32x4 w = *(const i32x4*)(p + k);
+      const I w = *(const I*)(p + k);
       V t[E];
-      __builtin_memcpy(t, &w, 16);
+      __builtin_memcpy(t, &w, B);
 #pragma unroll
       for (int e = 0; e < E; ++e) v[k + e] = (float)t[e];
     }
@@ -682,6 +708,256 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
   Tiled<T, F, FAST, BM, BN, WM, WN>::run(a, (LDS char*)lds);
 }
 
+// ---------------------------------------------------------------- few rows
+
+// Few rows of x (MT tiles of 16): a wavefront takes 16 or 32 rows of w (GATED:
+// 16 of each) and one of S parts of the contraction, straight from memory to
+// the matrix cores' registers, U steps of loads at a time; the workgroup's S
+// wavefronts join their sums in LDS, in order.  Every weight is read once, by
+// all lanes of a wavefront side by side (64 bytes of 16 rows a load); x is
+// small and comes from the caches.
+template <Type T, Form F, bool FAST, int MT, int S>
+struct Few {
+  using V = typename Elem<T>::V;
+  static constexpr int E = 16 / sizeof(V), K = 4 * E;   // per piece, per step
+  static constexpr bool kGated = F == Form::GATED;
+  static constexpr int NW = kGated || MT > 1 ? 2 : 1;
+  static constexpr int BJ = kGated ? 16 : 16 * NW;
+  static constexpr int U = MT * NW <= 2 ? 8 : 4;
+
+  static __device__ void run(Given& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const unsigned nt = (unsigned)((a.nj + BJ - 1) / BJ);
+    const unsigned rank = uniform(blockIdx.x / nt);
+    const size_t j0 = (size_t)uniform(blockIdx.x % nt) * BJ;
+    const unsigned steps = (unsigned)((a.nc + K - 1) / K);
+    const unsigned s0 = (unsigned)((uint64_t)steps * wave / S),
+                   s1 = (unsigned)((uint64_t)steps * (wave + 1) / S);
+    const V* w[NW];
+    const V* x[MT];
+#pragma unroll
+    for (int n = 0; n < NW; ++n) {
+      size_t j = j0 + (kGated ? 0 : n * 16) + r;
+      if (j >= a.nj) j = a.nj - 1;
+      w[n] = (const V*)a.b[kGated ? n : 0][rank] + j * a.ldb + q * E;
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      size_t i = m * 16 + r;
+      if (i >= a.ni) i = a.ni - 1;
+      x[m] = (const V*)a.a[0][rank] + i * a.lda + q * E;
+    }
+    f32x4 acc[MT][NW] = {};
+    unsigned s = s0;
+    const unsigned full = (unsigned)(a.nc / K) < s1 ? (unsigned)(a.nc / K) : s1;
+#pragma unroll 1
+    for (; s + U <= full; s += U) {
+      i32x4 fw[U][NW], fx[U][MT];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+#pragma unroll
+        for (int n = 0; n < NW; ++n)
+          fw[k][n] = load_whole<FAST>(w[n] + (size_t)(s + k) * K);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          fx[k][m] = load_whole<FAST>(x[m] + (size_t)(s + k) * K);
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+#pragma unroll
+        for (int n = 0; n < NW; ++n)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            acc[m][n] = Elem<T>::mma(fw[k][n], fx[k][m], acc[m][n]);
+    }
+#pragma unroll 1
+    for (; s < s1; ++s) {
+      const long left = (long)a.nc - (long)s * K - q * E;
+      i32x4 fw[NW], fx[MT];
+#pragma unroll
+      for (int n = 0; n < NW; ++n)
+        fw[n] = load_piece<V>(w[n] + (size_t)s * K, left);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        fx[m] = load_piece<V>(x[m] + (size_t)s * K, left);
+#pragma unroll
+      for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          acc[m][n] = Elem<T>::mma(fw[n], fx[m], acc[m][n]);
+    }
+    finish_all(a, (f32x4(LDS*)[MT * NW][64])lds, acc, rank, j0, wave, lane);
+  }
+
+  // Adds the S wavefronts' sums in their order and finishes the results.
+  static __device__ void finish_all(Given& a, f32x4 (LDS* part)[MT * NW][64],
+                                    f32x4 (&acc)[MT][NW], unsigned rank,
+                                    size_t j0, int wave, int lane) {
+    const int r = lane & 15, q = lane >> 4;
+    if (S > 1) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NW; ++n) part[wave][m * NW + n][lane] = acc[m][n];
+      __syncthreads();
+    }
+    // result tile (m, n): wavefront tile % S
+    constexpr int NO = kGated ? 1 : NW;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NO; ++n) {
+        if ((m * NO + n) % S != wave) continue;
+        f32x4 v = acc[m][n], u = acc[m][NW - 1];
+        if (S > 1) {
+          v = part[0][m * NW + n][lane];
+          for (int k = 1; k < S; ++k) v += part[k][m * NW + n][lane];
+          if (kGated) {
+            u = part[0][m * NW + 1][lane];
+            for (int k = 1; k < S; ++k) u += part[k][m * NW + 1][lane];
+          }
+        }
+        const size_t i = m * 16 + r, j = j0 + n * 16 + q * 4;
+        if (i >= a.ni || j >= a.nj) continue;
+        float va[4], ua[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) va[e] = v[e], ua[e] = u[e];
+        finish<T, F, 4>(a, rank, 0, i, j, va, ua);
+      }
+  }
+};
+
+// The same with whole 16-byte pieces: the weights go to LDS in chunks of 16
+// rows x 512 bytes, two rows of 512 bytes per load, which memory serves faster
+// than 64 bytes of 16 rows (a copy of the loads alone: 6.5 against 5.9 TB/s
+// at 268 MB); x goes to registers.  Each wavefront has two chunks of LDS of
+// its own and needs no barrier: while it multiplies one chunk the next is on
+// its way.  Two sets of weight rows (GATED, or MT > 1) alternate and share x.
+template <Type T, Form F, int MT, int S>
+struct FewFast {
+  using V = typename Elem<T>::V;
+  using Old = Few<T, F, true, MT, S>;
+  static constexpr bool kGated = F == Form::GATED;
+  static constexpr int NW = Old::NW, BJ = Old::BJ, E = Old::E;
+  static constexpr int kRow = 512, kChunk = 16 * kRow;
+  static constexpr int KC = kRow / (int)sizeof(V);   // contraction per chunk
+  static constexpr int U = kRow / 64;                // steps per chunk
+
+  static __device__ void run(Given& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const unsigned nt = (unsigned)((a.nj + BJ - 1) / BJ);
+    const unsigned rank = uniform(blockIdx.x / nt);
+    const size_t j0 = (size_t)uniform(blockIdx.x % nt) * BJ;
+    const unsigned chunks = (unsigned)((a.nc + KC - 1) / KC);
+    const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
+                   c1 = uniform((unsigned)((uint64_t)chunks * (wave + 1) / S));
+    // load h: rows 2 h, 2 h + 1; pieces exchanged by the row
+    const char* base[NW];
+    uint32_t off[NW][8];
+    const int slot = lane & 31;
+#pragma unroll
+    for (int n = 0; n < NW; ++n) {
+      const size_t jn = j0 + (kGated ? 0 : n * 16);
+      const size_t first = jn < a.nj ? jn : a.nj - 1;
+      base[n] = uniform((const char*)a.b[kGated ? n : 0][rank] +
+                        first * a.ldb * sizeof(V));
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const int row = h * 2 + (lane >> 5);
+        const size_t most = a.nj - first - 1;
+        const size_t at = (size_t)row < most ? row : most;
+        off[n][h] = (uint32_t)(at * a.ldb * sizeof(V)) +
+                    (slot ^ (row & 7)) * 16;
+      }
+    }
+    const uint32_t mine = (uint32_t)(uintptr_t)lds + wave * (2 * kChunk);
+    LDS char* const src = lds + wave * (2 * kChunk);
+    const V* x[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      size_t i = m * 16 + r;
+      if (i >= a.ni) i = a.ni - 1;
+      x[m] = (const V*)a.a[0][rank] + i * a.lda + q * E;
+    }
+    auto issue = [&](unsigned c, int n, int buf) {
+      const char* b = uniform(base[n] + (size_t)c * kRow);
+      const uint32_t d = mine + buf * kChunk;
+      if ((size_t)(c + 1) * KC <= a.nc) {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) dma16_once(d + h * 1024, b, off[n][h]);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const int row = h * 2 + (lane >> 5);
+          const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * E;
+          dma16_at(d + h * 1024,
+                   k < a.nc ? b + off[n][h] : (const char*)&g_zero);
+        }
+      }
+    };
+    i32x4 fx[U][MT];
+    auto load_x = [&](unsigned c) {
+      if ((size_t)(c + 1) * KC <= a.nc) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            fx[u][m] = *(const i32x4*)(x[m] + (size_t)c * KC + u * 4 * E);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const size_t k = (size_t)c * KC + u * 4 * E;
+            fx[u][m] = k + q * E < a.nc ? *(const i32x4*)(x[m] + k)
+                                        : i32x4{0, 0, 0, 0};
+          }
+      }
+    };
+    f32x4 acc[MT][NW] = {};
+    if (c0 < c1) issue(c0, 0, 0);
+    int buf = 0;
+#pragma unroll 1
+    for (unsigned c = c0; c < c1; ++c) {
+      load_x(c);
+#pragma unroll
+      for (int n = 0; n < NW; ++n) {
+        // (the wait also covers x)
+        landed<0>();
+        if (n + 1 < NW)
+          issue(c, n + 1, buf ^ 1);
+        else if (c + 1 < c1)
+          issue(c + 1, 0, buf ^ 1);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const i32x4 fw = *(LDS i32x4*)(src + buf * kChunk + r * kRow +
+                                         (((u * 4 + q) ^ (r & 7)) * 16));
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            acc[m][n] = Elem<T>::mma(fw, fx[u][m], acc[m][n]);
+        }
+        buf ^= 1;
+      }
+    }
+    // the parts meet in LDS where the chunks were
+    if (S > 1) __syncthreads();
+    Old::finish_all(a, (f32x4(LDS*)[MT * NW][64])lds, acc, rank, j0, wave,
+                    lane);
+  }
+};
+
+template <Type T, Form F, bool FAST, int MT, int S>
+__global__ __launch_bounds__(S * 64) void k_few(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  if constexpr (FAST)
+    FewFast<T, F, MT, S>::run(a, (LDS char*)lds);
+  else
+    Few<T, F, FAST, MT, S>::run(a, (LDS char*)lds);
+}
+
 // Joins the parts of a split contraction in their order and finishes: 4
 // results per thread.
 template <Type T, Form F>
@@ -784,8 +1060,44 @@ hipError_t go(const Args& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <Type T, Form F, bool FAST, int MT, int S>
+hipError_t go_few(const Args& a, hipStream_t stream) {
+  using K = Few<T, F, FAST, MT, S>;
+  const size_t n = (a.nj + K::BJ - 1) / K::BJ * a.ranks;
+  if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
+  const size_t parts = S > 1 ? (size_t)S * MT * K::NW * 1024 : 0;
+  const size_t bytes =
+      FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, S>::kChunk)
+           : parts;
+  auto k = k_few<T, F, FAST, MT, S>;
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(
+        (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
+        (int)bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(S * 64), bytes, stream, a);
+  return hipGetLastError();
+}
+
+template <Type T, Form F, bool FAST, int MT>
+hipError_t pick_few(const Args& a, hipStream_t stream) {
+  switch (a.waves) {
+    case 1: return go_few<T, F, FAST, MT, 1>(a, stream);
+    case 2: return go_few<T, F, FAST, MT, 2>(a, stream);
+    case 4: return go_few<T, F, FAST, MT, 4>(a, stream);
+    default: return go_few<T, F, FAST, MT, 8>(a, stream);
+  }
+}
+
 template <Type T, Form F, bool FAST>
 hipError_t pick(const Args& a, hipStream_t stream) {
+  if constexpr (F == Form::LINEAR || F == Form::GATED)
+    if (a.waves) {
+      if (a.ni <= 16) return pick_few<T, F, FAST, 1>(a, stream);
+      if (a.ni <= 32) return pick_few<T, F, FAST, 2>(a, stream);
+      return pick_few<T, F, FAST, 4>(a, stream);
+    }
   if constexpr (T != Type::F32 && FAST)
     if (a.tile == 2)
     return go<T, F, FAST, 256, 256, 128, 64>(a, stream);
