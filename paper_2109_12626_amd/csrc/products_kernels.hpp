@@ -466,6 +466,41 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
   }
 }
 
+// Which results a workgroup computes.
+template <int BM, int BJ>
+struct Place {
+  size_t i0, j0;        // first row and column
+  unsigned split;       // part of the contraction
+  int rank, pair;
+
+  __device__ Place(Given& a, Form form) {
+    // (weights' gradients without columns still have bias sums)
+    const size_t mt = (a.ni + BM - 1) / BM,
+                 nt = a.nj ? (a.nj + BJ - 1) / BJ : 1;
+    // consecutive workgroups go to the 8 XCDs in turn: give each XCD a run of
+    // neighbouring tiles so that they share operands in its L2
+    unsigned id = blockIdx.x;
+    {
+      const unsigned n = gridDim.x, per = n / 8, more = n % 8;
+      const unsigned x = id % 8, k = id / 8;
+      id = x * per + (x < more ? x : more) + k;
+    }
+    // (the host keeps the number of workgroups below 2^31)
+    const unsigned tiles = (unsigned)mt * (unsigned)nt;
+    split = uniform(id % a.splits);
+    unsigned rest = id / a.splits;
+    const unsigned tile = rest % tiles;
+    rest = uniform(rest / tiles);
+    pair = form == Form::DW ? rest % a.pairs : 0;
+    rank = form == Form::DW ? rest / a.pairs : rest;
+    // groups of 8 tile rows, columns inside
+    const unsigned row8 = tile / (8 * (unsigned)nt), in = tile % (8 * (unsigned)nt);
+    const unsigned left = (unsigned)mt - row8 * 8, high = left < 8 ? left : 8;
+    i0 = (size_t)uniform(row8 * 8 + in % high) * BM;
+    j0 = (size_t)uniform(in / high) * BJ;
+  }
+};
+
 // Stores a wavefront's WM x WN results (GATED: g's and u's halves) from row iw
 // and column jw on, and the sums of A that it holds (those of its tile rows m
 // with m % shares == share).
@@ -574,30 +609,10 @@ struct Tiled {
   static __device__ void run(Given& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
     const int wm = wave / (BN / WN), wn = wave % (BN / WN);
-    // (weights' gradients without columns still have bias sums)
-    const size_t mt = (a.ni + BM - 1) / BM,
-                 nt = a.nj ? (a.nj + BJ - 1) / BJ : 1;
-    // consecutive workgroups go to the 8 XCDs in turn: give each XCD a run of
-    // neighbouring tiles so that they share operands in its L2
-    unsigned id = blockIdx.x;
-    {
-      const unsigned n = gridDim.x, per = n / 8, more = n % 8;
-      const unsigned x = id % 8, k = id / 8;
-      id = x * per + (x < more ? x : more) + k;
-    }
-    // (the host keeps the number of workgroups below 2^31)
-    const unsigned tiles = (unsigned)mt * (unsigned)nt;
-    const unsigned split = uniform(id % a.splits);
-    unsigned rest = id / a.splits;
-    const unsigned tile = rest % tiles;
-    rest = uniform(rest / tiles);
-    const int pair = F == Form::DW ? rest % a.pairs : 0;
-    const int rank = F == Form::DW ? rest / a.pairs : rest;
-    // groups of 8 tile rows, columns inside
-    const unsigned row8 = tile / (8 * (unsigned)nt), in = tile % (8 * (unsigned)nt);
-    const unsigned left = (unsigned)mt - row8 * 8, high = left < 8 ? left : 8;
-    const size_t i0 = (size_t)uniform(row8 * 8 + in % high) * BM,
-                 j0 = (size_t)uniform(in / high) * BJ;
+    const Place<BM, BJ> at(a, F);
+    const int rank = at.rank, pair = at.pair;
+    const unsigned split = at.split;
+    const size_t i0 = at.i0, j0 = at.j0;
 
     const unsigned nk1 = (unsigned)((a.nc + KT - 1) / KT);
     const unsigned nk = F == Form::DX ? nk1 * a.pairs : nk1;
@@ -822,6 +837,183 @@ struct Tiled {
         wave, lane);
   }
 };
+
+// 16-bit types, 256 x 256 results (GATED: 256 x 128 of each), 8 wavefronts of
+// 128 x 64.  The contraction goes in stages of 64 bytes (32 values); five
+// stages of 32 KB fill the LDS, so four are on their way while one is used.
+//
+// Each SIMD has two wavefronts, one of either half of the workgroup, and the
+// halves run one phase apart: while one half reads its fragments and asks for
+// a later stage, the other has the matrix cores to itself; then a barrier,
+// and they change places.  A phase is 32 products of 16 x 16 x 32 (512
+// cycles); the reads of the other half (12 pieces of 16 bytes per lane) take
+// less.
+template <Type T, Form F>
+struct PingPong {
+  using V = typename Elem<T>::V;
+  static constexpr bool kGated = F == Form::GATED;
+  static constexpr bool kACC = F != Form::DW;
+  static constexpr bool kBCC = F == Form::LINEAR || F == Form::GATED;
+  static constexpr int BM = 256, BN = 256, WM = 128, WN = 64, kThreads = 512;
+  static constexpr int MI = WM / 16, NJ = WN / 16, NT = kGated ? NJ / 2 : NJ;
+  static constexpr int G = 4 * NT, BJ = kGated ? BN / 2 : BN;
+  static constexpr int kLineBytes = 64, NS = 5;
+  using OA = Operand<T, kACC, BM, 4, kThreads, kLineBytes>;
+  using OB = Operand<T, kBCC, BN, G, kThreads, kLineBytes>;
+  static constexpr int KT = OA::KT;
+  static constexpr int kBytesA = BM * kLineBytes,
+                       kBytes = (BM + BN) * kLineBytes;
+  static constexpr int kPieces = OA::N + OB::N;
+  static constexpr int kLds = NS * kBytes;
+
+  static __device__ void run(Given& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int wm = wave / 4, wn = wave % 4;
+    const Place<BM, BJ> at(a, F);
+    const int rank = at.rank, pair = at.pair;
+    const unsigned split = at.split;
+    const size_t i0 = at.i0, j0 = at.j0;
+
+    const unsigned nk1 = (unsigned)((a.nc + KT - 1) / KT);
+    const unsigned nk = F == Form::DX ? nk1 * a.pairs : nk1;
+    const unsigned k0 = uniform((unsigned)((uint64_t)nk * split / a.splits)),
+                   k1 = uniform((unsigned)((uint64_t)nk * (split + 1) /
+                                           a.splits));
+    const unsigned whole = uniform((unsigned)(a.nc / KT));
+
+    f32x4 acc[MI][NJ] = {};
+    f32x4 sum = {};
+    const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
+
+    uint32_t va[OA::N], vb[OB::N];
+#pragma unroll
+    for (int n = 0; n < OA::N; ++n)
+      va[n] = OA::offset(a.lda, i0, a.ni, n, t);
+#pragma unroll
+    for (int n = 0; n < OB::N; ++n)
+      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (OB::N / 2) : n, t);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds + wave * 1024;
+
+    auto issue = [&](unsigned kt, int slot) {
+      const int s = F == Form::DX ? (kt >= nk1) : pair;
+      const unsigned c = F == Form::DX && s ? kt - nk1 : kt;
+      const size_t c0 = (size_t)c * KT;
+      const char* pa = uniform((const char*)a.a[s][rank] +
+                               OA::origin(a.lda, i0) + c * OA::step(a.lda));
+      const size_t ob = OB::origin(a.ldb, j0) + c * OB::step(a.ldb);
+      const char* pb = uniform(
+          (const char*)a.b[kGated || F == Form::DW ? 0 : s][rank] + ob);
+      const char* pu = kGated ? uniform((const char*)a.b[1][rank] + ob) : pb;
+      const uint32_t ga = OA::guard(a.lda, i0, a.ni, c0, a.nc, 0, t);
+      const uint32_t d = lds0 + slot * kBytes;
+#pragma unroll
+      for (int n = 0; n < OA::N; ++n)
+        dma16(d + n * kThreads * 16, pa, OA::guarded(va[n], ga));
+#pragma unroll
+      for (int n = 0; n < OB::N; ++n)
+        dma16(d + kBytesA + n * kThreads * 16,
+              kGated && n >= OB::N / 2 ? pu : pb,
+              OB::guarded(vb[n],
+                          OB::guard(a.ldb, j0, a.nj, c0, a.nc, n, t)));
+    };
+    // As in Tiled: zeros past the contraction's end.
+    auto clear = [&](unsigned kt, int slot) {
+      const unsigned c = F == Form::DX && kt >= nk1 ? kt - nk1 : kt;
+      if (c < whole) return;
+      LDS char* d = lds + slot * kBytes + t * 16;
+      int o = t;
+      asm volatile("" : "+v"(o));
+#pragma unroll 1
+      for (int n = 0; n < kPieces; ++n)
+        if (n < OA::N ? OA::past((size_t)c * KT, a.nc, n, o)
+                      : OB::past((size_t)c * KT, a.nc, n - OA::N, o))
+          *(LDS i32x4*)(d + n * kThreads * 16) = i32x4{0, 0, 0, 0};
+    };
+    // Waits until this wavefront's pieces of stage kt have landed (`newer`:
+    // all NS - 2 stages after it have been asked for).
+    auto ready = [&](unsigned kt, int slot, bool newer) {
+      if (kt >= k1) return;
+      if (newer)
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((NS - 2) * kPieces)
+                     : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      clear(kt, slot);
+    };
+
+    auto loop = [&](auto with_sums) {
+      int slot = 0;
+#pragma unroll 1
+      for (unsigned kt = k0; kt < k1; ++kt) {
+        const bool more = kt + NS - 1 < k1;
+        const int next = slot + 1 == NS ? 0 : slot + 1;
+        LDS char* sa = lds + slot * kBytes;
+        LDS char* sb = sa + kBytesA;
+        i32x4 fa[MI], fb[NJ];
+#pragma unroll
+        for (int n = 0; n < NJ; ++n)
+          fb[n] = OB::frag(sb, 0, kGated ? (n < NT ? 0 : BJ) + wn * (WN / 2)
+                                         : wn * WN, n % NT, lane);
+#pragma unroll
+        for (int m = 0; m < MI; ++m)
+          fa[m] = OA::frag(sa, 0, wm * WM + m * 16, 0, lane);
+        if (more) issue(kt + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+        if (wm) ready(kt + 1, next, more);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int m = 0; m < MI; ++m) {
+#pragma unroll
+          for (int n = 0; n < NJ; ++n)
+            acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
+          if constexpr (with_sums)
+            if (m % 4 == wn)
+              sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
+                                 fa[m], sum);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!wm) ready(kt + 1, next, more);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        slot = next;
+      }
+    };
+
+    if (k0 < k1) {
+#pragma unroll 1
+      for (int n = 0; n < NS - 1; ++n)
+        if (k0 + n < k1) issue(k0 + n, n);
+      ready(k0, 0, k0 + NS - 2 < k1);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      if (wm) __builtin_amdgcn_s_barrier();   // half a stage behind
+      if constexpr (F == Form::DW) {
+        if (sums)
+          loop(Yes{});
+        else
+          loop(No{});
+      } else {
+        loop(No{});
+      }
+      if (!wm) __builtin_amdgcn_s_barrier();
+    }
+    Results<T, F, WM, WN, OB>::store(a, rank, pair, split, i0 + wm * WM,
+                                     j0 + wn * (kGated ? WN / 2 : WN), sums,
+                                     wn, 4, sum, acc, lds, wave, lane);
+  }
+};
+
+template <Type T, Form F>
+__global__ __launch_bounds__(512) void k_pingpong(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  PingPong<T, F>::run(a, (LDS char*)lds);
+}
 
 template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
@@ -1161,25 +1353,28 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
 
 // ---------------------------------------------------------------- launches
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
-hipError_t go(const Args& a, hipStream_t stream) {
-  using K = Tiled<T, F, FAST, BM, BN, WM, WN>;
-  const size_t tiles =
-      (a.ni + BM - 1) / BM * (a.nj ? (a.nj + K::BJ - 1) / K::BJ : 1);
-  const size_t n = tiles * a.ranks * (F == Form::DW ? a.pairs : 1) * a.splits;
+hipError_t launch_tiles(void (*k)(Args), Form f, const Args& a, int bm, int bj,
+                        int threads, size_t bytes, hipStream_t stream) {
+  const size_t tiles = (a.ni + bm - 1) / bm *
+                       (a.nj ? (a.nj + bj - 1) / bj : 1);
+  const size_t n = tiles * a.ranks * (f == Form::DW ? a.pairs : 1) * a.splits;
   if (n == 0) return hipSuccess;
   if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
-  const size_t bytes = 2 * K::kBytes;
-  auto k = k_tiled<T, F, FAST, BM, BN, WM, WN>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
         (int)bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(K::kThreads), bytes, stream,
-                     a);
+  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(threads), bytes, stream, a);
   return hipGetLastError();
+}
+
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+hipError_t go(const Args& a, hipStream_t stream) {
+  using K = Tiled<T, F, FAST, BM, BN, WM, WN>;
+  return launch_tiles(k_tiled<T, F, FAST, BM, BN, WM, WN>, F, a, BM, K::BJ,
+                      K::kThreads, 2 * K::kBytes, stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int S>
@@ -1221,8 +1416,11 @@ hipError_t pick(const Args& a, hipStream_t stream) {
       return pick_few<T, F, FAST, 4>(a, stream);
     }
   if constexpr (T != Type::F32 && FAST)
-    if (a.tile == 2)
-    return go<T, F, FAST, 256, 256, 128, 64>(a, stream);
+    if (a.tile == 2) {
+      using K = PingPong<T, F>;
+      return launch_tiles(k_pingpong<T, F>, F, a, K::BM, K::BJ, K::kThreads,
+                          K::kLds, stream);
+    }
   if (a.tile >= 1) return go<T, F, FAST, 128, 128, 64, 64>(a, stream);
   return go<T, F, FAST, 64, 64, 32, 32>(a, stream);
 }
