@@ -839,15 +839,17 @@ struct Tiled {
 };
 
 // 16-bit types, 256 x 256 results (GATED: 256 x 128 of each), 8 wavefronts of
-// 128 x 64.  The contraction goes in stages of 64 bytes (32 values); five
-// stages of 32 KB fill the LDS, so four are on their way while one is used.
+// 128 x 64.  A tile of the contraction (128 bytes of 256 rows of A and of B)
+// takes two of five 32 KB slots of LDS, so that up to three operands are on
+// their way while one tile is used.  (Stages of 64 bytes a row would leave
+// four, but loads of 64 bytes of 16 rows reach half the rate of 128 bytes of
+// 8: 67 against 123 GB/s per CU from L2.)
 //
 // Each SIMD has two wavefronts, one of either half of the workgroup, and the
-// halves run one phase apart: while one half reads its fragments and asks for
-// a later stage, the other has the matrix cores to itself; then a barrier,
-// and they change places.  A phase is 32 products of 16 x 16 x 32 (512
-// cycles); the reads of the other half (12 pieces of 16 bytes per lane) take
-// less.
+// halves run one phase apart: while one half reads the fragments of a step
+// (12 pieces of 16 bytes per lane) and asks for a later operand, the other has
+// the matrix cores to itself for 32 products of 16 x 16 x 32 (512 cycles);
+// then a barrier, and they change places.
 template <Type T, Form F>
 struct PingPong {
   using V = typename Elem<T>::V;
@@ -857,14 +859,12 @@ struct PingPong {
   static constexpr int BM = 256, BN = 256, WM = 128, WN = 64, kThreads = 512;
   static constexpr int MI = WM / 16, NJ = WN / 16, NT = kGated ? NJ / 2 : NJ;
   static constexpr int G = 4 * NT, BJ = kGated ? BN / 2 : BN;
-  static constexpr int kLineBytes = 64, NS = 5;
-  using OA = Operand<T, kACC, BM, 4, kThreads, kLineBytes>;
-  using OB = Operand<T, kBCC, BN, G, kThreads, kLineBytes>;
-  static constexpr int KT = OA::KT;
-  static constexpr int kBytesA = BM * kLineBytes,
-                       kBytes = (BM + BN) * kLineBytes;
-  static constexpr int kPieces = OA::N + OB::N;
-  static constexpr int kLds = NS * kBytes;
+  using OA = Operand<T, kACC, BM, 4, kThreads>;
+  using OB = Operand<T, kBCC, BN, G, kThreads>;
+  static constexpr int KT = OA::KT, NP = OA::N;
+  static_assert(OA::N == OB::N);
+  static constexpr int kSlots = 5, kSlot = BM * kLine;
+  static constexpr int kLds = kSlots * kSlot;
 
   static __device__ void run(Given& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
@@ -885,113 +885,129 @@ struct PingPong {
     f32x4 sum = {};
     const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
 
-    uint32_t va[OA::N], vb[OB::N];
+    uint32_t va[NP], vb[NP];
 #pragma unroll
-    for (int n = 0; n < OA::N; ++n)
+    for (int n = 0; n < NP; ++n) {
       va[n] = OA::offset(a.lda, i0, a.ni, n, t);
-#pragma unroll
-    for (int n = 0; n < OB::N; ++n)
-      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (OB::N / 2) : n, t);
+      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (NP / 2) : n, t);
+    }
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds + wave * 1024;
 
-    auto issue = [&](unsigned kt, int slot) {
+    // A's or B's part of tile kt into a slot.
+    auto ask_a = [&](unsigned kt, int slot) {
       const int s = F == Form::DX ? (kt >= nk1) : pair;
       const unsigned c = F == Form::DX && s ? kt - nk1 : kt;
-      const size_t c0 = (size_t)c * KT;
-      const char* pa = uniform((const char*)a.a[s][rank] +
-                               OA::origin(a.lda, i0) + c * OA::step(a.lda));
-      const size_t ob = OB::origin(a.ldb, j0) + c * OB::step(a.ldb);
-      const char* pb = uniform(
-          (const char*)a.b[kGated || F == Form::DW ? 0 : s][rank] + ob);
-      const char* pu = kGated ? uniform((const char*)a.b[1][rank] + ob) : pb;
-      const uint32_t ga = OA::guard(a.lda, i0, a.ni, c0, a.nc, 0, t);
-      const uint32_t d = lds0 + slot * kBytes;
+      const char* p = uniform((const char*)a.a[s][rank] +
+                              OA::origin(a.lda, i0) + c * OA::step(a.lda));
+      const uint32_t g =
+          OA::guard(a.lda, i0, a.ni, (size_t)c * KT, a.nc, 0, t);
 #pragma unroll
-      for (int n = 0; n < OA::N; ++n)
-        dma16(d + n * kThreads * 16, pa, OA::guarded(va[n], ga));
-#pragma unroll
-      for (int n = 0; n < OB::N; ++n)
-        dma16(d + kBytesA + n * kThreads * 16,
-              kGated && n >= OB::N / 2 ? pu : pb,
-              OB::guarded(vb[n],
-                          OB::guard(a.ldb, j0, a.nj, c0, a.nc, n, t)));
+      for (int n = 0; n < NP; ++n)
+        dma16(lds0 + slot * kSlot + n * kThreads * 16, p,
+              OA::guarded(va[n], g));
     };
+    auto ask_b = [&](unsigned kt, int slot) {
+      const int s = F == Form::DX ? (kt >= nk1) : 0;
+      const unsigned c = F == Form::DX && s ? kt - nk1 : kt;
+      const size_t ob = OB::origin(a.ldb, j0) + c * OB::step(a.ldb);
+      const char* p = uniform((const char*)a.b[s][rank] + ob);
+      const char* u = kGated ? uniform((const char*)a.b[1][rank] + ob) : p;
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        dma16(lds0 + slot * kSlot + n * kThreads * 16,
+              kGated && n >= NP / 2 ? u : p,
+              OB::guarded(vb[n], OB::guard(a.ldb, j0, a.nj, (size_t)c * KT,
+                                           a.nc, n, t)));
+    };
+    auto slot_of = [&](unsigned unit) { return (int)(unit % kSlots); };
     // As in Tiled: zeros past the contraction's end.
-    auto clear = [&](unsigned kt, int slot) {
+    auto clear = [&](unsigned kt) {
       const unsigned c = F == Form::DX && kt >= nk1 ? kt - nk1 : kt;
       if (c < whole) return;
-      LDS char* d = lds + slot * kBytes + t * 16;
+      const size_t c0 = (size_t)c * KT;
+      LDS char* da = lds + slot_of(2 * (kt - k0)) * kSlot + t * 16;
+      LDS char* db = lds + slot_of(2 * (kt - k0) + 1) * kSlot + t * 16;
       int o = t;
       asm volatile("" : "+v"(o));
 #pragma unroll 1
-      for (int n = 0; n < kPieces; ++n)
-        if (n < OA::N ? OA::past((size_t)c * KT, a.nc, n, o)
-                      : OB::past((size_t)c * KT, a.nc, n - OA::N, o))
-          *(LDS i32x4*)(d + n * kThreads * 16) = i32x4{0, 0, 0, 0};
+      for (int n = 0; n < NP; ++n) {
+        if (OA::past(c0, a.nc, n, o))
+          *(LDS i32x4*)(da + n * kThreads * 16) = i32x4{0, 0, 0, 0};
+        if (OB::past(c0, a.nc, n, o))
+          *(LDS i32x4*)(db + n * kThreads * 16) = i32x4{0, 0, 0, 0};
+      }
     };
-    // Waits until this wavefront's pieces of stage kt have landed (`newer`:
-    // all NS - 2 stages after it have been asked for).
-    auto ready = [&](unsigned kt, int slot, bool newer) {
+    // Waits until this wavefront's pieces of tile kt have landed; only A's of
+    // the tile after it (`newer`) have been asked for since.
+    auto ready = [&](unsigned kt, bool newer) {
       if (kt >= k1) return;
       if (newer)
-        asm volatile("s_waitcnt vmcnt(%0)" :: "n"((NS - 2) * kPieces)
-                     : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NP) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      clear(kt, slot);
+      clear(kt);
+    };
+    auto change = [] {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
     };
 
     auto loop = [&](auto with_sums) {
-      int slot = 0;
+      int sa = 0;                          // A's slot; B's is the next
 #pragma unroll 1
       for (unsigned kt = k0; kt < k1; ++kt) {
-        const bool more = kt + NS - 1 < k1;
-        const int next = slot + 1 == NS ? 0 : slot + 1;
-        LDS char* sa = lds + slot * kBytes;
-        LDS char* sb = sa + kBytesA;
-        i32x4 fa[MI], fb[NJ];
+        const int sb = sa + 1 == kSlots ? 0 : sa + 1;
+        const int s2 = sb + 1 == kSlots ? 0 : sb + 1;   // A of the next tile
+        const int s3 = s2 + 1 == kSlots ? 0 : s2 + 1;   // B of it
+        const int s4 = s3 + 1 == kSlots ? 0 : s3 + 1;   // A of the one after
+        LDS char* la = lds + sa * kSlot;
+        LDS char* lb = lds + sb * kSlot;
 #pragma unroll
-        for (int n = 0; n < NJ; ++n)
-          fb[n] = OB::frag(sb, 0, kGated ? (n < NT ? 0 : BJ) + wn * (WN / 2)
-                                         : wn * WN, n % NT, lane);
-#pragma unroll
-        for (int m = 0; m < MI; ++m)
-          fa[m] = OA::frag(sa, 0, wm * WM + m * 16, 0, lane);
-        if (more) issue(kt + NS - 1, slot == 0 ? NS - 1 : slot - 1);
-        if (wm) ready(kt + 1, next, more);
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int m = 0; m < MI; ++m) {
+        for (int ks = 0; ks < 2; ++ks) {
+          i32x4 fa[MI], fb[NJ];
 #pragma unroll
           for (int n = 0; n < NJ; ++n)
-            acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
-          if constexpr (with_sums)
-            if (m % 4 == wn)
-              sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
-                                 fa[m], sum);
+            fb[n] = OB::frag(lb, ks, kGated ? (n < NT ? 0 : BJ) + wn * (WN / 2)
+                                            : wn * WN, n % NT, lane);
+#pragma unroll
+          for (int m = 0; m < MI; ++m)
+            fa[m] = OA::frag(la, ks, wm * WM + m * 16, 0, lane);
+          if (ks == 0) {
+            if (kt + 1 < k1) ask_b(kt + 1, s3);
+          } else {
+            if (kt + 2 < k1) ask_a(kt + 2, s4);
+            if (wm) ready(kt + 1, kt + 2 < k1);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          change();
+          __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+          for (int m = 0; m < MI; ++m) {
+#pragma unroll
+            for (int n = 0; n < NJ; ++n)
+              acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
+            if constexpr (with_sums)
+              if (m % 4 == wn)
+                sum = Elem<T>::mma(
+                    (lane & 15) == m ? Elem<T>::ones() : i32x4{}, fa[m], sum);
+          }
+          __builtin_amdgcn_s_setprio(0);
+          __builtin_amdgcn_sched_barrier(0);
+          if (ks == 1 && !wm) ready(kt + 1, kt + 2 < k1);
+          change();
         }
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!wm) ready(kt + 1, next, more);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        slot = next;
+        sa = s2;
       }
     };
 
     if (k0 < k1) {
-#pragma unroll 1
-      for (int n = 0; n < NS - 1; ++n)
-        if (k0 + n < k1) issue(k0 + n, n);
-      ready(k0, 0, k0 + NS - 2 < k1);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      if (wm) __builtin_amdgcn_s_barrier();   // half a stage behind
+      ask_a(k0, 0);
+      ask_b(k0, 1);
+      if (k0 + 1 < k1) ask_a(k0 + 1, 2);
+      ready(k0, k0 + 1 < k1);
+      change();
+      if (wm) __builtin_amdgcn_s_barrier();   // one phase behind
       if constexpr (F == Form::DW) {
         if (sums)
           loop(Yes{});
