@@ -75,7 +75,11 @@ template <> struct Elem<Type::F32> {
 
 // ---------------------------------------------------------------- activations
 
-__device__ inline float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
+// 1 / x to 1 unit in the last place: a correctly rounded division takes ten
+// instructions, and the results are rounded further or no more exact.
+__device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }
+
+__device__ inline float sigmoid(float z) { return inverse(1.f + __expf(-z)); }
 
 // 0.5 (1 + tanh a) = sigmoid(2 a)
 constexpr float kTanh2 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
@@ -83,43 +87,60 @@ constexpr float kCubic = 0.044715f;
 constexpr float kInvSqrt2 = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
-// The limits at infinity included: below -128 every activation but RELU and
-// NONE is -0 in 32 bits.
-__device__ inline float act_of(int act, float z) {
-  if (act >= (int)Act::GELU) z = z < -128.f ? -128.f : z;
-  switch (act) {
-    case (int)Act::RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case (int)Act::GELU: return 0.5f * z * (1.f + erff(z * kInvSqrt2));
-    case (int)Act::GELU_TANH:
-      return z * sigmoid(kTanh2 * (z + kCubic * z * z * z));
-    case (int)Act::SILU: return z * sigmoid(z);
-    default: return z;
-  }
+// The activations beyond +-128 are z or -0 and their slopes 1 or 0 in 32 bits;
+// z is held there so that infinities give the limits.
+__device__ inline float held(float z) { return z < -128.f ? -128.f : z; }
+
+template <Act A>
+__device__ inline float act_of(float z) {
+  if (A == Act::RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+  if (A == Act::NONE) return z;
+  z = held(z);
+  if (A == Act::GELU) return 0.5f * z * (1.f + erff(z * kInvSqrt2));
+  if (A == Act::GELU_TANH)
+    return z * sigmoid(kTanh2 * (z + kCubic * z * z * z));
+  return z * sigmoid(z);
 }
 
-// act(z) and act'(z); beyond 128 the slopes are 0 and 1
-__device__ inline float slope_of(int act, float z, float* value) {
-  if (act >= (int)Act::GELU) {
-    *value = act_of(act, z);
-    z = z < -128.f ? -128.f : z > 128.f ? 128.f : z;
+// act(z) and act'(z)
+template <Act A>
+__device__ inline float slope_of(float z, float* value) {
+  if (A == Act::NONE) {
+    *value = z;
+    return 1.f;
   }
+  if (A == Act::RELU) {
+    *value = act_of<A>(z);
+    return z > 0.f ? 1.f : (z != z ? z : 0.f);
+  }
+  z = held(z);
+  const float y = z > 128.f ? 128.f : z;
+  if (A == Act::GELU) {
+    const float c = 0.5f * (1.f + erff(y * kInvSqrt2));
+    *value = z * c;
+    return c + y * kInvSqrt2Pi * __expf(-0.5f * y * y);
+  }
+  if (A == Act::GELU_TANH) {
+    const float s = sigmoid(kTanh2 * (y + kCubic * y * y * y));
+    *value = z * s;
+    return s + y * s * (1.f - s) * kTanh2 * (1.f + 3.f * kCubic * y * y);
+  }
+  const float s = sigmoid(y);
+  *value = z * s;
+  return s * (1.f + y * (1.f - s));
+}
+
+// f(activation) with the activation as a type: one branch for many values.
+template <typename Fn>
+__device__ inline void with_act(int act, Fn f) {
   switch (act) {
-    case (int)Act::RELU:
-      *value = act_of(act, z);
-      return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    case (int)Act::GELU: {
-      const float c = 0.5f * (1.f + erff(z * kInvSqrt2));
-      return c + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
-    }
-    case (int)Act::GELU_TANH: {
-      const float s = sigmoid(kTanh2 * (z + kCubic * z * z * z));
-      return s + z * s * (1.f - s) * kTanh2 * (1.f + 3.f * kCubic * z * z);
-    }
-    case (int)Act::SILU: {
-      const float s = sigmoid(z);
-      return s * (1.f + z * (1.f - s));
-    }
-    default: *value = z; return 1.f;
+    case (int)Act::RELU: f(std::integral_constant<Act, Act::RELU>()); break;
+    case (int)Act::GELU: f(std::integral_constant<Act, Act::GELU>()); break;
+    case (int)Act::GELU_TANH:
+      f(std::integral_constant<Act, Act::GELU_TANH>());
+      break;
+    case (int)Act::SILU: f(std::integral_constant<Act, Act::SILU>()); break;
+    default: f(std::integral_constant<Act, Act::NONE>());
   }
 }
 
@@ -411,54 +432,69 @@ __device__ inline void store_out(void* o, size_t at, const float* v, long left,
     store_vals<V, N>((V*)o + at, v, left, wide);
 }
 
+// The biases of N consecutive results from j on: b[0] (GATED: of g), b[1] of u.
+template <Type T, Form F, int N>
+__device__ inline void fetch_bias(Given& a, int rank, size_t j,
+                                  float (&b)[2][N]) {
+  using V = typename Elem<T>::V;
+  if constexpr (F == Form::LINEAR || F == Form::GATED) {
+    const long left = (long)a.nj - (long)j;
+#pragma unroll
+    for (int p = 0; p < (F == Form::GATED ? 2 : 1); ++p) {
+      if (const V* e = (const V*)a.e[p][rank]) {
+        fetch_vals<V, N>(e + j, b[p], left, a.wide_out);
+      } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) b[p][k] = 0.f;
+      }
+    }
+  }
+}
+
 // N consecutive values j .. of row i: bias, activation, residual, rounding,
 // stores.  v: the product's sums (GATED: v of g, u2 of u).
 template <Type T, Form F, int N>
 __device__ inline void finish(Given& a, int rank, int pair, size_t i,
-                              size_t j, float* v, float* u2) {
+                              size_t j, float* v, float* u2,
+                              const float (&b)[2][N]) {
   using V = typename Elem<T>::V;
   const long left = (long)a.nj - (long)j;
   const bool wide = a.wide_out;
   if constexpr (F == Form::LINEAR) {
-    if (const V* b = (const V*)a.e[0][rank]) {
-      float t[N];
-      fetch_vals<V, N>(b + j, t, left, wide);
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[k] += t[k];
-    }
-    if (V* z = (V*)a.o[1][rank])
-      store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
-    if (a.act)
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]);
-    if (const void* r = a.e[1][rank]) {
-      float t[N];
+    const void* r = a.e[1][rank];
+    float t[N];
+    if (r) {
       if (a.out32)
         fetch_vals<float, N>((const float*)r + i * a.lde + j, t, left, wide);
       else
         fetch_vals<V, N>((const V*)r + i * a.lde + j, t, left, wide);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += b[0][k];
+    if (V* z = (V*)a.o[1][rank])
+      store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = act_of<act.value>(v[k]);
+    });
+    if (r) {
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] += t[k];
     }
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else if constexpr (F == Form::GATED) {
-    float t[N];
-    if (const V* b = (const V*)a.e[0][rank]) {
-      fetch_vals<V, N>(b + j, t, left, wide);
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] += t[k];
-    }
-    if (const V* b = (const V*)a.e[1][rank]) {
-      fetch_vals<V, N>(b + j, t, left, wide);
+    for (int k = 0; k < N; ++k) v[k] += b[0][k];
 #pragma unroll
-      for (int k = 0; k < N; ++k) u2[k] += t[k];
-    }
+    for (int k = 0; k < N; ++k) u2[k] += b[1][k];
     if (V* g = (V*)a.o[1][rank])
       store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
     if (V* u = (V*)a.u[0][rank])
       store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = act_of(a.act, v[k]) * u2[k];
+      for (int k = 0; k < N; ++k) v[k] = act_of<act.value>(v[k]) * u2[k];
+    });
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else {
     store_out<N>(a.o[F == Form::DW ? pair : 0][rank], i * a.ldo + j, v, left,
@@ -538,6 +574,12 @@ struct Results {
     constexpr int MH = MI < 4 ? MI : 4, CH = WN / 4, PER = (kGated ? WN / 2 : WN) / 8;
     constexpr int kTurn = CH < 16 ? CH - 1 : 15;   // pieces exchanged by row
     LDS char* mine = lds + wave * (MH * 16 * WN * 4);
+    // a lane's results are all in the same 8 columns
+    static_assert(64 % PER == 0);
+    const int c = lane % PER * 2;
+    const size_t j = jw + c * 4;
+    float bias[2][8];
+    if (a.splits == 1 && j < a.nj) fetch_bias<T, F, 8>(a, rank, j, bias);
     landed<0>();
     __builtin_amdgcn_s_barrier();
 #pragma unroll
@@ -554,10 +596,8 @@ struct Results {
                         (c ^ (r & kTurn)) * 16) = acc[mh + m][n];
         }
 #pragma unroll 1
-      for (int w = lane; w < MH * 16 * PER; w += 64) {
-        const int row = w / PER, c = w % PER * 2;
+      for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
         const size_t i = iw + mh * 16 + row;
-        const size_t j = jw + c * 4;
         if (i >= a.ni || j >= a.nj) continue;
         float v[8], u2[8];
         LDS char* at = mine + row * (WN * 4);
@@ -569,7 +609,7 @@ struct Results {
           *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
         }
         if (a.splits == 1) {
-          finish<T, F, 8>(a, rank, pair, i, j, v, u2);
+          finish<T, F, 8>(a, rank, pair, i, j, v, u2, bias);
         } else {
           // [split][rank][pair or projection][row][column]
           const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
@@ -1153,7 +1193,9 @@ struct Few {
         float va[4], ua[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) va[e] = v[e], ua[e] = u[e];
-        finish<T, F, 4>(a, rank, 0, i, j, va, ua);
+        float bias[2][4];
+        fetch_bias<T, F, 4>(a, rank, j, bias);
+        finish<T, F, 4>(a, rank, 0, i, j, va, ua, bias);
       }
   }
 };
@@ -1317,7 +1359,9 @@ __global__ __launch_bounds__(256) void k_join(Args) {
         for (int k = 0; k < 4; ++k) u2[k] += t[k];
       }
     }
-    finish<T, F, 4>(a, rank, pair, i, j, v, u2);
+    float bias[2][4];
+    fetch_bias<T, F, 4>(a, rank, j, bias);
+    finish<T, F, 4>(a, rank, pair, i, j, v, u2, bias);
   }
   if (F == Form::DW) {
     const size_t n = (size_t)a.ranks * a.pairs * a.ni;
@@ -1352,16 +1396,19 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
     fetch_vals<V, E>(dy + i * a.ldy + j, d, left, a.wide);
     fetch_vals<V, E>(z + i * a.ldz + j, g, left, a.wide);
     if (GATED) fetch_vals<V, E>(u + i * a.ldz + j, s, left, a.wide);
-    for (int k = 0; k < E; ++k) {
-      float v;
-      const float c = slope_of(a.act, g[k], &v);
-      if (GATED) {
-        o[k] = d[k] * v;
-        d[k] = d[k] * s[k] * c;
-      } else {
-        d[k] *= c;
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        float v;
+        const float c = slope_of<act.value>(g[k], &v);
+        if (GATED) {
+          o[k] = d[k] * v;
+          d[k] = d[k] * s[k] * c;
+        } else {
+          d[k] *= c;
+        }
       }
-    }
+    });
     store_vals<V, E>(dz + i * a.ldz + j, d, left, a.wide);
     if (GATED) store_vals<V, E>(du + i * a.ldz + j, o, left, a.wide);
   }
