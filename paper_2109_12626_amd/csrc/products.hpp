@@ -47,6 +47,7 @@ struct Args {
   int splits;                // parts of the contraction
   int waves;                 // few rows: parts of the contraction per
                              // workgroup (0: tiles)
+  int sets;                  // few rows: sets of 16 weight rows per wavefront
   int tile;                  // 64 << tile rows and columns per workgroup
   int fast;                  // A, B: 16-byte rows and whole 16-byte pieces
   int wide_out;              // results, kept values, residual, bias: 16-byte

@@ -205,7 +205,7 @@ int ranks_per_launch(int p) {
 
 // How a product runs.
 struct Shape {
-  int waves, tile, splits;
+  int waves, sets, tile, splits;
   size_t part;           // bytes of workspace
 };
 
@@ -225,26 +225,47 @@ constexpr double kJoinNs = 4000, kJoinRate = 2300;
 constexpr double kStartNs = 2000;      // first loads and last stores
 constexpr size_t kMostPart = (size_t)256 << 20;
 
-// Rows up to which the forward forms take the few-rows kernel: 64 x 4096 x
-// 16384 43 us (tiles: 53), 48 x 4096 x 8192 gated 37 us (53).
+// Rows up to which the forward forms may take the few-rows kernel: 48 x 4096 x
+// 8192 gated 29 us (tiles: 53); half of that in 32 bits (8 x 64 x 2048 x 4096
+// 98 us, in tiles 89).
 constexpr size_t kFewRows = 64;
 
 Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
                size_t nc, int cus, bool split) {
-  if ((f == Form::LINEAR || f == Form::GATED) && ni <= kFewRows) {
-    // Wavefronts per workgroup: 16 per CU in all, 8 once there are 4 (each
-    // takes a part of the contraction, at least a chunk of 512 bytes).
-    // Measured with 16 / 8 per CU: 8 x 1 x 4096 x 2048 gated 42.4 / 46.2 us,
-    // 8 x 16 x 2048 x 4096 28.7 / 31.5 us; 16 x 4096 x 8192 gated 26.3 (8
-    // wavefronts) / 23.5 us (4).
-    const size_t cols = f == Form::GATED || ni <= 16 ? 16 : 32;
-    const size_t tiles = (nj + cols - 1) / cols * ranks;
-    const size_t chunks = nc / (t == Type::F32 ? 128 : 256);
-    int w = 1;
-    while (w < 8 && tiles * w < (size_t)cus * (w < 4 ? 16 : 8) &&
-           chunks >= (size_t)w * 2)
-      w *= 2;
-    return {w, 0, 1, 0};
+  if ((f == Form::LINEAR || f == Form::GATED) &&
+      ni <= (t == Type::F32 ? kFewRows / 2 : kFewRows)) {
+    // Sets of 16 weight rows per wavefront.  More share x's loads, fewer give
+    // more wavefronts: 16 x 4096 x 8192 15.1 us with one set, 13.3 with two; 16
+    // x 4096 x 4096 9.6 with one, 11.4 with two.  From 17 rows on four sets
+    // need a workgroup per CU (40 x 4096 x 16384 28.7 us against 32.4 with two
+    // and 36.5 in tiles); else two up to 32 rows (24 x 4096 x 8192 15.0 us, in
+    // tiles 18.2), and tiles beyond (40 x 4096 x 8192 18.7 and 17.9).
+    const size_t least = f == Form::GATED ? 2 : 1;
+    auto groups = [&](size_t sets) {
+      const size_t cols = 16 * sets / least;
+      return (nj + cols - 1) / cols * ranks;
+    };
+    size_t sets = 0;
+    if (ni <= 16)
+      sets = groups(2 * least) >= (size_t)cus ? 2 * least : least;
+    else if (groups(4) >= (size_t)cus)
+      sets = 4;
+    else if (ni <= 32)
+      sets = 2;
+    if (sets) {
+      // Wavefronts per workgroup: 16 per CU in all (8 with more sets), half
+      // of that once there are 4 and each has at most 4 chunks of 512 bytes.
+      // 8 x 1 x 4096 x 2048 gated: 42.9 us with 4, 47.0 with 2, 45.7 with 8.
+      const size_t chunks = nc / (t == Type::F32 ? 128 : 256);
+      const size_t many = (size_t)cus * (sets > least ? 8 : 16);
+      const size_t n = groups(sets);
+      int w = 1;
+      while (w < 8 && chunks >= (size_t)w * 2 &&
+             (w < 4 ? n * w < many || chunks > (size_t)w * 4
+                    : n * w < many / 2))
+        w *= 2;
+      return {w, (int)sets, 0, 1, 0};
+    }
   }
   const size_t kt = t == Type::F32 ? 32 : 64;
   const size_t nk = (nc + kt - 1) / kt * (f == Form::DX ? pairs : 1);
@@ -252,7 +273,7 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
                        (f == Form::GATED ? 2 : 1);
   const int tiles = t == Type::F32 ? 2 : 3;
   const TileCost* cost = t == Type::F32 ? kCost32 : kCost16;
-  Shape best = {0, 0, 1, 0};
+  Shape best = {0, 0, 0, 1, 0};
   double least = 0;
   for (int tile = 0; tile < tiles; ++tile) {
     const size_t bm = (size_t)64 << tile, bn = f == Form::GATED ? bm / 2 : bm;
@@ -270,7 +291,7 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
       if (s > 1) ns += kJoinNs + part / kJoinRate;
       if (least == 0 || ns < least) {
         least = ns;
-        best = {0, tile, s, part};
+        best = {0, 0, tile, s, part};
       }
     }
   }
@@ -343,6 +364,7 @@ int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
   const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
                            ws != nullptr);
   a->waves = s.waves;
+  a->sets = s.sets;
   a->tile = s.tile;
   a->splits = s.splits;
   a->part = (float*)ws;

@@ -60,11 +60,13 @@ template <> struct Elem<Type::F32> {
   using V = float;
   // Component s of the four lane groups' pieces makes one product of depth 4;
   // both operands order the contraction alike.
+  static __device__ f32x4 part(i32x4 a, i32x4 b, f32x4 c, int s) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(
+        __builtin_bit_cast(f32x4, a)[s], __builtin_bit_cast(f32x4, b)[s], c, 0,
+        0, 0);
+  }
   static __device__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
-    const f32x4 x = __builtin_bit_cast(f32x4, a),
-                y = __builtin_bit_cast(f32x4, b);
-    for (int s = 0; s < 4; ++s)
-      c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], y[s], c, 0, 0, 0);
+    for (int s = 0; s < 4; ++s) c = part(a, b, c, s);
     return c;
   }
   static __device__ i32x4 ones() {
@@ -72,6 +74,21 @@ template <> struct Elem<Type::F32> {
     return __builtin_bit_cast(i32x4, v);
   }
 };
+
+// c[n] += a[n] b for N independent sums, in an order that leaves time between
+// two products into one sum.
+template <Type T, int N>
+__device__ inline void mma_row(const i32x4 (&a)[N], i32x4 b, f32x4 (&c)[N]) {
+  if constexpr (T == Type::F32) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int n = 0; n < N; ++n) c[n] = Elem<T>::part(a[n], b, c[n], s);
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n) c[n] = Elem<T>::mma(a[n], b, c[n]);
+  }
+}
 
 // ---------------------------------------------------------------- activations
 
@@ -87,6 +104,21 @@ constexpr float kCubic = 0.044715f;
 constexpr float kInvSqrt2 = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
+// (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2): Abramowitz and Stegun 7.1.26,
+// 7.5e-8 off at most.
+__device__ inline float normal_cdf(float z, float* density) {
+  const float x = fabsf(z) * kInvSqrt2;
+  const float t = inverse(fmaf(0.3275911f, x, 1.f));
+  const float e = __expf(-x * x);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * e;
+  *density = e;
+  return z < 0.f ? tail : 1.f - tail;
+}
+
 // The activations beyond +-128 are z or -0 and their slopes 1 or 0 in 32 bits;
 // z is held there so that infinities give the limits.
 __device__ inline float held(float z) { return z < -128.f ? -128.f : z; }
@@ -96,7 +128,10 @@ __device__ inline float act_of(float z) {
   if (A == Act::RELU) return z > 0.f ? z : (z != z ? z : 0.f);
   if (A == Act::NONE) return z;
   z = held(z);
-  if (A == Act::GELU) return 0.5f * z * (1.f + erff(z * kInvSqrt2));
+  if (A == Act::GELU) {
+    float e;
+    return z * normal_cdf(z, &e);
+  }
   if (A == Act::GELU_TANH)
     return z * sigmoid(kTanh2 * (z + kCubic * z * z * z));
   return z * sigmoid(z);
@@ -116,9 +151,10 @@ __device__ inline float slope_of(float z, float* value) {
   z = held(z);
   const float y = z > 128.f ? 128.f : z;
   if (A == Act::GELU) {
-    const float c = 0.5f * (1.f + erff(y * kInvSqrt2));
+    float e;
+    const float c = normal_cdf(y, &e);
     *value = z * c;
-    return c + y * kInvSqrt2Pi * __expf(-0.5f * y * y);
+    return c + y * kInvSqrt2Pi * e;
   }
   if (A == Act::GELU_TANH) {
     const float s = sigmoid(kTanh2 * (y + kCubic * y * y * y));
@@ -786,9 +822,7 @@ struct Tiled {
       fa[m] = OA::frag(lds + buf * kBytes, ks, wm * WM + m * 16, 0, lane);
     };
     auto multiply = [&](int m, int ks, auto with_sums) {
-#pragma unroll
-      for (int n = 0; n < NJ; ++n)
-        acc[m][n] = Elem<T>::mma(fb[ks][n], fa[m], acc[m][n]);
+      mma_row<T>(fb[ks], fa[m], acc[m]);
       // row m of `sum`: sums of A's rows m * 16 .., by the wavefronts that
       // share them in turn
       if constexpr (with_sums)
@@ -1080,19 +1114,18 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
 
 // ---------------------------------------------------------------- few rows
 
-// Few rows of x (MT tiles of 16): a wavefront takes 16 or 32 rows of w (GATED:
-// 16 of each) and one of S parts of the contraction, straight from memory to
+// Few rows of x (MT tiles of 16): a wavefront takes NW x 16 rows of w (GATED:
+// half of them of each) and one of S parts of the contraction, straight from memory to
 // the matrix cores' registers, U steps of loads at a time; the workgroup's S
 // wavefronts join their sums in LDS, in order.  Every weight is read once, by
 // all lanes of a wavefront side by side (64 bytes of 16 rows a load); x is
 // small and comes from the caches.
-template <Type T, Form F, bool FAST, int MT, int S>
+template <Type T, Form F, bool FAST, int MT, int NW, int S>
 struct Few {
   using V = typename Elem<T>::V;
   static constexpr int E = 16 / sizeof(V), K = 4 * E;   // per piece, per step
   static constexpr bool kGated = F == Form::GATED;
-  static constexpr int NW = kGated || MT > 1 ? 2 : 1;
-  static constexpr int BJ = kGated ? 16 : 16 * NW;
+  static constexpr int BJ = kGated ? 8 * NW : 16 * NW;
   static constexpr int U = MT * NW <= 2 ? 8 : 4;
 
   static __device__ void run(Given& a, LDS char* lds) {
@@ -1108,9 +1141,9 @@ struct Few {
     const V* x[MT];
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
-      size_t j = j0 + (kGated ? 0 : n * 16) + r;
+      size_t j = j0 + (kGated ? n / 2 : n) * 16 + r;
       if (j >= a.nj) j = a.nj - 1;
-      w[n] = (const V*)a.b[kGated ? n : 0][rank] + j * a.ldb + q * E;
+      w[n] = (const V*)a.b[kGated ? n % 2 : 0][rank] + j * a.ldb + q * E;
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -1173,19 +1206,20 @@ struct Few {
       __syncthreads();
     }
     // result tile (m, n): wavefront tile % S
-    constexpr int NO = kGated ? 1 : NW;
+    constexpr int NO = kGated ? NW / 2 : NW, NS = kGated ? 2 : 1;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int n = 0; n < NO; ++n) {
         if ((m * NO + n) % S != wave) continue;
-        f32x4 v = acc[m][n], u = acc[m][NW - 1];
+        const int w = m * NW + n * NS;
+        f32x4 v = acc[m][n * NS], u = acc[m][n * NS + NS - 1];
         if (S > 1) {
-          v = part[0][m * NW + n][lane];
-          for (int k = 1; k < S; ++k) v += part[k][m * NW + n][lane];
+          v = part[0][w][lane];
+          for (int k = 1; k < S; ++k) v += part[k][w][lane];
           if (kGated) {
-            u = part[0][m * NW + 1][lane];
-            for (int k = 1; k < S; ++k) u += part[k][m * NW + 1][lane];
+            u = part[0][w + 1][lane];
+            for (int k = 1; k < S; ++k) u += part[k][w + 1][lane];
           }
         }
         const size_t i = m * 16 + r, j = j0 + n * 16 + q * 4;
@@ -1205,13 +1239,13 @@ struct Few {
 // than 64 bytes of 16 rows (a copy of the loads alone: 6.5 against 5.9 TB/s
 // at 268 MB); x goes to registers.  Each wavefront has two chunks of LDS of
 // its own and needs no barrier: while it multiplies one chunk the next is on
-// its way.  Two sets of weight rows (GATED, or MT > 1) alternate and share x.
-template <Type T, Form F, int MT, int S>
+// its way.  The NW sets of weight rows take turns and share x.
+template <Type T, Form F, int MT, int NW, int S>
 struct FewFast {
   using V = typename Elem<T>::V;
-  using Old = Few<T, F, true, MT, S>;
+  using Old = Few<T, F, true, MT, NW, S>;
   static constexpr bool kGated = F == Form::GATED;
-  static constexpr int NW = Old::NW, BJ = Old::BJ, E = Old::E;
+  static constexpr int BJ = Old::BJ, E = Old::E;
   static constexpr int kRow = 512, kChunk = 16 * kRow;
   static constexpr int KC = kRow / (int)sizeof(V);   // contraction per chunk
   static constexpr int U = kRow / 64;                // steps per chunk
@@ -1225,24 +1259,27 @@ struct FewFast {
     const unsigned chunks = (unsigned)((a.nc + KC - 1) / KC);
     const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
                    c1 = uniform((unsigned)((uint64_t)chunks * (wave + 1) / S));
-    // load h: rows 2 h, 2 h + 1; pieces exchanged by the row
+    // load h: rows 2 h, 2 h + 1; pieces exchanged by the row.  Rows past the
+    // last give its last piece.
     const char* base[NW];
-    uint32_t off[NW][8];
+    uint32_t cap[NW], off[8];
     const int slot = lane & 31;
+    auto set_row = [&](int n) {
+      return j0 + (kGated ? n / 2 : n) * 16;
+    };
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
-      const size_t jn = j0 + (kGated ? 0 : n * 16);
-      const size_t first = jn < a.nj ? jn : a.nj - 1;
-      base[n] = uniform((const char*)a.b[kGated ? n : 0][rank] +
+      const size_t jn = set_row(n), first = jn < a.nj ? jn : a.nj - 1;
+      const size_t most = a.nj - first - 1;
+      base[n] = uniform((const char*)a.b[kGated ? n % 2 : 0][rank] +
                         first * a.ldb * sizeof(V));
+      cap[n] = uniform((uint32_t)((most < 15 ? most : 15) * a.ldb *
+                                  sizeof(V)) + kRow - 16);
+    }
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const int row = h * 2 + (lane >> 5);
-        const size_t most = a.nj - first - 1;
-        const size_t at = (size_t)row < most ? row : most;
-        off[n][h] = (uint32_t)(at * a.ldb * sizeof(V)) +
-                    (slot ^ (row & 7)) * 16;
-      }
+    for (int h = 0; h < 8; ++h) {
+      const int row = h * 2 + (lane >> 5);
+      off[h] = (uint32_t)(row * a.ldb * sizeof(V)) + (slot ^ (row & 7)) * 16;
     }
     const uint32_t mine = (uint32_t)(uintptr_t)lds + wave * (2 * kChunk);
     LDS char* const src = lds + wave * (2 * kChunk);
@@ -1255,17 +1292,27 @@ struct FewFast {
     }
     auto issue = [&](unsigned c, int n, int buf) {
       const char* b = uniform(base[n] + (size_t)c * kRow);
-      const uint32_t d = mine + buf * kChunk;
+      const uint32_t d = uniform(mine + buf * kChunk);
       if ((size_t)(c + 1) * KC <= a.nc) {
 #pragma unroll
-        for (int h = 0; h < 8; ++h) dma16_once(d + h * 1024, b, off[n][h]);
+        for (int h = 0; h < 8; ++h)
+          dma16_once(d + h * 1024, b, off[h] < cap[n] ? off[h] : cap[n]);
       } else {
-#pragma unroll
+        // the contraction's last chunk: zeros past its end
+        const size_t left = a.nj - 1;
+        int o = lane;
+        asm volatile("" : "+v"(o));
+#pragma unroll 1
         for (int h = 0; h < 8; ++h) {
-          const int row = h * 2 + (lane >> 5);
-          const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * E;
-          dma16_at(d + h * 1024,
-                   k < a.nc ? b + off[n][h] : (const char*)&g_zero);
+          const int row = h * 2 + (o >> 5);
+          size_t at = set_row(n) + row;
+          if (at > left) at = left;
+          const size_t k = (size_t)c * KC + (size_t)((o & 31) ^ (row & 7)) * E;
+          dma16_at(uniform(d + h * 1024),
+                   k < a.nc ? (const char*)((const V*)
+                                  a.b[kGated ? n % 2 : 0][rank] + at * a.ldb +
+                                  k)
+                            : (const char*)&g_zero);
         }
       }
     };
@@ -1320,14 +1367,14 @@ struct FewFast {
   }
 };
 
-template <Type T, Form F, bool FAST, int MT, int S>
+template <Type T, Form F, bool FAST, int MT, int NW, int S>
 __global__ __launch_bounds__(S * 64) void k_few(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
   if constexpr (FAST)
-    FewFast<T, F, MT, S>::run(a, (LDS char*)lds);
+    FewFast<T, F, MT, NW, S>::run(a, (LDS char*)lds);
   else
-    Few<T, F, FAST, MT, S>::run(a, (LDS char*)lds);
+    Few<T, F, FAST, MT, NW, S>::run(a, (LDS char*)lds);
 }
 
 // Joins the parts of a split contraction in their order and finishes: 4
@@ -1440,16 +1487,16 @@ hipError_t go(const Args& a, hipStream_t stream) {
                       K::kThreads, 2 * K::kBytes, stream);
 }
 
-template <Type T, Form F, bool FAST, int MT, int S>
+template <Type T, Form F, bool FAST, int MT, int NW, int S>
 hipError_t go_few(const Args& a, hipStream_t stream) {
-  using K = Few<T, F, FAST, MT, S>;
+  using K = Few<T, F, FAST, MT, NW, S>;
   const size_t n = (a.nj + K::BJ - 1) / K::BJ * a.ranks;
   if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
-  const size_t parts = S > 1 ? (size_t)S * MT * K::NW * 1024 : 0;
+  const size_t parts = S > 1 ? (size_t)S * MT * NW * 1024 : 0;
   const size_t bytes =
-      FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, S>::kChunk)
+      FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, NW, S>::kChunk)
            : parts;
-  auto k = k_few<T, F, FAST, MT, S>;
+  auto k = k_few<T, F, FAST, MT, NW, S>;
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -1460,24 +1507,40 @@ hipError_t go_few(const Args& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <Type T, Form F, bool FAST, int MT>
-hipError_t pick_few(const Args& a, hipStream_t stream) {
+template <Type T, Form F, bool FAST, int MT, int NW>
+hipError_t pick_waves(const Args& a, hipStream_t stream) {
   switch (a.waves) {
-    case 1: return go_few<T, F, FAST, MT, 1>(a, stream);
-    case 2: return go_few<T, F, FAST, MT, 2>(a, stream);
-    case 4: return go_few<T, F, FAST, MT, 4>(a, stream);
-    default: return go_few<T, F, FAST, MT, 8>(a, stream);
+    case 1: return go_few<T, F, FAST, MT, NW, 1>(a, stream);
+    case 2: return go_few<T, F, FAST, MT, NW, 2>(a, stream);
+    case 4: return go_few<T, F, FAST, MT, NW, 4>(a, stream);
+    default: return go_few<T, F, FAST, MT, NW, 8>(a, stream);
   }
+}
+
+// Sets of 16 weight rows per wavefront: few_sets() of them.
+template <Type T, Form F, bool FAST>
+hipError_t pick_few(const Args& a, hipStream_t stream) {
+  constexpr int kOne = F == Form::GATED ? 2 : 1;
+  if (a.ni <= 16) {
+    if (a.sets == kOne) return pick_waves<T, F, FAST, 1, kOne>(a, stream);
+    return pick_waves<T, F, FAST, 1, 2 * kOne>(a, stream);
+  }
+  if (a.ni <= 32) {
+    if (a.sets == 2) return pick_waves<T, F, FAST, 2, 2>(a, stream);
+    return pick_waves<T, F, FAST, 2, 4>(a, stream);
+  }
+  if (a.ni <= 48) {
+    if (a.sets == 2) return pick_waves<T, F, FAST, 3, 2>(a, stream);
+    return pick_waves<T, F, FAST, 3, 4>(a, stream);
+  }
+  if (a.sets == 2) return pick_waves<T, F, FAST, 4, 2>(a, stream);
+  return pick_waves<T, F, FAST, 4, 4>(a, stream);
 }
 
 template <Type T, Form F, bool FAST>
 hipError_t pick(const Args& a, hipStream_t stream) {
   if constexpr (F == Form::LINEAR || F == Form::GATED)
-    if (a.waves) {
-      if (a.ni <= 16) return pick_few<T, F, FAST, 1>(a, stream);
-      if (a.ni <= 32) return pick_few<T, F, FAST, 2>(a, stream);
-      return pick_few<T, F, FAST, 4>(a, stream);
-    }
+    if (a.waves) return pick_few<T, F, FAST>(a, stream);
   if constexpr (T != Type::F32 && FAST)
     if (a.tile == 2) {
       using K = PingPong<T, F>;
