@@ -1,5 +1,5 @@
-"""Builds libdpar.so in place: HIP kernels for gfx950 with hipcc, host C++
-with g++, linked by hipcc.  ``python -m paper_2109_12626_amd.build``."""
+"""Builds libdpar.so and libdpar_products.so (the layer products' kernels) in
+place: HIP kernels for gfx950 with hipcc, host C++ with g++, linked by hipcc.  ``python -m paper_2109_12626_amd.build``."""
 
 import concurrent.futures
 import os
@@ -21,8 +21,9 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-result",
 ]
-HIP_SOURCES = ["kernels.hip", "products_bf16.hip", "products_f16.hip",
-               "products_f32.hip"]
+PRODUCT_SOURCES = ["products_bf16.hip", "products_f16.hip",
+                   "products_f32.hip"]
+PRODUCTS = "libdpar_products.so"
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
               "-Wno-unused-parameter", "-D__HIP_PLATFORM_AMD__"]
 
@@ -38,6 +39,14 @@ def _run_all(cmds):
     with concurrent.futures.ThreadPoolExecutor(max(1, jobs)) as pool:
         for done in [pool.submit(_run, c) for c in cmds]:
             done.result()
+
+
+def _link(hipcc, lib, objs, flags, libs, soname=None):
+    tmp = lib + ".tmp"
+    _run([hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}"] + flags
+         + ["-o", tmp] + objs + libs
+         + [f"-Wl,-soname,{soname or os.path.basename(lib)}"])
+    os.replace(tmp, lib)
 
 
 def build(verbose=True, out=None, defines=(), host_sanitize=False):
@@ -60,20 +69,22 @@ def build(verbose=True, out=None, defines=(), host_sanitize=False):
         _run(["g++"] + HOST_FLAGS + san + inc +
              ["-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    cmds = []
-    for src in HIP_SOURCES:
+    cmds, products = [], []
+    for src in ["kernels.hip"] + PRODUCT_SOURCES:
         obj = os.path.join(build_dir, src + ".o")
         cmds.append([hipcc] + HIP_FLAGS + [f"-D{d}" for d in defines] + inc
                     + ["-c", os.path.join(CSRC, src), "-o", obj])
-        objs.append(obj)
+        (products if src in PRODUCT_SOURCES else objs).append(obj)
     _run_all(cmds)
     lib = LIB if out is None else out
-    tmp = lib + ".tmp"
     link_san = (["-Xarch_host", "-fsanitize=address",
                  "-Xarch_host", "-fsanitize=undefined"] if host_sanitize else [])
-    _run([hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}"] + link_san
-         + ["-o", tmp] + objs + ["-Wl,-soname,libdpar.so"])
-    os.replace(tmp, lib)
+    # the layer products' kernels are a library of their own beside libdpar.so
+    where = os.path.dirname(os.path.abspath(lib))
+    _link(hipcc, os.path.join(where, PRODUCTS), products, link_san, [])
+    _link(hipcc, lib, objs, link_san,
+          [os.path.join(where, PRODUCTS), "-Wl,-rpath,$ORIGIN"],
+          soname="libdpar.so")
     return lib
 
 

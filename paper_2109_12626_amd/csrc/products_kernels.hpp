@@ -96,6 +96,13 @@ __device__ inline void mma_row(const i32x4 (&a)[N], i32x4 b, f32x4 (&c)[N]) {
 // instructions, and the results are rounded further or no more exact.
 __device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }
 
+// 1 / (1 + exp(-z)); *both: its product with 1 minus it.  From exp(-|z|), so
+// that neither end loses what 1 - (almost 1) would.
+__device__ inline float sigmoid(float z, float* both) {
+  const float e = __expf(-fabsf(z)), big = inverse(1.f + e), small = e * big;
+  *both = big * small;
+  return z < 0.f ? small : big;
+}
 __device__ inline float sigmoid(float z) { return inverse(1.f + __expf(-z)); }
 
 // 0.5 (1 + tanh a) = sigmoid(2 a)
@@ -157,13 +164,15 @@ __device__ inline float slope_of(float z, float* value) {
     return c + y * kInvSqrt2Pi * e;
   }
   if (A == Act::GELU_TANH) {
-    const float s = sigmoid(kTanh2 * (y + kCubic * y * y * y));
+    float both;
+    const float s = sigmoid(kTanh2 * (y + kCubic * y * y * y), &both);
     *value = z * s;
-    return s + y * s * (1.f - s) * kTanh2 * (1.f + 3.f * kCubic * y * y);
+    return s + y * both * kTanh2 * (1.f + 3.f * kCubic * y * y);
   }
-  const float s = sigmoid(y);
+  float both;
+  const float s = sigmoid(y, &both);
   *value = z * s;
-  return s * (1.f + y * (1.f - s));
+  return s + y * both;
 }
 
 // f(activation) with the activation as a type: one branch for many values.

@@ -382,3 +382,154 @@ def allreduce(x, y=None, dtype=None, op="sum", b=0, exec="auto", stream=None,
         stream = torch.cuda.current_stream(sample.device)
     dpar_allreduce_opt(xs, ys, p, m, dtype, op, b, alg, exec, 0, -1, stream)
     return y
+
+
+# Tensor front ends of the layer products.  x, dy, dh: [p, rows, ...] or, for
+# all ranks alike or one rank, [rows, ...]; weights [p, out, in] or [out, in];
+# biases [p, out] or [out]; a residual like the result.  Rows may be any
+# distance apart; the values of a row are consecutive.  The results are new
+# tensors [p, ...] (without the first dimension if w has none).  Only marshals
+# addresses: every product runs in the library's kernels.
+
+_NAMES = {torch.float32: "float32", torch.bfloat16: "bfloat16",
+          torch.float16: "float16"}
+
+
+class _Call:
+    """Shapes, row distances and addresses of one call's tensors."""
+
+    def __init__(self, w, rows_, out_dtype, act):
+        self.flat = w.dim() == 2
+        self.p = 1 if self.flat else w.shape[0]
+        self.n_out, self.n_in = w.shape[-2:]
+        self.rows = rows_
+        self.dtype = w.dtype
+        self.out_dtype = w.dtype if out_dtype is None else out_dtype
+        if w.dtype not in _NAMES or self.out_dtype not in _NAMES:
+            raise ValueError(f"types {w.dtype}, {self.out_dtype}")
+        self.opt = product_options(rows_, self.n_in, self.n_out,
+                                   _NAMES[w.dtype], _NAMES[self.out_dtype],
+                                   act)
+        self.device = w.device
+
+    def given(self, t, name, shape, ld=None, dtype=None):
+        """Addresses of an operand's ranks; sets its row distance."""
+        if t is None:
+            return None
+        if t.device != self.device or t.dtype != (dtype or self.dtype):
+            raise ValueError(f"{name}: {t.dtype} on {t.device}")
+        one = t.dim() == len(shape)
+        if tuple(t.shape[-len(shape):]) != shape or \
+                not (one or (t.dim() == len(shape) + 1
+                             and t.shape[0] == self.p)):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, want "
+                             f"{shape} or {(self.p,) + shape}")
+        if one and self.p > 1 and name not in ("x", "dy", "dh"):
+            raise ValueError(f"{name}: one matrix for {self.p} ranks")
+        if shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: values of a row are not consecutive")
+        if ld is not None:
+            far = t.stride(-2) if shape[0] > 1 else shape[1]
+            if far < 0:
+                raise ValueError(f"{name}: negative row distance")
+            if getattr(self.opt, ld) not in (0, far):
+                raise ValueError(f"{name}: another row distance than its "
+                                 "companion's")
+            setattr(self.opt, ld, far)
+        if one:
+            return pointers([t.data_ptr()] * self.p)
+        return rows(t)
+
+    def made(self, *shape, dtype=None):
+        return torch.empty((self.p,) + shape, dtype=dtype or self.out_dtype,
+                           device=self.device)
+
+    def run(self, call, fn, arrays):
+        n = dpar_product_workspace(call, self.p, self.opt)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device) \
+            if n else None
+        fn(*arrays, self.p, self.opt, ws, n,
+           torch.cuda.current_stream(self.device))
+
+    def result(self, t):
+        return t[0] if self.flat and t is not None else t
+
+
+def _addresses(t):
+    return None if t is None else rows(t)
+
+
+def linear(x, w, bias=None, residual=None, act="none", out_dtype=None,
+           keep=False):
+    """act(x w^T + bias) + residual, and with keep=True the value before the
+    activation too."""
+    c = _Call(w, x.shape[-2], out_dtype, act)
+    arrays = [c.given(x, "x", (c.rows, c.n_in), "ldx"),
+              c.given(w, "w", (c.n_out, c.n_in), "ldw"),
+              c.given(bias, "bias", (c.n_out,)),
+              c.given(residual, "residual", (c.rows, c.n_out), "ldr",
+                      c.out_dtype)]
+    y = c.made(c.rows, c.n_out)
+    z = c.made(c.rows, c.n_out, dtype=c.dtype) if keep else None
+    c.run("linear", dpar_linear, arrays + [_addresses(y), _addresses(z)])
+    return (c.result(y), c.result(z)) if keep else c.result(y)
+
+
+def linear_backward(dy, x, w, z=None, act="none", out_dtype=None, bias=False):
+    """(dx, dw), with bias=True (dx, dw, dbias); z: what linear() kept."""
+    c = _Call(w, x.shape[-2], out_dtype, act)
+    arrays = [c.given(dy, "dy", (c.rows, c.n_out), "ldy"),
+              c.given(x, "x", (c.rows, c.n_in), "ldx"),
+              c.given(w, "w", (c.n_out, c.n_in), "ldw")]
+    if act != "none":
+        if z is None:
+            raise ValueError("an activation's slope needs z")
+        z = z.contiguous()
+    else:
+        z = None
+    arrays.append(c.given(z, "z", (c.rows, c.n_out), "ldz"))
+    dx, dw = c.made(c.rows, c.n_in), c.made(c.n_out, c.n_in)
+    db = c.made(c.n_out) if bias else None
+    dz = None if z is None else c.made(c.rows, c.n_out, dtype=c.dtype)
+    c.run("linear_backward", dpar_linear_backward,
+          arrays + [_addresses(t) for t in (dx, dw, db, dz)])
+    out = (dx, dw, db) if bias else (dx, dw)
+    return tuple(c.result(t) for t in out)
+
+
+def gated(x, wg, wu, bg=None, bu=None, act="silu", out_dtype=None, keep=False):
+    """act(x wg^T + bg) * (x wu^T + bu), and with keep=True both projections
+    too."""
+    c = _Call(wg, x.shape[-2], out_dtype, act)
+    arrays = [c.given(x, "x", (c.rows, c.n_in), "ldx"),
+              c.given(wg, "wg", (c.n_out, c.n_in), "ldw"),
+              c.given(wu, "wu", (c.n_out, c.n_in), "ldw"),
+              c.given(bg, "bg", (c.n_out,)), c.given(bu, "bu", (c.n_out,))]
+    h = c.made(c.rows, c.n_out)
+    g, u = (c.made(c.rows, c.n_out, dtype=c.dtype) if keep else None
+            for _ in range(2))
+    c.run("gated", dpar_gated, arrays + [_addresses(t) for t in (h, g, u)])
+    out = (h, g, u) if keep else (h,)
+    return tuple(c.result(t) for t in out) if keep else c.result(h)
+
+
+def gated_backward(dh, x, wg, wu, g, u, act="silu", out_dtype=None,
+                   bias=False):
+    """(dx, dwg, dwu), with bias=True (dx, dwg, dwu, dbg, dbu); g, u: what
+    gated() kept."""
+    c = _Call(wg, x.shape[-2], out_dtype, act)
+    g, u = g.contiguous(), u.contiguous()
+    arrays = [c.given(dh, "dh", (c.rows, c.n_out), "ldy"),
+              c.given(x, "x", (c.rows, c.n_in), "ldx"),
+              c.given(wg, "wg", (c.n_out, c.n_in), "ldw"),
+              c.given(wu, "wu", (c.n_out, c.n_in), "ldw"),
+              c.given(g, "g", (c.rows, c.n_out), "ldz"),
+              c.given(u, "u", (c.rows, c.n_out), "ldz")]
+    dx = c.made(c.rows, c.n_in)
+    dwg, dwu = c.made(c.n_out, c.n_in), c.made(c.n_out, c.n_in)
+    dbg, dbu = (c.made(c.n_out) if bias else None for _ in range(2))
+    dg, du = (c.made(c.rows, c.n_out, dtype=c.dtype) for _ in range(2))
+    c.run("gated_backward", dpar_gated_backward,
+          arrays + [_addresses(t) for t in (dx, dwg, dwu, dbg, dbu, dg, du)])
+    out = (dx, dwg, dwu, dbg, dbu) if bias else (dx, dwg, dwu)
+    return tuple(c.result(t) for t in out)
