@@ -48,7 +48,9 @@ struct Args {
   int waves;                 // few rows: parts of the contraction per
                              // workgroup (0: tiles)
   int sets;                  // few rows: sets of 16 weight rows per wavefront
-  int tile;                  // 64 << tile rows and columns per workgroup
+  int tile;                  // results per workgroup: 64 x 64 with two (0)
+                             // or four (1) tiles in LDS, 128 x 128, 256 x
+                             // 128, 256 x 256
   int fast;                  // A, B: 16-byte rows and whole 16-byte pieces
   int wide_out;              // results, kept values, residual, bias: 16-byte
                              // pieces

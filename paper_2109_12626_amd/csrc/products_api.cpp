@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -217,8 +218,19 @@ struct TileCost {
   double rate, alone;
   int resident;
 };
-constexpr TileCost kCost16[] = {{220, 500, 5}, {610, 800, 2}, {1850, 1450, 1}};
-constexpr TileCost kCost32[] = {{530, 700, 5}, {2100, 2100, 2}};
+// 64 x 64 with two and with four tiles in LDS, 128 x 128, 256 x 128, 256 x 256;
+// the last two for 16-bit operands of whole aligned pieces only, and other
+// operands have no four-buffer form.
+constexpr int kTiles = 5;
+constexpr size_t kTileRows[kTiles] = {64, 64, 128, 256, 256},
+                 kTileCols[kTiles] = {64, 64, 128, 128, 256};
+constexpr TileCost kFast16[kTiles] = {
+    {220, 500, 5}, {270, 400, 2}, {610, 800, 2}, {1050, 950, 1},
+    {1600, 1200, 1}};
+constexpr TileCost kFast32[kTiles] = {
+    {530, 700, 5}, {600, 600, 2}, {2100, 2200, 2}};
+constexpr TileCost kSlow16[kTiles] = {{400, 1000, 4}, {}, {850, 1500, 2}};
+constexpr TileCost kSlow32[kTiles] = {{650, 1000, 4}, {}, {2400, 2700, 2}};
 // Joining a split contraction: a second launch, and its bytes (written by the
 // first) per ns.
 constexpr double kJoinNs = 4000, kJoinRate = 2300;
@@ -231,7 +243,7 @@ constexpr size_t kMostPart = (size_t)256 << 20;
 constexpr size_t kFewRows = 64;
 
 Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
-               size_t nc, int cus, bool split) {
+               size_t nc, int cus, bool split, bool fast) {
   if ((f == Form::LINEAR || f == Form::GATED) &&
       ni <= (t == Type::F32 ? kFewRows / 2 : kFewRows)) {
     // Sets of 16 weight rows per wavefront.  More share x's loads, fewer give
@@ -271,12 +283,14 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
   const size_t nk = (nc + kt - 1) / kt * (f == Form::DX ? pairs : 1);
   const size_t cells = ni * nj * ranks * (f == Form::DW ? pairs : 1) *
                        (f == Form::GATED ? 2 : 1);
-  const int tiles = t == Type::F32 ? 2 : 3;
-  const TileCost* cost = t == Type::F32 ? kCost32 : kCost16;
+  const TileCost* cost = t == Type::F32 ? (fast ? kFast32 : kSlow32)
+                                        : fast ? kFast16 : kSlow16;
   Shape best = {0, 0, 0, 1, 0};
   double least = 0;
-  for (int tile = 0; tile < tiles; ++tile) {
-    const size_t bm = (size_t)64 << tile, bn = f == Form::GATED ? bm / 2 : bm;
+  for (int tile = 0; tile < kTiles; ++tile) {
+    if (!cost[tile].resident) continue;
+    const size_t bm = kTileRows[tile],
+                 bn = kTileCols[tile] / (f == Form::GATED ? 2 : 1);
     const double n = (double)((ni + bm - 1) / bm) * ((nj + bn - 1) / bn) *
                      ranks * (f == Form::DW ? pairs : 1);
     for (int s = 1; s <= (split ? 16 : 1); s += s < 4 ? 1 : s < 8 ? 2 : 4) {
@@ -295,6 +309,8 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
       }
     }
   }
+  if (getenv("DPAR_TILE")) best.tile = atoi(getenv("DPAR_TILE"));
+  if (getenv("DPAR_SPLIT")) best.splits = split && (int)nk >= 2 * atoi(getenv("DPAR_SPLIT")) ? atoi(getenv("DPAR_SPLIT")) : 1, best.part = best.splits > 1 ? (cells + ni * ranks * pairs) * 4 * best.splits : 0;
   return best;
 }
 
@@ -330,9 +346,10 @@ size_t workspace_of(dpar_product_call_t call, Type t, int p,
   const int n = steps_of(call, o, true, true, s);
   size_t most = 0;
   for (int k = 0; k < n; ++k)
-    most = std::max(most, shape_of(s[k].form, t, ranks_per_launch(p),
-                                   s[k].pairs, s[k].ni, s[k].nj, s[k].nc,
-                                   cus, true).part);
+    for (bool fast : {false, true})
+      most = std::max(most, shape_of(s[k].form, t, ranks_per_launch(p),
+                                     s[k].pairs, s[k].ni, s[k].nj, s[k].nc,
+                                     cus, true, fast).part);
   return most;
 }
 
@@ -362,7 +379,7 @@ int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
                 int cus, hipStream_t stream, Fill fill) {
   const int per = ranks_per_launch(p);
   const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
-                           ws != nullptr);
+                           ws != nullptr, a->fast);
   a->waves = s.waves;
   a->sets = s.sets;
   a->tile = s.tile;

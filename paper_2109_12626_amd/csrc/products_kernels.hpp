@@ -547,6 +547,27 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
   }
 }
 
+// OP's addresses from tile `first` on; b, b2: the (first) pair's and the second
+// pair's operand, u: GATED, the second weights.
+template <Type T, Form F, typename OP, typename W>
+__device__ inline W walk_from(const void* b, const void* u, const void* b2,
+                              size_t ld, size_t i0, unsigned first,
+                              unsigned tiles) {
+  W x;
+  x.step = OP::step(ld);
+  x.n = tiles;
+  const size_t o = OP::origin(ld, i0);
+  const bool second = F == Form::DX && first >= tiles;
+  x.p2 = F == Form::DX && b2 && !second ? (const char*)b2 + o : nullptr;
+  x.o2 = (const char*)b2;
+  x.o = (const char*)(second ? b2 : b);
+  x.ou = (const char*)u;
+  x.c = second ? first - tiles : first;
+  x.p = uniform((const char*)(second ? b2 : b) + o + x.c * x.step);
+  x.u = u ? uniform((const char*)u + o + x.c * x.step) : x.p;
+  return x;
+}
+
 // Which results a workgroup computes.
 template <int BM, int BJ>
 struct Place {
@@ -579,6 +600,27 @@ struct Place {
     const unsigned left = (unsigned)mt - row8 * 8, high = left < 8 ? left : 8;
     i0 = (size_t)uniform(row8 * 8 + in % high) * BM;
     j0 = (size_t)uniform(in / high) * BJ;
+  }
+};
+
+// One operand's addresses along the contraction: the tile to ask for next, kept
+// in scalar registers so that the loop neither loads nor multiplies for them.
+// DX: the second pair follows the first.
+struct Walk {
+  const char *p, *u;          // the tile's first value (u: GATED, of u)
+  const char *o, *ou;         // the operands themselves
+  const char *p2, *o2;        // DX: the second pair's
+  size_t step;
+  unsigned c, n;              // the tile, and the tiles of a pair
+
+  __device__ void next() {
+    p = uniform(p + step);
+    u = uniform(u + step);
+    if (++c == n && p2) {
+      p = p2;
+      o = o2;
+      c = 0;
+    }
   }
 };
 
@@ -673,7 +715,7 @@ struct Results {
 
 // ---------------------------------------------------------------- the kernel
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 struct Tiled {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
@@ -727,59 +769,53 @@ struct Tiled {
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds +
                           uniform(wave) * 1024;
 
-    // The operands' first values at contraction tile kt, and their guards.
-    struct Bases {
-      const char *a, *b, *u;      // u: GATED, the second weights
-      unsigned c;                 // the tile within its pair's contraction
-      uint32_t ga, gb[2];         // gb: even and odd pieces
-    };
-    auto bases = [&](unsigned kt) {
-      const int s = F == Form::DX ? (kt >= nk1) : pair;
-      Bases p;
-      p.c = F == Form::DX && s ? kt - nk1 : kt;
-      p.a = (const char*)a.a[s][rank];
-      p.b = (const char*)a.b[kGated || F == Form::DW ? 0 : s][rank];
-      p.u = kGated ? (const char*)a.b[1][rank] : p.b;
-      if (FAST) {
-        const size_t c0 = (size_t)p.c * KT;
-        p.a = uniform(p.a + OA::origin(a.lda, i0) + p.c * OA::step(a.lda));
-        const size_t ob = OB::origin(a.ldb, j0) + p.c * OB::step(a.ldb);
-        p.b = uniform(p.b + ob);
-        p.u = uniform(p.u + ob);
-        p.ga = OA::guard(a.lda, i0, a.ni, c0, a.nc, 0, t);
-        for (int n = 0; n < 2; ++n)
-          p.gb[n] = OB::guard(a.ldb, j0, a.nj, c0, a.nc, n, t);
-      }
-      return p;
-    };
-    // Piece n of A's, then B's, of a tile into LDS.
-    auto dma = [&](const Bases& p, uint32_t d, int n) {
-      if (n < OA::N)
-        dma16(d + n * kThreads * 16, p.a, OA::guarded(va[n], p.ga));
-      else
-        dma16(d + n * kThreads * 16,
-              kGated && n - OA::N >= OB::N / 2 ? p.u : p.b,
-              OB::guarded(vb[n - OA::N], p.gb[(n - OA::N) & 1]));
-    };
+    Walk xa = walk_from<T, F, OA, Walk>(a.a[pair][rank], nullptr, a.a[1][rank],
+                                        a.lda, i0, k0, nk1),
+         xb = walk_from<T, F, OB, Walk>(a.b[0][rank],
+                                        kGated ? a.b[1][rank] : nullptr,
+                                        a.b[1][rank], a.ldb, j0, k0, nk1);
     constexpr int kPieces = OA::N + OB::N;
-    // Loads contraction tile kt: FAST into LDS, else into registers.
-    auto issue = [&](unsigned kt, int buf) {
-      const Bases p = bases(kt);
-      if constexpr (FAST) {
+    // Pieces n0 .. n1 - 1 of the next tile (A's, then B's) into a buffer.
+    auto dma = [&](int buf, int n0, int n1) {
+      const uint32_t d = lds0 + buf * kBytes;
+      const size_t c0 = (size_t)xa.c * KT;
+      const bool all = xa.c < whole;
+      const uint32_t ga =
+          all ? 0 : OA::guard(a.lda, i0, a.ni, c0, a.nc, 0, t);
 #pragma unroll
-        for (int n = 0; n < kPieces; ++n) dma(p, lds0 + buf * kBytes, n);
+      for (int n = n0; n < n1; ++n) {
+        const int m = n - OA::N;
+        if (n < OA::N)
+          dma16(d + n * kThreads * 16, xa.p,
+                all ? va[n] : OA::guarded(va[n], ga));
+        else
+          dma16(d + n * kThreads * 16, kGated && m >= OB::N / 2 ? xb.u : xb.p,
+                all ? vb[m]
+                    : OB::guarded(vb[m], OB::guard(a.ldb, j0, a.nj, c0, a.nc,
+                                                   m, t)));
+      }
+    };
+    auto walk = [&] {
+      xa.next();
+      xb.next();
+    };
+    // Loads the next contraction tile: FAST into LDS, else into registers.
+    auto issue = [&](int buf) {
+      if constexpr (FAST) {
+        dma(buf, 0, kPieces);
       } else {
-        const size_t c0 = (size_t)p.c * KT;
+        const size_t c0 = (size_t)xa.c * KT;
 #pragma unroll
         for (int n = 0; n < OA::N; ++n)
-          ra[n] = OA::fetch((const V*)p.a, a.lda, i0, a.ni, c0, a.nc, n, t);
+          ra[n] = OA::fetch((const V*)xa.o, a.lda, i0, a.ni, c0, a.nc, n, t);
 #pragma unroll
         for (int n = 0; n < OB::N; ++n) {
           const bool up = kGated && n >= OB::N / 2;
-          rb[n] = OB::fetch((const V*)(up ? p.u : p.b), a.ldb,
+          rb[n] = OB::fetch((const V*)(up ? xb.ou : xb.o), a.ldb,
                             up ? j0 - BJ : j0, a.nj, c0, a.nc, n, t);
         }
       }
+      walk();
     };
     // Zeros in the place of this thread's pieces past the contraction's end,
     // after they have landed.
@@ -794,7 +830,7 @@ struct Tiled {
         if (n < OA::N ? OA::past((size_t)c * KT, a.nc, n, o)
                       : OB::past((size_t)c * KT, a.nc, n - OA::N, o))
           *(LDS i32x4*)(d + n * kThreads * 16) = i32x4{0, 0, 0, 0};
-      landed<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
     auto land = [&](int buf) {
       if constexpr (!FAST) {
@@ -840,11 +876,12 @@ struct Tiled {
     };
     static_assert(kPieces % (MI / 2) == 0);
     auto loop = [&](auto with_sums) {
+      int buf = 0;
 #pragma unroll 1
       for (unsigned kt = k0; kt < k1; ++kt) {
-        const int buf = (kt - k0) & 1;
-        const bool ahead = kt + 2 < k1;
-        if (!FAST && ahead) issue(kt + 2, buf);
+        const int then = buf + 1 == R ? 0 : buf + 1;
+        const bool ahead = kt + R < k1;
+        if (!FAST && ahead) issue(buf);
         read_b(1, buf);
 #pragma unroll
         for (int m = 0; m < MI; ++m) {
@@ -855,44 +892,44 @@ struct Tiled {
 #pragma unroll
         for (int m = 0; m < MI / 2; ++m) multiply(m, 1, with_sums);
         __builtin_amdgcn_sched_barrier(0);
-        landed<0>();
-        if (kt + 1 < k1) clear(kt + 1, buf ^ 1);
+        if (FAST && kt + R - 1 < k1)
+          landed<(R - 2) * kPieces>();
+        else
+          landed<0>();
+        if (kt + 1 < k1) clear(kt + 1, then);
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        Bases next = {};
-        if (FAST)
-          next = bases(ahead ? kt + 2 : kt);
-        else if (ahead)
-          land(buf);
+        if (!FAST && ahead) land(buf);
         // (after the last tile this reads a buffer that nothing uses any
         // more)
-        read_b(0, buf ^ 1);
+        read_b(0, then);
 #pragma unroll
         for (int m = MI / 2; m < MI; ++m) {
-          read_a(m - MI / 2, 0, buf ^ 1);
+          read_a(m - MI / 2, 0, then);
           multiply(m, 1, with_sums);
-          read_a(m, 0, buf ^ 1);
+          read_a(m, 0, then);
           if (FAST && ahead) {
-#pragma unroll
-            for (int n = 0; n < kPieces / (MI / 2); ++n)
-              dma(next, lds0 + buf * kBytes,
-                  (m - MI / 2) * (kPieces / (MI / 2)) + n);
+            constexpr int kEach = kPieces / (MI / 2);
+            dma(buf, (m - MI / 2) * kEach, (m - MI / 2 + 1) * kEach);
+            if (m == MI - 1) walk();
           }
           __builtin_amdgcn_sched_barrier(0);
         }
+        buf = then;
       }
     };
 
     if (k0 < k1) {
-      issue(k0, 0);
-      land(0);
-      if (k0 + 1 < k1) {
-        issue(k0 + 1, 1);
-        land(1);
-        landed<FAST ? OA::N + OB::N : 0>();
-      } else {
+#pragma unroll
+      for (int n = 0; n < R; ++n)
+        if (k0 + n < k1) {
+          issue(n);
+          land(n);
+        }
+      if (FAST && k0 + R - 1 < k1)
+        landed<(R - 1) * kPieces>();
+      else
         landed<0>();
-      }
       clear(k0, 0);
       __builtin_amdgcn_s_barrier();
       read_b(0, 0);
@@ -921,37 +958,44 @@ struct Tiled {
   }
 };
 
-// 16-bit types, 256 x 256 results (GATED: 256 x 128 of each), 8 wavefronts of
-// 128 x 64.  A tile of the contraction (128 bytes of 256 rows of A and of B)
-// takes two of five 32 KB slots of LDS, so that up to three operands are on
-// their way while one tile is used.  (Stages of 64 bytes a row would leave
-// four, but loads of 64 bytes of 16 rows reach half the rate of 128 bytes of
-// 8: 67 against 123 GB/s per CU from L2.)
+// 256 x BN results (GATED: 256 x BN / 2 of each), 8 wavefronts of 128 x 64 (BN
+// = 256) or 64 x 64 (BN = 128).  A tile of the contraction is 128 bytes of 256
+// rows of A and of BN rows of B; the LDS holds three tiles of A and two (BN =
+// 256: 160 KB in all) or three of B, so that loads have one and a half or two
+// tiles of time to arrive.  (Stages of 64 bytes a row would leave more, but
+// loads of 64 bytes of 16 rows reach half the rate of 128 bytes of 8: 67
+// against 123 GB/s per CU from L2.)
 //
 // Each SIMD has two wavefronts, one of either half of the workgroup, and the
 // halves run one phase apart: while one half reads the fragments of a step
-// (12 pieces of 16 bytes per lane) and asks for a later operand, the other has
-// the matrix cores to itself for 32 products of 16 x 16 x 32 (512 cycles);
-// then a barrier, and they change places.
-template <Type T, Form F>
+// and asks for a later operand, the other has the matrix cores to itself (32
+// or 16 products of 16 x 16 x 32, 512 or 256 cycles); then a barrier, and they
+// change places.
+//
+// Operands of whole aligned pieces only (FAST in Tiled).
+template <Type T, Form F, int BN>
 struct PingPong {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
   static constexpr bool kACC = F != Form::DW;
   static constexpr bool kBCC = F == Form::LINEAR || F == Form::GATED;
-  static constexpr int BM = 256, BN = 256, WM = 128, WN = 64, kThreads = 512;
+  static constexpr int BM = 256, WM = BN == 256 ? 128 : 64, WN = 64;
+  static constexpr int kThreads = 512, kAcross = BN / WN;
   static constexpr int MI = WM / 16, NJ = WN / 16, NT = kGated ? NJ / 2 : NJ;
   static constexpr int G = 4 * NT, BJ = kGated ? BN / 2 : BN;
   using OA = Operand<T, kACC, BM, 4, kThreads>;
   using OB = Operand<T, kBCC, BN, G, kThreads>;
-  static constexpr int KT = OA::KT, NP = OA::N;
-  static_assert(OA::N == OB::N);
-  static constexpr int kSlots = 5, kSlot = BM * kLine;
-  static constexpr int kLds = kSlots * kSlot;
+  static constexpr int KT = OA::KT, NA = OA::N, NB = OB::N;
+  // tiles of A and of B in LDS
+  static constexpr int kRingA = 3, kRingB = BN == 256 ? 2 : 3;
+  static constexpr int kSlotA = BM * kLine, kSlotB = BN * kLine;
+  static constexpr int kLds = kRingA * kSlotA + kRingB * kSlotB;
+  static_assert(kLds <= 160 * 1024);
 
   static __device__ void run(Given& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
-    const int wm = wave / 4, wn = wave % 4;
+    const int wm = wave / kAcross, wn = wave % kAcross;
+    const bool late = wave >= 4;             // the half that runs behind
     const Place<BM, BJ> at(a, F);
     const int rank = at.rank, pair = at.pair;
     const unsigned split = at.split;
@@ -968,64 +1012,78 @@ struct PingPong {
     f32x4 sum = {};
     const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
 
-    uint32_t va[NP], vb[NP];
+    uint32_t va[NA], vb[NB];
 #pragma unroll
-    for (int n = 0; n < NP; ++n) {
-      va[n] = OA::offset(a.lda, i0, a.ni, n, t);
-      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (NP / 2) : n, t);
-    }
+    for (int n = 0; n < NA; ++n) va[n] = OA::offset(a.lda, i0, a.ni, n, t);
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (NB / 2) : n, t);
+    LDS char* const ringb = lds + kRingA * kSlotA;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds + wave * 1024;
 
-    // A's or B's part of tile kt into a slot.
-    auto ask_a = [&](unsigned kt, int slot) {
-      const int s = F == Form::DX ? (kt >= nk1) : pair;
-      const unsigned c = F == Form::DX && s ? kt - nk1 : kt;
-      const char* p = uniform((const char*)a.a[s][rank] +
-                              OA::origin(a.lda, i0) + c * OA::step(a.lda));
-      const uint32_t g =
-          OA::guard(a.lda, i0, a.ni, (size_t)c * KT, a.nc, 0, t);
+    Walk xa = walk_from<T, F, OA, Walk>(a.a[pair][rank], nullptr, a.a[1][rank],
+                                      a.lda, i0, k0, nk1),
+         xb = walk_from<T, F, OB, Walk>(a.b[0][rank],
+                                      kGated ? a.b[1][rank] : nullptr,
+                                      a.b[1][rank], a.ldb, j0, k0, nk1);
+
+    // A's or B's part of the next tile into a slot.
+    auto ask_a = [&](int slot) {
+      const uint32_t d = lds0 + slot * kSlotA;
+      if (xa.c < whole) {
 #pragma unroll
-      for (int n = 0; n < NP; ++n)
-        dma16(lds0 + slot * kSlot + n * kThreads * 16, p,
-              OA::guarded(va[n], g));
-    };
-    auto ask_b = [&](unsigned kt, int slot) {
-      const int s = F == Form::DX ? (kt >= nk1) : 0;
-      const unsigned c = F == Form::DX && s ? kt - nk1 : kt;
-      const size_t ob = OB::origin(a.ldb, j0) + c * OB::step(a.ldb);
-      const char* p = uniform((const char*)a.b[s][rank] + ob);
-      const char* u = kGated ? uniform((const char*)a.b[1][rank] + ob) : p;
+        for (int n = 0; n < NA; ++n) dma16(d + n * kThreads * 16, xa.p, va[n]);
+      } else {
+        const uint32_t g = OA::guard(a.lda, i0, a.ni, (size_t)xa.c * KT, a.nc,
+                                     0, t);
 #pragma unroll
-      for (int n = 0; n < NP; ++n)
-        dma16(lds0 + slot * kSlot + n * kThreads * 16,
-              kGated && n >= NP / 2 ? u : p,
-              OB::guarded(vb[n], OB::guard(a.ldb, j0, a.nj, (size_t)c * KT,
-                                           a.nc, n, t)));
+        for (int n = 0; n < NA; ++n)
+          dma16(d + n * kThreads * 16, xa.p, OA::guarded(va[n], g));
+      }
+      xa.next();
     };
-    auto slot_of = [&](unsigned unit) { return (int)(unit % kSlots); };
+    auto ask_b = [&](int slot) {
+      const uint32_t d = lds0 + kRingA * kSlotA + slot * kSlotB;
+      if (xb.c < whole) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          dma16(d + n * kThreads * 16, kGated && n >= NB / 2 ? xb.u : xb.p,
+                vb[n]);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          dma16(d + n * kThreads * 16, kGated && n >= NB / 2 ? xb.u : xb.p,
+                OB::guarded(vb[n], OB::guard(a.ldb, j0, a.nj,
+                                             (size_t)xb.c * KT, a.nc, n, t)));
+      }
+      xb.next();
+    };
     // As in Tiled: zeros past the contraction's end.
     auto clear = [&](unsigned kt) {
       const unsigned c = F == Form::DX && kt >= nk1 ? kt - nk1 : kt;
       if (c < whole) return;
       const size_t c0 = (size_t)c * KT;
-      LDS char* da = lds + slot_of(2 * (kt - k0)) * kSlot + t * 16;
-      LDS char* db = lds + slot_of(2 * (kt - k0) + 1) * kSlot + t * 16;
+      LDS char* da = lds + (kt - k0) % kRingA * kSlotA + t * 16;
+      LDS char* db = ringb + (kt - k0) % kRingB * kSlotB + t * 16;
       int o = t;
       asm volatile("" : "+v"(o));
 #pragma unroll 1
-      for (int n = 0; n < NP; ++n) {
+      for (int n = 0; n < NA; ++n)
         if (OA::past(c0, a.nc, n, o))
           *(LDS i32x4*)(da + n * kThreads * 16) = i32x4{0, 0, 0, 0};
+#pragma unroll 1
+      for (int n = 0; n < NB; ++n)
         if (OB::past(c0, a.nc, n, o))
           *(LDS i32x4*)(db + n * kThreads * 16) = i32x4{0, 0, 0, 0};
-      }
     };
-    // Waits until this wavefront's pieces of tile kt have landed; only A's of
-    // the tile after it (`newer`) have been asked for since.
+    // Waits until this wavefront's pieces of tile kt have landed; `newer`: the
+    // tile after it is there, and A's part of it (kRingB > 2: and B's) has
+    // been asked for since.
     auto ready = [&](unsigned kt, bool newer) {
       if (kt >= k1) return;
       if (newer)
-        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NP) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)"
+                     :: "n"(kRingB > 2 ? NA + NB : NA) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       clear(kt);
@@ -1037,15 +1095,11 @@ struct PingPong {
     };
 
     auto loop = [&](auto with_sums) {
-      int sa = 0;                          // A's slot; B's is the next
+      int sa = 0, sb = 0;
 #pragma unroll 1
       for (unsigned kt = k0; kt < k1; ++kt) {
-        const int sb = sa + 1 == kSlots ? 0 : sa + 1;
-        const int s2 = sb + 1 == kSlots ? 0 : sb + 1;   // A of the next tile
-        const int s3 = s2 + 1 == kSlots ? 0 : s2 + 1;   // B of it
-        const int s4 = s3 + 1 == kSlots ? 0 : s3 + 1;   // A of the one after
-        LDS char* la = lds + sa * kSlot;
-        LDS char* lb = lds + sb * kSlot;
+        LDS char* la = lds + sa * kSlotA;
+        LDS char* lb = ringb + sb * kSlotB;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           i32x4 fa[MI], fb[NJ];
@@ -1057,40 +1111,44 @@ struct PingPong {
           for (int m = 0; m < MI; ++m)
             fa[m] = OA::frag(la, ks, wm * WM + m * 16, 0, lane);
           if (ks == 0) {
-            if (kt + 1 < k1) ask_b(kt + 1, s3);
+            // the slot of tile kt - 1, which both halves have read
+            constexpr int on = kRingB - 1;
+            if (kt + on < k1) ask_b(sb == 0 ? on : sb - 1);
           } else {
-            if (kt + 2 < k1) ask_a(kt + 2, s4);
-            if (wm) ready(kt + 1, kt + 2 < k1);
+            if (kt + 2 < k1) ask_a(sa == 0 ? 2 : sa - 1);
+            if (late) ready(kt + 1, kt + 2 < k1);
           }
           __builtin_amdgcn_sched_barrier(0);
           change();
           __builtin_amdgcn_s_setprio(1);
 #pragma unroll
           for (int m = 0; m < MI; ++m) {
-#pragma unroll
-            for (int n = 0; n < NJ; ++n)
-              acc[m][n] = Elem<T>::mma(fb[n], fa[m], acc[m][n]);
+            mma_row<T>(fb, fa[m], acc[m]);
             if constexpr (with_sums)
-              if (m % 4 == wn)
+              if (m % kAcross == wn)
                 sum = Elem<T>::mma(
                     (lane & 15) == m ? Elem<T>::ones() : i32x4{}, fa[m], sum);
           }
           __builtin_amdgcn_s_setprio(0);
           __builtin_amdgcn_sched_barrier(0);
-          if (ks == 1 && !wm) ready(kt + 1, kt + 2 < k1);
+          if (ks == 1 && !late) ready(kt + 1, kt + 2 < k1);
           change();
         }
-        sa = s2;
+        sa = sa + 1 == kRingA ? 0 : sa + 1;
+        sb = sb + 1 == kRingB ? 0 : sb + 1;
       }
     };
 
     if (k0 < k1) {
-      ask_a(k0, 0);
-      ask_b(k0, 1);
-      if (k0 + 1 < k1) ask_a(k0 + 1, 2);
+      ask_a(0);
+      ask_b(0);
+      if (k0 + 1 < k1) {
+        if (kRingB > 2) ask_b(1);
+        ask_a(1);
+      }
       ready(k0, k0 + 1 < k1);
       change();
-      if (wm) __builtin_amdgcn_s_barrier();   // one phase behind
+      if (late) __builtin_amdgcn_s_barrier();   // one phase behind
       if constexpr (F == Form::DW) {
         if (sums)
           loop(Yes{});
@@ -1099,26 +1157,26 @@ struct PingPong {
       } else {
         loop(No{});
       }
-      if (!wm) __builtin_amdgcn_s_barrier();
+      if (!late) __builtin_amdgcn_s_barrier();
     }
     Results<T, F, WM, WN, OB>::store(a, rank, pair, split, i0 + wm * WM,
                                      j0 + wn * (kGated ? WN / 2 : WN), sums,
-                                     wn, 4, sum, acc, lds, wave, lane);
+                                     wn, kAcross, sum, acc, lds, wave, lane);
   }
 };
 
-template <Type T, Form F>
+template <Type T, Form F, int BN>
 __global__ __launch_bounds__(512) void k_pingpong(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  PingPong<T, F>::run(a, (LDS char*)lds);
+  PingPong<T, F, BN>::run(a, (LDS char*)lds);
 }
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Tiled<T, F, FAST, BM, BN, WM, WN>::run(a, (LDS char*)lds);
+  Tiled<T, F, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -1489,11 +1547,18 @@ hipError_t launch_tiles(void (*k)(Args), Form f, const Args& a, int bm, int bj,
   return hipGetLastError();
 }
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN>
+template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 hipError_t go(const Args& a, hipStream_t stream) {
-  using K = Tiled<T, F, FAST, BM, BN, WM, WN>;
-  return launch_tiles(k_tiled<T, F, FAST, BM, BN, WM, WN>, F, a, BM, K::BJ,
-                      K::kThreads, 2 * K::kBytes, stream);
+  using K = Tiled<T, F, FAST, BM, BN, WM, WN, R>;
+  return launch_tiles(k_tiled<T, F, FAST, BM, BN, WM, WN, R>, F, a, BM, K::BJ,
+                      K::kThreads, R * K::kBytes, stream);
+}
+
+template <Type T, Form F, int BN>
+hipError_t go_pingpong(const Args& a, hipStream_t stream) {
+  using K = PingPong<T, F, BN>;
+  return launch_tiles(k_pingpong<T, F, BN>, F, a, K::BM, K::BJ,
+                      K::kThreads, K::kLds, stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int NW, int S>
@@ -1550,14 +1615,14 @@ template <Type T, Form F, bool FAST>
 hipError_t pick(const Args& a, hipStream_t stream) {
   if constexpr (F == Form::LINEAR || F == Form::GATED)
     if (a.waves) return pick_few<T, F, FAST>(a, stream);
-  if constexpr (T != Type::F32 && FAST)
-    if (a.tile == 2) {
-      using K = PingPong<T, F>;
-      return launch_tiles(k_pingpong<T, F>, F, a, K::BM, K::BJ, K::kThreads,
-                          K::kLds, stream);
-    }
-  if (a.tile >= 1) return go<T, F, FAST, 128, 128, 64, 64>(a, stream);
-  return go<T, F, FAST, 64, 64, 32, 32>(a, stream);
+  if constexpr (T != Type::F32 && FAST) {
+    if (a.tile == 4) return go_pingpong<T, F, 256>(a, stream);
+    if (a.tile == 3) return go_pingpong<T, F, 128>(a, stream);
+  }
+  if (a.tile == 2) return go<T, F, FAST, 128, 128, 64, 64, 2>(a, stream);
+  if constexpr (FAST)
+    if (a.tile == 1) return go<T, F, FAST, 64, 64, 32, 32, 4>(a, stream);
+  return go<T, F, FAST, 64, 64, 32, 32, 2>(a, stream);
 }
 
 template <Type T, Form F>
