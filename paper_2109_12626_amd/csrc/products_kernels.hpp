@@ -439,6 +439,13 @@ __device__ inline void store_vals(V* p, const float* v, long left, bool wide) {
     }
     return;
   }
+  if (left >= N) {
+    V t[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[k] = (V)v[k];
+    __builtin_memcpy(p, t, N * sizeof(V));
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < N; ++k)
     if (k < left) p[k] = (V)v[k];
@@ -457,6 +464,13 @@ __device__ inline void fetch_vals(const V* p, float* v, long left, bool wide) {
 #pragma unroll
       for (int e = 0; e < E; ++e) v[k + e] = (float)t[e];
     }
+    return;
+  }
+  if (left >= N) {
+    V t[N];
+    __builtin_memcpy(t, p, N * sizeof(V));
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = (float)t[k];
     return;
   }
 #pragma unroll
