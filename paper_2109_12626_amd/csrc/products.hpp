@@ -38,6 +38,8 @@ struct Args {
   // GATED: u; DW: bias gradients
   void* u[2][kRanks];
   size_t ni, nj, nc;         // rows and columns of C, contraction
+  size_t na, nb;             // rows (columns, where stored so) of A and B
+                             // that loads may touch: ni, nj or more
   size_t lda, ldb, ldo, ldk, lde;  // row distances (elements): A, B, result,
                                    // kept values, residual
   float* part;               // partial results of a split contraction
@@ -66,6 +68,19 @@ struct SlopeArgs {
   size_t rows, cols, ldy, ldz;
   int ranks, act, gated, wide;
 };
+
+// Copies matrices to 16-byte rows `pitch` bytes apart, zeros after the values;
+// sizes in 2-byte units.  Up to two matrices of either operand.
+struct CopyArgs {
+  struct Job {
+    const void* from[kRanks];
+    char* to;
+    size_t rows, cols, ld, pitch;
+    int mats;
+  } job[4];
+  int jobs;
+};
+hipError_t launch_copy(const CopyArgs& a, hipStream_t stream);
 
 // One source file per type.
 hipError_t launch_bf16(Form f, const Args& a, hipStream_t stream);

@@ -6,7 +6,6 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -32,6 +31,10 @@ int fail(int code, const char* fmt, ...) {
   return dpar::set_error(code, buf);
 }
 
+// 256 rows of an operand lie within the kernels' 32-bit offsets (the fast
+// loads; others use 64-bit addresses throughout).
+constexpr size_t kFastPitch = (size_t)1 << 23;
+
 // One array argument: p matrices of rows x cols elements, `ld` elements
 // apart.
 struct Mat {
@@ -52,6 +55,11 @@ struct Mat {
     uintptr_t bits = rows > 1 ? ld * esz : 0;
     for (int i = 0; i < p; ++i) bits |= (uintptr_t)at[i];
     return (bits & 15) == 0;
+  }
+  // rows of whole aligned 16-byte pieces, 256 of them within 32 bits
+  bool fast(int p) const {
+    return !used || (extent() && aligned(p) && cols * esz % 16 == 0 &&
+                     ld < kFastPitch);
   }
   const void* rank(int i) const { return used ? at[i] : nullptr; }
 };
@@ -143,9 +151,6 @@ int check_mats(const Mat* mats, int n, int p, const char* call) {
   return check_alias(mats, n, p, call);
 }
 
-// 256 rows of an operand lie within the kernels' 32-bit offsets (the fast
-// loads; others use 64-bit addresses throughout).
-constexpr size_t kFastPitch = (size_t)1 << 23;
 constexpr size_t kMost = (size_t)1 << 31;     // rows, in, out
 constexpr size_t kMostPitch = (size_t)1 << 38;
 
@@ -208,6 +213,7 @@ int ranks_per_launch(int p) {
 struct Shape {
   int waves, sets, tile, splits;
   size_t part;           // bytes of workspace
+  double ns;             // estimate (tiles only)
 };
 
 // Time of one contraction tile (128 bytes of every row) of a workgroup on a
@@ -276,7 +282,7 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
              (w < 4 ? n * w < many || chunks > (size_t)w * 4
                     : n * w < many / 2))
         w *= 2;
-      return {w, (int)sets, 0, 1, 0};
+      return {w, (int)sets, 0, 1, 0, 0};
     }
   }
   const size_t kt = t == Type::F32 ? 32 : 64;
@@ -285,8 +291,7 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
                        (f == Form::GATED ? 2 : 1);
   const TileCost* cost = t == Type::F32 ? (fast ? kFast32 : kSlow32)
                                         : fast ? kFast16 : kSlow16;
-  Shape best = {0, 0, 0, 1, 0};
-  double least = 0;
+  Shape best = {0, 0, 0, 1, 0, 0};
   for (int tile = 0; tile < kTiles; ++tile) {
     if (!cost[tile].resident) continue;
     const size_t bm = kTileRows[tile],
@@ -303,38 +308,92 @@ Shape shape_of(Form f, Type t, int ranks, int pairs, size_t ni, size_t nj,
       double ns = kStartNs + steps * std::max(turns * cost[tile].alone,
                                               per * cost[tile].rate);
       if (s > 1) ns += kJoinNs + part / kJoinRate;
-      if (least == 0 || ns < least) {
-        least = ns;
-        best = {0, 0, tile, s, part};
-      }
+      if (best.ns == 0 || ns < best.ns) best = {0, 0, tile, s, part, ns};
     }
   }
-  if (getenv("DPAR_TILE")) best.tile = atoi(getenv("DPAR_TILE"));
-  if (getenv("DPAR_SPLIT")) best.splits = split && (int)nk >= 2 * atoi(getenv("DPAR_SPLIT")) ? atoi(getenv("DPAR_SPLIT")) : 1, best.part = best.splits > 1 ? (cells + ni * ranks * pairs) * 4 * best.splits : 0;
   return best;
 }
+
+// An operand of a product as it is stored: `mats` matrices per rank.
+struct Stored {
+  int mats;
+  size_t rows, cols, ld;
+  bool fast;
+};
 
 struct Step {
   Form form;
   int pairs;
   size_t ni, nj, nc;
+  Stored a, b;
 };
 
+// How a product runs, operands copied first (`copy_*`) or not.
+struct Plan {
+  Shape shape;
+  bool fast, copy_a, copy_b;
+  size_t ld_a, ld_b, bytes_a, bytes_b;   // of the copies
+  size_t bytes() const { return bytes_a + bytes_b + shape.part; }
+};
+
+// Operands off 16 bytes are read at a third of the rate of aligned ones (38
+// against 114 GB/s per CU from L2), again by every tile.  With enough reuse it
+// pays to copy them once into the workspace, rows 128 bytes apart and filled
+// with zeros, and to run the fast kernels: 2001 x 2001 x 2001 backward 160 ->
+// 83 us.
+constexpr double kCopyNs = 4000, kCopyRate = 1900;   // bytes of the copy per ns
+
+Plan plan_of(const Step& s, Type t, int ranks, int cus, size_t room) {
+  const size_t e = t == Type::F32 ? 4 : 2;
+  Plan n = {};
+  n.fast = s.a.fast && s.b.fast && s.nc != 0;
+  n.shape = shape_of(s.form, t, ranks, s.pairs, s.ni, s.nj, s.nc, cus,
+                     room != 0, n.fast);
+  if (n.fast || n.shape.waves || !room || !s.nc || !s.ni || !s.nj) return n;
+  Plan c = n;
+  c.fast = true;
+  c.shape = shape_of(s.form, t, ranks, s.pairs, s.ni, s.nj, s.nc, cus, true,
+                     true);
+  c.copy_a = !s.a.fast, c.copy_b = !s.b.fast;
+  const size_t line = 128 / e;
+  c.ld_a = (s.a.cols + line - 1) / line * line;
+  c.ld_b = (s.b.cols + line - 1) / line * line;
+  if (c.copy_a) c.bytes_a = s.a.mats * (size_t)ranks * s.a.rows * c.ld_a * e;
+  if (c.copy_b) c.bytes_b = s.b.mats * (size_t)ranks * s.b.rows * c.ld_b * e;
+  if (c.bytes_a + c.bytes_b > 2 * kMostPart || c.ld_a >= kFastPitch ||
+      c.ld_b >= kFastPitch || c.bytes() > room)
+    return n;
+  const double ns =
+      c.shape.ns + kCopyNs + (double)(c.bytes_a + c.bytes_b) / kCopyRate;
+  return ns < n.shape.ns ? c : n;
+}
+
 // The products of a call.
-int steps_of(dpar_product_call_t call, const dpar_product_t& o, bool dx,
-             bool dw, Step* s) {
+int steps_of(dpar_product_call_t call, const dpar_product_t& o, Type t,
+             bool dx, bool dw, Step* s) {
+  const size_t e = t == Type::F32 ? 4 : 2;
+  auto stored = [&](int mats, size_t rows, size_t cols, size_t ld) {
+    const bool fast = rows && cols && cols * e % 16 == 0 &&
+                      (rows == 1 || ld * e % 16 == 0) && ld < kFastPitch;
+    return Stored{mats, rows, cols, ld, fast};
+  };
+  const bool gated = call == DPAR_GATED || call == DPAR_GATED_BACKWARD;
+  const int m = gated ? 2 : 1;
+  const Stored x = stored(1, o.rows, o.in, o.ldx),
+               w = stored(m, o.out, o.in, o.ldw);
   int n = 0;
   switch (call) {
     case DPAR_LINEAR:
-      s[n++] = {Form::LINEAR, 1, o.rows, o.out, o.in};
+      s[n++] = {Form::LINEAR, 1, o.rows, o.out, o.in, x, w};
       break;
     case DPAR_GATED:
-      s[n++] = {Form::GATED, 1, o.rows, o.out, o.in};
+      s[n++] = {Form::GATED, 1, o.rows, o.out, o.in, x, w};
       break;
     default: {
-      const int pairs = call == DPAR_GATED_BACKWARD ? 2 : 1;
-      if (dx) s[n++] = {Form::DX, pairs, o.rows, o.in, o.out};
-      if (dw) s[n++] = {Form::DW, pairs, o.out, o.in, o.rows};
+      const bool slope = gated || o.act != DPAR_ACT_NONE;
+      const Stored dz = stored(m, o.rows, o.out, slope ? o.ldz : o.ldy);
+      if (dx) s[n++] = {Form::DX, m, o.rows, o.in, o.out, dz, w};
+      if (dw) s[n++] = {Form::DW, m, o.out, o.in, o.rows, dz, x};
     }
   }
   return n;
@@ -343,13 +402,18 @@ int steps_of(dpar_product_call_t call, const dpar_product_t& o, bool dx,
 size_t workspace_of(dpar_product_call_t call, Type t, int p,
                     const dpar_product_t& o, int cus) {
   Step s[2];
-  const int n = steps_of(call, o, true, true, s);
+  const int n = steps_of(call, o, t, true, true, s);
+  const size_t any = ~(size_t)0;
   size_t most = 0;
-  for (int k = 0; k < n; ++k)
-    for (bool fast : {false, true})
-      most = std::max(most, shape_of(s[k].form, t, ranks_per_launch(p),
-                                     s[k].pairs, s[k].ni, s[k].nj, s[k].nc,
-                                     cus, true, fast).part);
+  for (int k = 0; k < n; ++k) {
+    most = std::max(most, plan_of(s[k], t, ranks_per_launch(p), cus,
+                                  any).bytes());
+    // also without copies (operands off 16 bytes at the call)
+    s[k].a.fast = s[k].b.fast = false;
+    const Shape slow = shape_of(s[k].form, t, ranks_per_launch(p), s[k].pairs,
+                                s[k].ni, s[k].nj, s[k].nc, cus, true, false);
+    most = std::max(most, slow.part);
+  }
   return most;
 }
 
@@ -372,29 +436,73 @@ int launched(const char* call, hipError_t e) {
   return fail(DPAR_ERR_HIP, "%s: %s", call, hipGetErrorString(e));
 }
 
+// Copies one operand of a launch's ranks and points the launch at the copies.
+// One matrix read by every rank is copied once.
+void add_copy(dpar::products::CopyArgs* c, const Stored& m, int ranks,
+              size_t e, const void* (*at)[kRanks], size_t ld, char* to) {
+  for (int k = 0; k < m.mats; ++k) {
+    int n = 1;
+    for (int r = 1; r < ranks; ++r)
+      if (at[k][r] != at[k][0]) n = ranks;
+    auto& job = c->job[c->jobs++];
+    job.rows = m.rows, job.cols = m.cols * e / 2, job.ld = m.ld * e / 2;
+    job.pitch = ld * e, job.mats = n;
+    job.to = to;
+    const size_t one = m.rows * ld * e;
+    for (int r = 0; r < ranks; ++r) {
+      job.from[r] = at[k][r];
+      at[k][r] = to + (n == 1 ? 0 : r * one);
+    }
+    to += n * one;
+  }
+}
+
 // Runs one product over all ranks.  a: everything but the addresses, which
-// `fill` writes for a rank.
+// `fill` writes for a rank; s: the product with its operands' alignment.
 template <typename Fill>
-int run_product(const char* call, Form f, Type t, int p, Args* a, void* ws,
-                int cus, hipStream_t stream, Fill fill) {
+int run_product(const char* call, Type t, int p, const Step& s, Args* a,
+                void* ws, size_t bytes, int cus, hipStream_t stream,
+                Fill fill) {
   const int per = ranks_per_launch(p);
-  const Shape s = shape_of(f, t, per, a->pairs, a->ni, a->nj, a->nc, cus,
-                           ws != nullptr, a->fast);
-  a->waves = s.waves;
-  a->sets = s.sets;
-  a->tile = s.tile;
-  a->splits = s.splits;
-  a->part = (float*)ws;
+  const Plan n = plan_of(s, t, per, cus, ws ? bytes : 0);
+  const size_t e = t == Type::F32 ? 4 : 2;
+  a->ni = s.ni, a->nj = s.nj, a->nc = s.nc;
+  a->pairs = s.pairs;
+  a->lda = n.copy_a ? n.ld_a : s.a.ld;
+  a->ldb = n.copy_b ? n.ld_b : s.b.ld;
+  // values that may be loaded along a row of results' operands
+  a->na = n.copy_a && s.form == Form::DW ? n.ld_a : s.ni;
+  a->nb = n.copy_b && (s.form == Form::DW || s.form == Form::DX) ? n.ld_b
+                                                                 : s.nj;
+  a->fast = n.fast;
+  a->waves = n.shape.waves;
+  a->sets = n.shape.sets;
+  a->tile = n.shape.tile;
+  a->splits = n.shape.splits;
+  char* const work = (char*)ws;
+  a->part = (float*)(work + n.bytes_a + n.bytes_b);
   for (int r0 = 0; r0 < p; r0 += per) {
     a->ranks = std::min(per, p - r0);
     for (int k = 0; k < a->ranks; ++k) fill(k, r0 + k);
-    hipError_t e;
-    switch (t) {
-      case Type::BF16: e = dpar::products::launch_bf16(f, *a, stream); break;
-      case Type::F16: e = dpar::products::launch_f16(f, *a, stream); break;
-      default: e = dpar::products::launch_f32(f, *a, stream);
+    if (n.copy_a || n.copy_b) {
+      dpar::products::CopyArgs c = {};
+      if (n.copy_a) add_copy(&c, s.a, a->ranks, e, a->a, n.ld_a, work);
+      if (n.copy_b)
+        add_copy(&c, s.b, a->ranks, e, a->b, n.ld_b, work + n.bytes_a);
+      const int rc = launched(call, dpar::products::launch_copy(c, stream));
+      if (rc) return rc;
     }
-    const int rc = launched(call, e);
+    hipError_t err;
+    switch (t) {
+      case Type::BF16:
+        err = dpar::products::launch_bf16(s.form, *a, stream);
+        break;
+      case Type::F16:
+        err = dpar::products::launch_f16(s.form, *a, stream);
+        break;
+      default: err = dpar::products::launch_f32(s.form, *a, stream);
+    }
+    const int rc = launched(call, err);
     if (rc) return rc;
   }
   return DPAR_SUCCESS;
@@ -439,14 +547,14 @@ int linear_impl(const void* const* x, const void* const* w,
     return rc;
   if (!o.rows || !o.out) return DPAR_SUCCESS;
   Args a = {};
-  a.ni = o.rows, a.nj = o.out, a.nc = o.in;
-  a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz, a.lde = o.ldr;
-  a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
-  a.fast = m[0].aligned(p) && m[1].aligned(p) && o.in * e % 16 == 0 &&
-           o.in && o.ldx < kFastPitch && o.ldw < kFastPitch;
+  a.ldo = o.ldy, a.ldk = o.ldz, a.lde = o.ldr;
+  a.act = o.act, a.out32 = eo == 4;
+  Step s;
+  steps_of(DPAR_LINEAR, o, t, false, false, &s);
+  s.a.fast = m[0].fast(p), s.b.fast = m[1].fast(p);
   a.wide_out = m[2].aligned(p) && m[3].aligned(p) && m[4].aligned(p) &&
                m[5].aligned(p);
-  return run_product(call, Form::LINEAR, t, p, &a, ws, cus, stream,
+  return run_product(call, t, p, s, &a, ws, bytes, cus, stream,
                      [&](int k, int i) {
                        a.a[0][k] = m[0].rank(i);
                        a.b[0][k] = m[1].rank(i);
@@ -485,15 +593,14 @@ int gated_impl(const void* const* x, const void* const* wg,
     return rc;
   if (!o.rows || !o.out) return DPAR_SUCCESS;
   Args a = {};
-  a.ni = o.rows, a.nj = o.out, a.nc = o.in;
-  a.lda = o.ldx, a.ldb = o.ldw, a.ldo = o.ldy, a.ldk = o.ldz;
-  a.pairs = 1, a.act = o.act, a.out32 = eo == 4;
-  a.fast = m[0].aligned(p) && m[1].aligned(p) && m[2].aligned(p) &&
-           o.in * e % 16 == 0 && o.in && o.ldx < kFastPitch &&
-           o.ldw < kFastPitch;
+  a.ldo = o.ldy, a.ldk = o.ldz;
+  a.act = o.act, a.out32 = eo == 4;
+  Step s;
+  steps_of(DPAR_GATED, o, t, false, false, &s);
+  s.a.fast = m[0].fast(p), s.b.fast = m[1].fast(p) && m[2].fast(p);
   a.wide_out = m[3].aligned(p) && m[4].aligned(p) && m[5].aligned(p) &&
                m[6].aligned(p) && m[7].aligned(p);
-  return run_product(call, Form::GATED, t, p, &a, ws, cus, stream,
+  return run_product(call, t, p, s, &a, ws, bytes, cus, stream,
                      [&](int k, int i) {
                        a.a[0][k] = m[0].rank(i);
                        a.b[0][k] = m[1].rank(i);
@@ -596,16 +703,17 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
   // with no activation the products read dy itself
   const Mat& d0 = slope ? m[6] : m[0];
   const Mat& d1 = m[7];
+  const dpar_product_call_t which =
+      gated ? DPAR_GATED_BACKWARD : DPAR_LINEAR_BACKWARD;
+  const bool dz_fast = d0.fast(p) && d1.fast(p);
   if (dx && o.rows && o.in) {
     Args a = {};
-    a.ni = o.rows, a.nj = o.in, a.nc = o.out;
-    a.lda = d0.ld, a.ldb = o.ldw, a.ldo = o.lddx;
-    a.pairs = pairs, a.out32 = eo == 4;
-    a.fast = d0.aligned(p) && d1.aligned(p) && m[2].aligned(p) &&
-             m[3].aligned(p) && o.out * e % 16 == 0 && o.in * e % 16 == 0 &&
-             o.out && d0.ld < kFastPitch && o.ldw < kFastPitch;
+    a.ldo = o.lddx, a.out32 = eo == 4;
     a.wide_out = m[8].aligned(p);
-    rc = run_product(call, Form::DX, t, p, &a, ws, cus, stream,
+    Step s;
+    steps_of(which, o, t, true, false, &s);
+    s.a.fast = dz_fast, s.b.fast = m[2].fast(p) && m[3].fast(p);
+    rc = run_product(call, t, p, s, &a, ws, bytes, cus, stream,
                      [&](int k, int i) {
                        a.a[0][k] = d0.rank(i);
                        a.a[1][k] = d1.rank(i);
@@ -617,14 +725,12 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
   }
   if (dw && o.out && (o.in || db)) {
     Args a = {};
-    a.ni = o.out, a.nj = o.in, a.nc = o.rows;
-    a.lda = d0.ld, a.ldb = o.ldx, a.ldo = o.lddw;
-    a.pairs = pairs, a.out32 = eo == 4;
-    a.fast = d0.aligned(p) && d1.aligned(p) && m[1].aligned(p) &&
-             o.out * e % 16 == 0 && o.in * e % 16 == 0 && o.in && o.rows &&
-             d0.ld < kFastPitch && o.ldx < kFastPitch;
+    a.ldo = o.lddw, a.out32 = eo == 4;
     a.wide_out = m[9].aligned(p) && m[10].aligned(p);
-    rc = run_product(call, Form::DW, t, p, &a, ws, cus, stream,
+    Step s;
+    steps_of(which, o, t, false, true, &s);
+    s.a.fast = dz_fast, s.b.fast = m[1].fast(p);
+    rc = run_product(call, t, p, s, &a, ws, bytes, cus, stream,
                      [&](int k, int i) {
                        a.a[0][k] = d0.rank(i);
                        a.a[1][k] = d1.rank(i);

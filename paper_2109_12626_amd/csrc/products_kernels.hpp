@@ -773,12 +773,12 @@ struct Tiled {
     if constexpr (FAST) {
 #pragma unroll
       for (int n = 0; n < OA::N; ++n)
-        va[n] = OA::offset(a.lda, i0, a.ni, n, t);
+        va[n] = OA::offset(a.lda, i0, a.na, n, t);
       // (GATED: the tile's second half holds u's rows, from j0 again)
 #pragma unroll
       for (int n = 0; n < OB::N; ++n)
-        vb[n] = kGated ? OB::offset(a.ldb, j0, a.nj, n % (OB::N / 2), t)
-                       : OB::offset(a.ldb, j0, a.nj, n, t);
+        vb[n] = kGated ? OB::offset(a.ldb, j0, a.nb, n % (OB::N / 2), t)
+                       : OB::offset(a.ldb, j0, a.nb, n, t);
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds +
                           uniform(wave) * 1024;
@@ -795,7 +795,7 @@ struct Tiled {
       const size_t c0 = (size_t)xa.c * KT;
       const bool all = xa.c < whole;
       const uint32_t ga =
-          all ? 0 : OA::guard(a.lda, i0, a.ni, c0, a.nc, 0, t);
+          all ? 0 : OA::guard(a.lda, i0, a.na, c0, a.nc, 0, t);
 #pragma unroll
       for (int n = n0; n < n1; ++n) {
         const int m = n - OA::N;
@@ -805,7 +805,7 @@ struct Tiled {
         else
           dma16(d + n * kThreads * 16, kGated && m >= OB::N / 2 ? xb.u : xb.p,
                 all ? vb[m]
-                    : OB::guarded(vb[m], OB::guard(a.ldb, j0, a.nj, c0, a.nc,
+                    : OB::guarded(vb[m], OB::guard(a.ldb, j0, a.nb, c0, a.nc,
                                                    m, t)));
       }
     };
@@ -1028,10 +1028,10 @@ struct PingPong {
 
     uint32_t va[NA], vb[NB];
 #pragma unroll
-    for (int n = 0; n < NA; ++n) va[n] = OA::offset(a.lda, i0, a.ni, n, t);
+    for (int n = 0; n < NA; ++n) va[n] = OA::offset(a.lda, i0, a.na, n, t);
 #pragma unroll
     for (int n = 0; n < NB; ++n)
-      vb[n] = OB::offset(a.ldb, j0, a.nj, kGated ? n % (NB / 2) : n, t);
+      vb[n] = OB::offset(a.ldb, j0, a.nb, kGated ? n % (NB / 2) : n, t);
     LDS char* const ringb = lds + kRingA * kSlotA;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds + wave * 1024;
 
@@ -1048,7 +1048,7 @@ struct PingPong {
 #pragma unroll
         for (int n = 0; n < NA; ++n) dma16(d + n * kThreads * 16, xa.p, va[n]);
       } else {
-        const uint32_t g = OA::guard(a.lda, i0, a.ni, (size_t)xa.c * KT, a.nc,
+        const uint32_t g = OA::guard(a.lda, i0, a.na, (size_t)xa.c * KT, a.nc,
                                      0, t);
 #pragma unroll
         for (int n = 0; n < NA; ++n)
@@ -1067,7 +1067,7 @@ struct PingPong {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
           dma16(d + n * kThreads * 16, kGated && n >= NB / 2 ? xb.u : xb.p,
-                OB::guarded(vb[n], OB::guard(a.ldb, j0, a.nj,
+                OB::guarded(vb[n], OB::guard(a.ldb, j0, a.nb,
                                              (size_t)xb.c * KT, a.nc, n, t)));
       }
       xb.next();
