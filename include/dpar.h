@@ -463,12 +463,13 @@ const char* dpar_last_error(void);
  * result element the call does nothing.
  *
  * The calls enqueue kernels only: they allocate nothing, keep nothing from
- * one call to the next, may run on concurrent streams and may be captured into a
- * HIP graph with any executor state.  A product with few result tiles and a
- * long sum splits the sum over workgroups and joins the parts in a fixed order
- * in a workspace (dpar_product_workspace); without one it runs unsplit.
- * Results are the same from run to run; with and without a workspace they
- * differ by the order of 32-bit additions. */
+ * one call to the next, may run on concurrent streams (each with a workspace
+ * of its own) and may be captured into a HIP graph.  A product with few result
+ * tiles and a long sum splits the sum over workgroups and joins the parts in a
+ * fixed order in a workspace (dpar_product_workspace); a large one with
+ * operands off 16 bytes copies them there first.  Without a workspace it runs
+ * without either.  Results are the same from run to run; with and without a
+ * workspace they differ by the order of 32-bit additions. */
 typedef enum {
     DPAR_ACT_NONE = 0,
     DPAR_ACT_RELU = 1,      /* max(z, 0); slope 0 at 0 */
