@@ -1,4 +1,5 @@
-"""A gated feed-forward layer split over p ranks: y = x + W2 (silu(Wg x) * Wu x).
+"""A gated feed-forward layer split over p ranks:
+y = x + W2 (silu(Wg x) * Wu x).
 
 Each rank holds n_hidden / p columns of the hidden layer: rows of Wg and Wu,
 columns of W2.  Forward: the gated projections and the second product of all

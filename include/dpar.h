@@ -421,7 +421,9 @@ const char* dpar_last_error(void);
  *                           (unit=), work items, the kernel that runs
  *                           (kernel=: subtree calls of SPLIT and of fused
  *                           launches run level items, fused calls of at most
- *                           8 ranks the register kernel) */
+ *                           8 ranks the register kernel); of a layer product:
+ *                           its form, sizes, operands as they are read and
+ *                           kernel (few rows, or results per workgroup) */
 
 /* ---------------------------------------------------------------------------
  * Layer products: what makes the rows that reduction-to-all sums when a layer

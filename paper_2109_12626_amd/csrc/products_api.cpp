@@ -3,9 +3,11 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <new>
 #include <vector>
 
@@ -191,14 +193,23 @@ int check_options(const char* call, int p, const dpar_product_t* opt,
   return DPAR_SUCCESS;
 }
 
+// CUs of the current device (asked once per device).
 int cu_count() {
+  constexpr int kKnown = 64;
+  static std::atomic<int> known[kKnown];
   int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount,
+  if (hipGetDevice(&dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return 256;
+  }
+  if (dev < kKnown) cus = known[dev].load(std::memory_order_relaxed);
+  if (cus > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount,
                             dev) != hipSuccess || cus < 1) {
     (void)hipGetLastError();
     return 256;
   }
+  if (dev < kKnown) known[dev].store(cus, std::memory_order_relaxed);
   return cus;
 }
 
@@ -457,6 +468,27 @@ void add_copy(dpar::products::CopyArgs* c, const Stored& m, int ranks,
   }
 }
 
+// DPAR_LOG=1: one line per product on stderr with the kernel that runs.
+void log_plan(const Step& s, Type t, int ranks, const Plan& n) {
+  static const char* forms[] = {"linear", "gated", "dx", "dw"};
+  std::fprintf(stderr,
+               "dpar: product=%s %s ranks=%d rows=%zu cols=%zu sum=%zu "
+               "pairs=%d operands=%s",
+               forms[(int)s.form],
+               t == Type::F32 ? "float32" : t == Type::BF16 ? "bfloat16"
+                                                            : "float16",
+               ranks, s.ni, s.nj, s.nc, s.pairs,
+               n.copy_a || n.copy_b ? "copied" : n.fast ? "aligned"
+                                                        : "unaligned");
+  if (n.shape.waves)
+    std::fprintf(stderr, " kernel=few sets=%d waves=%d\n", n.shape.sets,
+                 n.shape.waves);
+  else
+    std::fprintf(stderr, " kernel=%zux%zu%s splits=%d\n",
+                 kTileRows[n.shape.tile], kTileCols[n.shape.tile],
+                 n.shape.tile == 1 ? "x4" : "", n.shape.splits);
+}
+
 // Runs one product over all ranks.  a: everything but the addresses, which
 // `fill` writes for a rank; s: the product with its operands' alignment.
 template <typename Fill>
@@ -466,6 +498,8 @@ int run_product(const char* call, Type t, int p, const Step& s, Args* a,
   const int per = ranks_per_launch(p);
   const Plan n = plan_of(s, t, per, cus, ws ? bytes : 0);
   const size_t e = t == Type::F32 ? 4 : 2;
+  const char* log = std::getenv("DPAR_LOG");
+  if (log && std::atoi(log) != 0) log_plan(s, t, per, n);
   a->ni = s.ni, a->nj = s.nj, a->nc = s.nc;
   a->pairs = s.pairs;
   a->lda = n.copy_a ? n.ld_a : s.a.ld;
@@ -693,8 +727,12 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
       }
       hipError_t e;
       switch (t) {
-        case Type::BF16: e = dpar::products::launch_slope_bf16(s, stream); break;
-        case Type::F16: e = dpar::products::launch_slope_f16(s, stream); break;
+        case Type::BF16:
+          e = dpar::products::launch_slope_bf16(s, stream);
+          break;
+        case Type::F16:
+          e = dpar::products::launch_slope_f16(s, stream);
+          break;
         default: e = dpar::products::launch_slope_f32(s, stream);
       }
       if ((rc = launched(call, e))) return rc;

@@ -1,10 +1,12 @@
-// Layer products on gfx950's matrix cores: one tiled kernel for every form
-// (products.hpp), types bf16, fp16 and fp32, results accumulated in fp32.
+// Layer products on gfx950's matrix cores: types bf16, fp16 and fp32, every
+// form of products.hpp, results accumulated in fp32.  Figures: one MI355X,
+// sizes as rows x in x out.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "products.hpp"
@@ -199,11 +201,9 @@ __device__ const i32x4 g_zero = {0, 0, 0, 0};
 //   RC (one step of the contraction, W values): lanes read 4 contraction
 //      rows x 16 values (16-bit, transposing reads), or one value each (32).
 // G: distance of the 4-value groups that one matrix row index takes.
-// L: bytes of a CC row (128, or 64: 4 pieces, 4 rows share the banks).
-template <Type T, bool CC, int W, int G, int L>
+template <Type T, bool CC, int W, int G>
 __device__ inline int key_of(int row) {
   if (CC) {
-    if (L == 64) return (row / G) & 3;
     if (G == 4) return row & 7;
     return (row & 3) | ((row / G & 1) << 2);
   }
@@ -285,19 +285,19 @@ using Yes = std::integral_constant<bool, true>;
 using No = std::integral_constant<bool, false>;
 
 // One operand's tile: W rows (CC) or W values of every contraction step (RC).
-template <Type T, bool CC, int W, int G, int THREADS, int L = kLine>
+template <Type T, bool CC, int W, int G, int THREADS>
 struct Operand {
   using V = typename Elem<T>::V;
   static constexpr int E = 16 / sizeof(V);       // values per piece
-  static constexpr int KT = L / sizeof(V);       // contraction per tile
-  static constexpr int N = W * L / 16 / THREADS; // pieces per thread
-  static constexpr int P = CC ? L / 16 : W / E;  // pieces per LDS row
+  static constexpr int KT = kLine / sizeof(V);   // contraction per tile
+  static constexpr int N = W * 8 / THREADS;      // pieces per thread
+  static constexpr int P = CC ? 8 : W / E;       // pieces per LDS row
 
   // row, first value of thread t's n-th piece (LDS order is linear in t)
   static __device__ void at(int n, int t, int* row, int* val) {
     const int o = n * THREADS + t;
     *row = o / P;
-    *val = ((o % P) ^ key_of<T, CC, W, G, L>(*row)) * E;
+    *val = ((o % P) ^ key_of<T, CC, W, G>(*row)) * E;
   }
 
   // Byte offset of a piece from the tile's first value at contraction 0.
@@ -318,7 +318,7 @@ struct Operand {
   // Bytes from one contraction tile to the next, and to the tile's first
   // value.
   static __device__ size_t step(size_t ld) {
-    return CC ? (size_t)L : (size_t)KT * ld * sizeof(V);
+    return CC ? (size_t)kLine : (size_t)KT * ld * sizeof(V);
   }
   static __device__ size_t origin(size_t ld, size_t i0) {
     return (CC ? i0 * ld : i0) * sizeof(V);
@@ -381,15 +381,15 @@ struct Operand {
     const int r = lane & 15, q = lane >> 4;
     if constexpr (CC) {
       const int row = first + (r >> 2) * G + group_of(r >> 2, n) + (r & 3);
-      const int piece = (ks * 4 + q) ^ key_of<T, CC, W, G, L>(row);
-      return *(LDS i32x4*)(s + row * L + piece * 16);
+      const int piece = (ks * 4 + q) ^ key_of<T, CC, W, G>(row);
+      return *(LDS i32x4*)(s + row * kLine + piece * 16);
     } else if constexpr (T == Type::F32) {
       i32x4 v;
       const int col = first + (r >> 2) * G + group_of(r >> 2, n) + (r & 3);
       for (int k = 0; k < 4; ++k) {
         const int c = ks * 16 + q * 4 + k;
         v[k] = *(LDS int*)(s + c * (W * 4) +
-                           ((col >> 2) ^ key_of<T, CC, W, G, L>(c)) * 16 +
+                           ((col >> 2) ^ key_of<T, CC, W, G>(c)) * 16 +
                            (col & 3) * 4);
       }
       return v;
@@ -403,7 +403,7 @@ struct Operand {
         const int c = ks * 32 + q * 8 + k * 4 + (r >> 2);
         h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (LDS i16x4*)(s + c * (W * 2) +
-                         ((col >> 3) ^ key_of<T, CC, W, G, L>(c)) * 16 +
+                         ((col >> 3) ^ key_of<T, CC, W, G>(c)) * 16 +
                          ((col >> 2) & 1) * 8));
       }
       i32x4 v;
@@ -561,13 +561,34 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
   }
 }
 
+// One operand's addresses along the contraction: the tile to ask for next, kept
+// in scalar registers so that the loop neither loads nor multiplies for them.
+// DX: the second pair follows the first.
+struct Walk {
+  const char *p, *u;          // the tile's first value (u: GATED, of u)
+  const char *o, *ou;         // the operands themselves
+  const char *p2, *o2;        // DX: the second pair's
+  size_t step;
+  unsigned c, n;              // the tile, and the tiles of a pair
+
+  __device__ void next() {
+    p = uniform(p + step);
+    u = uniform(u + step);
+    if (++c == n && p2) {
+      p = p2;
+      o = o2;
+      c = 0;
+    }
+  }
+};
+
 // OP's addresses from tile `first` on; b, b2: the (first) pair's and the second
 // pair's operand, u: GATED, the second weights.
-template <Type T, Form F, typename OP, typename W>
-__device__ inline W walk_from(const void* b, const void* u, const void* b2,
-                              size_t ld, size_t i0, unsigned first,
-                              unsigned tiles) {
-  W x;
+template <Form F, typename OP>
+__device__ inline Walk walk_from(const void* b, const void* u, const void* b2,
+                                 size_t ld, size_t i0, unsigned first,
+                                 unsigned tiles) {
+  Walk x;
   x.step = OP::step(ld);
   x.n = tiles;
   const size_t o = OP::origin(ld, i0);
@@ -610,31 +631,11 @@ struct Place {
     pair = form == Form::DW ? rest % a.pairs : 0;
     rank = form == Form::DW ? rest / a.pairs : rest;
     // groups of 8 tile rows, columns inside
-    const unsigned row8 = tile / (8 * (unsigned)nt), in = tile % (8 * (unsigned)nt);
+    const unsigned eight = 8 * (unsigned)nt;
+    const unsigned row8 = tile / eight, in = tile % eight;
     const unsigned left = (unsigned)mt - row8 * 8, high = left < 8 ? left : 8;
     i0 = (size_t)uniform(row8 * 8 + in % high) * BM;
     j0 = (size_t)uniform(in / high) * BJ;
-  }
-};
-
-// One operand's addresses along the contraction: the tile to ask for next, kept
-// in scalar registers so that the loop neither loads nor multiplies for them.
-// DX: the second pair follows the first.
-struct Walk {
-  const char *p, *u;          // the tile's first value (u: GATED, of u)
-  const char *o, *ou;         // the operands themselves
-  const char *p2, *o2;        // DX: the second pair's
-  size_t step;
-  unsigned c, n;              // the tile, and the tiles of a pair
-
-  __device__ void next() {
-    p = uniform(p + step);
-    u = uniform(u + step);
-    if (++c == n && p2) {
-      p = p2;
-      o = o2;
-      c = 0;
-    }
   }
 };
 
@@ -672,7 +673,8 @@ struct Results {
     // Results by way of LDS (each wavefront its own part, MH of its tile rows
     // at a time), so that 8 consecutive ones are in one lane, whole rows side
     // by side in a store, and the code that finishes them stays short.
-    constexpr int MH = MI < 4 ? MI : 4, CH = WN / 4, PER = (kGated ? WN / 2 : WN) / 8;
+    constexpr int MH = MI < 4 ? MI : 4, CH = WN / 4,
+                  PER = (kGated ? WN / 2 : WN) / 8;
     constexpr int kTurn = CH < 16 ? CH - 1 : 15;   // pieces exchanged by row
     LDS char* mine = lds + wave * (MH * 16 * WN * 4);
     // a lane's results are all in the same 8 columns
@@ -727,8 +729,22 @@ struct Results {
   }
 };
 
-// ---------------------------------------------------------------- the kernel
+// ---------------------------------------------------------------- the kernels
 
+// C = A B over BM x BN results per workgroup (GATED: BN / 2 of g and of u), a
+// tile of 128 bytes of the contraction at a time from one of R buffers in LDS.
+// A result costs 2 / BN + 2 / BM values read from L2 per product, so large
+// sizes are bound by the matrix cores with large tiles (PingPong below) and
+// small ones by how many workgroups there are: 64 x 64 with two buffers (5
+// workgroups per CU) or four (2 per CU, three tiles on their way: 128 x 4096 x
+// 4096 26.6 against 37.0 us), 128 x 128 with two (2 per CU).  fp32 always runs
+// here, bound by its matrix products (76% busy, 124 TFLOP/s at 8 x 256 x 1024
+// x 4096).
+//
+// FAST: operands of whole aligned pieces, straight to LDS.  Else by way of
+// registers, half a tile ahead (asking a whole tile ahead was no faster: 36 and
+// 38 us at 7 x 875 x 1001 x 1000; loads off 16 bytes take two to three times
+// as long).
 template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 struct Tiled {
   using V = typename Elem<T>::V;
@@ -783,11 +799,10 @@ struct Tiled {
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds +
                           uniform(wave) * 1024;
 
-    Walk xa = walk_from<T, F, OA, Walk>(a.a[pair][rank], nullptr, a.a[1][rank],
-                                        a.lda, i0, k0, nk1),
-         xb = walk_from<T, F, OB, Walk>(a.b[0][rank],
-                                        kGated ? a.b[1][rank] : nullptr,
-                                        a.b[1][rank], a.ldb, j0, k0, nk1);
+    Walk xa = walk_from<F, OA>(a.a[pair][rank], nullptr, a.a[1][rank], a.lda,
+                               i0, k0, nk1),
+         xb = walk_from<F, OB>(a.b[0][rank], kGated ? a.b[1][rank] : nullptr,
+                               a.b[1][rank], a.ldb, j0, k0, nk1);
     constexpr int kPieces = OA::N + OB::N;
     // Pieces n0 .. n1 - 1 of the next tile (A's, then B's) into a buffer.
     auto dma = [&](int buf, int n0, int n1) {
@@ -866,7 +881,7 @@ struct Tiled {
     // this tile, so its buffer takes the tile after next, and the next tile,
     // asked for one tile ago, has landed.  The order is the program's
     // (sched_barrier): left alone the compiler reads each fragment just before
-    // its use, 1.4 times slower at 8192 x 4096 x 16384.
+    // its use.
     i32x4 fa[MI], fb[2][NJ];
     auto read_b = [&](int ks, int buf) {
       LDS char* sb = lds + buf * kBytes + kBytesA;
@@ -885,8 +900,9 @@ struct Tiled {
       // row m of `sum`: sums of A's rows m * 16 .., by the wavefronts that
       // share them in turn
       if constexpr (with_sums)
-        if (m % (BN / WN) == wn) sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
-                           fa[m], sum);
+        if (m % (BN / WN) == wn)
+          sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
+                             fa[m], sum);
     };
     static_assert(kPieces % (MI / 2) == 0);
     auto loop = [&](auto with_sums) {
@@ -986,6 +1002,12 @@ struct Tiled {
 // or 16 products of 16 x 16 x 32, 512 or 256 cycles); then a barrier, and they
 // change places.
 //
+// 256 x 256 (two operands of 64 KB per 2 x 256 x 256 x 64 products) reaches
+// 1250 TFLOP/s at 8192 x 4096 x 16384 with both results stored, 1470 without
+// the stores: power bound, the matrix cores 63% busy at 1.9 GHz.  256 x 128
+// fills the card with half the results (1 x 2048 x 4096 x 4096: 69 us, 80 with
+// 256 x 256, 76 with 128 x 128).
+//
 // Operands of whole aligned pieces only (FAST in Tiled).
 template <Type T, Form F, int BN>
 struct PingPong {
@@ -1035,11 +1057,10 @@ struct PingPong {
     LDS char* const ringb = lds + kRingA * kSlotA;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds + wave * 1024;
 
-    Walk xa = walk_from<T, F, OA, Walk>(a.a[pair][rank], nullptr, a.a[1][rank],
-                                      a.lda, i0, k0, nk1),
-         xb = walk_from<T, F, OB, Walk>(a.b[0][rank],
-                                      kGated ? a.b[1][rank] : nullptr,
-                                      a.b[1][rank], a.ldb, j0, k0, nk1);
+    Walk xa = walk_from<F, OA>(a.a[pair][rank], nullptr, a.a[1][rank], a.lda,
+                               i0, k0, nk1),
+         xb = walk_from<F, OB>(a.b[0][rank], kGated ? a.b[1][rank] : nullptr,
+                               a.b[1][rank], a.ldb, j0, k0, nk1);
 
     // A's or B's part of the next tile into a slot.
     auto ask_a = [&](int slot) {
@@ -1195,12 +1216,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
 
 // ---------------------------------------------------------------- few rows
 
-// Few rows of x (MT tiles of 16): a wavefront takes NW x 16 rows of w (GATED:
-// half of them of each) and one of S parts of the contraction, straight from memory to
-// the matrix cores' registers, U steps of loads at a time; the workgroup's S
-// wavefronts join their sums in LDS, in order.  Every weight is read once, by
-// all lanes of a wavefront side by side (64 bytes of 16 rows a load); x is
-// small and comes from the caches.
+// Few rows of x (MT tiles of 16), bound by one read of the weights: a wavefront
+// takes NW x 16 rows of w (GATED: half of them of each) and one of S parts of
+// the contraction, straight from memory to the matrix cores' registers, U steps
+// of loads at a time; the workgroup's S wavefronts join their sums in LDS, in
+// order.  Every weight is read once, by all lanes of a wavefront side by side
+// (64 bytes of 16 rows a load); x is small and comes from the caches.  Runs
+// what FewFast cannot: operands off 16 bytes.
 template <Type T, Form F, bool FAST, int MT, int NW, int S>
 struct Few {
   using V = typename Elem<T>::V;
@@ -1320,7 +1342,9 @@ struct Few {
 // than 64 bytes of 16 rows (a copy of the loads alone: 6.5 against 5.9 TB/s
 // at 268 MB); x goes to registers.  Each wavefront has two chunks of LDS of
 // its own and needs no barrier: while it multiplies one chunk the next is on
-// its way.  The NW sets of weight rows take turns and share x.
+// its way.  The NW sets of weight rows take turns and share x.  8 x 1 x 4096 x
+// 2048 gated: 40.9 us, 6.6 TB/s (53.8 by way of registers); 48 x 4096 x 8192
+// gated 28.9, of which x's loads are a third.
 template <Type T, Form F, int MT, int NW, int S>
 struct FewFast {
   using V = typename Elem<T>::V;
@@ -1459,7 +1483,8 @@ __global__ __launch_bounds__(S * 64) void k_few(Args) {
 }
 
 // Joins the parts of a split contraction in their order and finishes: 4
-// results per thread.
+// results per thread, bound by reading the parts (about 4 us more than their
+// bytes at 2.3 TB/s, the writing of them included).
 template <Type T, Form F>
 __global__ __launch_bounds__(256) void k_join(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1504,6 +1529,10 @@ __global__ __launch_bounds__(256) void k_join(Args) {
   }
 }
 
+// The gradients before the activation: 16 bytes of a row per thread and turn,
+// bound by memory (5 x 8 x 2048 x 2048 bf16: 70 us, 4.8 TB/s, the rate of a
+// copy).  Kept apart from the products that read them, each value several
+// times: there the slope would be computed as often.
 template <Type T, bool GATED>
 __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
   GivenSlope& a = *(GivenSlope*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1544,55 +1573,64 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
 
 // ---------------------------------------------------------------- launches
 
-hipError_t launch_tiles(void (*k)(Args), Form f, const Args& a, int bm, int bj,
-                        int threads, size_t bytes, hipStream_t stream) {
+// Launches K; more than 64 KB of LDS is asked for once per device.
+template <void (*K)(Args)>
+hipError_t launch_kernel(const Args& a, size_t groups, int threads,
+                         size_t bytes, hipStream_t stream) {
+  if (groups > 0x7fffffffu) return hipErrorInvalidConfiguration;
+  if (bytes > 65536) {
+    static std::atomic<uint64_t> asked{0};     // one bit per device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(asked.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute((const void*)K,
+                              hipFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)bytes);
+      if (e != hipSuccess) return e;
+      asked.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL(K, dim3((unsigned)groups), dim3(threads), bytes, stream,
+                     a);
+  return hipGetLastError();
+}
+
+template <void (*K)(Args)>
+hipError_t launch_tiles(Form f, const Args& a, int bm, int bj, int threads,
+                        size_t bytes, hipStream_t stream) {
   const size_t tiles = (a.ni + bm - 1) / bm *
                        (a.nj ? (a.nj + bj - 1) / bj : 1);
   const size_t n = tiles * a.ranks * (f == Form::DW ? a.pairs : 1) * a.splits;
   if (n == 0) return hipSuccess;
-  if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
-  if (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(
-        (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
-        (int)bytes);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(threads), bytes, stream, a);
-  return hipGetLastError();
+  return launch_kernel<K>(a, n, threads, bytes, stream);
 }
 
 template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 hipError_t go(const Args& a, hipStream_t stream) {
   using K = Tiled<T, F, FAST, BM, BN, WM, WN, R>;
-  return launch_tiles(k_tiled<T, F, FAST, BM, BN, WM, WN, R>, F, a, BM, K::BJ,
-                      K::kThreads, R * K::kBytes, stream);
+  return launch_tiles<k_tiled<T, F, FAST, BM, BN, WM, WN, R>>(
+      F, a, BM, K::BJ, K::kThreads, R * K::kBytes, stream);
 }
 
 template <Type T, Form F, int BN>
 hipError_t go_pingpong(const Args& a, hipStream_t stream) {
   using K = PingPong<T, F, BN>;
-  return launch_tiles(k_pingpong<T, F, BN>, F, a, K::BM, K::BJ,
-                      K::kThreads, K::kLds, stream);
+  return launch_tiles<k_pingpong<T, F, BN>>(F, a, K::BM, K::BJ, K::kThreads,
+                                            K::kLds, stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int NW, int S>
 hipError_t go_few(const Args& a, hipStream_t stream) {
   using K = Few<T, F, FAST, MT, NW, S>;
   const size_t n = (a.nj + K::BJ - 1) / K::BJ * a.ranks;
-  if (n > 0x7fffffffu) return hipErrorInvalidConfiguration;
   const size_t parts = S > 1 ? (size_t)S * MT * NW * 1024 : 0;
   const size_t bytes =
       FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, NW, S>::kChunk)
            : parts;
-  auto k = k_few<T, F, FAST, MT, NW, S>;
-  if (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(
-        (const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize,
-        (int)bytes);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(S * 64), bytes, stream, a);
-  return hipGetLastError();
+  return launch_kernel<k_few<T, F, FAST, MT, NW, S>>(a, n, S * 64, bytes,
+                                                     stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int NW>
@@ -1605,7 +1643,6 @@ hipError_t pick_waves(const Args& a, hipStream_t stream) {
   }
 }
 
-// Sets of 16 weight rows per wavefront: few_sets() of them.
 template <Type T, Form F, bool FAST>
 hipError_t pick_few(const Args& a, hipStream_t stream) {
   constexpr int kOne = F == Form::GATED ? 2 : 1;

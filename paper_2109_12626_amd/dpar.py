@@ -308,12 +308,14 @@ def dpar_product_workspace(call, p, opt):
 
 
 def _product(fn, arrays, p, opt, workspace, workspace_bytes, stream):
-    if workspace is not None and not isinstance(workspace, int):
+    if isinstance(workspace, torch.Tensor):
         workspace = workspace.data_ptr()
-    return _check(fn(
-        *[a if a is None or isinstance(a, ctypes.Array) else _ptr_array(a)
-          for a in arrays],
-        p, ctypes.byref(opt), workspace, workspace_bytes, _stream(stream)))
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    rc = fn(*[a if a is None or isinstance(a, ctypes.Array)
+              else _ptr_array(a) for a in arrays],
+            p, ctypes.byref(opt), workspace, workspace_bytes, stream)
+    return rc if rc >= 0 else _check(rc)
 
 
 def dpar_linear(x, w, bias, residual, y, z, p, opt, workspace=None,
