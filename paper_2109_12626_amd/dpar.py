@@ -432,8 +432,8 @@ class _Call:
             raise ValueError(f"{name}: values of a row are not consecutive")
         if ld is not None:
             far = t.stride(-2) if shape[0] > 1 else shape[1]
-            if far < 0:
-                raise ValueError(f"{name}: negative row distance")
+            if far < shape[1]:
+                raise ValueError(f"{name}: rows {far} values apart overlap")
             if getattr(self.opt, ld) not in (0, far):
                 raise ValueError(f"{name}: another row distance than its "
                                  "companion's")

@@ -233,3 +233,29 @@ def test_tensor_front_ends_check_their_tensors():
         dpar.linear_backward(torch.zeros(3, 8), x, w, act="gelu")
     with pytest.raises(KeyError):
         dpar.linear(x, w, act="tanh")
+
+
+@pytest.mark.parametrize("name", ["x", "w", "dy", "residual"])
+@pytest.mark.parametrize("ranks", [(), (2,)])
+@pytest.mark.parametrize("view", ["expand", "window"])
+def test_front_ends_refuse_overlapping_rows(name, ranks, view):
+    # a distance of 0 would mean packed rows to the library
+    import torch
+
+    def repeated(t):
+        first = t[..., :1, :]
+        if view == "expand":
+            return first.expand(t.shape)
+        long = torch.zeros(ranks + (t.shape[-1] + t.shape[-2] - 1,))
+        return long.unfold(-1, t.shape[-1], 1)
+
+    t = {"x": torch.zeros(ranks + (3, 8)), "w": torch.zeros(ranks + (5, 8)),
+         "dy": torch.zeros(ranks + (3, 5)),
+         "residual": torch.zeros(ranks + (3, 5))}
+    assert t[name].shape == repeated(t[name]).shape
+    t[name] = repeated(t[name])
+    with pytest.raises(ValueError, match=f"{name}: rows .* overlap"):
+        if name == "dy":
+            dpar.linear_backward(t["dy"], t["x"], t["w"])
+        else:
+            dpar.linear(t["x"], t["w"], residual=t["residual"])
