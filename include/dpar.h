@@ -487,7 +487,9 @@ typedef enum {
  *   ldr   residual                   (packed: out)
  *   ldz   z, g, u, dz, dg, du        (packed: out)
  *   lddx  dx                         (packed: in)
- *   lddw  dw, dwg, dwu               (packed: in) */
+ *   lddw  dw, dwg, dwu               (packed: in)
+ * DPAR_ERR_UNSUPPORTED: a size of 2^31 or more, a distance beyond 2^38, a
+ * matrix of 2^48 bytes or more. */
 typedef struct {
     size_t rows, in, out;
     dpar_dtype_t dtype, out_dtype;

@@ -37,6 +37,10 @@ int fail(int code, const char* fmt, ...) {
 // loads; others use 64-bit addresses throughout).
 constexpr size_t kFastPitch = (size_t)1 << 23;
 
+// Addresses are below 2^48, so a matrix beyond that is none; it would overflow
+// the sizes computed from it.
+constexpr size_t kMostBytes = (size_t)1 << 48;
+
 // One array argument: p matrices of rows x cols elements, `ld` elements
 // apart.
 struct Mat {
@@ -134,6 +138,10 @@ int check_mats(const Mat* mats, int n, int p, const char* call) {
                   "%zu, length %zu", call, m.name, m.ld, m.cols);
     if (!m.at) return fail(DPAR_ERR_INVALID_ARG, "%s: null array %s", call,
                            m.name);
+    if (m.rows && m.cols &&
+        std::max(m.ld, m.cols) > kMostBytes / m.esz / m.rows)
+      return fail(DPAR_ERR_UNSUPPORTED, "%s: %s of 2^48 bytes or more", call,
+                  m.name);
     const bool empty = m.extent() == 0;
     for (int i = 0; i < p; ++i) {
       const uintptr_t a = (uintptr_t)m.at[i];

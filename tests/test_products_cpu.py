@@ -259,3 +259,16 @@ def test_front_ends_refuse_overlapping_rows(name, ranks, view):
             dpar.linear_backward(t["dy"], t["x"], t["w"])
         else:
             dpar.linear(t["x"], t["w"], residual=t["residual"])
+
+
+@needs_no_gpu
+def test_matrices_past_the_address_space_are_refused():
+    # 2^25 rows 2^38 values apart: 2^64 bytes in 16 bits, 0 in a 64-bit size
+    big = dict(rows=(1 << 25) + 1, ldx=1 << 38)
+    for call in CALLS:
+        act = "none" if call is _linear else "silu"
+        assert call(_opt(act=act, **big)) == UNSUPPORTED
+        assert call(_opt(act=act, rows=(1 << 31) - 1, ldy=1 << 38)) \
+            == UNSUPPORTED
+        assert call(_opt(act=act, n_in=(1 << 31) - 1,
+                         n_out=(1 << 31) - 1)) == UNSUPPORTED
