@@ -639,10 +639,25 @@ struct Place {
   }
 };
 
+// The sums of A over the contraction (bias gradients) that a wavefront holds:
+// of its rows m * 16 .. with m % SHARES == its share, each 16 in a product of
+// their own with ones, so that a value that is not finite stays in its row.
+template <int MI, int SHARES>
+struct Sums {
+  static constexpr int N = MI / SHARES;
+  static_assert(MI % SHARES == 0);
+  f32x4 v[N] = {};
+
+  template <Type T>
+  __device__ void add(int m, int share, i32x4 a) {
+    if (m % SHARES == share)
+      v[m / SHARES] = Elem<T>::mma(Elem<T>::ones(), a, v[m / SHARES]);
+  }
+};
+
 // Stores a wavefront's WM x WN results (GATED: g's and u's halves) from row iw
-// and column jw on, and the sums of A that it holds (those of its tile rows m
-// with m % shares == share).
-template <Type T, Form F, int WM, int WN, typename OB>
+// and column jw on, and the sums of A that it holds.
+template <Type T, Form F, int WM, int WN, int SHARES, typename OB>
 struct Results {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
@@ -650,17 +665,17 @@ struct Results {
 
   static __device__ void store(Given& a, int rank, int pair, unsigned split,
                                size_t iw, size_t jw, bool sums, int share,
-                               int shares, f32x4 sum, f32x4 (&acc)[MI][NJ],
-                               LDS char* lds, int wave, int lane) {
+                               const Sums<MI, SHARES>& sum,
+                               f32x4 (&acc)[MI][NJ], LDS char* lds, int wave,
+                               int lane) {
     if constexpr (F == Form::DW)
-      if (sums) {
-        // lane (r, q) holds the sums of rows r of tiles q * 4 ..
+      if (sums && lane < 16) {
+        // (every lane group holds the same sums, of row `lane`)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int m = (lane >> 4) * 4 + e;
-          const size_t i = iw + m * 16 + (lane & 15);
-          if (m >= MI || m % shares != share || i >= a.ni) continue;
-          float v = sum[e];
+        for (int n = 0; n < Sums<MI, SHARES>::N; ++n) {
+          const size_t i = iw + (n * SHARES + share) * 16 + lane;
+          if (i >= a.ni) continue;
+          float v = sum.v[n][0];
           if (a.splits == 1)
             store_out<1>(a.u[pair][rank], i, &v, 1, a.out32, false, V());
           else    // after all partial results: [split][rank][pair][row]
@@ -779,7 +794,7 @@ struct Tiled {
     const unsigned whole = uniform((unsigned)(a.nc / KT));  // tiles
 
     f32x4 acc[MI][NJ] = {};
-    f32x4 sum = {};
+    Sums<MI, BN / WN> sum;
     const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
 
     // addresses: a 64-bit base per operand and contraction tile (scalar), a
@@ -897,12 +912,7 @@ struct Tiled {
     };
     auto multiply = [&](int m, int ks, auto with_sums) {
       mma_row<T>(fb[ks], fa[m], acc[m]);
-      // row m of `sum`: sums of A's rows m * 16 .., by the wavefronts that
-      // share them in turn
-      if constexpr (with_sums)
-        if (m % (BN / WN) == wn)
-          sum = Elem<T>::mma((lane & 15) == m ? Elem<T>::ones() : i32x4{},
-                             fa[m], sum);
+      if constexpr (with_sums) sum.template add<T>(m, wn, fa[m]);
     };
     static_assert(kPieces % (MI / 2) == 0);
     auto loop = [&](auto with_sums) {
@@ -981,10 +991,9 @@ struct Tiled {
       }
     }
 
-    Results<T, F, WM, WN, OB>::store(
+    Results<T, F, WM, WN, BN / WN, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
-        j0 + wn * (kGated ? WN / 2 : WN), sums, wn, BN / WN, sum, acc, lds,
-        wave, lane);
+        j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
   }
 };
 
@@ -1045,7 +1054,7 @@ struct PingPong {
     const unsigned whole = uniform((unsigned)(a.nc / KT));
 
     f32x4 acc[MI][NJ] = {};
-    f32x4 sum = {};
+    Sums<MI, kAcross> sum;
     const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
 
     uint32_t va[NA], vb[NB];
@@ -1159,10 +1168,7 @@ struct PingPong {
 #pragma unroll
           for (int m = 0; m < MI; ++m) {
             mma_row<T>(fb, fa[m], acc[m]);
-            if constexpr (with_sums)
-              if (m % kAcross == wn)
-                sum = Elem<T>::mma(
-                    (lane & 15) == m ? Elem<T>::ones() : i32x4{}, fa[m], sum);
+            if constexpr (with_sums) sum.template add<T>(m, wn, fa[m]);
           }
           __builtin_amdgcn_s_setprio(0);
           __builtin_amdgcn_sched_barrier(0);
@@ -1194,9 +1200,9 @@ struct PingPong {
       }
       if (!late) __builtin_amdgcn_s_barrier();
     }
-    Results<T, F, WM, WN, OB>::store(a, rank, pair, split, i0 + wm * WM,
-                                     j0 + wn * (kGated ? WN / 2 : WN), sums,
-                                     wn, kAcross, sum, acc, lds, wave, lane);
+    Results<T, F, WM, WN, kAcross, OB>::store(
+        a, rank, pair, split, i0 + wm * WM,
+        j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
   }
 };
 

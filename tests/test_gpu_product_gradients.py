@@ -1,0 +1,146 @@
+"""Gradients of the layer products where the tests of whole results do not look:
+columns beside one that is not finite, at every kernel that sums weights'
+gradients."""
+
+import pytest
+import torch
+
+from tests._gpu import _Env, lib, need_gpu
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"float32": torch.float32, "bfloat16": torch.bfloat16,
+         "float16": torch.float16}
+
+
+def normal(gen, *shape, dtype, far=0, scale=1.0):
+    """Rows `far` values apart."""
+    t = torch.randn(*shape[:-1], shape[-1] + far, generator=gen,
+                    device="cuda") * scale
+    return t.to(TORCH[dtype])[..., :shape[-1]]
+
+
+# call, ranks, rows, in, out, type, distance between rows; the kernel of dw
+WEIGHT_KERNELS = [
+    ("gated_backward", 1, 2778, 720, 656, "bfloat16", 0,
+     "operands=aligned kernel=128x128 splits="),
+    ("gated_backward", 8, 47, 80, 1544, "float16", 0,
+     "operands=aligned kernel=128x128 splits=1"),
+    ("gated_backward", 1, 5174, 552, 920, "bfloat16", 0,
+     "operands=aligned kernel=256x128 splits="),
+    ("gated_backward", 4, 42, 72, 4512, "bfloat16", 0,
+     "operands=aligned kernel=256x128 splits=1"),
+    ("gated_backward", 1, 3813, 1640, 1432, "bfloat16", 0,
+     "operands=aligned kernel=256x256 splits="),
+    ("gated_backward", 4, 44, 272, 2856, "float16", 0,
+     "operands=aligned kernel=256x256 splits=1"),
+    ("gated_backward", 1, 2125, 144, 208, "bfloat16", 0,
+     "operands=aligned kernel=64x64 splits="),
+    ("gated_backward", 4, 44, 8, 2056, "float16", 0,
+     "operands=aligned kernel=64x64 splits=1"),
+    ("linear_backward", 1, 902, 8, 216, "bfloat16", 0,
+     "operands=aligned kernel=64x64x4 splits="),
+    ("linear_backward", 1, 43, 8, 216, "float16", 0,
+     "operands=aligned kernel=64x64x4 splits=1"),
+    ("gated_backward", 1, 5695, 396, 616, "float16", 0,
+     "operands=copied kernel=128x128 splits="),
+    ("gated_backward", 1, 402, 651, 2616, "bfloat16", 0,
+     "operands=copied kernel=128x128 splits=1"),
+    ("gated_backward", 1, 3767, 267, 1792, "bfloat16", 0,
+     "operands=copied kernel=256x128 splits="),
+    ("gated_backward", 1, 411, 3616, 521, "float16", 0,
+     "operands=copied kernel=256x128 splits=1"),
+    ("gated_backward", 1, 4272, 1731, 1193, "float16", 5,
+     "operands=copied kernel=256x256 splits="),
+    ("gated_backward", 1, 209, 2316, 1759, "float16", 5,
+     "operands=copied kernel=256x256 splits=1"),
+    ("gated_backward", 1, 2204, 155, 1360, "float16", 0,
+     "operands=copied kernel=64x64 splits="),
+    ("gated_backward", 1, 513, 657, 1168, "bfloat16", 0,
+     "operands=copied kernel=64x64 splits=1"),
+    ("linear_backward", 1, 405, 5, 205, "bfloat16", 0,
+     "operands=copied kernel=64x64x4 splits=1"),
+    ("gated_backward", 1, 2285, 695, 340, "float16", 0,
+     "operands=unaligned kernel=128x128 splits="),
+    ("gated_backward", 1, 44, 264, 4961, "bfloat16", 0,
+     "operands=unaligned kernel=128x128 splits=1"),
+    ("linear_backward", 1, 455, 7, 203, "float16", 0,
+     "operands=unaligned kernel=64x64 splits="),
+    ("linear_backward", 1, 42, 1, 200, "bfloat16", 0,
+     "operands=unaligned kernel=64x64 splits=1"),
+    ("linear_backward", 1, 4802, 992, 2608, "float32", 0,
+     "operands=aligned kernel=128x128 splits="),
+    ("gated_backward", 4, 46, 208, 3648, "float32", 0,
+     "operands=aligned kernel=128x128 splits=1"),
+    ("gated_backward", 1, 482, 8, 1376, "float32", 0,
+     "operands=aligned kernel=64x64 splits="),
+    ("gated_backward", 16, 41, 8, 544, "float32", 0,
+     "operands=aligned kernel=64x64 splits=1"),
+    ("gated_backward", 1, 299, 8, 216, "float32", 0,
+     "operands=aligned kernel=64x64x4 splits="),
+    ("gated_backward", 1, 42, 8, 208, "float32", 0,
+     "operands=aligned kernel=64x64x4 splits=1"),
+    ("gated_backward", 1, 3700, 1741, 1454, "float32", 0,
+     "operands=copied kernel=128x128 splits="),
+    ("gated_backward", 1, 439, 2166, 2671, "float32", 0,
+     "operands=copied kernel=128x128 splits=1"),
+    ("gated_backward", 1, 2568, 290, 900, "float32", 0,
+     "operands=copied kernel=64x64 splits="),
+    ("gated_backward", 1, 776, 1110, 500, "float32", 0,
+     "operands=copied kernel=64x64 splits=1"),
+    ("linear_backward", 1, 5293, 6, 256, "float32", 0,
+     "operands=copied kernel=64x64x4 splits="),
+    ("gated_backward", 1, 382, 887, 332, "float32", 0,
+     "operands=copied kernel=64x64x4 splits=1"),
+    ("gated_backward", 2, 3201, 846, 359, "float32", 0,
+     "operands=unaligned kernel=128x128 splits="),
+    ("gated_backward", 16, 41, 75, 1842, "float32", 5,
+     "operands=unaligned kernel=128x128 splits=1"),
+    ("linear_backward", 1, 232, 3, 215, "float32", 0,
+     "operands=unaligned kernel=64x64 splits="),
+    ("gated_backward", 1, 40, 1, 213, "float32", 0,
+     "operands=unaligned kernel=64x64 splits=1"),
+]
+
+
+@pytest.mark.parametrize("op,p,rows,n_in,n_out,dtype,far,plan",
+                         WEIGHT_KERNELS)
+def test_columns_that_are_not_finite_stay_alone(op, p, rows, n_in, n_out,
+                                                dtype, far, plan, capfd):
+    """An infinity and a NaN in two columns of dy: the other columns' bias
+    gradients, the other rows of dw and the other rows of dx are what they are
+    with finite values there, bit for bit."""
+    need_gpu()
+    if torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("the rules count CUs")
+    d = lib()
+    g = torch.Generator("cuda").manual_seed(31)
+    x = normal(g, p, rows, n_in, dtype=dtype, far=far)
+    w = normal(g, p, n_out, n_in, dtype=dtype, far=far, scale=n_in ** -0.5)
+    dy = normal(g, p, rows, n_out, dtype=dtype, far=far)
+    kept = normal(g, p, rows, n_out, dtype=dtype)
+
+    def run():
+        if op == "linear_backward":
+            return d.linear_backward(dy, x, w, kept, act="silu", bias=True)
+        return d.gated_backward(dy, x, w, w, kept, kept, bias=True)
+
+    capfd.readouterr()
+    with _Env("DPAR_LOG", 1):
+        want = [t.clone() for t in run()]
+    log = [ln for ln in capfd.readouterr().err.splitlines()
+           if "product=dw" in ln]
+    assert len(log) == 1 and plan in log[0] and \
+        (plan[-1] == "1") == log[0].endswith("splits=1"), log
+    at = {5: float("inf"), n_out - 9: float("nan")}      # columns
+    for c, v in at.items():
+        dy[:, rows // 2, c] = v
+    got = run()
+    rows_left = [i for i in range(rows) if i != rows // 2]
+    cols_left = [j for j in range(n_out) if j not in at]
+    assert torch.equal(got[0][:, rows_left], want[0][:, rows_left])
+    for a, b in zip(got[1:], want[1:]):
+        assert torch.isfinite(b).all()
+        assert torch.equal(a[:, cols_left], b[:, cols_left])
+        for c in at:
+            assert not torch.isfinite(a[:, c]).any()
