@@ -444,7 +444,8 @@ const char* dpar_last_error(void);
  * which is dtype or FLOAT32: 32-bit results of 16-bit products are the rows
  * dpar_allreduce sums.  Every sum is held in 32 bits and rounded once, to
  * nearest even.  dz, dg and du are rounded to dtype before the products that
- * read them.  FLOAT32 products are 32-bit throughout.
+ * read them; the bias gradients are sums of the values before that rounding.
+ * FLOAT32 products are 32-bit throughout.
  *
  * Every array argument is a HOST array of p DEVICE pointers, read before the
  * call returns; an entry may be NULL where its matrix has no element.  An

@@ -16,7 +16,7 @@ enum class Type : int { F32 = 1, BF16 = 3, F16 = 4 };
 enum class Act : int { NONE = 0, RELU = 1, GELU = 2, GELU_TANH = 3, SILU = 4 };
 
 // One launch covers up to this many ranks: their addresses travel in the
-// kernel arguments (8 arrays of 48 addresses, 3 KB of the 4 KB a launch
+// kernel arguments (10 arrays of 48 addresses, 3.8 KB of the 4 KB a launch
 // takes), so a call stages nothing, allocates nothing and can be captured.
 constexpr int kRanks = 48;
 
@@ -25,7 +25,7 @@ constexpr int kRanks = 48;
 //   GATED   A = x[i][c],  B = wg, wu[j][c];   C = act(g) * u
 //   DX      A = dz[i][c], B = w[c][j], one or two pairs summed
 //   DW      A = dz[c][i], B = x[c][j]; with two pairs two results, and the
-//           sums of A over c (bias gradients)
+//           sums of A over c (bias gradients, unless SumArgs has them)
 enum class Form : int { LINEAR = 0, GATED = 1, DX = 2, DW = 3 };
 
 struct Args {
@@ -35,7 +35,7 @@ struct Args {
   const void* e[2][kRanks];
   // LINEAR: y, z; GATED: h, g (u is in `u`); DX: dx; DW: dw, dw of u
   void* o[2][kRanks];
-  // GATED: u; DW: bias gradients
+  // GATED: u; DW: bias gradients (sums)
   void* u[2][kRanks];
   size_t ni, nj, nc;         // rows and columns of C, contraction
   size_t na, nb;             // rows (columns, where stored so) of A and B
@@ -46,6 +46,7 @@ struct Args {
   int ranks, pairs;
   int act;
   int out32;                 // result in 32 bits
+  int sums;                  // DW: with the sums of A
   int splits;                // parts of the contraction
   int waves;                 // few rows: parts of the contraction per
                              // workgroup (0: tiles)
@@ -69,6 +70,18 @@ struct SlopeArgs {
   int ranks, act, gated, wide;
 };
 
+// The same with the bias gradients, sums over the rows (16-bit types).
+struct SumArgs {
+  SlopeArgs s;
+  void* db[2][kRanks];
+  float* part;               // parts of the sums, [part][rank][pair][column]
+  int parts, all, first;     // parts of the rows; ranks of the call, and the
+                             // launch's first
+  int out32;
+};
+constexpr int kSumThreads = 512, kSumLine = 128;   // bytes of a row per
+                                                   // workgroup
+
 // Copies matrices to 16-byte rows `pitch` bytes apart, zeros after the values;
 // sizes in 2-byte units.  Up to two matrices of either operand.
 struct CopyArgs {
@@ -89,6 +102,8 @@ hipError_t launch_f32(Form f, const Args& a, hipStream_t stream);
 hipError_t launch_slope_bf16(const SlopeArgs& a, hipStream_t stream);
 hipError_t launch_slope_f16(const SlopeArgs& a, hipStream_t stream);
 hipError_t launch_slope_f32(const SlopeArgs& a, hipStream_t stream);
+hipError_t launch_sums_bf16(const SumArgs& a, hipStream_t stream);
+hipError_t launch_sums_f16(const SumArgs& a, hipStream_t stream);
 
 }  // namespace products
 }  // namespace dpar

@@ -19,6 +19,7 @@ using dpar::products::Args;
 using dpar::products::Form;
 using dpar::products::kRanks;
 using dpar::products::SlopeArgs;
+using dpar::products::SumArgs;
 using dpar::products::Type;
 
 namespace {
@@ -418,6 +419,27 @@ int steps_of(dpar_product_call_t call, const dpar_product_t& o, Type t,
   return n;
 }
 
+// Bias gradients that the slopes' kernel sums (rounded slopes, 16-bit types):
+// in how many parts of the rows, and the workspace of their sums.  Workgroups
+// take 128 bytes of the columns; where these are fewer than two per CU they
+// share the rows, 128 at least to each, and a second launch joins them.
+struct SumPlan {
+  int parts;
+  size_t bytes;
+};
+bool sums_apart(Type t, bool slope) { return t != Type::F32 && slope; }
+SumPlan sums_of(int p, int pairs, size_t rows, size_t out, int cus) {
+  const size_t cols = dpar::products::kSumLine / 2;
+  const size_t n = (out + cols - 1) / cols * ranks_per_launch(p),
+               most = (size_t)cus * 2;
+  const size_t parts =
+      n ? std::min(std::min(most / n, rows / 128), (size_t)64) : 0;
+  if (parts < 2) return {1, 0};
+  const size_t bytes = parts * p * pairs * out * 4;
+  return {(int)parts, (bytes + 127) / 128 * 128};
+}
+
+// Workspace of a call: its bias gradients', then its products' (in turn).
 size_t workspace_of(dpar_product_call_t call, Type t, int p,
                     const dpar_product_t& o, int cus) {
   Step s[2];
@@ -433,6 +455,10 @@ size_t workspace_of(dpar_product_call_t call, Type t, int p,
                                 s[k].ni, s[k].nj, s[k].nc, cus, true, false);
     most = std::max(most, slow.part);
   }
+  const bool gated = call == DPAR_GATED_BACKWARD;
+  if ((gated || call == DPAR_LINEAR_BACKWARD) &&
+      sums_apart(t, gated || o.act != DPAR_ACT_NONE))
+    most += sums_of(p, gated ? 2 : 1, o.rows, o.out, cus).bytes;
   return most;
 }
 
@@ -655,6 +681,19 @@ int gated_impl(const void* const* x, const void* const* wg,
                      });
 }
 
+hipError_t launch_slope(Type t, const SlopeArgs& a, hipStream_t stream) {
+  switch (t) {
+    case Type::BF16: return dpar::products::launch_slope_bf16(a, stream);
+    case Type::F16: return dpar::products::launch_slope_f16(a, stream);
+    default: return dpar::products::launch_slope_f32(a, stream);
+  }
+}
+
+hipError_t launch_sums(Type t, const SumArgs& a, hipStream_t stream) {
+  return t == Type::BF16 ? dpar::products::launch_sums_bf16(a, stream)
+                         : dpar::products::launch_sums_f16(a, stream);
+}
+
 // Both backward calls; pairs: 1 (dpar_linear_backward) or 2.
 struct Back {
   const void* const* dy;
@@ -717,33 +756,35 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
                             t, p, o, ws, bytes, &cus)))
     return rc;
 
-  if (slope && o.rows && o.out) {
-    SlopeArgs s = {};
+  const bool apart = db && sums_apart(t, slope);
+  if (o.out && (apart || (slope && o.rows))) {
+    SumArgs q = {};
+    SlopeArgs& s = q.s;
     s.rows = o.rows, s.cols = o.out, s.ldy = o.ldy, s.ldz = o.ldz;
     s.act = o.act, s.gated = gated;
     s.wide = m[0].aligned(p);
     for (int k = 4; k < 8; ++k) s.wide &= m[k].aligned(p);
+    q.out32 = eo == 4, q.all = p, q.parts = 1;
+    if (apart && ws) {
+      const SumPlan n = sums_of(p, pairs, o.rows, o.out, cus);
+      q.parts = n.parts, q.part = (float*)ws;
+      ws = (char*)ws + n.bytes, bytes -= n.bytes;
+    }
     const int per = ranks_per_launch(p);
     for (int r0 = 0; r0 < p; r0 += per) {
-      s.ranks = std::min(per, p - r0);
+      s.ranks = std::min(per, p - r0), q.first = r0;
       for (int k = 0; k < s.ranks; ++k) {
         s.dy[k] = m[0].rank(r0 + k);
         s.z[k] = m[4].rank(r0 + k);
         s.u[k] = m[5].rank(r0 + k);
         s.dz[k] = (void*)m[6].rank(r0 + k);
         s.du[k] = (void*)m[7].rank(r0 + k);
+        q.db[0][k] = (void*)m[11].rank(r0 + k);
+        q.db[1][k] = (void*)m[12].rank(r0 + k);
       }
-      hipError_t e;
-      switch (t) {
-        case Type::BF16:
-          e = dpar::products::launch_slope_bf16(s, stream);
-          break;
-        case Type::F16:
-          e = dpar::products::launch_slope_f16(s, stream);
-          break;
-        default: e = dpar::products::launch_slope_f32(s, stream);
-      }
-      if ((rc = launched(call, e))) return rc;
+      if ((rc = launched(call, apart ? launch_sums(t, q, stream)
+                                     : launch_slope(t, s, stream))))
+        return rc;
     }
   }
   // with no activation the products read dy itself
@@ -769,9 +810,9 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
                      });
     if (rc) return rc;
   }
-  if (dw && o.out && (o.in || db)) {
+  if (dw && o.out && (o.in || (db && !apart))) {
     Args a = {};
-    a.ldo = o.lddw, a.out32 = eo == 4;
+    a.ldo = o.lddw, a.out32 = eo == 4, a.sums = db && !apart;
     a.wide_out = m[9].aligned(p) && m[10].aligned(p);
     Step s;
     steps_of(which, o, t, false, true, &s);
@@ -783,6 +824,7 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
                        a.b[0][k] = m[1].rank(i);
                        a.o[0][k] = (void*)m[9].rank(i);
                        a.o[1][k] = (void*)m[10].rank(i);
+                       if (!a.sums) return;
                        a.u[0][k] = (void*)m[11].rank(i);
                        a.u[1][k] = (void*)m[12].rank(i);
                      });

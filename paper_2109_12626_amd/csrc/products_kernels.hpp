@@ -27,6 +27,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // (indexing a by-value copy by rank would put all of it in scratch memory).
 using Given = const __attribute__((address_space(4))) Args;
 using GivenSlope = const __attribute__((address_space(4))) SlopeArgs;
+using GivenSums = const __attribute__((address_space(4))) SumArgs;
 
 // A piece is 16 bytes; every tile holds 128 bytes of the contraction: 64
 // 16-bit or 32 32-bit values, in two steps of 4 pieces (one per lane group
@@ -657,7 +658,7 @@ struct Sums {
 
 // Stores a wavefront's WM x WN results (GATED: g's and u's halves) from row iw
 // and column jw on, and the sums of A that it holds.
-template <Type T, Form F, int WM, int WN, int SHARES, typename OB>
+template <Type T, Form F, bool SUMS, int WM, int WN, int SHARES, typename OB>
 struct Results {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
@@ -668,7 +669,7 @@ struct Results {
                                const Sums<MI, SHARES>& sum,
                                f32x4 (&acc)[MI][NJ], LDS char* lds, int wave,
                                int lane) {
-    if constexpr (F == Form::DW)
+    if constexpr (SUMS)
       if (sums && lane < 16) {
         // (every lane group holds the same sums, of row `lane`)
 #pragma unroll
@@ -760,7 +761,10 @@ struct Results {
 // registers, half a tile ahead (asking a whole tile ahead was no faster: 36 and
 // 38 us at 7 x 875 x 1001 x 1000; loads off 16 bytes take two to three times
 // as long).
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
+//
+// SUMS: DW with the sums of A.
+template <Type T, Form F, bool SUMS, bool FAST, int BM, int BN, int WM, int WN,
+          int R>
 struct Tiled {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
@@ -795,7 +799,7 @@ struct Tiled {
 
     f32x4 acc[MI][NJ] = {};
     Sums<MI, BN / WN> sum;
-    const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
+    const bool sums = SUMS && a.u[pair][rank] && j0 == 0;
 
     // addresses: a 64-bit base per operand and contraction tile (scalar), a
     // 32-bit offset per piece
@@ -981,7 +985,7 @@ struct Tiled {
       for (int m = 0; m < MI; ++m) asm volatile("" : "+v"(fa[m]));
 #pragma unroll
       for (int n = 0; n < NJ; ++n) asm volatile("" : "+v"(fb[0][n]));
-      if constexpr (F == Form::DW) {
+      if constexpr (SUMS) {
         if (sums)
           loop(Yes{});
         else
@@ -991,7 +995,7 @@ struct Tiled {
       }
     }
 
-    Results<T, F, WM, WN, BN / WN, OB>::store(
+    Results<T, F, SUMS, WM, WN, BN / WN, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
         j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
   }
@@ -1017,8 +1021,8 @@ struct Tiled {
 // fills the card with half the results (1 x 2048 x 4096 x 4096: 69 us, 80 with
 // 256 x 256, 76 with 128 x 128).
 //
-// Operands of whole aligned pieces only (FAST in Tiled).
-template <Type T, Form F, int BN>
+// Operands of whole aligned pieces only (FAST in Tiled); SUMS as there.
+template <Type T, Form F, bool SUMS, int BN>
 struct PingPong {
   using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
@@ -1055,7 +1059,7 @@ struct PingPong {
 
     f32x4 acc[MI][NJ] = {};
     Sums<MI, kAcross> sum;
-    const bool sums = F == Form::DW && a.u[pair][rank] && j0 == 0;
+    const bool sums = SUMS && a.u[pair][rank] && j0 == 0;
 
     uint32_t va[NA], vb[NB];
 #pragma unroll
@@ -1190,7 +1194,7 @@ struct PingPong {
       ready(k0, k0 + 1 < k1);
       change();
       if (late) __builtin_amdgcn_s_barrier();   // one phase behind
-      if constexpr (F == Form::DW) {
+      if constexpr (SUMS) {
         if (sums)
           loop(Yes{});
         else
@@ -1200,24 +1204,25 @@ struct PingPong {
       }
       if (!late) __builtin_amdgcn_s_barrier();
     }
-    Results<T, F, WM, WN, kAcross, OB>::store(
+    Results<T, F, SUMS, WM, WN, kAcross, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
         j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
   }
 };
 
-template <Type T, Form F, int BN>
+template <Type T, Form F, bool SUMS, int BN>
 __global__ __launch_bounds__(512) void k_pingpong(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  PingPong<T, F, BN>::run(a, (LDS char*)lds);
+  PingPong<T, F, SUMS, BN>::run(a, (LDS char*)lds);
 }
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
+template <Type T, Form F, bool SUMS, bool FAST, int BM, int BN, int WM, int WN,
+          int R>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Tiled<T, F, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
+  Tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -1535,6 +1540,29 @@ __global__ __launch_bounds__(256) void k_join(Args) {
   }
 }
 
+// One piece's gradients before the activation: d (dy) becomes dz or dg, and o
+// du; z and u: their places in the kept values.
+template <Type T, bool GATED, int E, typename V>
+__device__ inline void slopes(int act, const V* z, const V* u, long left,
+                              bool wide, float (&d)[E], float (&o)[E]) {
+  float s[E], g[E];
+  fetch_vals<V, E>(z, g, left, wide);
+  if (GATED) fetch_vals<V, E>(u, s, left, wide);
+  with_act(act, [&](auto a) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      float v;
+      const float c = slope_of<a.value>(g[k], &v);
+      if (GATED) {
+        o[k] = d[k] * v;
+        d[k] = d[k] * s[k] * c;
+      } else {
+        d[k] *= c;
+      }
+    }
+  });
+}
+
 // The gradients before the activation: 16 bytes of a row per thread and turn,
 // bound by memory (5 x 8 x 2048 x 2048 bf16: 70 us, 4.8 TB/s, the rate of a
 // copy).  Kept apart from the products that read them, each value several
@@ -1555,26 +1583,100 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
        id += (size_t)gridDim.x * 256) {
     const size_t i = id / per, j = id % per * E;
     const long left = (long)a.cols - (long)j;
-    float d[E], s[E], g[E], o[E];
+    float d[E], o[E];
     fetch_vals<V, E>(dy + i * a.ldy + j, d, left, a.wide);
-    fetch_vals<V, E>(z + i * a.ldz + j, g, left, a.wide);
-    if (GATED) fetch_vals<V, E>(u + i * a.ldz + j, s, left, a.wide);
-    with_act(a.act, [&](auto act) {
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        float v;
-        const float c = slope_of<act.value>(g[k], &v);
-        if (GATED) {
-          o[k] = d[k] * v;
-          d[k] = d[k] * s[k] * c;
-        } else {
-          d[k] *= c;
-        }
-      }
-    });
+    slopes<T, GATED, E, V>(a.act, z + i * a.ldz + j,
+                           GATED ? u + i * a.ldz + j : nullptr, left, a.wide,
+                           d, o);
     store_vals<V, E>(dz + i * a.ldz + j, d, left, a.wide);
     if (GATED) store_vals<V, E>(du + i * a.ldz + j, o, left, a.wide);
   }
+}
+
+// The same with the bias gradients of 16-bit types, the sums over the rows of
+// the values before they are rounded to 16 bits.  (The products read the
+// rounded ones, and so would sums made beside them on the matrix cores, as DW
+// does for 32-bit values and for dy itself: 16-bit bias gradients would be
+// sqrt 2 times as far off, 32-bit ones 2^-9.)  A workgroup takes 128 bytes of
+// the columns of a part of the rows, 64 rows at a time; a column's values meet
+// in an order that its place alone fixes, and columns never meet.
+template <Type T, bool GATED>
+__global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
+  GivenSums& a = *(GivenSums*)__builtin_amdgcn_kernarg_segment_ptr();
+  using V = typename Elem<T>::V;
+  constexpr int E = 16 / sizeof(V), kLanes = kSumLine / 16, kCols = E * kLanes,
+                NP = GATED ? 2 : 1, kWaves = kSumThreads / 64;
+  __shared__ float lds[kWaves][NP][kCols];
+  const int t = threadIdx.x, lane = t & 63, rank = blockIdx.y;
+  const bool wide = a.s.wide;
+  const size_t strips = (a.s.cols + kCols - 1) / kCols;
+  for (size_t id = blockIdx.x; id < strips * a.parts; id += gridDim.x) {
+    const size_t strip = id % strips, part = id / strips;
+    const size_t i1 = a.s.rows * (part + 1) / a.parts;
+    const size_t j = strip * kCols + t % kLanes * E;
+    const long left = (long)a.s.cols - (long)j;
+    const V* dy = (const V*)a.s.dy[rank] + j;
+    const V* z = (const V*)a.s.z[rank] + j;
+    const V* u = GATED ? (const V*)a.s.u[rank] + j : nullptr;
+    V* dz = (V*)a.s.dz[rank] + j;
+    V* du = GATED ? (V*)a.s.du[rank] + j : nullptr;
+    float sum[NP][E] = {};
+    if (left > 0)
+      for (size_t i = a.s.rows * part / a.parts + t / kLanes; i < i1;
+           i += kSumThreads / kLanes) {
+        float d[E], o[E];
+        fetch_vals<V, E>(dy + i * a.s.ldy, d, left, wide);
+        slopes<T, GATED, E, V>(a.s.act, z + i * a.s.ldz,
+                               GATED ? u + i * a.s.ldz : nullptr, left, wide,
+                               d, o);
+        store_vals<V, E>(dz + i * a.s.ldz, d, left, wide);
+        if (GATED) store_vals<V, E>(du + i * a.s.ldz, o, left, wide);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          sum[0][k] += d[k];
+          if (GATED) sum[NP - 1][k] += o[k];
+        }
+      }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        float v = sum[p][k];
+#pragma unroll
+        for (int far = kLanes; far < 64; far *= 2) v += __shfl_xor(v, far);
+        if (lane < kLanes) lds[t / 64][p][lane * E + k] = v;
+      }
+    __syncthreads();
+    const int p = t / kCols;
+    const size_t col = strip * kCols + t % kCols;
+    if (p < NP && col < a.s.cols) {
+      float v = 0.f;
+      for (int w = 0; w < kWaves; ++w) v += lds[w][p][t % kCols];
+      if (a.parts == 1)
+        store_out<1>(a.db[p][rank], col, &v, 1, a.out32, false, V());
+      else
+        a.part[((part * a.all + a.first + rank) * NP + p) * a.s.cols + col] =
+            v;
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the sums' parts in their order.
+template <Type T>
+__global__ __launch_bounds__(256) void k_join_sums(SumArgs) {
+  GivenSums& a = *(GivenSums*)__builtin_amdgcn_kernarg_segment_ptr();
+  const int np = a.s.gated ? 2 : 1, p = blockIdx.z, rank = blockIdx.y;
+  const size_t col = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (col >= a.s.cols) return;
+  const float* w = a.part + ((a.first + (size_t)rank) * np + p) * a.s.cols +
+                   col;
+  const size_t step = (size_t)a.all * np * a.s.cols;
+  float v = 0.f;
+#pragma unroll 16
+  for (int k = 0; k < a.parts; ++k) v += w[k * step];
+  store_out<1>(a.db[p][rank], col, &v, 1, a.out32, false,
+               typename Elem<T>::V());
 }
 
 // ---------------------------------------------------------------- launches
@@ -1613,18 +1715,19 @@ hipError_t launch_tiles(Form f, const Args& a, int bm, int bj, int threads,
   return launch_kernel<K>(a, n, threads, bytes, stream);
 }
 
-template <Type T, Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
+template <Type T, Form F, bool SUMS, bool FAST, int BM, int BN, int WM, int WN,
+          int R>
 hipError_t go(const Args& a, hipStream_t stream) {
-  using K = Tiled<T, F, FAST, BM, BN, WM, WN, R>;
-  return launch_tiles<k_tiled<T, F, FAST, BM, BN, WM, WN, R>>(
+  using K = Tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>;
+  return launch_tiles<k_tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>>(
       F, a, BM, K::BJ, K::kThreads, R * K::kBytes, stream);
 }
 
-template <Type T, Form F, int BN>
+template <Type T, Form F, bool SUMS, int BN>
 hipError_t go_pingpong(const Args& a, hipStream_t stream) {
-  using K = PingPong<T, F, BN>;
-  return launch_tiles<k_pingpong<T, F, BN>>(F, a, K::BM, K::BJ, K::kThreads,
-                                            K::kLds, stream);
+  using K = PingPong<T, F, SUMS, BN>;
+  return launch_tiles<k_pingpong<T, F, SUMS, BN>>(
+      F, a, K::BM, K::BJ, K::kThreads, K::kLds, stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int NW, int S>
@@ -1668,18 +1771,27 @@ hipError_t pick_few(const Args& a, hipStream_t stream) {
   return pick_waves<T, F, FAST, 4, 4>(a, stream);
 }
 
+template <Type T, Form F, bool SUMS, bool FAST>
+hipError_t pick_tile(const Args& a, hipStream_t stream) {
+  if constexpr (T != Type::F32 && FAST) {
+    if (a.tile == 4) return go_pingpong<T, F, SUMS, 256>(a, stream);
+    if (a.tile == 3) return go_pingpong<T, F, SUMS, 128>(a, stream);
+  }
+  if (a.tile == 2) return go<T, F, SUMS, FAST, 128, 128, 64, 64, 2>(a, stream);
+  if constexpr (FAST)
+    if (a.tile == 1) return go<T, F, SUMS, FAST, 64, 64, 32, 32, 4>(a, stream);
+  return go<T, F, SUMS, FAST, 64, 64, 32, 32, 2>(a, stream);
+}
+
 template <Type T, Form F, bool FAST>
 hipError_t pick(const Args& a, hipStream_t stream) {
   if constexpr (F == Form::LINEAR || F == Form::GATED)
     if (a.waves) return pick_few<T, F, FAST>(a, stream);
-  if constexpr (T != Type::F32 && FAST) {
-    if (a.tile == 4) return go_pingpong<T, F, 256>(a, stream);
-    if (a.tile == 3) return go_pingpong<T, F, 128>(a, stream);
-  }
-  if (a.tile == 2) return go<T, F, FAST, 128, 128, 64, 64, 2>(a, stream);
-  if constexpr (FAST)
-    if (a.tile == 1) return go<T, F, FAST, 64, 64, 32, 32, 4>(a, stream);
-  return go<T, F, FAST, 64, 64, 32, 32, 2>(a, stream);
+  // (the sums cost registers: without them 128 x 128 tiles of operands off 16
+  // bytes run two to a CU)
+  if constexpr (F == Form::DW)
+    if (a.sums) return pick_tile<T, F, true, FAST>(a, stream);
+  return pick_tile<T, F, false, FAST>(a, stream);
 }
 
 template <Type T, Form F>
@@ -1714,6 +1826,25 @@ hipError_t run_slope(const SlopeArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((k_slope<T, true>), grid, dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL((k_slope<T, false>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <Type T>
+hipError_t run_sums(const SumArgs& a, hipStream_t stream) {
+  constexpr size_t kCols = kSumLine / sizeof(typename Elem<T>::V);
+  const size_t strips = (a.s.cols + kCols - 1) / kCols;
+  const dim3 grid((unsigned)std::min<size_t>(strips * a.parts, 1 << 20),
+                  a.s.ranks), threads(kSumThreads);
+  if (a.s.gated)
+    hipLaunchKernelGGL((k_sums<T, true>), grid, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_sums<T, false>), grid, threads, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hipLaunchKernelGGL((k_join_sums<T>),
+                     dim3((unsigned)((a.s.cols + 255) / 256), a.s.ranks,
+                          a.s.gated ? 2 : 1),
+                     dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -1,10 +1,12 @@
 """Gradients of the layer products where the tests of whole results do not look:
 columns beside one that is not finite, at every kernel that sums weights'
-gradients."""
+gradients; bias gradients against sums of unrounded values."""
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import products as ref
 from tests._gpu import _Env, lib, need_gpu
 
 pytestmark = pytest.mark.gpu
@@ -144,3 +146,58 @@ def test_columns_that_are_not_finite_stay_alone(op, p, rows, n_in, n_out,
         assert torch.equal(a[:, cols_left], b[:, cols_left])
         for c in at:
             assert not torch.isfinite(a[:, c]).any()
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+# rows, out: one part, several, columns of less than a piece and of several
+# strips, rows off 16 bytes, more ranks than one launch takes
+@pytest.mark.parametrize("p,rows,n_out", [
+    (1, 1, 1), (2, 5, 72), (1, 63, 64), (3, 65, 131), (1, 700, 40),
+    (1, 2048, 200), (2, 4099, 129), (50, 1030, 24), (1, 8192, 1024)])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+def test_bias_gradients_sum_unrounded_values(p, rows, n_out, act, dtype):
+    """In 32 bits they are n products and additions off, each of 2^-24, and
+    what the activation's slope is; rounding each value to 16 bits first would
+    leave 2^-9 or 2^-12 of it.  With and without a workspace."""
+    need_gpu()
+    d = lib()
+    g = torch.Generator("cuda").manual_seed(32)
+    x = normal(g, p, rows, 8, dtype=dtype)
+    w = normal(g, p, n_out, 8, dtype=dtype)
+    dy, kg, ku = (normal(g, p, rows, n_out, dtype=dtype) for _ in range(3))
+    dz, du = torch.empty_like(dy), torch.empty_like(dy)
+    f32 = dict(dtype=torch.float32, device="cuda")
+    dw, dw2 = (torch.empty(p, n_out, 8, **f32) for _ in range(2))
+    opt = d.product_options(rows, 8, n_out, dtype, "float32", act)
+    r = d.rows
+    stream = torch.cuda.current_stream()
+
+    def check(got, terms, slack):
+        bound = (rows + 3) * 2.0 ** -24 * np.abs(terms).sum(1) + slack.sum(1)
+        assert (np.abs(np64(got) - terms.sum(1)) <= bound).all()
+
+    v, s = (np64(t) for t in (dy, kg))
+    a, slope = ref.act(s, act)
+    err = 0 * v if act in ("none", "relu") else \
+        2.0 ** -20 * (1 + np.abs(s)) * np.abs(v)
+    for split in (True, False):
+        db, dbu = (torch.full((p, n_out), 7.0, **f32) for _ in range(2))
+        n = d.dpar_product_workspace("linear_backward", p, opt)
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+        ws = (ws, n) if split else (None, 0)
+        d.dpar_linear_backward(
+            r(dy), r(x), r(w), r(kg) if act != "none" else None, None, r(dw),
+            r(db), r(dz) if act != "none" else None, p, opt, *ws, stream)
+        check(db, v * slope, err)
+        n = d.dpar_product_workspace("gated_backward", p, opt)
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+        ws = (ws, n) if split else (None, 0)
+        d.dpar_gated_backward(
+            r(dy), r(x), r(w), r(w), r(kg), r(ku), None, r(dw), r(dw2), r(db),
+            r(dbu), r(dz), r(du), p, opt, *ws, stream)
+        check(db, v * np64(ku) * slope, err * np.abs(np64(ku)))
+        check(dbu, v * a, err)
