@@ -95,18 +95,31 @@ __device__ inline void mma_row(const i32x4 (&a)[N], i32x4 b, f32x4 (&c)[N]) {
 
 // ---------------------------------------------------------------- activations
 
-// 1 / x to 1 unit in the last place: a correctly rounded division takes ten
-// instructions, and the results are rounded further or no more exact.
-__device__ inline float inverse(float x) { return __builtin_amdgcn_rcpf(x); }
+// EXACT: results stored in 32 bits, a few units in the last place off.  Else
+// what is rounded to 16 bits: there exponentials and reciprocals of one
+// instruction or two will do (a correctly rounded division alone takes ten).
+template <bool EXACT>
+__device__ inline float inverse(float x) {
+  return EXACT ? 1.f / x : __builtin_amdgcn_rcpf(x);
+}
+template <bool EXACT>
+__device__ inline float power(float x) {
+  return EXACT ? expf(x) : __expf(x);
+}
 
 // 1 / (1 + exp(-z)); *both: its product with 1 minus it.  From exp(-|z|), so
 // that neither end loses what 1 - (almost 1) would.
+template <bool EXACT>
 __device__ inline float sigmoid(float z, float* both) {
-  const float e = __expf(-fabsf(z)), big = inverse(1.f + e), small = e * big;
+  const float e = power<EXACT>(-fabsf(z)), big = inverse<EXACT>(1.f + e),
+              small = e * big;
   *both = big * small;
   return z < 0.f ? small : big;
 }
-__device__ inline float sigmoid(float z) { return inverse(1.f + __expf(-z)); }
+template <bool EXACT>
+__device__ inline float sigmoid(float z) {
+  return inverse<EXACT>(1.f + power<EXACT>(-z));
+}
 
 // 0.5 (1 + tanh a) = sigmoid(2 a)
 constexpr float kTanh2 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
@@ -114,11 +127,17 @@ constexpr float kCubic = 0.044715f;
 constexpr float kInvSqrt2 = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
-// (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2): Abramowitz and Stegun 7.1.26,
-// 7.5e-8 off at most.
+// (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2).  Not EXACT: Abramowitz and
+// Stegun 7.1.26, whose truncation is 7.5e-8 at most; in 32 bits the whole is
+// up to 2.8e-7 off, a hundredth of what rounding a result of 1 to fp16 costs.
+template <bool EXACT>
 __device__ inline float normal_cdf(float z, float* density) {
+  if (EXACT) {
+    *density = expf(-0.5f * z * z);
+    return 0.5f * erfcf(-z * kInvSqrt2);
+  }
   const float x = fabsf(z) * kInvSqrt2;
-  const float t = inverse(fmaf(0.3275911f, x, 1.f));
+  const float t = inverse<false>(fmaf(0.3275911f, x, 1.f));
   const float e = __expf(-x * x);
   float p = fmaf(1.061405429f, t, -1.453152027f);
   p = fmaf(p, t, 1.421413741f);
@@ -133,63 +152,79 @@ __device__ inline float normal_cdf(float z, float* density) {
 // z is held there so that infinities give the limits.
 __device__ inline float held(float z) { return z < -128.f ? -128.f : z; }
 
-template <Act A>
+template <Act A, bool EXACT>
 __device__ inline float act_of(float z) {
   if (A == Act::RELU) return z > 0.f ? z : (z != z ? z : 0.f);
   if (A == Act::NONE) return z;
   z = held(z);
   if (A == Act::GELU) {
     float e;
-    return z * normal_cdf(z, &e);
+    return z * normal_cdf<EXACT>(z, &e);
   }
   if (A == Act::GELU_TANH)
-    return z * sigmoid(kTanh2 * (z + kCubic * z * z * z));
-  return z * sigmoid(z);
+    return z * sigmoid<EXACT>(kTanh2 * (z + kCubic * z * z * z));
+  return z * sigmoid<EXACT>(z);
 }
 
 // act(z) and act'(z)
-template <Act A>
+template <Act A, bool EXACT>
 __device__ inline float slope_of(float z, float* value) {
   if (A == Act::NONE) {
     *value = z;
     return 1.f;
   }
   if (A == Act::RELU) {
-    *value = act_of<A>(z);
+    *value = act_of<A, EXACT>(z);
     return z > 0.f ? 1.f : (z != z ? z : 0.f);
   }
   z = held(z);
   const float y = z > 128.f ? 128.f : z;
   if (A == Act::GELU) {
     float e;
-    const float c = normal_cdf(y, &e);
+    const float c = normal_cdf<EXACT>(y, &e);
     *value = z * c;
     return c + y * kInvSqrt2Pi * e;
   }
   if (A == Act::GELU_TANH) {
     float both;
-    const float s = sigmoid(kTanh2 * (y + kCubic * y * y * y), &both);
+    const float s =
+        sigmoid<EXACT>(kTanh2 * (y + kCubic * y * y * y), &both);
     *value = z * s;
     return s + y * both * kTanh2 * (1.f + 3.f * kCubic * y * y);
   }
   float both;
-  const float s = sigmoid(y, &both);
+  const float s = sigmoid<EXACT>(y, &both);
   *value = z * s;
   return s + y * both;
 }
 
-// f(activation) with the activation as a type: one branch for many values.
-template <typename Fn>
+// f(activation, EXACT) with both as types: one branch for many values.
+template <bool EXACT, typename Fn>
 __device__ inline void with_act(int act, Fn f) {
+  constexpr std::integral_constant<bool, EXACT> exact;
   switch (act) {
-    case (int)Act::RELU: f(std::integral_constant<Act, Act::RELU>()); break;
-    case (int)Act::GELU: f(std::integral_constant<Act, Act::GELU>()); break;
-    case (int)Act::GELU_TANH:
-      f(std::integral_constant<Act, Act::GELU_TANH>());
+    case (int)Act::RELU:
+      f(std::integral_constant<Act, Act::RELU>(), exact);
       break;
-    case (int)Act::SILU: f(std::integral_constant<Act, Act::SILU>()); break;
-    default: f(std::integral_constant<Act, Act::NONE>());
+    case (int)Act::GELU:
+      f(std::integral_constant<Act, Act::GELU>(), exact);
+      break;
+    case (int)Act::GELU_TANH:
+      f(std::integral_constant<Act, Act::GELU_TANH>(), exact);
+      break;
+    case (int)Act::SILU:
+      f(std::integral_constant<Act, Act::SILU>(), exact);
+      break;
+    default: f(std::integral_constant<Act, Act::NONE>(), exact);
   }
+}
+// EXACT for 32-bit values and for 32-bit results (out32) of 16-bit ones.
+template <Type T, typename Fn>
+__device__ inline void with_act(int act, bool out32, Fn f) {
+  if (T == Type::F32 || out32)
+    with_act<true>(act, f);
+  else
+    with_act<false>(act, f);
 }
 
 // ---------------------------------------------------------------- tiles
@@ -533,9 +568,9 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
     for (int k = 0; k < N; ++k) v[k] += b[0][k];
     if (V* z = (V*)a.o[1][rank])
       store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
-    with_act(a.act, [&](auto act) {
+    with_act<T>(a.act, a.out32, [&](auto act, auto exact) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = act_of<act.value>(v[k]);
+      for (int k = 0; k < N; ++k) v[k] = act_of<act.value, exact.value>(v[k]);
     });
     if (r) {
 #pragma unroll
@@ -551,9 +586,10 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
       store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
     if (V* u = (V*)a.u[0][rank])
       store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
-    with_act(a.act, [&](auto act) {
+    with_act<T>(a.act, a.out32, [&](auto act, auto exact) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = act_of<act.value>(v[k]) * u2[k];
+      for (int k = 0; k < N; ++k)
+        v[k] = act_of<act.value, exact.value>(v[k]) * u2[k];
     });
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else {
@@ -1541,18 +1577,19 @@ __global__ __launch_bounds__(256) void k_join(Args) {
 }
 
 // One piece's gradients before the activation: d (dy) becomes dz or dg, and o
-// du; z and u: their places in the kept values.
+// du; z and u: their places in the kept values; out32: 32-bit sums of them.
 template <Type T, bool GATED, int E, typename V>
-__device__ inline void slopes(int act, const V* z, const V* u, long left,
-                              bool wide, float (&d)[E], float (&o)[E]) {
+__device__ inline void slopes(int act, bool out32, const V* z, const V* u,
+                              long left, bool wide, float (&d)[E],
+                              float (&o)[E]) {
   float s[E], g[E];
   fetch_vals<V, E>(z, g, left, wide);
   if (GATED) fetch_vals<V, E>(u, s, left, wide);
-  with_act(act, [&](auto a) {
+  with_act<T>(act, out32, [&](auto a, auto exact) {
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       float v;
-      const float c = slope_of<a.value>(g[k], &v);
+      const float c = slope_of<a.value, exact.value>(g[k], &v);
       if (GATED) {
         o[k] = d[k] * v;
         d[k] = d[k] * s[k] * c;
@@ -1585,7 +1622,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
     const long left = (long)a.cols - (long)j;
     float d[E], o[E];
     fetch_vals<V, E>(dy + i * a.ldy + j, d, left, a.wide);
-    slopes<T, GATED, E, V>(a.act, z + i * a.ldz + j,
+    slopes<T, GATED, E, V>(a.act, false, z + i * a.ldz + j,
                            GATED ? u + i * a.ldz + j : nullptr, left, a.wide,
                            d, o);
     store_vals<V, E>(dz + i * a.ldz + j, d, left, a.wide);
@@ -1626,7 +1663,7 @@ __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
            i += kSumThreads / kLanes) {
         float d[E], o[E];
         fetch_vals<V, E>(dy + i * a.s.ldy, d, left, wide);
-        slopes<T, GATED, E, V>(a.s.act, z + i * a.s.ldz,
+        slopes<T, GATED, E, V>(a.s.act, a.out32, z + i * a.s.ldz,
                                GATED ? u + i * a.s.ldz : nullptr, left, wide,
                                d, o);
         store_vals<V, E>(dz + i * a.s.ldz, d, left, wide);
