@@ -454,7 +454,9 @@ const char* dpar_last_error(void);
  * Inputs may coincide (p ranks may share one x); no output may overlap an
  * input or another output (DPAR_ERR_ALIAS), except that dz may be z or dy of
  * its rank, dg may be g or dh and du may be u (same address and row distance).
- * Matrices of one row distance may lie side by side in one buffer.
+ * Nor may the workspace's bytes that the call asks for (dpar_product_workspace)
+ * overlap any of them.  Matrices of one row distance may lie side by side in
+ * one buffer.
  *
  * Pointers are aligned to their element.  Rows that start on 16-byte
  * boundaries, and for operands an `in` and `out` that fill whole 16-byte

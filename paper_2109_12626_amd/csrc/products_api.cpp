@@ -462,9 +462,22 @@ size_t workspace_of(dpar_product_call_t call, Type t, int p,
   return most;
 }
 
+// Whether a row of rank i's matrix has a byte in [lo, hi).
+bool touches(const Mat& m, int i, uintptr_t lo, uintptr_t hi) {
+  const uintptr_t a = (uintptr_t)m.at[i];
+  if (!a || !m.extent() || a >= hi || a + m.extent() <= lo) return false;
+  const size_t pitch = m.rows > 1 ? m.ld * m.esz : m.extent();
+  // the last row that starts at or before lo (the first, if none does); what
+  // it leaves, the next one's start decides
+  const size_t r = lo > a ? (lo - a) / pitch : 0;
+  const uintptr_t row = a + r * pitch;
+  if (row < hi && row + m.cols * m.esz > lo) return true;
+  return r + 1 < m.rows && row + pitch < hi;
+}
+
 int check_workspace(const char* call, dpar_product_call_t which, Type t, int p,
-                    const dpar_product_t& o, void* ws, size_t bytes,
-                    int* cus) {
+                    const dpar_product_t& o, const Mat* mats, int n, void* ws,
+                    size_t bytes, int* cus) {
   *cus = cu_count();
   if (!ws) return DPAR_SUCCESS;
   const size_t need = workspace_of(which, t, p, o, *cus);
@@ -473,6 +486,14 @@ int check_workspace(const char* call, dpar_product_call_t which, Type t, int p,
                 call, bytes, need);
   if ((uintptr_t)ws & 15)
     return fail(DPAR_ERR_INVALID_ARG, "%s: workspace not on 16 bytes", call);
+  const uintptr_t lo = (uintptr_t)ws, hi = lo + need;
+  if (need && (hi >> 48 || hi < lo))
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: workspace above 2^48", call);
+  for (int k = 0; k < n && need; ++k)
+    for (int i = 0; i < p && mats[k].used; ++i)
+      if (touches(mats[k], i, lo, hi))
+        return fail(DPAR_ERR_ALIAS, "%s: workspace overlaps %s of rank %d",
+                    call, mats[k].name, i);
   return DPAR_SUCCESS;
 }
 
@@ -611,7 +632,8 @@ int linear_impl(const void* const* x, const void* const* w,
       {"z", in_array(z), o.rows, o.out, o.ldz, e, true, false, z != nullptr}};
   if ((rc = check_mats(m, 6, p, call))) return rc;
   int cus;
-  if ((rc = check_workspace(call, DPAR_LINEAR, t, p, o, ws, bytes, &cus)))
+  if ((rc = check_workspace(call, DPAR_LINEAR, t, p, o, m, 6, ws, bytes,
+                            &cus)))
     return rc;
   if (!o.rows || !o.out) return DPAR_SUCCESS;
   Args a = {};
@@ -657,7 +679,8 @@ int gated_impl(const void* const* x, const void* const* wg,
       {"u", in_array(u), o.rows, o.out, o.ldz, e, true, false, u != nullptr}};
   if ((rc = check_mats(m, 8, p, call))) return rc;
   int cus;
-  if ((rc = check_workspace(call, DPAR_GATED, t, p, o, ws, bytes, &cus)))
+  if ((rc = check_workspace(call, DPAR_GATED, t, p, o, m, 8, ws, bytes,
+                            &cus)))
     return rc;
   if (!o.rows || !o.out) return DPAR_SUCCESS;
   Args a = {};
@@ -753,7 +776,7 @@ int backward_impl(const char* call, int pairs, const Back& b, int p,
   int cus;
   if ((rc = check_workspace(call,
                             gated ? DPAR_GATED_BACKWARD : DPAR_LINEAR_BACKWARD,
-                            t, p, o, ws, bytes, &cus)))
+                            t, p, o, m, kMats, ws, bytes, &cus)))
     return rc;
 
   const bool apart = db && sums_apart(t, slope);

@@ -1,0 +1,101 @@
+"""Argument checks of the layer products: the workspace beside the operands and
+results.  No device work: the addresses are never read."""
+
+import os
+
+import pytest
+
+from paper_2109_12626_amd import dpar
+
+A = 1 << 40
+STEP = 1 << 36
+needs_no_gpu = pytest.mark.skipif(
+    os.path.exists("/dev/kfd"),
+    reason="would launch on fake addresses with a GPU present")
+INVALID, ALIAS, HIP = (dpar.DPAR_ERR_INVALID_ARG, dpar.DPAR_ERR_ALIAS,
+                       dpar.DPAR_ERR_HIP)
+
+# every array of each call, in order
+ARRAYS = {"linear": "x w bias residual y z",
+          "linear_backward": "dy x w z dx dw dbias dz",
+          "gated": "x wg wu bg bu h g u",
+          "gated_backward": "dh x wg wu g u dx dwg dwu dbg dbu dg du"}
+
+
+def _code(call, p, opt, at, ws, n):
+    try:
+        getattr(dpar, "dpar_" + call)(
+            *[[at[k] + i * (STEP // 4) for i in range(p)]
+              for k in ARRAYS[call].split()], p, opt, ws, n)
+        return 0
+    except dpar.DparError as e:
+        assert str(e).split(": ", 1)[1]
+        return e.code
+
+
+# rows, in, out of calls that take a workspace
+SIZES = {"linear": (128, 16001, 515), "linear_backward": (2000, 2001, 2003),
+         "gated": (2000, 2001, 2003), "gated_backward": (2000, 2001, 2003)}
+
+
+def _setup(call, **far):
+    opt = dpar.product_options(*SIZES[call], "bfloat16", act="silu", **far)
+    n = dpar.dpar_product_workspace(call, 2, opt)
+    assert n > 0
+    at = {k: A + i * STEP for i, k in enumerate(ARRAYS[call].split())}
+    return opt, n, at
+
+
+@pytest.mark.parametrize("call,name", [(c, k) for c, v in ARRAYS.items()
+                                       for k in v.split()])
+def test_workspace_over_an_array_is_refused(call, name):
+    opt, n, at = _setup(call)
+    n_rows, n_in, n_out = SIZES[call]
+    if name in ("x", "dx"):
+        rows, cols = n_rows, n_in
+    elif name.lstrip("d").startswith("w"):
+        rows, cols = n_out, n_in
+    elif name.lstrip("d").startswith("b"):
+        rows, cols = 1, n_out
+    else:
+        rows, cols = n_rows, n_out
+    first = at[name] + STEP // 4           # rank 1's
+    end = first + rows * cols * 2
+    for ws in (first // 16 * 16, (end - 1) // 16 * 16,
+               (first - n + 16) // 16 * 16):
+        assert _code(call, 2, opt, at, ws, n) == ALIAS, (call, name)
+
+
+@needs_no_gpu
+@pytest.mark.parametrize("call", ARRAYS)
+def test_workspace_beside_arrays(call):
+    opt, n, at = _setup(call)
+    for k in at:
+        # ends where the first rank's matrix begins
+        assert _code(call, 2, opt, at, at[k] - (n + 15) // 16 * 16, n) == HIP
+    # the bytes given beyond those asked for are not used
+    k = ARRAYS[call].split()[0]
+    assert _code(call, 2, opt, at, at[k] - (n + 15) // 16 * 16, 2 * n) == HIP
+
+
+@needs_no_gpu
+def test_workspace_between_rows():
+    """Rows far apart leave room for it; a byte over either row does not."""
+    far = 1 << 25                    # values: 64 MB between rows' starts
+    opt, n, at = _setup("linear", ldx=far)
+    assert n < 2 * far - 16001 * 2 - 64
+    row = at["x"] + 5 * far * 2
+    begin = row + 16001 * 2
+    assert _code("linear", 2, opt, at, -(-begin // 16) * 16, n) == HIP
+    assert _code("linear", 2, opt, at, begin // 16 * 16 - 16, n) == ALIAS
+    end = row + far * 2
+    ws = (end - n) // 16 * 16
+    assert _code("linear", 2, opt, at, ws, n) == HIP
+    assert _code("linear", 2, opt, at, ws + 16, n) == ALIAS
+
+
+def test_no_workspace_asked_for_is_none_used():
+    opt = dpar.product_options(0, 16, 24, "bfloat16", act="silu")
+    assert dpar.dpar_product_workspace("linear", 2, opt) == 0
+    at = {k: A + i * STEP for i, k in enumerate(ARRAYS["linear"].split())}
+    assert _code("linear", 2, opt, at, at["w"], 0) == 0
