@@ -2,7 +2,7 @@
 
 The work happens in libdpar.so (include/dpar.h): host tree builder and round
 schedule in C++, the round program in HIP kernels for gfx950; and the layer
-products that make the rows it sums (kernels in libdpar_products.so).  ``dpar``
+products that make the rows it sums (kernels in a library beside it).  ``dpar``
 is a thin ctypes binding with the same function names.
 """
 

@@ -1,7 +1,10 @@
-"""Builds libdpar.so and libdpar_products.so (the layer products' kernels) in
-place: HIP kernels for gfx950 with hipcc, host C++ with g++, linked by hipcc.  ``python -m paper_2109_12626_amd.build``."""
+"""Builds libdpar.so and libdpar_products-*.so (the layer products' kernels) in
+place: HIP kernels for gfx950 with hipcc, host C++ with g++, linked by hipcc.
+``python -m paper_2109_12626_amd.build``."""
 
 import concurrent.futures
+import glob
+import hashlib
 import os
 import subprocess
 import sys
@@ -23,7 +26,6 @@ HIP_FLAGS = [
 ]
 PRODUCT_SOURCES = ["products_bf16.hip", "products_f16.hip",
                    "products_f32.hip"]
-PRODUCTS = "libdpar_products.so"
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
               "-Wno-unused-parameter", "-D__HIP_PLATFORM_AMD__"]
 
@@ -41,12 +43,35 @@ def _run_all(cmds):
             done.result()
 
 
-def _link(hipcc, lib, objs, flags, libs, soname=None):
+def _link(hipcc, lib, objs, flags, libs, soname):
     tmp = lib + ".tmp"
     _run([hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}"] + flags
-         + ["-o", tmp] + objs + libs
-         + [f"-Wl,-soname,{soname or os.path.basename(lib)}"])
+         + ["-o", tmp] + objs + libs + [f"-Wl,-soname,{soname}"])
     os.replace(tmp, lib)
+
+
+def products_name(lib, objs):
+    """File of the products' kernels that belongs to a build: after the
+    library's own name and the kernels' contents, so that neither builds in one
+    directory nor builds loaded into one process take each other's."""
+    h = hashlib.sha256()
+    for obj in objs:
+        with open(obj, "rb") as f:
+            h.update(f.read())
+    return f"{_products_stem(lib)}{h.hexdigest()[:12]}.so"
+
+
+def _products_stem(lib):
+    return os.path.splitext(os.path.basename(lib))[0] + "_products-"
+
+
+def drop_old_products(lib, keep):
+    """Removes what earlier builds of this library left beside it."""
+    where = os.path.dirname(os.path.abspath(lib))
+    stem = os.path.join(glob.escape(where), glob.escape(_products_stem(lib)))
+    for old in glob.glob(stem + "[0-9a-f]" * 12 + ".so"):
+        if os.path.basename(old) != keep:
+            os.remove(old)
 
 
 def build(verbose=True, out=None, defines=(), host_sanitize=False):
@@ -79,12 +104,13 @@ def build(verbose=True, out=None, defines=(), host_sanitize=False):
     lib = LIB if out is None else out
     link_san = (["-Xarch_host", "-fsanitize=address",
                  "-Xarch_host", "-fsanitize=undefined"] if host_sanitize else [])
-    # the layer products' kernels are a library of their own beside libdpar.so
+    # the layer products' kernels are a library of their own beside it
     where = os.path.dirname(os.path.abspath(lib))
-    _link(hipcc, os.path.join(where, PRODUCTS), products, link_san, [])
+    name = products_name(lib, products)
+    _link(hipcc, os.path.join(where, name), products, link_san, [], name)
     _link(hipcc, lib, objs, link_san,
-          [os.path.join(where, PRODUCTS), "-Wl,-rpath,$ORIGIN"],
-          soname="libdpar.so")
+          [os.path.join(where, name), "-Wl,-rpath,$ORIGIN"], "libdpar.so")
+    drop_old_products(lib, name)
     return lib
 
 
