@@ -1779,33 +1779,41 @@ hipError_t go_few(const Args& a, hipStream_t stream) {
                                                      stream);
 }
 
+// Wavefronts: 8 only with the fewest sets of weight rows that a row count
+// takes (more sets are for a workgroup per CU at least, and those get 4).
 template <Type T, Form F, bool FAST, int MT, int NW>
 hipError_t pick_waves(const Args& a, hipStream_t stream) {
+  constexpr int kFewest = MT == 1 && F == Form::LINEAR ? 1 : 2;
   switch (a.waves) {
     case 1: return go_few<T, F, FAST, MT, NW, 1>(a, stream);
     case 2: return go_few<T, F, FAST, MT, NW, 2>(a, stream);
     case 4: return go_few<T, F, FAST, MT, NW, 4>(a, stream);
-    default: return go_few<T, F, FAST, MT, NW, 8>(a, stream);
+    case 8:
+      if constexpr (NW == kFewest)
+        return go_few<T, F, FAST, MT, NW, 8>(a, stream);
   }
+  return hipErrorInvalidConfiguration;
 }
 
+// The kernels that the host's rule asks for: up to 16 rows one or two sets
+// (GATED: of either weights), up to 32 two or four, beyond (16 bits) four.
 template <Type T, Form F, bool FAST>
 hipError_t pick_few(const Args& a, hipStream_t stream) {
   constexpr int kOne = F == Form::GATED ? 2 : 1;
   if (a.ni <= 16) {
     if (a.sets == kOne) return pick_waves<T, F, FAST, 1, kOne>(a, stream);
-    return pick_waves<T, F, FAST, 1, 2 * kOne>(a, stream);
-  }
-  if (a.ni <= 32) {
+    if (a.sets == 2 * kOne)
+      return pick_waves<T, F, FAST, 1, 2 * kOne>(a, stream);
+  } else if (a.ni <= 32) {
     if (a.sets == 2) return pick_waves<T, F, FAST, 2, 2>(a, stream);
-    return pick_waves<T, F, FAST, 2, 4>(a, stream);
+    if (a.sets == 4) return pick_waves<T, F, FAST, 2, 4>(a, stream);
+  } else if constexpr (T != Type::F32) {
+    if (a.sets == 4 && a.ni <= 48)
+      return pick_waves<T, F, FAST, 3, 4>(a, stream);
+    if (a.sets == 4 && a.ni <= 64)
+      return pick_waves<T, F, FAST, 4, 4>(a, stream);
   }
-  if (a.ni <= 48) {
-    if (a.sets == 2) return pick_waves<T, F, FAST, 3, 2>(a, stream);
-    return pick_waves<T, F, FAST, 3, 4>(a, stream);
-  }
-  if (a.sets == 2) return pick_waves<T, F, FAST, 4, 2>(a, stream);
-  return pick_waves<T, F, FAST, 4, 4>(a, stream);
+  return hipErrorInvalidConfiguration;
 }
 
 template <Type T, Form F, bool SUMS, bool FAST>
