@@ -307,6 +307,21 @@ __device__ inline void landed() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(LEFT) : "memory");
 }
 
+// The workgroup's wavefronts meet.  The barrier alone orders nothing that the
+// compiler moves; no access to memory or LDS crosses this.
+__device__ inline void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// The same for lanes of one wavefront that exchange values through LDS, which
+// serves a wavefront's accesses in their order.
+__device__ inline void in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // A value that is the same in every lane, in scalar registers.
 __device__ inline uint32_t uniform(uint32_t v) {
   return __builtin_amdgcn_readfirstlane(v);
@@ -736,7 +751,7 @@ struct Results {
     float bias[2][8];
     if (a.splits == 1 && j < a.nj) fetch_bias<T, F, 8>(a, rank, j, bias);
     landed<0>();
-    __builtin_amdgcn_s_barrier();
+    meet();
 #pragma unroll
     for (int mh = 0; mh < MI; mh += MH) {
       const int r = lane & 15, q = lane >> 4;
@@ -750,6 +765,7 @@ struct Results {
           *(LDS f32x4*)(mine + (m * 16 + r) * (WN * 4) +
                         (c ^ (r & kTurn)) * 16) = acc[mh + m][n];
         }
+      in_order();
 #pragma unroll 1
       for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
         const size_t i = iw + mh * 16 + row;
@@ -777,6 +793,7 @@ struct Results {
           if constexpr (kGated) store_vals<float, 8>(p + sz, u2, left, wide);
         }
       }
+      in_order();
     }
   }
 };
@@ -977,7 +994,7 @@ struct Tiled {
         else
           landed<0>();
         if (kt + 1 < k1) clear(kt + 1, then);
-        __builtin_amdgcn_s_barrier();
+        meet();
         __builtin_amdgcn_sched_barrier(0);
         if (!FAST && ahead) land(buf);
         // (after the last tile this reads a buffer that nothing uses any
@@ -1011,7 +1028,7 @@ struct Tiled {
       else
         landed<0>();
       clear(k0, 0);
-      __builtin_amdgcn_s_barrier();
+      meet();
       read_b(0, 0);
 #pragma unroll
       for (int m = 0; m < MI; ++m) read_a(m, 0, 0);
@@ -1174,7 +1191,7 @@ struct PingPong {
     };
     auto change = [] {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
+      meet();
       __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -1229,7 +1246,7 @@ struct PingPong {
       }
       ready(k0, k0 + 1 < k1);
       change();
-      if (late) __builtin_amdgcn_s_barrier();   // one phase behind
+      if (late) meet();   // one phase behind
       if constexpr (SUMS) {
         if (sums)
           loop(Yes{});
@@ -1238,7 +1255,7 @@ struct PingPong {
       } else {
         loop(No{});
       }
-      if (!late) __builtin_amdgcn_s_barrier();
+      if (!late) meet();
     }
     Results<T, F, SUMS, WM, WN, kAcross, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
