@@ -391,7 +391,8 @@ def allreduce(x, y=None, dtype=None, op="sum", b=0, exec="auto", stream=None,
 # biases [p, out] or [out]; a residual like the result.  Rows may be any
 # distance apart; the values of a row are consecutive.  The results are new
 # tensors [p, ...] (without the first dimension if w has none).  Only marshals
-# addresses: every product runs in the library's kernels.
+# addresses: every product runs in the library's kernels.  Nothing is recorded
+# for autograd: tensors that require a gradient are refused where it is on.
 
 _NAMES = {torch.float32: "float32", torch.bfloat16: "bfloat16",
           torch.float16: "float16"}
@@ -420,6 +421,10 @@ class _Call:
             return None
         if t.device != self.device or t.dtype != (dtype or self.dtype):
             raise ValueError(f"{name}: {t.dtype} on {t.device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, and these calls "
+                             "record none: call under torch.no_grad() (or "
+                             "detach it) and use the backward call")
         one = t.dim() == len(shape)
         if tuple(t.shape[-len(shape):]) != shape or \
                 not (one or (t.dim() == len(shape) + 1

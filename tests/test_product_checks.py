@@ -99,3 +99,25 @@ def test_no_workspace_asked_for_is_none_used():
     assert dpar.dpar_product_workspace("linear", 2, opt) == 0
     at = {k: A + i * STEP for i, k in enumerate(ARRAYS["linear"].split())}
     assert _code("linear", 2, opt, at, at["w"], 0) == 0
+
+
+@pytest.mark.parametrize("call,name", [
+    ("linear", "x"), ("linear", "w"), ("linear", "bias"),
+    ("linear", "residual"), ("linear_backward", "dy"),
+    ("linear_backward", "z"), ("gated", "wu"), ("gated", "bg"),
+    ("gated_backward", "dh"), ("gated_backward", "g")])
+def test_front_ends_refuse_gradients_they_would_drop(call, name):
+    import torch
+    x, w, y, b = (torch.zeros(*s) for s in ((3, 16), (8, 16), (3, 8), (8,)))
+    args = {"linear": dict(x=x, w=w, bias=b, residual=y),
+            "linear_backward": dict(dy=y, x=x, w=w, z=y, act="silu"),
+            "gated": dict(x=x, wg=w, wu=w, bg=b, bu=b),
+            "gated_backward": dict(dh=y, x=x, wg=w, wu=w, g=y, u=y)}[call]
+    args[name] = args[name].clone().requires_grad_()
+    with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+        getattr(dpar, call)(**args)
+    if not torch.cuda.is_available():
+        # past the check where none is recorded: then the device is missing
+        with torch.no_grad(), pytest.raises(Exception) as e:
+            getattr(dpar, call)(**args)
+        assert "gradient" not in str(e.value)
