@@ -483,7 +483,8 @@ typedef enum {
     DPAR_ACT_SILU = 4       /* z / (1 + exp(-z)) */
 } dpar_act_t;
 
-/* Sizes, types and row distances (in elements; 0: packed) of a layer product.
+/* Sizes, types and row distances (in elements; 0: packed; not read where a
+ * matrix has one row) of a layer product.
  *   ldx   x                          (packed: in)
  *   ldw   w, wg, wu                  (packed: in)
  *   ldy   y, h, dy, dh               (packed: out)

@@ -199,6 +199,11 @@ int check_options(const char* call, int p, const dpar_product_t* opt,
     if (v > kMostPitch)
       return fail(DPAR_ERR_UNSUPPORTED, "%s: a row distance beyond 2^38",
                   call);
+  // a single row has no distance (the kernels' offsets of rows that are not
+  // there, held inside the matrix, would be off 16 bytes with an odd one)
+  if (o->rows <= 1)
+    o->ldx = o->lddx = o->in, o->ldy = o->ldr = o->ldz = o->out;
+  if (o->out <= 1) o->ldw = o->lddw = o->in;
   return DPAR_SUCCESS;
 }
 

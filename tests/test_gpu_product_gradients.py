@@ -201,3 +201,29 @@ def test_bias_gradients_sum_unrounded_values(p, rows, n_out, act, dtype):
             r(dbu), r(dz), r(du), p, opt, *ws, stream)
         check(db, v * np64(ku) * slope, err * np.abs(np64(ku)))
         check(dbu, v * a, err)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_single_rows_of_any_distance(dtype):
+    """One row of x and dy, one of w, with odd distances that no second row
+    uses: the results of packed ones."""
+    need_gpu()
+    d = lib()
+    g = torch.Generator("cuda").manual_seed(33)
+    r, stream = d.rows, torch.cuda.current_stream()
+    for rows, n_in, n_out in ((1, 264, 136), (40, 264, 1)):
+        x, w, dy = (normal(g, 1, *s, dtype=dtype) for s in
+                    ((rows, n_in), (n_out, n_in), (rows, n_out)))
+        got = []
+        for far in ({}, {"ldx": 1, "ldy": 3, "lddx": 5} if rows == 1 else
+                    {"ldw": 1, "lddw": 3}):
+            opt = d.product_options(rows, n_in, n_out, dtype, **far)
+            out = [torch.empty_like(t) for t in (x, w, dy)]
+            d.dpar_linear_backward(r(dy), r(x), r(w), None, r(out[0]),
+                                   r(out[1]), None, None, 1, opt,
+                                   stream=stream)
+            d.dpar_linear(r(x), r(w), None, None, r(out[2]), None, 1, opt,
+                          stream=stream)
+            got.append(out)
+        for a, b in zip(*got):
+            assert torch.equal(a, b)

@@ -121,3 +121,19 @@ def test_front_ends_refuse_gradients_they_would_drop(call, name):
         with torch.no_grad(), pytest.raises(Exception) as e:
             getattr(dpar, call)(**args)
         assert "gradient" not in str(e.value)
+
+
+@needs_no_gpu
+def test_a_single_row_has_no_distance():
+    """In place with any distance, and with distances below its length."""
+    at = {k: A + i * STEP for i, k in
+          enumerate(ARRAYS["linear_backward"].split())}
+    at["dz"] = at["dy"]
+    for rows, want in ((1, HIP), (2, ALIAS)):
+        opt = dpar.product_options(rows, 16, 24, "bfloat16", act="silu",
+                                   ldy=48)
+        assert _code("linear_backward", 2, opt, at, None, 0) == want
+    at = {k: A + i * STEP for i, k in enumerate(ARRAYS["linear"].split())}
+    for rows, out, far in ((1, 24, {"ldx": 1}), (2, 1, {"ldw": 3})):
+        opt = dpar.product_options(rows, 16, out, "bfloat16", **far)
+        assert _code("linear", 2, opt, at, None, 0) == HIP
