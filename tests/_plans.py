@@ -56,3 +56,23 @@ def ask(exe, lines):
             plans, launches = [], []
     assert len(got) == len(lines)
     return got
+
+
+def ways(plans, launches):
+    """What each product of a call takes: form, 16 or 32 bits, operands and
+    kernel."""
+    # (a call of many ranks launches each product several times)
+    each = launches[::max(1, len(launches) // max(1, len(plans)))]
+    out = []
+    for plan, launch in zip(plans, each):
+        form, dtype, operands, kernel, rest = re.match(
+            r"dpar: product=(\w+) (\w+) .* operands=(\w+) kernel=(\S+) (.*)",
+            plan).groups()
+        bits = 32 if dtype == "float32" else 16
+        if kernel == "few":
+            rest += f" tiles={-(-launch[7] // 16)}"
+        else:
+            rest = "whole" if rest == "splits=1" else "split"
+            rest += " sums" * launch[8]
+        out.append((form, bits, operands, kernel, rest))
+    return out

@@ -1,6 +1,7 @@
 """Gradients of the layer products where the tests of whole results do not look:
 columns beside one that is not finite, at every kernel that sums weights'
-gradients; bias gradients against sums of unrounded values."""
+gradients; bias gradients against sums of unrounded values; the gradients
+before the activation themselves."""
 
 import numpy as np
 import pytest
@@ -8,6 +9,7 @@ import torch
 
 from oracle import products as ref
 from tests._gpu import _Env, lib, need_gpu
+from tests.test_gpu_products import Ranks, close
 
 pytestmark = pytest.mark.gpu
 
@@ -227,3 +229,47 @@ def test_single_rows_of_any_distance(dtype):
             got.append(out)
         for a, b in zip(*got):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,n_out", [(1, 1), (3, 40), (70, 137), (65, 64),
+                                        (130, 7)])
+@pytest.mark.parametrize("far,shift", [(0, 0), (8, 0), (3, 5), (64, 4)])
+@pytest.mark.parametrize("place", [None, "z", "dy"])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_gradients_before_the_activation(rows, n_out, far, shift, place, dtype,
+                                         bias):
+    """dz, dg and du, which the calls hand out: within their own rounding, in
+    place of what they may replace, and nothing between their rows."""
+    need_gpu()
+    d = lib()
+    p, n_in = 2, 8
+    g = torch.Generator("cuda").manual_seed(34)
+    for op, act in (("linear", "gelu"), ("gated", "silu")):
+        x, w = (Ranks(p, a, n_in, dtype, gen=g) for a in (rows, n_out))
+        dy, kg, ku = (Ranks(p, rows, n_out, dtype, far, shift, g)
+                      for _ in range(3))
+        dw, dw2 = (Ranks(p, n_out, n_in, dtype) for _ in range(2))
+        sums = [Ranks(p, 1, n_out, dtype) for _ in range(2)]
+        db, db2 = (t.at if bias else None for t in sums)
+        first = {None: Ranks(p, rows, n_out, dtype, far, shift), "z": kg,
+                 "dy": dy}[place]
+        second = ku if place else Ranks(p, rows, n_out, dtype, far, shift)
+        opt = d.product_options(rows, n_in, n_out, dtype, act=act, ldy=dy.ld,
+                                ldz=kg.ld)
+        v, z, u = (np64(t.t) for t in (dy, kg, ku))
+        a, slope = ref.act(z, act)
+        if op == "linear":
+            d.dpar_linear_backward(dy.at, x.at, w.at, kg.at, None, dw.at, db,
+                                   first.at, p, opt)
+            want = ref._slope(v, z, act, dtype)
+        else:
+            d.dpar_gated_backward(dy.at, x.at, w.at, w.at, kg.at, ku.at, None,
+                                  dw.at, dw2.at, db, db2, first.at, second.at,
+                                  p, opt)
+            err = 2.0 ** -20 * (1 + np.abs(z)) * np.abs(v)
+            want = ref._stored(v * u * slope, err * np.abs(u), dtype)
+            close(second.t, ref._stored(v * a, err, dtype), "du")
+            assert second.gaps_untouched()
+        close(first.t, want, op)
+        assert first.gaps_untouched()
