@@ -129,7 +129,8 @@ constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
 // (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2).  Not EXACT: Abramowitz and
 // Stegun 7.1.26, whose truncation is 7.5e-8 at most; in 32 bits the whole is
-// up to 2.8e-7 off, a hundredth of what rounding a result of 1 to fp16 costs.
+// 2.8e-7 off at most, measured over -12 .. 12 (EXACT: 9.3e-8): a thousandth of
+// what rounding a result of 1 to fp16 costs.
 template <bool EXACT>
 __device__ inline float normal_cdf(float z, float* density) {
   if (EXACT) {
