@@ -1070,8 +1070,9 @@ struct Tiled {
 // change places.
 //
 // 256 x 256 (two operands of 64 KB per 2 x 256 x 256 x 64 products) reaches
-// 1250 TFLOP/s at 8192 x 4096 x 16384 with both results stored, 1470 without
-// the stores: power bound, the matrix cores 63% busy at 1.9 GHz.  256 x 128
+// 1200 to 1290 TFLOP/s, by card, at 8192 x 4096 x 16384 with both results
+// stored, 1470 without the stores: power bound, the matrix cores 63% busy at 1.7
+// to 1.9 GHz.  256 x 128
 // fills the card with half the results (1 x 2048 x 4096 x 4096: 69 us, 80 with
 // 256 x 256, 76 with 128 x 128).
 //
@@ -1621,7 +1622,11 @@ __device__ inline void slopes(int act, bool out32, const V* z, const V* u,
 // The gradients before the activation: 16 bytes of a row per thread and turn,
 // bound by memory (5 x 8 x 2048 x 2048 bf16: 70 us, 4.8 TB/s, the rate of a
 // copy).  Kept apart from the products that read them, each value several
-// times: there the slope would be computed as often.
+// times: there the slope would be computed as often.  Rounded to the operands'
+// type, which the matrix cores take: 16-bit gradients are 2.4e-3 (bf16) off for
+// it, 1.7e-3 with the results' rounding alone.  As two 16-bit halves nothing
+// would be lost, at twice the operations (4096 x 4096 x 4096: dx 118 -> 188 us,
+// dw 107 -> 207).
 template <Type T, bool GATED>
 __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
   GivenSlope& a = *(GivenSlope*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1654,7 +1659,8 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
 // does for 32-bit values and for dy itself: 16-bit bias gradients would be
 // sqrt 2 times as far off, 32-bit ones 2^-9.)  A workgroup takes 128 bytes of
 // the columns of a part of the rows, 64 rows at a time; a column's values meet
-// in an order that its place alone fixes, and columns never meet.
+// in an order that its place alone fixes, and columns never meet.  4096 x 4096
+// bf16, 8 parts: 25 us and 5 to join them (k_slope 20); bound by memory.
 template <Type T, bool GATED>
 __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
   GivenSums& a = *(GivenSums*)__builtin_amdgcn_kernarg_segment_ptr();
