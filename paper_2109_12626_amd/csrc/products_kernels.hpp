@@ -199,33 +199,33 @@ __device__ inline float slope_of(float z, float* value) {
   return s + y * both;
 }
 
-// f(activation, EXACT) with both as types: one branch for many values.
-template <bool EXACT, typename Fn>
+// f(activation) with the activation as a type: one branch for many values.
+template <typename Fn>
 __device__ inline void with_act(int act, Fn f) {
-  constexpr std::integral_constant<bool, EXACT> exact;
   switch (act) {
-    case (int)Act::RELU:
-      f(std::integral_constant<Act, Act::RELU>(), exact);
-      break;
-    case (int)Act::GELU:
-      f(std::integral_constant<Act, Act::GELU>(), exact);
-      break;
+    case (int)Act::RELU: f(std::integral_constant<Act, Act::RELU>()); break;
+    case (int)Act::GELU: f(std::integral_constant<Act, Act::GELU>()); break;
     case (int)Act::GELU_TANH:
-      f(std::integral_constant<Act, Act::GELU_TANH>(), exact);
+      f(std::integral_constant<Act, Act::GELU_TANH>());
       break;
-    case (int)Act::SILU:
-      f(std::integral_constant<Act, Act::SILU>(), exact);
-      break;
-    default: f(std::integral_constant<Act, Act::NONE>(), exact);
+    case (int)Act::SILU: f(std::integral_constant<Act, Act::SILU>()); break;
+    default: f(std::integral_constant<Act, Act::NONE>());
   }
 }
-// EXACT for 32-bit values and for 32-bit results (out32) of 16-bit ones.
-template <Type T, typename Fn>
-__device__ inline void with_act(int act, bool out32, Fn f) {
-  if (T == Type::F32 || out32)
-    with_act<true>(act, f);
-  else
-    with_act<false>(act, f);
+// f(EXACT), which holds for 32-bit values and for 32-bit results (out32) of
+// 16-bit ones.  Around loops over results: inside, the longer code of the exact
+// forms made 16-bit results slower (7 x 875 x 1001 x 1000 fp16 gelu 37.0
+// against 35.8 us).
+template <Type T, bool ACTS = true, typename Fn>
+__device__ inline void with_exact(bool out32, Fn f) {
+  if constexpr (T == Type::F32) {
+    f(std::integral_constant<bool, true>());
+  } else {
+    if (ACTS && out32)
+      f(std::integral_constant<bool, true>());
+    else
+      f(std::integral_constant<bool, false>());
+  }
 }
 
 // ---------------------------------------------------------------- tiles
@@ -562,9 +562,12 @@ __device__ inline void fetch_bias(Given& a, int rank, size_t j,
   }
 }
 
+// Forms whose results have an activation.
+constexpr bool acts(Form f) { return f == Form::LINEAR || f == Form::GATED; }
+
 // N consecutive values j .. of row i: bias, activation, residual, rounding,
 // stores.  v: the product's sums (GATED: v of g, u2 of u).
-template <Type T, Form F, int N>
+template <Type T, Form F, bool EXACT, int N>
 __device__ inline void finish(Given& a, int rank, int pair, size_t i,
                               size_t j, float* v, float* u2,
                               const float (&b)[2][N]) {
@@ -584,9 +587,9 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
     for (int k = 0; k < N; ++k) v[k] += b[0][k];
     if (V* z = (V*)a.o[1][rank])
       store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
-    with_act<T>(a.act, a.out32, [&](auto act, auto exact) {
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = act_of<act.value, exact.value>(v[k]);
+      for (int k = 0; k < N; ++k) v[k] = act_of<act.value, EXACT>(v[k]);
     });
     if (r) {
 #pragma unroll
@@ -602,10 +605,10 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
       store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
     if (V* u = (V*)a.u[0][rank])
       store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
-    with_act<T>(a.act, a.out32, [&](auto act, auto exact) {
+    with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int k = 0; k < N; ++k)
-        v[k] = act_of<act.value, exact.value>(v[k]) * u2[k];
+        v[k] = act_of<act.value, EXACT>(v[k]) * u2[k];
     });
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else {
@@ -767,33 +770,35 @@ struct Results {
                         (c ^ (r & kTurn)) * 16) = acc[mh + m][n];
         }
       in_order();
+      with_exact<T, acts(F)>(a.out32, [&](auto exact) {
 #pragma unroll 1
-      for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
-        const size_t i = iw + mh * 16 + row;
-        if (i >= a.ni || j >= a.nj) continue;
-        float v[8], u2[8];
-        LDS char* at = mine + row * (WN * 4);
-        const int x = row & kTurn;
-        *(f32x4*)v = *(LDS f32x4*)(at + (c ^ x) * 16);
-        *(f32x4*)(v + 4) = *(LDS f32x4*)(at + ((c + 1) ^ x) * 16);
-        if constexpr (kGated) {
-          *(f32x4*)u2 = *(LDS f32x4*)(at + ((CH / 2 + c) ^ x) * 16);
-          *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
+        for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
+          const size_t i = iw + mh * 16 + row;
+          if (i >= a.ni || j >= a.nj) continue;
+          float v[8], u2[8];
+          LDS char* at = mine + row * (WN * 4);
+          const int x = row & kTurn;
+          *(f32x4*)v = *(LDS f32x4*)(at + (c ^ x) * 16);
+          *(f32x4*)(v + 4) = *(LDS f32x4*)(at + ((c + 1) ^ x) * 16);
+          if constexpr (kGated) {
+            *(f32x4*)u2 = *(LDS f32x4*)(at + ((CH / 2 + c) ^ x) * 16);
+            *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
+          }
+          if (a.splits == 1) {
+            finish<T, F, exact.value, 8>(a, rank, pair, i, j, v, u2, bias);
+          } else {
+            // [split][rank][pair or projection][row][column]
+            const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
+            const size_t sz = a.ni * a.nj;
+            float* p = a.part + (((size_t)split * a.ranks + rank) * np + pair)
+                       * sz + i * a.nj + j;
+            const long left = (long)a.nj - (long)j;
+            const bool wide = a.nj % 4 == 0;
+            store_vals<float, 8>(p, v, left, wide);
+            if constexpr (kGated) store_vals<float, 8>(p + sz, u2, left, wide);
+          }
         }
-        if (a.splits == 1) {
-          finish<T, F, 8>(a, rank, pair, i, j, v, u2, bias);
-        } else {
-          // [split][rank][pair or projection][row][column]
-          const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
-          const size_t sz = a.ni * a.nj;
-          float* p = a.part + (((size_t)split * a.ranks + rank) * np + pair)
-                     * sz + i * a.nj + j;
-          const long left = (long)a.nj - (long)j;
-          const bool wide = a.nj % 4 == 0;
-          store_vals<float, 8>(p, v, left, wide);
-          if constexpr (kGated) store_vals<float, 8>(p + sz, u2, left, wide);
-        }
-      }
+      });
       in_order();
     }
   }
@@ -1071,8 +1076,8 @@ struct Tiled {
 //
 // 256 x 256 (two operands of 64 KB per 2 x 256 x 256 x 64 products) reaches
 // 1200 to 1290 TFLOP/s, by card, at 8192 x 4096 x 16384 with both results
-// stored, 1470 without the stores: power bound, the matrix cores 63% busy at 1.7
-// to 1.9 GHz.  256 x 128
+// stored, 1470 without the stores: power bound, the matrix cores 63% busy at
+// 1.7 to 1.9 GHz.  256 x 128
 // fills the card with half the results (1 x 2048 x 4096 x 4096: 69 us, 80 with
 // 256 x 256, 76 with 128 x 128).
 //
@@ -1362,34 +1367,31 @@ struct Few {
     finish_all(a, (f32x4(LDS*)[MT * NW][64])lds, acc, rank, j0, wave, lane);
   }
 
-  // Adds the S wavefronts' sums in their order and finishes the results.
+  // Adds the S wavefronts' sums in their order and finishes the results, by way
+  // of LDS, so that the code that finishes a tile of results is there once.
   static __device__ void finish_all(Given& a, f32x4 (LDS* part)[MT * NW][64],
                                     f32x4 (&acc)[MT][NW], unsigned rank,
                                     size_t j0, int wave, int lane) {
     const int r = lane & 15, q = lane >> 4;
-    if (S > 1) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NW; ++n) part[wave][m * NW + n][lane] = acc[m][n];
-      __syncthreads();
-    }
-    // result tile (m, n): wavefront tile % S
-    constexpr int NO = kGated ? NW / 2 : NW, NS = kGated ? 2 : 1;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int n = 0; n < NO; ++n) {
-        if ((m * NO + n) % S != wave) continue;
-        const int w = m * NW + n * NS;
-        f32x4 v = acc[m][n * NS], u = acc[m][n * NS + NS - 1];
-        if (S > 1) {
-          v = part[0][w][lane];
-          for (int k = 1; k < S; ++k) v += part[k][w][lane];
-          if (kGated) {
-            u = part[0][w + 1][lane];
-            for (int k = 1; k < S; ++k) u += part[k][w + 1][lane];
-          }
+      for (int n = 0; n < NW; ++n) part[wave][m * NW + n][lane] = acc[m][n];
+    if (S > 1)
+      __syncthreads();
+    else
+      in_order();
+    // result tile (m, n): wavefront tile % S
+    constexpr int NO = kGated ? NW / 2 : NW, NS = kGated ? 2 : 1;
+    with_exact<T>(a.out32, [&](auto exact) {
+#pragma unroll 1
+      for (int t = wave; t < MT * NO; t += S) {
+        const int m = t / NO, n = t % NO, w = m * NW + n * NS;
+        f32x4 v = part[0][w][lane], u = part[0][w + NS - 1][lane];
+#pragma unroll
+        for (int k = 1; k < S; ++k) {
+          v += part[k][w][lane];
+          if (kGated) u += part[k][w + 1][lane];
         }
         const size_t i = m * 16 + r, j = j0 + n * 16 + q * 4;
         if (i >= a.ni || j >= a.nj) continue;
@@ -1398,8 +1400,9 @@ struct Few {
         for (int e = 0; e < 4; ++e) va[e] = v[e], ua[e] = u[e];
         float bias[2][4];
         fetch_bias<T, F, 4>(a, rank, j, bias);
-        finish<T, F, 4>(a, rank, 0, i, j, va, ua, bias);
+        finish<T, F, exact.value, 4>(a, rank, 0, i, j, va, ua, bias);
       }
+    });
   }
 };
 
@@ -1580,7 +1583,9 @@ __global__ __launch_bounds__(256) void k_join(Args) {
     }
     float bias[2][4];
     fetch_bias<T, F, 4>(a, rank, j, bias);
-    finish<T, F, 4>(a, rank, pair, i, j, v, u2, bias);
+    with_exact<T, acts(F)>(a.out32, [&](auto exact) {
+      finish<T, F, exact.value, 4>(a, rank, pair, i, j, v, u2, bias);
+    });
   }
   if (F == Form::DW) {
     const size_t n = (size_t)a.ranks * a.pairs * a.ni;
@@ -1596,19 +1601,18 @@ __global__ __launch_bounds__(256) void k_join(Args) {
 }
 
 // One piece's gradients before the activation: d (dy) becomes dz or dg, and o
-// du; z and u: their places in the kept values; out32: 32-bit sums of them.
-template <Type T, bool GATED, int E, typename V>
-__device__ inline void slopes(int act, bool out32, const V* z, const V* u,
-                              long left, bool wide, float (&d)[E],
-                              float (&o)[E]) {
+// du; z and u: their places in the kept values.
+template <bool GATED, bool EXACT, int E, typename V>
+__device__ inline void slopes(int act, const V* z, const V* u, long left,
+                              bool wide, float (&d)[E], float (&o)[E]) {
   float s[E], g[E];
   fetch_vals<V, E>(z, g, left, wide);
   if (GATED) fetch_vals<V, E>(u, s, left, wide);
-  with_act<T>(act, out32, [&](auto a, auto exact) {
+  with_act(act, [&](auto a) {
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       float v;
-      const float c = slope_of<a.value, exact.value>(g[k], &v);
+      const float c = slope_of<a.value, EXACT>(g[k], &v);
       if (GATED) {
         o[k] = d[k] * v;
         d[k] = d[k] * s[k] * c;
@@ -1645,9 +1649,9 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
     const long left = (long)a.cols - (long)j;
     float d[E], o[E];
     fetch_vals<V, E>(dy + i * a.ldy + j, d, left, a.wide);
-    slopes<T, GATED, E, V>(a.act, false, z + i * a.ldz + j,
-                           GATED ? u + i * a.ldz + j : nullptr, left, a.wide,
-                           d, o);
+    slopes<GATED, T == Type::F32, E, V>(
+        a.act, z + i * a.ldz + j, GATED ? u + i * a.ldz + j : nullptr, left,
+        a.wide, d, o);
     store_vals<V, E>(dz + i * a.ldz + j, d, left, a.wide);
     if (GATED) store_vals<V, E>(du + i * a.ldz + j, o, left, a.wide);
   }
@@ -1682,14 +1686,15 @@ __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
     V* dz = (V*)a.s.dz[rank] + j;
     V* du = GATED ? (V*)a.s.du[rank] + j : nullptr;
     float sum[NP][E] = {};
-    if (left > 0)
+    with_exact<T>(a.out32, [&](auto exact) {
+      if (left <= 0) return;
       for (size_t i = a.s.rows * part / a.parts + t / kLanes; i < i1;
            i += kSumThreads / kLanes) {
         float d[E], o[E];
         fetch_vals<V, E>(dy + i * a.s.ldy, d, left, wide);
-        slopes<T, GATED, E, V>(a.s.act, a.out32, z + i * a.s.ldz,
-                               GATED ? u + i * a.s.ldz : nullptr, left, wide,
-                               d, o);
+        slopes<GATED, exact.value, E, V>(a.s.act, z + i * a.s.ldz,
+                                         GATED ? u + i * a.s.ldz : nullptr,
+                                         left, wide, d, o);
         store_vals<V, E>(dz + i * a.s.ldz, d, left, wide);
         if (GATED) store_vals<V, E>(du + i * a.s.ldz, o, left, wide);
 #pragma unroll
@@ -1698,6 +1703,7 @@ __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
           if (GATED) sum[NP - 1][k] += o[k];
         }
       }
+    });
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -1795,7 +1801,7 @@ template <Type T, Form F, bool FAST, int MT, int NW, int S>
 hipError_t go_few(const Args& a, hipStream_t stream) {
   using K = Few<T, F, FAST, MT, NW, S>;
   const size_t n = (a.nj + K::BJ - 1) / K::BJ * a.ranks;
-  const size_t parts = S > 1 ? (size_t)S * MT * NW * 1024 : 0;
+  const size_t parts = (size_t)S * MT * NW * 1024;
   const size_t bytes =
       FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, NW, S>::kChunk)
            : parts;
