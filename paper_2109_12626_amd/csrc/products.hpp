@@ -43,6 +43,8 @@ struct Args {
   size_t lda, ldb, ldo, ldk, lde;  // row distances (elements): A, B, result,
                                    // kept values, residual
   float* part;               // partial results of a split contraction
+  const float* sum;          // DW: parts of the bias gradients (SumArgs)
+  int parts, all, first;     // as there
   int ranks, pairs;
   int act;
   int out32;                 // result in 32 bits
@@ -58,6 +60,8 @@ struct Args {
   int wide_out;              // results, kept values, residual, bias: 16-byte
                              // pieces
 };
+
+static_assert(sizeof(Args) <= 4096, "kernel arguments");
 
 // dz = dy act'(z) (gated == 0), or dg = dy u act'(g), du = dy act(g).
 struct SlopeArgs {

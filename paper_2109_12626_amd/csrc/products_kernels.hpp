@@ -711,6 +711,25 @@ struct Sums {
   }
 };
 
+// Joins the parts of bias gradients that SumArgs left, in their order: those of
+// the tile's rows, by the workgroup of its first columns (a launch of its own
+// took 5 us).
+template <Type T, int BM>
+__device__ inline void join_sums(Given& a, int rank, int pair, unsigned split,
+                                 size_t i0, size_t j0) {
+  const size_t i = i0 + threadIdx.x;
+  if (!a.sum || split != 0 || j0 != 0 || threadIdx.x >= BM || i >= a.ni)
+    return;
+  const float* w = a.sum + ((size_t)(a.first + rank) * a.pairs + pair) * a.ni +
+                   i;
+  const size_t step = (size_t)a.all * a.pairs * a.ni;
+  float v = 0.f;
+#pragma unroll 16
+  for (int k = 0; k < a.parts; ++k) v += w[k * step];
+  store_out<1>(a.u[pair][rank], i, &v, 1, a.out32, false,
+               typename Elem<T>::V());
+}
+
 // Stores a wavefront's WM x WN results (GATED: g's and u's halves) from row iw
 // and column jw on, and the sums of A that it holds.
 template <Type T, Form F, bool SUMS, int WM, int WN, int SHARES, typename OB>
@@ -1057,6 +1076,8 @@ struct Tiled {
     Results<T, F, SUMS, WM, WN, BN / WN, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
         j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
+    if constexpr (F == Form::DW && !SUMS)
+      join_sums<T, BM>(a, rank, pair, split, i0, j0);
   }
 };
 
@@ -1267,6 +1288,8 @@ struct PingPong {
     Results<T, F, SUMS, WM, WN, kAcross, OB>::store(
         a, rank, pair, split, i0 + wm * WM,
         j0 + wn * (kGated ? WN / 2 : WN), sums, wn, sum, acc, lds, wave, lane);
+    if constexpr (F == Form::DW && !SUMS)
+      join_sums<T, BM>(a, rank, pair, split, i0, j0);
   }
 };
 
@@ -1589,7 +1612,8 @@ __global__ __launch_bounds__(256) void k_join(Args) {
   }
   if (F == Form::DW) {
     const size_t n = (size_t)a.ranks * a.pairs * a.ni;
-    if (id < n && a.u[id / a.ni % a.pairs][id / a.ni / a.pairs]) {
+    if (a.sums && id < n &&
+        a.u[id / a.ni % a.pairs][id / a.ni / a.pairs]) {
       const float* w = a.part +
                        (size_t)a.splits * a.ranks * a.pairs * sz + id;
       float s = 0.f;
@@ -1664,7 +1688,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs) {
 // sqrt 2 times as far off, 32-bit ones 2^-9.)  A workgroup takes 128 bytes of
 // the columns of a part of the rows, 64 rows at a time; a column's values meet
 // in an order that its place alone fixes, and columns never meet.  4096 x 4096
-// bf16, 8 parts: 25 us and 5 to join them (k_slope 20); bound by memory.
+// bf16, 8 parts: 25 us (k_slope 20); bound by memory.
 template <Type T, bool GATED>
 __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
   GivenSums& a = *(GivenSums*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1727,23 +1751,6 @@ __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
     }
     __syncthreads();
   }
-}
-
-// Joins the sums' parts in their order.
-template <Type T>
-__global__ __launch_bounds__(256) void k_join_sums(SumArgs) {
-  GivenSums& a = *(GivenSums*)__builtin_amdgcn_kernarg_segment_ptr();
-  const int np = a.s.gated ? 2 : 1, p = blockIdx.z, rank = blockIdx.y;
-  const size_t col = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (col >= a.s.cols) return;
-  const float* w = a.part + ((a.first + (size_t)rank) * np + p) * a.s.cols +
-                   col;
-  const size_t step = (size_t)a.all * np * a.s.cols;
-  float v = 0.f;
-#pragma unroll 16
-  for (int k = 0; k < a.parts; ++k) v += w[k * step];
-  store_out<1>(a.db[p][rank], col, &v, 1, a.out32, false,
-               typename Elem<T>::V());
 }
 
 // ---------------------------------------------------------------- launches
@@ -1914,12 +1921,6 @@ hipError_t run_sums(const SumArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((k_sums<T, true>), grid, threads, 0, stream, a);
   else
     hipLaunchKernelGGL((k_sums<T, false>), grid, threads, 0, stream, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.parts == 1) return e;
-  hipLaunchKernelGGL((k_join_sums<T>),
-                     dim3((unsigned)((a.s.cols + 255) / 256), a.s.ranks,
-                          a.s.gated ? 2 : 1),
-                     dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
