@@ -452,8 +452,9 @@ const char* dpar_last_error(void);
  * array marked optional may be NULL as a whole; bias, bg, bu and residual may
  * also hold NULL for single ranks: a split layer adds them on one rank only.
  * Inputs may coincide (p ranks may share one x); no output may overlap an
- * input or another output (DPAR_ERR_ALIAS), except that dz may be z or dy of
- * its rank, dg may be g or dh and du may be u (same address and row distance).
+ * input or another output (DPAR_ERR_ALIAS), except that y may be its rank's
+ * residual, dz may be z or dy of its rank, dg may be g or dh and du may be u
+ * (same address and row distance).
  * Nor may the workspace's bytes that the call asks for (dpar_product_workspace)
  * overlap any of them.  Matrices of one row distance may lie side by side in
  * one buffer.

@@ -629,7 +629,7 @@ int linear_impl(const void* const* x, const void* const* w,
   size_t e, eo;
   int rc = check_options(call, p, opt, &o, &t, &e, &eo);
   if (rc) return rc;
-  const Mat m[] = {
+  Mat m[] = {
       {"x", x, o.rows, o.in, o.ldx, e, false, false, true},
       {"w", w, o.out, o.in, o.ldw, e, false, false, true},
       {"bias", bias, 1, o.out, o.out, e, false, true, bias != nullptr},
@@ -637,6 +637,8 @@ int linear_impl(const void* const* x, const void* const* w,
        residual != nullptr},
       {"y", in_array(y), o.rows, o.out, o.ldy, eo, true, false, true},
       {"z", in_array(z), o.rows, o.out, o.ldz, e, true, false, z != nullptr}};
+  // (each thread reads the residuals of its results before it stores these)
+  m[4].twin[0] = residual;
   if ((rc = check_mats(m, 6, p, call))) return rc;
   int cus;
   if ((rc = check_workspace(call, DPAR_LINEAR, t, p, o, m, 6, ws, bytes,

@@ -137,3 +137,27 @@ def test_a_single_row_has_no_distance():
     for rows, out, far in ((1, 24, {"ldx": 1}), (2, 1, {"ldw": 3})):
         opt = dpar.product_options(rows, 16, out, "bfloat16", **far)
         assert _code("linear", 2, opt, at, None, 0) == HIP
+
+
+@needs_no_gpu
+def test_a_result_may_be_its_residual():
+    """The update of a residual stream in place; not another rank's, another
+    distance's or one that a second rank reads too."""
+    at = {k: A + i * STEP for i, k in enumerate(ARRAYS["linear"].split())}
+    at["residual"] = at["y"]
+    opt = dpar.product_options(5, 16, 24, "bfloat16")
+    assert _code("linear", 2, opt, at, None, 0) == HIP
+    far = dpar.product_options(5, 16, 24, "bfloat16", ldr=48)
+    assert _code("linear", 2, far, at, None, 0) == ALIAS
+    y = [A, A + STEP]
+    rest = [[A + (2 + i) * STEP, A + (4 + i) * STEP] for i in range(2)]
+
+    def code(residual):
+        with pytest.raises(dpar.DparError) as e:
+            dpar.dpar_linear(*rest, None, residual, y, None, 2, opt)
+        return e.value.code
+
+    assert code(y) == HIP
+    assert code([y[0], 0]) == HIP
+    assert code(y[::-1]) == ALIAS
+    assert code([y[0], y[0]]) == ALIAS
