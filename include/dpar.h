@@ -473,8 +473,9 @@ const char* dpar_last_error(void);
  * of its own) and may be captured into a HIP graph.  A product with few result
  * tiles and a long sum splits the sum over workgroups and joins the parts in a
  * fixed order in a workspace (dpar_product_workspace); a large one with
- * operands off 16 bytes copies them there first.  Without a workspace it runs
- * without either.  Results are the same from run to run; with and without a
+ * operands off 16 bytes copies them there first; bias gradients over many rows
+ * are summed in parts there.  Without a workspace a call runs without all
+ * three.  Results are the same from run to run; with and without a
  * workspace they differ by the order of 32-bit additions. */
 typedef enum {
     DPAR_ACT_NONE = 0,
