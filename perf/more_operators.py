@@ -256,7 +256,7 @@ def _handle(s):
         r["y"] = made(p, rows, n_out, dtype=out, far=pad)
         opt = dpar.product_options(rows, n_in, n_out, "int8", c["out"],
                                    c["act"], ldx=n_in + pad, ldy=n_out + pad)
-        n = dpar.dpar_product_workspace(c["op"], p, opt)
+        n = dpar.dpar_product_workspace("gated" if gate else "linear", p, opt)
         args = [s["x"], s["sx"]]
         args += [s["wg"], s["sg"], s["wu"], s["su"], s["bg"], s["bu"]] \
             if gate else [s["wz"], s["sz"], s["bz"], s.get("r")]
