@@ -42,15 +42,16 @@ typedef enum {
 } dpar_status_t;
 
 /* Element types.  A DPAR_U32_MAT2X2 element is a 2x2 matrix of uint32 stored
- * row-major as [a00, a01, a10, a11] (16 bytes).  The 16-bit types belong to
- * the layer products (dpar_linear and the entry points after it); the
- * reduction sums their 32-bit results. */
+ * row-major as [a00, a01, a10, a11] (16 bytes).  The 16-bit and 8-bit types
+ * belong to the layer products (dpar_linear and the entry points after it);
+ * the reduction sums their 32-bit results. */
 typedef enum {
     DPAR_INT32 = 0,
     DPAR_FLOAT32 = 1,
     DPAR_U32_MAT2X2 = 2,
     DPAR_BFLOAT16 = 3,
-    DPAR_FLOAT16 = 4
+    DPAR_FLOAT16 = 4,
+    DPAR_INT8 = 5
 } dpar_dtype_t;
 
 /* Operators (Section 1: associative, possibly non-commutative).  Valid
@@ -554,6 +555,61 @@ int dpar_gated_backward(const void* const* dh, const void* const* x,
  * current device (0: it takes none).  No device work. */
 int dpar_product_workspace(dpar_product_call_t call, int p,
                            const dpar_product_t* opt, size_t* bytes);
+
+/* ---------------------------------------------------------------------------
+ * Layer products of 8-bit integers: rows and weights as whole numbers of -128
+ * .. 127 with a 32-bit scale for each row of x (a token) and each row of w (a
+ * channel).
+ *
+ *   dpar_quantize     scale_i = max |x_ij| / 127 over the row, q_ij = x_ij /
+ *                     scale_i to the nearest whole number, halves to even
+ *   dpar_linear_int8  z = sx_i sw_j (x w^T) + bias,  y = act(z) + residual
+ *   dpar_gated_int8   g = sx_i sg_j (x wg^T) + bg, u = sx_i su_j (x wu^T) + bu,
+ *                     h = act(g) * u
+ *
+ * Everything that is said of dpar_linear and dpar_gated holds, but for these:
+ * the options' dtype is DPAR_INT8, and their out_dtype (FLOAT32, BFLOAT16 or
+ * FLOAT16) is the type of y, h, the residual and the biases.  Scales are
+ * FLOAT32, one array of consecutive values per rank, of any sign.  The products
+ * are summed in 32-bit integers, exactly (`in` is at most 131071,
+ * DPAR_ERR_UNSUPPORTED beyond), converted to FLOAT32 and multiplied by the
+ * row's scale and then the channel's.  Nothing is kept for a backward pass, and
+ * there is none.  dpar_product_workspace answers for DPAR_LINEAR and DPAR_GATED
+ * with dtype DPAR_INT8; with and without a workspace the results are the
+ * same. */
+
+/* Sizes, type of x and row distances (in elements; 0: packed). */
+typedef struct {
+    size_t rows, cols;
+    dpar_dtype_t dtype;
+    size_t ldx, ldq;
+} dpar_quantize_t;
+
+/* x: FLOAT32, BFLOAT16 or FLOAT16; q: DPAR_INT8; scale: FLOAT32, `rows` values.
+ * The scale is rounded to 32 bits first; q is the exact quotient by it, rounded
+ * once, and held within -127 .. 127.  A row of zeros (or of values whose scale
+ * rounds to zero) has scale 0 and q 0; a row with an infinity or NaN has scale
+ * NaN and q 0, so that what is computed from it is NaN.  With cols == 0 the
+ * scales are 0. */
+int dpar_quantize(const void* const* x, void* const* q, void* const* scale,
+                  int p, const dpar_quantize_t* opt, hipStream_t stream);
+
+/* Optional: bias, residual. */
+int dpar_linear_int8(const void* const* x, const void* const* sx,
+                     const void* const* w, const void* const* sw,
+                     const void* const* bias, const void* const* residual,
+                     void* const* y, int p, const dpar_product_t* opt,
+                     void* workspace, size_t workspace_bytes,
+                     hipStream_t stream);
+
+/* Optional: bg, bu. */
+int dpar_gated_int8(const void* const* x, const void* const* sx,
+                    const void* const* wg, const void* const* sg,
+                    const void* const* wu, const void* const* su,
+                    const void* const* bg, const void* const* bu,
+                    void* const* h, int p, const dpar_product_t* opt,
+                    void* workspace, size_t workspace_bytes,
+                    hipStream_t stream);
 
 /* Frees every library-owned device and pinned host buffer (device tables,
  * counters, staging).  The library re-creates them lazily on the next call.

@@ -113,3 +113,51 @@ def gated_backward(dh, x, wg, wu, g, u, act_name, dtype, out):
     dg = _stored(dh * u * d, err * np.abs(u), dtype)
     du = _stored(dh * a, err, dtype)
     return _grads([("g", *dg), ("u", *du)], x, [wg, wu], out, dtype)
+
+
+# ------------------------------------------------------------------- 8 bits
+
+def quantize(x):
+    """(q, scale) of rows x (float64 of what is stored in 32 bits or fewer):
+    exact, the scale rounded to 32 bits."""
+    most = np.abs(x).max(axis=1, initial=0.0)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        scale = (most / 127).astype(np.float32)
+        scale[~np.isfinite(most)] = np.nan
+        q = np.rint(x / scale.astype(np.float64)[:, None])
+    q[~(scale > 0)] = 0
+    return np.clip(q, -127, 127), scale
+
+
+def _scaled(x, sx, w, sw):
+    """sx sw (x w^T): the sum is exact; its conversion and the two products are
+    rounded once each."""
+    z = (x @ w.T) * sx[:, None] * sw[None]
+    return z, 3.1 * _E * np.abs(z)
+
+
+def linear_int8(x, sx, w, sw, bias, residual, act_name, out):
+    z, e = _scaled(x, sx, w, sw)
+    if bias is not None:
+        z = z + bias
+        e = e + _E * (np.abs(z) + np.abs(bias))
+    y, _ = act(z, act_name)
+    ey = e * 1.13 + (0 if act_name == "none" else _ACT * (1 + np.abs(z)))
+    if residual is not None:
+        y = y + residual
+        ey = ey + _E * np.abs(y)
+    return _stored(y, ey, out)
+
+
+def gated_int8(x, sx, wg, sg, wu, su, bg, bu, act_name, out):
+    def affine(w, s, b):
+        z, e = _scaled(x, sx, w, s)
+        return (z, e) if b is None else \
+            (z + b, e + _E * (np.abs(z + b) + np.abs(b)))
+
+    (g, eg), (u, eu) = affine(wg, sg, bg), affine(wu, su, bu)
+    a, _ = act(g, act_name)
+    ea = eg * 1.13 + _ACT * (1 + np.abs(g))
+    h = a * u
+    return _stored(h, ea * np.abs(u) + np.abs(a) * eu + ea * eu
+                   + _E * np.abs(h), out)

@@ -11,7 +11,7 @@ namespace dpar {
 namespace products {
 
 // Element types (values of dpar_dtype_t).
-enum class Type : int { F32 = 1, BF16 = 3, F16 = 4 };
+enum class Type : int { F32 = 1, BF16 = 3, F16 = 4, I8 = 5 };
 // Activations (values of dpar_act_t).
 enum class Act : int { NONE = 0, RELU = 1, GELU = 2, GELU_TANH = 3, SILU = 4 };
 
@@ -37,6 +37,8 @@ struct Args {
   void* o[2][kRanks];
   // GATED: u; DW: bias gradients (sums)
   void* u[2][kRanks];
+  // I8: the scales of A's rows are in a[1], of B's in u[0] (GATED: wg's) and
+  // u[1] (wu's); nothing is kept
   size_t ni, nj, nc;         // rows and columns of C, contraction
   size_t na, nb;             // rows (columns, where stored so) of A and B
                              // that loads may touch: ni, nj or more
@@ -48,6 +50,7 @@ struct Args {
   int ranks, pairs;
   int act;
   int out32;                 // result in 32 bits
+  int out_type;              // I8: type of result, bias and residual
   int sums;                  // DW: with the sums of A
   int splits;                // parts of the contraction
   int waves;                 // few rows: parts of the contraction per
@@ -87,7 +90,7 @@ constexpr int kSumThreads = 512, kSumLine = 128;   // bytes of a row per
                                                    // workgroup
 
 // Copies matrices to 16-byte rows `pitch` bytes apart, zeros after the values;
-// sizes in 2-byte units.  Up to two matrices of either operand.
+// sizes in 2-byte units (launch_copy_int8: in bytes).  Up to two matrices of either operand.
 struct CopyArgs {
   struct Job {
     const void* from[kRanks];
@@ -103,11 +106,23 @@ hipError_t launch_copy(const CopyArgs& a, hipStream_t stream);
 hipError_t launch_bf16(Form f, const Args& a, hipStream_t stream);
 hipError_t launch_f16(Form f, const Args& a, hipStream_t stream);
 hipError_t launch_f32(Form f, const Args& a, hipStream_t stream);
+hipError_t launch_int8(Form f, const Args& a, hipStream_t stream);
+hipError_t launch_copy_int8(const CopyArgs& a, hipStream_t stream);
 hipError_t launch_slope_bf16(const SlopeArgs& a, hipStream_t stream);
 hipError_t launch_slope_f16(const SlopeArgs& a, hipStream_t stream);
 hipError_t launch_slope_f32(const SlopeArgs& a, hipStream_t stream);
 hipError_t launch_sums_bf16(const SumArgs& a, hipStream_t stream);
 hipError_t launch_sums_f16(const SumArgs& a, hipStream_t stream);
+
+// Rows to 8 bits with a scale each.
+struct QuantizeArgs {
+  const void* x[kRanks];
+  signed char* q[kRanks];
+  float* scale[kRanks];
+  size_t rows, cols, ldx, ldq;
+  int ranks, type;
+};
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t stream);
 
 }  // namespace products
 }  // namespace dpar

@@ -1,6 +1,7 @@
 // Layer products on gfx950's matrix cores: types bf16, fp16 and fp32, every
-// form of products.hpp, results accumulated in fp32.  Figures: one MI355X,
-// sizes as rows x in x out.
+// form of products.hpp, results accumulated in fp32; and 8-bit integers, LINEAR
+// and GATED, accumulated in 32-bit integers.  Figures: one MI355X, sizes as
+// rows x in x out.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -29,9 +30,9 @@ using Given = const __attribute__((address_space(4))) Args;
 using GivenSlope = const __attribute__((address_space(4))) SlopeArgs;
 using GivenSums = const __attribute__((address_space(4))) SumArgs;
 
-// A piece is 16 bytes; every tile holds 128 bytes of the contraction: 64
-// 16-bit or 32 32-bit values, in two steps of 4 pieces (one per lane group
-// of 16).
+// A piece is 16 bytes; every tile holds 128 bytes of the contraction: 128
+// 8-bit, 64 16-bit or 32 32-bit values, in two steps of 4 pieces (one per lane
+// group of 16).
 constexpr int kLine = 128;
 
 template <Type T> struct Elem;
@@ -78,10 +79,25 @@ template <> struct Elem<Type::F32> {
   }
 };
 
+// 8 bits: a piece per lane and step as for 16 bits, with twice the values, so
+// everything that moves bytes is the same.  The order of the contraction within
+// a step is the same for both operands and does not matter to an integer sum.
+template <> struct Elem<Type::I8> {
+  using V = signed char;
+  static __device__ i32x4 mma(i32x4 a, i32x4 b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+  }
+};
+
+// Four sums of a lane.
+template <Type T>
+using Acc = std::conditional_t<T == Type::I8, i32x4, f32x4>;
+
 // c[n] += a[n] b for N independent sums, in an order that leaves time between
 // two products into one sum.
 template <Type T, int N>
-__device__ inline void mma_row(const i32x4 (&a)[N], i32x4 b, f32x4 (&c)[N]) {
+__device__ inline void mma_row(const i32x4 (&a)[N], i32x4 b,
+                               Acc<T> (&c)[N]) {
   if constexpr (T == Type::F32) {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
@@ -212,19 +228,26 @@ __device__ inline void with_act(int act, Fn f) {
     default: f(std::integral_constant<Act, Act::NONE>());
   }
 }
-// f(EXACT), which holds for 32-bit values and for 32-bit results (out32) of
-// 16-bit ones.  Around loops over results: inside, the longer code of the exact
-// forms made 16-bit results slower (7 x 875 x 1001 x 1000 fp16 gelu 37.0
-// against 35.8 us).
+// f(EXACT, V()): EXACT holds for 32-bit values and for 32-bit results (out32)
+// of 16-bit ones; V is the type of what is not 32 bits (I8: of the results).
+// Around loops over results: inside, the longer code of the exact forms made
+// 16-bit results slower (7 x 875 x 1001 x 1000 fp16 gelu 37.0 against 35.8 us).
 template <Type T, bool ACTS = true, typename Fn>
-__device__ inline void with_exact(bool out32, Fn f) {
-  if constexpr (T == Type::F32) {
-    f(std::integral_constant<bool, true>());
+__device__ inline void with_exact(bool out32, int out_type, Fn f) {
+  if constexpr (T == Type::I8) {
+    if (out32)
+      f(std::integral_constant<bool, true>(), float());
+    else if (out_type == (int)Type::BF16)
+      f(std::integral_constant<bool, false>(), __bf16());
+    else
+      f(std::integral_constant<bool, false>(), _Float16());
+  } else if constexpr (T == Type::F32) {
+    f(std::integral_constant<bool, true>(), float());
   } else {
     if (ACTS && out32)
-      f(std::integral_constant<bool, true>());
+      f(std::integral_constant<bool, true>(), typename Elem<T>::V());
     else
-      f(std::integral_constant<bool, false>());
+      f(std::integral_constant<bool, false>(), typename Elem<T>::V());
   }
 }
 
@@ -543,21 +566,55 @@ __device__ inline void store_out(void* o, size_t at, const float* v, long left,
     store_vals<V, N>((V*)o + at, v, left, wide);
 }
 
-// The biases of N consecutive results from j on: b[0] (GATED: of g), b[1] of u.
+// What the results of N consecutive columns share: the biases, b[0] (GATED: of
+// g) and b[1] of u; I8: the columns' scales too.
+template <Type T, int N>
+struct Columns {
+  float b[2][N];
+  float s[2][T == Type::I8 ? N : 1];
+};
+
 template <Type T, Form F, int N>
-__device__ inline void fetch_bias(Given& a, int rank, size_t j,
-                                  float (&b)[2][N]) {
-  using V = typename Elem<T>::V;
+__device__ inline void fetch_columns(Given& a, int rank, size_t j,
+                                     Columns<T, N>& c) {
   if constexpr (F == Form::LINEAR || F == Form::GATED) {
     const long left = (long)a.nj - (long)j;
 #pragma unroll
     for (int p = 0; p < (F == Form::GATED ? 2 : 1); ++p) {
-      if (const V* e = (const V*)a.e[p][rank]) {
-        fetch_vals<V, N>(e + j, b[p], left, a.wide_out);
+      if (const void* e = a.e[p][rank]) {
+        if constexpr (T == Type::I8)
+          with_exact<T>(a.out32, a.out_type, [&](auto, auto v) {
+            using V = decltype(v);
+            fetch_vals<V, N>((const V*)e + j, c.b[p], left, a.wide_out);
+          });
+        else
+          fetch_vals<typename Elem<T>::V, N>(
+              (const typename Elem<T>::V*)e + j, c.b[p], left, a.wide_out);
       } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) b[p][k] = 0.f;
+        for (int k = 0; k < N; ++k) c.b[p][k] = 0.f;
       }
+      if constexpr (T == Type::I8)
+        fetch_vals<float, N>((const float*)a.u[p][rank] + j, c.s[p], left,
+                             a.wide_out);
+    }
+  }
+}
+
+// Sums as 32-bit values.  I8: (sum * the row's scale) * the column's, each
+// rounded once, as the sum itself is beyond 2^24.
+template <Type T, Form F, int N>
+__device__ inline void values(Given& a, int rank, size_t i,
+                              const Columns<T, N>& c, float* v, float* u2) {
+  if constexpr (T == Type::I8) {
+    const float row = ((const float*)a.a[1][rank])[i];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      v[k] = (float)__builtin_bit_cast(int, v[k]) * row * c.s[0][k];
+    if constexpr (F == Form::GATED) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        u2[k] = (float)__builtin_bit_cast(int, u2[k]) * row * c.s[1][k];
     }
   }
 }
@@ -567,13 +624,14 @@ constexpr bool acts(Form f) { return f == Form::LINEAR || f == Form::GATED; }
 
 // N consecutive values j .. of row i: bias, activation, residual, rounding,
 // stores.  v: the product's sums (GATED: v of g, u2 of u).
-template <Type T, Form F, bool EXACT, int N>
+template <Type T, Form F, bool EXACT, typename V, int N>
 __device__ inline void finish(Given& a, int rank, int pair, size_t i,
                               size_t j, float* v, float* u2,
-                              const float (&b)[2][N]) {
-  using V = typename Elem<T>::V;
+                              const Columns<T, N>& c) {
+  constexpr bool kKeeps = T != Type::I8;
   const long left = (long)a.nj - (long)j;
   const bool wide = a.wide_out;
+  values<T, F, N>(a, rank, i, c, v, u2);
   if constexpr (F == Form::LINEAR) {
     const void* r = a.e[1][rank];
     float t[N];
@@ -584,9 +642,10 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
         fetch_vals<V, N>((const V*)r + i * a.lde + j, t, left, wide);
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += b[0][k];
-    if (V* z = (V*)a.o[1][rank])
-      store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
+    for (int k = 0; k < N; ++k) v[k] += c.b[0][k];
+    if constexpr (kKeeps)
+      if (V* z = (V*)a.o[1][rank])
+        store_vals<V, N>(z + i * a.ldk + j, v, left, wide);
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] = act_of<act.value, EXACT>(v[k]);
@@ -598,13 +657,15 @@ __device__ inline void finish(Given& a, int rank, int pair, size_t i,
     store_out<N>(a.o[0][rank], i * a.ldo + j, v, left, a.out32, wide, V());
   } else if constexpr (F == Form::GATED) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += b[0][k];
+    for (int k = 0; k < N; ++k) v[k] += c.b[0][k];
 #pragma unroll
-    for (int k = 0; k < N; ++k) u2[k] += b[1][k];
-    if (V* g = (V*)a.o[1][rank])
-      store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
-    if (V* u = (V*)a.u[0][rank])
-      store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
+    for (int k = 0; k < N; ++k) u2[k] += c.b[1][k];
+    if constexpr (kKeeps) {
+      if (V* g = (V*)a.o[1][rank])
+        store_vals<V, N>(g + i * a.ldk + j, v, left, wide);
+      if (V* u = (V*)a.u[0][rank])
+        store_vals<V, N>(u + i * a.ldk + j, u2, left, wide);
+    }
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int k = 0; k < N; ++k)
@@ -734,14 +795,13 @@ __device__ inline void join_sums(Given& a, int rank, int pair, unsigned split,
 // and column jw on, and the sums of A that it holds.
 template <Type T, Form F, bool SUMS, int WM, int WN, int SHARES, typename OB>
 struct Results {
-  using V = typename Elem<T>::V;
   static constexpr bool kGated = F == Form::GATED;
   static constexpr int MI = WM / 16, NJ = WN / 16, NT = kGated ? NJ / 2 : NJ;
 
   static __device__ void store(Given& a, int rank, int pair, unsigned split,
                                size_t iw, size_t jw, bool sums, int share,
                                const Sums<MI, SHARES>& sum,
-                               f32x4 (&acc)[MI][NJ], LDS char* lds, int wave,
+                               Acc<T> (&acc)[MI][NJ], LDS char* lds, int wave,
                                int lane) {
     if constexpr (SUMS)
       if (sums && lane < 16) {
@@ -752,7 +812,8 @@ struct Results {
           if (i >= a.ni) continue;
           float v = sum.v[n][0];
           if (a.splits == 1)
-            store_out<1>(a.u[pair][rank], i, &v, 1, a.out32, false, V());
+            store_out<1>(a.u[pair][rank], i, &v, 1, a.out32, false,
+                         typename Elem<T>::V());
           else    // after all partial results: [split][rank][pair][row]
             a.part[(size_t)a.splits * a.ranks * a.pairs * a.ni * a.nj +
                    (((size_t)split * a.ranks + rank) * a.pairs + pair) * a.ni +
@@ -771,8 +832,8 @@ struct Results {
     static_assert(64 % PER == 0);
     const int c = lane % PER * 2;
     const size_t j = jw + c * 4;
-    float bias[2][8];
-    if (a.splits == 1 && j < a.nj) fetch_bias<T, F, 8>(a, rank, j, bias);
+    Columns<T, 8> cols;
+    if (a.splits == 1 && j < a.nj) fetch_columns<T, F, 8>(a, rank, j, cols);
     landed<0>();
     meet();
 #pragma unroll
@@ -786,10 +847,12 @@ struct Results {
           const int c = n < NT ? q * NT + OB::group_of(q, n) / 4
                                : CH / 2 + q * NT + OB::group_of(q, n - NT) / 4;
           *(LDS f32x4*)(mine + (m * 16 + r) * (WN * 4) +
-                        (c ^ (r & kTurn)) * 16) = acc[mh + m][n];
+                        (c ^ (r & kTurn)) * 16) =
+              __builtin_bit_cast(f32x4, acc[mh + m][n]);
         }
       in_order();
-      with_exact<T, acts(F)>(a.out32, [&](auto exact) {
+      with_exact<T, acts(F)>(a.out32, a.out_type, [&](auto exact, auto type) {
+        using V = decltype(type);
 #pragma unroll 1
         for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
           const size_t i = iw + mh * 16 + row;
@@ -804,7 +867,7 @@ struct Results {
             *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
           }
           if (a.splits == 1) {
-            finish<T, F, exact.value, 8>(a, rank, pair, i, j, v, u2, bias);
+            finish<T, F, exact.value, V, 8>(a, rank, pair, i, j, v, u2, cols);
           } else {
             // [split][rank][pair or projection][row][column]
             const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
@@ -875,7 +938,7 @@ struct Tiled {
                                            a.splits));
     const unsigned whole = uniform((unsigned)(a.nc / KT));  // tiles
 
-    f32x4 acc[MI][NJ] = {};
+    Acc<T> acc[MI][NJ] = {};
     Sums<MI, BN / WN> sum;
     const bool sums = SUMS && a.u[pair][rank] && j0 == 0;
 
@@ -1138,7 +1201,7 @@ struct PingPong {
                                            a.splits));
     const unsigned whole = uniform((unsigned)(a.nc / KT));
 
-    f32x4 acc[MI][NJ] = {};
+    Acc<T> acc[MI][NJ] = {};
     Sums<MI, kAcross> sum;
     const bool sums = SUMS && a.u[pair][rank] && j0 == 0;
 
@@ -1308,6 +1371,22 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
   Tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
 }
 
+// The same for 8 bits.
+template <Form F, int BN>
+__global__ __launch_bounds__(512) void k_int8_pingpong(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  PingPong<Type::I8, F, false, BN>::run(a, (LDS char*)lds);
+}
+
+template <Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
+__global__
+__launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_tiled(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  Tiled<Type::I8, F, false, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
+}
+
 // ---------------------------------------------------------------- few rows
 
 // Few rows of x (MT tiles of 16), bound by one read of the weights: a wavefront
@@ -1348,7 +1427,7 @@ struct Few {
       if (i >= a.ni) i = a.ni - 1;
       x[m] = (const V*)a.a[0][rank] + i * a.lda + q * E;
     }
-    f32x4 acc[MT][NW] = {};
+    Acc<T> acc[MT][NW] = {};
     unsigned s = s0;
     const unsigned full = (unsigned)(a.nc / K) < s1 ? (unsigned)(a.nc / K) : s1;
 #pragma unroll 1
@@ -1387,13 +1466,13 @@ struct Few {
         for (int m = 0; m < MT; ++m)
           acc[m][n] = Elem<T>::mma(fw[n], fx[m], acc[m][n]);
     }
-    finish_all(a, (f32x4(LDS*)[MT * NW][64])lds, acc, rank, j0, wave, lane);
+    finish_all(a, (Acc<T>(LDS*)[MT * NW][64])lds, acc, rank, j0, wave, lane);
   }
 
   // Adds the S wavefronts' sums in their order and finishes the results, by way
   // of LDS, so that the code that finishes a tile of results is there once.
-  static __device__ void finish_all(Given& a, f32x4 (LDS* part)[MT * NW][64],
-                                    f32x4 (&acc)[MT][NW], unsigned rank,
+  static __device__ void finish_all(Given& a, Acc<T> (LDS* part)[MT * NW][64],
+                                    Acc<T> (&acc)[MT][NW], unsigned rank,
                                     size_t j0, int wave, int lane) {
     const int r = lane & 15, q = lane >> 4;
 #pragma unroll
@@ -1406,11 +1485,12 @@ struct Few {
       in_order();
     // result tile (m, n): wavefront tile % S
     constexpr int NO = kGated ? NW / 2 : NW, NS = kGated ? 2 : 1;
-    with_exact<T>(a.out32, [&](auto exact) {
+    with_exact<T>(a.out32, a.out_type, [&](auto exact, auto type) {
+      using V = decltype(type);
 #pragma unroll 1
       for (int t = wave; t < MT * NO; t += S) {
         const int m = t / NO, n = t % NO, w = m * NW + n * NS;
-        f32x4 v = part[0][w][lane], u = part[0][w + NS - 1][lane];
+        Acc<T> v = part[0][w][lane], u = part[0][w + NS - 1][lane];
 #pragma unroll
         for (int k = 1; k < S; ++k) {
           v += part[k][w][lane];
@@ -1420,10 +1500,15 @@ struct Few {
         if (i >= a.ni || j >= a.nj) continue;
         float va[4], ua[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) va[e] = v[e], ua[e] = u[e];
-        float bias[2][4];
-        fetch_bias<T, F, 4>(a, rank, j, bias);
-        finish<T, F, exact.value, 4>(a, rank, 0, i, j, va, ua, bias);
+        for (int e = 0; e < 4; ++e) {
+          // (values first: a cast of a vector's element took the first one)
+          const auto ve = v[e], ue = u[e];
+          va[e] = __builtin_bit_cast(float, ve);
+          ua[e] = __builtin_bit_cast(float, ue);
+        }
+        Columns<T, 4> cols;
+        fetch_columns<T, F, 4>(a, rank, j, cols);
+        finish<T, F, exact.value, V, 4>(a, rank, 0, i, j, va, ua, cols);
       }
     });
   }
@@ -1532,7 +1617,7 @@ struct FewFast {
           }
       }
     };
-    f32x4 acc[MT][NW] = {};
+    Acc<T> acc[MT][NW] = {};
     if (c0 < c1) issue(c0, 0, 0);
     int buf = 0;
 #pragma unroll 1
@@ -1559,7 +1644,7 @@ struct FewFast {
     }
     // the parts meet in LDS where the chunks were
     if (S > 1) __syncthreads();
-    Old::finish_all(a, (f32x4(LDS*)[MT * NW][64])lds, acc, rank, j0, wave,
+    Old::finish_all(a, (Acc<T>(LDS*)[MT * NW][64])lds, acc, rank, j0, wave,
                     lane);
   }
 };
@@ -1574,13 +1659,22 @@ __global__ __launch_bounds__(S * 64) void k_few(Args) {
     Few<T, F, FAST, MT, NW, S>::run(a, (LDS char*)lds);
 }
 
+template <Form F, bool FAST, int MT, int NW, int S>
+__global__ __launch_bounds__(S * 64) void k_int8_few(Args) {
+  Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  if constexpr (FAST)
+    FewFast<Type::I8, F, MT, NW, S>::run(a, (LDS char*)lds);
+  else
+    Few<Type::I8, F, FAST, MT, NW, S>::run(a, (LDS char*)lds);
+}
+
 // Joins the parts of a split contraction in their order and finishes: 4
 // results per thread, bound by reading the parts (about 4 us more than their
 // bytes at 2.3 TB/s, the writing of them included).
 template <Type T, Form F>
 __global__ __launch_bounds__(256) void k_join(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
-  using V = typename Elem<T>::V;
   const size_t per = (a.nj + 3) / 4;
   const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
   const int np = F == Form::DW ? a.pairs : 1;
@@ -1592,25 +1686,34 @@ __global__ __launch_bounds__(256) void k_join(Args) {
     const size_t i = x % a.ni;
     const int pair = x / a.ni % np, rank = x / a.ni / np;
     const long left = (long)a.nj - (long)j;
+    // (I8: sums of 32-bit integers, in the floats' bits)
     float v[4] = {}, u2[4] = {}, t[4];
+    auto add = [](float& sum, float more) {
+      if constexpr (T == Type::I8)
+        sum = __builtin_bit_cast(float, __builtin_bit_cast(int, sum) +
+                                            __builtin_bit_cast(int, more));
+      else
+        sum += more;
+    };
     const size_t step = (size_t)a.ranks * np * NP * sz;
     const float* w = a.part + ((size_t)rank * np + pair) * NP * sz + i * a.nj
                      + j;
     for (int s = 0; s < a.splits; ++s, w += step) {
       fetch_vals<float, 4>(w, t, left, a.nj % 4 == 0);
-      for (int k = 0; k < 4; ++k) v[k] += t[k];
+      for (int k = 0; k < 4; ++k) add(v[k], t[k]);
       if (F == Form::GATED) {
         fetch_vals<float, 4>(w + sz, t, left, a.nj % 4 == 0);
-        for (int k = 0; k < 4; ++k) u2[k] += t[k];
+        for (int k = 0; k < 4; ++k) add(u2[k], t[k]);
       }
     }
-    float bias[2][4];
-    fetch_bias<T, F, 4>(a, rank, j, bias);
-    with_exact<T, acts(F)>(a.out32, [&](auto exact) {
-      finish<T, F, exact.value, 4>(a, rank, pair, i, j, v, u2, bias);
+    Columns<T, 4> cols;
+    fetch_columns<T, F, 4>(a, rank, j, cols);
+    with_exact<T, acts(F)>(a.out32, a.out_type, [&](auto exact, auto type) {
+      finish<T, F, exact.value, decltype(type), 4>(a, rank, pair, i, j, v, u2,
+                                                   cols);
     });
   }
-  if (F == Form::DW) {
+  if constexpr (F == Form::DW) {
     const size_t n = (size_t)a.ranks * a.pairs * a.ni;
     if (a.sums && id < n &&
         a.u[id / a.ni % a.pairs][id / a.ni / a.pairs]) {
@@ -1619,7 +1722,7 @@ __global__ __launch_bounds__(256) void k_join(Args) {
       float s = 0.f;
       for (int k = 0; k < a.splits; ++k) s += w[k * n];
       store_out<1>(a.u[id / a.ni % a.pairs][id / a.ni / a.pairs], id % a.ni,
-                   &s, 1, a.out32, false, V());
+                   &s, 1, a.out32, false, typename Elem<T>::V());
     }
   }
 }
@@ -1710,7 +1813,7 @@ __global__ __launch_bounds__(kSumThreads) void k_sums(SumArgs) {
     V* dz = (V*)a.s.dz[rank] + j;
     V* du = GATED ? (V*)a.s.du[rank] + j : nullptr;
     float sum[NP][E] = {};
-    with_exact<T>(a.out32, [&](auto exact) {
+    with_exact<T>(a.out32, 0, [&](auto exact, auto) {
       if (left <= 0) return;
       for (size_t i = a.s.rows * part / a.parts + t / kLanes; i < i1;
            i += kSumThreads / kLanes) {
@@ -1793,15 +1896,23 @@ template <Type T, Form F, bool SUMS, bool FAST, int BM, int BN, int WM, int WN,
           int R>
 hipError_t go(const Args& a, hipStream_t stream) {
   using K = Tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>;
-  return launch_tiles<k_tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>>(
-      F, a, BM, K::BJ, K::kThreads, R * K::kBytes, stream);
+  if constexpr (T == Type::I8)
+    return launch_tiles<k_int8_tiled<F, FAST, BM, BN, WM, WN, R>>(
+        F, a, BM, K::BJ, K::kThreads, R * K::kBytes, stream);
+  else
+    return launch_tiles<k_tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>>(
+        F, a, BM, K::BJ, K::kThreads, R * K::kBytes, stream);
 }
 
 template <Type T, Form F, bool SUMS, int BN>
 hipError_t go_pingpong(const Args& a, hipStream_t stream) {
   using K = PingPong<T, F, SUMS, BN>;
-  return launch_tiles<k_pingpong<T, F, SUMS, BN>>(
-      F, a, K::BM, K::BJ, K::kThreads, K::kLds, stream);
+  if constexpr (T == Type::I8)
+    return launch_tiles<k_int8_pingpong<F, BN>>(
+        F, a, K::BM, K::BJ, K::kThreads, K::kLds, stream);
+  else
+    return launch_tiles<k_pingpong<T, F, SUMS, BN>>(
+        F, a, K::BM, K::BJ, K::kThreads, K::kLds, stream);
 }
 
 template <Type T, Form F, bool FAST, int MT, int NW, int S>
@@ -1812,8 +1923,12 @@ hipError_t go_few(const Args& a, hipStream_t stream) {
   const size_t bytes =
       FAST ? std::max(parts, (size_t)S * 2 * FewFast<T, F, MT, NW, S>::kChunk)
            : parts;
-  return launch_kernel<k_few<T, F, FAST, MT, NW, S>>(a, n, S * 64, bytes,
-                                                     stream);
+  if constexpr (T == Type::I8)
+    return launch_kernel<k_int8_few<F, FAST, MT, NW, S>>(a, n, S * 64, bytes,
+                                                         stream);
+  else
+    return launch_kernel<k_few<T, F, FAST, MT, NW, S>>(a, n, S * 64, bytes,
+                                                       stream);
 }
 
 // Wavefronts: 8 only with the fewest sets of weight rows that a row count

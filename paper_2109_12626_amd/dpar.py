@@ -24,8 +24,8 @@ DPAR_ERR_NOMEM = -4
 DPAR_ERR_HIP = -5
 DPAR_ERR_TIMEOUT = -6
 
-DPAR_INT32, DPAR_FLOAT32, DPAR_U32_MAT2X2, DPAR_BFLOAT16, DPAR_FLOAT16 = \
-    0, 1, 2, 3, 4
+DPAR_INT32, DPAR_FLOAT32, DPAR_U32_MAT2X2, DPAR_BFLOAT16, DPAR_FLOAT16, \
+    DPAR_INT8 = 0, 1, 2, 3, 4, 5
 DPAR_SUM, DPAR_MAX, DPAR_MATMUL = 0, 1, 2
 DPAR_EXEC_AUTO, DPAR_EXEC_LAUNCH_PER_ROUND, DPAR_EXEC_GRID_BARRIER, \
     DPAR_EXEC_TICKET, DPAR_EXEC_SPLIT, DPAR_EXEC_ROUNDS, \
@@ -38,7 +38,7 @@ DPAR_LINEAR, DPAR_LINEAR_BACKWARD, DPAR_GATED, DPAR_GATED_BACKWARD = 0, 1, 2, 3
 
 DTYPES = {"int32": DPAR_INT32, "float32": DPAR_FLOAT32,
           "u32mat2x2": DPAR_U32_MAT2X2, "bfloat16": DPAR_BFLOAT16,
-          "float16": DPAR_FLOAT16}
+          "float16": DPAR_FLOAT16, "int8": DPAR_INT8}
 OPS = {"sum": DPAR_SUM, "max": DPAR_MAX, "matmul": DPAR_MATMUL}
 EXECS = {"auto": DPAR_EXEC_AUTO, "launch": DPAR_EXEC_LAUNCH_PER_ROUND,
          "barrier": DPAR_EXEC_GRID_BARRIER, "ticket": DPAR_EXEC_TICKET,
@@ -88,6 +88,12 @@ class dpar_product_t(ctypes.Structure):
                 ("lddw", ctypes.c_size_t)]
 
 
+class dpar_quantize_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_size_t), ("cols", ctypes.c_size_t),
+                ("dtype", ctypes.c_int), ("ldx", ctypes.c_size_t),
+                ("ldq", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -125,6 +131,10 @@ def lib():
     L.dpar_gated.argtypes = [vp] * 8 + tail
     L.dpar_gated_backward.argtypes = [vp] * 13 + tail
     L.dpar_product_workspace.argtypes = [i, i, opt, ctypes.POINTER(sz)]
+    L.dpar_quantize.argtypes = [vp] * 3 + [i, ctypes.POINTER(dpar_quantize_t),
+                                           vp]
+    L.dpar_linear_int8.argtypes = [vp] * 7 + tail
+    L.dpar_gated_int8.argtypes = [vp] * 9 + tail
     L.dpar_last_error.restype = ctypes.c_char_p
     L.dpar_last_error.argtypes = []
     L.dpar_finalize.argtypes = []
@@ -136,7 +146,8 @@ def lib():
                  "dpar_check_status", "dpar_finalize",
                  "dpar_set_phase_event", "dpar_linear",
                  "dpar_linear_backward", "dpar_gated", "dpar_gated_backward",
-                 "dpar_product_workspace"):
+                 "dpar_product_workspace", "dpar_quantize",
+                 "dpar_linear_int8", "dpar_gated_int8"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -346,6 +357,35 @@ def dpar_gated_backward(dh, x, wg, wu, g, u, dx, dwg, dwu, dbg, dbu, dg, du, p,
                     opt, workspace, workspace_bytes, stream)
 
 
+def quantize_options(rows, cols, dtype, ldx=0, ldq=0):
+    """Sizes, type of x and row distances of a quantisation
+    (dpar_quantize_t)."""
+    return dpar_quantize_t(rows, cols, _enum(DTYPES, dtype), ldx, ldq)
+
+
+def dpar_quantize(x, q, scale, p, opt, stream=None):
+    """Sequences of p device addresses; opt: quantize_options()."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    rc = lib().dpar_quantize(_ptr_array(x), _ptr_array(q), _ptr_array(scale),
+                             p, ctypes.byref(opt), stream)
+    return rc if rc >= 0 else _check(rc)
+
+
+def dpar_linear_int8(x, sx, w, sw, bias, residual, y, p, opt, workspace=None,
+                     workspace_bytes=0, stream=None):
+    """As dpar_linear; opt: product_options() with dtype "int8"."""
+    return _product(lib().dpar_linear_int8, (x, sx, w, sw, bias, residual, y),
+                    p, opt, workspace, workspace_bytes, stream)
+
+
+def dpar_gated_int8(x, sx, wg, sg, wu, su, bg, bu, h, p, opt, workspace=None,
+                    workspace_bytes=0, stream=None):
+    return _product(lib().dpar_gated_int8,
+                    (x, sx, wg, sg, wu, su, bg, bu, h), p, opt, workspace,
+                    workspace_bytes, stream)
+
+
 def dpar_last_error():
     return lib().dpar_last_error().decode()
 
@@ -401,6 +441,8 @@ _NAMES = {torch.float32: "float32", torch.bfloat16: "bfloat16",
 class _Call:
     """Shapes, row distances and addresses of one call's tensors."""
 
+    types = _NAMES
+
     def __init__(self, w, rows_, out_dtype, act):
         self.flat = w.dim() == 2
         self.p = 1 if self.flat else w.shape[0]
@@ -408,11 +450,11 @@ class _Call:
         self.rows = rows_
         self.dtype = w.dtype
         self.out_dtype = w.dtype if out_dtype is None else out_dtype
-        if w.dtype not in _NAMES or self.out_dtype not in _NAMES:
+        if w.dtype not in self.types or self.out_dtype not in _NAMES:
             raise ValueError(f"types {w.dtype}, {self.out_dtype}")
         self.opt = product_options(rows_, self.n_in, self.n_out,
-                                   _NAMES[w.dtype], _NAMES[self.out_dtype],
-                                   act)
+                                   self.types[w.dtype],
+                                   _NAMES[self.out_dtype], act)
         self.device = w.device
 
     def given(self, t, name, shape, ld=None, dtype=None):
@@ -431,7 +473,7 @@ class _Call:
                              and t.shape[0] == self.p)):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, want "
                              f"{shape} or {(self.p,) + shape}")
-        if one and self.p > 1 and name not in ("x", "dy", "dh"):
+        if one and self.p > 1 and name not in ("x", "sx", "dy", "dh"):
             raise ValueError(f"{name}: one matrix for {self.p} ranks")
         if shape[-1] > 1 and t.stride(-1) != 1:
             raise ValueError(f"{name}: values of a row are not consecutive")
@@ -540,3 +582,68 @@ def gated_backward(dh, x, wg, wu, g, u, act="silu", out_dtype=None,
           arrays + [_addresses(t) for t in (dx, dwg, dwu, dbg, dbu, dg, du)])
     out = (dx, dwg, dwu, dbg, dbu) if bias else (dx, dwg, dwu)
     return tuple(c.result(t) for t in out)
+
+
+# The 8-bit products: x and weights int8, their scales float32 [.., rows] and
+# [.., out]; the result, biases and residual have out_dtype.
+
+class _Int8Call(_Call):
+    types = {torch.int8: "int8"}
+
+
+def quantize(x):
+    """(q, scale): the rows of x [p, rows, cols] or [rows, cols] as whole
+    numbers of 8 bits and what a step of each row is."""
+    if x.dim() not in (2, 3) or x.dtype not in _NAMES:
+        raise ValueError(f"x: {x.dtype}, shape {tuple(x.shape)}")
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("x requires a gradient, and rounding has none: call "
+                         "under torch.no_grad() or detach it")
+    t = x if x.dim() == 3 else x[None]
+    p, n, cols = t.shape
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError("x: values of a row are not consecutive")
+    far = t.stride(-2) if n > 1 else cols
+    if far < cols:
+        raise ValueError(f"x: rows {far} values apart overlap")
+    q = torch.empty(p, n, cols, dtype=torch.int8, device=x.device)
+    scale = torch.empty(p, n, dtype=torch.float32, device=x.device)
+    dpar_quantize(rows(t), rows(q), rows(scale), p,
+                  quantize_options(n, cols, _NAMES[x.dtype], far),
+                  torch.cuda.current_stream(x.device))
+    return (q, scale) if x.dim() == 3 else (q[0], scale[0])
+
+
+def linear_int8(x, sx, w, sw, bias=None, residual=None, act="none",
+                out_dtype=torch.bfloat16):
+    """act(sx sw (x w^T) + bias) + residual."""
+    c = _Int8Call(w, x.shape[-2], out_dtype, act)
+    f32 = torch.float32
+    y = c.made(c.rows, c.n_out)
+    c.run("linear", dpar_linear_int8,
+          [c.given(x, "x", (c.rows, c.n_in), "ldx"),
+           c.given(sx, "sx", (c.rows,), dtype=f32),
+           c.given(w, "w", (c.n_out, c.n_in), "ldw"),
+           c.given(sw, "sw", (c.n_out,), dtype=f32),
+           c.given(bias, "bias", (c.n_out,), dtype=c.out_dtype),
+           c.given(residual, "residual", (c.rows, c.n_out), "ldr",
+                   c.out_dtype), _addresses(y)])
+    return c.result(y)
+
+
+def gated_int8(x, sx, wg, sg, wu, su, bg=None, bu=None, act="silu",
+               out_dtype=torch.bfloat16):
+    """act(sx sg (x wg^T) + bg) * (sx su (x wu^T) + bu)."""
+    c = _Int8Call(wg, x.shape[-2], out_dtype, act)
+    f32 = torch.float32
+    h = c.made(c.rows, c.n_out)
+    c.run("gated", dpar_gated_int8,
+          [c.given(x, "x", (c.rows, c.n_in), "ldx"),
+           c.given(sx, "sx", (c.rows,), dtype=f32),
+           c.given(wg, "wg", (c.n_out, c.n_in), "ldw"),
+           c.given(sg, "sg", (c.n_out,), dtype=f32),
+           c.given(wu, "wu", (c.n_out, c.n_in), "ldw"),
+           c.given(su, "su", (c.n_out,), dtype=f32),
+           c.given(bg, "bg", (c.n_out,), dtype=c.out_dtype),
+           c.given(bu, "bu", (c.n_out,), dtype=c.out_dtype), _addresses(h)])
+    return c.result(h)
