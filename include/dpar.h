@@ -611,6 +611,81 @@ int dpar_gated_int8(const void* const* x, const void* const* sx,
                     void* workspace, size_t workspace_bytes,
                     hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * A mixture-of-experts layer for a few tokens: every token goes through the
+ * `top` experts that its logits are largest for, each a gated layer, and gets
+ * the sum of their results by the choice's weights.  p ranks hold `experts`
+ * experts each, numbers i * experts .. (i + 1) * experts - 1 those of rank i;
+ * every rank chooses among all p * experts and sums what its own ones
+ * contribute: dpar_allreduce joins the ranks' results.
+ *
+ *   h_te = act(wg_e x_t) * (wu_e x_t)
+ *   y_t  = sum over t's chosen experts e of the rank of weight_te (wd_e h_te)
+ *          + residual_t
+ *
+ * Types: x, wg, wu and wd of one type (BFLOAT16, FLOAT16 or FLOAT32), or, for
+ * 16-bit x, weights in DPAR_INT8 with a FLOAT32 scale for each row of a matrix
+ * (sg, su: [expert][hidden], sd: [expert][in], consecutive); y and the residual
+ * in out_dtype, which is dtype or FLOAT32.  Sums, logits and weights are 32
+ * bits; h is held to 2^-16 (to 2^-24 where y is FLOAT32).
+ *
+ * The choice, with logits [tokens][p * experts] in FLOAT32: the largest first,
+ * of equal ones the lowest expert (NaN counts as the largest); a logit of
+ * -infinity is never chosen, so a token may have fewer experts than `top`, or
+ * none (its y is the residual, or 0).  Weights: DPAR_ROUTE_SOFTMAX, the softmax
+ * over all experts, with `normalize` over the chosen ones; DPAR_ROUTE_SIGMOID,
+ * 1 / (1 + exp(-logit)), with `normalize` divided by the chosen ones' sum
+ * (where that is not 0); each times weight_scale.  The choice is written to
+ * index [tokens][top] (int32; -1 with weight 0 for no expert) and weight
+ * [tokens][top] (FLOAT32) of the ranks that have them.  With logits NULL, index
+ * and weight are inputs: an index outside 0 .. p * experts - 1 is no expert, and
+ * an expert named twice counts with both weights.
+ *
+ * Arrays, pointers, aliases (y may be its rank's residual), streams, graphs and
+ * errors are as for the products above.  Up to 128 tokens, `top` up to 16, up to
+ * 1024 experts in all (DPAR_ERR_UNSUPPORTED beyond).  wg, wu [expert][hidden]
+ * [in] and wd [expert][in][hidden] of a rank lie in one piece of memory each.
+ * The workspace holds the choice and h: it is required, 16-byte aligned, of
+ * dpar_moe_workspace bytes. */
+typedef enum {
+    DPAR_ROUTE_SOFTMAX = 0,
+    DPAR_ROUTE_SIGMOID = 1
+} dpar_route_t;
+
+/* Sizes, types and distances (in elements; 0: packed) of the layer.
+ *   ldx   rows of x              (packed: in)
+ *   ldl   rows of logits         (packed: p * experts)
+ *   ldw   rows of wg, wu         (packed: in)
+ *   ldd   rows of wd             (packed: hidden)
+ *   xw    matrices of wg, wu     (packed: hidden * ldw)
+ *   xd    matrices of wd         (packed: in * ldd)
+ *   ldy   rows of y              (packed: in)
+ *   ldr   rows of the residual   (packed: in) */
+typedef struct {
+    size_t tokens, in, hidden, experts;
+    int top;
+    dpar_dtype_t dtype, weight_dtype, out_dtype;
+    dpar_act_t act;
+    dpar_route_t route;
+    int normalize;
+    float weight_scale;
+    size_t ldx, ldl, ldw, ldd, xw, xd, ldy, ldr;
+} dpar_moe_t;
+
+/* Optional: sg, su, sd (all three with DPAR_INT8 weights, else none), residual;
+ * index and weight (single ranks' too; inputs of every rank with logits
+ * NULL). */
+int dpar_moe(const void* const* x, const void* const* logits,
+             const void* const* wg, const void* const* wu,
+             const void* const* wd, const void* const* sg,
+             const void* const* su, const void* const* sd,
+             const void* const* residual, void* const* y, void* const* index,
+             void* const* weight, int p, const dpar_moe_t* opt,
+             void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* *bytes: the workspace of a call of these sizes.  No device work. */
+int dpar_moe_workspace(int p, const dpar_moe_t* opt, size_t* bytes);
+
 /* Frees every library-owned device and pinned host buffer (device tables,
  * counters, staging).  The library re-creates them lazily on the next call.
  * The caller must make sure no enqueued call is still running. */

@@ -161,3 +161,77 @@ def gated_int8(x, sx, wg, sg, wu, su, bg, bu, act_name, out):
     h = a * u
     return _stored(h, ea * np.abs(u) + np.abs(a) * eu + ea * eu
                    + _E * np.abs(h), out)
+
+
+# ------------------------------------------------------- mixture of experts
+
+def choice(logits, top, route, normalize, scale=1.0):
+    """(index, weight) [tokens, top] of logits in 64 bits."""
+    tokens, experts = logits.shape
+    index = np.full((tokens, top), -1, dtype=np.int32)
+    weight = np.zeros((tokens, top))
+    with np.errstate(all="ignore"):
+        for t in range(tokens):
+            v = logits[t]
+            best = sorted((e for e in range(experts) if v[e] != -np.inf),
+                          key=lambda e: (not np.isnan(v[e]), -v[e], e))[:top]
+            if not best:
+                continue
+            if route == "softmax":
+                a = np.exp(v[best] - v[best[0]])
+                w = a / (a if normalize else np.exp(v - v[best[0]])).sum()
+            else:
+                w = 1 / (1 + np.exp(-v[best]))
+                if normalize and w.sum() != 0:
+                    w = w / w.sum()
+            index[t, :len(best)] = best
+            weight[t, :len(best)] = w * scale
+    return index, weight
+
+
+def moe(x, index, weight, wg, wu, wd, scales, residual, act_name, dtype, out,
+        first=0, chosen=True):
+    """y of the rank that holds experts first .. (wg [experts, hidden, in]);
+    scales: of 8-bit weights, (sg, su, sd) or None; chosen: the weights are the
+    library's own, a few 2^-24 off."""
+    tokens, top = index.shape
+    hidden, n_in = wg.shape[1:]
+    parts = 6                     # products per hidden value at most
+    y, ey = np.zeros((tokens, n_in)), np.zeros((tokens, n_in))
+    size = np.zeros((tokens, n_in))
+    for e in range(len(wg)):
+        t, s = np.nonzero(index == first + e)
+        if not len(t):
+            continue
+
+        def affine(w, sc):
+            z, err = _product(x[t], w[e].T)
+            return (z, err) if sc is None else \
+                (z * sc[e], (err + _E * np.abs(z)) * np.abs(sc[e]))
+
+        sg, su, sd = scales or (None,) * 3
+        (g, eg), (u, eu) = affine(wg, sg), affine(wu, su)
+        a, _ = act(g, act_name)
+        ea = eg * 1.13 + _ACT * (1 + np.abs(g))
+        h = a * u
+        eh = ea * np.abs(u) + np.abs(a) * eu + ea * eu + _E * np.abs(h)
+        # as it is held
+        eh = eh + (2.0 ** -24 if out == "float32" else 2.0 ** -16) \
+            * (np.abs(h) + eh) + TINY["bfloat16"]
+        o = h @ wd[e].T
+        big = (np.abs(h) + eh) @ np.abs(wd[e].T)
+        eo = (parts * hidden + 3) * _E * big + eh @ np.abs(wd[e].T)
+        if sd is not None:
+            o, big, eo = (v * np.abs(sd[e]) if v is not o else v * sd[e]
+                          for v in (o, big, eo))
+        w = weight[t, s][:, None]
+        np.add.at(y, t, w * o)
+        np.add.at(size, t, np.abs(w) * big)
+        np.add.at(ey, t, np.abs(w) * (eo + (_ACT if chosen else 0)
+                                      * (np.abs(o) + eo)))
+    # each expert's part in up to 8 pieces, times two factors
+    ey += (9 * top + 8) * _E * size
+    if residual is not None:
+        y = y + residual
+        ey = ey + _E * np.abs(y)
+    return _stored(y, ey, out)

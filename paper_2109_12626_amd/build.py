@@ -25,7 +25,9 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-result",
 ]
 PRODUCT_SOURCES = ["products_bf16.hip", "products_f16.hip",
-                   "products_f32.hip", "products_int8.hip"]
+                   "products_f32.hip", "products_int8.hip",
+                   "moe_route.hip", "moe_bf16.hip", "moe_f16.hip",
+                   "moe_f32.hip"]
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra",
               "-Wno-unused-parameter", "-D__HIP_PLATFORM_AMD__"]
 
@@ -89,7 +91,8 @@ def build(verbose=True, out=None, defines=(), host_sanitize=False):
     hipcc = os.path.join(ROCM, "bin", "hipcc")
     objs = []
     san = ["-fsanitize=address,undefined", "-g"] if host_sanitize else []
-    for src in ("plan.cpp", "api.cpp", "products_api.cpp", "int8_api.cpp"):
+    for src in ("plan.cpp", "api.cpp", "products_api.cpp", "int8_api.cpp",
+                "moe_api.cpp"):
         obj = os.path.join(build_dir, src + ".o")
         _run(["g++"] + HOST_FLAGS + san + inc +
              ["-c", os.path.join(CSRC, src), "-o", obj])

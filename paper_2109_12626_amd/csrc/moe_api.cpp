@@ -1,0 +1,253 @@
+// C entry points of the mixture-of-experts layer.
+#include "moe.hpp"
+#include "products_host.hpp"
+
+namespace {
+
+namespace moe = dpar::moe;
+
+struct Options {
+  dpar_moe_t o;              // with distances filled in
+  Type t, w;
+  size_t e, ew, eo, all;     // element sizes; experts of all ranks
+};
+
+int check_moe(const char* call, int p, const dpar_moe_t* opt, Options* c) {
+  dpar::set_error(0, "");
+  if (p < 1) return fail(DPAR_ERR_INVALID_ARG, "%s: p must be >= 1", call);
+  if (!opt) return fail(DPAR_ERR_INVALID_ARG, "%s: null options", call);
+  dpar_moe_t& o = c->o = *opt;
+  switch (o.dtype) {
+    case DPAR_FLOAT32: c->t = Type::F32; break;
+    case DPAR_BFLOAT16: c->t = Type::BF16; break;
+    case DPAR_FLOAT16: c->t = Type::F16; break;
+    default:
+      return fail(DPAR_ERR_UNSUPPORTED, "%s: dtype %d", call, (int)o.dtype);
+  }
+  c->w = c->t;
+  if (o.weight_dtype == DPAR_INT8 && c->t != Type::F32)
+    c->w = Type::I8;
+  else if (o.weight_dtype != o.dtype)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: weight_dtype %d with dtype %d", call,
+                (int)o.weight_dtype, (int)o.dtype);
+  if (o.out_dtype != o.dtype && o.out_dtype != DPAR_FLOAT32)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: out_dtype %d with dtype %d", call,
+                (int)o.out_dtype, (int)o.dtype);
+  if ((int)o.act < DPAR_ACT_NONE || (int)o.act > DPAR_ACT_SILU)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: unknown activation %d", call,
+                (int)o.act);
+  if ((int)o.route < DPAR_ROUTE_SOFTMAX || (int)o.route > DPAR_ROUTE_SIGMOID)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: unknown route %d", call,
+                (int)o.route);
+  if (o.experts < 1 || o.top < 1)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: no experts, or none chosen", call);
+  if (o.tokens > (size_t)moe::kTokens || o.top > moe::kTop ||
+      o.experts > (size_t)moe::kExperts ||
+      o.experts * p > (size_t)moe::kExperts)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: %zu tokens, top %d, %d x %zu "
+                "experts: beyond %d, %d, %d", call, o.tokens, o.top, p,
+                o.experts, moe::kTokens, moe::kTop, moe::kExperts);
+  c->all = o.experts * p;
+  if ((size_t)o.top > c->all)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: %d chosen of %zu experts", call,
+                o.top, c->all);
+  if (o.in >= kMost || o.hidden >= kMost)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: a size beyond 2^31", call);
+  c->e = size_of(c->t), c->ew = size_of(c->w);
+  c->eo = o.out_dtype == DPAR_FLOAT32 ? 4 : 2;
+  if (!o.ldx || o.tokens <= 1) o.ldx = o.in;
+  if (!o.ldl || o.tokens <= 1) o.ldl = c->all;
+  if (!o.ldy || o.tokens <= 1) o.ldy = o.in;
+  if (!o.ldr || o.tokens <= 1) o.ldr = o.in;
+  if (!o.ldw || o.hidden <= 1) o.ldw = o.in;
+  if (!o.ldd || o.in <= 1) o.ldd = o.hidden;
+  for (size_t v : {o.ldx, o.ldl, o.ldw, o.ldd, o.ldy, o.ldr, o.xw, o.xd})
+    if (v > kMostPitch)
+      return fail(DPAR_ERR_UNSUPPORTED, "%s: a distance beyond 2^38", call);
+  if (o.ldw < o.in || o.ldd < o.hidden)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: rows of the weights overlap", call);
+  if ((o.hidden && o.ldw > kMostBytes / o.hidden) ||
+      (o.in && o.ldd > kMostBytes / o.in))
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: weights of 2^48 bytes or more",
+                call);
+  if (!o.xw || o.experts <= 1) o.xw = o.hidden * o.ldw;
+  if (!o.xd || o.experts <= 1) o.xd = o.in * o.ldd;
+  return DPAR_SUCCESS;
+}
+
+// A rank's experts that can be chosen.
+int most_of(const dpar_moe_t& o) {
+  return (int)std::min(o.experts, o.tokens * (size_t)o.top);
+}
+
+// 16-bit parts of a hidden value.
+int planes_of(const Options& c) {
+  return c.t == Type::F32 ? 2 : c.eo == 4 ? 3 : 2;
+}
+
+moe::Layout layout_of(const Options& c) {
+  const size_t pairs = c.o.tokens * c.o.top;
+  auto up = [](size_t v) { return (v + 127) / 128 * 128; };
+  moe::Layout l;
+  l.records = 128;
+  l.pairs = l.records + up((size_t)most_of(c.o) * sizeof(moe::Record));
+  l.weights = l.pairs + up(pairs * 4);
+  l.hidden = l.weights + up(pairs * 4);
+  // (an fp32 value: as two parts of 16 bits)
+  l.bytes = l.hidden + up(pairs * ((c.o.hidden + 7) / 8 * 8) * 2 *
+                          planes_of(c));
+  return l;
+}
+
+// Wavefronts per workgroup for a matrix of `chunks` chunks of 512 bytes a row,
+// with n workgroups that have work.
+int waves_of(size_t n, size_t chunks, int cus) {
+  int w = 2;
+  while (w < 8 && chunks >= (size_t)w * 2 && n * w < (size_t)cus * 8) w *= 2;
+  return w;
+}
+
+int moe_impl(const void* const* x, const void* const* logits,
+             const void* const* wg, const void* const* wu,
+             const void* const* wd, const void* const* sg,
+             const void* const* su, const void* const* sd,
+             const void* const* residual, void* const* y, void* const* index,
+             void* const* weight, int p, const dpar_moe_t* opt, void* ws,
+             size_t bytes, hipStream_t stream) {
+  const char* call = "dpar_moe";
+  Options c;
+  int rc = check_moe(call, p, opt, &c);
+  if (rc) return rc;
+  const dpar_moe_t& o = c.o;
+  const bool eight = c.w == Type::I8, given = !logits;
+  if (eight ? !sg || !su || !sd : sg || su || sd)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: scales belong to 8-bit weights, all "
+                "three", call);
+  if (given && (!index || !weight))
+    return fail(DPAR_ERR_INVALID_ARG, "%s: neither logits nor a choice", call);
+  const size_t n = o.experts, span_w = o.hidden ? (o.hidden - 1) * o.ldw + o.in
+                                                : 0,
+               span_d = o.in ? (o.in - 1) * o.ldd + o.hidden : 0;
+  const size_t top = o.top;
+  Mat m[] = {
+      {"x", x, o.tokens, o.in, o.ldx, c.e, false, false, true},
+      {"logits", logits, o.tokens, c.all, o.ldl, 4, false, false, !given},
+      {"wg", wg, n, o.in ? span_w : 0, o.xw, c.ew, false, false, true},
+      {"wu", wu, n, o.in ? span_w : 0, o.xw, c.ew, false, false, true},
+      {"wd", wd, n, o.hidden ? span_d : 0, o.xd, c.ew, false, false, true},
+      {"sg", sg, 1, n * o.hidden, n * o.hidden, 4, false, false, eight},
+      {"su", su, 1, n * o.hidden, n * o.hidden, 4, false, false, eight},
+      {"sd", sd, 1, n * o.in, n * o.in, 4, false, false, eight},
+      {"residual", residual, o.tokens, o.in, o.ldr, c.eo, false, true,
+       residual != nullptr},
+      {"y", in_array(y), o.tokens, o.in, o.ldy, c.eo, true, false, true},
+      {"index", in_array(index), o.tokens, top, top, 4, !given, !given,
+       index != nullptr},
+      {"weight", in_array(weight), o.tokens, top, top, 4, !given, !given,
+       weight != nullptr}};
+  constexpr int kMats = 12;
+  m[9].twin[0] = residual;
+  if ((rc = check_mats(m, kMats, p, call))) return rc;
+  const moe::Layout at = layout_of(c);
+  if (!o.tokens) return DPAR_SUCCESS;
+  if (!ws || bytes < at.bytes * p)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: workspace of %zu bytes, %zu needed",
+                call, ws ? bytes : 0, at.bytes * p);
+  if ((uintptr_t)ws & 15)
+    return fail(DPAR_ERR_INVALID_ARG, "%s: workspace not on 16 bytes", call);
+  const uintptr_t lo = (uintptr_t)ws, hi = lo + at.bytes * p;
+  if (hi >> 48 || hi < lo)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: workspace above 2^48", call);
+  for (int k = 0; k < kMats; ++k)
+    for (int i = 0; i < p && m[k].used; ++i)
+      if (touches(m[k], i, lo, hi))
+        return fail(DPAR_ERR_ALIAS, "%s: workspace overlaps %s of rank %d",
+                    call, m[k].name, i);
+
+  const int cus = cu_count();
+  const int per = (p + (p + moe::kRanks - 1) / moe::kRanks - 1) /
+                  ((p + moe::kRanks - 1) / moe::kRanks);
+  moe::Args a = {};
+  a.in = o.in, a.hidden = o.hidden;
+  a.ldx = o.ldx, a.ldl = o.ldl, a.ldw = o.ldw, a.ldd = o.ldd;
+  a.xw = o.xw, a.xd = o.xd, a.ldy = o.ldy, a.ldr = o.ldr;
+  a.work = (char*)ws, a.at = at;
+  a.scale = o.weight_scale;
+  a.tokens = (int)o.tokens, a.experts = (int)o.experts, a.top = o.top;
+  a.all = p;
+  a.act = o.act, a.route = o.route, a.normalize = o.normalize != 0;
+  a.given = given, a.out32 = c.eo == 4, a.planes = planes_of(c);
+  a.most = most_of(o);
+  // weights of whole aligned pieces, 16 rows of them within 32-bit offsets
+  auto fast = [&](size_t cols, size_t ld, size_t far, int k0, int k1) {
+    uintptr_t bits = cols * c.ew | ld * c.ew | (n > 1 ? far * c.ew : 0);
+    for (int k = k0; k < k1; ++k)
+      for (int i = 0; i < p; ++i) bits |= (uintptr_t)m[k].at[i];
+    return bits % 16 == 0 && ld < kFastPitch;
+  };
+  a.fast[0] = fast(o.in, o.ldw, o.xw, 2, 4);
+  a.fast[1] = fast(o.hidden, o.ldd, o.xd, 4, 5);
+  const size_t chosen = std::min(c.all, o.tokens * top);
+  a.waves[0] = waves_of((o.hidden + 15) / 16 * chosen, o.in * c.ew / 512, cus);
+  a.waves[1] = (o.in + 15) / 16 * std::min((size_t)per, chosen) <
+                       (size_t)cus * 2 ? 8 : 4;
+  const size_t groups = std::max((o.hidden + 15) / 16 * a.most,
+                                 (o.in + 15) / 16) * per;
+  if (groups > 0xffffffffu / 512)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: %zu workgroups in a launch", call,
+                groups);
+  for (int r0 = 0; r0 < p; r0 += per) {
+    a.ranks = std::min(per, p - r0), a.first = r0;
+    for (int k = 0; k < a.ranks; ++k) {
+      const int i = r0 + k;
+      a.x[k] = m[0].rank(i);
+      a.logits[k] = (const float*)m[1].rank(i);
+      for (int j = 0; j < 3; ++j) {
+        a.w[j][k] = m[2 + j].rank(i);
+        a.s[j][k] = (const float*)m[5 + j].rank(i);
+      }
+      a.r[k] = m[8].rank(i);
+      a.y[k] = (void*)m[9].rank(i);
+      a.index[k] = (int*)m[10].rank(i);
+      a.weight[k] = (float*)m[11].rank(i);
+    }
+    if ((rc = launched(call, moe::launch_route(a, stream)))) return rc;
+    if (!o.in) continue;
+    const hipError_t e = c.t == Type::BF16  ? moe::launch_bf16(eight, a, stream)
+                         : c.t == Type::F16 ? moe::launch_f16(eight, a, stream)
+                                            : moe::launch_f32(a, stream);
+    if ((rc = launched(call, e))) return rc;
+  }
+  return DPAR_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dpar_moe(const void* const* x, const void* const* logits,
+             const void* const* wg, const void* const* wu,
+             const void* const* wd, const void* const* sg,
+             const void* const* su, const void* const* sd,
+             const void* const* residual, void* const* y, void* const* index,
+             void* const* weight, int p, const dpar_moe_t* opt,
+             void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return guarded("dpar_moe", [&] {
+    return moe_impl(x, logits, wg, wu, wd, sg, su, sd, residual, y, index,
+                    weight, p, opt, workspace, workspace_bytes, stream);
+  });
+}
+
+int dpar_moe_workspace(int p, const dpar_moe_t* opt, size_t* bytes) {
+  return guarded("dpar_moe_workspace", [&] {
+    const char* call = "dpar_moe_workspace";
+    Options c;
+    const int rc = check_moe(call, p, opt, &c);
+    if (rc) return rc;
+    if (!bytes) return fail(DPAR_ERR_INVALID_ARG, "%s: null result", call);
+    *bytes = c.o.tokens ? layout_of(c).bytes * p : 0;
+    return (int)DPAR_SUCCESS;
+  });
+}
+
+}  // extern "C"

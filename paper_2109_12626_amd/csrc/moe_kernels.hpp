@@ -1,0 +1,712 @@
+// The mixture-of-experts layer for a few tokens on gfx950: the choice of
+// experts, both gated projections of the chosen ones, and their second products
+// summed by token.  Every matrix of a chosen expert is read once, and that read
+// is what bounds the layer: 16 rows of a matrix at a time go to the matrix
+// cores, the tokens that chose it are the columns.
+#pragma once
+
+#include "moe.hpp"
+#include "products_kernels.hpp"
+
+namespace dpar {
+namespace moe {
+namespace {
+
+using namespace products;
+using MoeArgs = moe::Args;
+using GivenMoe = const __attribute__((address_space(4))) MoeArgs;
+
+__device__ inline char* work_of(GivenMoe& a, int rank) {
+  return a.work + (size_t)(a.first + rank) * a.at.bytes;
+}
+
+// ---------------------------------------------------------------- types
+
+// Values as the upper halves of 32-bit floats, two of them in a register.
+__device__ inline int upper_halves(float even, float odd) {
+  return (int)__builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, odd),
+                                    __builtin_bit_cast(uint32_t, even),
+                                    0x07060302u);
+}
+__device__ inline float from_byte(int word, int k) {
+  return (float)(signed char)(word >> (8 * k));
+}
+
+// Weights of type W beside activations of type X.  A piece is 16 bytes of
+// weights, VB values; a lane group's activations for it are NX 16-byte pieces.
+template <Type W, Type X> struct Mix {
+  using V = typename Elem<W>::V;
+  using XV = typename Elem<X>::V;
+  static constexpr int VB = 16 / (int)sizeof(V);
+  static constexpr int NX = VB * (int)sizeof(XV) / 16;
+  // hidden values: 32-bit ones as they are, else P parts of 16 bits
+  static constexpr bool kWhole = X == Type::F32;
+  static constexpr int parts(int P) { return kWhole ? 1 : P * VB / 8; }
+
+  static __device__ f32x4 up(i32x4 w, const i32x4 (&x)[NX], f32x4 c) {
+    if constexpr (W != Type::I8) {
+      return Elem<X>::mma(w, x[0], c);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        i32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int word = h * 2 + k / 2;
+          const int bytes = w[word];
+          const float even = from_byte(bytes, k % 2 * 2),
+                      odd = from_byte(bytes, k % 2 * 2 + 1);
+          if constexpr (X == Type::BF16) {
+            v[k] = upper_halves(even, odd);
+          } else {
+            const auto two = __builtin_amdgcn_cvt_pkrtz(even, odd);
+            v[k] = __builtin_bit_cast(int, two);
+          }
+        }
+        c = Elem<X>::mma(v, x[h], c);
+      }
+      return c;
+    }
+  }
+
+  // c += weights by hidden values, P parts of 8 values each: every weight as
+  // one or two bfloat16 parts, which hold it exactly.
+  template <int P, int N>
+  static __device__ f32x4 down(i32x4 w, const i32x4 (&h)[N], f32x4 c) {
+    static_assert(N == parts(P));
+    if constexpr (kWhole) {
+      return Elem<Type::F32>::mma(w, h[0], c);
+    } else if constexpr (W == Type::BF16) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) c = Elem<Type::BF16>::mma(w, h[p], c);
+      return c;
+    } else if constexpr (W == Type::F16) {
+      const f16x8 f = __builtin_bit_cast(f16x8, w);
+      i32x4 hi, lo;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float a = (float)f[2 * k], b = (float)f[2 * k + 1];
+        const int both = upper_halves(a, b);
+        hi[k] = both;
+        const float ah = __builtin_bit_cast(float, both << 16),
+                    bh = __builtin_bit_cast(float, both & (int)0xffff0000);
+        lo[k] = upper_halves(a - ah, b - bh);
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        c = Elem<Type::BF16>::mma(hi, h[p], c);
+        c = Elem<Type::BF16>::mma(lo, h[p], c);
+      }
+      return c;
+    } else {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        i32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int bytes = w[g * 2 + k / 2];
+          v[k] = upper_halves(from_byte(bytes, k % 2 * 2),
+                              from_byte(bytes, k % 2 * 2 + 1));
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          c = Elem<Type::BF16>::mma(v, h[g * P + p], c);
+      }
+      return c;
+    }
+  }
+};
+
+// A 32-bit hidden value as bfloat16 parts: the upper half, the rest's upper
+// half, and what is left, which together are the value (two parts: the second
+// one rounded, 2^-16 of the value off at most).  Infinities and NaN are the
+// first part's alone.
+template <int P>
+__device__ inline void split(float v, unsigned short (&part)[P]) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  uint32_t hi = b & 0xffff0000u;
+  const bool fine = (b & 0x7f800000u) != 0x7f800000u;
+  if (!fine && (b & 0x7fffffu)) hi |= 0x00400000u;       // a NaN stays one
+  part[0] = (unsigned short)(hi >> 16);
+  float rest = fine ? v - __builtin_bit_cast(float, hi) : 0.f;
+#pragma unroll
+  for (int p = 1; p < P; ++p) {
+    if (p == P - 1) {
+      part[p] = __builtin_bit_cast(unsigned short, (__bf16)rest);
+    } else {
+      const uint32_t r = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
+      part[p] = (unsigned short)(r >> 16);
+      rest -= __builtin_bit_cast(float, r);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- streams
+
+constexpr int kRow = 512, kChunk = 16 * kRow;      // bytes
+
+// 16 rows of a matrix, `left` of them there, from memory to a wavefront's LDS in
+// chunks of 512 bytes a row, pieces exchanged by the row (as FewFast does).
+template <typename V>
+struct Stream {
+  static constexpr int VB = 16 / (int)sizeof(V), KC = kRow / (int)sizeof(V);
+
+  // Chunk c (of a contraction of nc values) of the rows from `base` on.
+  static __device__ void ask(const char* base, size_t ld, int left, size_t nc,
+                             unsigned c, uint32_t lds, int lane) {
+    const int slot = lane & 31;
+    const char* b = uniform(base + (size_t)c * kRow);
+    if ((size_t)(c + 1) * KC <= nc) {
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const int row = h * 2 + (lane >> 5);
+        const int at = row < left ? row : left - 1;
+        dma16_once(uniform(lds + h * 1024), b,
+                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 7)) * 16);
+      }
+    } else {
+      // the last chunk: zeros past the contraction's end
+#pragma unroll 1
+      for (int h = 0; h < 8; ++h) {
+        const int row = h * 2 + (lane >> 5);
+        const int at = row < left ? row : left - 1;
+        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * VB;
+        dma16_at(uniform(lds + h * 1024),
+                 k < nc ? base + (at * ld + k) * sizeof(V)
+                        : (const char*)&g_zero);
+      }
+    }
+  }
+  // Step u's piece of row r for lane group q.
+  static __device__ i32x4 take(LDS char* src, int u, int r, int q) {
+    return *(LDS i32x4*)(src + r * kRow + (((u * 4 + q) ^ (r & 7)) * 16));
+  }
+};
+
+// NX pieces of a row of activations of which `left` values are left (WHOLE: a
+// multiple of a piece's); rows may start anywhere.
+template <bool WHOLE, typename XV, int NX>
+__device__ inline void fetch_row(const XV* x, long left, i32x4 (&v)[NX]) {
+  constexpr int E = 16 / (int)sizeof(XV);
+#pragma unroll
+  for (int n = 0; n < NX; ++n) {
+    if constexpr (WHOLE)
+      v[n] = n * E < left ? load_whole<false>(x + n * E) : i32x4{0, 0, 0, 0};
+    else
+      v[n] = load_piece<XV>(x + n * E, left - n * E);
+  }
+}
+
+// ---------------------------------------------------------------- gate and up
+
+// h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 columns
+// (16 rows of either matrix) of one chosen expert, its S wavefronts a part of
+// the contraction each; up to MT tiles of 16 pairs at a time.
+template <Type W, Type X, bool FAST, int MT, int S>
+struct Up {
+  using M = Mix<W, X>;
+  using V = typename M::V;
+  using XV = typename M::XV;
+  using St = Stream<V>;
+  static constexpr int VB = M::VB, NX = M::NX, K = 4 * VB;   // per step
+  static constexpr int U = FAST ? kRow / 64 : 4;             // steps a chunk
+  static constexpr int KC = U * K;
+  static constexpr int kLds =
+      FAST ? S * 2 * kChunk : S * MT * 2 * 1024;
+  static_assert(kLds >= S * MT * 2 * 1024);
+
+  static __device__ void run(GivenMoe& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const unsigned tiles = (unsigned)((a.hidden + 15) / 16);
+    const unsigned id = uniform(blockIdx.x / tiles);
+    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 16;
+    const int rank = uniform(id / a.most), at = uniform(id % a.most);
+    char* const work = work_of(a, rank);
+    if (at >= *(const int*)work) return;
+    const Record rec = ((const Record*)(work + a.at.records))[at];
+    const int expert = uniform(rec.expert), count = uniform(rec.count);
+    const int* list = (const int*)(work + a.at.pairs) + uniform(rec.first);
+    const size_t origin =
+        ((size_t)expert * a.xw + j0 * a.ldw) * sizeof(V);
+    const char* base[2] = {(const char*)a.w[0][rank] + origin,
+                           (const char*)a.w[1][rank] + origin};
+    const int left =
+        a.hidden - j0 < 16 ? (int)(a.hidden - j0) : 16;
+
+    const unsigned chunks = (unsigned)((a.in + KC - 1) / KC);
+    const unsigned c0 = (unsigned)((uint64_t)chunks * wave / S),
+                   c1 = (unsigned)((uint64_t)chunks * (wave + 1) / S);
+    for (int i0 = 0; i0 < count; i0 += MT * 16) {
+      const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
+      const XV* x[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        int i = m * 16 + r;
+        if (i >= here) i = here - 1;
+        x[m] = (const XV*)a.x[rank] +
+               (size_t)(list[i0 + i] / a.top) * a.ldx + q * VB;
+      }
+      f32x4 acc[MT][2] = {};
+      if constexpr (FAST)
+        stream(a, base, left, c0, c1, lds, wave, lane, x, here, acc);
+      else
+        fetch(a, base, left, c0, c1, lane, x, here, acc);
+      finish(a, rank, expert, list + i0, here, j0, lds, wave, lane, acc, work);
+      if (i0 + MT * 16 < count) __syncthreads();
+    }
+  }
+
+  static __device__ void stream(GivenMoe& a, const char* const (&base)[2],
+                                int left, unsigned c0, unsigned c1,
+                                LDS char* lds, int wave, int lane,
+                                const XV* const (&x)[MT], int here,
+                                f32x4 (&acc)[MT][2]) {
+    const int r = lane & 15, q = lane >> 4;
+    const uint32_t mine =
+        uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
+    LDS char* const src = lds + wave * (2 * kChunk);
+    if (c0 < c1) St::ask(base[0], a.ldw, left, a.in, c0, mine, lane);
+#pragma unroll 1
+    for (unsigned c = c0; c < c1; ++c) {
+      i32x4 fx[MT][U][NX];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        if (m == 0 || m * 16 < here) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const size_t k = (size_t)c * KC + u * K;
+            fetch_row<true>(x[m] + k, (long)a.in - (long)(k + q * VB),
+                            fx[m][u]);
+          }
+        }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        landed<0>();                      // (x too)
+        if (n == 0)
+          St::ask(base[1], a.ldw, left, a.in, c, mine + kChunk, lane);
+        else if (c + 1 < c1)
+          St::ask(base[0], a.ldw, left, a.in, c + 1, mine, lane);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const i32x4 w = St::take(src + n * kChunk, u, r, q);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            if (m == 0 || m * 16 < here)
+              acc[m][n] = M::up(w, fx[m][u], acc[m][n]);
+        }
+      }
+    }
+    if (S > 1) __syncthreads();
+  }
+
+  // The same for rows of any alignment, by way of registers.
+  static __device__ void fetch(GivenMoe& a, const char* const (&base)[2],
+                               int left, unsigned c0, unsigned c1, int lane,
+                               const XV* const (&x)[MT], int here,
+                               f32x4 (&acc)[MT][2]) {
+    const int r = lane & 15, q = lane >> 4, row = r < left ? r : left - 1;
+    const V* w[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+      w[n] = (const V*)base[n] + (size_t)row * a.ldw + q * VB;
+#pragma unroll 1
+    for (unsigned c = c0; c < c1; ++c) {
+      i32x4 fw[U][2], fx[MT][U][NX];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t k = (size_t)c * KC + u * K;
+        const long rest = (long)a.in - (long)(k + q * VB);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) fw[u][n] = load_piece<V>(w[n] + k, rest);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          if (m == 0 || m * 16 < here)
+            fetch_row<false>(x[m] + k, rest, fx[m][u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            if (m == 0 || m * 16 < here)
+              acc[m][n] = M::up(fw[u][n], fx[m][u], acc[m][n]);
+    }
+  }
+
+  // Adds the wavefronts' sums in their order; tile m is finished by wavefront m
+  // % S: h of 16 pairs and 16 columns, zeros past the last column.
+  static __device__ void finish(GivenMoe& a, int rank, int expert,
+                                const int* list, int here, size_t j0,
+                                LDS char* lds, int wave, int lane,
+                                const f32x4 (&acc)[MT][2], char* work) {
+    const int r = lane & 15, q = lane >> 4;
+    auto part = (f32x4(LDS*)[MT * 2][64])lds;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) part[wave][m * 2 + n][lane] = acc[m][n];
+    if (S > 1)
+      __syncthreads();
+    else
+      in_order();
+    const size_t j = j0 + q * 4;
+#pragma unroll 1
+    for (int m = wave; m * 16 < here; m += S) {
+      f32x4 g = part[0][m * 2][lane], u = part[0][m * 2 + 1][lane];
+#pragma unroll
+      for (int k = 1; k < S; ++k) {
+        g += part[k][m * 2][lane];
+        u += part[k][m * 2 + 1][lane];
+      }
+      const int i = m * 16 + r;
+      if (i >= here) continue;
+      float h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float gate = g[e], up = u[e];
+        const bool there = j + e < a.hidden;
+        if constexpr (W == Type::I8) {
+          const size_t row = (size_t)expert * a.hidden + j + e;
+          if (there) {
+            gate *= a.s[0][rank][row];
+            up *= a.s[1][rank][row];
+          }
+        }
+        h[e] = there ? up : 0.f;
+        g[e] = gate;
+      }
+      with_act(a.act, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = act_of<act.value, true>(g[e]) * h[e];
+          h[e] = j + e < a.hidden ? v : 0.f;
+        }
+      });
+      const size_t pair = list[i], groups = (a.hidden + 7) / 8;
+      char* const row = work + a.at.hidden;
+      if constexpr (M::kWhole) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = h[e];
+        if (j / 8 < groups)
+          *(f32x4*)(row + (pair * groups * 8 + j) * 4) = v;
+      } else {
+        if (j / 8 >= groups) continue;
+        if (a.planes == 2)
+          put<2>(row, pair * groups + j / 8, j % 8, h);
+        else
+          put<3>(row, pair * groups + j / 8, j % 8, h);
+      }
+    }
+  }
+
+  // Four values in their group of 8: [group][part][value].
+  template <int P>
+  static __device__ void put(char* to, size_t group, size_t first,
+                             const float (&h)[4]) {
+    unsigned short part[4][P];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split<P>(h[e], part[e]);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      unsigned short v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = part[e][p];
+      long all;
+      __builtin_memcpy(&all, v, 8);
+      *(long*)(to + ((group * P + p) * 8 + first) * 2) = all;
+    }
+  }
+};
+
+// ---------------------------------------------------------------- down
+
+// y = sum of weight * (wd h) + residual: a workgroup takes 16 columns (16 rows
+// of wd) of a rank and goes over all its chosen experts, so that a token's sum
+// stays in LDS: the S wavefronts take parts of equal length of (expert,
+// contraction), and join their sums in order.
+template <Type W, Type X, bool FAST, int P, int MT, int S>
+struct Down {
+  using M = Mix<W, X>;
+  using V = typename M::V;
+  using St = Stream<V>;
+  static constexpr int VB = M::VB, K = 4 * VB;
+  static constexpr int N = M::parts(P);
+  static constexpr int U = FAST ? kRow / 64 : 4;
+  static constexpr int KC = U * K;
+  static constexpr int kBuffers = FAST ? S * 2 * kChunk : 0;
+
+  static size_t lds_bytes(int tokens) {
+    return kBuffers + (size_t)S * tokens * 64;
+  }
+
+  // What a wavefront is working at.
+  struct At {
+    Record rec;
+    unsigned unit, chunk;
+  };
+
+  static __device__ void run(GivenMoe& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int r = lane & 15, q = lane >> 4;
+    const unsigned tiles = (unsigned)((a.in + 15) / 16);
+    const int rank = uniform(blockIdx.x / tiles);
+    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 16;
+    char* const work = work_of(a, rank);
+    const int chosen = uniform(*(const int*)work);
+    const Record* records = (const Record*)(work + a.at.records);
+    const int* list = (const int*)(work + a.at.pairs);
+    const float* weights = (const float*)(work + a.at.weights);
+    const char* hidden = work + a.at.hidden;
+    const size_t groups = (a.hidden + 7) / 8;
+    const int left = a.in - j0 < 16 ? (int)(a.in - j0) : 16;
+
+    LDS float* const sums = (LDS float*)(lds + kBuffers);
+    LDS float* const mine = sums + (size_t)wave * a.tokens * 16;
+    for (int i = lane; i < a.tokens * 16; i += 64) mine[i] = 0.f;
+    in_order();
+
+    const unsigned chunks = (unsigned)((a.hidden + KC - 1) / KC);
+    const unsigned units = (unsigned)chosen * chunks;
+    const unsigned u0 = uniform((unsigned)((uint64_t)units * wave / S)),
+                   u1 = uniform((unsigned)((uint64_t)units * (wave + 1) / S));
+    const uint32_t buffer =
+        uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
+    LDS char* const src = lds + wave * (2 * kChunk);
+    auto matrix = [&](const Record& rec) {
+      return uniform((const char*)a.w[2][rank] +
+                     ((size_t)rec.expert * a.xd + j0 * a.ldd) * sizeof(V));
+    };
+    At now, next;
+    auto first = [&](At& x) {
+      x.unit = u0, x.chunk = u0 % chunks;
+      x.rec = records[u0 / chunks];
+    };
+    auto step = [&](At& x) {
+      ++x.unit;
+      if (++x.chunk == chunks) {
+        x.chunk = 0;
+        if (x.unit < u1) x.rec = records[x.unit / chunks];
+      }
+    };
+    f32x4 acc[MT] = {};
+    if (u0 < u1) {
+      first(now);
+      next = now;
+      if constexpr (FAST)
+        St::ask(matrix(now.rec), a.ldd, left, a.hidden, now.chunk, buffer,
+                lane);
+    }
+    int buf = 0;
+#pragma unroll 1
+    while (u0 < u1 && now.unit < u1) {
+      step(next);
+      const int count = uniform(now.rec.count), from = uniform(now.rec.first);
+      auto fetch = [&](int i0, int u, i32x4 (&h)[N]) {
+        int i = i0 + r;
+        if (i >= count) i = count - 1;
+        const size_t pair = list[from + i];
+        const size_t k = (size_t)now.chunk * KC + u * K + q * VB;
+        if constexpr (M::kWhole) {
+          const bool there = k < groups * 8;
+          h[0] = there ? *(const i32x4*)(hidden + (pair * groups * 8 + k) * 4)
+                       : i32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+          for (int g = 0; g < VB / 8; ++g) {
+            const size_t group = k / 8 + g;
+            const i32x4* at = (const i32x4*)hidden +
+                              (pair * groups + group) * P;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+              h[g * P + p] = group < groups ? at[p] : i32x4{0, 0, 0, 0};
+          }
+        }
+      };
+      i32x4 h[U][N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) fetch(0, u, h[u]);
+      i32x4 w[FAST ? 1 : U];
+      if constexpr (FAST) {
+        landed<0>();
+        if (next.unit < u1)
+          St::ask(matrix(next.rec), a.ldd, left, a.hidden, next.chunk,
+                  buffer + (buf ^ 1) * kChunk, lane);
+      } else {
+        const int row = r < left ? r : left - 1;
+        const V* at = (const V*)matrix(now.rec) + (size_t)row * a.ldd;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const size_t k = (size_t)now.chunk * KC + u * K + q * VB;
+          w[u] = load_piece<V>(at + k, (long)a.hidden - (long)k);
+        }
+      }
+      auto weight = [&](int u) {
+        if constexpr (FAST)
+          return St::take(src + buf * kChunk, u, r, q);
+        else
+          return w[u];
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        acc[0] = M::template down<P>(weight(u), h[u], acc[0]);
+#pragma unroll
+      for (int m = 1; m < MT; ++m)
+        if (m * 16 < count) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) fetch(m * 16, u, h[u]);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            acc[m] = M::template down<P>(weight(u), h[u], acc[m]);
+        }
+      const bool last = next.unit >= u1 || next.chunk == 0;
+      if (last) {
+        // lane (r, q): pair r, columns q * 4 ..
+        f32x4 scale = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (W == Type::I8) {
+          const float* s = a.s[2][rank] + (size_t)now.rec.expert * a.in;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            scale[e] = j0 + q * 4 + e < a.in ? s[j0 + q * 4 + e] : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          if (m * 16 + r < count) {
+            const int i = from + m * 16 + r;
+            LDS f32x4* to = (LDS f32x4*)(mine + list[i] / a.top * 16 + q * 4);
+            const float share = weights[i];
+            f32x4 v = acc[m];
+            if constexpr (W == Type::I8) v *= scale;
+            *to += v * share;
+            acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+          } else {
+            acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+        in_order();
+      }
+      now = next;
+      buf ^= 1;
+    }
+    __syncthreads();
+    using Out = typename M::XV;
+    for (int i = t; i < a.tokens * 4; i += S * 64) {
+      const int token = i / 4;
+      const size_t j = j0 + i % 4 * 4;
+      if (j >= a.in) continue;
+      f32x4 v = *(LDS f32x4*)(sums + i * 4);
+#pragma unroll
+      for (int k = 1; k < S; ++k)
+        v += *(LDS f32x4*)(sums + (size_t)k * a.tokens * 16 + i * 4);
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = v[e];
+      const long rest = (long)a.in - (long)j;
+      if (const void* res = a.r[rank]) {
+        float p[4];
+        const size_t from = (size_t)token * a.ldr + j;
+        if (a.out32)
+          fetch_vals<float, 4>((const float*)res + from, p, rest, false);
+        else
+          fetch_vals<Out, 4>((const Out*)res + from, p, rest, false);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += p[e];
+      }
+      store_out<4>(a.y[rank], (size_t)token * a.ldy + j, o, rest, a.out32,
+                   false, Out());
+    }
+  }
+};
+
+// ---------------------------------------------------------------- launches
+
+template <Type W, Type X, bool FAST, int MT, int S>
+__global__ __launch_bounds__(S * 64) void k_moe_up(MoeArgs) {
+  GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  Up<W, X, FAST, MT, S>::run(a, (LDS char*)lds);
+}
+
+template <Type W, Type X, bool FAST, int P, int MT, int S>
+__global__ __launch_bounds__(S * 64) void k_moe_down(MoeArgs) {
+  GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  Down<W, X, FAST, P, MT, S>::run(a, (LDS char*)lds);
+}
+
+template <void (*K)(MoeArgs)>
+hipError_t launch_moe(const MoeArgs& a, size_t groups, int threads,
+                      size_t bytes, hipStream_t stream) {
+  if (groups == 0) return hipSuccess;
+  if (groups * threads > 0xffffffffu) return hipErrorInvalidConfiguration;
+  if (bytes > 65536) {
+    static std::atomic<uint64_t> asked{0};     // one bit per device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(asked.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute((const void*)K,
+                              hipFuncAttributeMaxDynamicSharedMemorySize,
+                              160 * 1024);
+      if (e != hipSuccess) return e;
+      asked.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL(K, dim3((unsigned)groups), dim3(threads), bytes, stream,
+                     a);
+  return hipGetLastError();
+}
+
+template <Type W, Type X, bool FAST, int MT, int S>
+hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
+  using K = Up<W, X, FAST, MT, S>;
+  return launch_moe<k_moe_up<W, X, FAST, MT, S>>(
+      a, (a.hidden + 15) / 16 * a.most * a.ranks, S * 64, K::kLds, stream);
+}
+
+template <Type W, Type X, int MT>
+hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
+  if (!a.fast[0]) return go_up<W, X, false, 4, 4>(a, stream);
+  if (a.waves[0] == 8) return go_up<W, X, true, MT, 8>(a, stream);
+  if (a.waves[0] == 4) return go_up<W, X, true, MT, 4>(a, stream);
+  return go_up<W, X, true, MT, 2>(a, stream);
+}
+
+template <Type W, Type X, bool FAST, int P, int MT, int S>
+hipError_t go_down(const MoeArgs& a, hipStream_t stream) {
+  using K = Down<W, X, FAST, P, MT, S>;
+  return launch_moe<k_moe_down<W, X, FAST, P, MT, S>>(
+      a, (a.in + 15) / 16 * a.ranks, S * 64, K::lds_bytes(a.tokens), stream);
+}
+
+template <Type W, Type X, int P, int MT>
+hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
+  if (!a.fast[1]) return go_down<W, X, false, P, 8, 4>(a, stream);
+  if constexpr (MT == 1)
+    if (a.waves[1] == 8) return go_down<W, X, true, P, 1, 8>(a, stream);
+  return go_down<W, X, true, P, MT, 4>(a, stream);
+}
+
+template <Type W, Type X>
+hipError_t run_moe(const MoeArgs& a, hipStream_t stream) {
+  const bool few = a.tokens <= 16;
+  hipError_t e;
+  e = few ? pick_up<W, X, 1>(a, stream) : pick_up<W, X, 4>(a, stream);
+  if (e != hipSuccess) return e;
+  if constexpr (X == Type::F32) {
+    return few ? pick_down<W, X, 1, 1>(a, stream)
+               : pick_down<W, X, 1, 8>(a, stream);
+  } else {
+    if (a.planes == 2)
+      return few ? pick_down<W, X, 2, 1>(a, stream)
+                 : pick_down<W, X, 2, 8>(a, stream);
+    return few ? pick_down<W, X, 3, 1>(a, stream)
+               : pick_down<W, X, 3, 8>(a, stream);
+  }
+}
+
+}  // namespace
+}  // namespace moe
+}  // namespace dpar

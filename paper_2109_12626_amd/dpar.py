@@ -49,6 +49,8 @@ ALGS = {"dual": DPAR_ALG_DUAL_ROOT, "single": DPAR_ALG_SINGLE_TREE,
 
 ACTS = {"none": DPAR_ACT_NONE, "relu": DPAR_ACT_RELU, "gelu": DPAR_ACT_GELU,
         "gelu_tanh": DPAR_ACT_GELU_TANH, "silu": DPAR_ACT_SILU}
+DPAR_ROUTE_SOFTMAX, DPAR_ROUTE_SIGMOID = 0, 1
+ROUTES = {"softmax": DPAR_ROUTE_SOFTMAX, "sigmoid": DPAR_ROUTE_SIGMOID}
 PRODUCTS = {"linear": DPAR_LINEAR, "linear_backward": DPAR_LINEAR_BACKWARD,
             "gated": DPAR_GATED, "gated_backward": DPAR_GATED_BACKWARD}
 
@@ -94,6 +96,19 @@ class dpar_quantize_t(ctypes.Structure):
                 ("ldq", ctypes.c_size_t)]
 
 
+class dpar_moe_t(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_size_t), ("in_", ctypes.c_size_t),
+                ("hidden", ctypes.c_size_t), ("experts", ctypes.c_size_t),
+                ("top", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("weight_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
+                ("act", ctypes.c_int), ("route", ctypes.c_int),
+                ("normalize", ctypes.c_int), ("weight_scale", ctypes.c_float),
+                ("ldx", ctypes.c_size_t), ("ldl", ctypes.c_size_t),
+                ("ldw", ctypes.c_size_t), ("ldd", ctypes.c_size_t),
+                ("xw", ctypes.c_size_t), ("xd", ctypes.c_size_t),
+                ("ldy", ctypes.c_size_t), ("ldr", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -135,6 +150,9 @@ def lib():
                                            vp]
     L.dpar_linear_int8.argtypes = [vp] * 7 + tail
     L.dpar_gated_int8.argtypes = [vp] * 9 + tail
+    moe = ctypes.POINTER(dpar_moe_t)
+    L.dpar_moe.argtypes = [vp] * 12 + [i, moe, vp, sz, vp]
+    L.dpar_moe_workspace.argtypes = [i, moe, ctypes.POINTER(sz)]
     L.dpar_last_error.restype = ctypes.c_char_p
     L.dpar_last_error.argtypes = []
     L.dpar_finalize.argtypes = []
@@ -147,7 +165,8 @@ def lib():
                  "dpar_set_phase_event", "dpar_linear",
                  "dpar_linear_backward", "dpar_gated", "dpar_gated_backward",
                  "dpar_product_workspace", "dpar_quantize",
-                 "dpar_linear_int8", "dpar_gated_int8"):
+                 "dpar_linear_int8", "dpar_gated_int8", "dpar_moe",
+                 "dpar_moe_workspace"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -384,6 +403,37 @@ def dpar_gated_int8(x, sx, wg, sg, wu, su, bg, bu, h, p, opt, workspace=None,
     return _product(lib().dpar_gated_int8,
                     (x, sx, wg, sg, wu, su, bg, bu, h), p, opt, workspace,
                     workspace_bytes, stream)
+
+
+def moe_options(tokens, n_in, hidden, experts, top, dtype, weight_dtype=None,
+                out_dtype=None, act="silu", route="softmax", normalize=True,
+                weight_scale=1.0, ldx=0, ldl=0, ldw=0, ldd=0, xw=0, xd=0,
+                ldy=0, ldr=0):
+    """Sizes, types and distances of a mixture-of-experts layer (dpar_moe_t);
+    experts: of each rank."""
+    dt = _enum(DTYPES, dtype)
+    return dpar_moe_t(tokens, n_in, hidden, experts, top, dt,
+                      dt if weight_dtype is None
+                      else _enum(DTYPES, weight_dtype),
+                      dt if out_dtype is None else _enum(DTYPES, out_dtype),
+                      _enum(ACTS, act), _enum(ROUTES, route), int(normalize),
+                      weight_scale, ldx, ldl, ldw, ldd, xw, xd, ldy, ldr)
+
+
+def dpar_moe(x, logits, wg, wu, wd, sg, su, sd, residual, y, index, weight, p,
+             opt, workspace=None, workspace_bytes=0, stream=None):
+    """Sequences of p device addresses (0 where a rank has no residual, index
+    or weight), or None where optional; opt: moe_options()."""
+    return _product(lib().dpar_moe,
+                    (x, logits, wg, wu, wd, sg, su, sd, residual, y, index,
+                     weight), p, opt, workspace, workspace_bytes, stream)
+
+
+def dpar_moe_workspace(p, opt):
+    out = ctypes.c_size_t()
+    _check(lib().dpar_moe_workspace(int(p), ctypes.byref(opt),
+                                    ctypes.byref(out)))
+    return out.value
 
 
 def dpar_last_error():
@@ -647,3 +697,111 @@ def gated_int8(x, sx, wg, sg, wu, su, bg=None, bu=None, act="silu",
            c.given(bg, "bg", (c.n_out,), dtype=c.out_dtype),
            c.given(bu, "bu", (c.n_out,), dtype=c.out_dtype), _addresses(h)])
     return c.result(h)
+
+
+def moe(x, logits, wg, wu, wd, top=None, sg=None, su=None, sd=None,
+        residual=None, act="silu", route="softmax", normalize=True,
+        weight_scale=1.0, out_dtype=None, index=None, weight=None):
+    """A mixture-of-experts layer: (y, index, weight).  x [tokens, in]; wg, wu
+    [experts, hidden, in] and wd [experts, in, hidden], or [p, experts, ...]:
+    then y is [p, tokens, in], the ranks' parts; int8 weights with their scales
+    sg, su [.., experts, hidden], sd [.., experts, in].  logits [tokens,
+    experts of all ranks] with `top`, or logits None and the choice in index
+    and weight [tokens, top] (int32, float32)."""
+    flat = wg.dim() == 3
+    if wg.dim() not in (3, 4) or wu.shape != wg.shape \
+            or wd.dim() != wg.dim() or x.dim() != 2:
+        raise ValueError("x [tokens, in], weights [(p,) experts, .., ..]")
+    lead = wg.shape[:-2]
+    p, experts = (1, lead[0]) if flat else lead
+    hidden, n_in = wg.shape[-2:]
+    tokens = x.shape[0]
+    eight = wg.dtype == torch.int8
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if x.dtype not in _NAMES or out_dtype not in _NAMES \
+            or not (eight or wg.dtype == x.dtype):
+        raise ValueError(f"types {x.dtype}, {wg.dtype}, {out_dtype}")
+
+    def checked(t, name, shape, dtype):
+        if t is None:
+            raise ValueError(f"{name} is missing")
+        if tuple(t.shape) != tuple(shape) or t.dtype != dtype \
+                or t.device != x.device:
+            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on "
+                             f"{t.device}, want {dtype} {tuple(shape)}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, and this call has "
+                             "no backward pass")
+        return t
+
+    def row_distance(t, name):
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: values of a row are not consecutive")
+        far = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+        if far < t.shape[-1]:
+            raise ValueError(f"{name}: rows {far} values apart overlap")
+        return far
+
+    def each(t):                       # the same for all ranks
+        return pointers([t.data_ptr()] * p)
+
+    def split(t):
+        return each(t) if flat else rows(t)
+
+    def matrices(t, name, shape):
+        far = row_distance(checked(t, name, lead + shape, wg.dtype), name)
+        apart = t.stride(-3) if experts > 1 else shape[0] * far
+        if apart < (shape[0] - 1) * far + shape[1]:
+            raise ValueError(f"{name}: matrices {apart} values apart overlap")
+        return far, apart
+
+    checked(x, "x", (tokens, n_in), x.dtype)
+    at_w, at_u = (matrices(t, k, (hidden, n_in))
+                  for t, k in ((wg, "wg"), (wu, "wu")))
+    if at_w != at_u:
+        raise ValueError("wu: other distances than wg's")
+    at_d = matrices(wd, "wd", (n_in, hidden))
+    scales = []
+    for t, k, n in ((sg, "sg", hidden), (su, "su", hidden), (sd, "sd", n_in)):
+        if eight:
+            checked(t, k, lead + (n,), torch.float32)
+            if not t.is_contiguous():
+                raise ValueError(f"{k}: not contiguous")
+        elif t is not None:
+            raise ValueError(f"{k}: scales of {wg.dtype} weights")
+        scales.append(split(t) if eight else None)
+    if logits is None:
+        if index is None or weight is None or index.dim() != 2:
+            raise ValueError("neither logits nor a choice")
+        top = index.shape[1]
+        index = checked(index, "index", (tokens, top), torch.int32)
+        weight = checked(weight, "weight", (tokens, top), torch.float32)
+        index, weight = index.contiguous(), weight.contiguous()
+        choice = [each(index), each(weight)]
+        ldl = 0
+    else:
+        if index is not None or weight is not None or top is None:
+            raise ValueError("logits with `top`, or index and weight")
+        checked(logits, "logits", (tokens, p * experts), torch.float32)
+        ldl = row_distance(logits, "logits")
+        index = torch.empty(tokens, top, dtype=torch.int32, device=x.device)
+        weight = torch.empty(tokens, top, device=x.device)
+        choice = [pointers([t.data_ptr()] + [0] * (p - 1))
+                  for t in (index, weight)]
+    ldr = 0
+    if residual is not None:
+        checked(residual, "residual", (tokens, n_in) if flat else
+                (p, tokens, n_in), out_dtype)
+        ldr = row_distance(residual, "residual")
+    y = torch.empty((p, tokens, n_in), dtype=out_dtype, device=x.device)
+    opt = moe_options(tokens, n_in, hidden, experts, top, _NAMES[x.dtype],
+                      "int8" if eight else None, _NAMES[out_dtype], act, route,
+                      normalize, weight_scale, row_distance(x, "x"), ldl,
+                      at_w[0], at_d[0], at_w[1], at_d[1], n_in, ldr)
+    n = dpar_moe_workspace(p, opt)
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+    dpar_moe(each(x), None if logits is None else each(logits), split(wg),
+             split(wu), split(wd), *scales,
+             None if residual is None else split(residual), rows(y), *choice,
+             p, opt, ws, n, torch.cuda.current_stream(x.device))
+    return (y[0] if flat else y), index, weight

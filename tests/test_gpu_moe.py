@@ -1,0 +1,368 @@
+"""The mixture-of-experts layer on the GPU against the definition in 64 bits
+(oracle/products.py): the choice exactly, results element by element within the
+bound of the stated roundings."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import products as ref
+from tests._gpu import lib, need_gpu
+from tests.test_gpu_int8 import TORCH, Ranks, close, gen, np64
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(autouse=True)
+def gpu():
+    need_gpu()
+
+
+class Layer:
+    """Operands of a layer whose matrices, rows and buffers may lie apart."""
+
+    def __init__(self, p, tokens, n_in, hidden, experts, top,
+                 dtype="bfloat16", weights=None, out=None, act="silu",
+                 route="softmax", normalize=True, scale=1.0, residual=True,
+                 far=0, shift=0, seed=0):
+        d = lib()
+        g = self.g = gen(seed)
+        weights, out = weights or dtype, out or dtype
+        self.p, self.tokens, self.top, self.experts = p, tokens, top, experts
+        self.dtype, self.out, self.act = dtype, out, act
+        self.route, self.normalize, self.scale = route, normalize, scale
+        self.x = Ranks(1, tokens, n_in, dtype, far, shift).normal(g)
+        eight = weights == "int8"
+
+        def matrices(rows, cols):
+            # `far` elements between rows, `far` between matrices too
+            r = Ranks(p * experts, rows + (1 if far else 0), cols, weights,
+                      far, shift)
+            r.normal(g, max(cols, 1) ** -0.5)
+            r.per = (rows + (1 if far else 0)) * r.ld
+            r.ranks = d.pointers([
+                r.t.data_ptr() + i * experts * r.per * r.t.element_size()
+                for i in range(p)])
+            r.m = r.t[:, :rows]
+            return r
+
+        def scales(n, size):
+            r = Ranks(p, experts, n, "float32", 0, shift)
+            r.normal(g, max(size, 1) ** -0.5 / 74)
+            return r
+
+        self.wg, self.wu = matrices(hidden, n_in), matrices(hidden, n_in)
+        self.wd = matrices(n_in, hidden)
+        self.s = [scales(hidden, n_in), scales(hidden, n_in),
+                  scales(n_in, hidden)] if eight else None
+        self.r = Ranks(p, tokens, n_in, out, far, shift).normal(g) \
+            if residual else None
+        self.y = Ranks(p, tokens, n_in, out, far, shift)
+        self.logits = Ranks(1, tokens, p * experts, "float32", far,
+                            shift).normal(g, 2.0)
+        self.opt = d.moe_options(
+            tokens, n_in, hidden, experts, top, dtype, weights, out, act,
+            route, normalize, scale, self.x.ld, self.logits.ld, self.wg.ld,
+            self.wd.ld, self.wg.per, self.wd.per, self.y.ld, n_in + far)
+        n = d.dpar_moe_workspace(p, self.opt)
+        self.ws = torch.full((max(n, 16),), 0xff, dtype=torch.uint8,
+                             device="cuda")
+        self.index = torch.full((tokens, top), 99, dtype=torch.int32,
+                                device="cuda")
+        self.weight = torch.full((tokens, top), 99.0, device="cuda")
+
+    def run(self, given=None, stream=None, y=None):
+        """given: (index, weight), the choice as an input."""
+        d, p = lib(), self.p
+
+        def every(t):
+            return d.pointers([t.data_ptr()] * p)
+
+        if given is None:
+            choice = [d.pointers([t.data_ptr()] + [0] * (p - 1))
+                      for t in (self.index, self.weight)]
+        else:
+            self.index, self.weight = given
+            choice = [every(t) for t in given]
+        d.dpar_moe(every(self.x.t), None if given else every(self.logits.t),
+                   self.wg.ranks, self.wu.ranks, self.wd.ranks,
+                   *([t.at for t in self.s] if self.s else [None] * 3),
+                   self.r.at if self.r else None, y or self.y.at, *choice, p,
+                   self.opt, self.ws, self.ws.numel(),
+                   stream or torch.cuda.current_stream())
+
+    def check(self, given=None):
+        if given is None:
+            index, weight = ref.choice(np64(self.logits.t[0]), self.top,
+                                       self.route, self.normalize, self.scale)
+            np.testing.assert_array_equal(self.index.cpu().numpy(), index)
+            np.testing.assert_allclose(np64(self.weight), weight,
+                                       rtol=2.0 ** -20, atol=2.0 ** -126)
+        else:
+            index, weight = given[0].cpu().numpy(), np64(given[1])
+        n = self.experts
+        for i in range(self.p):
+            part = slice(i * n, (i + 1) * n)
+            want = ref.moe(
+                np64(self.x.t[0]), index, weight, np64(self.wg.m[part]),
+                np64(self.wu.m[part]), np64(self.wd.m[part]),
+                [np64(t.t[i]) for t in self.s] if self.s else None,
+                np64(self.r.t[i]) if self.r else None, self.act, self.dtype,
+                self.out, i * n, given is None)
+            close(self.y.t[i], want, f"rank {i}")
+        assert self.y.gaps_untouched()
+
+
+def run_moe(*args, edit=None, **kw):
+    layer = Layer(*args, **kw)
+    if edit:
+        edit(layer.logits.t[0])
+    layer.run()
+    layer.check()
+    return layer
+
+
+TYPES = [("bfloat16", "bfloat16", "bfloat16"),
+         ("bfloat16", "bfloat16", "float32"),
+         ("float16", "float16", "float16"), ("float16", "float16", "float32"),
+         ("float32", "float32", "float32"), ("bfloat16", "int8", "bfloat16"),
+         ("bfloat16", "int8", "float32"), ("float16", "int8", "float16"),
+         ("float16", "int8", "float32")]
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.mark.parametrize("dtype,weights,out", TYPES)
+@pytest.mark.parametrize("p,tokens,n_in,hidden,experts,top", [
+    (1, 1, 64, 48, 4, 2), (1, 1, 1024, 528, 9, 3), (2, 5, 256, 64, 3, 4),
+    (1, 16, 512, 128, 8, 2), (1, 17, 272, 80, 5, 5), (4, 33, 144, 176, 2, 3),
+    (1, 128, 128, 96, 3, 2), (1, 100, 64, 32, 70, 6)])
+def test_layer(dtype, weights, out, p, tokens, n_in, hidden, experts, top):
+    run_moe(p, tokens, n_in, hidden, experts, top, dtype, weights, out,
+            act=ACTS[tokens % 5], route=["softmax", "sigmoid"][top % 2],
+            normalize=hidden % 32 == 0, scale=[1.0, 2.5][p % 2],
+            residual=tokens % 2 == 1, seed=tokens)
+
+
+@pytest.mark.parametrize("dtype,weights,out", TYPES)
+@pytest.mark.parametrize("tokens,n_in,hidden,far,shift", [
+    (1, 1, 1, 0, 0), (3, 33, 15, 0, 0), (20, 1001, 501, 0, 0),
+    (2, 64, 48, 16, 0), (2, 64, 48, 5, 0), (2, 64, 48, 0, 1),
+    (40, 65, 64, 0, 0), (40, 64, 65, 0, 0), (7, 2064, 1040, 0, 0)])
+def test_odd_sizes_distances_and_alignment(dtype, weights, out, tokens, n_in,
+                                           hidden, far, shift):
+    run_moe(2, tokens, n_in, hidden, 3, 2, dtype, weights, out, far=far,
+            shift=shift, seed=n_in)
+
+
+@pytest.mark.parametrize("tokens", [1, 16, 64, 65, 128])
+@pytest.mark.parametrize("dtype,weights", [("bfloat16", "bfloat16"),
+                                           ("float32", "float32"),
+                                           ("float16", "int8")])
+@pytest.mark.parametrize("n_in,hidden", [(528, 272), (101, 67)])
+def test_every_token_in_one_expert(tokens, dtype, weights, n_in, hidden):
+    def one(logits):
+        logits[:] = -INF
+        logits[:, 2] = torch.arange(logits.shape[0])
+
+    layer = run_moe(1, tokens, n_in, hidden, 4, 3, dtype, weights, edit=one)
+    assert (layer.index == torch.tensor([2, -1, -1], device="cuda")).all()
+
+
+@pytest.mark.parametrize("route", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("normalize", [False, True])
+def test_masked_logits_ties_and_empty_tokens(route, normalize):
+    def edit(logits):
+        logits.copy_(torch.round(logits))            # ties
+        logits[1] = -INF                             # no expert
+        logits[2, 1:] = -INF                         # one
+        logits[3] = 0
+        logits[3, ::2] = -0.0                        # equal to 0
+        logits[4] = 1e30
+        logits[5] = -1e30
+        logits[6, 3] = 1e38
+        logits[7] = torch.finfo(torch.float32).min
+        logits[8, :5] = -INF
+
+    layer = run_moe(2, 11, 64, 48, 6, 4, route=route, normalize=normalize,
+                    edit=edit, seed=3)
+    assert (layer.index[1] == -1).all() and (layer.weight[1] == 0).all()
+    assert torch.equal(layer.y.t[0, 1], layer.r.t[0, 1])
+    assert layer.index[3].tolist() == [0, 1, 2, 3]
+
+
+def test_tokens_without_experts_only():
+    def edit(logits):
+        logits[:] = -INF
+
+    layer = run_moe(1, 5, 64, 48, 6, 4, residual=False, edit=edit)
+    assert (layer.y.t == 0).all()
+
+
+@pytest.mark.parametrize("route", ["softmax", "sigmoid"])
+def test_infinities_and_nan_among_logits(route):
+    layer = Layer(1, 6, 64, 48, 5, 2, route=route)
+    l = layer.logits.t[0]
+    l[1, 3] = NAN
+    l[2, 4] = INF
+    l[3, 0], l[3, 2] = -INF, NAN
+    l[4] = NAN
+    layer.run()
+    index, weight = ref.choice(np64(l), 2, route, True)
+    np.testing.assert_array_equal(layer.index.cpu().numpy(), index)
+    np.testing.assert_allclose(np64(layer.weight), weight, rtol=2.0 ** -20)
+    y = layer.y.t[0]
+    assert y[0].isfinite().all() and y[5].isfinite().all()
+    for t in (1, 3, 4):
+        assert y[t].isnan().all()
+
+
+@pytest.mark.parametrize("weights", ["bfloat16", "int8"])
+def test_values_that_are_not_finite_stay_in_their_token(weights):
+    clean = Layer(1, 20, 72, 40, 4, 2, weights=weights, seed=5)
+    clean.run()
+    for v in (INF, NAN):
+        layer = Layer(1, 20, 72, 40, 4, 2, weights=weights, seed=5)
+        layer.x.t[0, 7, 3] = v
+        layer.run()
+        keep = torch.arange(20, device="cuda") != 7
+        assert torch.equal(layer.y.t[0, keep], clean.y.t[0, keep])
+        assert not layer.y.t[0, 7].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,weights,out", TYPES)
+def test_choice_as_an_input(dtype, weights, out):
+    layer = Layer(2, 30, 128, 64, 4, 5, dtype, weights, out, seed=9)
+    g = layer.g
+    index = torch.randint(-2, 10, (30, 5), generator=g, device="cuda",
+                          dtype=torch.int32)
+    index[3] = 6                                   # the same one five times
+    index[4] = torch.tensor([1, 7, 1, 7, 1])
+    index[5] = -1
+    index[6, 0], index[6, 1] = 2 ** 31 - 1, -2 ** 31
+    weight = torch.randn(30, 5, generator=g, device="cuda")
+    held = index.clone(), weight.clone()
+    layer.run((index, weight))
+    layer.check((index, weight))
+    assert torch.equal(index, held[0]) and torch.equal(weight, held[1])
+
+
+def test_given_as_chosen():
+    a = run_moe(4, 21, 64, 80, 5, 3, seed=1)
+    b = Layer(4, 21, 64, 80, 5, 3, seed=1)
+    b.run((a.index, a.weight))
+    assert torch.equal(a.y.t, b.y.t)
+
+
+def test_largest_counts():
+    run_moe(1, 128, 32, 16, 1024, 16, seed=2)
+    run_moe(64, 9, 32, 32, 16, 16, out="float32", seed=3)
+    run_moe(33, 2, 32, 16, 1, 16, seed=4)
+
+
+@pytest.mark.parametrize("tokens,n_in,hidden", [(0, 64, 48), (3, 0, 48),
+                                                (3, 64, 0)])
+def test_empty_sizes(tokens, n_in, hidden):
+    run_moe(2, tokens, n_in, hidden, 3, 2)
+
+
+def test_wide_layers():
+    run_moe(1, 3, 8192, 48, 3, 2, seed=1)
+    run_moe(1, 3, 48, 8192, 3, 2, out="float32", seed=2)
+    run_moe(1, 20, 4100, 2052, 2, 1, "float16", seed=3)
+
+
+def test_runs_are_the_same_bits():
+    for kw in (dict(p=1, tokens=50, n_in=256, hidden=512, experts=16, top=4),
+               dict(p=1, tokens=1, n_in=1024, hidden=512, experts=16, top=4)):
+        layer = run_moe(**kw, out="float32")
+        first = layer.y.t.clone()
+        for _ in range(10):
+            layer.ws.fill_(0x5a)
+            layer.run()
+            assert torch.equal(layer.y.t, first)
+
+
+def test_result_in_place_of_the_residual():
+    a = run_moe(2, 9, 64, 48, 3, 2, seed=6)
+    b = Layer(2, 9, 64, 48, 3, 2, seed=6)
+    b.run(y=b.r.at)
+    assert torch.equal(b.r.t, a.y.t)
+
+
+def test_streams_and_a_graph():
+    layers = [Layer(1, t, 512, 256, 16, 4, seed=t) for t in (1, 24)]
+    want = []
+    for layer in layers:
+        layer.run()
+        want.append(layer.y.t.clone())
+    streams = [torch.cuda.Stream() for _ in layers]
+    for s, layer in zip(streams, layers):
+        layer.y.t.zero_()
+        s.wait_stream(torch.cuda.current_stream())
+        for _ in range(5):
+            layer.run(stream=s)
+    for s, layer, w in zip(streams, layers, want):
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(layer.y.t, w)
+    for layer in layers:
+        layer.run()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            layer.run()
+        for k in range(4):
+            layer.logits.t.copy_(layer.logits.t.roll(1, -1))
+            layer.run()
+            eager, index = layer.y.t.clone(), layer.index.clone()
+            layer.y.t.zero_()
+            graph.replay()
+            assert torch.equal(layer.y.t, eager)
+            assert torch.equal(layer.index, index)
+
+
+def test_a_workspace_shared_in_turn():
+    """A capture's workspace that an eager call of another size uses between
+    replays."""
+    d = lib()
+    a, b = Layer(1, 8, 256, 64, 8, 2), Layer(1, 30, 128, 96, 4, 3, seed=2)
+    a.ws = b.ws = torch.empty(max(a.ws.numel(), b.ws.numel()),
+                              dtype=torch.uint8, device="cuda")
+    a.run()
+    want = a.y.t.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run()
+    for _ in range(3):
+        b.run()
+        b.check()
+        a.y.t.zero_()
+        graph.replay()
+        assert torch.equal(a.y.t, want)
+    assert d.dpar_last_error() == ""
+
+
+def test_front_end():
+    d = lib()
+    g = gen(4)
+
+    def normal(*shape, dtype=torch.bfloat16):
+        return (torch.randn(*shape, generator=g, device="cuda")
+                * shape[-1] ** -0.5).to(dtype)
+
+    x = normal(6, 64) * 8
+    wg, wu, wd = normal(4, 48, 64), normal(4, 48, 64), normal(4, 64, 48)
+    logits = normal(6, 4, dtype=torch.float32)
+    y, index, weight = d.moe(x, logits, wg, wu, wd, 2)
+    again, _, _ = d.moe(x, None, wg, wu, wd, index=index, weight=weight)
+    assert torch.equal(y, again)
+    ranks = [t.view(2, 2, *t.shape[1:]) for t in (wg, wu, wd)]
+    parts, i2, w2 = d.moe(x, logits, *ranks, 2, out_dtype=torch.float32)
+    assert parts.shape == (2, 6, 64) and torch.equal(i2, index)
+    whole, _, _ = d.moe(x, logits, wg, wu, wd, 2, out_dtype=torch.float32)
+    assert torch.allclose(parts.sum(0), whole, rtol=0, atol=1e-5)
+    # 8-bit weights as dpar.quantize makes them
+    q = [d.quantize(t) for t in (wg, wu, wd)]
+    near, _, _ = d.moe(x, logits, *(a for a, _ in q), 2, *(b for _, b in q),
+                       residual=y)
+    assert near.shape == y.shape
+    assert ((near - y).float() - y.float()).norm() < 0.05 * y.float().norm()
