@@ -23,9 +23,10 @@ struct Record {
 };
 
 // A rank's part of the workspace: the number of records, the records, the pairs
-// by expert and their weights, and the hidden values of every pair.
+// by expert and their weights, whether a pair is the rank's, and the hidden
+// values and the result of every pair.
 struct Layout {
-  size_t records, pairs, weights, hidden, bytes;
+  size_t records, pairs, weights, owned, hidden, parts, bytes;
 };
 
 struct Args {
@@ -39,6 +40,7 @@ struct Args {
   float* weight[kRanks];
   size_t in, hidden;
   size_t ldx, ldl, ldw, ldd, xw, xd, ldy, ldr;   // as in dpar_moe_t
+  size_t pitch;                  // of the pairs' results
   char* work;
   Layout at;
   float scale;

@@ -85,6 +85,9 @@ int planes_of(const Options& c) {
   return c.t == Type::F32 ? 2 : c.eo == 4 ? 3 : 2;
 }
 
+// Distance of the pairs' results, in 32-bit values.
+size_t pitch_of(const dpar_moe_t& o) { return (o.in + 3) / 4 * 4; }
+
 moe::Layout layout_of(const Options& c) {
   const size_t pairs = c.o.tokens * c.o.top;
   auto up = [](size_t v) { return (v + 127) / 128 * 128; };
@@ -92,10 +95,12 @@ moe::Layout layout_of(const Options& c) {
   l.records = 128;
   l.pairs = l.records + up((size_t)most_of(c.o) * sizeof(moe::Record));
   l.weights = l.pairs + up(pairs * 4);
-  l.hidden = l.weights + up(pairs * 4);
+  l.owned = l.weights + up(pairs * 4);
+  l.hidden = l.owned + up(pairs * 4);
   // (an fp32 value: as two parts of 16 bits)
-  l.bytes = l.hidden + up(pairs * ((c.o.hidden + 7) / 8 * 8) * 2 *
+  l.parts = l.hidden + up(pairs * ((c.o.hidden + 7) / 8 * 8) * 2 *
                           planes_of(c));
+  l.bytes = l.parts + up(pairs * pitch_of(c.o) * 4);
   return l;
 }
 
@@ -171,6 +176,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.in = o.in, a.hidden = o.hidden;
   a.ldx = o.ldx, a.ldl = o.ldl, a.ldw = o.ldw, a.ldd = o.ldd;
   a.xw = o.xw, a.xd = o.xd, a.ldy = o.ldy, a.ldr = o.ldr;
+  a.pitch = pitch_of(o);
   a.work = (char*)ws, a.at = at;
   a.scale = o.weight_scale;
   a.tokens = (int)o.tokens, a.experts = (int)o.experts, a.top = o.top;
@@ -189,8 +195,8 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.fast[1] = fast(o.hidden, o.ldd, o.xd, 4, 5);
   const size_t chosen = std::min(c.all, o.tokens * top);
   a.waves[0] = waves_of((o.hidden + 15) / 16 * chosen, o.in * c.ew / 512, cus);
-  a.waves[1] = (o.in + 15) / 16 * std::min((size_t)per, chosen) <
-                       (size_t)cus * 2 ? 8 : 4;
+  a.waves[1] = std::min(waves_of((o.in + 63) / 64 * chosen,
+                                 o.hidden * c.ew / 512, cus), 4);
   const size_t groups = std::max((o.hidden + 15) / 16 * a.most,
                                  (o.in + 15) / 16) * per;
   if (groups > 0xffffffffu / 512)

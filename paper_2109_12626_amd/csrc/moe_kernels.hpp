@@ -39,6 +39,8 @@ template <Type W, Type X> struct Mix {
   using XV = typename Elem<X>::V;
   static constexpr int VB = 16 / (int)sizeof(V);
   static constexpr int NX = VB * (int)sizeof(XV) / 16;
+  // bytes of a row in a chunk: 8 bits' activations fill twice the registers
+  static constexpr int kRow = W == Type::I8 ? 256 : 512;
   // hidden values: 32-bit ones as they are, else P parts of 16 bits
   static constexpr bool kWhole = X == Type::F32;
   static constexpr int parts(int P) { return kWhole ? 1 : P * VB / 8; }
@@ -143,23 +145,24 @@ __device__ inline void split(float v, unsigned short (&part)[P]) {
 
 // ---------------------------------------------------------------- streams
 
-constexpr int kRow = 512, kChunk = 16 * kRow;      // bytes
-
 // 16 rows of a matrix, `left` of them there, from memory to a wavefront's LDS in
-// chunks of 512 bytes a row, pieces exchanged by the row (as FewFast does).
-template <typename V>
+// chunks of ROW bytes a row, pieces exchanged by the row (as FewFast does).
+template <typename V, int ROW>
 struct Stream {
-  static constexpr int VB = 16 / (int)sizeof(V), KC = kRow / (int)sizeof(V);
+  static constexpr int VB = 16 / (int)sizeof(V), KC = ROW / (int)sizeof(V);
+  static constexpr int kChunk = 16 * ROW, kSteps = ROW / 64;
+  static constexpr int kLanes = ROW / 16;          // of a row
+  static constexpr int kLoads = kChunk / 1024, kRows = 64 / kLanes;
 
   // Chunk c (of a contraction of nc values) of the rows from `base` on.
   static __device__ void ask(const char* base, size_t ld, int left, size_t nc,
                              unsigned c, uint32_t lds, int lane) {
-    const int slot = lane & 31;
-    const char* b = uniform(base + (size_t)c * kRow);
+    const int slot = lane % kLanes;
+    const char* b = uniform(base + (size_t)c * ROW);
     if ((size_t)(c + 1) * KC <= nc) {
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const int row = h * 2 + (lane >> 5);
+      for (int h = 0; h < kLoads; ++h) {
+        const int row = h * kRows + lane / kLanes;
         const int at = row < left ? row : left - 1;
         dma16_once(uniform(lds + h * 1024), b,
                    (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 7)) * 16);
@@ -167,8 +170,8 @@ struct Stream {
     } else {
       // the last chunk: zeros past the contraction's end
 #pragma unroll 1
-      for (int h = 0; h < 8; ++h) {
-        const int row = h * 2 + (lane >> 5);
+      for (int h = 0; h < kLoads; ++h) {
+        const int row = h * kRows + lane / kLanes;
         const int at = row < left ? row : left - 1;
         const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * VB;
         dma16_at(uniform(lds + h * 1024),
@@ -179,7 +182,7 @@ struct Stream {
   }
   // Step u's piece of row r for lane group q.
   static __device__ i32x4 take(LDS char* src, int u, int r, int q) {
-    return *(LDS i32x4*)(src + r * kRow + (((u * 4 + q) ^ (r & 7)) * 16));
+    return *(LDS i32x4*)(src + r * ROW + (((u * 4 + q) ^ (r & 7)) * 16));
   }
 };
 
@@ -207,13 +210,13 @@ struct Up {
   using M = Mix<W, X>;
   using V = typename M::V;
   using XV = typename M::XV;
-  using St = Stream<V>;
+  using St = Stream<V, M::kRow>;
   static constexpr int VB = M::VB, NX = M::NX, K = 4 * VB;   // per step
-  static constexpr int U = FAST ? kRow / 64 : 4;             // steps a chunk
-  static constexpr int KC = U * K;
+  static constexpr int U = FAST ? St::kSteps : 4;            // steps a chunk
+  static constexpr int KC = U * K, kChunk = St::kChunk;
+  static constexpr int kParts = S * MT * 2 * 1024;
   static constexpr int kLds =
-      FAST ? S * 2 * kChunk : S * MT * 2 * 1024;
-  static_assert(kLds >= S * MT * 2 * 1024);
+      FAST && S * 2 * kChunk > kParts ? S * 2 * kChunk : kParts;
 
   static __device__ void run(GivenMoe& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
@@ -423,201 +426,202 @@ struct Up {
 
 // ---------------------------------------------------------------- down
 
-// y = sum of weight * (wd h) + residual: a workgroup takes 16 columns (16 rows
-// of wd) of a rank and goes over all its chosen experts, so that a token's sum
-// stays in LDS: the S wavefronts take parts of equal length of (expert,
-// contraction), and join their sums in order.
-template <Type W, Type X, bool FAST, int P, int MT, int S>
+// weight * (wd h) of the pairs that chose an expert: a workgroup takes 16 * NW
+// columns (rows of wd) of one chosen expert, its S wavefronts a part of the
+// contraction each; MT tiles of 16 pairs at a time.  The NW sets of 16 rows take
+// turns and share the hidden values in registers: P parts of 16 bits each, they
+// are P n / 16 NW times the weights' bytes with n pairs, and come from L2.
+template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V>;
-  static constexpr int VB = M::VB, K = 4 * VB;
-  static constexpr int N = M::parts(P);
-  static constexpr int U = FAST ? kRow / 64 : 4;
-  static constexpr int KC = U * K;
-  static constexpr int kBuffers = FAST ? S * 2 * kChunk : 0;
-
-  static size_t lds_bytes(int tokens) {
-    return kBuffers + (size_t)S * tokens * 64;
-  }
-
-  // What a wavefront is working at.
-  struct At {
-    Record rec;
-    unsigned unit, chunk;
-  };
+  using St = Stream<V, M::kRow>;
+  static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
+  static constexpr int U = FAST ? St::kSteps : 4;
+  static constexpr int KC = U * K, kChunk = St::kChunk, BJ = 16 * NW;
+  static constexpr int kParts = S * MT * NW * 1024;
+  static constexpr int kLds =
+      FAST && S * 2 * kChunk > kParts ? S * 2 * kChunk : kParts;
 
   static __device__ void run(GivenMoe& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
     const int r = lane & 15, q = lane >> 4;
-    const unsigned tiles = (unsigned)((a.in + 15) / 16);
-    const int rank = uniform(blockIdx.x / tiles);
-    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 16;
+    const unsigned tiles = (unsigned)((a.in + BJ - 1) / BJ);
+    const unsigned id = uniform(blockIdx.x / tiles);
+    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * BJ;
+    const int rank = uniform(id / a.most), at = uniform(id % a.most);
     char* const work = work_of(a, rank);
-    const int chosen = uniform(*(const int*)work);
-    const Record* records = (const Record*)(work + a.at.records);
-    const int* list = (const int*)(work + a.at.pairs);
-    const float* weights = (const float*)(work + a.at.weights);
+    if (at >= *(const int*)work) return;
+    const Record rec = ((const Record*)(work + a.at.records))[at];
+    const int expert = uniform(rec.expert), count = uniform(rec.count),
+              first = uniform(rec.first);
+    const int* list = (const int*)(work + a.at.pairs) + first;
+    const float* weights = (const float*)(work + a.at.weights) + first;
     const char* hidden = work + a.at.hidden;
     const size_t groups = (a.hidden + 7) / 8;
-    const int left = a.in - j0 < 16 ? (int)(a.in - j0) : 16;
 
-    LDS float* const sums = (LDS float*)(lds + kBuffers);
-    LDS float* const mine = sums + (size_t)wave * a.tokens * 16;
-    for (int i = lane; i < a.tokens * 16; i += 64) mine[i] = 0.f;
-    in_order();
-
+    // (sets past the last row: that row, and no results)
+    const char* base[NW];
+    int left[NW];
+#pragma unroll
+    for (int n = 0; n < NW; ++n) {
+      const size_t j = j0 + n * 16 < a.in ? j0 + n * 16 : a.in - 1;
+      left[n] = a.in - j < 16 ? (int)(a.in - j) : 16;
+      base[n] = uniform((const char*)a.w[2][rank] +
+                        ((size_t)expert * a.xd + j * a.ldd) * sizeof(V));
+    }
     const unsigned chunks = (unsigned)((a.hidden + KC - 1) / KC);
-    const unsigned units = (unsigned)chosen * chunks;
-    const unsigned u0 = uniform((unsigned)((uint64_t)units * wave / S)),
-                   u1 = uniform((unsigned)((uint64_t)units * (wave + 1) / S));
-    const uint32_t buffer =
+    const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
+                   c1 = uniform((unsigned)((uint64_t)chunks * (wave + 1) / S));
+    const uint32_t mine =
         uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
     LDS char* const src = lds + wave * (2 * kChunk);
-    auto matrix = [&](const Record& rec) {
-      return uniform((const char*)a.w[2][rank] +
-                     ((size_t)rec.expert * a.xd + j0 * a.ldd) * sizeof(V));
-    };
-    At now, next;
-    auto first = [&](At& x) {
-      x.unit = u0, x.chunk = u0 % chunks;
-      x.rec = records[u0 / chunks];
-    };
-    auto step = [&](At& x) {
-      ++x.unit;
-      if (++x.chunk == chunks) {
-        x.chunk = 0;
-        if (x.unit < u1) x.rec = records[x.unit / chunks];
-      }
-    };
-    f32x4 acc[MT] = {};
-    if (u0 < u1) {
-      first(now);
-      next = now;
+
+    for (int i0 = 0; i0 < count; i0 += MT * 16) {
+      const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
       if constexpr (FAST)
-        St::ask(matrix(now.rec), a.ldd, left, a.hidden, now.chunk, buffer,
-                lane);
-    }
-    int buf = 0;
-#pragma unroll 1
-    while (u0 < u1 && now.unit < u1) {
-      step(next);
-      const int count = uniform(now.rec.count), from = uniform(now.rec.first);
-      auto fetch = [&](int i0, int u, i32x4 (&h)[N]) {
-        int i = i0 + r;
-        if (i >= count) i = count - 1;
-        const size_t pair = list[from + i];
-        const size_t k = (size_t)now.chunk * KC + u * K + q * VB;
-        if constexpr (M::kWhole) {
-          const bool there = k < groups * 8;
-          h[0] = there ? *(const i32x4*)(hidden + (pair * groups * 8 + k) * 4)
-                       : i32x4{0, 0, 0, 0};
-        } else {
+        if (c0 < c1) St::ask(base[0], a.ldd, left[0], a.hidden, c0, mine, lane);
+      size_t pair[MT];
 #pragma unroll
-          for (int g = 0; g < VB / 8; ++g) {
-            const size_t group = k / 8 + g;
-            const i32x4* at = (const i32x4*)hidden +
-                              (pair * groups + group) * P;
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-              h[g * P + p] = group < groups ? at[p] : i32x4{0, 0, 0, 0};
-          }
-        }
-      };
-      i32x4 h[U][N];
-#pragma unroll
-      for (int u = 0; u < U; ++u) fetch(0, u, h[u]);
-      i32x4 w[FAST ? 1 : U];
-      if constexpr (FAST) {
-        landed<0>();
-        if (next.unit < u1)
-          St::ask(matrix(next.rec), a.ldd, left, a.hidden, next.chunk,
-                  buffer + (buf ^ 1) * kChunk, lane);
-      } else {
-        const int row = r < left ? r : left - 1;
-        const V* at = (const V*)matrix(now.rec) + (size_t)row * a.ldd;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const size_t k = (size_t)now.chunk * KC + u * K + q * VB;
-          w[u] = load_piece<V>(at + k, (long)a.hidden - (long)k);
-        }
+      for (int m = 0; m < MT; ++m) {
+        int i = m * 16 + r;
+        if (i >= here) i = here - 1;
+        pair[m] = (size_t)list[i0 + i] * groups;
       }
-      auto weight = [&](int u) {
-        if constexpr (FAST)
-          return St::take(src + buf * kChunk, u, r, q);
-        else
-          return w[u];
-      };
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        acc[0] = M::template down<P>(weight(u), h[u], acc[0]);
-#pragma unroll
-      for (int m = 1; m < MT; ++m)
-        if (m * 16 < count) {
-#pragma unroll
-          for (int u = 0; u < U; ++u) fetch(m * 16, u, h[u]);
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            acc[m] = M::template down<P>(weight(u), h[u], acc[m]);
-        }
-      const bool last = next.unit >= u1 || next.chunk == 0;
-      if (last) {
-        // lane (r, q): pair r, columns q * 4 ..
-        f32x4 scale = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (W == Type::I8) {
-          const float* s = a.s[2][rank] + (size_t)now.rec.expert * a.in;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            scale[e] = j0 + q * 4 + e < a.in ? s[j0 + q * 4 + e] : 0.f;
-        }
+      f32x4 acc[MT][NW] = {};
+      int buf = 0;
+#pragma unroll 1
+      for (unsigned c = c0; c < c1; ++c) {
+        i32x4 h[MT][U][N];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
-          if (m * 16 + r < count) {
-            const int i = from + m * 16 + r;
-            LDS f32x4* to = (LDS f32x4*)(mine + list[i] / a.top * 16 + q * 4);
-            const float share = weights[i];
-            f32x4 v = acc[m];
-            if constexpr (W == Type::I8) v *= scale;
-            *to += v * share;
-            acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-          } else {
-            acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (m == 0 || m * 16 < here) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const size_t k = (size_t)c * KC + u * K + q * VB;
+              if constexpr (M::kWhole) {
+                h[m][u][0] = k < groups * 8
+                                 ? *(const i32x4*)(hidden +
+                                                   (pair[m] * 8 + k) * 4)
+                                 : i32x4{0, 0, 0, 0};
+              } else {
+#pragma unroll
+                for (int g = 0; g < VB / 8; ++g) {
+                  const size_t group = k / 8 + g;
+                  const i32x4* from =
+                      (const i32x4*)hidden + (pair[m] + group) * P;
+#pragma unroll
+                  for (int p = 0; p < P; ++p)
+                    h[m][u][g * P + p] =
+                        group < groups ? from[p] : i32x4{0, 0, 0, 0};
+                }
+              }
+            }
           }
+#pragma unroll
+        for (int n = 0; n < NW; ++n) {
+          i32x4 w[FAST ? 1 : U];
+          if constexpr (FAST) {
+            landed<0>();                    // (h too)
+            const uint32_t to = uniform(mine + (buf ^ 1) * kChunk);
+            if (n + 1 < NW)
+              St::ask(base[(n + 1) % NW], a.ldd, left[(n + 1) % NW], a.hidden,
+                      c, to, lane);
+            else if (c + 1 < c1)
+              St::ask(base[0], a.ldd, left[0], a.hidden, c + 1, to, lane);
+          } else {
+            const int row = r < left[n] ? r : left[n] - 1;
+            const V* at = (const V*)base[n] + (size_t)row * a.ldd;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const size_t k = (size_t)c * KC + u * K + q * VB;
+              w[u] = load_piece<V>(at + k, (long)a.hidden - (long)k);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            i32x4 v;
+            if constexpr (FAST)
+              v = St::take(src + buf * kChunk, u, r, q);
+            else
+              v = w[u];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+              if (m == 0 || m * 16 < here)
+                acc[m][n] = M::template down<P>(v, h[m][u], acc[m][n]);
+          }
+          buf ^= 1;
+        }
+      }
+      // the wavefronts' sums in their order
+      if (FAST && S > 1) __syncthreads();
+      auto part = (f32x4(LDS*)[MT * NW][64])lds;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NW; ++n)
+          part[wave][m * NW + n][lane] = acc[m][n];
+      if (S > 1)
+        __syncthreads();
+      else
         in_order();
+#pragma unroll 1
+      for (int x = wave; x < MT * NW; x += S) {
+        const int m = x / NW, n = x % NW, i = m * 16 + r;
+        if (i >= here) continue;
+        f32x4 v = part[0][x][lane];
+#pragma unroll
+        for (int k = 1; k < S; ++k) v += part[k][x][lane];
+        const size_t j = j0 + n * 16 + q * 4;
+        if (j >= a.in) continue;
+        if constexpr (W == Type::I8) {
+          const float* s = a.s[2][rank] + (size_t)expert * a.in + j;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] *= j + e < a.in ? s[e] : 0.f;
+        }
+        v *= weights[i0 + i];
+        float* to = (float*)(work + a.at.parts) +
+                    (size_t)list[i0 + i] * a.pitch + j;
+        *(f32x4*)to = v;
       }
-      now = next;
-      buf ^= 1;
-    }
-    __syncthreads();
-    using Out = typename M::XV;
-    for (int i = t; i < a.tokens * 4; i += S * 64) {
-      const int token = i / 4;
-      const size_t j = j0 + i % 4 * 4;
-      if (j >= a.in) continue;
-      f32x4 v = *(LDS f32x4*)(sums + i * 4);
-#pragma unroll
-      for (int k = 1; k < S; ++k)
-        v += *(LDS f32x4*)(sums + (size_t)k * a.tokens * 16 + i * 4);
-      float o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = v[e];
-      const long rest = (long)a.in - (long)j;
-      if (const void* res = a.r[rank]) {
-        float p[4];
-        const size_t from = (size_t)token * a.ldr + j;
-        if (a.out32)
-          fetch_vals<float, 4>((const float*)res + from, p, rest, false);
-        else
-          fetch_vals<Out, 4>((const Out*)res + from, p, rest, false);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += p[e];
-      }
-      store_out<4>(a.y[rank], (size_t)token * a.ldy + j, o, rest, a.out32,
-                   false, Out());
+      if (i0 + MT * 16 < count) __syncthreads();
     }
   }
 };
+
+// y = the sum of a token's parts, in the order of its choices, + residual: four
+// columns per thread.
+template <Type X>
+__global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
+  GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
+  using Out = typename Elem<X>::V;
+  const size_t j = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const int token = blockIdx.y, rank = blockIdx.z;
+  if (j >= a.in) return;
+  char* const work = work_of(a, rank);
+  const int* owned = (const int*)(work + a.at.owned) + (size_t)token * a.top;
+  const float* parts = (const float*)(work + a.at.parts) +
+                       (size_t)token * a.top * a.pitch + j;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < a.top; ++k)
+    if (owned[k]) v += *(const f32x4*)(parts + (size_t)k * a.pitch);
+  float o[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = v[e];
+  const long rest = (long)a.in - (long)j;
+  if (const void* res = a.r[rank]) {
+    float p[4];
+    const size_t from = (size_t)token * a.ldr + j;
+    if (a.out32)
+      fetch_vals<float, 4>((const float*)res + from, p, rest, false);
+    else
+      fetch_vals<Out, 4>((const Out*)res + from, p, rest, false);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += p[e];
+  }
+  store_out<4>(a.y[rank], (size_t)token * a.ldy + j, o, rest, a.out32, false,
+               Out());
+}
 
 // ---------------------------------------------------------------- launches
 
@@ -628,11 +632,11 @@ __global__ __launch_bounds__(S * 64) void k_moe_up(MoeArgs) {
   Up<W, X, FAST, MT, S>::run(a, (LDS char*)lds);
 }
 
-template <Type W, Type X, bool FAST, int P, int MT, int S>
+template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
 __global__ __launch_bounds__(S * 64) void k_moe_down(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Down<W, X, FAST, P, MT, S>::run(a, (LDS char*)lds);
+  Down<W, X, FAST, P, MT, NW, S>::run(a, (LDS char*)lds);
 }
 
 template <void (*K)(MoeArgs)>
@@ -674,19 +678,19 @@ hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
   return go_up<W, X, true, MT, 2>(a, stream);
 }
 
-template <Type W, Type X, bool FAST, int P, int MT, int S>
+template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
 hipError_t go_down(const MoeArgs& a, hipStream_t stream) {
-  using K = Down<W, X, FAST, P, MT, S>;
-  return launch_moe<k_moe_down<W, X, FAST, P, MT, S>>(
-      a, (a.in + 15) / 16 * a.ranks, S * 64, K::lds_bytes(a.tokens), stream);
+  using K = Down<W, X, FAST, P, MT, NW, S>;
+  return launch_moe<k_moe_down<W, X, FAST, P, MT, NW, S>>(
+      a, (a.in + K::BJ - 1) / K::BJ * a.most * a.ranks, S * 64, K::kLds,
+      stream);
 }
 
 template <Type W, Type X, int P, int MT>
 hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
-  if (!a.fast[1]) return go_down<W, X, false, P, 8, 4>(a, stream);
-  if constexpr (MT == 1)
-    if (a.waves[1] == 8) return go_down<W, X, true, P, 1, 8>(a, stream);
-  return go_down<W, X, true, P, MT, 4>(a, stream);
+  if (!a.fast[1]) return go_down<W, X, false, P, 2, 2, 4>(a, stream);
+  if (a.waves[1] == 4) return go_down<W, X, true, P, MT, 4, 4>(a, stream);
+  return go_down<W, X, true, P, MT, 4, 2>(a, stream);
 }
 
 template <Type W, Type X>
@@ -696,15 +700,21 @@ hipError_t run_moe(const MoeArgs& a, hipStream_t stream) {
   e = few ? pick_up<W, X, 1>(a, stream) : pick_up<W, X, 4>(a, stream);
   if (e != hipSuccess) return e;
   if constexpr (X == Type::F32) {
-    return few ? pick_down<W, X, 1, 1>(a, stream)
-               : pick_down<W, X, 1, 8>(a, stream);
+    e = few ? pick_down<W, X, 1, 1>(a, stream)
+            : pick_down<W, X, 1, 2>(a, stream);
   } else {
     if (a.planes == 2)
-      return few ? pick_down<W, X, 2, 1>(a, stream)
-                 : pick_down<W, X, 2, 8>(a, stream);
-    return few ? pick_down<W, X, 3, 1>(a, stream)
-               : pick_down<W, X, 3, 8>(a, stream);
+      e = few ? pick_down<W, X, 2, 1>(a, stream)
+              : pick_down<W, X, 2, 2>(a, stream);
+    else
+      e = few ? pick_down<W, X, 3, 1>(a, stream)
+              : pick_down<W, X, 3, 2>(a, stream);
   }
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_moe_join<X>,
+                     dim3((unsigned)((a.in + 1023) / 1024), a.tokens, a.ranks),
+                     dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -5,7 +5,7 @@ namespace dpar {
 namespace moe {
 namespace {
 
-constexpr int kRouteThreads = 512;
+constexpr int kRouteThreads = 1024;
 
 // Floats in their order as unsigned numbers: -0 equals 0, NaN comes last.
 __device__ inline uint32_t ordered(float v) {
@@ -15,19 +15,33 @@ __device__ inline uint32_t ordered(float v) {
 }
 constexpr uint32_t kNever = 0x007fffffu;    // -inf
 
-// The largest value of a wavefront's lanes.
+// Exchanges within a wavefront: `v` of the lane that CTRL names, 0 where there is
+// none.
+template <int CTRL>
+__device__ inline uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf,
+                                               false);
+}
+// Four steps within 16 lanes, two across: the last lane has met all.
+template <typename Fn>
+__device__ inline uint32_t gather(uint32_t v, Fn join) {
+  v = join(v, from_lane<0x111>(v));        // one lane up the row of 16
+  v = join(v, from_lane<0x112>(v));
+  v = join(v, from_lane<0x114>(v));
+  v = join(v, from_lane<0x118>(v));
+  v = join(v, from_lane<0x142>(v));        // a row's last to the next row
+  v = join(v, from_lane<0x143>(v));        // the lower half's to the upper
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 __device__ inline uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int far = 1; far < 64; far *= 2) {
-    const uint32_t o = __shfl_xor(v, far);
-    v = o > v ? o : v;
-  }
-  return v;
+  return gather(v, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
 }
 __device__ inline float wave_sum(float v) {
-#pragma unroll
-  for (int far = 1; far < 64; far *= 2) v += __shfl_xor(v, far);
-  return v;
+  return __builtin_bit_cast(
+      float, gather(__builtin_bit_cast(uint32_t, v), [](uint32_t x, uint32_t y) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, x) +
+                                                __builtin_bit_cast(float, y));
+      }));
 }
 
 // One token's choice by a wavefront: lane i < top ends with its i-th expert
@@ -48,7 +62,7 @@ __device__ inline void choose(GivenMoe& a, const float* logits, int experts,
 #pragma unroll
     for (int n = 0; n < N; ++n)
       if (n * 64 < experts) best = key[n] > best ? key[n] : best;
-    best = uniform(wave_max(best));
+    best = wave_max(best);
     if (best <= kNever) break;
     // the lowest expert that has it
     int found = -1;
@@ -169,9 +183,12 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs) {
   __syncthreads();
   int* const list = (int*)(work + a.at.pairs);
   float* const weights = (float*)(work + a.at.weights);
+  int* const owned = (int*)(work + a.at.owned);
   for (int i = t; i < pairs; i += kRouteThreads) {
     const int e = expert[i] - mine;
-    if (expert[i] >= 0 && e >= 0 && e < a.experts) {
+    const bool own = expert[i] >= 0 && e >= 0 && e < a.experts;
+    owned[i] = own;
+    if (own) {
       const int at = start[e] + place[i];
       list[at] = i;
       weights[at] = share[i];
