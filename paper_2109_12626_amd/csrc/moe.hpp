@@ -15,18 +15,22 @@ enum class Route : int { SOFTMAX = 0, SIGMOID = 1 };
 // Ranks of a launch, as in products.hpp: 12 arrays of 32 addresses.
 constexpr int kRanks = 32;
 constexpr int kTokens = 128, kTop = 16, kExperts = 1024;
+constexpr int kSmall = 8;      // tokens of the kernels for the fewest
 
-// An expert that some token chose: its list of pairs (token, place among the
-// token's choices) starts at `first`.
+// An expert that some token chose: its rank of the launch, its number there, and
+// its list of pairs (token, place among the token's choices).
 struct Record {
-  int expert, first, count, pad;
+  int rank, expert, first, count;
 };
 
-// A rank's part of the workspace: the number of records, the records, the pairs
-// by expert and their weights, whether a pair is the rank's, and the hidden
-// values and the result of every pair.
+// A table of the workspace: how many records there are and which is each rank's
+// first (`kStarts` numbers), the records in the experts' order, the pairs by
+// expert, their weights, a pair's rank (-1: none of the launch), and the hidden
+// values and the result of every pair.  Ranks that choose from the same logits
+// (or by the same index and weight) share one table, others have one each.
+constexpr int kStarts = kRanks + 2;
 struct Layout {
-  size_t records, pairs, weights, owned, hidden, parts, bytes;
+  size_t records, pairs, weights, owner, hidden, parts, bytes;
 };
 
 struct Args {
@@ -46,17 +50,22 @@ struct Args {
   float scale;
   int tokens, experts, top;
   int ranks, first, all;         // of the launch, its first, of the call
+  int tables;                    // 1, or one for each rank
   int act, route, normalize;
   int given;                     // index and weight are inputs
   int out32;
   int planes;                    // 16-bit parts of a hidden value
-  int most;                      // experts of a rank that can be chosen
+  int most;                      // records of a table at most
   int waves[2];                  // wavefronts per workgroup: up, down
   int fast[2];                   // up, down: weights of whole 16-byte pieces
+  int tiles[2];                  // up, down: pairs at a time / 16
+  int fused;                     // up makes the choice itself
+  int small;                     // down sums by token itself
 };
 static_assert(sizeof(Args) <= 4096, "kernel arguments");
 
-// The choice of experts, then the products (eight: 8-bit weights).
+// The choice of experts (unless fused), then the products (eight: 8-bit
+// weights).
 hipError_t launch_route(const Args& a, hipStream_t stream);
 hipError_t launch_bf16(bool eight, const Args& a, hipStream_t stream);
 hipError_t launch_f16(bool eight, const Args& a, hipStream_t stream);

@@ -75,9 +75,14 @@ int check_moe(const char* call, int p, const dpar_moe_t* opt, Options* c) {
   return DPAR_SUCCESS;
 }
 
-// A rank's experts that can be chosen.
-int most_of(const dpar_moe_t& o) {
-  return (int)std::min(o.experts, o.tokens * (size_t)o.top);
+// Records of a table for the experts of `ranks` ranks.
+int most_of(const dpar_moe_t& o, size_t ranks) {
+  return (int)std::min(o.experts * ranks, o.tokens * (size_t)o.top);
+}
+
+int ranks_of(int p) {
+  const int n = (p + moe::kRanks - 1) / moe::kRanks;
+  return (p + n - 1) / n;
 }
 
 // 16-bit parts of a hidden value.
@@ -88,15 +93,16 @@ int planes_of(const Options& c) {
 // Distance of the pairs' results, in 32-bit values.
 size_t pitch_of(const dpar_moe_t& o) { return (o.in + 3) / 4 * 4; }
 
-moe::Layout layout_of(const Options& c) {
+moe::Layout layout_of(const Options& c, int p) {
   const size_t pairs = c.o.tokens * c.o.top;
   auto up = [](size_t v) { return (v + 127) / 128 * 128; };
   moe::Layout l;
-  l.records = 128;
-  l.pairs = l.records + up((size_t)most_of(c.o) * sizeof(moe::Record));
+  l.records = up(moe::kStarts * 4);
+  l.pairs = l.records +
+            up((size_t)most_of(c.o, ranks_of(p)) * sizeof(moe::Record));
   l.weights = l.pairs + up(pairs * 4);
-  l.owned = l.weights + up(pairs * 4);
-  l.hidden = l.owned + up(pairs * 4);
+  l.owner = l.weights + up(pairs * 4);
+  l.hidden = l.owner + up(pairs * 4);
   // (an fp32 value: as two parts of 16 bits)
   l.parts = l.hidden + up(pairs * ((c.o.hidden + 7) / 8 * 8) * 2 *
                           planes_of(c));
@@ -153,7 +159,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   constexpr int kMats = 12;
   m[9].twin[0] = residual;
   if ((rc = check_mats(m, kMats, p, call))) return rc;
-  const moe::Layout at = layout_of(c);
+  const moe::Layout at = layout_of(c, p);
   if (!o.tokens) return DPAR_SUCCESS;
   if (!ws || bytes < at.bytes * p)
     return fail(DPAR_ERR_INVALID_ARG, "%s: workspace of %zu bytes, %zu needed",
@@ -170,8 +176,7 @@ int moe_impl(const void* const* x, const void* const* logits,
                     call, m[k].name, i);
 
   const int cus = cu_count();
-  const int per = (p + (p + moe::kRanks - 1) / moe::kRanks - 1) /
-                  ((p + moe::kRanks - 1) / moe::kRanks);
+  const int per = ranks_of(p);
   moe::Args a = {};
   a.in = o.in, a.hidden = o.hidden;
   a.ldx = o.ldx, a.ldl = o.ldl, a.ldw = o.ldw, a.ldd = o.ldd;
@@ -183,7 +188,13 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.all = p;
   a.act = o.act, a.route = o.route, a.normalize = o.normalize != 0;
   a.given = given, a.out32 = c.eo == 4, a.planes = planes_of(c);
-  a.most = most_of(o);
+  // one table if all ranks make the same choice
+  bool same = true;
+  for (int i = 1; i < p; ++i)
+    same = same && (given ? index[i] == index[0] && weight[i] == weight[0]
+                          : logits[i] == logits[0]);
+  a.tables = same ? 1 : per;
+  a.most = most_of(o, same ? per : 1);
   // weights of whole aligned pieces, 16 rows of them within 32-bit offsets
   auto fast = [&](size_t cols, size_t ld, size_t far, int k0, int k1) {
     uintptr_t bits = cols * c.ew | ld * c.ew | (n > 1 ? far * c.ew : 0);
@@ -197,13 +208,24 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.waves[0] = waves_of((o.hidden + 15) / 16 * chosen, o.in * c.ew / 512, cus);
   a.waves[1] = std::min(waves_of((o.in + 63) / 64 * chosen,
                                  o.hidden * c.ew / 512, cus), 4);
-  const size_t groups = std::max((o.hidden + 15) / 16 * a.most,
-                                 (o.in + 15) / 16) * per;
+  // Tiles of 16 pairs at a time, by an expert's share of them; more take another
+  // turn over its matrices.
+  const size_t mean = o.tokens * top / c.all;
+  a.tiles[0] = mean <= 8 ? 1 : mean <= 24 ? 2 : 4;
+  a.tiles[1] = mean <= 8 ? 1 : 2;
+  const bool few = o.tokens <= (size_t)moe::kSmall;
+  a.fused = few && a.fast[0] && o.in && o.hidden && c.all <= 256;
+  a.small = few && a.fast[1] && o.hidden;
+  const size_t groups =
+      std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * a.most *
+                   a.tables,
+               (o.in + 7) / 8 * per);
   if (groups > 0xffffffffu / 512)
     return fail(DPAR_ERR_UNSUPPORTED, "%s: %zu workgroups in a launch", call,
                 groups);
   for (int r0 = 0; r0 < p; r0 += per) {
     a.ranks = std::min(per, p - r0), a.first = r0;
+    if (!same) a.tables = a.ranks;
     for (int k = 0; k < a.ranks; ++k) {
       const int i = r0 + k;
       a.x[k] = m[0].rank(i);
@@ -217,7 +239,8 @@ int moe_impl(const void* const* x, const void* const* logits,
       a.index[k] = (int*)m[10].rank(i);
       a.weight[k] = (float*)m[11].rank(i);
     }
-    if ((rc = launched(call, moe::launch_route(a, stream)))) return rc;
+    if (!a.fused && (rc = launched(call, moe::launch_route(a, stream))))
+      return rc;
     if (!o.in) continue;
     const hipError_t e = c.t == Type::BF16  ? moe::launch_bf16(eight, a, stream)
                          : c.t == Type::F16 ? moe::launch_f16(eight, a, stream)
@@ -251,7 +274,7 @@ int dpar_moe_workspace(int p, const dpar_moe_t* opt, size_t* bytes) {
     const int rc = check_moe(call, p, opt, &c);
     if (rc) return rc;
     if (!bytes) return fail(DPAR_ERR_INVALID_ARG, "%s: null result", call);
-    *bytes = c.o.tokens ? layout_of(c).bytes * p : 0;
+    *bytes = c.o.tokens ? layout_of(c, p).bytes * p : 0;
     return (int)DPAR_SUCCESS;
   });
 }

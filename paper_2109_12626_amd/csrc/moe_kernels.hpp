@@ -16,8 +16,271 @@ using namespace products;
 using MoeArgs = moe::Args;
 using GivenMoe = const __attribute__((address_space(4))) MoeArgs;
 
-__device__ inline char* work_of(GivenMoe& a, int rank) {
-  return a.work + (size_t)(a.first + rank) * a.at.bytes;
+__device__ inline char* table_of(GivenMoe& a, int table) {
+  return a.work + (size_t)(a.first + table) * a.at.bytes;
+}
+
+// ---------------------------------------------------------------- the choice
+
+// Floats in their order as unsigned numbers: -0 equals 0, NaN comes last.
+__device__ inline uint32_t ordered(float v) {
+  if (v != v) return 0xffffffffu;
+  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);
+  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+constexpr uint32_t kNever = 0x007fffffu;    // -inf
+__device__ inline float as_value(uint32_t key) {
+  return __builtin_bit_cast(float, key >> 31 ? key ^ 0x80000000u : ~key);
+}
+
+// Exchanges within a wavefront: `v` of the lane that CTRL names, 0 where there is
+// none.
+template <int CTRL>
+__device__ inline uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf,
+                                               false);
+}
+// Four steps within 16 lanes, two across: the last lane has met all.
+template <typename Fn>
+__device__ inline uint32_t gather(uint32_t v, Fn join) {
+  v = join(v, from_lane<0x111>(v));        // one lane up the row of 16
+  v = join(v, from_lane<0x112>(v));
+  v = join(v, from_lane<0x114>(v));
+  v = join(v, from_lane<0x118>(v));
+  v = join(v, from_lane<0x142>(v));        // a row's last to the next row
+  v = join(v, from_lane<0x143>(v));        // the lower half's to the upper
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline uint32_t wave_max(uint32_t v) {
+  return gather(v, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+}
+__device__ inline float wave_sum(float v) {
+  return __builtin_bit_cast(
+      float, gather(__builtin_bit_cast(uint32_t, v), [](uint32_t x, uint32_t y) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, x) +
+                                                __builtin_bit_cast(float, y));
+      }));
+}
+
+// Sums of the lanes up to each.
+__device__ inline int wave_scan(int v) {
+  v += (int)from_lane<0x111>((uint32_t)v);
+  v += (int)from_lane<0x112>((uint32_t)v);
+  v += (int)from_lane<0x114>((uint32_t)v);
+  v += (int)from_lane<0x118>((uint32_t)v);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// One token's choice by a wavefront, of at most 64 * N experts: lane i < top
+// ends with its i-th expert (-1: none) and weight.
+template <int N>
+__device__ inline void choose(GivenMoe& a, const float* logits, int experts,
+                              int lane, int* index, float* weight) {
+  float value[N];
+  uint32_t key[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int e = n * 64 + lane;
+    value[n] = e < experts ? logits[e] : -__builtin_inff();
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) key[n] = ordered(value[n]);
+  int mine = -1;
+  float v = 0.f, most = 0.f;
+  for (int i = 0; i < a.top; ++i) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int n = 1; n < N; ++n) best = key[n] > best ? key[n] : best;
+    best = wave_max(best);
+    if (best <= kNever) break;
+    // the lowest expert that has it
+    int found = -1;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (found < 0) {
+        const uint64_t has = __ballot(key[n] == best);
+        if (has) {
+          const int at = __builtin_ctzll(has);
+          found = n * 64 + at;
+          if (lane == at) key[n] = 0;
+        }
+      }
+    const float of = as_value(best);
+    if (i == 0) most = of;
+    if (lane == i) {
+      mine = found;
+      v = of;
+    }
+  }
+  float w = 0.f;
+  if (a.route == (int)Route::SOFTMAX) {
+    if (mine >= 0) w = expf(v - most);
+    float sum = w;
+    if (!a.normalize) {
+      sum = 0.f;
+#pragma unroll
+      for (int n = 0; n < N; ++n) sum += expf(value[n] - most);
+    }
+    sum = wave_sum(sum);
+    if (mine >= 0) w = w / sum;
+  } else {
+    if (mine >= 0) w = 1.f / (1.f + expf(-v));
+    if (a.normalize) {
+      const float sum = wave_sum(w);
+      if (mine >= 0 && sum != 0.f) w = w / sum;
+    }
+  }
+  *index = mine;
+  *weight = w * a.scale;
+}
+
+// LDS of a workgroup that makes the choice.
+struct Choice {
+  LDS int* expert;           // of a pair
+  LDS float* share;
+  LDS int* place;            // among its expert's pairs
+  LDS int* list;             // pairs by expert
+  LDS int* count;            // of an expert's pairs, and the first of them
+  LDS int* start;
+  LDS Record* record;        // the one asked for
+  LDS int* starts;           // as in the table
+
+  static __host__ __device__ constexpr int bytes(int pairs, int experts) {
+    return pairs * 16 + experts * 8 + (int)sizeof(Record) + kStarts * 4 + 8;
+  }
+  __device__ Choice(LDS char* lds, int pairs, int experts) {
+    record = (LDS Record*)lds;
+    expert = (LDS int*)(record + 1);
+    share = (LDS float*)(expert + pairs);
+    place = (LDS int*)(share + pairs);
+    list = place + pairs;
+    count = list + pairs;
+    start = count + experts;
+    starts = start + experts;
+  }
+};
+
+// Every token's choice and, by expert, the pairs of a table's own ones, by a
+// workgroup: into LDS, with the record `at`, and where asked to into the
+// workspace and the index and weight arrays.  False if there are not so many
+// records.  The order of an expert's pairs is not fixed, and no result depends
+// on it.
+template <int THREADS>
+__device__ inline bool route(GivenMoe& a, int table, const Choice& c, int at,
+                             bool write) {
+  const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+  const int top = a.top, pairs = a.tokens * top, all = a.experts * a.all;
+  const bool one = a.tables == 1;
+  // (the table's experts)
+  const int low = a.experts * (a.first + (one ? 0 : table)),
+            own = a.experts * (one ? a.ranks : 1);
+
+  for (int e = t; e < own; e += THREADS) c.count[e] = 0;
+  if (a.given) {
+    for (int i = t; i < pairs; i += THREADS) {
+      const int e = a.index[table][i];
+      c.expert[i] = e >= 0 && e < all ? e : -1;
+      c.share[i] = a.weight[table][i];
+    }
+  } else {
+    for (int k = wave; k < a.tokens; k += THREADS / 64) {
+      int e;
+      float w;
+      const float* l = a.logits[table] + (size_t)k * a.ldl;
+      if (all <= 64)
+        choose<1>(a, l, all, lane, &e, &w);
+      else if (all <= 256)
+        choose<4>(a, l, all, lane, &e, &w);
+      else
+        choose<kExperts / 64>(a, l, all, lane, &e, &w);
+      if (lane < top) {
+        const int i = k * top + lane;
+        c.expert[i] = e;
+        c.share[i] = w;
+        if (write)
+          for (int n = one ? 0 : table; n < (one ? a.ranks : table + 1); ++n) {
+            if (a.index[n]) a.index[n][i] = e;
+            if (a.weight[n]) a.weight[n][i] = w;
+          }
+      }
+    }
+  }
+  __syncthreads();
+  if (a.given) {
+    // an expert that a token names twice has one pair, with both weights
+    for (int k = t; k < a.tokens; k += THREADS)
+      for (int i = 1; i < top; ++i)
+        for (int j = 0; j < i; ++j)
+          if (c.expert[k * top + i] >= 0 &&
+              c.expert[k * top + i] == c.expert[k * top + j]) {
+            c.share[k * top + j] += c.share[k * top + i];
+            c.expert[k * top + i] = -1;
+          }
+    __syncthreads();
+  }
+  for (int i = t; i < pairs; i += THREADS) {
+    const int e = c.expert[i] - low;
+    if (c.expert[i] >= 0 && e >= 0 && e < own)
+      c.place[i] = __hip_atomic_fetch_add(&c.count[e], 1, __ATOMIC_RELAXED,
+                                          __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+  __syncthreads();
+  char* const work = table_of(a, table);
+  if (wave == 0) {
+    Record* const records = (Record*)(work + a.at.records);
+    int before = 0, chosen = 0;
+    for (int e0 = 0; e0 < own; e0 += 64) {
+      const int e = e0 + lane, n = e < own ? c.count[e] : 0;
+      const int sum = wave_scan(n);
+      const uint64_t some = __ballot(n > 0);
+      const int first = before + sum - n;
+      const int place = chosen + __popcll(some & ((1ull << lane) - 1));
+      const int rank = (one ? 0 : table) + e / a.experts;
+      if (e < own) {
+        c.start[e] = first;
+        if (e % a.experts == 0) c.starts[1 + rank] = place;
+      }
+      if (n > 0) {
+        const Record r = {rank, e % a.experts, first, n};
+        if (place == at) {
+          c.record->rank = r.rank;
+          c.record->expert = r.expert;
+          c.record->first = r.first;
+          c.record->count = r.count;
+        }
+        if (write) records[place] = r;
+      }
+      before += __builtin_amdgcn_readlane(sum, 63);
+      chosen += __popcll(some);
+    }
+    if (lane == 0) {
+      c.starts[0] = chosen;
+      c.starts[1 + (one ? a.ranks : table + 1)] = chosen;
+    }
+  }
+  __syncthreads();
+  for (int i = t; i < pairs; i += THREADS) {
+    const int e = c.expert[i] - low;
+    const bool mine = c.expert[i] >= 0 && e >= 0 && e < own;
+    if (mine) c.list[c.start[e] + c.place[i]] = i;
+    if (!write) continue;
+    ((int*)(work + a.at.owner))[i] =
+        mine ? (one ? 0 : table) + e / a.experts : -1;
+    if (mine) {
+      const int to = c.start[e] + c.place[i];
+      ((int*)(work + a.at.pairs))[to] = i;
+      ((float*)(work + a.at.weights))[to] = c.share[i];
+    }
+  }
+  if (write)
+    for (int i = t; i < kStarts; i += THREADS)
+      if (i == 0 || (one ? i <= 1 + a.ranks
+                         : i == 1 + table || i == 2 + table))
+        ((int*)work)[i] = c.starts[i];
+  __syncthreads();
+  return at < c.starts[0];
 }
 
 // ---------------------------------------------------------------- types
@@ -154,25 +417,27 @@ struct Stream {
   static constexpr int kLanes = ROW / 16;          // of a row
   static constexpr int kLoads = kChunk / 1024, kRows = 64 / kLanes;
 
-  // Chunk c (of a contraction of nc values) of the rows from `base` on.
+  // Chunk c (of a contraction of nc values) of the rows from `base` on, as rows
+  // FROM .. FROM + ROWS - 1 of the chunk.
+  template <int FROM = 0, int ROWS = 16>
   static __device__ void ask(const char* base, size_t ld, int left, size_t nc,
                              unsigned c, uint32_t lds, int lane) {
     const int slot = lane % kLanes;
     const char* b = uniform(base + (size_t)c * ROW);
     if ((size_t)(c + 1) * KC <= nc) {
 #pragma unroll
-      for (int h = 0; h < kLoads; ++h) {
+      for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
-        const int at = row < left ? row : left - 1;
+        const int at = row - FROM < left ? row - FROM : left - 1;
         dma16_once(uniform(lds + h * 1024), b,
                    (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 7)) * 16);
       }
     } else {
       // the last chunk: zeros past the contraction's end
 #pragma unroll 1
-      for (int h = 0; h < kLoads; ++h) {
+      for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
-        const int at = row < left ? row : left - 1;
+        const int at = row - FROM < left ? row - FROM : left - 1;
         const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * VB;
         dma16_at(uniform(lds + h * 1024),
                  k < nc ? base + (at * ld + k) * sizeof(V)
@@ -202,10 +467,33 @@ __device__ inline void fetch_row(const XV* x, long left, i32x4 (&v)[NX]) {
 
 // ---------------------------------------------------------------- gate and up
 
+// What a workgroup of up or down works at: a chosen expert and its pairs.
+struct Task {
+  int rank, expert, count;
+  const int* list;
+  const float* weights;
+  char* work;
+
+  // The record `at` of a table; false if there are not so many.
+  __device__ bool find(GivenMoe& a, int table, int at) {
+    work = table_of(a, table);
+    if (at >= *(const int*)work) return false;
+    const Record r = ((const Record*)(work + a.at.records))[at];
+    rank = uniform(r.rank);
+    expert = uniform(r.expert);
+    count = uniform(r.count);
+    const int first = uniform(r.first);
+    list = (const int*)(work + a.at.pairs) + first;
+    weights = (const float*)(work + a.at.weights) + first;
+    return true;
+  }
+};
+
 // h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 columns
 // (16 rows of either matrix) of one chosen expert, its S wavefronts a part of
-// the contraction each; up to MT tiles of 16 pairs at a time.
-template <Type W, Type X, bool FAST, int MT, int S>
+// the contraction each; MT tiles of 16 pairs at a time.  FUSED: every workgroup
+// makes the choice for itself (few tokens), the first one of a table keeps it.
+template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
 struct Up {
   using M = Mix<W, X>;
   using V = typename M::V;
@@ -224,38 +512,54 @@ struct Up {
     const unsigned tiles = (unsigned)((a.hidden + 15) / 16);
     const unsigned id = uniform(blockIdx.x / tiles);
     const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 16;
-    const int rank = uniform(id / a.most), at = uniform(id % a.most);
-    char* const work = work_of(a, rank);
-    if (at >= *(const int*)work) return;
-    const Record rec = ((const Record*)(work + a.at.records))[at];
-    const int expert = uniform(rec.expert), count = uniform(rec.count);
-    const int* list = (const int*)(work + a.at.pairs) + uniform(rec.first);
+    const int table = uniform(id / a.most), at = uniform(id % a.most);
+    Task task;
+    const Choice choice(lds + kLds, a.tokens * a.top,
+                        a.experts * (a.tables == 1 ? a.ranks : 1));
+    if constexpr (FUSED) {
+      if (!route<S * 64>(a, table, choice, at, at == 0 && j0 == 0)) return;
+      task.rank = uniform(choice.record->rank);
+      task.expert = uniform(choice.record->expert);
+      task.count = uniform(choice.record->count);
+      task.work = table_of(a, table);
+    } else {
+      if (!task.find(a, table, at)) return;
+    }
+    const int rank = task.rank, count = task.count;
     const size_t origin =
-        ((size_t)expert * a.xw + j0 * a.ldw) * sizeof(V);
-    const char* base[2] = {(const char*)a.w[0][rank] + origin,
-                           (const char*)a.w[1][rank] + origin};
-    const int left =
-        a.hidden - j0 < 16 ? (int)(a.hidden - j0) : 16;
+        ((size_t)task.expert * a.xw + j0 * a.ldw) * sizeof(V);
+    const char* base[2] = {uniform((const char*)a.w[0][rank] + origin),
+                           uniform((const char*)a.w[1][rank] + origin)};
+    const int left = a.hidden - j0 < 16 ? (int)(a.hidden - j0) : 16;
 
     const unsigned chunks = (unsigned)((a.in + KC - 1) / KC);
-    const unsigned c0 = (unsigned)((uint64_t)chunks * wave / S),
-                   c1 = (unsigned)((uint64_t)chunks * (wave + 1) / S);
+    const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
+                   c1 = uniform((unsigned)((uint64_t)chunks * (wave + 1) / S));
+    const uint32_t mine =
+        uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
     for (int i0 = 0; i0 < count; i0 += MT * 16) {
       const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
+      if constexpr (FAST)
+        if (c0 < c1) St::ask(base[0], a.ldw, left, a.in, c0, mine, lane);
       const XV* x[MT];
+      int pair[MT];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         int i = m * 16 + r;
         if (i >= here) i = here - 1;
-        x[m] = (const XV*)a.x[rank] +
-               (size_t)(list[i0 + i] / a.top) * a.ldx + q * VB;
+        if constexpr (FUSED)
+          pair[m] = choice.list[choice.record->first + i0 + i];
+        else
+          pair[m] = task.list[i0 + i];
+        x[m] = (const XV*)a.x[rank] + (size_t)(pair[m] / a.top) * a.ldx +
+               q * VB;
       }
       f32x4 acc[MT][2] = {};
       if constexpr (FAST)
         stream(a, base, left, c0, c1, lds, wave, lane, x, here, acc);
       else
         fetch(a, base, left, c0, c1, lane, x, here, acc);
-      finish(a, rank, expert, list + i0, here, j0, lds, wave, lane, acc, work);
+      finish(a, task, pair, here, j0, lds, wave, lane, acc);
       if (i0 + MT * 16 < count) __syncthreads();
     }
   }
@@ -269,7 +573,6 @@ struct Up {
     const uint32_t mine =
         uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
     LDS char* const src = lds + wave * (2 * kChunk);
-    if (c0 < c1) St::ask(base[0], a.ldw, left, a.in, c0, mine, lane);
 #pragma unroll 1
     for (unsigned c = c0; c < c1; ++c) {
       i32x4 fx[MT][U][NX];
@@ -340,10 +643,10 @@ struct Up {
 
   // Adds the wavefronts' sums in their order; tile m is finished by wavefront m
   // % S: h of 16 pairs and 16 columns, zeros past the last column.
-  static __device__ void finish(GivenMoe& a, int rank, int expert,
-                                const int* list, int here, size_t j0,
+  static __device__ void finish(GivenMoe& a, const Task& task,
+                                const int (&pairs)[MT], int here, size_t j0,
                                 LDS char* lds, int wave, int lane,
-                                const f32x4 (&acc)[MT][2], char* work) {
+                                const f32x4 (&acc)[MT][2]) {
     const int r = lane & 15, q = lane >> 4;
     auto part = (f32x4(LDS*)[MT * 2][64])lds;
 #pragma unroll
@@ -371,10 +674,10 @@ struct Up {
         float gate = g[e], up = u[e];
         const bool there = j + e < a.hidden;
         if constexpr (W == Type::I8) {
-          const size_t row = (size_t)expert * a.hidden + j + e;
+          const size_t row = (size_t)task.expert * a.hidden + j + e;
           if (there) {
-            gate *= a.s[0][rank][row];
-            up *= a.s[1][rank][row];
+            gate *= a.s[0][task.rank][row];
+            up *= a.s[1][task.rank][row];
           }
         }
         h[e] = there ? up : 0.f;
@@ -387,8 +690,12 @@ struct Up {
           h[e] = j + e < a.hidden ? v : 0.f;
         }
       });
-      const size_t pair = list[i], groups = (a.hidden + 7) / 8;
-      char* const row = work + a.at.hidden;
+      int one = pairs[0];
+#pragma unroll
+      for (int k = 1; k < MT; ++k)
+        if (m == k) one = pairs[k];
+      const size_t pair = one, groups = (a.hidden + 7) / 8;
+      char* const row = task.work + a.at.hidden;
       if constexpr (M::kWhole) {
         f32x4 v;
 #pragma unroll
@@ -449,15 +756,11 @@ struct Down {
     const unsigned tiles = (unsigned)((a.in + BJ - 1) / BJ);
     const unsigned id = uniform(blockIdx.x / tiles);
     const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * BJ;
-    const int rank = uniform(id / a.most), at = uniform(id % a.most);
-    char* const work = work_of(a, rank);
-    if (at >= *(const int*)work) return;
-    const Record rec = ((const Record*)(work + a.at.records))[at];
-    const int expert = uniform(rec.expert), count = uniform(rec.count),
-              first = uniform(rec.first);
-    const int* list = (const int*)(work + a.at.pairs) + first;
-    const float* weights = (const float*)(work + a.at.weights) + first;
-    const char* hidden = work + a.at.hidden;
+    Task task;
+    if (!task.find(a, uniform(id / a.most), uniform(id % a.most))) return;
+    const int rank = task.rank, expert = task.expert, count = task.count;
+    const int* list = task.list;
+    const char* hidden = task.work + a.at.hidden;
     const size_t groups = (a.hidden + 7) / 8;
 
     // (sets past the last row: that row, and no results)
@@ -579,13 +882,211 @@ struct Down {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] *= j + e < a.in ? s[e] : 0.f;
         }
-        v *= weights[i0 + i];
-        float* to = (float*)(work + a.at.parts) +
+        v *= task.weights[i0 + i];
+        float* to = (float*)(task.work + a.at.parts) +
                     (size_t)list[i0 + i] * a.pitch + j;
         *(f32x4*)to = v;
       }
       if (i0 + MT * 16 < count) __syncthreads();
     }
+  }
+};
+
+// y = sum of weight * (wd h) + residual for at most 8 tokens, whole: a workgroup
+// takes 8 columns of a rank and goes over all the chosen experts.  A unit is a
+// chunk of one expert's 8 rows; a wavefront takes two at a time, one in the upper
+// and one in the lower 8 of the matrix cores' rows, their pairs in the left and
+// right 8 columns: of the product the two blocks that belong together count.
+// A token's sums stay in LDS, a wavefront's own, and are joined in order.
+template <Type W, Type X, int P>
+struct DownSmall {
+  using M = Mix<W, X>;
+  using V = typename M::V;
+  using St = Stream<V, M::kRow>;
+  static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
+  static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
+  static constexpr int S = 8, kMost = kSmall * kTop;     // pairs
+  static constexpr int kSums = S * 2 * kChunk;
+  static constexpr int kRecords = kSums + S * kSmall * 8 * 4,
+                       kList = kRecords + kMost * (int)sizeof(Record),
+                       kWeights = kList + kMost * 4,
+                       kLds = kWeights + kMost * 4;
+
+  // One of a wavefront's two units.
+  struct Half {
+    unsigned unit, end;        // this one, and past the last
+    unsigned chunk;
+    int expert, first, count;
+  };
+
+  static __device__ void run(GivenMoe& a, LDS char* lds) {
+    const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+    const int r = lane & 15, q = lane >> 4, side = r >> 3;
+    const unsigned tiles = (unsigned)((a.in + 7) / 8);
+    const int rank = uniform(blockIdx.x / tiles);
+    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 8;
+    const int left = a.in - j0 < 8 ? (int)(a.in - j0) : 8;
+    const int pairs = a.tokens * a.top;
+    char* const work = table_of(a, a.tables == 1 ? 0 : rank);
+    const char* hidden = work + a.at.hidden;
+    const size_t groups = (a.hidden + 7) / 8;
+
+    // the table's lists in LDS
+    LDS Record* const records = (LDS Record*)(lds + kRecords);
+    LDS int* const list = (LDS int*)(lds + kList);
+    LDS float* const weights = (LDS float*)(lds + kWeights);
+    LDS float* const mine = (LDS float*)(lds + kSums) + wave * (kSmall * 8);
+    const int* starts = (const int*)work + 1 + rank;
+    const int low = uniform(starts[0]), high = uniform(starts[1]);
+    for (int i = t; i < a.most * 4; i += S * 64)
+      ((LDS int*)records)[i] = ((const int*)(work + a.at.records))[i];
+    for (int i = t; i < pairs; i += S * 64) {
+      list[i] = ((const int*)(work + a.at.pairs))[i];
+      weights[i] = ((const float*)(work + a.at.weights))[i];
+    }
+    mine[lane] = 0.f;
+    __syncthreads();
+
+    const unsigned chunks = (unsigned)((a.hidden + KC - 1) / KC);
+    const unsigned units = (unsigned)(high - low) * chunks;
+    const unsigned u0 = uniform((unsigned)((uint64_t)units * wave / S)),
+                   u1 = uniform((unsigned)((uint64_t)units * (wave + 1) / S));
+    const unsigned turns = (u1 - u0 + 1) / 2;
+    const uint32_t buffer =
+        uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
+    LDS char* const src = lds + wave * (2 * kChunk);
+    auto set = [&](Half& x) {
+      LDS Record* rec = records + low + x.unit / chunks;
+      x.expert = uniform(rec->expert);
+      x.first = uniform(rec->first);
+      x.count = uniform(rec->count);
+    };
+    Half now[2];
+    auto start = [&](Half& x, unsigned from, unsigned end) {
+      x = {from, end, from % chunks, 0, 0, 0};
+      if (from < end) set(x);
+    };
+    auto step = [&](Half& x) {
+      if (x.unit >= x.end) return;
+      ++x.unit;
+      if (++x.chunk == chunks) {
+        x.chunk = 0;
+        if (x.unit < x.end) set(x);
+      }
+    };
+    // (a half that is through, the second one of an odd number, stays where it
+    // is: its block of the product is left out)
+    auto ask = [&](const Half (&x)[2], int buf) {
+      auto base = [&](const Half& y) {
+        return uniform((const char*)a.w[2][rank] +
+                       ((size_t)y.expert * a.xd + j0 * a.ldd) * sizeof(V));
+      };
+      const uint32_t to = uniform(buffer + buf * kChunk);
+      St::template ask<0, 8>(base(x[0]), a.ldd, left, a.hidden, x[0].chunk, to,
+                             lane);
+      if (x[1].unit < x[1].end)
+        St::template ask<8, 8>(base(x[1]), a.ldd, left, a.hidden, x[1].chunk,
+                               to, lane);
+    };
+    auto fetch = [&](const Half (&x)[2], i32x4 (&h)[U][N]) {
+      const int count = side ? x[1].count : x[0].count,
+                first = side ? x[1].first : x[0].first;
+      const unsigned chunk = side ? x[1].chunk : x[0].chunk;
+      const bool some = side ? x[1].unit < x[1].end : true;
+      const int i = (r & 7) < count ? r & 7 : count - 1;
+      const size_t pair = some ? (size_t)list[first + i] * groups : 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t k = (size_t)chunk * KC + u * K + q * VB;
+        if constexpr (M::kWhole) {
+          h[u][0] = some && k < groups * 8
+                        ? *(const i32x4*)(hidden + (pair * 8 + k) * 4)
+                        : i32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+          for (int g = 0; g < VB / 8; ++g) {
+            const size_t group = k / 8 + g;
+            const i32x4* from = (const i32x4*)hidden + (pair + group) * P;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+              h[u][g * P + p] =
+                  some && group < groups ? from[p] : i32x4{0, 0, 0, 0};
+          }
+        }
+      }
+    };
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    // Adds one half's sums to its tokens': lane (r, q): pair r % 8, columns q %
+    // 2 * 4 ..
+    auto flush = [&](const Half& x, int which) {
+      const int i = r & 7;
+      if (side == which && q >> 1 == which) {
+        if (i < x.count) {
+          f32x4 v = acc;
+          const int j = (q & 1) * 4;
+          if constexpr (W == Type::I8) {
+            const float* s =
+                a.s[2][rank] + (size_t)x.expert * a.in + j0 + j;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= j + e < left ? s[e] : 0.f;
+          }
+          LDS f32x4* to =
+              (LDS f32x4*)(mine + list[x.first + i] / a.top * 8 + j);
+          *to += v * weights[x.first + i];
+        }
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      in_order();
+    };
+    if (turns) {
+      start(now[0], u0, u0 + turns);
+      start(now[1], u0 + turns, u1);
+      i32x4 h[2][U][N];
+      ask(now, 0);
+      fetch(now, h[0]);
+      // one turn: the next one's loads go out before this one's products
+      auto turn = [&](unsigned k, int buf, i32x4 (&h)[U][N],
+                      i32x4 (&then)[U][N]) {
+        landed<0>();
+        const Half was[2] = {now[0], now[1]};
+        step(now[0]);
+        step(now[1]);
+        if (k + 1 < turns) {
+          ask(now, buf ^ 1);
+          fetch(now, then);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          acc = M::template down<P>(St::take(src + buf * kChunk, u, r, q),
+                                    h[u], acc);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (was[s].unit < was[s].end &&
+              (now[s].unit == now[s].end || now[s].chunk == 0))
+            flush(was[s], s);
+      };
+#pragma unroll 1
+      for (unsigned k = 0; k < turns; k += 2) {
+        turn(k, 0, h[0], h[1]);
+        if (k + 1 < turns) turn(k + 1, 1, h[1], h[0]);
+      }
+    }
+    __syncthreads();
+    using Out = typename M::XV;
+    const int token = t / 8, col = t % 8;
+    if (token >= a.tokens || col >= left) return;
+    LDS float* const sums = (LDS float*)(lds + kSums);
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < S; ++k) v += sums[k * (kSmall * 8) + t];
+    const size_t j = j0 + col;
+    if (const void* res = a.r[rank]) {
+      const size_t from = (size_t)token * a.ldr + j;
+      v += a.out32 ? ((const float*)res)[from]
+                   : (float)((const Out*)res)[from];
+    }
+    store_out<1>(a.y[rank], (size_t)token * a.ldy + j, &v, 1, a.out32, false,
+                 Out());
   }
 };
 
@@ -598,13 +1099,13 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
   const size_t j = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   const int token = blockIdx.y, rank = blockIdx.z;
   if (j >= a.in) return;
-  char* const work = work_of(a, rank);
-  const int* owned = (const int*)(work + a.at.owned) + (size_t)token * a.top;
+  char* const work = table_of(a, a.tables == 1 ? 0 : rank);
+  const int* owner = (const int*)(work + a.at.owner) + (size_t)token * a.top;
   const float* parts = (const float*)(work + a.at.parts) +
                        (size_t)token * a.top * a.pitch + j;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < a.top; ++k)
-    if (owned[k]) v += *(const f32x4*)(parts + (size_t)k * a.pitch);
+    if (owner[k] == rank) v += *(const f32x4*)(parts + (size_t)k * a.pitch);
   float o[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = v[e];
@@ -625,11 +1126,11 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
 
 // ---------------------------------------------------------------- launches
 
-template <Type W, Type X, bool FAST, int MT, int S>
+template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
 __global__ __launch_bounds__(S * 64) void k_moe_up(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Up<W, X, FAST, MT, S>::run(a, (LDS char*)lds);
+  Up<W, X, FAST, FUSED, MT, S>::run(a, (LDS char*)lds);
 }
 
 template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
@@ -637,6 +1138,13 @@ __global__ __launch_bounds__(S * 64) void k_moe_down(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
   Down<W, X, FAST, P, MT, NW, S>::run(a, (LDS char*)lds);
+}
+
+template <Type W, Type X, int P>
+__global__ __launch_bounds__(512) void k_moe_down_small(MoeArgs) {
+  GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
+  extern __shared__ char lds[];
+  DownSmall<W, X, P>::run(a, (LDS char*)lds);
 }
 
 template <void (*K)(MoeArgs)>
@@ -663,54 +1171,73 @@ hipError_t launch_moe(const MoeArgs& a, size_t groups, int threads,
   return hipGetLastError();
 }
 
-template <Type W, Type X, bool FAST, int MT, int S>
+template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
 hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
-  using K = Up<W, X, FAST, MT, S>;
-  return launch_moe<k_moe_up<W, X, FAST, MT, S>>(
-      a, (a.hidden + 15) / 16 * a.most * a.ranks, S * 64, K::kLds, stream);
+  using K = Up<W, X, FAST, FUSED, MT, S>;
+  const int more =
+      FUSED ? Choice::bytes(a.tokens * a.top,
+                            a.experts * (a.tables == 1 ? a.ranks : 1))
+            : 0;
+  return launch_moe<k_moe_up<W, X, FAST, FUSED, MT, S>>(
+      a, (a.hidden + 15) / 16 * a.most * a.tables, S * 64, K::kLds + more,
+      stream);
 }
 
-template <Type W, Type X, int MT>
+template <Type W, Type X, bool FUSED, int MT>
+hipError_t waves_up(const MoeArgs& a, hipStream_t stream) {
+  switch (a.waves[0]) {
+    case 8: return go_up<W, X, true, FUSED, MT, 8>(a, stream);
+    case 4: return go_up<W, X, true, FUSED, MT, 4>(a, stream);
+    case 2: return go_up<W, X, true, FUSED, MT, 2>(a, stream);
+  }
+  return hipErrorInvalidConfiguration;
+}
+
+template <Type W, Type X>
 hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
-  if (!a.fast[0]) return go_up<W, X, false, 4, 4>(a, stream);
-  if (a.waves[0] == 8) return go_up<W, X, true, MT, 8>(a, stream);
-  if (a.waves[0] == 4) return go_up<W, X, true, MT, 4>(a, stream);
-  return go_up<W, X, true, MT, 2>(a, stream);
+  if (!a.fast[0]) return go_up<W, X, false, false, 4, 4>(a, stream);
+  if (a.fused) return waves_up<W, X, true, 1>(a, stream);
+  switch (a.tiles[0]) {
+    case 1: return waves_up<W, X, false, 1>(a, stream);
+    case 2: return waves_up<W, X, false, 2>(a, stream);
+    case 4: return waves_up<W, X, false, 4>(a, stream);
+  }
+  return hipErrorInvalidConfiguration;
 }
 
 template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
 hipError_t go_down(const MoeArgs& a, hipStream_t stream) {
   using K = Down<W, X, FAST, P, MT, NW, S>;
   return launch_moe<k_moe_down<W, X, FAST, P, MT, NW, S>>(
-      a, (a.in + K::BJ - 1) / K::BJ * a.most * a.ranks, S * 64, K::kLds,
+      a, (a.in + K::BJ - 1) / K::BJ * a.most * a.tables, S * 64, K::kLds,
       stream);
 }
 
-template <Type W, Type X, int P, int MT>
+template <Type W, Type X, int P>
 hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
+  if (a.small) {
+    using K = DownSmall<W, X, P>;
+    return launch_moe<k_moe_down_small<W, X, P>>(
+        a, (a.in + 7) / 8 * a.ranks, 512, K::kLds, stream);
+  }
   if (!a.fast[1]) return go_down<W, X, false, P, 2, 2, 4>(a, stream);
-  if (a.waves[1] == 4) return go_down<W, X, true, P, MT, 4, 4>(a, stream);
-  return go_down<W, X, true, P, MT, 4, 2>(a, stream);
+  if (a.tiles[1] == 1)
+    return a.waves[1] == 4 ? go_down<W, X, true, P, 1, 4, 4>(a, stream)
+                           : go_down<W, X, true, P, 1, 4, 2>(a, stream);
+  return a.waves[1] == 4 ? go_down<W, X, true, P, 2, 4, 4>(a, stream)
+                         : go_down<W, X, true, P, 2, 4, 2>(a, stream);
 }
 
 template <Type W, Type X>
 hipError_t run_moe(const MoeArgs& a, hipStream_t stream) {
-  const bool few = a.tokens <= 16;
-  hipError_t e;
-  e = few ? pick_up<W, X, 1>(a, stream) : pick_up<W, X, 4>(a, stream);
+  hipError_t e = pick_up<W, X>(a, stream);
   if (e != hipSuccess) return e;
-  if constexpr (X == Type::F32) {
-    e = few ? pick_down<W, X, 1, 1>(a, stream)
-            : pick_down<W, X, 1, 2>(a, stream);
-  } else {
-    if (a.planes == 2)
-      e = few ? pick_down<W, X, 2, 1>(a, stream)
-              : pick_down<W, X, 2, 2>(a, stream);
-    else
-      e = few ? pick_down<W, X, 3, 1>(a, stream)
-              : pick_down<W, X, 3, 2>(a, stream);
-  }
-  if (e != hipSuccess) return e;
+  if constexpr (X == Type::F32)
+    e = pick_down<W, X, 1>(a, stream);
+  else
+    e = a.planes == 2 ? pick_down<W, X, 2>(a, stream)
+                      : pick_down<W, X, 3>(a, stream);
+  if (e != hipSuccess || a.small) return e;
   hipLaunchKernelGGL(k_moe_join<X>,
                      dim3((unsigned)((a.in + 1023) / 1024), a.tokens, a.ranks),
                      dim3(256), 0, stream, a);
