@@ -16,6 +16,11 @@ enum class Route : int { SOFTMAX = 0, SIGMOID = 1 };
 constexpr int kRanks = 32;
 constexpr int kTokens = 128, kTop = 16, kExperts = 1024;
 constexpr int kSmall = 8;      // tokens of the kernels for the fewest
+// Sets of 16 columns of a workgroup of up.  With two, activations are read half
+// as often: 8-bit weights are no more bytes than the activations of 16 pairs.
+constexpr int columns_up(Type w, bool fused, int tiles) {
+  return !fused && (w == Type::I8 || tiles > 1) ? 2 : 1;
+}
 
 // An expert that some token chose: its rank of the launch, its number there, and
 // its list of pairs (token, place among the token's choices).
@@ -59,6 +64,7 @@ struct Args {
   int waves[2];                  // wavefronts per workgroup: up, down
   int fast[2];                   // up, down: weights of whole 16-byte pieces
   int tiles[2];                  // up, down: pairs at a time / 16
+  int sets;                      // of 16 columns, of a workgroup of down
   int fused;                     // up makes the choice itself
   int small;                     // down sums by token itself
 };

@@ -104,7 +104,7 @@ moe::Layout layout_of(const Options& c, int p) {
   l.owner = l.weights + up(pairs * 4);
   l.hidden = l.owner + up(pairs * 4);
   // (an fp32 value: as two parts of 16 bits)
-  l.parts = l.hidden + up(pairs * ((c.o.hidden + 7) / 8 * 8) * 2 *
+  l.parts = l.hidden + up(pairs * ((c.o.hidden + 31) / 32 * 32) * 2 *
                           planes_of(c));
   l.bytes = l.parts + up(pairs * pitch_of(c.o) * 4);
   return l;
@@ -113,6 +113,7 @@ moe::Layout layout_of(const Options& c, int p) {
 // Wavefronts per workgroup for a matrix of `chunks` chunks of 512 bytes a row,
 // with n workgroups that have work.
 int waves_of(size_t n, size_t chunks, int cus) {
+  if (chunks >= 16) return 4;
   int w = 2;
   while (w < 8 && chunks >= (size_t)w * 2 && n * w < (size_t)cus * 8) w *= 2;
   return w;
@@ -205,17 +206,23 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.fast[0] = fast(o.in, o.ldw, o.xw, 2, 4);
   a.fast[1] = fast(o.hidden, o.ldd, o.xd, 4, 5);
   const size_t chosen = std::min(c.all, o.tokens * top);
-  a.waves[0] = waves_of((o.hidden + 15) / 16 * chosen, o.in * c.ew / 512, cus);
-  a.waves[1] = std::min(waves_of((o.in + 63) / 64 * chosen,
-                                 o.hidden * c.ew / 512, cus), 4);
   // Tiles of 16 pairs at a time, by an expert's share of them; more take another
   // turn over its matrices.
   const size_t mean = o.tokens * top / c.all;
   a.tiles[0] = mean <= 8 ? 1 : mean <= 24 ? 2 : 4;
   a.tiles[1] = mean <= 8 ? 1 : 2;
-  const bool few = o.tokens <= (size_t)moe::kSmall;
-  a.fused = few && a.fast[0] && o.in && o.hidden && c.all <= 256;
-  a.small = few && a.fast[1] && o.hidden;
+  const size_t blocks = o.tokens <= (size_t)moe::kSmall
+                            ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
+  a.fused = o.in && o.hidden && c.all <= 256 &&
+            (o.hidden + 15) / 16 * blocks <= (size_t)cus * 4;
+  a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
+            (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1);
+  const size_t up = 16 * moe::columns_up(c.w, a.fused, a.tiles[0]);
+  a.waves[0] = waves_of((o.hidden + up - 1) / up * chosen, o.in * c.ew / 512,
+                        cus);
+  a.sets = (o.in + 63) / 64 * chosen < (size_t)cus * 2 ? 2 : 4;
+  a.waves[1] = std::min(waves_of((o.in + 16 * a.sets - 1) / (16 * a.sets) *
+                                     chosen, o.hidden * c.ew / 512, cus), 4);
   const size_t groups =
       std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * a.most *
                    a.tables,

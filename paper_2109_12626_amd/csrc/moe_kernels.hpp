@@ -295,15 +295,21 @@ __device__ inline float from_byte(int word, int k) {
   return (float)(signed char)(word >> (8 * k));
 }
 
-// Weights of type W beside activations of type X.  A piece is 16 bytes of
-// weights, VB values; a lane group's activations for it are NX 16-byte pieces.
+// Weights of type W beside activations of type X.  A step of the contraction is
+// 16 bytes of weights per lane group, VB values, beside NX 16-byte pieces of
+// activations: lane group q has E values of each run of 4 E, so that the four
+// read 64 bytes of a row side by side.  (8 bits: two runs of 32 values.)
 template <Type W, Type X> struct Mix {
   using V = typename Elem<W>::V;
   using XV = typename Elem<X>::V;
-  static constexpr int VB = 16 / (int)sizeof(V);
-  static constexpr int NX = VB * (int)sizeof(XV) / 16;
-  // bytes of a row in a chunk: 8 bits' activations fill twice the registers
-  static constexpr int kRow = W == Type::I8 ? 256 : 512;
+  static constexpr int VB = 16 / (int)sizeof(V), E = 16 / (int)sizeof(XV);
+  static constexpr int NX = VB / E;
+  // Bytes of a row in a chunk: 512, or 256 where the activations of that many,
+  // `pieces` of each step, take more than 128 registers, and for SHIFT, which
+  // needs some for itself.
+  static constexpr int row(int pieces, bool shift) {
+    return shift || pieces * 8 * 4 > 128 ? 256 : 512;
+  }
   // hidden values: 32-bit ones as they are, else P parts of 16 bits
   static constexpr bool kWhole = X == Type::F32;
   static constexpr int parts(int P) { return kWhole ? 1 : P * VB / 8; }
@@ -410,58 +416,196 @@ __device__ inline void split(float v, unsigned short (&part)[P]) {
 
 // 16 rows of a matrix, `left` of them there, from memory to a wavefront's LDS in
 // chunks of ROW bytes a row, pieces exchanged by the row (as FewFast does).
-template <typename V, int ROW>
+//
+// SHIFT: rows that start anywhere and hold any number of values.  The pieces are
+// those that lie on 16 bytes in memory, one more of a row than its chunk fills,
+// and LDS is read from the row's own first byte on (33 x 20 experts 1001 x 501
+// fp16 36 us; by way of registers 41).  A piece that holds a byte of the row is
+// read whole; it lies in one page with that byte.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+template <typename T, bool SHIFT> struct At { typedef T Type; };
+template <typename T> struct At<T, true> {
+  typedef T Type __attribute__((aligned(1)));
+};
+template <typename T, bool SHIFT>
+using Anywhere = typename At<T, SHIFT>::Type;
+
+template <typename V, int ROW, bool SHIFT>
 struct Stream {
   static constexpr int VB = 16 / (int)sizeof(V), KC = ROW / (int)sizeof(V);
-  static constexpr int kChunk = 16 * ROW, kSteps = ROW / 64;
-  static constexpr int kLanes = ROW / 16;          // of a row
-  static constexpr int kLoads = kChunk / 1024, kRows = 64 / kLanes;
+  static constexpr int kSteps = ROW / 64;
+  static constexpr int kLanes = ROW / 16 + (SHIFT ? 1 : 0);    // of a row
+  static constexpr int kPitch = kLanes * 16;
+  static constexpr int kLoads = (16 * kLanes + 63) / 64;
+  static constexpr int kChunk = kLoads * 1024, kRows = 64 / kLanes;
 
   // Chunk c (of a contraction of nc values) of the rows from `base` on, as rows
   // FROM .. FROM + ROWS - 1 of the chunk.
   template <int FROM = 0, int ROWS = 16>
   static __device__ void ask(const char* base, size_t ld, int left, size_t nc,
                              unsigned c, uint32_t lds, int lane) {
-    const int slot = lane % kLanes;
-    const char* b = uniform(base + (size_t)c * ROW);
-    if ((size_t)(c + 1) * KC <= nc) {
+    if constexpr (SHIFT) {
+      constexpr int kPieces = ROWS * kLanes;
+      const uint32_t low = (uint32_t)(uintptr_t)base & 15,
+                     far = (uint32_t)(ld * sizeof(V)),
+                     bytes = (uint32_t)(nc * sizeof(V));
+      const char* b = uniform(base - low);
+#pragma unroll
+      for (int h = 0; h < (kPieces + 63) / 64; ++h) {
+        const int n = h * 64 + lane, row = n / kLanes, piece = n % kLanes;
+        // the row's first byte and its last piece; pieces past that are not
+        // used, and it stands for them
+        const uint32_t first = low + (row < left ? row : left - 1) * far,
+                       last = (first + bytes - 1) & ~15u;
+        const uint32_t at = (first & ~15u) + c * ROW + piece * 16;
+        if (n < kPieces)
+          dma16_once(uniform(lds + FROM * kPitch + h * 1024), b,
+                     at < last ? at : last);
+      }
+    } else if ((size_t)(c + 1) * KC <= nc) {
+      const int slot = lane % kLanes;
+      const char* b = uniform(base + (size_t)c * ROW);
 #pragma unroll
       for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
         dma16_once(uniform(lds + h * 1024), b,
-                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 7)) * 16);
+                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 15)) * 16);
       }
     } else {
       // the last chunk: zeros past the contraction's end
+      const int slot = lane % kLanes;
 #pragma unroll 1
       for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
-        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 7)) * VB;
+        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 15)) * VB;
         dma16_at(uniform(lds + h * 1024),
                  k < nc ? base + (at * ld + k) * sizeof(V)
                         : (const char*)&g_zero);
       }
     }
   }
-  // Step u's piece of row r for lane group q.
-  static __device__ i32x4 take(LDS char* src, int u, int r, int q) {
-    return *(LDS i32x4*)(src + r * ROW + (((u * 4 + q) ^ (r & 7)) * 16));
+  // Where row r of the rows from `base` on starts in its first piece.
+  static __device__ int offset(const char* base, size_t ld, int left, int r) {
+    if constexpr (!SHIFT) return 0;
+    return (int)((uintptr_t)(base + (size_t)(r < left ? r : left - 1) * ld *
+                                        sizeof(V)) &
+                 15);
+  }
+  // Step u's values of row r for lane group q (Mix); off: offset(r); rest:
+  // values from the chunk's first to the contraction's end (SHIFT: what lies
+  // past it are another row's).
+  static __device__ i32x4 take(LDS char* src, int u, int r, int q, int off,
+                               int rest) {
+    constexpr int kRuns = sizeof(V) == 1 ? 2 : 1, kBytes = 16 / kRuns;
+    i32x4 v;
+#pragma unroll
+    for (int n = 0; n < kRuns; ++n) {
+      const int at = u * 64 + n * 4 * kBytes + q * kBytes;
+      LDS char* from =
+          SHIFT ? src + r * kPitch + off + at
+                : src + r * ROW + ((at / 16) ^ (r & 15)) * 16 + at % 16;
+      if constexpr (kRuns == 1) {
+        v = *(LDS Anywhere<i32x4, SHIFT>*)from;
+      } else {
+        const i32x2 half = *(LDS Anywhere<i32x2, SHIFT>*)from;
+        v[n * 2] = half[0];
+        v[n * 2 + 1] = half[1];
+      }
+      if (SHIFT && rest < KC) {
+        const int bytes = rest * (int)sizeof(V) - at;
+#pragma unroll
+        for (int k = n * kBytes / 4; k < (n + 1) * kBytes / 4; ++k) {
+          const int b = bytes - (k - n * kBytes / 4) * 4;
+          v[k] = b >= 4 ? v[k] : b <= 0 ? 0 : v[k] & ((1 << (b * 8)) - 1);
+        }
+      }
+    }
+    return v;
   }
 };
 
-// NX pieces of a row of activations of which `left` values are left (WHOLE: a
-// multiple of a piece's); rows may start anywhere.
+// Values from chunk c on, as far as the chunk.
+template <typename St>
+__device__ inline int rest_of(size_t nc, unsigned c) {
+  const size_t left = nc - (size_t)c * St::KC;
+  return left < (size_t)St::KC ? (int)left : St::KC;
+}
+
+// Waits until all but the last LEFT of this wavefront's loads have landed, and
+// its LDS reads.
+template <int LEFT>
+__device__ inline void landed_but(bool all) {
+  if (all)
+    landed<0>();
+  else
+    landed<LEFT>();
+}
+
+// A wavefront's way through the chunks c0 .. c1 - 1 of NS sets of rows that share
+// activations, with two buffers: load(c) loads a chunk's activations, ask(n, c,
+// buffer) asks for set n's part, use(n, c, buffer) multiplies it.  Two parts are
+// on their way whenever the wavefront waits: 16 KB, with 8 wavefronts 128 KB
+// per CU.
+template <int NS, int LOADS, typename Load, typename Pin, typename Ask,
+          typename Use>
+__device__ inline void sweep(unsigned c0, unsigned c1, Load load, Pin pin,
+                             Ask ask, Use use) {
+  static_assert(NS % 2 == 0);
+#pragma unroll 1
+  for (unsigned c = c0; c < c1; ++c) {
+    load(c);
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      if (n == 0) {
+        landed<0>();                 // the activations, sets 0 and 1
+        pin();
+      } else if (n > 1) {
+        landed_but<LOADS>(n + 1 == NS && c + 1 == c1);
+      }
+      use(n, c, n & 1);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (n + 2 < NS)
+        ask(n + 2, c, n & 1);
+      else if (c + 1 < c1)
+        ask(n + 2 - NS, c + 1, n & 1);
+    }
+  }
+}
+
+// The first `left` values at x, zeros behind them; 16 bytes before x + left are
+// the row's too.
+template <typename XV>
+__device__ inline i32x4 load_tail(const XV* x, int left) {
+  constexpr int E = 16 / (int)sizeof(XV);
+  const int back = left < E ? left > 0 ? E - left : E : 0;
+  uint64_t v[2];
+  __builtin_memcpy(v, x + (left < E ? left - E : 0), 16);
+  const int bits = back * (int)sizeof(XV) * 8;
+  const uint64_t low =
+      bits >= 64 ? v[1] >> (bits & 63)
+                 : v[0] >> bits | (bits ? v[1] << (64 - bits) : 0);
+  v[1] = bits >= 64 ? 0 : v[1] >> bits;
+  v[0] = bits >= 128 ? 0 : low;
+  i32x4 r;
+  __builtin_memcpy(&r, v, 16);
+  return r;
+}
+
+// NX pieces of a row of activations, of which `left` values are left (WHOLE: a
+// multiple of a piece's; else the row has a piece at least), one of each run;
+// rows may start anywhere.
 template <bool WHOLE, typename XV, int NX>
-__device__ inline void fetch_row(const XV* x, long left, i32x4 (&v)[NX]) {
+__device__ inline void fetch_row(const XV* x, int left, i32x4 (&v)[NX]) {
   constexpr int E = 16 / (int)sizeof(XV);
 #pragma unroll
   for (int n = 0; n < NX; ++n) {
     if constexpr (WHOLE)
-      v[n] = n * E < left ? load_whole<false>(x + n * E) : i32x4{0, 0, 0, 0};
+      v[n] = n * 4 * E < left ? load_whole<false>(x + n * 4 * E)
+                              : i32x4{0, 0, 0, 0};
     else
-      v[n] = load_piece<XV>(x + n * E, left - n * E);
+      v[n] = load_tail(x + n * 4 * E, left - n * 4 * E);
   }
 }
 
@@ -477,8 +621,9 @@ struct Task {
   // The record `at` of a table; false if there are not so many.
   __device__ bool find(GivenMoe& a, int table, int at) {
     work = table_of(a, table);
-    if (at >= *(const int*)work) return false;
+    // (at < a.most: there is room for the record, whether it is one or not)
     const Record r = ((const Record*)(work + a.at.records))[at];
+    if (at >= *(const int*)work) return false;
     rank = uniform(r.rank);
     expert = uniform(r.expert);
     count = uniform(r.count);
@@ -489,29 +634,36 @@ struct Task {
   }
 };
 
-// h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 columns
-// (16 rows of either matrix) of one chosen expert, its S wavefronts a part of
-// the contraction each; MT tiles of 16 pairs at a time.  FUSED: every workgroup
-// makes the choice for itself (few tokens), the first one of a table keeps it.
-template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
+// Distance of the hidden values' rows, in runs of 32, and the values that are
+// written: whole tiles of 16 columns, zeros past the last one.
+__device__ inline size_t runs_of(GivenMoe& a) { return (a.hidden + 31) / 32; }
+__device__ inline size_t held_of(GivenMoe& a) {
+  return (a.hidden + 15) / 16 * 16;
+}
+
+// h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 * C
+// columns (as many rows of either matrix) of one chosen expert, its S wavefronts
+// a part of the contraction each; MT tiles of 16 pairs at a time.  FUSED: every
+// workgroup makes the choice for itself (few tokens), the first one of a table
+// keeps it.
+template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int C, int S>
 struct Up {
   using M = Mix<W, X>;
   using V = typename M::V;
   using XV = typename M::XV;
-  using St = Stream<V, M::kRow>;
+  using St = Stream<V, M::row(MT * M::NX, SHIFT), SHIFT>;
   static constexpr int VB = M::VB, NX = M::NX, K = 4 * VB;   // per step
-  static constexpr int U = FAST ? St::kSteps : 4;            // steps a chunk
-  static constexpr int KC = U * K, kChunk = St::kChunk;
-  static constexpr int kParts = S * MT * 2 * 1024;
-  static constexpr int kLds =
-      FAST && S * 2 * kChunk > kParts ? S * 2 * kChunk : kParts;
+  static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
+  static constexpr int NS = 2 * C, BJ = 16 * C;
+  static constexpr int kParts = S * MT * NS * 1024;
+  static constexpr int kLds = std::max(S * 2 * kChunk, kParts);
 
   static __device__ void run(GivenMoe& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
     const int r = lane & 15, q = lane >> 4;
-    const unsigned tiles = (unsigned)((a.hidden + 15) / 16);
+    const unsigned tiles = (unsigned)((a.hidden + BJ - 1) / BJ);
     const unsigned id = uniform(blockIdx.x / tiles);
-    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * 16;
+    const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * BJ;
     const int table = uniform(id / a.most), at = uniform(id % a.most);
     Task task;
     const Choice choice(lds + kLds, a.tokens * a.top,
@@ -525,22 +677,37 @@ struct Up {
     } else {
       if (!task.find(a, table, at)) return;
     }
-    const int rank = task.rank, count = task.count;
-    const size_t origin =
-        ((size_t)task.expert * a.xw + j0 * a.ldw) * sizeof(V);
-    const char* base[2] = {uniform((const char*)a.w[0][rank] + origin),
-                           uniform((const char*)a.w[1][rank] + origin)};
-    const int left = a.hidden - j0 < 16 ? (int)(a.hidden - j0) : 16;
-
+    const int count = task.count;
+    // set n: gate (even) or up, of columns n / 2 * 16 .. (past the last one: that
+    // one, and no results)
+    const char* base[NS];
+    int left[NS], off[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      size_t j = j0 + n / 2 * 16;
+      if (j >= a.hidden) j = a.hidden - 1;
+      base[n] = uniform(
+          (const char*)a.w[n & 1][task.rank] +
+          ((size_t)task.expert * a.xw + j * a.ldw) * sizeof(V));
+      left[n] = a.hidden - j < 16 ? (int)(a.hidden - j) : 16;
+      off[n] = St::offset(base[n], a.ldw, left[n], r);
+    }
     const unsigned chunks = (unsigned)((a.in + KC - 1) / KC);
     const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
                    c1 = uniform((unsigned)((uint64_t)chunks * (wave + 1) / S));
     const uint32_t mine =
         uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
+    LDS char* const src = lds + wave * (2 * kChunk);
+    auto ask = [&](int n, unsigned c, int buf) {
+      St::ask(base[n], a.ldw, left[n], a.in, c, uniform(mine + buf * kChunk),
+              lane);
+    };
     for (int i0 = 0; i0 < count; i0 += MT * 16) {
       const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
-      if constexpr (FAST)
-        if (c0 < c1) St::ask(base[0], a.ldw, left, a.in, c0, mine, lane);
+      if (c0 < c1) {
+        ask(0, c0, 0);
+        ask(1, c0, 1);
+      }
       const XV* x[MT];
       int pair[MT];
 #pragma unroll
@@ -551,122 +718,90 @@ struct Up {
           pair[m] = choice.list[choice.record->first + i0 + i];
         else
           pair[m] = task.list[i0 + i];
-        x[m] = (const XV*)a.x[rank] + (size_t)(pair[m] / a.top) * a.ldx +
-               q * VB;
+        x[m] = (const XV*)a.x[task.rank] + (size_t)(pair[m] / a.top) * a.ldx +
+               q * M::E;
       }
-      f32x4 acc[MT][2] = {};
-      if constexpr (FAST)
-        stream(a, base, left, c0, c1, lds, wave, lane, x, here, acc);
-      else
-        fetch(a, base, left, c0, c1, lane, x, here, acc);
-      finish(a, task, pair, here, j0, lds, wave, lane, acc);
-      if (i0 + MT * 16 < count) __syncthreads();
-    }
-  }
-
-  static __device__ void stream(GivenMoe& a, const char* const (&base)[2],
-                                int left, unsigned c0, unsigned c1,
-                                LDS char* lds, int wave, int lane,
-                                const XV* const (&x)[MT], int here,
-                                f32x4 (&acc)[MT][2]) {
-    const int r = lane & 15, q = lane >> 4;
-    const uint32_t mine =
-        uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
-    LDS char* const src = lds + wave * (2 * kChunk);
-#pragma unroll 1
-    for (unsigned c = c0; c < c1; ++c) {
+      f32x4 acc[MT][NS] = {};
       i32x4 fx[MT][U][NX];
+      auto load = [&](unsigned c) {
+        const int rest = rest_of<St>(a.in, c);
+        auto all = [&](auto whole) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        if (m == 0 || m * 16 < here) {
+          for (int m = 0; m < MT; ++m)
+            if (m == 0 || m * 16 < here) {
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const size_t k = (size_t)c * KC + u * K;
-            fetch_row<true>(x[m] + k, (long)a.in - (long)(k + q * VB),
-                            fx[m][u]);
-          }
+              for (int u = 0; u < U; ++u)
+                fetch_row<whole.value>(x[m] + (size_t)c * KC + u * K,
+                                       rest - u * K - q * M::E, fx[m][u]);
+            }
+        };
+        if (!SHIFT || rest == KC) {
+          all(Yes());
+        } else if (a.in >= M::E) {
+          all(No());
+        } else {
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+              for (int n = 0; n < NX; ++n)
+                fx[m][u][n] = u == 0 && n == 0 && q == 0
+                                  ? load_piece<XV>(x[m], a.in)
+                                  : i32x4{0, 0, 0, 0};
         }
+      };
+      auto pin = [&] {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        landed<0>();                      // (x too)
-        if (n == 0)
-          St::ask(base[1], a.ldw, left, a.in, c, mine + kChunk, lane);
-        else if (c + 1 < c1)
-          St::ask(base[0], a.ldw, left, a.in, c + 1, mine, lane);
+        for (int m = 0; m < MT; ++m)
+          if (m == 0 || m * 16 < here) arrived(fx[m]);
+      };
+      auto use = [&](int n, unsigned c, int buf) {
+        const int rest = rest_of<St>(a.in, c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const i32x4 w = St::take(src + n * kChunk, u, r, q);
+          const i32x4 w =
+              St::take(src + buf * kChunk, u, r, q, off[n], rest);
 #pragma unroll
           for (int m = 0; m < MT; ++m)
             if (m == 0 || m * 16 < here)
               acc[m][n] = M::up(w, fx[m][u], acc[m][n]);
         }
-      }
-    }
-    if (S > 1) __syncthreads();
-  }
-
-  // The same for rows of any alignment, by way of registers.
-  static __device__ void fetch(GivenMoe& a, const char* const (&base)[2],
-                               int left, unsigned c0, unsigned c1, int lane,
-                               const XV* const (&x)[MT], int here,
-                               f32x4 (&acc)[MT][2]) {
-    const int r = lane & 15, q = lane >> 4, row = r < left ? r : left - 1;
-    const V* w[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-      w[n] = (const V*)base[n] + (size_t)row * a.ldw + q * VB;
-#pragma unroll 1
-    for (unsigned c = c0; c < c1; ++c) {
-      i32x4 fw[U][2], fx[MT][U][NX];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const size_t k = (size_t)c * KC + u * K;
-        const long rest = (long)a.in - (long)(k + q * VB);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) fw[u][n] = load_piece<V>(w[n] + k, rest);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-          if (m == 0 || m * 16 < here)
-            fetch_row<false>(x[m] + k, rest, fx[m][u]);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-            if (m == 0 || m * 16 < here)
-              acc[m][n] = M::up(fw[u][n], fx[m][u], acc[m][n]);
+      };
+      sweep<NS, St::kLoads>(c0, c1, load, pin, ask, use);
+      if (S > 1) __syncthreads();
+      finish(a, task, pair, here, j0, lds, wave, lane, acc);
+      if (i0 + MT * 16 < count) __syncthreads();
     }
   }
 
-  // Adds the wavefronts' sums in their order; tile m is finished by wavefront m
-  // % S: h of 16 pairs and 16 columns, zeros past the last column.
+  // Adds the wavefronts' sums in their order; of the results' MT * C tiles of 16
+  // pairs and 16 columns wavefront w finishes those w, w + S ..
   static __device__ void finish(GivenMoe& a, const Task& task,
                                 const int (&pairs)[MT], int here, size_t j0,
                                 LDS char* lds, int wave, int lane,
-                                const f32x4 (&acc)[MT][2]) {
+                                const f32x4 (&acc)[MT][NS]) {
     const int r = lane & 15, q = lane >> 4;
-    auto part = (f32x4(LDS*)[MT * 2][64])lds;
+    auto part = (f32x4(LDS*)[MT * NS][64])lds;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int n = 0; n < 2; ++n) part[wave][m * 2 + n][lane] = acc[m][n];
+      for (int n = 0; n < NS; ++n) part[wave][m * NS + n][lane] = acc[m][n];
     if (S > 1)
       __syncthreads();
     else
       in_order();
-    const size_t j = j0 + q * 4;
 #pragma unroll 1
-    for (int m = wave; m * 16 < here; m += S) {
-      f32x4 g = part[0][m * 2][lane], u = part[0][m * 2 + 1][lane];
+    for (int x = wave; x < MT * C; x += S) {
+      const int m = x / C, i = m * 16 + r, from = m * NS + x % C * 2;
+      const size_t j = j0 + x % C * 16 + q * 4;
+      if (m * 16 >= here || j >= held_of(a)) continue;
+      f32x4 g = part[0][from][lane], u = part[0][from + 1][lane];
 #pragma unroll
       for (int k = 1; k < S; ++k) {
-        g += part[k][m * 2][lane];
-        u += part[k][m * 2 + 1][lane];
+        g += part[k][from][lane];
+        u += part[k][from + 1][lane];
       }
-      const int i = m * 16 + r;
       if (i >= here) continue;
       float h[4];
 #pragma unroll
@@ -694,27 +829,23 @@ struct Up {
 #pragma unroll
       for (int k = 1; k < MT; ++k)
         if (m == k) one = pairs[k];
-      const size_t pair = one, groups = (a.hidden + 7) / 8;
       char* const row = task.work + a.at.hidden;
       if constexpr (M::kWhole) {
         f32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = h[e];
-        if (j / 8 < groups)
-          *(f32x4*)(row + (pair * groups * 8 + j) * 4) = v;
+        *(f32x4*)(row + ((size_t)one * runs_of(a) * 32 + j) * 4) = v;
+      } else if (a.planes == 2) {
+        put<2>(row, (size_t)one * runs_of(a) + j / 32, j % 32, h);
       } else {
-        if (j / 8 >= groups) continue;
-        if (a.planes == 2)
-          put<2>(row, pair * groups + j / 8, j % 8, h);
-        else
-          put<3>(row, pair * groups + j / 8, j % 8, h);
+        put<3>(row, (size_t)one * runs_of(a) + j / 32, j % 32, h);
       }
     }
   }
 
-  // Four values in their group of 8: [group][part][value].
+  // Four values in their run of 32: [run][part][value].
   template <int P>
-  static __device__ void put(char* to, size_t group, size_t first,
+  static __device__ void put(char* to, size_t run, size_t first,
                              const float (&h)[4]) {
     unsigned short part[4][P];
 #pragma unroll
@@ -726,29 +857,54 @@ struct Up {
       for (int e = 0; e < 4; ++e) v[e] = part[e][p];
       long all;
       __builtin_memcpy(&all, v, 8);
-      *(long*)(to + ((group * P + p) * 8 + first) * 2) = all;
+      *(long*)(to + ((run * P + p) * 32 + first) * 2) = all;
     }
   }
 };
 
 // ---------------------------------------------------------------- down
 
+// A lane group's hidden values of a step, from value k (of the step's first run)
+// of a row of `hidden` on: zeros past what is held.
+template <typename M, int P>
+__device__ inline void fetch_hidden(const char* row, size_t k, size_t held,
+                                    int q, i32x4 (&h)[M::parts(P)]) {
+  if constexpr (M::kWhole) {
+    const size_t at = k + q * 4;
+    h[0] = at < held ? *(const i32x4*)(row + at * 4) : i32x4{0, 0, 0, 0};
+  } else {
+#pragma unroll
+    for (int g = 0; g < M::VB / 8; ++g) {
+      const size_t at = k + g * 32 + q * 8;
+      const char* from = row + (k / 32 + g) * (P * 64) + q * 16;
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        h[g * P + p] =
+            at < held ? *(const i32x4*)(from + p * 64) : i32x4{0, 0, 0, 0};
+    }
+  }
+}
+// Bytes of a row of hidden values.
+template <typename M, int P>
+__device__ inline size_t hidden_bytes(GivenMoe& a) {
+  return runs_of(a) * 32 * (M::kWhole ? 4 : 2 * P);
+}
+
 // weight * (wd h) of the pairs that chose an expert: a workgroup takes 16 * NW
 // columns (rows of wd) of one chosen expert, its S wavefronts a part of the
 // contraction each; MT tiles of 16 pairs at a time.  The NW sets of 16 rows take
 // turns and share the hidden values in registers: P parts of 16 bits each, they
 // are P n / 16 NW times the weights' bytes with n pairs, and come from L2.
-template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
+template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V, M::kRow>;
+  using St = Stream<V, M::row(MT * M::parts(P), SHIFT), SHIFT>;
   static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
-  static constexpr int U = FAST ? St::kSteps : 4;
-  static constexpr int KC = U * K, kChunk = St::kChunk, BJ = 16 * NW;
+  static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk,
+                       BJ = 16 * NW;
   static constexpr int kParts = S * MT * NW * 1024;
-  static constexpr int kLds =
-      FAST && S * 2 * kChunk > kParts ? S * 2 * kChunk : kParts;
+  static constexpr int kLds = std::max(S * 2 * kChunk, kParts);
 
   static __device__ void run(GivenMoe& a, LDS char* lds) {
     const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
@@ -761,17 +917,18 @@ struct Down {
     const int rank = task.rank, expert = task.expert, count = task.count;
     const int* list = task.list;
     const char* hidden = task.work + a.at.hidden;
-    const size_t groups = (a.hidden + 7) / 8;
+    const size_t held = held_of(a);
 
     // (sets past the last row: that row, and no results)
     const char* base[NW];
-    int left[NW];
+    int left[NW], off[NW];
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
       const size_t j = j0 + n * 16 < a.in ? j0 + n * 16 : a.in - 1;
       left[n] = a.in - j < 16 ? (int)(a.in - j) : 16;
       base[n] = uniform((const char*)a.w[2][rank] +
                         ((size_t)expert * a.xd + j * a.ldd) * sizeof(V));
+      off[n] = St::offset(base[n], a.ldd, left[n], r);
     }
     const unsigned chunks = (unsigned)((a.hidden + KC - 1) / KC);
     const unsigned c0 = uniform((unsigned)((uint64_t)chunks * wave / S)),
@@ -779,85 +936,54 @@ struct Down {
     const uint32_t mine =
         uniform((uint32_t)(uintptr_t)lds + wave * (2 * kChunk));
     LDS char* const src = lds + wave * (2 * kChunk);
-
+    auto ask = [&](int n, unsigned c, int buf) {
+      St::ask(base[n], a.ldd, left[n], a.hidden, c,
+              uniform(mine + buf * kChunk), lane);
+    };
     for (int i0 = 0; i0 < count; i0 += MT * 16) {
       const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
-      if constexpr (FAST)
-        if (c0 < c1) St::ask(base[0], a.ldd, left[0], a.hidden, c0, mine, lane);
-      size_t pair[MT];
+      if (c0 < c1) {
+        ask(0, c0, 0);
+        ask(1, c0, 1);
+      }
+      const char* row[MT];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         int i = m * 16 + r;
         if (i >= here) i = here - 1;
-        pair[m] = (size_t)list[i0 + i] * groups;
+        row[m] = hidden + (size_t)list[i0 + i] * hidden_bytes<M, P>(a);
       }
       f32x4 acc[MT][NW] = {};
-      int buf = 0;
-#pragma unroll 1
-      for (unsigned c = c0; c < c1; ++c) {
-        i32x4 h[MT][U][N];
+      i32x4 h[MT][U][N];
+      auto load = [&](unsigned c) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
           if (m == 0 || m * 16 < here) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const size_t k = (size_t)c * KC + u * K + q * VB;
-              if constexpr (M::kWhole) {
-                h[m][u][0] = k < groups * 8
-                                 ? *(const i32x4*)(hidden +
-                                                   (pair[m] * 8 + k) * 4)
-                                 : i32x4{0, 0, 0, 0};
-              } else {
-#pragma unroll
-                for (int g = 0; g < VB / 8; ++g) {
-                  const size_t group = k / 8 + g;
-                  const i32x4* from =
-                      (const i32x4*)hidden + (pair[m] + group) * P;
-#pragma unroll
-                  for (int p = 0; p < P; ++p)
-                    h[m][u][g * P + p] =
-                        group < groups ? from[p] : i32x4{0, 0, 0, 0};
-                }
-              }
-            }
+            for (int u = 0; u < U; ++u)
+              fetch_hidden<M, P>(row[m], (size_t)c * KC + u * K, held, q,
+                                 h[m][u]);
           }
+      };
+      auto pin = [&] {
 #pragma unroll
-        for (int n = 0; n < NW; ++n) {
-          i32x4 w[FAST ? 1 : U];
-          if constexpr (FAST) {
-            landed<0>();                    // (h too)
-            const uint32_t to = uniform(mine + (buf ^ 1) * kChunk);
-            if (n + 1 < NW)
-              St::ask(base[(n + 1) % NW], a.ldd, left[(n + 1) % NW], a.hidden,
-                      c, to, lane);
-            else if (c + 1 < c1)
-              St::ask(base[0], a.ldd, left[0], a.hidden, c + 1, to, lane);
-          } else {
-            const int row = r < left[n] ? r : left[n] - 1;
-            const V* at = (const V*)base[n] + (size_t)row * a.ldd;
+        for (int m = 0; m < MT; ++m)
+          if (m == 0 || m * 16 < here) arrived(h[m]);
+      };
+      auto use = [&](int n, unsigned c, int buf) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const size_t k = (size_t)c * KC + u * K + q * VB;
-              w[u] = load_piece<V>(at + k, (long)a.hidden - (long)k);
-            }
-          }
+        for (int u = 0; u < U; ++u) {
+          const i32x4 v = St::take(src + buf * kChunk, u, r, q, off[n],
+                                   rest_of<St>(a.hidden, c));
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            i32x4 v;
-            if constexpr (FAST)
-              v = St::take(src + buf * kChunk, u, r, q);
-            else
-              v = w[u];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-              if (m == 0 || m * 16 < here)
-                acc[m][n] = M::template down<P>(v, h[m][u], acc[m][n]);
-          }
-          buf ^= 1;
+          for (int m = 0; m < MT; ++m)
+            if (m == 0 || m * 16 < here)
+              acc[m][n] = M::template down<P>(v, h[m][u], acc[m][n]);
         }
-      }
+      };
+      sweep<NW, St::kLoads>(c0, c1, load, pin, ask, use);
       // the wavefronts' sums in their order
-      if (FAST && S > 1) __syncthreads();
+      if (S > 1) __syncthreads();
       auto part = (f32x4(LDS*)[MT * NW][64])lds;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -898,11 +1024,11 @@ struct Down {
 // and one in the lower 8 of the matrix cores' rows, their pairs in the left and
 // right 8 columns: of the product the two blocks that belong together count.
 // A token's sums stay in LDS, a wavefront's own, and are joined in order.
-template <Type W, Type X, int P>
+template <Type W, Type X, bool SHIFT, int P>
 struct DownSmall {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V, M::kRow>;
+  using St = Stream<V, M::row(M::parts(P), SHIFT), SHIFT>;
   static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
   static constexpr int S = 8, kMost = kSmall * kTop;     // pairs
@@ -929,22 +1055,31 @@ struct DownSmall {
     const int pairs = a.tokens * a.top;
     char* const work = table_of(a, a.tables == 1 ? 0 : rank);
     const char* hidden = work + a.at.hidden;
-    const size_t groups = (a.hidden + 7) / 8;
+    const size_t held = held_of(a);
 
     // the table's lists in LDS
     LDS Record* const records = (LDS Record*)(lds + kRecords);
     LDS int* const list = (LDS int*)(lds + kList);
     LDS float* const weights = (LDS float*)(lds + kWeights);
     LDS float* const mine = (LDS float*)(lds + kSums) + wave * (kSmall * 8);
+    // (a.most * 4 <= 512 threads, and pairs are fewer; all loads go out at once)
+    static_assert(kMost * 4 <= S * 64);
     const int* starts = (const int*)work + 1 + rank;
-    const int low = uniform(starts[0]), high = uniform(starts[1]);
-    for (int i = t; i < a.most * 4; i += S * 64)
-      ((LDS int*)records)[i] = ((const int*)(work + a.at.records))[i];
-    for (int i = t; i < pairs; i += S * 64) {
-      list[i] = ((const int*)(work + a.at.pairs))[i];
-      weights[i] = ((const float*)(work + a.at.weights))[i];
+    const int low1 = starts[0], high1 = starts[1];
+    int word = 0, one = 0;
+    float share = 0.f;
+    if (t < a.most * 4) word = ((const int*)(work + a.at.records))[t];
+    if (t < pairs) {
+      one = ((const int*)(work + a.at.pairs))[t];
+      share = ((const float*)(work + a.at.weights))[t];
+    }
+    ((LDS int*)records)[t] = word;
+    if (t < kMost) {
+      list[t] = one;
+      weights[t] = share;
     }
     mine[lane] = 0.f;
+    const int low = uniform(low1), high = uniform(high1);
     __syncthreads();
 
     const unsigned chunks = (unsigned)((a.hidden + KC - 1) / KC);
@@ -974,13 +1109,13 @@ struct DownSmall {
         if (x.unit < x.end) set(x);
       }
     };
+    auto base = [&](const Half& x) {
+      return uniform((const char*)a.w[2][rank] +
+                     ((size_t)x.expert * a.xd + j0 * a.ldd) * sizeof(V));
+    };
     // (a half that is through, the second one of an odd number, stays where it
     // is: its block of the product is left out)
     auto ask = [&](const Half (&x)[2], int buf) {
-      auto base = [&](const Half& y) {
-        return uniform((const char*)a.w[2][rank] +
-                       ((size_t)y.expert * a.xd + j0 * a.ldd) * sizeof(V));
-      };
       const uint32_t to = uniform(buffer + buf * kChunk);
       St::template ask<0, 8>(base(x[0]), a.ldd, left, a.hidden, x[0].chunk, to,
                              lane);
@@ -994,26 +1129,13 @@ struct DownSmall {
       const unsigned chunk = side ? x[1].chunk : x[0].chunk;
       const bool some = side ? x[1].unit < x[1].end : true;
       const int i = (r & 7) < count ? r & 7 : count - 1;
-      const size_t pair = some ? (size_t)list[first + i] * groups : 0;
+      const char* row =
+          hidden + (some ? (size_t)list[first + i] : 0) *
+                       hidden_bytes<M, P>(a);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const size_t k = (size_t)chunk * KC + u * K + q * VB;
-        if constexpr (M::kWhole) {
-          h[u][0] = some && k < groups * 8
-                        ? *(const i32x4*)(hidden + (pair * 8 + k) * 4)
-                        : i32x4{0, 0, 0, 0};
-        } else {
-#pragma unroll
-          for (int g = 0; g < VB / 8; ++g) {
-            const size_t group = k / 8 + g;
-            const i32x4* from = (const i32x4*)hidden + (pair + group) * P;
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-              h[u][g * P + p] =
-                  some && group < groups ? from[p] : i32x4{0, 0, 0, 0};
-          }
-        }
-      }
+      for (int u = 0; u < U; ++u)
+        fetch_hidden<M, P>(row, (size_t)chunk * KC + u * K, some ? held : 0, q,
+                           h[u]);
     };
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     // Adds one half's sums to its tokens': lane (r, q): pair r % 8, columns q %
@@ -1041,34 +1163,43 @@ struct DownSmall {
     if (turns) {
       start(now[0], u0, u0 + turns);
       start(now[1], u0 + turns, u1);
-      i32x4 h[2][U][N];
-      ask(now, 0);
-      fetch(now, h[0]);
-      // one turn: the next one's loads go out before this one's products
-      auto turn = [&](unsigned k, int buf, i32x4 (&h)[U][N],
-                      i32x4 (&then)[U][N]) {
-        landed<0>();
-        const Half was[2] = {now[0], now[1]};
-        step(now[0]);
-        step(now[1]);
-        if (k + 1 < turns) {
-          ask(now, buf ^ 1);
-          fetch(now, then);
-        }
+      // two turns at a time: both are asked for at once
+      auto turn = [&](const Half (&was)[2], const Half (&then)[2], int buf,
+                      i32x4 (&h)[U][N]) {
+        const Half& own = side ? was[1] : was[0];
+        const int off = St::offset(side ? base(was[1]) : base(was[0]), a.ldd,
+                                   left, r & 7);
+        const int rest = rest_of<St>(a.hidden, own.chunk);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          acc = M::template down<P>(St::take(src + buf * kChunk, u, r, q),
-                                    h[u], acc);
+          acc = M::template down<P>(
+              St::take(src + buf * kChunk, u, r, q, off, rest), h[u], acc);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
           if (was[s].unit < was[s].end &&
-              (now[s].unit == now[s].end || now[s].chunk == 0))
+              (then[s].unit == then[s].end || then[s].chunk == 0))
             flush(was[s], s);
       };
 #pragma unroll 1
       for (unsigned k = 0; k < turns; k += 2) {
-        turn(k, 0, h[0], h[1]);
-        if (k + 1 < turns) turn(k + 1, 1, h[1], h[0]);
+        i32x4 h[2][U][N];
+        const bool two = k + 1 < turns;
+        const Half one[2] = {now[0], now[1]};
+        ask(now, 0);
+        fetch(now, h[0]);
+        step(now[0]);
+        step(now[1]);
+        const Half other[2] = {now[0], now[1]};
+        if (two) {
+          ask(now, 1);
+          fetch(now, h[1]);
+          step(now[0]);
+          step(now[1]);
+        }
+        landed<0>();
+        turn(one, other, 0, h[0]);
+        if (two) turn(other, now, 1, h[1]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
     }
     __syncthreads();
@@ -1126,25 +1257,25 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
 
 // ---------------------------------------------------------------- launches
 
-template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
-__global__ __launch_bounds__(S * 64) void k_moe_up(MoeArgs) {
+template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int C, int S>
+__global__ __launch_bounds__(S * 64, 2) void k_moe_up(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Up<W, X, FAST, FUSED, MT, S>::run(a, (LDS char*)lds);
+  Up<W, X, SHIFT, FUSED, MT, C, S>::run(a, (LDS char*)lds);
 }
 
-template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
-__global__ __launch_bounds__(S * 64) void k_moe_down(MoeArgs) {
+template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
+__global__ __launch_bounds__(S * 64, 2) void k_moe_down(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Down<W, X, FAST, P, MT, NW, S>::run(a, (LDS char*)lds);
+  Down<W, X, SHIFT, P, MT, NW, S>::run(a, (LDS char*)lds);
 }
 
-template <Type W, Type X, int P>
+template <Type W, Type X, bool SHIFT, int P>
 __global__ __launch_bounds__(512) void k_moe_down_small(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  DownSmall<W, X, P>::run(a, (LDS char*)lds);
+  DownSmall<W, X, SHIFT, P>::run(a, (LDS char*)lds);
 }
 
 template <void (*K)(MoeArgs)>
@@ -1171,31 +1302,32 @@ hipError_t launch_moe(const MoeArgs& a, size_t groups, int threads,
   return hipGetLastError();
 }
 
-template <Type W, Type X, bool FAST, bool FUSED, int MT, int S>
+template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int S>
 hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
-  using K = Up<W, X, FAST, FUSED, MT, S>;
+  constexpr int C = columns_up(W, FUSED, MT);
+  using K = Up<W, X, SHIFT, FUSED, MT, C, S>;
   const int more =
       FUSED ? Choice::bytes(a.tokens * a.top,
                             a.experts * (a.tables == 1 ? a.ranks : 1))
             : 0;
-  return launch_moe<k_moe_up<W, X, FAST, FUSED, MT, S>>(
-      a, (a.hidden + 15) / 16 * a.most * a.tables, S * 64, K::kLds + more,
-      stream);
+  return launch_moe<k_moe_up<W, X, SHIFT, FUSED, MT, C, S>>(
+      a, (a.hidden + K::BJ - 1) / K::BJ * a.most * a.tables, S * 64,
+      K::kLds + more, stream);
 }
 
 template <Type W, Type X, bool FUSED, int MT>
 hipError_t waves_up(const MoeArgs& a, hipStream_t stream) {
+  if (!a.fast[0]) return go_up<W, X, true, FUSED, MT, 4>(a, stream);
   switch (a.waves[0]) {
-    case 8: return go_up<W, X, true, FUSED, MT, 8>(a, stream);
-    case 4: return go_up<W, X, true, FUSED, MT, 4>(a, stream);
-    case 2: return go_up<W, X, true, FUSED, MT, 2>(a, stream);
+    case 8: return go_up<W, X, false, FUSED, MT, 8>(a, stream);
+    case 4: return go_up<W, X, false, FUSED, MT, 4>(a, stream);
+    case 2: return go_up<W, X, false, FUSED, MT, 2>(a, stream);
   }
   return hipErrorInvalidConfiguration;
 }
 
 template <Type W, Type X>
 hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
-  if (!a.fast[0]) return go_up<W, X, false, false, 4, 4>(a, stream);
   if (a.fused) return waves_up<W, X, true, 1>(a, stream);
   switch (a.tiles[0]) {
     case 1: return waves_up<W, X, false, 1>(a, stream);
@@ -1205,27 +1337,38 @@ hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
   return hipErrorInvalidConfiguration;
 }
 
-template <Type W, Type X, bool FAST, int P, int MT, int NW, int S>
+template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
 hipError_t go_down(const MoeArgs& a, hipStream_t stream) {
-  using K = Down<W, X, FAST, P, MT, NW, S>;
-  return launch_moe<k_moe_down<W, X, FAST, P, MT, NW, S>>(
+  using K = Down<W, X, SHIFT, P, MT, NW, S>;
+  return launch_moe<k_moe_down<W, X, SHIFT, P, MT, NW, S>>(
       a, (a.in + K::BJ - 1) / K::BJ * a.most * a.tables, S * 64, K::kLds,
       stream);
 }
 
+template <Type W, Type X, bool SHIFT, int P>
+hipError_t go_small(const MoeArgs& a, hipStream_t stream) {
+  return launch_moe<k_moe_down_small<W, X, SHIFT, P>>(
+      a, (a.in + 7) / 8 * a.ranks, 512, DownSmall<W, X, SHIFT, P>::kLds,
+      stream);
+}
+
+template <Type W, Type X, int P, int MT>
+hipError_t waves_down(const MoeArgs& a, hipStream_t stream) {
+  if (!a.fast[1])
+    return a.sets == 2 ? go_down<W, X, true, P, MT, 2, 4>(a, stream)
+                       : go_down<W, X, true, P, MT, 4, 4>(a, stream);
+  if (a.sets == 2) return go_down<W, X, false, P, MT, 2, 4>(a, stream);
+  return a.waves[1] == 4 ? go_down<W, X, false, P, MT, 4, 4>(a, stream)
+                         : go_down<W, X, false, P, MT, 4, 2>(a, stream);
+}
+
 template <Type W, Type X, int P>
 hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
-  if (a.small) {
-    using K = DownSmall<W, X, P>;
-    return launch_moe<k_moe_down_small<W, X, P>>(
-        a, (a.in + 7) / 8 * a.ranks, 512, K::kLds, stream);
-  }
-  if (!a.fast[1]) return go_down<W, X, false, P, 2, 2, 4>(a, stream);
-  if (a.tiles[1] == 1)
-    return a.waves[1] == 4 ? go_down<W, X, true, P, 1, 4, 4>(a, stream)
-                           : go_down<W, X, true, P, 1, 4, 2>(a, stream);
-  return a.waves[1] == 4 ? go_down<W, X, true, P, 2, 4, 4>(a, stream)
-                         : go_down<W, X, true, P, 2, 4, 2>(a, stream);
+  if (a.small)
+    return a.fast[1] ? go_small<W, X, false, P>(a, stream)
+                     : go_small<W, X, true, P>(a, stream);
+  return a.tiles[1] == 1 ? waves_down<W, X, P, 1>(a, stream)
+                         : waves_down<W, X, P, 2>(a, stream);
 }
 
 template <Type W, Type X>

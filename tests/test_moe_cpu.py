@@ -135,11 +135,11 @@ def test_workspace():
     for k in (0, 1, 4, 8, 9, 10, 11):
         assert _moe(ws=_at(k)[1] - n + 16, n=n) == ALIAS
     assert dpar.dpar_moe_workspace(1, _opt(tokens=0)) == 0
-    # a choice, its records, and three 16-bit parts of every hidden value
-    small = dpar.dpar_moe_workspace(1, _opt(hidden=1024))
-    assert 15 * 1024 * 4 <= small <= 15 * 1024 * 4 + 2048
-    large = dpar.dpar_moe_workspace(1, _opt(hidden=1024, out_dtype="float32"))
-    assert large - small == 15 * 1024 * 2
+    # two 16-bit parts of every hidden value, three where y has 32 bits
+    for out, parts in (("bfloat16", 2), ("float32", 3)):
+        one, two = (dpar.dpar_moe_workspace(1, _opt(hidden=h, out_dtype=out))
+                    for h in (1024, 2048))
+        assert two - one == 15 * 1024 * 2 * parts
     f = dpar.lib().dpar_moe_workspace
     assert f(1, ctypes.byref(_opt()), None) == INVALID
     assert f(1, None, None) == INVALID
