@@ -16,10 +16,13 @@ enum class Route : int { SOFTMAX = 0, SIGMOID = 1 };
 constexpr int kRanks = 32;
 constexpr int kTokens = 128, kTop = 16, kExperts = 1024;
 constexpr int kSmall = 8;      // tokens of the kernels for the fewest
-// Sets of 16 columns of a workgroup of up.  With two, activations are read half
-// as often: 8-bit weights are no more bytes than the activations of 16 pairs.
-constexpr int columns_up(Type w, bool fused, int tiles) {
-  return !fused && (w == Type::I8 || tiles > 1) ? 2 : 1;
+// Sets of 16 columns of a workgroup of up, which share the activations: as many
+// as let those be half of the loads (8-bit weights are half the bytes), and as
+// the registers have sums for (shift: rows off 16 bytes, which need some too).
+constexpr int columns_up(Type w, bool fused, bool shift, int tiles) {
+  if (fused) return 1;
+  const int n = w != Type::I8 ? tiles : tiles < 4 ? 2 * tiles : 2;
+  return shift && n > 2 ? 2 : n;
 }
 
 // An expert that some token chose: its rank of the launch, its number there, and

@@ -209,7 +209,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   // Tiles of 16 pairs at a time, by an expert's share of them; more take another
   // turn over its matrices.
   const size_t mean = o.tokens * top / c.all;
-  a.tiles[0] = mean <= 8 ? 1 : mean <= 24 ? 2 : 4;
+  a.tiles[0] = mean <= 8 ? 1 : mean <= 24 || !a.fast[0] ? 2 : 4;
   a.tiles[1] = mean <= 8 ? 1 : 2;
   const size_t blocks = o.tokens <= (size_t)moe::kSmall
                             ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
@@ -217,10 +217,11 @@ int moe_impl(const void* const* x, const void* const* logits,
             (o.hidden + 15) / 16 * blocks <= (size_t)cus * 4;
   a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
             (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1);
-  const size_t up = 16 * moe::columns_up(c.w, a.fused, a.tiles[0]);
+  const size_t up = 16 * moe::columns_up(c.w, a.fused, !a.fast[0],
+                                               a.tiles[0]);
   a.waves[0] = waves_of((o.hidden + up - 1) / up * chosen, o.in * c.ew / 512,
                         cus);
-  a.sets = (o.in + 63) / 64 * chosen < (size_t)cus * 2 ? 2 : 4;
+  a.sets = (o.in + 63) / 64 * chosen < (size_t)cus * 3 / 2 ? 2 : 4;
   a.waves[1] = std::min(waves_of((o.in + 16 * a.sets - 1) / (16 * a.sets) *
                                      chosen, o.hidden * c.ew / 512, cus), 4);
   const size_t groups =

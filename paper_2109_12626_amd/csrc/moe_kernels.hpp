@@ -305,10 +305,10 @@ template <Type W, Type X> struct Mix {
   static constexpr int VB = 16 / (int)sizeof(V), E = 16 / (int)sizeof(XV);
   static constexpr int NX = VB / E;
   // Bytes of a row in a chunk: 512, or 256 where the activations of that many,
-  // `pieces` of each step, take more than 128 registers, and for SHIFT, which
-  // needs some for itself.
-  static constexpr int row(int pieces, bool shift) {
-    return shift || pieces * 8 * 4 > 128 ? 256 : 512;
+  // `pieces` of each step, and `sums` take more than 160 registers, and for
+  // SHIFT, which needs some for itself.
+  static constexpr int row(int pieces, int sums, bool shift) {
+    return shift || (pieces * 8 + sums) * 4 > 160 ? 256 : 512;
   }
   // hidden values: 32-bit ones as they are, else P parts of 16 bits
   static constexpr bool kWhole = X == Type::F32;
@@ -651,7 +651,7 @@ struct Up {
   using M = Mix<W, X>;
   using V = typename M::V;
   using XV = typename M::XV;
-  using St = Stream<V, M::row(MT * M::NX, SHIFT), SHIFT>;
+  using St = Stream<V, M::row(MT * M::NX, MT * C * 2, SHIFT), SHIFT>;
   static constexpr int VB = M::VB, NX = M::NX, K = 4 * VB;   // per step
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
   static constexpr int NS = 2 * C, BJ = 16 * C;
@@ -899,7 +899,7 @@ template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V, M::row(MT * M::parts(P), SHIFT), SHIFT>;
+  using St = Stream<V, M::row(MT * M::parts(P), MT * NW, SHIFT), SHIFT>;
   static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk,
                        BJ = 16 * NW;
@@ -1028,7 +1028,9 @@ template <Type W, Type X, bool SHIFT, int P>
 struct DownSmall {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V, M::row(M::parts(P), SHIFT), SHIFT>;
+  // (of two turns; three parts of 512 bytes just fit)
+  static constexpr int kPieces = M::parts(P) * (M::parts(P) > 3 ? 2 : 1);
+  using St = Stream<V, M::row(kPieces, 1, SHIFT), SHIFT>;
   static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
   static constexpr int S = 8, kMost = kSmall * kTop;     // pairs
@@ -1304,7 +1306,7 @@ hipError_t launch_moe(const MoeArgs& a, size_t groups, int threads,
 
 template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int S>
 hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
-  constexpr int C = columns_up(W, FUSED, MT);
+  constexpr int C = columns_up(W, FUSED, SHIFT, MT);
   using K = Up<W, X, SHIFT, FUSED, MT, C, S>;
   const int more =
       FUSED ? Choice::bytes(a.tokens * a.top,
@@ -1317,7 +1319,8 @@ hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
 
 template <Type W, Type X, bool FUSED, int MT>
 hipError_t waves_up(const MoeArgs& a, hipStream_t stream) {
-  if (!a.fast[0]) return go_up<W, X, true, FUSED, MT, 4>(a, stream);
+  if constexpr (MT < 4)
+    if (!a.fast[0]) return go_up<W, X, true, FUSED, MT, 4>(a, stream);
   switch (a.waves[0]) {
     case 8: return go_up<W, X, false, FUSED, MT, 8>(a, stream);
     case 4: return go_up<W, X, false, FUSED, MT, 4>(a, stream);
@@ -1367,8 +1370,10 @@ hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
   if (a.small)
     return a.fast[1] ? go_small<W, X, false, P>(a, stream)
                      : go_small<W, X, true, P>(a, stream);
-  return a.tiles[1] == 1 ? waves_down<W, X, P, 1>(a, stream)
-                         : waves_down<W, X, P, 2>(a, stream);
+  // (three parts of a value beside 8-bit weights fill the registers with one)
+  if constexpr (W != Type::I8 || P < 3)
+    if (a.tiles[1] == 2) return waves_down<W, X, P, 2>(a, stream);
+  return waves_down<W, X, P, 1>(a, stream);
 }
 
 template <Type W, Type X>
