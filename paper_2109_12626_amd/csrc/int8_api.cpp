@@ -141,6 +141,9 @@ int quantize_impl(const void* const* x, void* const* q, void* const* scale,
   const int rc = check_mats(m, 3, p, call);
   if (rc || !o.rows) return rc;
   const int per = ranks_per_launch(p);
+  if (logs())
+    std::fprintf(stderr, "dpar: quantize %s ranks=%d rows=%zu cols=%zu\n",
+                 name_of((Type)type_code(o.dtype)), per, o.rows, o.cols);
   for (int r0 = 0; r0 < p; r0 += per) {
     QuantizeArgs a = {};
     a.rows = o.rows, a.cols = o.cols, a.ldx = o.ldx, a.ldq = o.ldq;

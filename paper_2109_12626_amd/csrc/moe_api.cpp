@@ -64,12 +64,12 @@ int check_moe(const char* call, int p, const dpar_moe_t* opt, Options* c) {
   for (size_t v : {o.ldx, o.ldl, o.ldw, o.ldd, o.ldy, o.ldr, o.xw, o.xd})
     if (v > kMostPitch)
       return fail(DPAR_ERR_UNSUPPORTED, "%s: a distance beyond 2^38", call);
+  // (16 rows of a matrix lie within the kernels' 32-bit offsets)
+  if (o.ldw >= kFastPitch || o.ldd >= kFastPitch)
+    return fail(DPAR_ERR_UNSUPPORTED, "%s: rows of the weights 2^23 values or "
+                "more apart", call);
   if (o.ldw < o.in || o.ldd < o.hidden)
     return fail(DPAR_ERR_INVALID_ARG, "%s: rows of the weights overlap", call);
-  if ((o.hidden && o.ldw > kMostBytes / o.hidden) ||
-      (o.in && o.ldd > kMostBytes / o.in))
-    return fail(DPAR_ERR_UNSUPPORTED, "%s: weights of 2^48 bytes or more",
-                call);
   if (!o.xw || o.experts <= 1) o.xw = o.hidden * o.ldw;
   if (!o.xd || o.experts <= 1) o.xd = o.in * o.ldd;
   return DPAR_SUCCESS;
@@ -110,13 +110,30 @@ moe::Layout layout_of(const Options& c, int p) {
   return l;
 }
 
-// Wavefronts per workgroup for a matrix of `chunks` chunks of 512 bytes a row,
-// with n workgroups that have work.
+// Wavefronts per workgroup, 2 or 4, for a matrix of `chunks` chunks of 512 bytes
+// a row, with n workgroups that have work: 4 for 16 or more chunks (8 experts
+// 4096 x 4096, 64 tokens: 143 us, 154 with 2), else where two do not fill the
+// card (100 tokens, 64 experts 2048 x 1024: 141 us, 144 with 4).
 int waves_of(size_t n, size_t chunks, int cus) {
-  if (chunks >= 16) return 4;
-  int w = 2;
-  while (w < 8 && chunks >= (size_t)w * 2 && n * w < (size_t)cus * 8) w *= 2;
-  return w;
+  return chunks >= 16 || (chunks >= 4 && n * 2 < (size_t)cus * 8) ? 4 : 2;
+}
+
+// DPAR_LOG=1: the layer, its choice and its kernels.
+void log_layer(const Options& c, const moe::Args& a, int ranks) {
+  std::fprintf(stderr,
+               "dpar: moe %s weights=%s ranks=%d tokens=%d in=%zu hidden=%zu "
+               "experts=%zu top=%d tables=%d choice=%s up=%dx%d waves=%d%s "
+               "down=",
+               name_of(c.t), name_of(c.w), ranks, a.tokens, a.in, a.hidden,
+               c.all, a.top, a.tables, a.fused ? "up" : "apart",
+               a.tiles[0] * 16,
+               16 * moe::columns_up(c.w, a.fused, !a.fast[0], a.tiles[0]),
+               a.waves[0], a.fast[0] ? "" : " unaligned");
+  if (a.small)
+    std::fprintf(stderr, "small%s\n", a.fast[1] ? "" : " unaligned");
+  else
+    std::fprintf(stderr, "%dx%d waves=%d%s\n", a.tiles[1] * 16, a.sets * 16,
+                 a.waves[1], a.fast[1] ? "" : " unaligned");
 }
 
 int moe_impl(const void* const* x, const void* const* logits,
@@ -196,34 +213,48 @@ int moe_impl(const void* const* x, const void* const* logits,
                           : logits[i] == logits[0]);
   a.tables = same ? 1 : per;
   a.most = most_of(o, same ? per : 1);
-  // weights of whole aligned pieces, 16 rows of them within 32-bit offsets
+  // weights of whole aligned pieces
   auto fast = [&](size_t cols, size_t ld, size_t far, int k0, int k1) {
     uintptr_t bits = cols * c.ew | ld * c.ew | (n > 1 ? far * c.ew : 0);
     for (int k = k0; k < k1; ++k)
       for (int i = 0; i < p; ++i) bits |= (uintptr_t)m[k].at[i];
-    return bits % 16 == 0 && ld < kFastPitch;
+    return bits % 16 == 0;
   };
   a.fast[0] = fast(o.in, o.ldw, o.xw, 2, 4);
   a.fast[1] = fast(o.hidden, o.ldd, o.xd, 4, 5);
   const size_t chosen = std::min(c.all, o.tokens * top);
   // Tiles of 16 pairs at a time, by an expert's share of them; more take another
-  // turn over its matrices.
+  // turn over its matrices (128 tokens, 2 of 8 experts: 202 us with 4, 233 with
+  // 2; 64 tokens: 148 with 2, 164 with 1).
   const size_t mean = o.tokens * top / c.all;
   a.tiles[0] = mean <= 8 ? 1 : mean <= 24 || !a.fast[0] ? 2 : 4;
   a.tiles[1] = mean <= 8 ? 1 : 2;
   const size_t blocks = o.tokens <= (size_t)moe::kSmall
                             ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
+  // Each workgroup of up may make the choice for itself: 1 token 2048 x 1024 of
+  // 64 experts 27 us, 30 with a launch for it; 8 tokens (4096 workgroups) 114
+  // and 98.
   a.fused = o.in && o.hidden && c.all <= 256 &&
             (o.hidden + 15) / 16 * blocks <= (size_t)cus * 4;
+  // Down by token, a workgroup per CU (8 tokens 97.7 us, by expert and joined
+  // 99; one token 27 and 31; 8 ranks, with 8 times the workgroups, 39 and 30).
   a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
             (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1);
+  if (a.fused) a.tiles[0] = 1;
   const size_t up = 16 * moe::columns_up(c.w, a.fused, !a.fast[0],
                                                a.tiles[0]);
   a.waves[0] = waves_of((o.hidden + up - 1) / up * chosen, o.in * c.ew / 512,
                         cus);
+  // Fewer columns where that fills the card: 20 experts 1001 x 501 36.0 us with
+  // 32 of them, 37.1 with 64; 8 experts 4001 x 4001 225 and 214.
   a.sets = (o.in + 63) / 64 * chosen < (size_t)cus * 3 / 2 ? 2 : 4;
-  a.waves[1] = std::min(waves_of((o.in + 16 * a.sets - 1) / (16 * a.sets) *
-                                     chosen, o.hidden * c.ew / 512, cus), 4);
+  a.waves[1] = waves_of((o.in + 16 * a.sets - 1) / (16 * a.sets) * chosen,
+                        o.hidden * c.ew / 512, cus);
+  // (rows off 16 bytes, and few columns, have one form each)
+  if (!a.fast[0]) a.waves[0] = 4;
+  if (!a.fast[1] || a.sets == 2) a.waves[1] = 4;
+  if (eight && a.planes == 3) a.tiles[1] = 1;
+  if (logs()) log_layer(c, a, per);
   const size_t groups =
       std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * a.most *
                    a.tables,

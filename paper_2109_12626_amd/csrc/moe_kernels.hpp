@@ -1321,23 +1321,16 @@ template <Type W, Type X, bool FUSED, int MT>
 hipError_t waves_up(const MoeArgs& a, hipStream_t stream) {
   if constexpr (MT < 4)
     if (!a.fast[0]) return go_up<W, X, true, FUSED, MT, 4>(a, stream);
-  switch (a.waves[0]) {
-    case 8: return go_up<W, X, false, FUSED, MT, 8>(a, stream);
-    case 4: return go_up<W, X, false, FUSED, MT, 4>(a, stream);
-    case 2: return go_up<W, X, false, FUSED, MT, 2>(a, stream);
-  }
-  return hipErrorInvalidConfiguration;
+  return a.waves[0] == 4 ? go_up<W, X, false, FUSED, MT, 4>(a, stream)
+                         : go_up<W, X, false, FUSED, MT, 2>(a, stream);
 }
 
 template <Type W, Type X>
 hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
   if (a.fused) return waves_up<W, X, true, 1>(a, stream);
-  switch (a.tiles[0]) {
-    case 1: return waves_up<W, X, false, 1>(a, stream);
-    case 2: return waves_up<W, X, false, 2>(a, stream);
-    case 4: return waves_up<W, X, false, 4>(a, stream);
-  }
-  return hipErrorInvalidConfiguration;
+  if (a.tiles[0] == 1) return waves_up<W, X, false, 1>(a, stream);
+  if (a.tiles[0] == 2) return waves_up<W, X, false, 2>(a, stream);
+  return waves_up<W, X, false, 4>(a, stream);
 }
 
 template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>

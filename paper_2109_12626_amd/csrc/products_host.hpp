@@ -561,6 +561,12 @@ inline void add_copy(dpar::products::CopyArgs* c, const Stored& m, int ranks,
   }
 }
 
+// Whether calls print their plans.
+inline bool logs() {
+  const char* log = std::getenv("DPAR_LOG");
+  return log && std::atoi(log) != 0;
+}
+
 // DPAR_LOG=1: one line per product on stderr with the kernel that runs.
 inline void log_plan(const Step& s, Type t, int ranks, const Plan& n) {
   static const char* forms[] = {"linear", "gated", "dx", "dw"};
@@ -591,8 +597,7 @@ int run_product(const char* call, Type t, int p, const Step& s, Args* a,
   const int per = ranks_per_launch(p);
   const Plan n = plan_of(s, t, per, cus, ws ? bytes : 0);
   const size_t e = size_of(t);
-  const char* log = std::getenv("DPAR_LOG");
-  if (log && std::atoi(log) != 0) log_plan(s, t, per, n);
+  if (logs()) log_plan(s, t, per, n);
   a->ni = s.ni, a->nj = s.nj, a->nc = s.nc;
   a->pairs = s.pairs;
   a->lda = n.copy_a ? n.ld_a : s.a.ld;

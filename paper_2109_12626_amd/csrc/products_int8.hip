@@ -8,22 +8,19 @@ namespace {
 using GivenCopy = const __attribute__((address_space(4))) CopyArgs;
 using GivenQuantize = const __attribute__((address_space(4))) QuantizeArgs;
 
-// One 16-byte piece per thread and turn, sizes in bytes.
+// A wavefront per row and turn, sizes in bytes.
 __global__ __launch_bounds__(256) void k_int8_copy(CopyArgs) {
   GivenCopy& a = *(GivenCopy*)__builtin_amdgcn_kernarg_segment_ptr();
   auto& job = a.job[blockIdx.z];
-  const int mat = blockIdx.y;
+  const int mat = blockIdx.y, lane = threadIdx.x % 64;
   if (mat >= job.mats) return;
   const signed char* from = (const signed char*)job.from[mat];
-  const size_t per = job.pitch / 16, all = per * job.rows;
   char* to = job.to + (size_t)mat * job.rows * job.pitch;
-  for (size_t id = (size_t)blockIdx.x * 256 + threadIdx.x; id < all;
-       id += (size_t)gridDim.x * 256) {
-    const size_t row = id / per, piece = id % per;
-    *(i32x4*)(to + id * 16) = load_piece<signed char>(
-        from + row * job.ld + piece * 16,
-        (long)job.cols - (long)piece * 16);
-  }
+  for (size_t row = (size_t)blockIdx.x * 4 + uniform(threadIdx.x / 64);
+       row < job.rows; row += (size_t)gridDim.x * 4)
+    for (size_t at = (size_t)lane * 16; at < job.pitch; at += 1024)
+      *(i32x4*)(to + row * job.pitch + at) = load_piece<signed char>(
+          from + row * job.ld + at, (long)job.cols - (long)at);
 }
 
 // What orders values by size, as whole numbers: infinities and NaN come after
@@ -195,10 +192,10 @@ hipError_t launch_copy_int8(const CopyArgs& a, hipStream_t stream) {
   size_t most = 0;
   int mats = 0;
   for (int k = 0; k < a.jobs; ++k) {
-    most = std::max(most, a.job[k].pitch / 16 * a.job[k].rows);
+    most = std::max(most, a.job[k].rows);
     mats = std::max(mats, a.job[k].mats);
   }
-  const size_t blocks = std::min<size_t>((most + 255) / 256, 2048);
+  const size_t blocks = std::min<size_t>((most + 3) / 4, 4096);
   hipLaunchKernelGGL(k_int8_copy, dim3((unsigned)blocks, mats, a.jobs),
                      dim3(256), 0, stream, a);
   return hipGetLastError();

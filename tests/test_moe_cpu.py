@@ -83,6 +83,9 @@ def test_options():
     assert _moe(_opt(experts=513)) == UNSUPPORTED
     assert _moe(_opt(experts=1 << 62)) == UNSUPPORTED
     assert _moe(_opt(n_in=1 << 31)) == UNSUPPORTED
+    assert _moe(_opt(ldw=1 << 23)) == UNSUPPORTED
+    assert _moe(_opt(ldd=1 << 23)) == UNSUPPORTED
+    assert _moe(_opt(n_in=1 << 23, hidden=1)) == UNSUPPORTED
     assert _moe(_opt(hidden=(1 << 31) - 1, n_in=(1 << 31) - 1)) == UNSUPPORTED
     assert _moe(_opt(ldx=31)) == INVALID
     assert _moe(_opt(ldl=7)) == INVALID
