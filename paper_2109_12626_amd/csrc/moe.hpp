@@ -11,10 +11,14 @@ using products::Act;
 using products::Type;
 
 enum class Route : int { SOFTMAX = 0, SIGMOID = 1 };
+// How the projections' launch knows who chose what: from a launch of the choice;
+// every workgroup by itself; every workgroup for its own expert.
+enum class Mode : int { TABLE = 0, FUSED = 1, DIRECT = 2 };
 
 // Ranks of a launch, as in products.hpp: 12 arrays of 32 addresses.
 constexpr int kRanks = 32;
 constexpr int kTokens = 128, kTop = 16, kExperts = 1024;
+constexpr int kDirect = 256;   // experts of Mode::DIRECT
 constexpr int kSmall = 8;      // tokens of the kernels for the fewest
 // Sets of 16 columns of a workgroup of up, which share the activations: as many
 // as let those be half of the loads (8-bit weights are half the bytes), and as
@@ -32,9 +36,9 @@ struct Record {
 };
 
 // A table of the workspace: how many records there are and which is each rank's
-// first (`kStarts` numbers), the records in the experts' order, the pairs by
-// expert, their weights, a pair's rank (-1: none of the launch), and the hidden
-// values and the result of every pair.  Ranks that choose from the same logits
+// first (`kStarts` numbers; not with Mode::DIRECT), the records in the experts'
+// order, the pairs by expert, every pair's weight and rank (-1: none of the
+// launch), and its hidden values and result.  Ranks that choose from the same logits
 // (or by the same index and weight) share one table, others have one each.
 constexpr int kStarts = kRanks + 2;
 struct Layout {
@@ -68,12 +72,12 @@ struct Args {
   int fast[2];                   // up, down: weights of whole 16-byte pieces
   int tiles[2];                  // up, down: pairs at a time / 16
   int sets;                      // of 16 columns, of a workgroup of down
-  int fused;                     // up makes the choice itself
+  int mode;                      // how up knows the choice (Mode)
   int small;                     // down sums by token itself
 };
 static_assert(sizeof(Args) <= 4096, "kernel arguments");
 
-// The choice of experts (unless fused), then the products (eight: 8-bit
+// The choice of experts (Mode::TABLE), then the products (eight: 8-bit
 // weights).
 hipError_t launch_route(const Args& a, hipStream_t stream);
 hipError_t launch_bf16(bool eight, const Args& a, hipStream_t stream);

@@ -98,9 +98,13 @@ moe::Layout layout_of(const Options& c, int p) {
   auto up = [](size_t v) { return (v + 127) / 128 * 128; };
   moe::Layout l;
   l.records = up(moe::kStarts * 4);
+  // (Mode::DIRECT: every expert has a record and room for all tokens)
+  const size_t own = c.o.experts * ranks_of(p),
+               direct = c.all <= (size_t)moe::kDirect ? own : 0;
   l.pairs = l.records +
-            up((size_t)most_of(c.o, ranks_of(p)) * sizeof(moe::Record));
-  l.weights = l.pairs + up(pairs * 4);
+            up(std::max((size_t)most_of(c.o, ranks_of(p)), direct) *
+               sizeof(moe::Record));
+  l.weights = l.pairs + up(std::max(pairs, direct * c.o.tokens) * 4);
   l.owner = l.weights + up(pairs * 4);
   l.hidden = l.owner + up(pairs * 4);
   // (an fp32 value: as two parts of 16 bits)
@@ -125,9 +129,13 @@ void log_layer(const Options& c, const moe::Args& a, int ranks) {
                "experts=%zu top=%d tables=%d choice=%s up=%dx%d waves=%d%s "
                "down=",
                name_of(c.t), name_of(c.w), ranks, a.tokens, a.in, a.hidden,
-               c.all, a.top, a.tables, a.fused ? "up" : "apart",
+               c.all, a.top, a.tables,
+               a.mode == (int)moe::Mode::FUSED    ? "fused"
+               : a.mode == (int)moe::Mode::DIRECT ? "direct"
+                                                  : "apart",
                a.tiles[0] * 16,
-               16 * moe::columns_up(c.w, a.fused, !a.fast[0], a.tiles[0]),
+               16 * moe::columns_up(c.w, a.mode == (int)moe::Mode::FUSED,
+                                    !a.fast[0], a.tiles[0]),
                a.waves[0], a.fast[0] ? "" : " unaligned");
   if (a.small)
     std::fprintf(stderr, "small%s\n", a.fast[1] ? "" : " unaligned");
@@ -231,18 +239,31 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.tiles[1] = mean <= 8 ? 1 : 2;
   const size_t blocks = o.tokens <= (size_t)moe::kSmall
                             ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
-  // Each workgroup of up may make the choice for itself: 1 token 2048 x 1024 of
-  // 64 experts 27 us, 30 with a launch for it; 8 tokens (4096 workgroups) 114
-  // and 98.
-  a.fused = o.in && o.hidden && c.all <= 256 &&
-            (o.hidden + 15) / 16 * blocks <= (size_t)cus * 4;
   // Down by token, a workgroup per CU (8 tokens 97.7 us, by expert and joined
   // 99; one token 27 and 31; 8 ranks, with 8 times the workgroups, 39 and 30).
   a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
             (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1);
-  if (a.fused) a.tiles[0] = 1;
-  const size_t up = 16 * moe::columns_up(c.w, a.fused, !a.fast[0],
-                                               a.tiles[0]);
+  // Each workgroup of up may make the choice for itself: 1 token 2048 x 1024 of
+  // 64 experts 27.1 us, 29.4 with a launch for it; 8 tokens (4096 workgroups) 114
+  // and 98.  Where most experts have 3 tokens, each may find those of its own
+  // expert: 20 experts 1001 x 501, 33 tokens 31.7 us, 36.1 with a launch; with 2
+  // tokens too many experts have none (16 tokens, 8 of 64 experts, a quarter of
+  // the logits masked: 124.6 and 121.2).
+  using moe::Mode;
+  Mode mode = Mode::TABLE;
+  if (o.in && o.hidden && c.all <= 256 &&
+      (o.hidden + 15) / 16 * blocks <= (size_t)cus * 4)
+    mode = Mode::FUSED;
+  else if (o.in && o.hidden && !a.small && c.all <= (size_t)moe::kDirect &&
+           o.tokens * top >= 3 * c.all)
+    mode = Mode::DIRECT;
+  a.mode = (int)mode;
+  if (mode == Mode::DIRECT) a.most = (int)n;     // (of one rank's table)
+  // (others have at most 8 pairs an expert on the average: of 2048 pairs and
+  // more than 256 experts)
+  if (mode != Mode::DIRECT) a.tiles[0] = 1;
+  const size_t up = 16 * moe::columns_up(c.w, mode == Mode::FUSED, !a.fast[0],
+                                         a.tiles[0]);
   a.waves[0] = waves_of((o.hidden + up - 1) / up * chosen, o.in * c.ew / 512,
                         cus);
   // Fewer columns where that fills the card: 20 experts 1001 x 501 36.0 us with
@@ -256,8 +277,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   if (eight && a.planes == 3) a.tiles[1] = 1;
   if (logs()) log_layer(c, a, per);
   const size_t groups =
-      std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * a.most *
-                   a.tables,
+      std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * n * per,
                (o.in + 7) / 8 * per);
   if (groups > 0xffffffffu / 512)
     return fail(DPAR_ERR_UNSUPPORTED, "%s: %zu workgroups in a launch", call,
@@ -265,6 +285,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   for (int r0 = 0; r0 < p; r0 += per) {
     a.ranks = std::min(per, p - r0), a.first = r0;
     if (!same) a.tables = a.ranks;
+    if (mode == Mode::DIRECT && same) a.most = (int)n * a.ranks;
     for (int k = 0; k < a.ranks; ++k) {
       const int i = r0 + k;
       a.x[k] = m[0].rank(i);
@@ -278,7 +299,8 @@ int moe_impl(const void* const* x, const void* const* logits,
       a.index[k] = (int*)m[10].rank(i);
       a.weight[k] = (float*)m[11].rank(i);
     }
-    if (!a.fused && (rc = launched(call, moe::launch_route(a, stream))))
+    if (mode == Mode::TABLE &&
+        (rc = launched(call, moe::launch_route(a, stream))))
       return rc;
     if (!o.in) continue;
     const hipError_t e = c.t == Type::BF16  ? moe::launch_bf16(eight, a, stream)

@@ -73,18 +73,13 @@ __device__ inline int wave_scan(int v) {
   return v;
 }
 
-// One token's choice by a wavefront, of at most 64 * N experts: lane i < top
-// ends with its i-th expert (-1: none) and weight.
+// One token's choice by a wavefront, of at most 64 * N experts (value[n]: the
+// lane's n-th logit): lane i < top ends with its i-th expert (-1: none) and
+// weight.
 template <int N>
-__device__ inline void choose(GivenMoe& a, const float* logits, int experts,
-                              int lane, int* index, float* weight) {
-  float value[N];
+__device__ inline void choose(GivenMoe& a, const float (&value)[N], int lane,
+                              int* index, float* weight) {
   uint32_t key[N];
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int e = n * 64 + lane;
-    value[n] = e < experts ? logits[e] : -__builtin_inff();
-  }
 #pragma unroll
   for (int n = 0; n < N; ++n) key[n] = ordered(value[n]);
   int mine = -1;
@@ -136,6 +131,33 @@ __device__ inline void choose(GivenMoe& a, const float* logits, int experts,
   *weight = w * a.scale;
 }
 
+// The choice of every tokens-th one, f(token, index, weight) for each: the
+// logits of B of them are on their way at a time.
+template <int N, int B, typename Fn>
+__device__ inline void choose_each(GivenMoe& a, const float* logits, int all,
+                                   int first, int step, int lane, Fn f) {
+  for (int k0 = first; k0 < a.tokens; k0 += B * step) {
+    float value[B][N];
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int k = k0 + b * step, e = n * 64 + lane;
+        value[b][n] = k < a.tokens && e < all
+                          ? logits[(size_t)k * a.ldl + e]
+                          : -__builtin_inff();
+      }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+      if (k0 + b * step < a.tokens) {
+        int e;
+        float w;
+        choose<N>(a, value[b], lane, &e, &w);
+        f(k0 + b * step, e, w);
+      }
+  }
+}
+
 // LDS of a workgroup that makes the choice.
 struct Choice {
   LDS int* expert;           // of a pair
@@ -185,27 +207,25 @@ __device__ inline bool route(GivenMoe& a, int table, const Choice& c, int at,
       c.share[i] = a.weight[table][i];
     }
   } else {
-    for (int k = wave; k < a.tokens; k += THREADS / 64) {
-      int e;
-      float w;
-      const float* l = a.logits[table] + (size_t)k * a.ldl;
-      if (all <= 64)
-        choose<1>(a, l, all, lane, &e, &w);
-      else if (all <= 256)
-        choose<4>(a, l, all, lane, &e, &w);
-      else
-        choose<kExperts / 64>(a, l, all, lane, &e, &w);
-      if (lane < top) {
-        const int i = k * top + lane;
-        c.expert[i] = e;
-        c.share[i] = w;
-        if (write)
-          for (int n = one ? 0 : table; n < (one ? a.ranks : table + 1); ++n) {
-            if (a.index[n]) a.index[n][i] = e;
-            if (a.weight[n]) a.weight[n][i] = w;
-          }
-      }
-    }
+    auto keep = [&](int token, int e, float w) {
+      if (lane >= top) return;
+      const int i = token * top + lane;
+      c.expert[i] = e;
+      c.share[i] = w;
+      if (write)
+        for (int n = one ? 0 : table; n < (one ? a.ranks : table + 1); ++n) {
+          if (a.index[n]) a.index[n][i] = e;
+          if (a.weight[n]) a.weight[n][i] = w;
+        }
+    };
+    const float* l = a.logits[table];
+    constexpr int kStep = THREADS / 64;
+    if (all <= 64)
+      choose_each<1, 8>(a, l, all, wave, kStep, lane, keep);
+    else if (all <= 256)
+      choose_each<4, 4>(a, l, all, wave, kStep, lane, keep);
+    else
+      choose_each<kExperts / 64, 1>(a, l, all, wave, kStep, lane, keep);
   }
   __syncthreads();
   if (a.given) {
@@ -269,9 +289,8 @@ __device__ inline bool route(GivenMoe& a, int table, const Choice& c, int at,
     ((int*)(work + a.at.owner))[i] =
         mine ? (one ? 0 : table) + e / a.experts : -1;
     if (mine) {
-      const int to = c.start[e] + c.place[i];
-      ((int*)(work + a.at.pairs))[to] = i;
-      ((float*)(work + a.at.weights))[to] = c.share[i];
+      ((int*)(work + a.at.pairs))[c.start[e] + c.place[i]] = i;
+      ((float*)(work + a.at.weights))[i] = c.share[i];
     }
   }
   if (write)
@@ -627,12 +646,126 @@ struct Task {
     rank = uniform(r.rank);
     expert = uniform(r.expert);
     count = uniform(r.count);
-    const int first = uniform(r.first);
-    list = (const int*)(work + a.at.pairs) + first;
-    weights = (const float*)(work + a.at.weights) + first;
-    return true;
+    list = (const int*)(work + a.at.pairs) + uniform(r.first);
+    weights = (const float*)(work + a.at.weights);
+    return count > 0;
   }
 };
+
+// A token's choice by a wavefront into a table's weights and owners, and where
+// the choice is not an input into the index and weight arrays.
+__device__ inline void keep_choice(GivenMoe& a, int table, int token,
+                                   int lane) {
+  const bool one = a.tables == 1;
+  const int top = a.top, all = a.experts * a.all, i = token * top + lane;
+  int e = -1;
+  float w = 0.f;
+  if (a.given) {
+    if (lane < top) {
+      e = a.index[table][i];
+      w = a.weight[table][i];
+      if (e < 0 || e >= all) e = -1;
+    }
+    // an expert named twice has one pair, the first, with both weights
+    const int named = e;
+    const float each = w;
+    for (int k = 0; k < top; ++k) {
+      const int other = __shfl(named, k);
+      const float more = __shfl(each, k);
+      if (named >= 0 && other == named) {
+        if (k < lane) e = -1;
+        if (k > lane) w += more;
+      }
+    }
+  } else {
+    const float* l = a.logits[table] + (size_t)token * a.ldl;
+    float value[kDirect / 64];
+#pragma unroll
+    for (int n = 0; n < kDirect / 64; ++n)
+      value[n] = n * 64 + lane < all ? l[n * 64 + lane] : -__builtin_inff();
+    choose<kDirect / 64>(a, value, lane, &e, &w);
+    if (lane < top)
+      for (int n = one ? 0 : table; n < (one ? a.ranks : table + 1); ++n) {
+        if (a.index[n]) a.index[n][i] = e;
+        if (a.weight[n]) a.weight[n][i] = w;
+      }
+  }
+  if (lane >= top) return;
+  char* const work = table_of(a, table);
+  const int low = a.experts * (a.first + (one ? 0 : table)),
+            own = a.experts * (one ? a.ranks : 1);
+  ((int*)(work + a.at.owner))[i] =
+      e >= low && e < low + own ? (one ? 0 : table) + (e - low) / a.experts
+                                : -1;
+  ((float*)(work + a.at.weights))[i] = w;
+}
+
+// The pairs of one expert, in the order of the tokens, by a workgroup of S
+// wavefronts into LDS (kDirectList numbers); how many.  A token's threads, as
+// many as there are for each, count the experts that come before this one.
+constexpr int kDirectList = 2 * kTokens + 4;
+template <int S>
+__device__ inline int chosen_by(GivenMoe& a, const Task& task, LDS int* list) {
+  constexpr int kThreads = S * 64, kTurns = (kTokens + kThreads - 1) / kThreads;
+  const int t = threadIdx.x, lane = t & 63, wave = uniform(t >> 6);
+  const int all = a.experts * a.all,
+            e = (a.first + task.rank) * a.experts + task.expert;
+  LDS int* const before = list + kTokens;
+  LDS int* const counts = before + kTokens;
+  if (!a.given) {
+    for (int i = t; i < kTokens; i += kThreads) before[i] = 0;
+    __syncthreads();
+    int places = 1;                    // (uniform)
+    while (places < a.tokens) places *= 2;
+    const int parts = places < kThreads ? kThreads / places : 1;
+    for (int k0 = 0; k0 < a.tokens; k0 += kThreads) {
+      const int token = k0 + t % places % kThreads, part = t / places;
+      if (token < a.tokens) {
+        const float* l = a.logits[task.rank] + (size_t)token * a.ldl;
+        const uint32_t own = ordered(l[e]);
+        int n = own <= kNever ? a.top : 0;
+#pragma unroll 8
+        for (int k = part; k < all; k += parts) {
+          const uint32_t key = ordered(l[k]);
+          n += key > own || (key == own && k < e);
+        }
+        if (n)
+          __hip_atomic_fetch_add(&before[token], n, __ATOMIC_RELAXED,
+                                 __HIP_MEMORY_SCOPE_WORKGROUP);
+      }
+    }
+    __syncthreads();
+  }
+  int total = 0;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int token = k * kThreads + t;
+    int place = -1;
+    if (token < a.tokens) {
+      if (a.given) {
+        const int* index = a.index[task.rank] + (size_t)token * a.top;
+        for (int i = a.top - 1; i >= 0; --i)
+          if (index[i] == e) place = i;
+      } else if (before[token] < a.top) {
+        place = before[token];
+      }
+    }
+    const uint64_t some = __ballot(place >= 0);
+    if (lane == 0) counts[wave] = __popcll(some);
+    __syncthreads();
+    int from = total;
+#pragma unroll
+    for (int w = 0; w < S; ++w) {
+      from += w < wave ? counts[w] : 0;
+      total += counts[w];
+    }
+    if (place >= 0)
+      list[from + __popcll(some & ((1ull << lane) - 1))] =
+          token * a.top + place;
+    __syncthreads();
+  }
+  return uniform(total);
+}
 
 // Distance of the hidden values' rows, in runs of 32, and the values that are
 // written: whole tiles of 16 columns, zeros past the last one.
@@ -643,10 +776,16 @@ __device__ inline size_t held_of(GivenMoe& a) {
 
 // h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 * C
 // columns (as many rows of either matrix) of one chosen expert, its S wavefronts
-// a part of the contraction each; MT tiles of 16 pairs at a time.  FUSED: every
-// workgroup makes the choice for itself (few tokens), the first one of a table
-// keeps it.
-template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int C, int S>
+// a part of the contraction each; MT tiles of 16 pairs at a time.  Where the pairs
+// come from (MODE):
+//   TABLE   the choice's launch.
+//   FUSED   every workgroup makes the choice for itself (few tokens), the first
+//           one of a table keeps it.
+//   DIRECT  (most experts are chosen) a workgroup belongs to an expert, asks for
+//           its weights and, while they come, finds the tokens that chose it; for
+//           the launches that follow the first workgroups make a token's choice
+//           each, and those of the first columns keep their experts' pairs.
+template <Type W, Type X, bool SHIFT, Mode MODE, int MT, int C, int S>
 struct Up {
   using M = Mix<W, X>;
   using V = typename M::V;
@@ -664,20 +803,25 @@ struct Up {
     const unsigned tiles = (unsigned)((a.hidden + BJ - 1) / BJ);
     const unsigned id = uniform(blockIdx.x / tiles);
     const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * BJ;
-    const int table = uniform(id / a.most), at = uniform(id % a.most);
-    Task task;
     const Choice choice(lds + kLds, a.tokens * a.top,
                         a.experts * (a.tables == 1 ? a.ranks : 1));
-    if constexpr (FUSED) {
-      if (!route<S * 64>(a, table, choice, at, at == 0 && j0 == 0)) return;
-      task.rank = uniform(choice.record->rank);
-      task.expert = uniform(choice.record->expert);
-      task.count = uniform(choice.record->count);
-      task.work = table_of(a, table);
+    Task task;
+    if constexpr (MODE == Mode::DIRECT) {
+      task.rank = uniform(id / a.experts);
+      task.expert = uniform(id % a.experts);
+      task.work = table_of(a, a.tables == 1 ? 0 : task.rank);
     } else {
-      if (!task.find(a, table, at)) return;
+      const int table = uniform(id / a.most), at = uniform(id % a.most);
+      if constexpr (MODE == Mode::FUSED) {
+        if (!route<S * 64>(a, table, choice, at, at == 0 && j0 == 0)) return;
+        task.rank = uniform(choice.record->rank);
+        task.expert = uniform(choice.record->expert);
+        task.count = uniform(choice.record->count);
+        task.work = table_of(a, table);
+      } else {
+        if (!task.find(a, table, at)) return;
+      }
     }
-    const int count = task.count;
     // set n: gate (even) or up, of columns n / 2 * 16 .. (past the last one: that
     // one, and no results)
     const char* base[NS];
@@ -702,20 +846,50 @@ struct Up {
       St::ask(base[n], a.ldw, left[n], a.in, c, uniform(mine + buf * kChunk),
               lane);
     };
-    for (int i0 = 0; i0 < count; i0 += MT * 16) {
-      const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
+    auto begin = [&] {
       if (c0 < c1) {
         ask(0, c0, 0);
         ask(1, c0, 1);
       }
+    };
+    LDS int* const mine_list = (LDS int*)(lds + kLds);
+    if constexpr (MODE == Mode::DIRECT) {
+      begin();
+      // the choices of all tables' tokens, one to a workgroup
+      if (wave == 0)
+        for (int n = blockIdx.x; n < a.tokens * a.tables; n += gridDim.x)
+          keep_choice(a, n / a.tokens, n % a.tokens, lane);
+      task.count = chosen_by<S>(a, task, mine_list);
+      if (j0 == 0) {
+        // (a record of every expert, a list of `tokens` pairs for each)
+        const int at = a.tables == 1 ? (int)id : task.expert;
+        if (t == 0) {
+          const Record r = {task.rank, task.expert, at * a.tokens, task.count};
+          ((Record*)(task.work + a.at.records))[at] = r;
+          if (at == 0) *(int*)task.work = a.most;
+        }
+        for (int i = t; i < task.count; i += S * 64)
+          ((int*)(task.work + a.at.pairs))[at * a.tokens + i] = mine_list[i];
+      }
+      if (task.count == 0) {
+        landed<0>();
+        return;
+      }
+    }
+    const int count = task.count;
+    for (int i0 = 0; i0 < count; i0 += MT * 16) {
+      const int here = count - i0 < MT * 16 ? count - i0 : MT * 16;
+      if (MODE != Mode::DIRECT || i0 > 0) begin();
       const XV* x[MT];
       int pair[MT];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         int i = m * 16 + r;
         if (i >= here) i = here - 1;
-        if constexpr (FUSED)
+        if constexpr (MODE == Mode::FUSED)
           pair[m] = choice.list[choice.record->first + i0 + i];
+        else if constexpr (MODE == Mode::DIRECT)
+          pair[m] = mine_list[i0 + i];
         else
           pair[m] = task.list[i0 + i];
         x[m] = (const XV*)a.x[task.rank] + (size_t)(pair[m] / a.top) * a.ldx +
@@ -1008,9 +1182,10 @@ struct Down {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] *= j + e < a.in ? s[e] : 0.f;
         }
-        v *= task.weights[i0 + i];
+        const int pair = list[i0 + i];
+        v *= task.weights[pair];
         float* to = (float*)(task.work + a.at.parts) +
-                    (size_t)list[i0 + i] * a.pitch + j;
+                    (size_t)pair * a.pitch + j;
         *(f32x4*)to = v;
       }
       if (i0 + MT * 16 < count) __syncthreads();
@@ -1156,7 +1331,7 @@ struct DownSmall {
           }
           LDS f32x4* to =
               (LDS f32x4*)(mine + list[x.first + i] / a.top * 8 + j);
-          *to += v * weights[x.first + i];
+          *to += v * weights[list[x.first + i]];
         }
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
       }
@@ -1259,11 +1434,11 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
 
 // ---------------------------------------------------------------- launches
 
-template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int C, int S>
+template <Type W, Type X, bool SHIFT, Mode MODE, int MT, int C, int S>
 __global__ __launch_bounds__(S * 64, 2) void k_moe_up(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Up<W, X, SHIFT, FUSED, MT, C, S>::run(a, (LDS char*)lds);
+  Up<W, X, SHIFT, MODE, MT, C, S>::run(a, (LDS char*)lds);
 }
 
 template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
@@ -1304,33 +1479,42 @@ hipError_t launch_moe(const MoeArgs& a, size_t groups, int threads,
   return hipGetLastError();
 }
 
-template <Type W, Type X, bool SHIFT, bool FUSED, int MT, int S>
+template <Type W, Type X, bool SHIFT, Mode MODE, int MT, int S>
 hipError_t go_up(const MoeArgs& a, hipStream_t stream) {
-  constexpr int C = columns_up(W, FUSED, SHIFT, MT);
-  using K = Up<W, X, SHIFT, FUSED, MT, C, S>;
-  const int more =
-      FUSED ? Choice::bytes(a.tokens * a.top,
-                            a.experts * (a.tables == 1 ? a.ranks : 1))
-            : 0;
-  return launch_moe<k_moe_up<W, X, SHIFT, FUSED, MT, C, S>>(
-      a, (a.hidden + K::BJ - 1) / K::BJ * a.most * a.tables, S * 64,
-      K::kLds + more, stream);
+  constexpr int C = columns_up(W, MODE == Mode::FUSED, SHIFT, MT);
+  using K = Up<W, X, SHIFT, MODE, MT, C, S>;
+  const size_t tiles = (a.hidden + K::BJ - 1) / K::BJ;
+  const size_t choice =
+      Choice::bytes(a.tokens * a.top,
+                    a.experts * (a.tables == 1 ? a.ranks : 1));
+  size_t groups = tiles * a.most * a.tables, bytes = K::kLds;
+  if (MODE == Mode::FUSED) bytes += choice;
+  if (MODE == Mode::DIRECT) {
+    groups = tiles * a.experts * a.ranks;
+    bytes += kDirectList * 4;
+  }
+  return launch_moe<k_moe_up<W, X, SHIFT, MODE, MT, C, S>>(
+      a, groups, S * 64, bytes, stream);
 }
 
-template <Type W, Type X, bool FUSED, int MT>
+template <Type W, Type X, Mode MODE, int MT>
 hipError_t waves_up(const MoeArgs& a, hipStream_t stream) {
   if constexpr (MT < 4)
-    if (!a.fast[0]) return go_up<W, X, true, FUSED, MT, 4>(a, stream);
-  return a.waves[0] == 4 ? go_up<W, X, false, FUSED, MT, 4>(a, stream)
-                         : go_up<W, X, false, FUSED, MT, 2>(a, stream);
+    if (!a.fast[0]) return go_up<W, X, true, MODE, MT, 4>(a, stream);
+  return a.waves[0] == 4 ? go_up<W, X, false, MODE, MT, 4>(a, stream)
+                         : go_up<W, X, false, MODE, MT, 2>(a, stream);
 }
 
 template <Type W, Type X>
 hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
-  if (a.fused) return waves_up<W, X, true, 1>(a, stream);
-  if (a.tiles[0] == 1) return waves_up<W, X, false, 1>(a, stream);
-  if (a.tiles[0] == 2) return waves_up<W, X, false, 2>(a, stream);
-  return waves_up<W, X, false, 4>(a, stream);
+  switch ((Mode)a.mode) {
+    case Mode::TABLE: return waves_up<W, X, Mode::TABLE, 1>(a, stream);
+    case Mode::FUSED: return waves_up<W, X, Mode::FUSED, 1>(a, stream);
+    default: break;
+  }
+  if (a.tiles[0] == 1) return waves_up<W, X, Mode::DIRECT, 1>(a, stream);
+  if (a.tiles[0] == 2) return waves_up<W, X, Mode::DIRECT, 2>(a, stream);
+  return waves_up<W, X, Mode::DIRECT, 4>(a, stream);
 }
 
 template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>

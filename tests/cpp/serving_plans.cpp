@@ -6,7 +6,7 @@
 // tokens in hidden experts top dtype weight_dtype out_dtype far apart" (the C
 // values; far: elements between rows; apart: every rank has logits of its own)
 // and prints a line "int8 form fast waves sets tile splits rows" or "moe type
-// eight fused fast0 tiles0 waves0 small fast1 tiles1 waves1 sets planes" per
+// eight mode fast0 tiles0 waves0 small fast1 tiles1 waves1 sets planes" per
 // launch, "route" for one of its own, and "rc code".
 #include <cstdint>
 #include <cstdio>
@@ -69,7 +69,7 @@ hipError_t launch_sums_f16(const SumArgs&, hipStream_t) { return hipSuccess; }
 namespace moe {
 static hipError_t note(int type, bool eight, const Args& a) {
   std::printf("moe %d %d %d %d %d %d %d %d %d %d %d %d\n", type, (int)eight,
-              a.fused, a.fast[0], a.tiles[0], a.waves[0], a.small, a.fast[1],
+              a.mode, a.fast[0], a.tiles[0], a.waves[0], a.small, a.fast[1],
               a.tiles[1], a.waves[1], a.sets, a.planes);
   return hipSuccess;
 }

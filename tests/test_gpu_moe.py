@@ -184,6 +184,9 @@ def test_masked_logits_ties_and_empty_tokens(route, normalize):
         logits[7] = torch.finfo(torch.float32).min
         logits[8, :5] = -INF
 
+    # by a launch of the choice, and by every expert's workgroups
+    run_moe(2, 11, 64, 48, 12, 4, route=route, normalize=normalize, edit=edit,
+            seed=3)
     layer = run_moe(2, 11, 64, 48, 6, 4, route=route, normalize=normalize,
                     edit=edit, seed=3)
     assert (layer.index[1] == -1).all() and (layer.weight[1] == 0).all()
@@ -200,8 +203,9 @@ def test_tokens_without_experts_only():
 
 
 @pytest.mark.parametrize("route", ["softmax", "sigmoid"])
-def test_infinities_and_nan_among_logits(route):
-    layer = Layer(1, 6, 64, 48, 5, 2, route=route)
+@pytest.mark.parametrize("tokens", [6, 9])     # two ways of the choice
+def test_infinities_and_nan_among_logits(route, tokens):
+    layer = Layer(1, tokens, 64, 48, 5, 2, route=route)
     l = layer.logits.t[0]
     l[1, 3] = NAN
     l[2, 4] = INF
@@ -245,6 +249,45 @@ def test_choice_as_an_input(dtype, weights, out):
     layer.run((index, weight))
     layer.check((index, weight))
     assert torch.equal(index, held[0]) and torch.equal(weight, held[1])
+
+
+@pytest.mark.parametrize("p,tokens,experts,top", [
+    (3, 1, 5, 4), (2, 8, 40, 3), (3, 30, 4, 2), (2, 20, 100, 5),
+    (34, 3, 2, 4), (35, 40, 1, 3)])
+@pytest.mark.parametrize("given", [False, True])
+def test_ranks_with_a_choice_of_their_own(p, tokens, experts, top, given):
+    """Every rank chooses from its own logits (or by its own index and weight)
+    and sums what its experts contribute by that choice."""
+    d = lib()
+    layer = Layer(p, tokens, 72, 40, experts, top, seed=tokens)
+    g = layer.g
+    every = d.pointers([layer.x.t.data_ptr()] * p)
+    logits = torch.randn(p, tokens, p * experts, generator=g, device="cuda")
+    index = torch.full((p, tokens, top), 99, dtype=torch.int32, device="cuda")
+    weight = torch.zeros(p, tokens, top, device="cuda")
+    if given:
+        index = torch.randint(-1, p * experts, index.shape, generator=g,
+                              device="cuda", dtype=torch.int32)
+        weight = torch.randn(weight.shape, generator=g, device="cuda")
+    layer.opt.ldl = 0
+    d.dpar_moe(every, None if given else d.rows(logits), layer.wg.ranks,
+               layer.wu.ranks, layer.wd.ranks, None, None, None, layer.r.at,
+               layer.y.at, d.rows(index), d.rows(weight), p, layer.opt,
+               layer.ws, layer.ws.numel(), torch.cuda.current_stream())
+    for i in range(p):
+        if given:
+            chosen = index[i].cpu().numpy(), np64(weight[i])
+        else:
+            chosen = ref.choice(np64(logits[i]), top, "softmax", True)
+            np.testing.assert_array_equal(index[i].cpu().numpy(), chosen[0])
+            np.testing.assert_allclose(np64(weight[i]), chosen[1],
+                                       rtol=2.0 ** -20)
+        part = slice(i * experts, (i + 1) * experts)
+        want = ref.moe(np64(layer.x.t[0]), *chosen, np64(layer.wg.m[part]),
+                       np64(layer.wu.m[part]), np64(layer.wd.m[part]), None,
+                       np64(layer.r.t[i]), "silu", "bfloat16", "bfloat16",
+                       i * experts, not given)
+        close(layer.y.t[i], want, f"rank {i}")
 
 
 def test_given_as_chosen():

@@ -63,7 +63,7 @@ def _there(pattern):
                                   "libdpar_products*.so"))
     out = subprocess.run([nm, "-C", lib], check=True, text=True,
                          capture_output=True).stdout
-    out = re.sub(r"\(dpar::products::(Type|Form)\)", "", out)
+    out = re.sub(r"\(dpar::(products|moe)::(Type|Form|Mode)\)", "", out)
     return {(k, tuple(a.split(", "))) for k, a in re.findall(
         rf"__device_stub__({pattern})<(.*?)>", out)}
 
@@ -104,14 +104,14 @@ def _columns(eight, fused, shift, tiles):
 
 
 def _moe_kernels(launch):
-    (_, x, eight, fused, fast0, tiles0, waves0, small, fast1, tiles1, waves1,
+    (_, x, eight, mode, fast0, tiles0, waves0, small, fast1, tiles1, waves1,
      sets, planes) = launch
     w = 5 if eight else x
     head = (str(w), str(x))
     parts = str(1 if x == 1 else planes)
-    yield "k_moe_up", head + (BOOL[not fast0], BOOL[fused], str(tiles0),
-                              str(_columns(eight, fused, not fast0, tiles0)),
-                              str(waves0))
+    columns = _columns(eight, mode == 1, not fast0, tiles0)
+    yield "k_moe_up", head + (BOOL[not fast0], str(mode), str(tiles0),
+                              str(columns), str(waves0))
     if small:
         yield "k_moe_down_small", head + (BOOL[not fast1], parts)
     else:
@@ -147,12 +147,15 @@ def test_every_kernel_of_the_mixture_of_experts(ask):
 
 
 def test_the_choice_has_a_launch_unless_up_makes_it(ask):
-    for line, apart in (("moe 1 1 2048 1024 64 8 3 3 3 0 0", False),
-                        ("moe 1 8 2048 1024 64 8 3 3 3 0 0", True),
-                        ("moe 1 1 2048 1024 512 8 3 3 3 0 0", True)):
+    for line, mode in (("moe 1 1 2048 1024 64 8 3 3 3 0 0", 1),
+                       ("moe 1 8 2048 1024 64 8 3 3 3 0 0", 0),
+                       ("moe 1 1 2048 1024 512 8 3 3 3 0 0", 0),
+                       ("moe 1 24 2048 1024 64 8 3 3 3 0 0", 2),
+                       ("moe 1 23 2048 1024 64 8 3 3 3 0 0", 0),
+                       ("moe 4 24 2048 1024 16 8 3 3 3 0 1", 2)):
         launches, = ask([line])
-        assert [n for n, *_ in launches] == ["route"] * apart + ["moe"]
-        assert launches[-1][3] == (not apart)
+        assert [n for n, *_ in launches] == ["route"] * (mode == 0) + ["moe"]
+        assert launches[-1][3] == mode
 
 
 def test_ranks_take_turns(ask):
