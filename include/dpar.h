@@ -424,7 +424,9 @@ const char* dpar_last_error(void);
  *                           launches run level items, fused calls of at most
  *                           8 ranks the register kernel); of a layer product:
  *                           its form, sizes, operands as they are read and
- *                           kernel (few rows, or results per workgroup) */
+ *                           kernel (few rows, or results per workgroup); of
+ *                           a mixture-of-experts layer: its sizes, types,
+ *                           choice of experts and kernels */
 
 /* ---------------------------------------------------------------------------
  * Layer products: what makes the rows that reduction-to-all sums when a layer

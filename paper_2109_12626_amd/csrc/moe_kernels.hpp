@@ -1,8 +1,10 @@
 // The mixture-of-experts layer for a few tokens on gfx950: the choice of
-// experts, both gated projections of the chosen ones, and their second products
-// summed by token.  Every matrix of a chosen expert is read once, and that read
-// is what bounds the layer: 16 rows of a matrix at a time go to the matrix
-// cores, the tokens that chose it are the columns.
+// experts, both gated projections of the chosen ones (up), and their second
+// products (down) summed by token.  Every matrix of a chosen expert is read once,
+// and that read is what bounds the layer: 16 rows of a matrix at a time go to the
+// matrix cores, the tokens that chose it are the columns.  Figures: one MI355X;
+// every launch costs about 4 us beside it (its start and one wait for memory), so
+// there are two for the fewest tokens and three or four else.
 #pragma once
 
 #include "moe.hpp"
@@ -438,8 +440,8 @@ __device__ inline void split(float v, unsigned short (&part)[P]) {
 //
 // SHIFT: rows that start anywhere and hold any number of values.  The pieces are
 // those that lie on 16 bytes in memory, one more of a row than its chunk fills,
-// and LDS is read from the row's own first byte on (33 x 20 experts 1001 x 501
-// fp16 36 us; by way of registers 41).  A piece that holds a byte of the row is
+// and LDS is read from the row's own first byte on (33 tokens, 20 experts 1001 x
+// 501 fp16, with a launch for the choice: 36 us; by way of registers 41).  A piece that holds a byte of the row is
 // read whole; it lies in one page with that byte.
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 template <typename T, bool SHIFT> struct At { typedef T Type; };
@@ -544,6 +546,17 @@ struct Stream {
     return v;
   }
 };
+
+// After landed(): values that ordinary loads brought are taken as read here.
+// Else the compiler, which does not know of that wait, waits for them at their
+// first use, and there for everything asked for since.
+template <int U, int N>
+__device__ inline void arrived(i32x4 (&v)[U][N]) {
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[u][n]));
+}
 
 // Values from chunk c on, as far as the chunk.
 template <typename St>
@@ -776,8 +789,11 @@ __device__ inline size_t held_of(GivenMoe& a) {
 
 // h = act(g) * u of the pairs that chose an expert: a workgroup takes 16 * C
 // columns (as many rows of either matrix) of one chosen expert, its S wavefronts
-// a part of the contraction each; MT tiles of 16 pairs at a time.  Where the pairs
-// come from (MODE):
+// a part of the contraction each; MT tiles of 16 pairs at a time.  Bound by the
+// weights: 64 experts 2048 x 1024 bf16, 100 tokens 84 to 88 us for 537 MB (6.1 to
+// 6.4 TB/s); 8-bit ones are as many loads of activations as of weights (8 experts
+// 4096 x 8192, 64 tokens: 114 us with 16 columns, 101 with 32, 93 with 64).  Where
+// the pairs come from (MODE):
 //   TABLE   the choice's launch.
 //   FUSED   every workgroup makes the choice for itself (few tokens), the first
 //           one of a table keeps it.
@@ -1068,7 +1084,9 @@ __device__ inline size_t hidden_bytes(GivenMoe& a) {
 // columns (rows of wd) of one chosen expert, its S wavefronts a part of the
 // contraction each; MT tiles of 16 pairs at a time.  The NW sets of 16 rows take
 // turns and share the hidden values in registers: P parts of 16 bits each, they
-// are P n / 16 NW times the weights' bytes with n pairs, and come from L2.
+// are P n / 16 NW times the weights' bytes with n pairs, and come from L2.  100
+// tokens, 64 experts 2048 x 1024: 48 us for 268 MB (270 us with 16 columns of all
+// experts to a workgroup, whose hidden values were three times the weights).
 template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
@@ -1198,7 +1216,9 @@ struct Down {
 // chunk of one expert's 8 rows; a wavefront takes two at a time, one in the upper
 // and one in the lower 8 of the matrix cores' rows, their pairs in the left and
 // right 8 columns: of the product the two blocks that belong together count.
-// A token's sums stay in LDS, a wavefront's own, and are joined in order.
+// A token's sums stay in LDS, a wavefront's own, and are joined in order.  One
+// token, 8 experts 2048 x 1024: 10 us for 34 MB, of which half is the way to the
+// first weights (records, pairs, hidden values); by expert and joined 15.
 template <Type W, Type X, bool SHIFT, int P>
 struct DownSmall {
   using M = Mix<W, X>;

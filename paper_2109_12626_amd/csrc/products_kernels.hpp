@@ -331,17 +331,6 @@ __device__ inline void landed() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(LEFT) : "memory");
 }
 
-// After landed(): values that ordinary loads brought are taken as read here.
-// Else the compiler, which does not know of that wait, waits for them at their
-// first use, and there for everything asked for since.
-template <int U, int N>
-__device__ inline void arrived(i32x4 (&v)[U][N]) {
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int n = 0; n < N; ++n) asm volatile("" : "+v"(v[u][n]));
-}
-
 // The workgroup's wavefronts meet.  The barrier alone orders nothing that the
 // compiler moves; no access to memory or LDS crosses this.
 __device__ inline void meet() {
@@ -1638,7 +1627,6 @@ struct FewFast {
       for (int n = 0; n < NW; ++n) {
         // (the wait also covers x)
         landed<0>();
-        if (n == 0) arrived(fx);
         if (n + 1 < NW)
           issue(c, n + 1, buf ^ 1);
         else if (c + 1 < c1)
