@@ -646,8 +646,11 @@ int dpar_gated_int8(const void* const* x, const void* const* sx,
  * Arrays, pointers, aliases (y may be its rank's residual), streams, graphs and
  * errors are as for the products above.  Up to 128 tokens, `top` up to 16, up to
  * 1024 experts in all, rows of the weights less than 2^23 values apart
- * (DPAR_ERR_UNSUPPORTED beyond).  wg, wu [expert][hidden]
- * [in] and wd [expert][in][hidden] of a rank lie in one piece of memory each.
+ * (DPAR_ERR_UNSUPPORTED beyond).  wg, wu [expert][hidden][in] and wd [expert]
+ * [in][hidden] of a rank lie in one piece of memory each.  An infinity or NaN of
+ * x stays in its token's results, one of the weights in those of the tokens that
+ * chose the expert, one of wd in its column; a product with an infinity of wd or
+ * h may be NaN (h is several terms).
  * The workspace holds the choice and h: it is required, 16-byte aligned, of
  * dpar_moe_workspace bytes. */
 typedef enum {

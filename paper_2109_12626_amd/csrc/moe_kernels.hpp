@@ -441,8 +441,8 @@ __device__ inline void split(float v, unsigned short (&part)[P]) {
 // SHIFT: rows that start anywhere and hold any number of values.  The pieces are
 // those that lie on 16 bytes in memory, one more of a row than its chunk fills,
 // and LDS is read from the row's own first byte on (33 tokens, 20 experts 1001 x
-// 501 fp16, with a launch for the choice: 36 us; by way of registers 41).  A piece that holds a byte of the row is
-// read whole; it lies in one page with that byte.
+// 501 fp16, with a launch for the choice: 36 us; by way of registers 41).  A piece
+// that holds a byte of the row is read whole; it lies in one page with that byte.
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 template <typename T, bool SHIFT> struct At { typedef T Type; };
 template <typename T> struct At<T, true> {

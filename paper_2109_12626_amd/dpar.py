@@ -6,6 +6,7 @@ the library binds to the HIP runtime torch already loaded (one runtime per
 process); torch serves only for device memory and streams.
 """
 
+import contextlib
 import ctypes
 import os
 
@@ -488,6 +489,14 @@ _NAMES = {torch.float32: "float32", torch.bfloat16: "bfloat16",
           torch.float16: "float16"}
 
 
+def _on(device):
+    """Work for tensors of this device: the library asks for the current
+    device's properties and launches there."""
+    if device.index in (None, torch.cuda.current_device()):
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
 class _Call:
     """Shapes, row distances and addresses of one call's tensors."""
 
@@ -544,11 +553,12 @@ class _Call:
                            device=self.device)
 
     def run(self, call, fn, arrays):
-        n = dpar_product_workspace(call, self.p, self.opt)
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device) \
-            if n else None
-        fn(*arrays, self.p, self.opt, ws, n,
-           torch.cuda.current_stream(self.device))
+        with _on(self.device):
+            n = dpar_product_workspace(call, self.p, self.opt)
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device) \
+                if n else None
+            fn(*arrays, self.p, self.opt, ws, n,
+               torch.cuda.current_stream(self.device))
 
     def result(self, t):
         return t[0] if self.flat and t is not None else t
@@ -658,9 +668,10 @@ def quantize(x):
         raise ValueError(f"x: rows {far} values apart overlap")
     q = torch.empty(p, n, cols, dtype=torch.int8, device=x.device)
     scale = torch.empty(p, n, dtype=torch.float32, device=x.device)
-    dpar_quantize(rows(t), rows(q), rows(scale), p,
-                  quantize_options(n, cols, _NAMES[x.dtype], far),
-                  torch.cuda.current_stream(x.device))
+    with _on(x.device):
+        dpar_quantize(rows(t), rows(q), rows(scale), p,
+                      quantize_options(n, cols, _NAMES[x.dtype], far),
+                      torch.cuda.current_stream(x.device))
     return (q, scale) if x.dim() == 3 else (q[0], scale[0])
 
 
@@ -800,8 +811,9 @@ def moe(x, logits, wg, wu, wd, top=None, sg=None, su=None, sd=None,
                       at_w[0], at_d[0], at_w[1], at_d[1], n_in, ldr)
     n = dpar_moe_workspace(p, opt)
     ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-    dpar_moe(each(x), None if logits is None else each(logits), split(wg),
-             split(wu), split(wd), *scales,
-             None if residual is None else split(residual), rows(y), *choice,
-             p, opt, ws, n, torch.cuda.current_stream(x.device))
+    with _on(x.device):
+        dpar_moe(each(x), None if logits is None else each(logits), split(wg),
+                 split(wu), split(wd), *scales,
+                 None if residual is None else split(residual), rows(y),
+                 *choice, p, opt, ws, n, torch.cuda.current_stream(x.device))
     return (y[0] if flat else y), index, weight

@@ -382,3 +382,66 @@ def test_front_ends():
         assert torch.equal(h[i], d.gated_int8(q[i], s[i], w[i], sw[i], w[i],
                                               sw[i],
                                               out_dtype=torch.float32))
+
+
+def test_quantize_many_rows():
+    """More workgroups than a launch has along its first axis."""
+    d = lib()
+    for rows, cols in ((2 ** 24 + 9, 3), (2 ** 22 + 3, 1025)):
+        x = torch.randn(rows, cols, generator=gen(rows), device="cuda").half()
+        q, scale = d.quantize(x)
+        for part in (slice(0, 1000), slice(2 ** 22 - 500, 2 ** 22 + 500),
+                     slice(rows - 1000, rows)):
+            want, s = ref.quantize(np64(x[part]))
+            np.testing.assert_array_equal(scale[part].cpu().numpy(), s)
+            np.testing.assert_array_equal(np64(q[part]), want)
+
+
+def apart(t, distance):
+    """A copy of the rows of a matrix, `distance` elements apart."""
+    n, cols = t.shape
+    flat = torch.empty((n - 1) * distance + cols, dtype=t.dtype, device="cuda")
+    far = flat.as_strided((n, cols), (distance, 1))
+    far.copy_(t)
+    return far
+
+
+@pytest.mark.parametrize("n_in", [512, 515])
+def test_distances_past_32_bits(n_in):
+    d = lib()
+    g = gen(5)
+    x = torch.randn(9, n_in, generator=g, device="cuda").bfloat16()
+    w = torch.randn(40, n_in, generator=g, device="cuda")
+    r = torch.randn(9, 40, generator=g, device="cuda").bfloat16()
+    far = apart(x, 2 ** 28 + 16)
+    q, s = d.quantize(x)
+    for a, b in zip(d.quantize(far), (q, s)):
+        assert torch.equal(a, b)
+    wq, sw = d.quantize(w)
+    want = d.linear_int8(q, s, wq, sw, residual=r, act="gelu")
+    got = d.linear_int8(apart(q, 2 ** 29 + 16), s, apart(wq, 2 ** 27 + 16), sw,
+                        residual=apart(r, 2 ** 28 + 8), act="gelu")
+    assert torch.equal(got, want)
+    want = d.gated_int8(q, s, wq, sw, wq.flip(0).contiguous(), sw)
+    got = d.gated_int8(apart(q, 2 ** 29 + 3), s, apart(wq, 2 ** 27 + 5), sw,
+                       apart(wq.flip(0).contiguous(), 2 ** 27 + 5), sw)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [2, 40])
+def test_values_between_rows_are_not_read(rows):
+    """Scales and residual beside NaN, rows beside others."""
+    d = lib()
+    g = gen(6)
+    nan = float("nan")
+    x = torch.full((rows, 600), nan, device="cuda")
+    x[:, :515] = torch.randn(rows, 515, generator=g, device="cuda")
+    q, s = d.quantize(x[:, :515])
+    assert torch.equal(q, d.quantize(x[:, :515].contiguous())[0])
+    wq, sw = d.quantize(torch.randn(33, 515, generator=g, device="cuda"))
+    r = torch.full((rows, 40), nan, device="cuda").bfloat16()
+    r[:, :33] = 1
+    got = d.linear_int8(q, s, wq, sw, residual=r[:, :33])
+    assert torch.equal(got, d.linear_int8(q, s, wq, sw,
+                                          residual=r[:, :33].contiguous()))
+    assert got.isfinite().all()

@@ -409,3 +409,147 @@ def test_front_end():
                        residual=y)
     assert near.shape == y.shape
     assert ((near - y).float() - y.float()).norm() < 0.05 * y.float().norm()
+
+
+def poison_gaps(r):
+    """NaN between a matrix's rows and after it."""
+    keep = r.t.clone()
+    r.flat.fill_(NAN)
+    r.t.copy_(keep)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("tokens,n_in,hidden,far,shift", [
+    (1, 72, 40, 8, 0), (5, 101, 67, 3, 1), (30, 264, 136, 8, 0),
+    (30, 333, 77, 5, 3), (100, 67, 131, 1, 0)])
+def test_nan_between_rows_and_matrices(dtype, tokens, n_in, hidden, far,
+                                       shift):
+    layer = Layer(2, tokens, n_in, hidden, 4, 3, dtype, far=far, shift=shift)
+    for r in (layer.x, layer.r, layer.logits):
+        poison_gaps(r)
+    for r in (layer.wg, layer.wu, layer.wd):
+        poison_gaps(r)
+        r.t[:, r.m.shape[1]:] = NAN
+    layer.run()
+    layer.check()
+
+
+# tokens: the choice within the projections, by a launch, by every expert
+@pytest.mark.parametrize("tokens,experts", [(1, 8), (6, 8), (20, 32), (40, 8)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+def test_experts_that_nobody_chose_are_not_read(dtype, tokens, experts):
+    clean = Layer(1, tokens, 128, 64, experts, 2, dtype, seed=7)
+    clean.logits.t[..., ::2] = -INF
+    clean.run()
+    clean.check()
+    layer = Layer(1, tokens, 128, 64, experts, 2, dtype, seed=7)
+    layer.logits.t[..., ::2] = -INF
+    for r in (layer.wg, layer.wu, layer.wd):
+        r.m[::2] = NAN
+    layer.run()
+    assert torch.equal(layer.y.t, clean.y.t)
+
+
+@pytest.mark.parametrize("tokens", [1, 6, 20, 40])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+def test_weights_that_are_not_finite_stay_with_their_expert(dtype, tokens):
+    clean = Layer(1, tokens, 128, 64, 6, 2, dtype, seed=8)
+    clean.run()
+    for which in (0, 2):
+        for v in (INF, NAN):
+            layer = Layer(1, tokens, 128, 64, 6, 2, dtype, seed=8)
+            (layer.wg, layer.wu, layer.wd)[which].m[3, 17, 5] = v
+            layer.run()
+            chose = (layer.index == 3).any(1)
+            touched = torch.zeros_like(layer.y.t[0], dtype=torch.bool)
+            if which == 2:
+                touched[chose, 17] = True
+                assert not layer.y.t[0, chose, 17].isfinite().any()
+            else:
+                touched[chose] = True
+                # (silu of -inf is 0, so an infinity may leave no trace)
+                if v != v:
+                    assert layer.y.t[0, chose].isnan().all()
+            assert torch.equal(layer.y.t[0][~touched], clean.y.t[0][~touched])
+
+
+def apart(t, distance):
+    """A copy of the rows of a matrix, `distance` elements apart."""
+    n = t.shape[0]
+    flat = torch.empty((n - 1) * distance + t[0].numel(), dtype=t.dtype,
+                       device="cuda")
+    far = flat.as_strided(t.shape, (distance,) + t[0].stride())
+    far.copy_(t)
+    return far
+
+
+@pytest.mark.parametrize("tokens,dtype,n_in,hidden", [
+    (2, "bfloat16", 128, 64), (9, "bfloat16", 136, 72), (9, "float16", 101, 67),
+    (3, "float32", 64, 36)])
+def test_distances_past_32_bits(tokens, dtype, n_in, hidden):
+    """Rows and experts more than 2^32 bytes apart in all."""
+    d = lib()
+    g = gen(9)
+    t = TORCH[dtype]
+
+    def normal(*shape, dtype=t):
+        return (torch.randn(*shape, generator=g, device="cuda")
+                * shape[-1] ** -0.5).to(dtype)
+
+    x, r = normal(tokens, n_in) * 8, normal(tokens, n_in)
+    logits = normal(tokens, 3, dtype=torch.float32)
+    w = [normal(3, hidden, n_in), normal(3, hidden, n_in),
+         normal(3, n_in, hidden)]
+    want, index, weight = d.moe(x, logits, *w, 2, residual=r)
+    rows = (2 ** 32 // (tokens - 1) // x.element_size() // 16 + 5) * 16
+    far = [apart(m, 2 ** 32 // x.element_size() // 2 + 48) for m in w]
+    got = d.moe(apart(x, rows), apart(logits, 2 ** 30 // (tokens - 1) + 3),
+                *far, 2, residual=apart(r, rows))
+    for a, b in zip(got, (want, index, weight)):
+        assert torch.equal(a, b)
+
+
+CHOICES = [(1, 64, 8), (6, 8, 2), (16, 64, 2), (40, 8, 2)]
+
+
+@pytest.mark.parametrize("n_in,hidden", [(512, 256), (333, 131)])
+def test_every_way_of_the_choice_on_streams_and_in_graphs(n_in, hidden):
+    """Layers of every kind in turn on two streams, then recorded together, with
+    a workspace each, and replayed beside an eager call on another stream."""
+    layers = [Layer(1, t, n_in, hidden, e, k, seed=t) for t, e, k in CHOICES]
+    other = [Layer(1, t, n_in, hidden, e, k, seed=t) for t, e, k in CHOICES]
+    want = []
+    for layer in layers:
+        layer.run()
+        layer.check()
+        want.append(layer.y.t.clone())
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        for a, b in zip(layers, reversed(other)):
+            a.run(stream=streams[0])
+            b.run(stream=streams[1])
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    for a, b, w in zip(layers, other, want):
+        assert torch.equal(a.y.t, w) and torch.equal(b.y.t, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for layer in layers:
+            layer.run()
+    for k in range(3):
+        for a, b in zip(layers, other):
+            rolled = a.logits.t.roll(k + 1, -1)
+            a.logits.t.copy_(rolled)
+            b.logits.t.copy_(rolled)
+            a.y.t.zero_()
+        streams[0].wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        for b in other:
+            b.run(stream=streams[0])
+        torch.cuda.current_stream().wait_stream(streams[0])
+        for a, b in zip(layers, other):
+            b.check()
+            assert torch.equal(a.y.t, b.y.t)
+            assert torch.equal(a.index, b.index)

@@ -190,3 +190,24 @@ def test_oracle_chooses_as_written():
     assert index.tolist() == [[1, 2, 0], [-1, -1, -1], [0, 3, 2]]
     assert weight[0, 0] == weight[0, 1] and abs(weight[0].sum() - 1) < 1e-15
     assert (weight[1] == 0).all() and np.isnan(weight[2]).all()
+
+
+def test_work_runs_on_the_tensors_device(monkeypatch):
+    """The front ends make the tensors' device the current one."""
+    import contextlib
+    import torch
+    from paper_2109_12626_amd import dpar
+    asked = []
+
+    @contextlib.contextmanager
+    def device(d):
+        asked.append(d)
+        yield
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    for index, want in ((0, []), (1, [torch.device("cuda", 1)])):
+        asked.clear()
+        with dpar._on(torch.device("cuda", index)):
+            pass
+        assert asked == want
