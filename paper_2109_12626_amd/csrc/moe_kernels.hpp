@@ -821,6 +821,12 @@ struct Up {
     const size_t j0 = (size_t)uniform(blockIdx.x % tiles) * BJ;
     const Choice choice(lds + kLds, a.tokens * a.top,
                         a.experts * (a.tables == 1 ? a.ranks : 1));
+    // Asks for what follows the choice from the arguments, of rank 0 (and below
+    // in down_small; one token 27.2 -> 26.6 us).
+    if constexpr (MODE == Mode::FUSED)
+      asm volatile("" ::"s"(a.w[0][0]), "s"(a.w[1][0]), "s"(a.x[0]),
+                   "s"(a.ldx), "s"(a.xw), "s"(a.work), "s"(a.act),
+                   "s"(a.at.hidden), "s"(a.s[0][0]), "s"(a.s[1][0]));
     Task task;
     if constexpr (MODE == Mode::DIRECT) {
       task.rank = uniform(id / a.experts);
@@ -1276,6 +1282,9 @@ struct DownSmall {
       weights[t] = share;
     }
     mine[lane] = 0.f;
+    // Asks for what follows the lists from the arguments.
+    asm volatile("" ::"s"(a.w[2][rank]), "s"(a.xd), "s"(a.ldd), "s"(a.r[rank]),
+                 "s"(a.y[rank]), "s"(a.ldy), "s"(a.ldr), "s"(a.s[2][rank]));
     const int low = uniform(low1), high = uniform(high1);
     __syncthreads();
 

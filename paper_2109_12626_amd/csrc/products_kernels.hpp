@@ -601,13 +601,18 @@ __device__ inline void fetch_columns(Given& a, int rank, size_t j,
   }
 }
 
+// I8: a row's scale.
+template <Type T>
+__device__ inline float row_scale(Given& a, int rank, size_t i) {
+  return T == Type::I8 ? ((const float*)a.a[1][rank])[i] : 0.f;
+}
+
 // Sums as 32-bit values.  I8: (sum * the row's scale) * the column's, each
 // rounded once, as the sum itself is beyond 2^24.
 template <Type T, Form F, int N>
-__device__ inline void values(Given& a, int rank, size_t i,
-                              const Columns<T, N>& c, float* v, float* u2) {
+__device__ inline void values(float row, const Columns<T, N>& c, float* v,
+                              float* u2) {
   if constexpr (T == Type::I8) {
-    const float row = ((const float*)a.a[1][rank])[i];
 #pragma unroll
     for (int k = 0; k < N; ++k)
       v[k] = (float)__builtin_bit_cast(int, v[k]) * row * c.s[0][k];
@@ -619,19 +624,28 @@ __device__ inline void values(Given& a, int rank, size_t i,
   }
 }
 
+// Asks for what the end of the kernel takes from the arguments, while the
+// product's first loads are on their way (a row of 4096 x 4096 from a graph 6.2
+// -> 5.4 us, 7 x 875 x 1001 x 1000 28.8 -> 28.5).
+__device__ inline void ask_ahead(Given& a, int rank) {
+  asm volatile("" ::"s"(a.a[1][rank]), "s"(a.o[0][rank]), "s"(a.e[0][rank]),
+               "s"(a.e[1][rank]), "s"(a.u[0][rank]), "s"(a.u[1][rank]),
+               "s"(a.ldo), "s"(a.lde), "s"(a.act), "s"(a.splits));
+}
+
 // Forms whose results have an activation.
 constexpr bool acts(Form f) { return f == Form::LINEAR || f == Form::GATED; }
 
 // N consecutive values j .. of row i: bias, activation, residual, rounding,
-// stores.  v: the product's sums (GATED: v of g, u2 of u).
+// stores.  v: the product's sums (GATED: v of g, u2 of u); scale: row_scale().
 template <Type T, Form F, bool EXACT, typename V, int N>
 __device__ inline void finish(Given& a, int rank, int pair, size_t i,
                               size_t j, float* v, float* u2,
-                              const Columns<T, N>& c) {
+                              const Columns<T, N>& c, float scale) {
   constexpr bool kKeeps = T != Type::I8;
   const long left = (long)a.nj - (long)j;
   const bool wide = a.wide_out;
-  values<T, F, N>(a, rank, i, c, v, u2);
+  values<T, F, N>(scale, c, v, u2);
   if constexpr (F == Form::LINEAR) {
     const void* r = a.e[1][rank];
     float t[N];
@@ -834,6 +848,17 @@ struct Results {
     const size_t j = jw + c * 4;
     Columns<T, 8> cols;
     if (a.splits == 1 && j < a.nj) fetch_columns<T, F, 8>(a, rank, j, cols);
+    // (64 rows' scales in a register; asked for row by row in the loop below
+    // each would be waited for)
+    float scales[(WM + 63) / 64] = {};
+    if constexpr (T == Type::I8)
+      if (a.splits == 1) {
+#pragma unroll
+        for (int n = 0; n < (WM + 63) / 64; ++n) {
+          const size_t i = iw + n * 64 + lane;
+          scales[n] = row_scale<T>(a, rank, i < a.ni ? i : a.ni - 1);
+        }
+      }
     landed<0>();
     meet();
 #pragma unroll
@@ -856,6 +881,9 @@ struct Results {
 #pragma unroll 1
         for (int row = lane / PER; row < MH * 16; row += 64 / PER) {
           const size_t i = iw + mh * 16 + row;
+          // (before any lane is through)
+          const float scale =
+              T == Type::I8 ? __shfl(scales[mh / 4], row) : 0.f;
           if (i >= a.ni || j >= a.nj) continue;
           float v[8], u2[8];
           LDS char* at = mine + row * (WN * 4);
@@ -867,7 +895,8 @@ struct Results {
             *(f32x4*)(u2 + 4) = *(LDS f32x4*)(at + ((CH / 2 + c + 1) ^ x) * 16);
           }
           if (a.splits == 1) {
-            finish<T, F, exact.value, V, 8>(a, rank, pair, i, j, v, u2, cols);
+            finish<T, F, exact.value, V, 8>(a, rank, pair, i, j, v, u2, cols,
+                                            scale);
           } else {
             // [split][rank][pair or projection][row][column]
             const int np = F == Form::DW ? a.pairs : kGated ? 2 : 1;
@@ -1111,6 +1140,7 @@ struct Tiled {
           issue(n);
           land(n);
         }
+      if constexpr (T == Type::I8) ask_ahead(a, rank);
       if (FAST && k0 + R - 1 < k1)
         landed<(R - 1) * kPieces>();
       else
@@ -1371,7 +1401,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
   Tiled<T, F, SUMS, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
 }
 
-// The same for 8 bits.
+// The same for 8 bits.  Off 16 bytes two workgroups to a CU, which takes a bound
+// on the registers: 7 x 875 x 1001 x 1000 gated 90.5 -> 59.8 us, linear 28.5 ->
+// 27.8.
 template <Form F, int BN>
 __global__ __launch_bounds__(512) void k_int8_pingpong(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -1381,7 +1413,8 @@ __global__ __launch_bounds__(512) void k_int8_pingpong(Args) {
 
 template <Form F, bool FAST, int BM, int BN, int WM, int WN, int R>
 __global__
-__launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_tiled(Args) {
+__launch_bounds__((BM / WM) * (BN / WN) * 64, FAST ? 1 : 2) void k_int8_tiled(
+    Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
   Tiled<Type::I8, F, false, FAST, BM, BN, WM, WN, R>::run(a, (LDS char*)lds);
@@ -1508,7 +1541,8 @@ struct Few {
         }
         Columns<T, 4> cols;
         fetch_columns<T, F, 4>(a, rank, j, cols);
-        finish<T, F, exact.value, V, 4>(a, rank, 0, i, j, va, ua, cols);
+        finish<T, F, exact.value, V, 4>(a, rank, 0, i, j, va, ua, cols,
+                                        row_scale<T>(a, rank, i));
       }
     });
   }
@@ -1619,6 +1653,9 @@ struct FewFast {
     };
     Acc<T> acc[MT][NW] = {};
     if (c0 < c1) issue(c0, 0, 0);
+    // (beside two weights' loads it delays x: 8 x 16 x 4096 x 2048 23.4 us, 22.8
+    // without)
+    if constexpr (T == Type::I8 && !kGated) ask_ahead(a, rank);
     int buf = 0;
 #pragma unroll 1
     for (unsigned c = c0; c < c1; ++c) {
@@ -1709,8 +1746,8 @@ __global__ __launch_bounds__(256) void k_join(Args) {
     Columns<T, 4> cols;
     fetch_columns<T, F, 4>(a, rank, j, cols);
     with_exact<T, acts(F)>(a.out32, a.out_type, [&](auto exact, auto type) {
-      finish<T, F, exact.value, decltype(type), 4>(a, rank, pair, i, j, v, u2,
-                                                   cols);
+      finish<T, F, exact.value, decltype(type), 4>(
+          a, rank, pair, i, j, v, u2, cols, row_scale<T>(a, rank, i));
     });
   }
   if constexpr (F == Form::DW) {
