@@ -174,6 +174,8 @@ def main(argv):
     print(f"{p} ranks, {tokens} tokens, {width} wide, {hidden} hidden, {top} of "
           f"{experts} experts of 1024: {a.elapsed_time(b) * 20:.1f} us a "
           f"step, {off:.2%} off the same block with 64-bit activations")
+    del block, graph
+    dpar.dpar_finalize()       # what a recorded reduction holds
 
 
 if __name__ == "__main__":

@@ -11,12 +11,22 @@ import pytest
 import torch
 
 from oracle import products as ref
-from tests._gpu import need_gpu
+from tests._gpu import lib, need_gpu
 from tests.test_gpu_int8 import close, np64
 
 pytestmark = pytest.mark.gpu
 EXAMPLES = os.path.join(os.path.dirname(os.path.dirname(
     os.path.abspath(__file__))), "examples")
+
+
+@pytest.fixture(autouse=True)
+def release():
+    """A recorded reduction keeps its table of addresses until dpar_finalize, of
+    which there are few: later tests record too."""
+    need_gpu()
+    yield
+    torch.cuda.synchronize()
+    lib().dpar_finalize()
 
 
 def block(*args):
