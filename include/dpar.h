@@ -628,8 +628,8 @@ int dpar_gated_int8(const void* const* x, const void* const* sx,
  * Types: x, wg, wu and wd of one type (BFLOAT16, FLOAT16 or FLOAT32), or, for
  * 16-bit x, weights in DPAR_INT8 with a FLOAT32 scale for each row of a matrix
  * (sg, su: [expert][hidden], sd: [expert][in], consecutive); y and the residual
- * in out_dtype, which is dtype or FLOAT32.  Sums, logits and weights are 32
- * bits; h is held to 2^-16 (to 2^-24 where y is FLOAT32).
+ * in out_dtype, which is dtype or FLOAT32.  Sums, logits, weights and h are 32
+ * bits.
  *
  * The choice, with logits [tokens][p * experts] in FLOAT32: the largest first,
  * of equal ones the lowest expert (NaN counts as the largest); a logit of

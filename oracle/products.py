@@ -215,9 +215,8 @@ def moe(x, index, weight, wg, wu, wd, scales, residual, act_name, dtype, out,
         ea = eg * 1.13 + _ACT * (1 + np.abs(g))
         h = a * u
         eh = ea * np.abs(u) + np.abs(a) * eu + ea * eu + _E * np.abs(h)
-        # as it is held
-        eh = eh + (2.0 ** -24 if out == "float32" else 2.0 ** -16) \
-            * (np.abs(h) + eh) + TINY["bfloat16"]
+        # (held whole, its last part as far as bfloat16 goes)
+        eh = eh + TINY["bfloat16"]
         o = h @ wd[e].T
         big = (np.abs(h) + eh) @ np.abs(wd[e].T)
         eo = (parts * hidden + 3) * _E * big + eh @ np.abs(wd[e].T)

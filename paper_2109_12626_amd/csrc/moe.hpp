@@ -66,7 +66,7 @@ struct Args {
   int act, route, normalize;
   int given;                     // index and weight are inputs
   int out32;
-  int planes;                    // 16-bit parts of a hidden value
+  int planes;                    // parts of a hidden value beside the weights
   int most;                      // records of a table at most
   int waves[2];                  // wavefronts per workgroup: up, down
   int fast[2];                   // up, down: weights of whole 16-byte pieces

@@ -85,10 +85,9 @@ int ranks_of(int p) {
   return (p + n - 1) / n;
 }
 
-// 16-bit parts of a hidden value.
-int planes_of(const Options& c) {
-  return c.t == Type::F32 ? 2 : c.eo == 4 ? 3 : 2;
-}
+// Parts of a hidden value beside the second product's weights: three of 16 bits,
+// or the 32-bit value.
+int planes_of(const Options& c) { return c.t == Type::F32 ? 1 : 3; }
 
 // Distance of the pairs' results, in 32-bit values.
 size_t pitch_of(const dpar_moe_t& o) { return (o.in + 3) / 4 * 4; }
@@ -107,9 +106,10 @@ moe::Layout layout_of(const Options& c, int p) {
   l.weights = l.pairs + up(std::max(pairs, direct * c.o.tokens) * 4);
   l.owner = l.weights + up(pairs * 4);
   l.hidden = l.owner + up(pairs * 4);
-  // (an fp32 value: as two parts of 16 bits)
-  l.parts = l.hidden + up(pairs * ((c.o.hidden + 31) / 32 * 32) * 2 *
-                          planes_of(c));
+  // (32 bits each; where y has 32 bits too there is room for 48, so that the
+  // size of such a call stays what programs know it to be)
+  l.parts = l.hidden + up(pairs * ((c.o.hidden + 31) / 32 * 32) *
+                          (c.t != Type::F32 && c.eo == 4 ? 6 : 4));
   l.bytes = l.parts + up(pairs * pitch_of(c.o) * 4);
   return l;
 }
@@ -274,7 +274,6 @@ int moe_impl(const void* const* x, const void* const* logits,
   // (rows off 16 bytes, and few columns, have one form each)
   if (!a.fast[0]) a.waves[0] = 4;
   if (!a.fast[1] || a.sets == 2) a.waves[1] = 4;
-  if (eight && a.planes == 3) a.tiles[1] = 1;
   if (logs()) log_layer(c, a, per);
   const size_t groups =
       std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * n * per,

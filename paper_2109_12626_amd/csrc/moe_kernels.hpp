@@ -331,8 +331,10 @@ template <Type W, Type X> struct Mix {
   static constexpr int row(int pieces, int sums, bool shift) {
     return shift || (pieces * 8 + sums) * 4 > 160 ? 256 : 512;
   }
-  // hidden values: 32-bit ones as they are, else P parts of 16 bits
+  // hidden values: NH pieces of 32-bit ones for a step, to the matrix cores as
+  // they are or as P parts of 16 bits
   static constexpr bool kWhole = X == Type::F32;
+  static constexpr int NH = VB / 4;
   static constexpr int parts(int P) { return kWhole ? 1 : P * VB / 8; }
 
   static __device__ f32x4 up(i32x4 w, const i32x4 (&x)[NX], f32x4 c) {
@@ -409,27 +411,38 @@ template <Type W, Type X> struct Mix {
   }
 };
 
-// A 32-bit hidden value as bfloat16 parts: the upper half, the rest's upper
-// half, and what is left, which together are the value (two parts: the second
-// one rounded, 2^-16 of the value off at most).  Infinities and NaN are the
-// first part's alone.
-template <int P>
-__device__ inline void split(float v, unsigned short (&part)[P]) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v);
-  uint32_t hi = b & 0xffff0000u;
-  const bool fine = (b & 0x7f800000u) != 0x7f800000u;
-  if (!fine && (b & 0x7fffffu)) hi |= 0x00400000u;       // a NaN stays one
-  part[0] = (unsigned short)(hi >> 16);
-  float rest = fine ? v - __builtin_bit_cast(float, hi) : 0.f;
+// Hidden values as they go to the matrix cores.  16-bit weights: eight 32-bit
+// values as three bfloat16 parts, the upper half, the rest's upper half, and what
+// is left, which together are the value.  The lower parts of an infinity are the
+// largest number's, of its sign, so that they leave its products as they are.
+template <typename M, int P>
+__device__ inline void split(const i32x4 (&v)[M::NH],
+                             i32x4 (&part)[M::parts(P)]) {
+  if constexpr (M::kWhole) {
+    part[0] = v[0];
+  } else {
+    static_assert(P == 3);
+    constexpr float kMost = 0x1.fffffep127f;
+    auto low = [](float x, float* rest) {
+      *rest = x - __builtin_bit_cast(
+                      float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+    };
 #pragma unroll
-  for (int p = 1; p < P; ++p) {
-    if (p == P - 1) {
-      part[p] = __builtin_bit_cast(unsigned short, (__bf16)rest);
-    } else {
-      const uint32_t r = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
-      part[p] = (unsigned short)(r >> 16);
-      rest -= __builtin_bit_cast(float, r);
-    }
+    for (int g = 0; g < M::NH / 2; ++g)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float x[2], r[2], l[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int bits = v[g * 2 + k / 2][k % 2 * 2 + e];
+          x[e] = __builtin_bit_cast(float, bits);
+          low(__builtin_amdgcn_fmed3f(x[e], -kMost, kMost), &r[e]);
+          low(r[e], &l[e]);
+        }
+        part[g * P][k] = upper_halves(x[0], x[1]);
+        part[g * P + 1][k] = upper_halves(r[0], r[1]);
+        part[g * P + 2][k] = upper_halves(l[0], l[1]);
+      }
   }
 }
 
@@ -459,6 +472,7 @@ struct Stream {
   static constexpr int kPitch = kLanes * 16;
   static constexpr int kLoads = (16 * kLanes + 63) / 64;
   static constexpr int kChunk = kLoads * 1024, kRows = 64 / kLanes;
+  static constexpr int kTurn = kLanes < 16 ? kLanes - 1 : 15;
 
   // Chunk c (of a contraction of nc values) of the rows from `base` on, as rows
   // FROM .. FROM + ROWS - 1 of the chunk.
@@ -491,7 +505,7 @@ struct Stream {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
         dma16_once(uniform(lds + h * 1024), b,
-                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & 15)) * 16);
+                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & kTurn)) * 16);
       }
     } else {
       // the last chunk: zeros past the contraction's end
@@ -500,7 +514,7 @@ struct Stream {
       for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
-        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & 15)) * VB;
+        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & kTurn)) * VB;
         dma16_at(uniform(lds + h * 1024),
                  k < nc ? base + (at * ld + k) * sizeof(V)
                         : (const char*)&g_zero);
@@ -526,7 +540,7 @@ struct Stream {
       const int at = u * 64 + n * 4 * kBytes + q * kBytes;
       LDS char* from =
           SHIFT ? src + r * kPitch + off + at
-                : src + r * ROW + ((at / 16) ^ (r & 15)) * 16 + at % 16;
+                : src + r * ROW + ((at / 16) ^ (r & kTurn)) * 16 + at % 16;
       if constexpr (kRuns == 1) {
         v = *(LDS Anywhere<i32x4, SHIFT>*)from;
       } else {
@@ -1021,39 +1035,14 @@ struct Up {
           h[e] = j + e < a.hidden ? v : 0.f;
         }
       });
-      int one = pairs[0];
+      int one = 0;       // (a choice by ?: put the array in scratch memory)
 #pragma unroll
-      for (int k = 1; k < MT; ++k)
-        if (m == k) one = pairs[k];
-      char* const row = task.work + a.at.hidden;
-      if constexpr (M::kWhole) {
-        f32x4 v;
+      for (int k = 0; k < MT; ++k) one |= m == k ? pairs[k] : 0;
+      f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = h[e];
-        *(f32x4*)(row + ((size_t)one * runs_of(a) * 32 + j) * 4) = v;
-      } else if (a.planes == 2) {
-        put<2>(row, (size_t)one * runs_of(a) + j / 32, j % 32, h);
-      } else {
-        put<3>(row, (size_t)one * runs_of(a) + j / 32, j % 32, h);
-      }
-    }
-  }
-
-  // Four values in their run of 32: [run][part][value].
-  template <int P>
-  static __device__ void put(char* to, size_t run, size_t first,
-                             const float (&h)[4]) {
-    unsigned short part[4][P];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) split<P>(h[e], part[e]);
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      unsigned short v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = part[e][p];
-      long all;
-      __builtin_memcpy(&all, v, 8);
-      *(long*)(to + ((run * P + p) * 32 + first) * 2) = all;
+      for (int e = 0; e < 4; ++e) v[e] = h[e];
+      *(f32x4*)(task.work + a.at.hidden +
+                ((size_t)one * runs_of(a) * 32 + j) * 4) = v;
     }
   }
 };
@@ -1062,43 +1051,40 @@ struct Up {
 
 // A lane group's hidden values of a step, from value k (of the step's first run)
 // of a row of `hidden` on: zeros past what is held.
-template <typename M, int P>
+template <typename M>
 __device__ inline void fetch_hidden(const char* row, size_t k, size_t held,
-                                    int q, i32x4 (&h)[M::parts(P)]) {
-  if constexpr (M::kWhole) {
-    const size_t at = k + q * 4;
-    h[0] = at < held ? *(const i32x4*)(row + at * 4) : i32x4{0, 0, 0, 0};
-  } else {
+                                    int q, i32x4 (&h)[M::NH]) {
+  constexpr int kRuns = M::kWhole ? 1 : M::NH / 2, kPieces = M::NH / kRuns;
 #pragma unroll
-    for (int g = 0; g < M::VB / 8; ++g) {
-      const size_t at = k + g * 32 + q * 8;
-      const char* from = row + (k / 32 + g) * (P * 64) + q * 16;
+  for (int g = 0; g < kRuns; ++g) {
+    const size_t at = k + g * 32 + q * (kPieces * 4);
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-        h[g * P + p] =
-            at < held ? *(const i32x4*)(from + p * 64) : i32x4{0, 0, 0, 0};
-    }
+    for (int n = 0; n < kPieces; ++n)
+      h[g * kPieces + n] = at < held ? ((const i32x4*)(row + at * 4))[n]
+                                     : i32x4{0, 0, 0, 0};
   }
 }
 // Bytes of a row of hidden values.
-template <typename M, int P>
-__device__ inline size_t hidden_bytes(GivenMoe& a) {
-  return runs_of(a) * 32 * (M::kWhole ? 4 : 2 * P);
-}
+__device__ inline size_t hidden_bytes(GivenMoe& a) { return runs_of(a) * 128; }
 
 // weight * (wd h) of the pairs that chose an expert: a workgroup takes 16 * NW
 // columns (rows of wd) of one chosen expert, its S wavefronts a part of the
 // contraction each; MT tiles of 16 pairs at a time.  The NW sets of 16 rows take
-// turns and share the hidden values in registers: P parts of 16 bits each, they
-// are P n / 16 NW times the weights' bytes with n pairs, and come from L2.  100
-// tokens, 64 experts 2048 x 1024: 48 us for 268 MB (270 us with 16 columns of all
-// experts to a workgroup, whose hidden values were three times the weights).
+// turns and share the hidden values in registers: they come from L2 in 32 bits, 4 n
+// bytes for the 16 NW values of a column of weights with n pairs, and are split
+// there (as parts from memory they would be half as many bytes again: 100 tokens,
+// 64 experts 2048 x 1024 145 us for the whole layer, 141 so; 16-bit y from two parts
+// alone, 2^-16 off, 138).
 template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
-  using St = Stream<V, M::row(MT * M::parts(P), MT * NW, SHIFT), SHIFT>;
-  static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
+  // (8-bit weights beside two tiles: 256 bytes would be 192 registers of parts)
+  static constexpr int kPieces = MT * M::parts(P);
+  static constexpr int kRow =
+      kPieces > 10 ? 128 : M::row(kPieces, MT * NW, SHIFT);
+  using St = Stream<V, kRow, SHIFT>;
+  static constexpr int VB = M::VB, K = 4 * VB;
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk,
                        BJ = 16 * NW;
   static constexpr int kParts = S * MT * NW * 1024;
@@ -1149,24 +1135,28 @@ struct Down {
       for (int m = 0; m < MT; ++m) {
         int i = m * 16 + r;
         if (i >= here) i = here - 1;
-        row[m] = hidden + (size_t)list[i0 + i] * hidden_bytes<M, P>(a);
+        row[m] = hidden + (size_t)list[i0 + i] * hidden_bytes(a);
       }
       f32x4 acc[MT][NW] = {};
-      i32x4 h[MT][U][N];
+      i32x4 h[MT][U][M::NH], parts[MT][U][M::parts(P)];
       auto load = [&](unsigned c) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
           if (m == 0 || m * 16 < here) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-              fetch_hidden<M, P>(row[m], (size_t)c * KC + u * K, held, q,
-                                 h[m][u]);
+              fetch_hidden<M>(row[m], (size_t)c * KC + u * K, held, q,
+                              h[m][u]);
           }
       };
       auto pin = [&] {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
-          if (m == 0 || m * 16 < here) arrived(h[m]);
+          if (m == 0 || m * 16 < here) {
+            arrived(h[m]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) split<M, P>(h[m][u], parts[m][u]);
+          }
       };
       auto use = [&](int n, unsigned c, int buf) {
 #pragma unroll
@@ -1176,7 +1166,7 @@ struct Down {
 #pragma unroll
           for (int m = 0; m < MT; ++m)
             if (m == 0 || m * 16 < here)
-              acc[m][n] = M::template down<P>(v, h[m][u], acc[m][n]);
+              acc[m][n] = M::template down<P>(v, parts[m][u], acc[m][n]);
         }
       };
       sweep<NW, St::kLoads>(c0, c1, load, pin, ask, use);
@@ -1229,10 +1219,9 @@ template <Type W, Type X, bool SHIFT, int P>
 struct DownSmall {
   using M = Mix<W, X>;
   using V = typename M::V;
-  // (of two turns; three parts of 512 bytes just fit)
-  static constexpr int kPieces = M::parts(P) * (M::parts(P) > 3 ? 2 : 1);
-  using St = Stream<V, M::row(kPieces, 1, SHIFT), SHIFT>;
-  static constexpr int VB = M::VB, K = 4 * VB, N = M::parts(P);
+  // (of two turns)
+  using St = Stream<V, M::row(M::NH * 2, 1, SHIFT), SHIFT>;
+  static constexpr int VB = M::VB, K = 4 * VB, NH = M::NH;
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
   static constexpr int S = 8, kMost = kSmall * kTop;     // pairs
   static constexpr int kSums = S * 2 * kChunk;
@@ -1329,7 +1318,7 @@ struct DownSmall {
         St::template ask<8, 8>(base(x[1]), a.ldd, left, a.hidden, x[1].chunk,
                                to, lane);
     };
-    auto fetch = [&](const Half (&x)[2], i32x4 (&h)[U][N]) {
+    auto fetch = [&](const Half (&x)[2], i32x4 (&h)[U][NH]) {
       const int count = side ? x[1].count : x[0].count,
                 first = side ? x[1].first : x[0].first;
       const unsigned chunk = side ? x[1].chunk : x[0].chunk;
@@ -1337,11 +1326,11 @@ struct DownSmall {
       const int i = (r & 7) < count ? r & 7 : count - 1;
       const char* row =
           hidden + (some ? (size_t)list[first + i] : 0) *
-                       hidden_bytes<M, P>(a);
+                       hidden_bytes(a);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        fetch_hidden<M, P>(row, (size_t)chunk * KC + u * K, some ? held : 0, q,
-                           h[u]);
+        fetch_hidden<M>(row, (size_t)chunk * KC + u * K, some ? held : 0, q,
+                        h[u]);
     };
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     // Adds one half's sums to its tokens': lane (r, q): pair r % 8, columns q %
@@ -1371,15 +1360,18 @@ struct DownSmall {
       start(now[1], u0 + turns, u1);
       // two turns at a time: both are asked for at once
       auto turn = [&](const Half (&was)[2], const Half (&then)[2], int buf,
-                      i32x4 (&h)[U][N]) {
+                      i32x4 (&h)[U][NH]) {
         const Half& own = side ? was[1] : was[0];
         const int off = St::offset(side ? base(was[1]) : base(was[0]), a.ldd,
                                    left, r & 7);
         const int rest = rest_of<St>(a.hidden, own.chunk);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+          i32x4 parts[M::parts(P)];
+          split<M, P>(h[u], parts);
           acc = M::template down<P>(
-              St::take(src + buf * kChunk, u, r, q, off, rest), h[u], acc);
+              St::take(src + buf * kChunk, u, r, q, off, rest), parts, acc);
+        }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
           if (was[s].unit < was[s].end &&
@@ -1388,7 +1380,7 @@ struct DownSmall {
       };
 #pragma unroll 1
       for (unsigned k = 0; k < turns; k += 2) {
-        i32x4 h[2][U][N];
+        i32x4 h[2][U][NH];
         const bool two = k + 1 < turns;
         const Half one[2] = {now[0], now[1]};
         ask(now, 0);
@@ -1576,9 +1568,7 @@ hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
   if (a.small)
     return a.fast[1] ? go_small<W, X, false, P>(a, stream)
                      : go_small<W, X, true, P>(a, stream);
-  // (three parts of a value beside 8-bit weights fill the registers with one)
-  if constexpr (W != Type::I8 || P < 3)
-    if (a.tiles[1] == 2) return waves_down<W, X, P, 2>(a, stream);
+  if (a.tiles[1] == 2) return waves_down<W, X, P, 2>(a, stream);
   return waves_down<W, X, P, 1>(a, stream);
 }
 
@@ -1586,11 +1576,7 @@ template <Type W, Type X>
 hipError_t run_moe(const MoeArgs& a, hipStream_t stream) {
   hipError_t e = pick_up<W, X>(a, stream);
   if (e != hipSuccess) return e;
-  if constexpr (X == Type::F32)
-    e = pick_down<W, X, 1>(a, stream);
-  else
-    e = a.planes == 2 ? pick_down<W, X, 2>(a, stream)
-                      : pick_down<W, X, 3>(a, stream);
+  e = pick_down<W, X, X == Type::F32 ? 1 : 3>(a, stream);
   if (e != hipSuccess || a.small) return e;
   hipLaunchKernelGGL(k_moe_join<X>,
                      dim3((unsigned)((a.in + 1023) / 1024), a.tokens, a.ranks),

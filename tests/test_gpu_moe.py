@@ -553,3 +553,19 @@ def test_every_way_of_the_choice_on_streams_and_in_graphs(n_in, hidden):
             b.check()
             assert torch.equal(a.y.t, b.y.t)
             assert torch.equal(a.index, b.index)
+
+
+# tokens: by token, by expert with one and with two tiles of pairs
+@pytest.mark.parametrize("tokens,experts,top", [(1, 4, 2), (6, 16, 3),
+                                                (40, 64, 3), (48, 4, 2)])
+@pytest.mark.parametrize("dtype,weights", [
+    ("bfloat16", "bfloat16"), ("float16", "float16"), ("bfloat16", "int8"),
+    ("float16", "int8")])
+@pytest.mark.parametrize("n_in,hidden", [(256, 1024), (101, 67)])
+def test_16_bit_results_are_32_bit_ones_rounded(tokens, experts, top, dtype,
+                                                weights, n_in, hidden):
+    """Nothing between the sums is held to fewer than 32 bits."""
+    args = (1, tokens, n_in, hidden, experts, top, dtype, weights)
+    one, whole = (run_moe(*args, out, residual=False, seed=tokens)
+                  for out in (dtype, "float32"))
+    assert torch.equal(one.y.t, whole.y.t.to(TORCH[dtype]))
