@@ -649,8 +649,8 @@ int dpar_gated_int8(const void* const* x, const void* const* sx,
  * (DPAR_ERR_UNSUPPORTED beyond).  wg, wu [expert][hidden][in] and wd [expert]
  * [in][hidden] of a rank lie in one piece of memory each.  An infinity or NaN of
  * x stays in its token's results, one of the weights in those of the tokens that
- * chose the expert, one of wd in its column; a product with an infinity of wd or
- * h may be NaN (h is several terms).
+ * chose the expert, one of wd in its column, and gives what it gives in 32 bits
+ * (beside an h below 2^-126, for 0, NaN).
  * The workspace holds the choice and h: it is required, 16-byte aligned, of
  * dpar_moe_workspace bytes. */
 typedef enum {

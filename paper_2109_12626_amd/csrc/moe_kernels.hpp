@@ -315,6 +315,18 @@ __device__ inline int upper_halves(float even, float odd) {
 __device__ inline float from_byte(int word, int k) {
   return (float)(signed char)(word >> (8 * k));
 }
+// bfloat16 values, the largest of its sign in an infinity's (and NaN's) place.
+__device__ inline i32x4 finite(i32x4 v) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const u16x2 size = __builtin_elementwise_min(
+        __builtin_bit_cast(u16x2, v[k] & 0x7fff7fff),
+        __builtin_bit_cast(u16x2, 0x7f7f7f7f));
+    v[k] = (v[k] & (int)0x80008000) | __builtin_bit_cast(int, size);
+  }
+  return v;
+}
 
 // Weights of type W beside activations of type X.  A step of the contraction is
 // 16 bytes of weights per lane group, VB values, beside NX 16-byte pieces of
@@ -364,7 +376,11 @@ template <Type W, Type X> struct Mix {
   }
 
   // c += weights by hidden values, P parts of 8 values each: every weight as
-  // one or two bfloat16 parts, which hold it exactly.
+  // one or two bfloat16 parts, which hold it exactly.  An infinity has one
+  // product that is one, the rest are finite and of its sign (or 0), so that the
+  // sum is what it is in 32 bits: lower parts of hidden values meet finite weights,
+  // and both parts of an fp16 weight other than 0 have its sign (the upper one is
+  // below it), so that no 0 meets an infinite hidden value.
   template <int P, int N>
   static __device__ f32x4 down(i32x4 w, const i32x4 (&h)[N], f32x4 c) {
     static_assert(N == parts(P));
@@ -372,15 +388,19 @@ template <Type W, Type X> struct Mix {
       return Elem<Type::F32>::mma(w, h[0], c);
     } else if constexpr (W == Type::BF16) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) c = Elem<Type::BF16>::mma(w, h[p], c);
+      for (int p = 0; p < P; ++p)
+        c = Elem<Type::BF16>::mma(p ? finite(w) : w, h[p], c);
       return c;
     } else if constexpr (W == Type::F16) {
       const f16x8 f = __builtin_bit_cast(f16x8, w);
       i32x4 hi, lo;
+      constexpr float kMost = 65504.f, kBelow = 1.f - 0x1p-12f;   // (exact)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float a = (float)f[2 * k], b = (float)f[2 * k + 1];
-        const int both = upper_halves(a, b);
+        const int both = upper_halves(
+            __builtin_amdgcn_fmed3f(a, -kMost, kMost) * kBelow,
+            __builtin_amdgcn_fmed3f(b, -kMost, kMost) * kBelow);
         hi[k] = both;
         const float ah = __builtin_bit_cast(float, both << 16),
                     bh = __builtin_bit_cast(float, both & (int)0xffff0000);
@@ -389,7 +409,7 @@ template <Type W, Type X> struct Mix {
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         c = Elem<Type::BF16>::mma(hi, h[p], c);
-        c = Elem<Type::BF16>::mma(lo, h[p], c);
+        c = Elem<Type::BF16>::mma(p ? finite(lo) : lo, h[p], c);
       }
       return c;
     } else {

@@ -569,3 +569,81 @@ def test_16_bit_results_are_32_bit_ones_rounded(tokens, experts, top, dtype,
     one, whole = (run_moe(*args, out, residual=False, seed=tokens)
                   for out in (dtype, "float32"))
     assert torch.equal(one.y.t, whole.y.t.to(TORCH[dtype]))
+
+
+@pytest.mark.parametrize("tokens,experts", [(1, 2), (6, 2), (20, 16), (40, 2)])
+@pytest.mark.parametrize("n_in,hidden", [(256, 128), (101, 67)])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("out", ["same", "float32"])
+def test_infinities_of_the_second_product(tokens, experts, n_in, hidden,
+                                          dtype, out):
+    """An infinity of wd gives one of the sum's sign (it meets values of few
+    bits too), two of opposite signs NaN, and one beside a hidden value of 0
+    NaN."""
+    layer = Layer(1, tokens, n_in, hidden, experts, 1, dtype,
+                  out=dtype if out == "same" else out, act="none",
+                  residual=False, seed=3)
+    layer.logits.t.fill_(-1)
+    layer.logits.t[..., 1] = 1
+    # hidden values 1, 2, 3 ..: of few bits; the fifth one is 0
+    layer.x.t.zero_()
+    layer.x.t[..., 0] = 1
+    layer.wg.m.zero_()
+    layer.wu.m.zero_()
+    values = torch.arange(hidden, device="cuda") % 7 + 1.0
+    values[::2] *= -1
+    layer.wg.m[1, :, 0] = values.to(layer.wg.t.dtype)
+    layer.wu.m[1, :, 0] = 1
+    layer.wg.m[1, 4, 0] = 0
+    h = layer.wg.m[1, :, 0].float()
+    w = layer.wd.m[1]
+    w[3, 1] = INF
+    w[5, 2] = INF
+    w[7, hidden - 1] = -INF
+    w[11, 8], w[11, 9] = INF, INF               # opposite signs of h
+    w[13, 4] = INF                              # beside 0
+    w[17, 6] = NAN
+    layer.run()
+    want = (w.float() * h).sum(1)
+    assert want[3] == INF and want[5] == -INF and want[11].isnan()
+    assert want[13].isnan() and want[17].isnan()
+    y = layer.y.t[0].float()
+    special = ~want.isfinite()
+    assert y[:, ~special].isfinite().all()
+    for t in range(tokens):
+        assert torch.equal(y[t, special].nan_to_num(nan=5.0),
+                           want[special].nan_to_num(nan=5.0)), t
+
+
+@pytest.mark.parametrize("tokens,experts", [(1, 2), (6, 2), (20, 16), (40, 2)])
+@pytest.mark.parametrize("dtype,weights", [
+    ("bfloat16", "bfloat16"), ("float16", "float16"), ("float32", "float32"),
+    ("bfloat16", "int8"), ("float16", "int8")])
+def test_an_infinite_hidden_value(tokens, experts, dtype, weights):
+    """Beside weights of few bits, of either sign and of 0."""
+    n_in, hidden = 128, 64
+    layer = Layer(1, tokens, n_in, hidden, experts, 1, dtype, weights,
+                  out="float32", act="none", residual=False, seed=3)
+    layer.logits.t.fill_(-1)
+    layer.logits.t[..., 1] = 1
+    layer.x.t.fill_(0)
+    layer.x.t[..., 0] = 1
+    layer.x.t[0, 0, 1] = INF                    # of the first token
+    for r in (layer.wg, layer.wu):
+        r.m.zero_()
+        r.m[1, :, :2] = 1
+    if layer.s:
+        for s in layer.s:
+            s.t.fill_(1)
+    w = layer.wd.m[1]
+    w[:, 1:] = w[:, :1]                         # one sign a row
+    w[9] = 0
+    w[10] = 1
+    w[10, 3] = -1
+    layer.run()
+    want = (w.float() * INF).sum(1)
+    assert want[9].isnan() and want[10].isnan()
+    assert (want == INF).any() and (want == -INF).any()
+    y = layer.y.t[0]
+    assert torch.equal(y[0].nan_to_num(nan=5.0), want.nan_to_num(nan=5.0))
+    assert y[1:].isfinite().all()
