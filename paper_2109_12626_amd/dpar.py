@@ -13,6 +13,7 @@ import os
 import numpy as np
 
 import torch  # noqa: F401  (must precede loading libdpar: one HIP runtime)
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DPAR_LIB_PATH") or os.path.join(_HERE, "libdpar.so")
@@ -483,7 +484,8 @@ def allreduce(x, y=None, dtype=None, op="sum", b=0, exec="auto", stream=None,
 # distance apart; the values of a row are consecutive.  The results are new
 # tensors [p, ...] (without the first dimension if w has none).  Only marshals
 # addresses: every product runs in the library's kernels.  Nothing is recorded
-# for autograd: tensors that require a gradient are refused where it is on.
+# for autograd: tensors that require a gradient are refused where it is on, and
+# so are those that carry a tangent of forward mode.
 
 _NAMES = {torch.float32: "float32", torch.bfloat16: "bfloat16",
           torch.float16: "float16"}
@@ -495,6 +497,16 @@ def _on(device):
     if device.index in (None, torch.cuda.current_device()):
         return contextlib.nullcontext()
     return torch.cuda.device(device)
+
+
+def _no_derivative(t, name, advice):
+    """Refuses a tensor whose gradient or tangent the call would drop."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and {advice}")
+    if t.is_floating_point() and torch._C._is_fwd_grad_enabled() \
+            and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} carries a tangent of forward mode, and no "
+                         "call here has one: take its primal")
 
 
 class _Call:
@@ -522,10 +534,9 @@ class _Call:
             return None
         if t.device != self.device or t.dtype != (dtype or self.dtype):
             raise ValueError(f"{name}: {t.dtype} on {t.device}")
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{name} requires a gradient, and these calls "
-                             "record none: call under torch.no_grad() (or "
-                             "detach it) and use the backward call")
+        _no_derivative(t, name, "these calls record none: call under "
+                       "torch.no_grad() (or detach it) and use the backward "
+                       "call")
         one = t.dim() == len(shape)
         if tuple(t.shape[-len(shape):]) != shape or \
                 not (one or (t.dim() == len(shape) + 1
@@ -656,9 +667,8 @@ def quantize(x):
     numbers of 8 bits and what a step of each row is."""
     if x.dim() not in (2, 3) or x.dtype not in _NAMES:
         raise ValueError(f"x: {x.dtype}, shape {tuple(x.shape)}")
-    if x.requires_grad and torch.is_grad_enabled():
-        raise ValueError("x requires a gradient, and rounding has none: call "
-                         "under torch.no_grad() or detach it")
+    _no_derivative(x, "x", "rounding has none: call under torch.no_grad() or "
+                   "detach it")
     t = x if x.dim() == 3 else x[None]
     p, n, cols = t.shape
     if cols > 1 and t.stride(-1) != 1:
@@ -740,9 +750,7 @@ def moe(x, logits, wg, wu, wd, top=None, sg=None, su=None, sd=None,
                 or t.device != x.device:
             raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on "
                              f"{t.device}, want {dtype} {tuple(shape)}")
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{name} requires a gradient, and this call has "
-                             "no backward pass")
+        _no_derivative(t, name, "this call has no backward pass")
         return t
 
     def row_distance(t, name):
