@@ -15,6 +15,11 @@ enum class Route : int { SOFTMAX = 0, SIGMOID = 1 };
 // every workgroup by itself; every workgroup for its own expert.
 enum class Mode : int { TABLE = 0, FUSED = 1, DIRECT = 2 };
 
+// Hidden values between the products: 32-bit ones as the second product takes
+// them (fp32), 32-bit ones that its kernels split into three 16-bit parts, or
+// these parts.
+enum class Hidden : int { WHOLE = 1, VALUES = 2, PARTS = 3 };
+
 // Ranks of a launch, as in products.hpp: 12 arrays of 32 addresses.
 constexpr int kRanks = 32;
 constexpr int kTokens = 128, kTop = 16, kExperts = 1024;
@@ -66,7 +71,7 @@ struct Args {
   int act, route, normalize;
   int given;                     // index and weight are inputs
   int out32;
-  int planes;                    // parts of a hidden value beside the weights
+  int planes;                    // how hidden values are held (Hidden)
   int most;                      // records of a table at most
   int waves[2];                  // wavefronts per workgroup: up, down
   int fast[2];                   // up, down: weights of whole 16-byte pieces

@@ -85,10 +85,6 @@ int ranks_of(int p) {
   return (p + n - 1) / n;
 }
 
-// Parts of a hidden value beside the second product's weights: three of 16 bits,
-// or the 32-bit value.
-int planes_of(const Options& c) { return c.t == Type::F32 ? 1 : 3; }
-
 // Distance of the pairs' results, in 32-bit values.
 size_t pitch_of(const dpar_moe_t& o) { return (o.in + 3) / 4 * 4; }
 
@@ -106,8 +102,7 @@ moe::Layout layout_of(const Options& c, int p) {
   l.weights = l.pairs + up(std::max(pairs, direct * c.o.tokens) * 4);
   l.owner = l.weights + up(pairs * 4);
   l.hidden = l.owner + up(pairs * 4);
-  // (32 bits each; where y has 32 bits too there is room for 48, so that the
-  // size of such a call stays what programs know it to be)
+  // (room for the parts of 16-bit calls where y has 32 bits)
   l.parts = l.hidden + up(pairs * ((c.o.hidden + 31) / 32 * 32) *
                           (c.t != Type::F32 && c.eo == 4 ? 6 : 4));
   l.bytes = l.parts + up(pairs * pitch_of(c.o) * 4);
@@ -213,7 +208,7 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.tokens = (int)o.tokens, a.experts = (int)o.experts, a.top = o.top;
   a.all = p;
   a.act = o.act, a.route = o.route, a.normalize = o.normalize != 0;
-  a.given = given, a.out32 = c.eo == 4, a.planes = planes_of(c);
+  a.given = given, a.out32 = c.eo == 4;
   // one table if all ranks make the same choice
   bool same = true;
   for (int i = 1; i < p; ++i)
@@ -239,10 +234,16 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.tiles[1] = mean <= 8 ? 1 : 2;
   const size_t blocks = o.tokens <= (size_t)moe::kSmall
                             ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
-  // Down by token, a workgroup per CU (8 tokens 97.7 us, by expert and joined
-  // 99; one token 27 and 31; 8 ranks, with 8 times the workgroups, 39 and 30).
+  // Down by token, a workgroup per CU (one token 28 us, by expert and joined 32; 8
+  // ranks, with 8 times the workgroups, 39 and 30; 8 tokens 8 of 64 experts 103.5
+  // and 104.7, 8-bit 78 and 75.5, with a fourth of the pairs 34 and 37.7; 4 tokens
+  // through 2 of 8 experts 1024 x 4096, where 16-bit results leave no room for parts
+  // of hidden values, below, 44.7 and 44.7, 8-bit 40.9 and 37.2).
   a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
-            (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1);
+            (o.in + 7) / 8 * per <= (size_t)cus * (o.tokens == 1 ? 2 : 1) &&
+            (o.tokens == 1 || c.t == Type::F32 ||
+             ((o.hidden + 31) / 32 * 32 <= 2 * a.pitch &&
+              (!eight || o.tokens * top <= 24)));
   // Each workgroup of up may make the choice for itself: 1 token 2048 x 1024 of
   // 64 experts 27.1 us, 29.4 with a launch for it; 8 tokens (4096 workgroups) 114
   // and 98.  Where most experts have 3 tokens, each may find those of its own
@@ -274,6 +275,17 @@ int moe_impl(const void* const* x, const void* const* logits,
   // (rows off 16 bytes, and few columns, have one form each)
   if (!a.fast[0]) a.waves[0] = 4;
   if (!a.fast[1] || a.sets == 2) a.waves[1] = 4;
+  // Parts, where there is room for them (by token no pair's result is kept), are
+  // half as many bytes again as values, which every workgroup has to split (one token
+  // 27.8 and 28.2 us, 8-bit weights 23.5 and 25.0, fp16 29.1 and 30.3).  Two tiles of
+  // pairs beside 8-bit weights have registers for values alone (64 tokens, 2 of 8
+  // experts 4096 x 8192: 177 us, parts and one tile 208).
+  const size_t room = (a.small ? at.bytes : at.parts) - at.hidden;
+  a.planes = (int)(c.t == Type::F32 ? moe::Hidden::WHOLE
+                   : o.tokens * top * ((o.hidden + 31) / 32) * 192 <= room &&
+                           (a.small || !eight || a.tiles[1] == 1)
+                       ? moe::Hidden::PARTS
+                       : moe::Hidden::VALUES);
   if (logs()) log_layer(c, a, per);
   const size_t groups =
       std::max(std::max((o.hidden + 15) / 16, (o.in + 31) / 32) * n * per,

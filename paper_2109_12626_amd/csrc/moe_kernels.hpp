@@ -306,6 +306,8 @@ __device__ inline bool route(GivenMoe& a, int table, const Choice& c, int at,
 
 // ---------------------------------------------------------------- types
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
 // Values as the upper halves of 32-bit floats, two of them in a register.
 __device__ inline int upper_halves(float even, float odd) {
   return (int)__builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, odd),
@@ -314,18 +316,6 @@ __device__ inline int upper_halves(float even, float odd) {
 }
 __device__ inline float from_byte(int word, int k) {
   return (float)(signed char)(word >> (8 * k));
-}
-// bfloat16 values, the largest of its sign in an infinity's (and NaN's) place.
-__device__ inline i32x4 finite(i32x4 v) {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const u16x2 size = __builtin_elementwise_min(
-        __builtin_bit_cast(u16x2, v[k] & 0x7fff7fff),
-        __builtin_bit_cast(u16x2, 0x7f7f7f7f));
-    v[k] = (v[k] & (int)0x80008000) | __builtin_bit_cast(int, size);
-  }
-  return v;
 }
 
 // Weights of type W beside activations of type X.  A step of the contraction is
@@ -343,11 +333,13 @@ template <Type W, Type X> struct Mix {
   static constexpr int row(int pieces, int sums, bool shift) {
     return shift || (pieces * 8 + sums) * 4 > 160 ? 256 : 512;
   }
-  // hidden values: NH pieces of 32-bit ones for a step, to the matrix cores as
-  // they are or as P parts of 16 bits
+  // Hidden values: 32-bit ones as they are, else three parts of 16 bits; their
+  // pieces of a step, and those that come from memory (FORM: Hidden).
   static constexpr bool kWhole = X == Type::F32;
-  static constexpr int NH = VB / 4;
-  static constexpr int parts(int P) { return kWhole ? 1 : P * VB / 8; }
+  static constexpr int kParts = kWhole ? 1 : 3 * VB / 8;
+  static constexpr int pieces(int FORM) {
+    return FORM == (int)Hidden::PARTS ? kParts : VB / 4;
+  }
 
   static __device__ f32x4 up(i32x4 w, const i32x4 (&x)[NX], f32x4 c) {
     if constexpr (W != Type::I8) {
@@ -375,32 +367,23 @@ template <Type W, Type X> struct Mix {
     }
   }
 
-  // c += weights by hidden values, P parts of 8 values each: every weight as
-  // one or two bfloat16 parts, which hold it exactly.  An infinity has one
-  // product that is one, the rest are finite and of its sign (or 0), so that the
-  // sum is what it is in 32 bits: lower parts of hidden values meet finite weights,
-  // and both parts of an fp16 weight other than 0 have its sign (the upper one is
-  // below it), so that no 0 meets an infinite hidden value.
-  template <int P, int N>
-  static __device__ f32x4 down(i32x4 w, const i32x4 (&h)[N], f32x4 c) {
-    static_assert(N == parts(P));
+  // c += weights by hidden values, three parts of 8 values each: every weight as
+  // one or two bfloat16 parts, which hold it exactly.
+  static __device__ f32x4 down(i32x4 w, const i32x4 (&h)[kParts], f32x4 c) {
+    constexpr int P = 3;
     if constexpr (kWhole) {
       return Elem<Type::F32>::mma(w, h[0], c);
     } else if constexpr (W == Type::BF16) {
 #pragma unroll
-      for (int p = 0; p < P; ++p)
-        c = Elem<Type::BF16>::mma(p ? finite(w) : w, h[p], c);
+      for (int p = 0; p < P; ++p) c = Elem<Type::BF16>::mma(w, h[p], c);
       return c;
     } else if constexpr (W == Type::F16) {
       const f16x8 f = __builtin_bit_cast(f16x8, w);
       i32x4 hi, lo;
-      constexpr float kMost = 65504.f, kBelow = 1.f - 0x1p-12f;   // (exact)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float a = (float)f[2 * k], b = (float)f[2 * k + 1];
-        const int both = upper_halves(
-            __builtin_amdgcn_fmed3f(a, -kMost, kMost) * kBelow,
-            __builtin_amdgcn_fmed3f(b, -kMost, kMost) * kBelow);
+        const int both = upper_halves(a, b);
         hi[k] = both;
         const float ah = __builtin_bit_cast(float, both << 16),
                     bh = __builtin_bit_cast(float, both & (int)0xffff0000);
@@ -409,7 +392,7 @@ template <Type W, Type X> struct Mix {
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         c = Elem<Type::BF16>::mma(hi, h[p], c);
-        c = Elem<Type::BF16>::mma(p ? finite(lo) : lo, h[p], c);
+        c = Elem<Type::BF16>::mma(lo, h[p], c);
       }
       return c;
     } else {
@@ -431,39 +414,18 @@ template <Type W, Type X> struct Mix {
   }
 };
 
-// Hidden values as they go to the matrix cores.  16-bit weights: eight 32-bit
-// values as three bfloat16 parts, the upper half, the rest's upper half, and what
-// is left, which together are the value.  The lower parts of an infinity are the
-// largest number's, of its sign, so that they leave its products as they are.
-template <typename M, int P>
-__device__ inline void split(const i32x4 (&v)[M::NH],
-                             i32x4 (&part)[M::parts(P)]) {
-  if constexpr (M::kWhole) {
-    part[0] = v[0];
-  } else {
-    static_assert(P == 3);
-    constexpr float kMost = 0x1.fffffep127f;
-    auto low = [](float x, float* rest) {
-      *rest = x - __builtin_bit_cast(
-                      float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
-    };
-#pragma unroll
-    for (int g = 0; g < M::NH / 2; ++g)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float x[2], r[2], l[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int bits = v[g * 2 + k / 2][k % 2 * 2 + e];
-          x[e] = __builtin_bit_cast(float, bits);
-          low(__builtin_amdgcn_fmed3f(x[e], -kMost, kMost), &r[e]);
-          low(r[e], &l[e]);
-        }
-        part[g * P][k] = upper_halves(x[0], x[1]);
-        part[g * P + 1][k] = upper_halves(r[0], r[1]);
-        part[g * P + 2][k] = upper_halves(l[0], l[1]);
-      }
-  }
+// Two 32-bit hidden values as three bfloat16 parts each: the upper half, the
+// rest's upper half, and what is left, which together are the value.  (What an
+// infinity leaves is NaN: whole_result().)
+__device__ inline void split(float even, float odd, int (&part)[3]) {
+  auto rest = [](float x) {
+    return x - __builtin_bit_cast(
+                   float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u);
+  };
+  const float e1 = rest(even), o1 = rest(odd);
+  part[0] = upper_halves(even, odd);
+  part[1] = upper_halves(e1, o1);
+  part[2] = upper_halves(rest(e1), rest(o1));
 }
 
 // ---------------------------------------------------------------- streams
@@ -476,7 +438,6 @@ __device__ inline void split(const i32x4 (&v)[M::NH],
 // and LDS is read from the row's own first byte on (33 tokens, 20 experts 1001 x
 // 501 fp16, with a launch for the choice: 36 us; by way of registers 41).  A piece
 // that holds a byte of the row is read whole; it lies in one page with that byte.
-typedef int i32x2 __attribute__((ext_vector_type(2)));
 template <typename T, bool SHIFT> struct At { typedef T Type; };
 template <typename T> struct At<T, true> {
   typedef T Type __attribute__((aligned(1)));
@@ -1058,11 +1019,24 @@ struct Up {
       int one = 0;       // (a choice by ?: put the array in scratch memory)
 #pragma unroll
       for (int k = 0; k < MT; ++k) one |= m == k ? pairs[k] : 0;
-      f32x4 v;
+      char* const row = task.work + a.at.hidden;
+      if (M::kWhole || a.planes != (int)Hidden::PARTS) {
+        f32x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = h[e];
-      *(f32x4*)(task.work + a.at.hidden +
-                ((size_t)one * runs_of(a) * 32 + j) * 4) = v;
+        for (int e = 0; e < 4; ++e) v[e] = h[e];
+        *(f32x4*)(row + ((size_t)one * runs_of(a) * 32 + j) * 4) = v;
+      } else {
+        // in their run of 32: [run][part][value]
+        int part[2][3];
+        split(h[0], h[1], part[0]);
+        split(h[2], h[3], part[1]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          i32x2 v = {part[0][p], part[1][p]};
+          *(i32x2*)(row + ((((size_t)one * runs_of(a) + j / 32) * 3 + p) * 32 +
+                           j % 32) * 2) = v;
+        }
+      }
     }
   }
 };
@@ -1071,21 +1045,74 @@ struct Up {
 
 // A lane group's hidden values of a step, from value k (of the step's first run)
 // of a row of `hidden` on: zeros past what is held.
-template <typename M>
+template <typename M, int FORM>
 __device__ inline void fetch_hidden(const char* row, size_t k, size_t held,
-                                    int q, i32x4 (&h)[M::NH]) {
-  constexpr int kRuns = M::kWhole ? 1 : M::NH / 2, kPieces = M::NH / kRuns;
+                                    int q, i32x4 (&h)[M::pieces(FORM)]) {
+  constexpr int kRuns = M::kWhole ? 1 : M::VB / 8,
+                N = M::pieces(FORM) / kRuns;
 #pragma unroll
   for (int g = 0; g < kRuns; ++g) {
-    const size_t at = k + g * 32 + q * (kPieces * 4);
+    const size_t at = k + g * 32 + q * (M::kWhole ? 4 : 8);
+    const char* from = FORM == (int)Hidden::PARTS
+                           ? row + (k / 32 + g) * 192 + q * 16
+                           : row + at * 4;
 #pragma unroll
-    for (int n = 0; n < kPieces; ++n)
-      h[g * kPieces + n] = at < held ? ((const i32x4*)(row + at * 4))[n]
-                                     : i32x4{0, 0, 0, 0};
+    for (int n = 0; n < N; ++n)
+      h[g * N + n] =
+          at < held ? *(const i32x4*)(from +
+                                      n * (FORM == (int)Hidden::PARTS ? 64 : 16))
+                    : i32x4{0, 0, 0, 0};
   }
 }
+// Values as they go to the matrix cores.
+template <typename M>
+__device__ inline void to_parts(const i32x4 (&h)[M::VB / 4],
+                                i32x4 (&part)[M::kParts]) {
+#pragma unroll
+  for (int g = 0; g < M::VB / 8; ++g)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 v = __builtin_bit_cast(f32x4, h[g * 2 + k / 2]);
+      int two[3];
+      split(v[k % 2 * 2], v[k % 2 * 2 + 1], two);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) part[g * 3 + p][k] = two[p];
+    }
+}
 // Bytes of a row of hidden values.
-__device__ inline size_t hidden_bytes(GivenMoe& a) { return runs_of(a) * 128; }
+template <int FORM>
+__device__ inline size_t hidden_bytes(GivenMoe& a) {
+  return runs_of(a) * (FORM == (int)Hidden::PARTS ? 192 : 128);
+}
+
+// weight * (wd h) of one pair and column, value by value in 32 bits: for results
+// that are NaN, since where values are several parts an infinity may have met a part
+// that is 0 or has the other sign.  (What is NaN by itself is soon found to be.)
+template <typename M, int FORM>
+__device__ inline float whole_result(GivenMoe& a, const char* work, int rank,
+                                     int expert, int pair, size_t j) {
+  const char* h = work + a.at.hidden + (size_t)pair * hidden_bytes<FORM>(a);
+  const auto w = (const typename M::V*)a.w[2][rank] + (size_t)expert * a.xd +
+                 j * a.ldd;
+  float sum = 0.f;
+  for (size_t k = 0; k < a.hidden && sum == sum; ++k) {
+    float v;
+    if constexpr (FORM == (int)Hidden::PARTS) {
+      const auto part = (const unsigned short*)(h + k / 32 * 192) + k % 32;
+      auto value = [&](int p) {
+        return __builtin_bit_cast(float, (uint32_t)part[p * 32] << 16);
+      };
+      v = value(0);
+      if (fabsf(v) < __builtin_inff()) v += value(1) + value(2);
+    } else {
+      v = ((const float*)h)[k];
+    }
+    sum += v * (float)w[k];
+  }
+  if constexpr (sizeof(typename M::V) == 1)
+    sum *= a.s[2][rank][(size_t)expert * a.in + j];
+  return sum * ((const float*)(work + a.at.weights))[pair];
+}
 
 // weight * (wd h) of the pairs that chose an expert: a workgroup takes 16 * NW
 // columns (rows of wd) of one chosen expert, its S wavefronts a part of the
@@ -1095,12 +1122,13 @@ __device__ inline size_t hidden_bytes(GivenMoe& a) { return runs_of(a) * 128; }
 // there (as parts from memory they would be half as many bytes again: 100 tokens,
 // 64 experts 2048 x 1024 145 us for the whole layer, 141 so; 16-bit y from two parts
 // alone, 2^-16 off, 138).
-template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
+template <Type W, Type X, bool SHIFT, int FORM, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
   // (8-bit weights beside two tiles: 256 bytes would be 192 registers of parts)
-  static constexpr int kPieces = MT * M::parts(P);
+  static constexpr int kPieces = MT * M::kParts, NH = M::pieces(FORM);
+  static constexpr bool kSplits = FORM == (int)Hidden::VALUES;
   static constexpr int kRow =
       kPieces > 10 ? 128 : M::row(kPieces, MT * NW, SHIFT);
   using St = Stream<V, kRow, SHIFT>;
@@ -1155,18 +1183,25 @@ struct Down {
       for (int m = 0; m < MT; ++m) {
         int i = m * 16 + r;
         if (i >= here) i = here - 1;
-        row[m] = hidden + (size_t)list[i0 + i] * hidden_bytes(a);
+        row[m] = hidden + (size_t)list[i0 + i] * hidden_bytes<FORM>(a);
       }
       f32x4 acc[MT][NW] = {};
-      i32x4 h[MT][U][M::NH], parts[MT][U][M::parts(P)];
+      i32x4 h[MT][U][NH];
+      i32x4 split_h[kSplits ? MT : 1][kSplits ? U : 1][M::kParts];
+      auto& parts = *[&] {
+        if constexpr (kSplits)
+          return &split_h;
+        else
+          return &h;
+      }();
       auto load = [&](unsigned c) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
           if (m == 0 || m * 16 < here) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-              fetch_hidden<M>(row[m], (size_t)c * KC + u * K, held, q,
-                              h[m][u]);
+              fetch_hidden<M, FORM>(row[m], (size_t)c * KC + u * K, held, q,
+                                    h[m][u]);
           }
       };
       auto pin = [&] {
@@ -1174,8 +1209,9 @@ struct Down {
         for (int m = 0; m < MT; ++m)
           if (m == 0 || m * 16 < here) {
             arrived(h[m]);
+            if constexpr (kSplits)
 #pragma unroll
-            for (int u = 0; u < U; ++u) split<M, P>(h[m][u], parts[m][u]);
+              for (int u = 0; u < U; ++u) to_parts<M>(h[m][u], split_h[m][u]);
           }
       };
       auto use = [&](int n, unsigned c, int buf) {
@@ -1186,7 +1222,7 @@ struct Down {
 #pragma unroll
           for (int m = 0; m < MT; ++m)
             if (m == 0 || m * 16 < here)
-              acc[m][n] = M::template down<P>(v, parts[m][u], acc[m][n]);
+              acc[m][n] = M::down(v, parts[m][u], acc[m][n]);
         }
       };
       sweep<NW, St::kLoads>(c0, c1, load, pin, ask, use);
@@ -1211,12 +1247,12 @@ struct Down {
         for (int k = 1; k < S; ++k) v += part[k][x][lane];
         const size_t j = j0 + n * 16 + q * 4;
         if (j >= a.in) continue;
+        const int pair = list[i0 + i];
         if constexpr (W == Type::I8) {
           const float* s = a.s[2][rank] + (size_t)expert * a.in + j;
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] *= j + e < a.in ? s[e] : 0.f;
         }
-        const int pair = list[i0 + i];
         v *= task.weights[pair];
         float* to = (float*)(task.work + a.at.parts) +
                     (size_t)pair * a.pitch + j;
@@ -1235,13 +1271,14 @@ struct Down {
 // A token's sums stay in LDS, a wavefront's own, and are joined in order.  One
 // token, 8 experts 2048 x 1024: 10 us for 34 MB, of which half is the way to the
 // first weights (records, pairs, hidden values); by expert and joined 15.
-template <Type W, Type X, bool SHIFT, int P>
+template <Type W, Type X, bool SHIFT, int FORM>
 struct DownSmall {
   using M = Mix<W, X>;
   using V = typename M::V;
-  // (of two turns)
-  using St = Stream<V, M::row(M::NH * 2, 1, SHIFT), SHIFT>;
-  static constexpr int VB = M::VB, K = 4 * VB, NH = M::NH;
+  // (of two turns; three parts of 512 bytes just fit)
+  static constexpr int NH = M::pieces(FORM), kPieces = NH * (NH > 3 ? 2 : 1);
+  using St = Stream<V, M::row(kPieces, 1, SHIFT), SHIFT>;
+  static constexpr int VB = M::VB, K = 4 * VB;
   static constexpr int U = St::kSteps, KC = U * K, kChunk = St::kChunk;
   static constexpr int S = 8, kMost = kSmall * kTop;     // pairs
   static constexpr int kSums = S * 2 * kChunk;
@@ -1342,15 +1379,16 @@ struct DownSmall {
       const int count = side ? x[1].count : x[0].count,
                 first = side ? x[1].first : x[0].first;
       const unsigned chunk = side ? x[1].chunk : x[0].chunk;
-      const bool some = side ? x[1].unit < x[1].end : true;
-      const int i = (r & 7) < count ? r & 7 : count - 1;
+      // (lanes past the pairs load nothing, and their columns do not count)
+      const bool some = (!side || x[1].unit < x[1].end) && (r & 7) < count;
+      const int i = r & 7;
       const char* row =
           hidden + (some ? (size_t)list[first + i] : 0) *
-                       hidden_bytes(a);
+                       hidden_bytes<FORM>(a);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        fetch_hidden<M>(row, (size_t)chunk * KC + u * K, some ? held : 0, q,
-                        h[u]);
+        fetch_hidden<M, FORM>(row, (size_t)chunk * KC + u * K,
+                              some ? held : 0, q, h[u]);
     };
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     // Adds one half's sums to its tokens': lane (r, q): pair r % 8, columns q %
@@ -1387,10 +1425,14 @@ struct DownSmall {
         const int rest = rest_of<St>(a.hidden, own.chunk);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          i32x4 parts[M::parts(P)];
-          split<M, P>(h[u], parts);
-          acc = M::template down<P>(
-              St::take(src + buf * kChunk, u, r, q, off, rest), parts, acc);
+          const i32x4 w = St::take(src + buf * kChunk, u, r, q, off, rest);
+          if constexpr (FORM == (int)Hidden::VALUES) {
+            i32x4 parts[M::kParts];
+            to_parts<M>(h[u], parts);
+            acc = M::down(w, parts, acc);
+          } else {
+            acc = M::down(w, h[u], acc);
+          }
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -1429,6 +1471,16 @@ struct DownSmall {
 #pragma unroll
     for (int k = 0; k < S; ++k) v += sums[k * (kSmall * 8) + t];
     const size_t j = j0 + col;
+    if (!M::kWhole && v != v) {
+      v = 0.f;
+      for (int n = low; n < high && v == v; ++n)
+        for (int i = 0; i < records[n].count; ++i) {
+          const int pair = list[records[n].first + i];
+          if (pair / a.top == token)
+            v += whole_result<M, FORM>(a, work, rank, records[n].expert, pair,
+                                       j);
+        }
+    }
     if (const void* res = a.r[rank]) {
       const size_t from = (size_t)token * a.ldr + j;
       v += a.out32 ? ((const float*)res)[from]
@@ -1439,9 +1491,26 @@ struct DownSmall {
   }
 };
 
+// A pair's result that is NaN: whole_result() by the record that has the pair.
+template <typename M>
+__device__ inline float whole_part(GivenMoe& a, const char* work, int rank,
+                                   int pair, size_t j) {
+  const auto records = (const Record*)(work + a.at.records);
+  const auto list = (const int*)(work + a.at.pairs);
+  for (int n = 0; n < *(const int*)work; ++n)
+    for (int i = 0; i < records[n].count; ++i)
+      if (records[n].rank == rank && list[records[n].first + i] == pair)
+        return a.planes == (int)Hidden::PARTS
+                   ? whole_result<M, (int)Hidden::PARTS>(
+                         a, work, rank, records[n].expert, pair, j)
+                   : whole_result<M, (int)Hidden::VALUES>(
+                         a, work, rank, records[n].expert, pair, j);
+  return 0.f;
+}
+
 // y = the sum of a token's parts, in the order of its choices, + residual: four
 // columns per thread.
-template <Type X>
+template <Type W, Type X>
 __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   using Out = typename Elem<X>::V;
@@ -1454,7 +1523,16 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
                        (size_t)token * a.top * a.pitch + j;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < a.top; ++k)
-    if (owner[k] == rank) v += *(const f32x4*)(parts + (size_t)k * a.pitch);
+    if (owner[k] == rank) {
+      f32x4 p = *(const f32x4*)(parts + (size_t)k * a.pitch);
+      if (X != Type::F32)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (p[e] != p[e] && j + e < a.in)
+            p[e] = whole_part<Mix<W, X>>(a, work, rank, token * a.top + k,
+                                         j + e);
+      v += p;
+    }
   float o[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = v[e];
@@ -1482,18 +1560,18 @@ __global__ __launch_bounds__(S * 64, 2) void k_moe_up(MoeArgs) {
   Up<W, X, SHIFT, MODE, MT, C, S>::run(a, (LDS char*)lds);
 }
 
-template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
+template <Type W, Type X, bool SHIFT, int FORM, int MT, int NW, int S>
 __global__ __launch_bounds__(S * 64, 2) void k_moe_down(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  Down<W, X, SHIFT, P, MT, NW, S>::run(a, (LDS char*)lds);
+  Down<W, X, SHIFT, FORM, MT, NW, S>::run(a, (LDS char*)lds);
 }
 
-template <Type W, Type X, bool SHIFT, int P>
+template <Type W, Type X, bool SHIFT, int FORM>
 __global__ __launch_bounds__(512) void k_moe_down_small(MoeArgs) {
   GivenMoe& a = *(GivenMoe*)__builtin_amdgcn_kernarg_segment_ptr();
   extern __shared__ char lds[];
-  DownSmall<W, X, SHIFT, P>::run(a, (LDS char*)lds);
+  DownSmall<W, X, SHIFT, FORM>::run(a, (LDS char*)lds);
 }
 
 template <void (*K)(MoeArgs)>
@@ -1558,47 +1636,54 @@ hipError_t pick_up(const MoeArgs& a, hipStream_t stream) {
   return waves_up<W, X, Mode::DIRECT, 4>(a, stream);
 }
 
-template <Type W, Type X, bool SHIFT, int P, int MT, int NW, int S>
+template <Type W, Type X, bool SHIFT, int FORM, int MT, int NW, int S>
 hipError_t go_down(const MoeArgs& a, hipStream_t stream) {
-  using K = Down<W, X, SHIFT, P, MT, NW, S>;
-  return launch_moe<k_moe_down<W, X, SHIFT, P, MT, NW, S>>(
+  using K = Down<W, X, SHIFT, FORM, MT, NW, S>;
+  return launch_moe<k_moe_down<W, X, SHIFT, FORM, MT, NW, S>>(
       a, (a.in + K::BJ - 1) / K::BJ * a.most * a.tables, S * 64, K::kLds,
       stream);
 }
 
-template <Type W, Type X, bool SHIFT, int P>
+template <Type W, Type X, bool SHIFT, int FORM>
 hipError_t go_small(const MoeArgs& a, hipStream_t stream) {
-  return launch_moe<k_moe_down_small<W, X, SHIFT, P>>(
-      a, (a.in + 7) / 8 * a.ranks, 512, DownSmall<W, X, SHIFT, P>::kLds,
+  return launch_moe<k_moe_down_small<W, X, SHIFT, FORM>>(
+      a, (a.in + 7) / 8 * a.ranks, 512, DownSmall<W, X, SHIFT, FORM>::kLds,
       stream);
 }
 
-template <Type W, Type X, int P, int MT>
+template <Type W, Type X, int FORM, int MT>
 hipError_t waves_down(const MoeArgs& a, hipStream_t stream) {
   if (!a.fast[1])
-    return a.sets == 2 ? go_down<W, X, true, P, MT, 2, 4>(a, stream)
-                       : go_down<W, X, true, P, MT, 4, 4>(a, stream);
-  if (a.sets == 2) return go_down<W, X, false, P, MT, 2, 4>(a, stream);
-  return a.waves[1] == 4 ? go_down<W, X, false, P, MT, 4, 4>(a, stream)
-                         : go_down<W, X, false, P, MT, 4, 2>(a, stream);
+    return a.sets == 2 ? go_down<W, X, true, FORM, MT, 2, 4>(a, stream)
+                       : go_down<W, X, true, FORM, MT, 4, 4>(a, stream);
+  if (a.sets == 2) return go_down<W, X, false, FORM, MT, 2, 4>(a, stream);
+  return a.waves[1] == 4 ? go_down<W, X, false, FORM, MT, 4, 4>(a, stream)
+                         : go_down<W, X, false, FORM, MT, 4, 2>(a, stream);
 }
 
-template <Type W, Type X, int P>
+template <Type W, Type X, int FORM>
 hipError_t pick_down(const MoeArgs& a, hipStream_t stream) {
   if (a.small)
-    return a.fast[1] ? go_small<W, X, false, P>(a, stream)
-                     : go_small<W, X, true, P>(a, stream);
-  if (a.tiles[1] == 2) return waves_down<W, X, P, 2>(a, stream);
-  return waves_down<W, X, P, 1>(a, stream);
+    return a.fast[1] ? go_small<W, X, false, FORM>(a, stream)
+                     : go_small<W, X, true, FORM>(a, stream);
+  // (8-bit weights' parts come from memory for one tile of pairs only)
+  if constexpr (W != Type::I8 || FORM != (int)Hidden::PARTS)
+    if (a.tiles[1] == 2) return waves_down<W, X, FORM, 2>(a, stream);
+  return waves_down<W, X, FORM, 1>(a, stream);
 }
 
 template <Type W, Type X>
 hipError_t run_moe(const MoeArgs& a, hipStream_t stream) {
   hipError_t e = pick_up<W, X>(a, stream);
   if (e != hipSuccess) return e;
-  e = pick_down<W, X, X == Type::F32 ? 1 : 3>(a, stream);
+  if constexpr (X == Type::F32)
+    e = pick_down<W, X, (int)Hidden::WHOLE>(a, stream);
+  else
+    e = a.planes == (int)Hidden::PARTS
+            ? pick_down<W, X, (int)Hidden::PARTS>(a, stream)
+            : pick_down<W, X, (int)Hidden::VALUES>(a, stream);
   if (e != hipSuccess || a.small) return e;
-  hipLaunchKernelGGL(k_moe_join<X>,
+  hipLaunchKernelGGL((k_moe_join<W, X>),
                      dim3((unsigned)((a.in + 1023) / 1024), a.tokens, a.ranks),
                      dim3(256), 0, stream, a);
   return hipGetLastError();

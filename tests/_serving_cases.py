@@ -133,38 +133,51 @@ gated 33 712 48 1 0 1
 MOE = [(*map(int, c[:6]), *c[6:9], *map(int, c[9:]))
        for c in map(str.split, """\
 1 1 16 11 2 1 bfloat16 bfloat16 bfloat16 0 0
-1 1 16 32 1 1 bfloat16 bfloat16 float32 1 1
-1 1 32 15 2 2 float16 int8 float16 0 0
+1 1 30 186 1 1 bfloat16 bfloat16 bfloat16 0 1
 1 1 32 16 1 1 float16 float16 float16 0 1
+1 1 32 67 1 1 float16 float16 float16 0 1
+1 1 32 80 1 1 bfloat16 int8 bfloat16 1 1
+1 1 32 128 1 1 bfloat16 bfloat16 bfloat16 0 0
+1 1 48 160 1 1 bfloat16 int8 bfloat16 0 0
+1 1 64 147 1 1 float16 int8 float16 0 1
 1 1 2048 29 1 1 bfloat16 int8 bfloat16 0 1
-1 2 16 13 3 2 bfloat16 int8 bfloat16 0 0
 1 2 16 16 1 1 float32 float32 float32 0 0
 1 2 28 16 1 1 bfloat16 int8 float32 0 0
 1 2 29 16 1 1 float16 int8 float16 0 1
 1 2 32 16 1 1 bfloat16 bfloat16 float32 0 1
 1 7 2191 9 12 4 float16 int8 float16 0 0
 1 8 16 9 2 1 float16 float16 float32 1 0
-1 8 2048 14 1 1 float16 int8 float32 0 1
+1 8 2496 8 12 3 float16 float16 float16 0 1
 1 9 22 16 3 2 bfloat16 int8 bfloat16 0 1
+1 9 25 8 2 2 float16 float16 float16 0 1
 1 9 28 16 2 1 float16 int8 float32 0 0
 1 9 32 19 2 1 bfloat16 bfloat16 float32 0 0
 1 9 48 11 1 1 float16 int8 float32 0 1
 1 9 48 16 1 1 float16 float16 float32 0 0
+1 9 64 9 1 1 bfloat16 bfloat16 bfloat16 1 0
 1 9 64 16 1 1 bfloat16 int8 bfloat16 0 1
 1 9 2048 8 2 1 bfloat16 int8 float32 0 1
 1 9 8192 8 4 3 float32 float32 float32 0 0
 1 9 8192 1024 3 3 bfloat16 bfloat16 float32 0 0
 1 16 16 32 8 1 float32 float32 float32 0 0
+1 16 18 48 1 1 float16 float16 float16 1 1
+1 16 20 32 2 1 bfloat16 int8 float32 0 0
+1 16 24 16 4 1 bfloat16 bfloat16 bfloat16 0 1
 1 16 32 14 2 1 bfloat16 int8 float32 0 1
 1 16 32 16 1 1 bfloat16 bfloat16 bfloat16 0 1
 1 16 32 16 1 1 float16 int8 float16 1 1
+1 16 32 16 2 1 float16 int8 float32 1 1
 1 16 34 18 2 1 float16 float16 float16 0 1
 1 16 2048 10 12 8 bfloat16 int8 bfloat16 0 1
 1 16 2048 16 12 8 float32 float32 float32 0 0
 1 17 16 16 2 1 float16 int8 float16 0 1
+1 17 32 12 3 1 float16 float16 float32 0 0
+1 17 64 16 1 1 bfloat16 bfloat16 float32 0 1
 1 17 720 8 32 3 bfloat16 int8 float32 0 1
+1 17 2688 8 12 8 bfloat16 bfloat16 bfloat16 0 0
 1 17 7146 8 4 3 bfloat16 bfloat16 float32 0 1
 1 17 8192 9 3 2 bfloat16 bfloat16 bfloat16 0 1
+1 17 8192 16 3 2 float16 float16 float32 0 1
 1 26 64 11 1 1 float16 float16 float32 0 1
 1 30 48 16 1 1 float32 float32 float32 0 1
 1 40 32 10 1 1 bfloat16 bfloat16 float32 0 0
@@ -172,15 +185,16 @@ MOE = [(*map(int, c[:6]), *c[6:9], *map(int, c[9:]))
 1 40 80 12 1 1 float16 int8 float32 0 0
 1 40 512 9 1 1 float32 float32 float32 0 1
 1 40 1024 8 1 1 float16 float16 float32 0 0
-1 40 1024 23 1 1 bfloat16 bfloat16 float32 0 1
 1 40 2048 11 12 4 float16 int8 float16 0 0
 1 40 4096 16 1 1 float16 int8 float32 0 0
 1 40 8192 16 3 1 float16 int8 float32 0 0
 1 83 2048 9 1 1 bfloat16 int8 bfloat16 0 1
 1 128 224 512 100 8 float32 float32 float32 0 0
+1 128 239 1024 100 8 float16 float16 float32 0 0
+1 128 330 2048 64 1 bfloat16 int8 float32 0 0
+2 1 24 80 1 1 float16 int8 float16 0 1
 2 8 4096 9 3 1 float32 float32 float32 0 1
-2 9 16 32 1 1 float16 float16 float16 0 0
-2 9 27 8 2 1 float16 float16 float32 0 0
+2 9 28 16 1 1 float16 float16 float16 0 1
 2 9 1808 8 4 1 float16 float16 float32 0 1
 2 9 2272 8 2 1 bfloat16 int8 bfloat16 0 1
 2 10 1088 11 3 1 bfloat16 bfloat16 bfloat16 0 0
@@ -188,15 +202,25 @@ MOE = [(*map(int, c[:6]), *c[6:9], *map(int, c[9:]))
 2 16 4096 2048 3 4 float16 int8 float16 0 1
 2 17 26 16 1 1 bfloat16 bfloat16 float32 0 1
 2 17 2112 11 3 1 float16 int8 float16 0 1
+2 40 976 1024 12 8 bfloat16 bfloat16 bfloat16 0 1
+3 1 8192 16 1 3 float16 int8 float16 0 0
 3 2 4096 8 2 4 bfloat16 bfloat16 bfloat16 0 1
+3 8 1024 9 8 3 bfloat16 bfloat16 float32 0 1
+3 8 3040 8 3 1 bfloat16 bfloat16 float32 0 0
 3 9 1024 8 8 8 float16 float16 float32 0 1
+3 9 1024 16 8 3 bfloat16 int8 float32 0 0
 3 9 2048 14 1 1 float16 int8 float16 0 1
+3 9 3111 8 3 1 bfloat16 int8 bfloat16 0 0
 3 16 8192 16 1 2 bfloat16 int8 float32 0 1
 3 17 8192 11 1 2 float16 float16 float16 0 1
+3 17 8192 13 1 2 float16 float16 float32 0 1
+3 40 8192 9 1 2 bfloat16 bfloat16 float32 0 0
 3 73 80 1024 64 3 float16 float16 float16 0 1
 3 128 71 512 64 4 float32 float32 float32 0 0
 3 128 221 1024 32 8 float16 float16 float16 0 1
 3 128 454 2048 16 4 bfloat16 int8 bfloat16 0 1
+4 1 21 112 1 3 float16 float16 float16 0 1
+4 1 8192 9 1 4 float16 int8 float32 0 1
 4 8 713 16 8 4 bfloat16 int8 bfloat16 0 0
 4 8 3168 9 2 2 float16 float16 float16 0 1
 4 16 512 10 2 1 float32 float32 float32 0 1
@@ -204,12 +228,16 @@ MOE = [(*map(int, c[:6]), *c[6:9], *map(int, c[9:]))
 4 16 2151 9 3 8 float32 float32 float32 0 1
 4 16 8912 8 1 4 float16 float16 float16 0 0
 4 17 2048 8 3 1 bfloat16 bfloat16 bfloat16 1 1
+4 128 22 4096 100 4 float16 int8 float32 0 0
+4 128 32 1024 100 8 float16 float16 float32 0 1
 4 128 32 2048 100 4 bfloat16 int8 bfloat16 0 0
 4 128 32 2368 100 3 float16 int8 float16 0 1
 35 1 16 12 1 2 float32 float32 float32 1 1
 35 2 20 11 1 1 float16 int8 float32 0 0
 35 9 17 19 1 2 bfloat16 int8 bfloat16 0 0
 35 16 25 16 1 8 float32 float32 float32 0 1
+35 40 748 9 1 1 float16 float16 float32 0 1
 35 119 32 16 1 1 float32 float32 float32 0 0
 35 128 16 1024 12 4 bfloat16 bfloat16 float32 0 1
+35 128 24 1040 12 4 bfloat16 bfloat16 bfloat16 0 1
 """.splitlines())]
