@@ -572,7 +572,7 @@ def test_16_bit_results_are_32_bit_ones_rounded(tokens, experts, top, dtype,
 
 
 @pytest.mark.parametrize("tokens,experts", [(1, 2), (6, 2), (20, 16), (40, 2)])
-@pytest.mark.parametrize("n_in,hidden", [(256, 128), (101, 67)])
+@pytest.mark.parametrize("n_in,hidden", [(256, 128), (101, 67), (48, 256)])
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("out", ["same", "float32"])
 def test_infinities_of_the_second_product(tokens, experts, n_in, hidden,
@@ -619,11 +619,14 @@ def test_infinities_of_the_second_product(tokens, experts, n_in, hidden,
 @pytest.mark.parametrize("dtype,weights", [
     ("bfloat16", "bfloat16"), ("float16", "float16"), ("float32", "float32"),
     ("bfloat16", "int8"), ("float16", "int8")])
-def test_an_infinite_hidden_value(tokens, experts, dtype, weights):
+@pytest.mark.parametrize("n_in,hidden", [(128, 64), (32, 256)])
+@pytest.mark.parametrize("out", ["same", "float32"])
+def test_an_infinite_hidden_value(tokens, experts, dtype, weights, n_in,
+                                  hidden, out):
     """Beside weights of few bits, of either sign and of 0."""
-    n_in, hidden = 128, 64
     layer = Layer(1, tokens, n_in, hidden, experts, 1, dtype, weights,
-                  out="float32", act="none", residual=False, seed=3)
+                  out=dtype if out == "same" else out, act="none",
+                  residual=False, seed=3)
     layer.logits.t.fill_(-1)
     layer.logits.t[..., 1] = 1
     layer.x.t.fill_(0)
@@ -644,6 +647,6 @@ def test_an_infinite_hidden_value(tokens, experts, dtype, weights):
     want = (w.float() * INF).sum(1)
     assert want[9].isnan() and want[10].isnan()
     assert (want == INF).any() and (want == -INF).any()
-    y = layer.y.t[0]
+    y = layer.y.t[0].float()
     assert torch.equal(y[0].nan_to_num(nan=5.0), want.nan_to_num(nan=5.0))
     assert y[1:].isfinite().all()
