@@ -453,7 +453,11 @@ struct Stream {
   static constexpr int kPitch = kLanes * 16;
   static constexpr int kLoads = (16 * kLanes + 63) / 64;
   static constexpr int kChunk = kLoads * 1024, kRows = 64 / kLanes;
-  static constexpr int kTurn = kLanes < 16 ? kLanes - 1 : 15;
+  // By what pieces are exchanged: the 16 rows' pieces read together lie in as many
+  // banks (of rows of 128 bytes, two lie side by side across them).
+  static __device__ int key(int row) {
+    return kLanes < 16 ? row >> 1 & (kLanes - 1) : row & 15;
+  }
 
   // Chunk c (of a contraction of nc values) of the rows from `base` on, as rows
   // FROM .. FROM + ROWS - 1 of the chunk.
@@ -486,7 +490,7 @@ struct Stream {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
         dma16_once(uniform(lds + h * 1024), b,
-                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ (row & kTurn)) * 16);
+                   (uint32_t)(at * ld * sizeof(V)) + (slot ^ key(row)) * 16);
       }
     } else {
       // the last chunk: zeros past the contraction's end
@@ -495,7 +499,7 @@ struct Stream {
       for (int h = FROM / kRows; h < (FROM + ROWS) / kRows; ++h) {
         const int row = h * kRows + lane / kLanes;
         const int at = row - FROM < left ? row - FROM : left - 1;
-        const size_t k = (size_t)c * KC + (size_t)(slot ^ (row & kTurn)) * VB;
+        const size_t k = (size_t)c * KC + (size_t)(slot ^ key(row)) * VB;
         dma16_at(uniform(lds + h * 1024),
                  k < nc ? base + (at * ld + k) * sizeof(V)
                         : (const char*)&g_zero);
@@ -521,7 +525,7 @@ struct Stream {
       const int at = u * 64 + n * 4 * kBytes + q * kBytes;
       LDS char* from =
           SHIFT ? src + r * kPitch + off + at
-                : src + r * ROW + ((at / 16) ^ (r & kTurn)) * 16 + at % 16;
+                : src + r * ROW + ((at / 16) ^ key(r)) * 16 + at % 16;
       if constexpr (kRuns == 1) {
         v = *(LDS Anywhere<i32x4, SHIFT>*)from;
       } else {
