@@ -651,8 +651,11 @@ int dpar_gated_int8(const void* const* x, const void* const* sx,
  * x stays in its token's results, one of the weights in those of the tokens that
  * chose the expert, one of wd in its column, and gives what it gives in 32 bits
  * (beside an h below 2^-126, for 0, NaN).
- * The workspace holds the choice and h: it is required, 16-byte aligned, of
- * dpar_moe_workspace bytes. */
+ * The workspace holds the choice, h and the pairs' results: it is required,
+ * 16-byte aligned, of dpar_moe_workspace bytes.  That is a table for every rank,
+ * each of about tokens * top * (4 hidden + 4 in) bytes, 6 hidden with FLOAT32 y of
+ * 16-bit x; ranks of a launch (up to 32) that choose from one array of logits, or by
+ * one index and weight, use the first one's alone. */
 typedef enum {
     DPAR_ROUTE_SOFTMAX = 0,
     DPAR_ROUTE_SIGMOID = 1

@@ -27,7 +27,9 @@ constexpr int kDirect = 256;   // experts of Mode::DIRECT
 constexpr int kSmall = 8;      // tokens of the kernels for the fewest
 // Sets of 16 columns of a workgroup of up, which share the activations: as many
 // as let those be half of the loads (8-bit weights are half the bytes), and as
-// the registers have sums for (shift: rows off 16 bytes, which need some too).
+// the registers have sums for (shift: rows off 16 bytes, which need some too; with
+// 8-bit weights and two tiles 192 bytes per lane are in scratch memory all the same:
+// 64 tokens, 2 of 8 experts 4097 x 8191 395 us, 4096 x 8192 177).
 constexpr int columns_up(Type w, bool fused, bool shift, int tiles) {
   if (fused) return 1;
   const int n = w != Type::I8 ? tiles : tiles < 4 ? 2 * tiles : 2;

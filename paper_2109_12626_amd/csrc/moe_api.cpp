@@ -110,9 +110,11 @@ moe::Layout layout_of(const Options& c, int p) {
 }
 
 // Wavefronts per workgroup, 2 or 4, for a matrix of `chunks` chunks of 512 bytes
-// a row, with n workgroups that have work: 4 for 16 or more chunks (8 experts
-// 4096 x 4096, 64 tokens: 143 us, 154 with 2), else where two do not fill the
-// card (100 tokens, 64 experts 2048 x 1024: 141 us, 144 with 4).
+// a row, with n workgroups that have work: 4 for 16 or more chunks (64 tokens, 2 of
+// 8 experts 4096 x 4096 bf16: 141 us, with 2 in up 147, in down 158), else where two
+// do not fill the card (100 tokens, a given 4 of 64 experts 2048 x 1024 bf16: 141
+// us, with 4 in up 147; 64 tokens, 2 of 8 experts 2048 x 1024 fp32: 57, with 2 in up
+// 75).
 int waves_of(size_t n, size_t chunks, int cus) {
   return chunks >= 16 || (chunks >= 4 && n * 2 < (size_t)cus * 8) ? 4 : 2;
 }
@@ -226,17 +228,20 @@ int moe_impl(const void* const* x, const void* const* logits,
   a.fast[0] = fast(o.in, o.ldw, o.xw, 2, 4);
   a.fast[1] = fast(o.hidden, o.ldd, o.xd, 4, 5);
   const size_t chosen = std::min(c.all, o.tokens * top);
-  // Tiles of 16 pairs at a time, by an expert's share of them; more take another
-  // turn over its matrices (128 tokens, 2 of 8 experts: 202 us with 4, 233 with
-  // 2; 64 tokens: 148 with 2, 164 with 1).
+  // Tiles of 16 pairs at a time, by an expert's share of them if all have alike;
+  // more take another turn over its matrices (2 of 8 experts 4096 x 4096 bf16: up of
+  // 128 tokens 193 us with 4, 225 with 2, of 64 tokens 141 with 2, 149 with 4, 177
+  // with 1; down of 128 tokens 193 with 2, 222 with 1).  A choice that prefers one
+  // expert pays for its turns: 193 us, with one of the two for every token 271.
   const size_t mean = o.tokens * top / c.all;
   a.tiles[0] = mean <= 8 ? 1 : mean <= 24 || !a.fast[0] ? 2 : 4;
   a.tiles[1] = mean <= 8 ? 1 : 2;
   const size_t blocks = o.tokens <= (size_t)moe::kSmall
                             ? (size_t)a.most * a.tables : ~(size_t)0 / kMost;
-  // Down by token, a workgroup per CU (one token 28 us, by expert and joined 32; 8
-  // ranks, with 8 times the workgroups, 39 and 30; 8 tokens 8 of 64 experts 103.5
-  // and 104.7, 8-bit 78 and 75.5, with a fourth of the pairs 34 and 37.7; 4 tokens
+  // Down by token, a workgroup per CU (8 of 64 experts 2048 x 1024 bf16: one token
+  // 27.7 us, by expert and joined 32.2; on 4 and 8 ranks, with as many times the
+  // workgroups, 34.9 and 40.8 by token, 31.0 and 30.5 by expert; 8 tokens 103.5 and
+  // 103.7, 8-bit weights 78 and 75.5, with a fourth of the pairs 34 and 37.7; 4 tokens
   // through 2 of 8 experts 1024 x 4096, where 16-bit results leave no room for parts
   // of hidden values, below, 44.7 and 44.7, 8-bit 40.9 and 37.2).
   a.small = o.hidden && o.tokens <= (size_t)moe::kSmall &&
@@ -244,12 +249,13 @@ int moe_impl(const void* const* x, const void* const* logits,
             (o.tokens == 1 || c.t == Type::F32 ||
              ((o.hidden + 31) / 32 * 32 <= 2 * a.pitch &&
               (!eight || o.tokens * top <= 24)));
-  // Each workgroup of up may make the choice for itself: 1 token 2048 x 1024 of
-  // 64 experts 27.1 us, 29.4 with a launch for it; 8 tokens (4096 workgroups) 114
-  // and 98.  Where most experts have 3 tokens, each may find those of its own
-  // expert: 20 experts 1001 x 501, 33 tokens 31.7 us, 36.1 with a launch; with 2
-  // tokens too many experts have none (16 tokens, 8 of 64 experts, a quarter of
-  // the logits masked: 124.6 and 121.2).
+  // Each workgroup of up may make the choice for itself: 1 token, 8 of 64 experts
+  // 2048 x 1024 bf16 27.7 us, 30.0 with a launch for it; 8 tokens (4096 workgroups)
+  // 117 and 103.5.  Where most experts have 3 tokens, each may find those of its own
+  // expert: 33 tokens, 3 of 20 experts 1001 x 501 fp16 32.8 us, 37.1 with a launch;
+  // 64 tokens, 2 of 8 experts 4096 x 4096 bf16 141 and 181 (which has one tile at a
+  // time); 100 tokens of 4 given experts of 64 141 and 144.  (From logits, of which
+  // every workgroup reads all, those are 177 and 151.)
   using moe::Mode;
   Mode mode = Mode::TABLE;
   if (o.in && o.hidden && c.all <= 256 &&
@@ -267,8 +273,9 @@ int moe_impl(const void* const* x, const void* const* logits,
                                          a.tiles[0]);
   a.waves[0] = waves_of((o.hidden + up - 1) / up * chosen, o.in * c.ew / 512,
                         cus);
-  // Fewer columns where that fills the card: 20 experts 1001 x 501 36.0 us with
-  // 32 of them, 37.1 with 64; 8 experts 4001 x 4001 225 and 214.
+  // Fewer columns where that fills the card: 33 tokens, 3 of 20 experts 1001 x 501
+  // fp16 32.8 us with 32 of them, 33.8 with 64; 3 of 8 experts 4001 x 4001 215 and
+  // 207.
   a.sets = (o.in + 63) / 64 * chosen < (size_t)cus * 3 / 2 ? 2 : 4;
   a.waves[1] = waves_of((o.in + 16 * a.sets - 1) / (16 * a.sets) * chosen,
                         o.hidden * c.ew / 512, cus);

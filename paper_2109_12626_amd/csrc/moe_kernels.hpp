@@ -1,8 +1,9 @@
 // The mixture-of-experts layer for a few tokens on gfx950: the choice of
 // experts, both gated projections of the chosen ones (up), and their second
-// products (down) summed by token.  Every matrix of a chosen expert is read once,
-// and that read is what bounds the layer: 16 rows of a matrix at a time go to the
-// matrix cores, the tokens that chose it are the columns.  Figures: one MI355X;
+// products (down) summed by token.  Reading the matrices of the chosen experts is
+// what bounds the layer: 16 rows of a matrix at a time go to the matrix cores, the
+// tokens that chose it are the columns, 16 to 64 at a time by an expert's mean share;
+// an expert that has more takes further turns over its matrices.  Figures: one MI355X;
 // every launch costs about 4 us beside it (its start and one wait for memory), so
 // there are two for the fewest tokens and three or four else.
 #pragma once
@@ -1130,7 +1131,9 @@ template <Type W, Type X, bool SHIFT, int FORM, int MT, int NW, int S>
 struct Down {
   using M = Mix<W, X>;
   using V = typename M::V;
-  // (8-bit weights beside two tiles: 256 bytes would be 192 registers of parts)
+  // (8-bit weights beside two tiles: 256 bytes would be 192 registers of parts, and
+  // with 16-bit ones 512: 64 tokens, 2 of 8 experts 4096 x 8192 8-bit 177 us, bf16 295;
+  // with two parts of a value, 2^-16 off, 166 and 271)
   static constexpr int kPieces = MT * M::kParts, NH = M::pieces(FORM);
   static constexpr bool kSplits = FORM == (int)Hidden::VALUES;
   static constexpr int kRow =
@@ -1273,7 +1276,7 @@ struct Down {
 // and one in the lower 8 of the matrix cores' rows, their pairs in the left and
 // right 8 columns: of the product the two blocks that belong together count.
 // A token's sums stay in LDS, a wavefront's own, and are joined in order.  One
-// token, 8 experts 2048 x 1024: 10 us for 34 MB, of which half is the way to the
+// token, 8 experts 2048 x 1024: 11 us for 34 MB, of which half is the way to the
 // first weights (records, pairs, hidden values); by expert and joined 15.
 template <Type W, Type X, bool SHIFT, int FORM>
 struct DownSmall {

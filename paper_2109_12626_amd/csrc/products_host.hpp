@@ -281,7 +281,9 @@ struct TileCost {
 };
 // 64 x 64 with two and with four tiles in LDS, 128 x 128, 256 x 128, 256 x 256;
 // the last two for 16-bit operands of whole aligned pieces only, and other
-// operands have no four-buffer form.
+// operands have no four-buffer form.  8-bit operands go by the 16-bit ones' figures
+// (a tile of as many bytes), which leave out that their results are twice as large
+// a share: 7 x 875 x 1001 x 1000 linear 15.6 us by them, 27.8 measured.
 constexpr int kTiles = 5;
 constexpr size_t kTileRows[kTiles] = {64, 64, 128, 256, 256},
                  kTileCols[kTiles] = {64, 64, 128, 128, 256};

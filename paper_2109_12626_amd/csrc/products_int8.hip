@@ -155,8 +155,8 @@ __device__ inline void quantize_row(GivenQuantize& a, int rank, size_t row,
     give(load_piece<V>(x + j, cols - j), j);
 }
 
-// 4 / W rows per workgroup.  Bound by memory: 8192 x 4096 bf16 24.8 us with four
-// wavefronts to a row (4.1 TB/s; a copy of as many bytes 20.6), 30.9 with one,
+// 4 / W rows per workgroup.  Bound by memory: 8192 x 4096 bf16 23.8 us with four
+// wavefronts to a row (4.2 TB/s; at the rate of a large copy 19.4), 30.9 with one,
 // 34.5 with one that asks for the next row ahead in a quarter of the workgroups.
 constexpr size_t kGroups = (size_t)1 << 22;      // along a launch's first axis
 template <typename V, int W, int P>

@@ -1402,8 +1402,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_tiled(Args) {
 }
 
 // The same for 8 bits.  Off 16 bytes two workgroups to a CU, which takes a bound
-// on the registers: 7 x 875 x 1001 x 1000 gated 90.5 -> 59.8 us, linear 28.5 ->
-// 27.8.
+// on the registers (gated 248 bytes per lane are in scratch memory then): 7 x 875 x
+// 1001 x 1000 gated 90.5 -> 59.8 us, linear 28.5 -> 27.8.
 template <Form F, int BN>
 __global__ __launch_bounds__(512) void k_int8_pingpong(Args) {
   Given& a = *(Given*)__builtin_amdgcn_kernarg_segment_ptr();
