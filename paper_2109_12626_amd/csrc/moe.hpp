@@ -44,8 +44,8 @@ struct Record {
 
 // A table of the workspace: how many records there are and which is each rank's
 // first (`kStarts` numbers; not with Mode::DIRECT), the records in the experts'
-// order, the pairs by expert, every pair's weight and rank (-1: none of the
-// launch), and its hidden values and result.  Ranks that choose from the same logits
+// order, the pairs by expert, every pair's weight and owner (expert of the rank *
+// kRanks + rank; -1: none of the launch), and its hidden values and result.  Ranks that choose from the same logits
 // (or by the same index and weight) share one table, others have one each.
 constexpr int kStarts = kRanks + 2;
 struct Layout {

@@ -23,6 +23,11 @@ __device__ inline char* table_of(GivenMoe& a, int table) {
   return a.work + (size_t)(a.first + table) * a.at.bytes;
 }
 
+// Who has a pair: a rank of the launch and its expert in one number.
+__device__ inline int owner_of(int rank, int expert) {
+  return expert * kRanks + rank;
+}
+
 // ---------------------------------------------------------------- the choice
 
 // Floats in their order as unsigned numbers: -0 equals 0, NaN comes last.
@@ -290,7 +295,7 @@ __device__ inline bool route(GivenMoe& a, int table, const Choice& c, int at,
     if (mine) c.list[c.start[e] + c.place[i]] = i;
     if (!write) continue;
     ((int*)(work + a.at.owner))[i] =
-        mine ? (one ? 0 : table) + e / a.experts : -1;
+        mine ? owner_of((one ? 0 : table) + e / a.experts, e % a.experts) : -1;
     if (mine) {
       ((int*)(work + a.at.pairs))[c.start[e] + c.place[i]] = i;
       ((float*)(work + a.at.weights))[i] = c.share[i];
@@ -708,8 +713,10 @@ __device__ inline void keep_choice(GivenMoe& a, int table, int token,
   const int low = a.experts * (a.first + (one ? 0 : table)),
             own = a.experts * (one ? a.ranks : 1);
   ((int*)(work + a.at.owner))[i] =
-      e >= low && e < low + own ? (one ? 0 : table) + (e - low) / a.experts
-                                : -1;
+      e >= low && e < low + own
+          ? owner_of((one ? 0 : table) + (e - low) / a.experts,
+                     (e - low) % a.experts)
+          : -1;
   ((float*)(work + a.at.weights))[i] = w;
 }
 
@@ -1498,23 +1505,6 @@ struct DownSmall {
   }
 };
 
-// A pair's result that is NaN: whole_result() by the record that has the pair.
-template <typename M>
-__device__ inline float whole_part(GivenMoe& a, const char* work, int rank,
-                                   int pair, size_t j) {
-  const auto records = (const Record*)(work + a.at.records);
-  const auto list = (const int*)(work + a.at.pairs);
-  for (int n = 0; n < *(const int*)work; ++n)
-    for (int i = 0; i < records[n].count; ++i)
-      if (records[n].rank == rank && list[records[n].first + i] == pair)
-        return a.planes == (int)Hidden::PARTS
-                   ? whole_result<M, (int)Hidden::PARTS>(
-                         a, work, rank, records[n].expert, pair, j)
-                   : whole_result<M, (int)Hidden::VALUES>(
-                         a, work, rank, records[n].expert, pair, j);
-  return 0.f;
-}
-
 // y = the sum of a token's parts, in the order of its choices, + residual: four
 // columns per thread.
 template <Type W, Type X>
@@ -1529,17 +1519,25 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs) {
   const float* parts = (const float*)(work + a.at.parts) +
                        (size_t)token * a.top * a.pitch + j;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < a.top; ++k)
-    if (owner[k] == rank) {
-      f32x4 p = *(const f32x4*)(parts + (size_t)k * a.pitch);
-      if (X != Type::F32)
+  for (int k = 0; k < a.top; ++k) {
+    const int own = owner[k];
+    if (own < 0 || own % kRanks != rank) continue;
+    f32x4 p = *(const f32x4*)(parts + (size_t)k * a.pitch);
+    if (X != Type::F32)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (p[e] != p[e] && j + e < a.in)
-            p[e] = whole_part<Mix<W, X>>(a, work, rank, token * a.top + k,
-                                         j + e);
-      v += p;
-    }
+      for (int e = 0; e < 4; ++e)
+        if (p[e] != p[e] && j + e < a.in) {
+          auto result = [&](auto form) {
+            return whole_result<Mix<W, X>, form.value>(
+                a, work, rank, own / kRanks, token * a.top + k, j + e);
+          };
+          if (a.planes == (int)Hidden::PARTS)
+            p[e] = result(std::integral_constant<int, (int)Hidden::PARTS>());
+          else
+            p[e] = result(std::integral_constant<int, (int)Hidden::VALUES>());
+        }
+    v += p;
+  }
   float o[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = v[e];
