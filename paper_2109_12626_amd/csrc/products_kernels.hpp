@@ -146,7 +146,9 @@ constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 // (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2).  Not EXACT: Abramowitz and
 // Stegun 7.1.26, whose truncation is 7.5e-8 at most; in 32 bits the whole is
 // 2.8e-7 off at most, measured over -12 .. 12 (EXACT: 9.3e-8): a thousandth of
-// what rounding a result of 1 to fp16 costs.
+// what rounding a result of 1 to fp16 costs.  Of GELU's small results that is more:
+// up to 1 step of fp16 at z = -4.2 (below 0.01 from -2 on, 0.4 from -3.5 on; in 32
+// bits by 1 + erf(z / sqrt 2) up to 1.4, at -5), an eighth of that in bf16.
 template <bool EXACT>
 __device__ inline float normal_cdf(float z, float* density) {
   if (EXACT) {
